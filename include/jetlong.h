@@ -445,6 +445,161 @@ int jl_rope_attention_decode_paged(const void* q, const void* k_pages, const voi
                                    size_t workspace_bytes, void* stream);
 
 /*
+ * ---- 8-bit cache -----------------------------------------------------------
+ * Keys (raw, before RoPE) and values held as OCP e4m3 in blocks of 64 tokens
+ * of one kv head, with one fp32 power-of-two scale per block for K and one for
+ * V: a value is its scale times its e4m3 number.  256 bytes per token and kv
+ * head instead of 512.  Pools, all on one device and owned by the caller:
+ *   k, v             uint8 [n_pages, Hkv, page_size, head_dim]: per (page, head)
+ *                    page_size / 64 images of 8192 bytes.  Inside an image
+ *     K  key 32 a + 16 t + r,         channel 64 p + 32 u + 8 g + j  at [a 2][t 2][u 2][g 4][r 16][j 8][p 2]
+ *     V  key 32 a + 16 t + 4 g + i,   channel 32 c + 16 e + m        at [a 2][c 4][g 4][m 16][e 2][t 2][i 4]
+ *   k_scale, v_scale fp32 [n_pages, Hkv, page_size / 64]
+ *   k_mean           bf16 [n_pages, Hkv, page_size / 64, head_dim]: the mean of
+ *                    the block's dequantised keys
+ * page_size is a multiple of 64.  Zero-filled pools are an empty cache.
+ * Paged: block_table int32 [B, max_pages] on the device, token x of sequence b
+ * in row x % page_size of page block_table[b][x / page_size].  Dense:
+ * block_table NULL, sequence b is page b, B <= n_pages, max_pages is not read.
+ * A sequence holds at most 8388608 (2^23) positions and the pools fewer than
+ * 2^31 blocks (JL_ERR_UNSUPPORTED beyond).  Tables, lengths and lists are device
+ * arrays that the host cannot check: reads clamp page indices into the pool and
+ * lengths into [0, capacity], so bad ones give wrong values and never an access
+ * outside the pools; writes to a page outside the pool are dropped.
+ */
+typedef struct jl_cache8 {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  void* k_mean;
+  int n_pages, page_size, Hkv, head_dim;
+} jl_cache8;
+
+/*
+ * Appends rows to an 8-bit cache: n tokens of prefill, or one of decode.
+ *   k, v    bf16 [B, n, Hkv, head_dim] raw keys and values
+ *   starts  int32 [B] DEVICE array: position of each sequence's first new row,
+ *           i.e. its length before the call
+ *   n_new   int32 [B] DEVICE array or NULL: rows of sequence b that are appended
+ *           (its first ones; clamped into [0, n]); NULL: all n
+ * Rows at positions outside [0, capacity) are dropped.  For each block that
+ * takes new rows
+ *   scale = 2^e with the smallest e in [-117, 119] such that the largest
+ *           magnitude of the new rows is at most 448 * 2^e (NaN is passed over,
+ *           an infinity counts as the largest finite value), or the scale it
+ *           had where that is larger and the block holds rows before the first
+ *           new one;
+ *   rows before the first new one are kept, rounded again where the scale grew;
+ *   new rows are x / scale rounded to nearest even e4m3, saturated at 448 (NaN
+ *           stays NaN);
+ *   rows behind the last new one become zero; the block's mean is taken anew.
+ * Every other block is left as it was.  Two sequences whose new rows meet in one
+ * block (a shared page) race.  Nothing is allocated and nothing waited for.
+ */
+int jl_cache8_append(const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                     const void* k, const void* v, const int32_t* starts, const int32_t* n_new,
+                     int B, int n, void* stream);
+
+/*
+ * Rows start .. start + n - 1 of every sequence back as bf16 [B, n, Hkv,
+ * head_dim] (written), exactly: a bf16 holds every value of the cache.  With
+ * them the prefill entry points continue a prompt (jl_bifocal_prefill_chunk with
+ * q_start behind the rows).  start + n must not exceed the capacity; rows that
+ * were never appended come as the pools hold them.  Nothing is allocated.
+ */
+int jl_cache8_read(const jl_cache8* cache, const int32_t* block_table, int max_pages, void* k,
+                   void* v, int B, int start, int n, void* stream);
+
+/*
+ * Bytes of workspace the 8-bit decode entry points need; 0 for invalid arguments.
+ * It does not depend on the batch or the lengths.  Its first 4096 bytes (arrival
+ * counters) must be zero when it is first used; every call leaves them zero, so
+ * one fill serves all later calls, of any shape that fits.  Calls that share a
+ * workspace must be ordered by the caller.
+ */
+size_t jl_decode8_workspace_bytes(int Hq, int Hkv, int head_dim);
+
+/*
+ * jl_bifocal_decode over an 8-bit cache.
+ *   q        bf16 [B, Hq, head_dim]  raw queries, sequence b's at kv_lens[b] - 1
+ *   kv_lens  int32 [B] DEVICE array, the new token already appended; what the
+ *            cache holds at or past kv_lens[b] does not matter.  A sequence of
+ *            length 0 gets zeros.
+ *   o        bf16 [B, Hq, head_dim]  output (written)
+ *   workspace, workspace_bytes: jl_decode8_workspace_bytes(Hq, Hkv, head_dim)
+ *            bytes, 16-byte aligned, see there
+ * Requires Hq % Hkv == 0 and Hq / Hkv <= 8.  Only the cos/sin table may be
+ * allocated or grown (to the cache's capacity).  The
+ * sums are kept in fp32; the same call gives the same bits.
+ */
+int jl_bifocal_decode8(const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                       const void* q, const int32_t* kv_lens, void* o, int B, int Hq,
+                       double rope_theta, int w_pretrained, int w_local, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* The vanilla counterpart of jl_bifocal_decode8 (base rotation for every key). */
+int jl_rope_attention_decode8(const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                              const void* q, const int32_t* kv_lens, void* o, int B, int Hq,
+                              double rope_theta, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/*
+ * jl_bifocal_decode8 over listed blocks only: the softmax runs over the keys
+ * below kv_lens[b] of the blocks that blocks[b][h] names.
+ *   blocks   int32 [B, Hkv, n_select] DEVICE array of block indices (token / 64),
+ *            in any order, one list per kv head.  Entries outside the sequence
+ *            (-1 among them) are passed over; one listed twice counts twice.
+ * A list without a key gives zeros.  The view of a key, G and the query's
+ * position follow from kv_lens[b] as in jl_bifocal_decode8: the full list gives
+ * its result up to the order of the sums.
+ */
+int jl_bifocal_decode8_blocks(const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                              const void* q, const int32_t* kv_lens, const int32_t* blocks,
+                              int n_select, void* o, int B, int Hq, double rope_theta,
+                              int w_pretrained, int w_local, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* The vanilla counterpart of jl_bifocal_decode8_blocks. */
+int jl_rope_attention_decode8_blocks(const jl_cache8* cache, const int32_t* block_table,
+                                     int max_pages, const void* q, const int32_t* kv_lens,
+                                     const int32_t* blocks, int n_select, void* o, int B, int Hq,
+                                     double rope_theta, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
+/*
+ * A cheap score of every block for the query of each sequence:
+ *   scores fp32 [B, Hkv, n_blocks] (written), n_blocks = capacity / 64:
+ *   max over the query heads of kv head h of
+ *     <R(f(q)) x_q, R(f(64 j + 31)) k_mean_j> / sqrt(head_dim)
+ * i.e. what the block's mean key would score in the remote view at its middle
+ * position; -inf for blocks at or past kv_lens[b].  Arguments as in
+ * jl_bifocal_decode8.  A NaN in a query or mean gives NaN.
+ */
+int jl_bifocal_block_scores8(const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                             const void* q, const int32_t* kv_lens, float* scores, int B, int Hq,
+                             double rope_theta, int w_pretrained, void* stream);
+
+/* The same with base rotations, for the vanilla decode. */
+int jl_rope_block_scores8(const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                          const void* q, const int32_t* kv_lens, float* scores, int B, int Hq,
+                          double rope_theta, void* stream);
+
+/*
+ * The blocks that a query attends to: always the first n_first of its sequence
+ * and those that hold a key of the local band (kv_lens[b] - 1 - k <= w_local), then
+ * the others by falling score, n_select in all.  Equal scores go to the lower
+ * index; NaN counts as larger than any number.
+ *   scores  fp32 [B, Hkv, n_blocks]
+ *   blocks  int32 [B, Hkv, n_select] output (written): ascending, -1 behind the
+ *           last where the sequence has fewer blocks
+ * n_select must hold the blocks that are always chosen: at least
+ * min(n_blocks, (w_local + 127) / 64 + n_first).  n_blocks <= 131072.
+ */
+int jl_select_blocks(const float* scores, const int32_t* kv_lens, int32_t* blocks, int B, int Hkv,
+                     int n_blocks, int n_select, int w_local, int n_first, void* stream);
+
+/*
  * Debug view of the schedule as the device computes it (Eqs. (2), (3), (5)),
  * for bit-exact tests.  All pointers are device pointers.
  *   lengths    int32 [n_lengths]              sequence lengths L (>= 1)

@@ -105,6 +105,29 @@ def lib() -> ctypes.CDLL:
         L.jl_rope_attention_decode_paged.restype = i32
         L.jl_rope_attention_decode_paged.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, i32,
                                                      i32, i32, i32, dbl, vp, sz, vp]
+        L.jl_cache8_append.restype = i32
+        L.jl_cache8_append.argtypes = [vp, vp, i32, vp, vp, vp, vp, i32, i32, vp]
+        L.jl_cache8_read.restype = i32
+        L.jl_cache8_read.argtypes = [vp, vp, i32, vp, vp, i32, i32, i32, vp]
+        L.jl_decode8_workspace_bytes.restype = sz
+        L.jl_decode8_workspace_bytes.argtypes = [i32, i32, i32]
+        L.jl_bifocal_decode8.restype = i32
+        L.jl_bifocal_decode8.argtypes = [vp, vp, i32, vp, vp, vp, i32, i32, dbl, i32, i32, vp, sz,
+                                         vp]
+        L.jl_rope_attention_decode8.restype = i32
+        L.jl_rope_attention_decode8.argtypes = [vp, vp, i32, vp, vp, vp, i32, i32, dbl, vp, sz, vp]
+        L.jl_bifocal_decode8_blocks.restype = i32
+        L.jl_bifocal_decode8_blocks.argtypes = [vp, vp, i32, vp, vp, vp, i32, vp, i32, i32, dbl,
+                                                i32, i32, vp, sz, vp]
+        L.jl_rope_attention_decode8_blocks.restype = i32
+        L.jl_rope_attention_decode8_blocks.argtypes = [vp, vp, i32, vp, vp, vp, i32, vp, i32, i32,
+                                                       dbl, vp, sz, vp]
+        L.jl_bifocal_block_scores8.restype = i32
+        L.jl_bifocal_block_scores8.argtypes = [vp, vp, i32, vp, vp, vp, i32, i32, dbl, i32, vp]
+        L.jl_rope_block_scores8.restype = i32
+        L.jl_rope_block_scores8.argtypes = [vp, vp, i32, vp, vp, vp, i32, i32, dbl, vp]
+        L.jl_select_blocks.restype = i32
+        L.jl_select_blocks.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, i32, vp]
         L.jl_debug_schedule.restype = i32
         L.jl_debug_schedule.argtypes = [vp, i32, vp, i32, i32, vp, vp, vp, vp]
         L.jl_debug_prefill_tiles.restype = i32
@@ -512,6 +535,251 @@ def decode_paged(q, k_pages, v_pages, block_table, kv_lens, *, w_pretrained: int
                                              _stream(stream)))
     else:
         _check(lib().jl_rope_attention_decode_paged(*args, *ws, _stream(stream)))
+    return out
+
+
+# ------------------------------------------------------------- 8-bit cache
+BLOCK8 = 64  # tokens of a block: one scale, one mean key, one unit of selection
+
+
+class _Cache8Struct(ctypes.Structure):  # jl_cache8
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "k_mean")]
+                + [(n, ctypes.c_int) for n in ("n_pages", "page_size", "Hkv", "head_dim")])
+
+
+class Cache8:
+    """The pools of an 8-bit cache (jl_cache8): k, v uint8 [n_pages, Hkv, page_size, 128],
+    k_scale, v_scale fp32 [n_pages, Hkv, page_size // 64], k_mean bf16 [n_pages, Hkv,
+    page_size // 64, 128], contiguous on one device.  cache8_alloc makes an empty one.
+    Without a block table page b is sequence b."""
+
+    def __init__(self, k, v, k_scale, v_scale, k_mean):
+        torch = _t()
+        if k.dim() != 4:
+            raise ValueError("k must be [n_pages, Hkv, page_size, 128]")
+        n_pages, Hkv, page_size, D = k.shape
+        if page_size % BLOCK8:
+            raise ValueError("page_size must be a multiple of %d, got %d" % (BLOCK8, page_size))
+        blocks = (n_pages, Hkv, page_size // BLOCK8)
+        ptrs = [_dev(k, "k", torch.uint8), _dev(v, "v", torch.uint8, k.shape, k.device),
+                _dev(k_scale, "k_scale", torch.float32, blocks, k.device),
+                _dev(v_scale, "v_scale", torch.float32, blocks, k.device),
+                _dev(k_mean, "k_mean", torch.bfloat16, blocks + (D,), k.device)]
+        self.k, self.v, self.k_scale, self.v_scale, self.k_mean = k, v, k_scale, v_scale, k_mean
+        self.n_pages, self.page_size, self.Hkv, self.head_dim = n_pages, page_size, Hkv, D
+        self.device = k.device
+        self._struct = _Cache8Struct(*ptrs, n_pages, page_size, Hkv, D)
+        self._ref = ctypes.cast(ctypes.pointer(self._struct), ctypes.c_void_p)
+
+
+def cache8_alloc(n_pages: int, page_size: int, Hkv: int, *, head_dim: int = 128,
+                 device="cuda") -> Cache8:
+    """An empty 8-bit cache: n_pages pages of page_size tokens; for a dense one a page per
+    sequence, page_size its capacity (a multiple of 64)."""
+    torch = _t()
+    kw = dict(device=device)
+    blocks = (n_pages, Hkv, page_size // BLOCK8)
+    return Cache8(torch.zeros((n_pages, Hkv, page_size, head_dim), dtype=torch.uint8, **kw),
+                  torch.zeros((n_pages, Hkv, page_size, head_dim), dtype=torch.uint8, **kw),
+                  torch.zeros(blocks, dtype=torch.float32, **kw),
+                  torch.zeros(blocks, dtype=torch.float32, **kw),
+                  torch.zeros(blocks + (head_dim,), dtype=torch.bfloat16, **kw))
+
+
+class _On:
+    """Allocations of a call that is given a stream come from that stream's pool, so that
+    neither their fill nor their reuse crosses streams."""
+
+    def __init__(self, stream):
+        self.ctx = None if stream is None else _t().cuda.stream(stream)
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+
+def _is_cache8(cache) -> None:
+    if not isinstance(cache, Cache8):
+        raise TypeError("cache must be a Cache8")
+
+
+def _query8(q, cache):
+    """(B, Hq, 128) of a query over an 8-bit cache."""
+    _is_cache8(cache)
+    if q.dim() != 3 or q.shape[2] != cache.head_dim:
+        raise ValueError("q must be [B, Hq, %d]" % cache.head_dim)
+    return q.shape
+
+
+def _cache8(cache, block_table, B):
+    """The checks of a call of B sequences on a cache -> (jl_cache8 pointer, table pointer,
+    max_pages, capacity)."""
+    torch = _t()
+    # the library launches on the current device
+    if cache.device.index != torch.cuda.current_device():
+        raise ValueError("cache is on %s, the current device is cuda:%d"
+                         % (cache.device, torch.cuda.current_device()))
+    if block_table is None:
+        if B > cache.n_pages:
+            raise ValueError("a dense cache of %d sequences cannot hold %d" % (cache.n_pages, B))
+        return cache._ref, None, 0, cache.page_size
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [B, max_pages]")
+    max_pages = block_table.shape[1]
+    return (cache._ref, _dev(block_table, "block_table", torch.int32, None, cache.device),
+            max_pages, max_pages * cache.page_size)
+
+
+def _ints(t, name, cache, shape):
+    return _dev(t, name, _t().int32, shape, cache.device)
+
+
+def cache8_append(cache, k, v, starts, *, n_new=None, block_table=None, stream=None) -> None:
+    """jl_cache8_append: rows k, v [B, n, Hkv, 128] bf16 to positions starts[b] .. of sequence
+    b (starts int32 [B]); n_new int32 [B]: only the first n_new[b] of them."""
+    torch = _t()
+    _is_cache8(cache)
+    if k.dim() != 4 or k.shape[2:] != (cache.Hkv, cache.head_dim):
+        raise ValueError("k and v must be [B, n, %d, %d]" % (cache.Hkv, cache.head_dim))
+    B, n = k.shape[:2]
+    ref, table, max_pages, _ = _cache8(cache, block_table, B)
+    _check(lib().jl_cache8_append(
+        ref, table, max_pages, _dev(k, "k", torch.bfloat16, None, cache.device),
+        _dev(v, "v", torch.bfloat16, k.shape, cache.device), _ints(starts, "starts", cache, (B,)),
+        None if n_new is None else _ints(n_new, "n_new", cache, (B,)), B, n, _stream(stream)))
+
+
+def cache8_read(cache, n: int, *, start: int = 0, B=None, block_table=None, k_out=None, v_out=None,
+                stream=None):
+    """jl_cache8_read: rows start .. start + n - 1 of every sequence as bf16 (k, v), each
+    [B, n, Hkv, 128].  B: sequences of a dense cache, all of them if not given."""
+    torch = _t()
+    _is_cache8(cache)
+    if B is None:
+        B = cache.n_pages if block_table is None else block_table.shape[0]
+    shape = (B, n, cache.Hkv, cache.head_dim)
+    ref, table, max_pages, _ = _cache8(cache, block_table, B)
+    with _On(stream):
+        if k_out is None:
+            k_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+        if v_out is None:
+            v_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+    _check(lib().jl_cache8_read(
+        ref, table, max_pages, _dev(k_out, "k_out", torch.bfloat16, shape, cache.device),
+        _dev(v_out, "v_out", torch.bfloat16, shape, cache.device), B, int(start), int(n),
+        _stream(stream)))
+    return k_out, v_out
+
+
+def decode8_workspace_bytes(Hq: int, Hkv: int, head_dim: int = 128) -> int:
+    return int(lib().jl_decode8_workspace_bytes(Hq, Hkv, head_dim))
+
+
+def decode8_workspace(Hq: int, Hkv: int, *, head_dim: int = 128, device="cuda"):
+    """A workspace for decode8 and decode8_blocks, zeroed as they need it before their first
+    call; a decoding loop keeps one per stream."""
+    torch = _t()
+    return torch.zeros(decode8_workspace_bytes(Hq, Hkv, head_dim), dtype=torch.uint8,
+                       device=device)
+
+
+def _decode8(q, cache, kv_lens, blocks, w_pretrained, w_local, rope_theta, bifocal, block_table,
+             out, workspace, stream):
+    torch = _t()
+    B, Hq, D = _query8(q, cache)
+    ref, table, max_pages, _ = _cache8(cache, block_table, B)
+    if out is None or workspace is None:
+        with _On(stream):
+            if out is None:
+                out = torch.empty_like(q)
+            if workspace is None:
+                workspace = torch.zeros(max(decode8_workspace_bytes(Hq, cache.Hkv, D), 16),
+                                        dtype=torch.uint8, device=q.device)
+    args = [ref, table, max_pages, _dev(q, "q", torch.bfloat16, None, cache.device),
+            _ints(kv_lens, "kv_lens", cache, (B,))]
+    name = "decode8"
+    if blocks is not None:
+        name = "decode8_blocks"
+        if blocks.dim() != 3 or blocks.shape[:2] != (B, cache.Hkv):
+            raise ValueError("blocks must be [B, Hkv, n_select]")
+        args += [_ints(blocks, "blocks", cache, None), blocks.shape[2]]
+    args += [_dev(out, "out", torch.bfloat16, q.shape, cache.device), B, Hq, float(rope_theta)]
+    ws = [_dev(workspace, "workspace", None, None, cache.device),
+          workspace.numel() * workspace.element_size(), _stream(stream)]
+    if bifocal:
+        _check(getattr(lib(), "jl_bifocal_" + name)(*args, int(w_pretrained), int(w_local), *ws))
+    else:
+        _check(getattr(lib(), "jl_rope_attention_" + name)(*args, *ws))
+    return out
+
+
+def decode8(q, cache, kv_lens, *, w_pretrained: int = 1, w_local: int = 0,
+            rope_theta: float = 1e6, bifocal: bool = True, block_table=None, out=None,
+            workspace=None, stream=None):
+    """jl_bifocal_decode8 / jl_rope_attention_decode8: q [B, Hq, 128] raw over an 8-bit cache,
+    kv_lens int32 [B] (0: zeros).  workspace: decode8_workspace(Hq, Hkv), kept between calls;
+    without one every call fills one of its own."""
+    return _decode8(q, cache, kv_lens, None, w_pretrained, w_local, rope_theta, bifocal,
+                    block_table, out, workspace, stream)
+
+
+def decode8_blocks(q, cache, kv_lens, blocks, *, w_pretrained: int = 1, w_local: int = 0,
+                   rope_theta: float = 1e6, bifocal: bool = True, block_table=None, out=None,
+                   workspace=None, stream=None):
+    """jl_bifocal_decode8_blocks / jl_rope_attention_decode8_blocks: decode8 over the blocks that
+    blocks int32 [B, Hkv, n_select] lists (select_blocks)."""
+    if blocks is None:
+        raise ValueError("blocks must be [B, Hkv, n_select]")
+    return _decode8(q, cache, kv_lens, blocks, w_pretrained, w_local, rope_theta, bifocal,
+                    block_table, out, workspace, stream)
+
+
+def block_scores8(q, cache, kv_lens, *, w_pretrained: int = 1, rope_theta: float = 1e6,
+                  bifocal: bool = True, block_table=None, out=None, stream=None):
+    """jl_bifocal_block_scores8 / jl_rope_block_scores8: fp32 [B, Hkv, capacity // 64], the score
+    of every block's mean key, -inf past the sequence."""
+    torch = _t()
+    B, Hq, _ = _query8(q, cache)
+    ref, table, max_pages, cap = _cache8(cache, block_table, B)
+    shape = (B, cache.Hkv, cap // BLOCK8)
+    if out is None:
+        with _On(stream):
+            out = torch.empty(shape, dtype=torch.float32, device=q.device)
+    args = [ref, table, max_pages, _dev(q, "q", torch.bfloat16, None, cache.device),
+            _ints(kv_lens, "kv_lens", cache, (B,)),
+            _dev(out, "out", torch.float32, shape, cache.device), B, Hq, float(rope_theta)]
+    if bifocal:
+        _check(lib().jl_bifocal_block_scores8(*args, int(w_pretrained), _stream(stream)))
+    else:
+        _check(lib().jl_rope_block_scores8(*args, _stream(stream)))
+    return out
+
+
+def select_blocks(scores, kv_lens, n_select: int, *, w_local: int, n_first: int = 1, out=None,
+                  stream=None):
+    """jl_select_blocks: int32 [B, Hkv, n_select] from scores fp32 [B, Hkv, n_blocks]: the first
+    n_first blocks and those of the local band always, then the largest scores; ascending,
+    -1 behind the last."""
+    torch = _t()
+    if scores.dim() != 3:
+        raise ValueError("scores must be [B, Hkv, n_blocks]")
+    B, Hkv, n_blocks = scores.shape
+    if scores.is_cuda and scores.device.index != torch.cuda.current_device():
+        raise ValueError("scores are on %s, the current device is cuda:%d"
+                         % (scores.device, torch.cuda.current_device()))
+    shape = (B, Hkv, int(n_select))
+    ptr = _dev(scores, "scores", torch.float32)
+    if out is None:
+        with _On(stream):
+            out = torch.empty(shape, dtype=torch.int32, device=scores.device)
+    _check(lib().jl_select_blocks(
+        ptr, _dev(kv_lens, "kv_lens", torch.int32, (B,), scores.device),
+        _dev(out, "out", torch.int32, shape, scores.device), B, Hkv, n_blocks, int(n_select),
+        int(w_local), int(n_first), _stream(stream)))
     return out
 
 

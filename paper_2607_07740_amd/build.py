@@ -16,7 +16,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libjetlong.so")
-SOURCES = ["prefill.hip", "decode.hip", "aux.hip", "jl_api.cpp"]
+SOURCES = ["prefill.hip", "decode.hip", "cache8.hip", "decode8.hip", "blocks8.hip", "aux.hip",
+           "jl_api.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -1,0 +1,264 @@
+// cache8.hip -- rows into and out of the 8-bit cache (layout: cache8.h).
+#include "cache8.h"
+
+namespace jl {
+
+struct AppendArgs {
+  Cache8 c;
+  const uint16_t* k;  // [B][n][Hkv][128] bf16
+  const uint16_t* v;
+  const int32_t* starts;
+  const int32_t* n_new;  // or nullptr: n rows of every sequence
+  int n, nb;             // nb: blocks a sequence's new rows can touch
+};
+
+// Workgroup = one block of one kv head that takes new rows.  Its rows are read
+// once into registers, their largest magnitude gives the block's scale, and the
+// images are put together in LDS and written whole.  Rows the block held before
+// are kept; where the scale grows they are rounded again to the new one (a power
+// of two further, so only values that fall among the subnormals move).  The
+// mean key sums e4m3 values, multiples of 2^-9 below 2^15 in all: exactly.
+__global__ __launch_bounds__(256) void append8_kernel(AppendArgs a) {
+  __shared__ __attribute__((aligned(16))) unsigned char img[2][kBlkBytes];
+  __shared__ float s_top[2][4];
+  const int tid = threadIdx.x;
+  const int h = blockIdx.x % a.c.Hkv;
+  const int bi = blockIdx.x / a.c.Hkv;
+  const int b = bi / a.nb;
+  const long long start = a.starts[b];
+  const long long cap = (long long)a.c.n_blocks * kBlk;
+  const int n = a.n_new != nullptr ? min(max(a.n_new[b], 0), a.n) : a.n;
+  const long long lo = max(start, 0LL), hi = min(start + n, cap);
+  const long long base = (lo / kBlk + (bi - b * a.nb)) * kBlk;  // the block's first position
+  if (base >= hi || lo >= hi) return;
+  const int blk = (int)(base / kBlk);
+  const int page = page_of(a.c, b, blk);
+  if (page < 0 || page >= a.c.n_pages) return;  // a page outside the pool is never written
+  const int r0 = (int)max(start - base, 0LL);               // rows held before
+  const int r1 = (int)min(hi - base, (long long)kBlk);      // rows held after
+  const size_t at = (size_t)pool_block(a.c, page, h, in_page(a.c, blk));
+
+  // ---- new rows: K as (row, 16 rotate-half pairs), V as (8 keys of a lane group, 4 channels)
+  const size_t row = (size_t)a.c.Hkv * kHeadDim;
+  const uint16_t* ksrc = a.k + ((size_t)b * a.n * a.c.Hkv + h) * kHeadDim;
+  const uint16_t* vsrc = a.v + ((size_t)b * a.n * a.c.Hkv + h) * kHeadDim;
+  const int kr = tid >> 2, kc = tid & 3;
+  float kf[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) kf[i] = 0.f;
+  if (kr >= r0 && kr < r1) {
+    const uint16_t* src = ksrc + (size_t)(base + kr - start) * row;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      unpack8(load16(src + 16 * kc + 8 * i), kf + 8 * i);
+      unpack8(load16(src + 64 + 16 * kc + 8 * i), kf + 16 + 8 * i);
+    }
+  }
+  const int va = tid >> 7, vg = (tid >> 5) & 3, vd = 4 * (tid & 31);
+  float vf[8][4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int key = 32 * va + 16 * (i >> 2) + 4 * vg + (i & 3);
+    uint2 w = make_uint2(0, 0);
+    if (key >= r0 && key < r1) w = *(const uint2*)(vsrc + (size_t)(base + key - start) * row + vd);
+    vf[i][0] = bf16_lo(w.x);
+    vf[i][1] = bf16_hi(w.x);
+    vf[i][2] = bf16_lo(w.y);
+    vf[i][3] = bf16_hi(w.y);
+  }
+
+  // ---- scales: fmaxf passes NaN over; an infinity counts as the largest finite value
+  float ktop = 0.f, vtop = 0.f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) ktop = fmaxf(ktop, fabsf(kf[i]));
+#pragma unroll
+  for (int i = 0; i < 32; ++i) vtop = fmaxf(vtop, fabsf(vf[i >> 2][i & 3]));
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    ktop = fmaxf(ktop, __shfl_xor(ktop, o));
+    vtop = fmaxf(vtop, __shfl_xor(vtop, o));
+  }
+  if ((tid & 63) == 0) {
+    s_top[0][tid >> 6] = ktop;
+    s_top[1][tid >> 6] = vtop;
+  }
+  __syncthreads();
+  float scale[2], back[2];  // the new scale, and old / new
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float top = fmaxf(fmaxf(s_top[i][0], s_top[i][1]), fmaxf(s_top[i][2], s_top[i][3]));
+    const float now = pow2f(scale_exponent(top));
+    const float old = r0 > 0 ? (i == 0 ? a.c.k_scale : a.c.v_scale)[at] : 0.f;
+    scale[i] = fmaxf(now, old);
+    back[i] = old / scale[i];
+  }
+  {
+    const float inv = 1.f / scale[0];
+    const int aa = kr >> 5, t = (kr >> 4) & 1, r = kr & 15;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      u32x4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float* x = kf + 8 * q + 2 * i;
+        w[i] = e4m3_word(x[0] * inv, x[16] * inv, x[1] * inv, x[17] * inv);
+      }
+      const int u = kc >> 1, g = 2 * (kc & 1) + q;
+      *(u32x4*)&img[0][((((aa * 2 + t) * 2 + u) * 4 + g) * 16 + r) * 16] = w;
+    }
+  }
+  {
+    const float inv = 1.f / scale[1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint2 w = make_uint2(
+          e4m3_word(vf[0][j] * inv, vf[1][j] * inv, vf[2][j] * inv, vf[3][j] * inv),
+          e4m3_word(vf[4][j] * inv, vf[5][j] * inv, vf[6][j] * inv, vf[7][j] * inv));
+      *(uint2*)&img[1][v_offset(32 * va + 4 * vg, vd + j)] = w;
+    }
+  }
+  __syncthreads();
+
+  // ---- earlier rows back in, and the images out
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int which = i >> 1;
+    const int unit = tid + 256 * (i & 1);  // 16-byte unit of the image
+    unsigned char* dst = (which == 0 ? a.c.k : a.c.v) + at * kBlkBytes + 16 * unit;
+    u32x4 w = *(const u32x4*)&img[which][16 * unit];
+    if (r0 > 0) {
+      const u32x4 was = load16(dst);
+      float f[16];
+      e4m3_16(was, f);
+      const int key0 = which == 0 ? 32 * (unit >> 8) + 16 * ((unit >> 7) & 1) + (unit & 15)
+                                  : 32 * (unit >> 8) + 4 * ((unit >> 4) & 3);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t again = e4m3_word(f[4 * j] * back[which], f[4 * j + 1] * back[which],
+                                         f[4 * j + 2] * back[which], f[4 * j + 3] * back[which]);
+        uint32_t keep = 0;  // bytes of earlier rows
+        if (which == 0) {
+          keep = key0 < r0 ? ~0u : 0u;
+        } else {
+          const int left = r0 - (key0 + 16 * (j & 1));  // keys of this word (i = 0..3) below r0
+          keep = left >= 4 ? ~0u : left > 0 ? (1u << (8 * left)) - 1 : 0u;
+        }
+        w[j] = (again & keep) | (w[j] & ~keep);
+      }
+      *(u32x4*)&img[which][16 * unit] = w;
+    }
+    *(u32x4*)dst = w;
+  }
+  if (tid == 0) {
+    a.c.k_scale[at] = scale[0];
+    a.c.v_scale[at] = scale[1];
+  }
+  __syncthreads();
+
+  // ---- mean key: thread = (channel, half of the keys)
+  const int d = tid >> 1;
+  float sum = 0.f;
+  for (int i = 0; i < 32; ++i) {
+    const uint32_t byte = img[0][k_offset(32 * (tid & 1) + i, d)];
+    sum += e4m3_pair<false>(byte).x;
+  }
+  sum += __shfl_xor(sum, 1);
+  if ((tid & 1) == 0) {
+    const __bf16 m = (__bf16)(sum / (float)r1 * scale[0]);
+    a.c.k_mean[at * kHeadDim + d] = __builtin_bit_cast(uint16_t, m);
+  }
+}
+
+struct ReadArgs {
+  Cache8 c;
+  uint16_t* k;  // [B][n][Hkv][128] bf16
+  uint16_t* v;
+  int start, n, blk0, nb;
+};
+
+__device__ inline uint32_t bf16_pair(float a, float b) {
+  f32x2 t = {a, b};
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(t, bf16x2));
+}
+
+// Workgroup = one block of one kv head.  A value has 4 significant bits and a
+// magnitude of at least 2^-126 or zero, so bf16 holds it exactly.
+__global__ __launch_bounds__(256) void read8_kernel(ReadArgs a) {
+  const int tid = threadIdx.x;
+  const int h = blockIdx.x % a.c.Hkv;
+  const int bi = blockIdx.x / a.c.Hkv;
+  const int b = bi / a.nb;
+  const int blk = a.blk0 + bi - b * a.nb;
+  const int page = min(max(page_of(a.c, b, blk), 0), a.c.n_pages - 1);
+  const size_t at = (size_t)pool_block(a.c, page, h, in_page(a.c, blk));
+  const size_t row = (size_t)a.c.Hkv * kHeadDim;
+  const size_t out0 = ((size_t)b * a.n * a.c.Hkv + h) * kHeadDim;
+  const int pos0 = blk * kBlk - a.start;  // output row of the block's first key
+  const float ks = a.c.k_scale[at], vs = a.c.v_scale[at];
+  {
+    const int kr = tid >> 2, kc = tid & 3;
+    const int o = pos0 + kr;
+    if (o >= 0 && o < a.n) {
+      const unsigned char* src = a.c.k + at * kBlkBytes;
+      uint16_t* dst = a.k + out0 + (size_t)o * row;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int d = 16 * kc + 8 * q;
+        float f[16];
+        e4m3_16(load16(src + k_offset(kr, d)), f);
+        u32x4 lo, hi;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          lo[i] = bf16_pair(f[4 * i] * ks, f[4 * i + 2] * ks);
+          hi[i] = bf16_pair(f[4 * i + 1] * ks, f[4 * i + 3] * ks);
+        }
+        *(u32x4*)(dst + d) = lo;
+        *(u32x4*)(dst + 64 + d) = hi;
+      }
+    }
+  }
+  {
+    const int va = tid >> 7, vg = (tid >> 5) & 3, vd = 4 * (tid & 31);
+    const unsigned char* src = a.c.v + at * kBlkBytes;
+    float f[4][8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint2 w = *(const uint2*)(src + v_offset(32 * va + 4 * vg, vd + j));
+      const float2 x0 = e4m3_pair<false>(w.x), x1 = e4m3_pair<true>(w.x);
+      const float2 x2 = e4m3_pair<false>(w.y), x3 = e4m3_pair<true>(w.y);
+      f[j][0] = x0.x; f[j][1] = x0.y; f[j][2] = x1.x; f[j][3] = x1.y;
+      f[j][4] = x2.x; f[j][5] = x2.y; f[j][6] = x3.x; f[j][7] = x3.y;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int o = pos0 + 32 * va + 16 * (i >> 2) + 4 * vg + (i & 3);
+      if (o < 0 || o >= a.n) continue;
+      *(uint2*)(a.v + out0 + (size_t)o * row + vd) =
+          make_uint2(bf16_pair(f[0][i] * vs, f[1][i] * vs), bf16_pair(f[2][i] * vs, f[3][i] * vs));
+    }
+  }
+}
+
+// ---------------------------------------------------------------- launchers
+hipError_t launch_append8(const Cache8& c, const uint16_t* k, const uint16_t* v,
+                          const int32_t* starts, const int32_t* n_new, int B, int n,
+                          hipStream_t stream) {
+  AppendArgs a{c, k, v, starts, n_new, n, (int)((n + kBlk - 2LL) / kBlk + 1)};
+  const long long wgs = (long long)B * a.nb * c.Hkv;
+  if (wgs > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL(append8_kernel, dim3((unsigned)wgs), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_read8(const Cache8& c, uint16_t* k, uint16_t* v, int B, int start, int n,
+                        hipStream_t stream) {
+  ReadArgs a{c, k, v, start, n, start / kBlk, 0};
+  a.nb = (start + n - 1) / kBlk - a.blk0 + 1;
+  const long long wgs = (long long)B * a.nb * c.Hkv;
+  if (wgs > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL(read8_kernel, dim3((unsigned)wgs), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace jl

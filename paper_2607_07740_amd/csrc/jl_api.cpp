@@ -15,9 +15,10 @@
 #include <vector>
 
 #include "../../include/jetlong.h"
+#include "cache8.h"
 
 namespace jl {
-// kernels (prefill.hip, decode.hip, aux.hip)
+// kernels (prefill.hip, decode.hip, cache8.hip, decode8.hip, blocks8.hip, aux.hip)
 hipError_t launch_prefill_chunk(bool bifocal, const uint16_t* q, const uint16_t* k,
                                 const uint16_t* v, uint16_t* o, float* lse, const float2* table,
                                 const float2* rtable, const uint32_t* table16,
@@ -61,6 +62,21 @@ size_t noalloc_decode_state_bytes();
 size_t noalloc_decode_slot_bytes();
 hipError_t noalloc_decode_buffers(double theta, const double* omega, hipStream_t stream,
                                   const float2** table, float** states);
+hipError_t launch_append8(const Cache8& c, const uint16_t* k, const uint16_t* v,
+                          const int32_t* starts, const int32_t* n_new, int B, int n,
+                          hipStream_t stream);
+hipError_t launch_read8(const Cache8& c, uint16_t* k, uint16_t* v, int B, int start, int n,
+                        hipStream_t stream);
+size_t decode8_workspace_bytes(int g);
+hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, const int32_t* kv_lens,
+                          const int32_t* blocks, int n_select, uint16_t* o, const float2* table,
+                          int B, int Hq, int w_pre, int w0, void* ws, hipStream_t stream);
+hipError_t launch_block_scores8(bool bifocal, const Cache8& c, const uint16_t* q,
+                                const int32_t* kv_lens, float* scores, const float2* table, int B,
+                                int Hq, int w_pre, hipStream_t stream);
+hipError_t launch_select_blocks(const float* scores, const int32_t* kv_lens, int32_t* blocks,
+                                int B, int Hkv, int n_blocks, int n_select, int w0, int n_first,
+                                hipStream_t stream);
 hipError_t launch_build_table(float2* table, uint32_t* table16, int n_pos, const double* omega,
                               hipStream_t stream);
 hipError_t launch_debug_schedule(const int32_t* lengths, int nl, const int32_t* positions, int np,
@@ -72,7 +88,7 @@ hipError_t launch_debug_tiles(int L, int BQ, int BK, int w0, int nqb, int nkt, i
 
 namespace {
 
-constexpr int kHeadDim = 128;
+using jl::kHeadDim;
 constexpr int kDecodeMaxLen = 1 << 23;
 // paged chunked prefill: a page holds whole 64-key tiles, and one sequence's
 // page list fits the attention kernel's LDS table
@@ -596,6 +612,115 @@ int decode_common(bool bifocal, const void* q, const void* kc, const void* vc,
   return ok();
 }
 
+// ------------------------------------------------------------ 8-bit cache
+// The checks that every entry point over an 8-bit cache makes of it, for B
+// sequences; *out is what the kernels take.
+int check_cache8(const jl_cache8* c, const int32_t* block_table, int max_pages, int B,
+                 jl::Cache8* out) {
+  if (c == nullptr) return fail(JL_ERR_INVALID_ARG, "cache must be non-null");
+  if (B < 1 || c->Hkv < 1 || c->n_pages < 1)
+    return fail(JL_ERR_INVALID_ARG, "B, Hkv, n_pages must be >= 1 (got %d, %d, %d)", B, c->Hkv,
+                c->n_pages);
+  if (c->head_dim < 2 || c->head_dim % 2 != 0)
+    return fail(JL_ERR_INVALID_ARG, "head_dim must be even and >= 2 (got %d)", c->head_dim);
+  if (c->head_dim != kHeadDim)
+    return fail(JL_ERR_UNSUPPORTED, "head_dim %d not built (only 128)", c->head_dim);
+  if (c->page_size < jl::kBlk || c->page_size % jl::kBlk != 0)
+    return fail(JL_ERR_INVALID_ARG, "page_size must be a multiple of %d (got %d)", jl::kBlk,
+                c->page_size);
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->k_mean))
+    return fail(JL_ERR_INVALID_ARG, "the cache's k, v, k_mean must be non-null and 16-byte aligned");
+  if (!aligned4(c->k_scale) || !aligned4(c->v_scale))
+    return fail(JL_ERR_INVALID_ARG, "the cache's scales must be non-null and 4-byte aligned");
+  const int per = c->page_size / jl::kBlk;
+  if ((long long)c->n_pages * c->Hkv * per > 0x7fffffffLL)
+    return fail(JL_ERR_UNSUPPORTED, "a cache holds fewer than 2^31 blocks");
+  long long cap = c->page_size;
+  if (block_table != nullptr) {
+    if (!aligned4(block_table))
+      return fail(JL_ERR_INVALID_ARG, "block_table must be 4-byte aligned");
+    if (max_pages < 1) return fail(JL_ERR_INVALID_ARG, "max_pages must be >= 1 (got %d)", max_pages);
+    cap *= max_pages;
+  } else if (B > c->n_pages) {
+    return fail(JL_ERR_INVALID_ARG, "a dense cache of %d sequences cannot hold %d", c->n_pages, B);
+  }
+  if (cap > kDecodeMaxLen)
+    return fail(JL_ERR_UNSUPPORTED, "an 8-bit cache holds at most %d positions a sequence (got %lld)",
+                kDecodeMaxLen, cap);
+  *out = jl::Cache8{(unsigned char*)c->k, (unsigned char*)c->v, c->k_scale, c->v_scale,
+                    (uint16_t*)c->k_mean, block_table, c->n_pages, per, c->Hkv,
+                    block_table != nullptr ? max_pages : 1, (int)(cap / jl::kBlk)};
+  return JL_OK;
+}
+
+int check_query8(const jl::Cache8& c, const void* q, const int32_t* kv_lens, int Hq, double theta,
+                 bool bifocal, int w_pre) {
+  if (Hq < 1 || Hq % c.Hkv != 0)
+    return fail(JL_ERR_INVALID_ARG, "Hq (%d) must be a positive multiple of Hkv (%d)", Hq, c.Hkv);
+  if (Hq / c.Hkv > 8) return fail(JL_ERR_UNSUPPORTED, "decode GQA group %d > 8", Hq / c.Hkv);
+  if (!(theta > 0.0) || !std::isfinite(theta))
+    return fail(JL_ERR_INVALID_ARG, "rope_theta must be finite and > 0");
+  if (bifocal && w_pre < 1)
+    return fail(JL_ERR_INVALID_ARG, "w_pretrained must be >= 1 (got %d)", w_pre);
+  if (!aligned16(q)) return fail(JL_ERR_INVALID_ARG, "q must be non-null and 16-byte aligned");
+  if (!aligned4(kv_lens)) return fail(JL_ERR_INVALID_ARG, "kv_lens must be non-null and aligned");
+  return JL_OK;
+}
+
+// blocks == nullptr: every block of the sequences
+int decode8_common(bool bifocal, const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                   const void* q, const int32_t* kv_lens, bool listed, const int32_t* blocks,
+                   int n_select, void* o, int B, int Hq, double theta, int w_pre, int w0, void* ws,
+                   size_t ws_bytes, void* stream) {
+  jl::Cache8 c;
+  int st = check_cache8(cache, block_table, max_pages, B, &c);
+  if (st == JL_OK) st = check_query8(c, q, kv_lens, Hq, theta, bifocal, w_pre);
+  if (st != JL_OK) return st;
+  if (bifocal && w0 < 0) return fail(JL_ERR_INVALID_ARG, "w_local must be >= 0 (got %d)", w0);
+  if (!aligned16(o)) return fail(JL_ERR_INVALID_ARG, "o must be non-null and 16-byte aligned");
+  if (listed) {
+    if (!aligned4(blocks)) return fail(JL_ERR_INVALID_ARG, "blocks must be non-null and aligned");
+    if (n_select < 1) return fail(JL_ERR_INVALID_ARG, "n_select must be >= 1 (got %d)", n_select);
+    if ((long long)B * c.Hkv * n_select > 0x7fffffffLL)
+      return fail(JL_ERR_INVALID_ARG, "problem too large");
+  }
+  if ((long long)B * c.Hkv * c.n_blocks > 0x7fffffffLL)
+    return fail(JL_ERR_INVALID_ARG, "problem too large");
+  const size_t need = jl::decode8_workspace_bytes(Hq / c.Hkv);
+  if (ws == nullptr || ws_bytes < need)
+    return fail(JL_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, ws_bytes);
+  if (!aligned16(ws)) return fail(JL_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+  Tables tab{};
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  st = get_table(theta, c.n_blocks * jl::kBlk, s, &tab);
+  if (st != JL_OK) return st;
+  const hipError_t e =
+      jl::launch_decode8(bifocal, c, (const uint16_t*)q, kv_lens, listed ? blocks : nullptr,
+                         n_select, (uint16_t*)o, tab.f32, B, Hq, w_pre, w0, ws, s);
+  if (e != hipSuccess) return hip_fail(e, "8-bit decode launch");
+  return ok();
+}
+
+int block_scores8(bool bifocal, const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                  const void* q, const int32_t* kv_lens, float* scores, int B, int Hq,
+                  double theta, int w_pre, void* stream) {
+  jl::Cache8 c;
+  int st = check_cache8(cache, block_table, max_pages, B, &c);
+  if (st == JL_OK) st = check_query8(c, q, kv_lens, Hq, theta, bifocal, w_pre);
+  if (st != JL_OK) return st;
+  if (!aligned4(scores)) return fail(JL_ERR_INVALID_ARG, "scores must be non-null and aligned");
+  if ((long long)B * c.Hkv * c.n_blocks > 0x7fffffffLL)
+    return fail(JL_ERR_INVALID_ARG, "problem too large");
+  Tables tab{};
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  st = get_table(theta, c.n_blocks * jl::kBlk, s, &tab);
+  if (st != JL_OK) return st;
+  const hipError_t e = jl::launch_block_scores8(bifocal, c, (const uint16_t*)q, kv_lens, scores,
+                                                tab.f32, B, Hq, w_pre, s);
+  if (e != hipSuccess) return hip_fail(e, "block scores launch");
+  return ok();
+}
+
 }  // namespace
 
 extern "C" {
@@ -841,6 +966,127 @@ int jl_rope_attention_decode_paged(const void* q, const void* k_pages, const voi
   return decode_common(false, q, k_pages, v_pages, kv_lens, 0, o, B, Hq, Hkv, head_dim,
                        rope_theta, 1, 0, workspace, workspace_bytes, stream, block_table,
                        max_pages, page_size, n_pages);
+}
+
+int jl_cache8_append(const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                     const void* k, const void* v, const int32_t* starts, const int32_t* n_new,
+                     int B, int n, void* stream) {
+  jl::Cache8 c;
+  const int st = check_cache8(cache, block_table, max_pages, B, &c);
+  if (st != JL_OK) return st;
+  if (n < 1) return fail(JL_ERR_INVALID_ARG, "n must be >= 1 (got %d)", n);
+  if (!aligned16(k) || !aligned16(v))
+    return fail(JL_ERR_INVALID_ARG, "k, v must be non-null and 16-byte aligned");
+  if (!aligned4(starts)) return fail(JL_ERR_INVALID_ARG, "starts must be non-null and aligned");
+  if (n_new != nullptr && !aligned4(n_new))
+    return fail(JL_ERR_INVALID_ARG, "n_new must be 4-byte aligned");
+  if (((long long)n + jl::kBlk - 2) / jl::kBlk + 1 > 0x7fffffffLL / B / c.Hkv)
+    return fail(JL_ERR_INVALID_ARG, "problem too large");
+  const hipError_t e =
+      jl::launch_append8(c, (const uint16_t*)k, (const uint16_t*)v, starts, n_new, B, n,
+                         reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "append launch");
+  return ok();
+}
+
+int jl_cache8_read(const jl_cache8* cache, const int32_t* block_table, int max_pages, void* k,
+                   void* v, int B, int start, int n, void* stream) {
+  jl::Cache8 c;
+  const int st = check_cache8(cache, block_table, max_pages, B, &c);
+  if (st != JL_OK) return st;
+  if (start < 0 || n < 1 || (long long)start + n > (long long)c.n_blocks * jl::kBlk)
+    return fail(JL_ERR_INVALID_ARG, "rows %d .. %lld are not in a cache of %lld positions", start,
+                (long long)start + n - 1, (long long)c.n_blocks * jl::kBlk);
+  if (!aligned16(k) || !aligned16(v))
+    return fail(JL_ERR_INVALID_ARG, "k, v must be non-null and 16-byte aligned");
+  if ((long long)n / jl::kBlk + 2 > 0x7fffffffLL / B / c.Hkv)
+    return fail(JL_ERR_INVALID_ARG, "problem too large");
+  const hipError_t e = jl::launch_read8(c, (uint16_t*)k, (uint16_t*)v, B, start, n,
+                                        reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "cache read launch");
+  return ok();
+}
+
+size_t jl_decode8_workspace_bytes(int Hq, int Hkv, int head_dim) {
+  if (Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq / Hkv > 8 || head_dim != kHeadDim) return 0;
+  return jl::decode8_workspace_bytes(Hq / Hkv);
+}
+
+int jl_bifocal_decode8(const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                       const void* q, const int32_t* kv_lens, void* o, int B, int Hq,
+                       double rope_theta, int w_pretrained, int w_local, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  return decode8_common(true, cache, block_table, max_pages, q, kv_lens, false, nullptr, 0, o, B,
+                        Hq, rope_theta, w_pretrained, w_local, workspace, workspace_bytes, stream);
+}
+
+int jl_rope_attention_decode8(const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                              const void* q, const int32_t* kv_lens, void* o, int B, int Hq,
+                              double rope_theta, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+  return decode8_common(false, cache, block_table, max_pages, q, kv_lens, false, nullptr, 0, o, B,
+                        Hq, rope_theta, 1, 0, workspace, workspace_bytes, stream);
+}
+
+int jl_bifocal_decode8_blocks(const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                              const void* q, const int32_t* kv_lens, const int32_t* blocks,
+                              int n_select, void* o, int B, int Hq, double rope_theta,
+                              int w_pretrained, int w_local, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  return decode8_common(true, cache, block_table, max_pages, q, kv_lens, true, blocks, n_select, o,
+                        B, Hq, rope_theta, w_pretrained, w_local, workspace, workspace_bytes,
+                        stream);
+}
+
+int jl_rope_attention_decode8_blocks(const jl_cache8* cache, const int32_t* block_table,
+                                     int max_pages, const void* q, const int32_t* kv_lens,
+                                     const int32_t* blocks, int n_select, void* o, int B, int Hq,
+                                     double rope_theta, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
+  return decode8_common(false, cache, block_table, max_pages, q, kv_lens, true, blocks, n_select,
+                        o, B, Hq, rope_theta, 1, 0, workspace, workspace_bytes, stream);
+}
+
+int jl_bifocal_block_scores8(const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                             const void* q, const int32_t* kv_lens, float* scores, int B, int Hq,
+                             double rope_theta, int w_pretrained, void* stream) {
+  return block_scores8(true, cache, block_table, max_pages, q, kv_lens, scores, B, Hq, rope_theta,
+                       w_pretrained, stream);
+}
+
+int jl_rope_block_scores8(const jl_cache8* cache, const int32_t* block_table, int max_pages,
+                          const void* q, const int32_t* kv_lens, float* scores, int B, int Hq,
+                          double rope_theta, void* stream) {
+  return block_scores8(false, cache, block_table, max_pages, q, kv_lens, scores, B, Hq, rope_theta,
+                       1, stream);
+}
+
+int jl_select_blocks(const float* scores, const int32_t* kv_lens, int32_t* blocks, int B, int Hkv,
+                     int n_blocks, int n_select, int w_local, int n_first, void* stream) {
+  if (B < 1 || Hkv < 1 || n_blocks < 1 || n_select < 1)
+    return fail(JL_ERR_INVALID_ARG, "B, Hkv, n_blocks, n_select must be >= 1 (got %d, %d, %d, %d)",
+                B, Hkv, n_blocks, n_select);
+  if (w_local < 0 || n_first < 0)
+    return fail(JL_ERR_INVALID_ARG, "w_local and n_first must be >= 0 (got %d, %d)", w_local,
+                n_first);
+  if (!aligned4(scores) || !aligned4(kv_lens) || !aligned4(blocks))
+    return fail(JL_ERR_INVALID_ARG, "scores, kv_lens, blocks must be non-null and aligned");
+  if (n_blocks > kDecodeMaxLen / jl::kBlk)
+    return fail(JL_ERR_UNSUPPORTED, "n_blocks %d exceeds %d", n_blocks, kDecodeMaxLen / jl::kBlk);
+  // the band's w_local + 1 keys lie in at most this many blocks
+  const long long always = std::min<long long>(
+      n_blocks, ((long long)w_local + 127) / jl::kBlk + n_first);
+  if (n_select < always)
+    return fail(JL_ERR_INVALID_ARG,
+                "n_select (%d) must hold the first n_first blocks and those of the band (%lld)",
+                n_select, always);
+  if ((long long)B * Hkv * std::max(n_blocks, n_select) > 0x7fffffffLL)
+    return fail(JL_ERR_INVALID_ARG, "problem too large");
+  const hipError_t e = jl::launch_select_blocks(scores, kv_lens, blocks, B, Hkv, n_blocks, n_select,
+                                                w_local, n_first,
+                                                reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "block choice launch");
+  return ok();
 }
 
 int jl_debug_schedule(const int32_t* lengths, int n_lengths, const int32_t* positions,
