@@ -3,11 +3,29 @@
 //
 // The method is decode.hip's (Jet-Long, arXiv 2607.07740, Sec. 3.2): the query of
 // sequence b sits at kv_len[b] - 1, G follows from kv_len[b], a key is rotated to
-// the view its distance selects (Eq. (1)).  A sequence without keys, or whose list
-// names none, gets zeros.
+// the view its distance selects (Eq. (1)), and the 16 columns of a matrix
+// instruction are the group's heads in the base (0..7) and the remote view (8..15);
+// a column keeps the keys of its own view, so that each is a partial softmax state,
+// and the states merge by Eq. (7).  A sequence without keys, or whose list names
+// none, gets zeros.
+#include <algorithm>
+#include <climits>
+
 #include "cache8.h"
 
 namespace jl {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kD8Waves = 4;
+constexpr int kD8Threads = 64 * kD8Waves;
+constexpr int kD8MaxWg = 512;    // workgroups of a call: workspaces are sized for as many
+constexpr int kD8List = 256;     // steps whose blocks are looked up at a time
+constexpr int kD8SegCost = 2;    // what a workgroup pays for a further segment, in steps
+constexpr int kD8State = 132;    // floats of a state: m, l, pad, pad, O[128]
+constexpr float kD8Up = 15.f, kD8Down = 0x1p-15f;  // weights in fp16 are times 2^15
+constexpr int kD8Counters = 1024;  // at the front of the workspace (4096 bytes)
 
 struct Decode8Args {
   Cache8 c;
@@ -16,126 +34,558 @@ struct Decode8Args {
   const int32_t* blocks;  // [B][Hkv][n_select], or nullptr: every block
   uint16_t* o;
   const float2* table;
+  int* counters;
+  float* states;  // [2 n_wg][g][kD8State]
   int B, Hq, g, n_select;
-  int w_pre, w0;
+  int n_wg, w_pre, w0;
   float q_scale;
 };
 
-// Workgroup = (sequence, kv head), fp32 throughout: scores of 64 keys, softmax
-// step, values.
-template <bool BIFOCAL>
-__global__ __launch_bounds__(256) void decode8_kernel(Decode8Args a) {
-  __shared__ float sq[2][8][kHeadDim];  // the rotated queries of both views
-  __shared__ float sp[8][kBlk];
-  __shared__ float so[8][kHeadDim];
+// The (sequence, kv head) pairs are segments of a list, each as long as its steps of
+// 64 keys and kD8SegCost empty ones, and workgroup w takes the w-th of n equal
+// ranges.  Two workgroups that share a segment meet in its counter: the first's
+// index names it, since only a range's last segment goes on in the next range.
+struct Segments {
+  uint32_t V, q, r;  // entries; per range, and ranges (the first ones) with one more
+  int n;             // ranges
+};
+
+__device__ inline void make_ranges(Segments& s, int n_wg, uint32_t V) {
+  s.V = V;
+  // no range shorter than one step per wave and the cost of its segment
+  s.n = (int)min((uint32_t)n_wg, (V + kD8Waves + kD8SegCost - 1) / (kD8Waves + kD8SegCost));
+  s.q = V / (uint32_t)s.n;
+  s.r = V - s.q * (uint32_t)s.n;
+}
+__device__ inline uint32_t range_start(const Segments& s, uint32_t w) {
+  return s.q * w + min(w, s.r);
+}
+__device__ inline int range_at(const Segments& s, uint32_t x) {
+  const uint32_t head = s.r * (s.q + 1);
+  return (int)(x < head ? x / (s.q + 1) : s.r + (x - head) / s.q);
+}
+
+__device__ inline int len8(const Decode8Args& a, int b) {
+  return min(max(a.kv_lens[b], 0), a.c.n_blocks * kBlk);
+}
+// list entries of a segment of sequence b
+__device__ inline int entries8(const Decode8Args& a, int b) {
+  return (len8(a, b) + kBlk - 1) / kBlk + kD8SegCost;
+}
+
+// Maximum over the lanes l, l ^ 16, l ^ 32, l ^ 48, by lane swaps in registers.
+__device__ inline float max_over_groups(float x) {
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ inline f32x4 mfma16h(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Two e4m3 numbers of a word's low or high half as fp16 (exact).
+template <bool HIGH>
+__device__ inline f16x2 e4m3_f16(uint32_t w) {
+  return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH);
+}
+// The pair (x_i, x_{i+64}) rotated by cs = (cos, sin): two packed fp16 instructions.
+__device__ inline f16x2 rotate_pair(f16x2 x, f16x2 cs) {
+  const f16x2 c = __builtin_shufflevector(cs, cs, 0, 0);
+  const f16x2 s = {-cs[1], cs[1]};
+  const f16x2 sw = __builtin_shufflevector(x, x, 1, 0);
+  return __builtin_elementwise_fma(x, c, sw * s);
+}
+
+constexpr int kD8TabRow = kHalf * 4 + 16;  // 64 fp16 (cos, sin) and 16 bytes, so that rows start 4 banks apart
+constexpr int kD8Row = kHeadDim + 4;       // floats of a merge row
+
+struct __attribute__((aligned(16))) Decode8Smem {
+  unsigned char tab[kBlk * kD8TabRow];      // (cos, sin)(t omega_i), t < 64
+  float2 rows[kD8Waves][2][kHalf];          // a step's (cos, sin) rows that rotate its query
+  int2 list[kD8List];                       // (block of the sequence or -1, block of the pools)
+  union {
+    float o[kD8Waves][16][kD8Row];          // the waves' states
+    float w[8][kD8MaxWg];                   // the weights of a segment's parts
+  };
+  float m[kD8Waves][16], l[kD8Waves][16];
+  float top[8][kD8Waves * 2];
+  unsigned long long sum[kD8Waves];
+  int last;
+};
+
+// Workgroup w of four waves: its range's segments one after another; a wave takes every
+// fourth step of 64 keys and keeps the 16 columns' states in registers.
+//
+// A step is 16 KB, K and V, that go from memory into registers, 16 bytes a lane and
+// 1 KB an instruction, one step ahead; the layout is the matrix operands' own.
+// Rotation by offset in the block: with k0 the block's first position, a key is
+// rotated by t = k - k0 (base) or f(k) - f(k0) (remote), from 64 rows of fp16
+// (cos, sin) in LDS, and the query's columns by q - k0 or f(q) - f(k0) in fp32:
+// only relative positions matter (Sec. 3.2, Eq. (6)).  A rotated pair costs a
+// conversion and two packed fp16 instructions and goes to the matrix cores as
+// it is: e4m3 numbers are exact in fp16, and with |x| <= 448 none overflows.  The
+// block's scale of K multiplies the scores, that of V the step's product.
+// The query is brought to [1, 2) by a power of two first, its own range aside.
+template <bool BIFOCAL, bool LISTED>
+__global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
+  __shared__ Decode8Smem sm;
   const int tid = threadIdx.x;
-  const int b = blockIdx.x / a.c.Hkv, h = blockIdx.x - b * a.c.Hkv;
-  const int kv_len = min(max(a.kv_lens[b], 0), a.c.n_blocks * kBlk);
-  const int qpos = kv_len - 1;
-  const FastDiv gdiv = make_fastdiv(BIFOCAL ? group_size(max(kv_len, 1), a.w_pre) : 1);
-  for (int i = tid; i < a.g * kHalf; i += 256) {
-    const int j = i >> 6, f = i & 63;
-    const uint16_t* q = a.q + ((size_t)b * a.Hq + h * a.g + j) * kHeadDim;
-    const float lo = __uint_as_float((uint32_t)q[f] << 16) * a.q_scale;
-    const float hi = __uint_as_float((uint32_t)q[f + 64] << 16) * a.q_scale;
-    for (int view = 0; view < 2; ++view) {
-      const int pos = max(view == 0 ? qpos : remote_pos(max(qpos, 0), gdiv), 0);
-      const float2 cs = a.table[(size_t)pos * kHalf + f];
-      sq[view][j][f] = lo * cs.x - hi * cs.y;
-      sq[view][j][f + 64] = hi * cs.x + lo * cs.y;
-    }
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i16 = lane & 15, g4 = lane >> 4;
+  const int w = blockIdx.x;
+
+  // ---- offset rows, fp32 to fp16
+  for (int i = tid; i < kBlk * kHalf / 4; i += kD8Threads) {
+    const float4 x = ((const float4*)a.table)[2 * i], y = ((const float4*)a.table)[2 * i + 1];
+    const f16x8 h = {(_Float16)x.x, (_Float16)x.y, (_Float16)x.z, (_Float16)x.w,
+                     (_Float16)y.x, (_Float16)y.y, (_Float16)y.z, (_Float16)y.w};
+    *(f16x8*)(sm.tab + (i >> 4) * kD8TabRow + 16 * (i & 15)) = h;
   }
-  __syncthreads();
-  const int key = tid >> 2, part = tid & 3;
-  const int d = tid & 127, half = tid >> 7;
-  float m[8], l[8], acc[8];
+
+  // ---- this workgroup's range, and the sequence and head it begins in
+  Segments sg;
+  uint32_t pos;  // list entry of the current segment's first step
+  int b, h;
+  uint32_t x0, x1;
+  if (LISTED) {
+    const uint32_t e = (uint32_t)(a.n_select + kD8SegCost);
+    make_ranges(sg, a.n_wg, e * (uint32_t)(a.B * a.c.Hkv));
+    if (w >= sg.n) return;
+    x0 = range_start(sg, w);
+    const uint32_t seg = x0 / e;
+    b = (int)(seg / (uint32_t)a.c.Hkv);
+    h = (int)(seg - (uint32_t)b * a.c.Hkv);
+    pos = seg * e;
+  } else {
+    // all lengths, 64 at a time; every wave for itself
+    uint32_t V = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+      uint32_t v = b0 + lane < a.B ? (uint32_t)entries8(a, b0 + lane) * a.c.Hkv : 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    m[j] = -INFINITY;
-    l[j] = acc[j] = 0.f;
-  }
-  const int n_steps = a.blocks != nullptr ? a.n_select : (kv_len + kBlk - 1) / kBlk;
-  for (int s = 0; s < n_steps; ++s) {
-    const int blk =
-        a.blocks != nullptr ? a.blocks[((size_t)b * a.c.Hkv + h) * a.n_select + s] : s;
-    if (blk < 0 || blk >= a.c.n_blocks || blk * kBlk >= kv_len) continue;
-    const int page = min(max(page_of(a.c, b, blk), 0), a.c.n_pages - 1);
-    const size_t at = (size_t)pool_block(a.c, page, h, in_page(a.c, blk));
-    const unsigned char* kb = a.c.k + at * kBlkBytes;
-    const unsigned char* vb = a.c.v + at * kBlkBytes;
-    const int pos = blk * kBlk + key;
-    const int view = BIFOCAL && qpos - pos > a.w0 ? 1 : 0;
-    const int rp = view == 1 ? remote_pos(pos, gdiv) : pos;
-    float sc[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sc[j] = 0.f;
-    for (int i = 0; i < 16; ++i) {
-      const int f = 16 * part + i;
-      const uint32_t w = *(const uint16_t*)(kb + k_offset(key, f));
-      const float2 x = e4m3_pair<false>(w);
-      const float2 cs = a.table[(size_t)rp * kHalf + f];
-      const float lo = x.x * cs.x - x.y * cs.y, hi = x.y * cs.x + x.x * cs.y;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < a.g) sc[j] += lo * sq[view][j][f] + hi * sq[view][j][f + 64];
+      for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+      V += v;
     }
-    const float ks = a.c.k_scale[at], vs = a.c.v_scale[at];
+    make_ranges(sg, a.n_wg, __builtin_amdgcn_readfirstlane(V));
+    if (w >= sg.n) return;
+    x0 = range_start(sg, w);
+    uint32_t before = 0;
+    b = 0;
+    pos = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+      const uint32_t v = b0 + lane < a.B ? (uint32_t)entries8(a, b0 + lane) * a.c.Hkv : 0;
+      uint32_t incl = v;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      sc[j] += __shfl_xor(sc[j], 1);
-      sc[j] += __shfl_xor(sc[j], 2);
-      if (part == 0 && j < a.g) sp[j][key] = pos < kv_len ? sc[j] * ks : -INFINITY;
-    }
-    __syncthreads();
-    for (int j = 0; j < a.g; ++j) {
-      float mx = m[j];
-      for (int i = 0; i < kBlk; ++i) mx = fmaxf(mx, sp[j][i]);
-      const float use = mx == -INFINITY ? 0.f : mx;
-      const float alpha = fast_exp2(m[j] - use);
-      m[j] = mx;
-      float sum = 0.f, o = 0.f;
-      for (int i = 0; i < 32; ++i) {
-        const int k2 = 32 * half + i;
-        const float p = fast_exp2(sp[j][k2] - use);
-        const float v = e4m3_pair<false>(vb[v_offset(k2, d)]).x;
-        sum += p;
-        if (blk * kBlk + k2 < kv_len) o += p * v;
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t t = __shfl_up(incl, o);
+        if (lane >= o) incl += t;
       }
-      l[j] = l[j] * alpha + sum;
-      acc[j] = acc[j] * alpha + o * vs;
+      const uint32_t all = __builtin_amdgcn_readlane(incl, 63);
+      if (x0 < before + all) {
+        const int i = (int)__popcll(__ballot(before + incl <= x0));
+        b = b0 + i;
+        pos = before + __builtin_amdgcn_readlane(incl - v, i);
+        break;
+      }
+      before += all;
     }
-    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(b);
+    pos = __builtin_amdgcn_readfirstlane(pos);
+    const uint32_t e = (uint32_t)entries8(a, b);
+    h = (int)((x0 - pos) / e);
+    pos += (uint32_t)h * e;
   }
-  for (int j = 0; j < a.g; ++j) {
-    if (half == 1) {
-      so[j][d] = acc[j];
-      if (d == 0) sp[j][0] = l[j];
+  x1 = range_start(sg, (uint32_t)w + 1);
+  h = __builtin_amdgcn_readfirstlane(h);
+  __syncthreads();  // the offset rows
+
+  // query columns: col = (view, head); the distances q - k that a column keeps are
+  // [keep_lo, keep_lo + keep_n) as one unsigned compare (none for unused columns)
+  const int view = i16 >> 3, hj = i16 & 7;
+  const bool col_on = hj < a.g && (BIFOCAL || view == 0);
+
+  for (; pos < x1 && b < a.B;) {
+    const int kv_len = __builtin_amdgcn_readfirstlane(len8(a, b));
+    const int n_real = LISTED ? a.n_select : (kv_len + kBlk - 1) / kBlk;
+    const uint32_t end = pos + (uint32_t)n_real;
+    const uint32_t from = max(x0, pos);
+    const int off = (int)(from - pos);
+    const int n_steps = (int)min(x1, end) - (int)from;  // of this segment, here
+    const size_t o_at = ((size_t)b * a.Hq + h * a.g) * kHeadDim;
+    if (n_real == 0 && pos >= x0) {  // a sequence without keys
+      for (int i = tid; i < a.g * kHeadDim / 8; i += kD8Threads) ((u32x4*)(a.o + o_at))[i] = u32x4{};
     }
-  }
-  __syncthreads();
-  if (half == 0) {
-    for (int j = 0; j < a.g; ++j) {
-      const float den = l[j] + sp[j][0];
-      const __bf16 r = (__bf16)(den == 0.f ? 0.f : (acc[j] + so[j][d]) / den);
-      a.o[((size_t)b * a.Hq + h * a.g + j) * kHeadDim + d] = __builtin_bit_cast(uint16_t, r);
+    if (n_steps > 0) {
+      const int G = BIFOCAL ? group_size(max(kv_len, 1), a.w_pre) : 1;
+      const FastDiv gdiv = make_fastdiv((uint32_t)G);
+      const int w0 = G > 1 ? a.w0 : INT_MAX;  // one view only where f is the identity
+      const int qpos = max(kv_len - 1, 0);
+      const int fq = (int)fastdiv((uint32_t)qpos, gdiv);
+      const int keep_lo = BIFOCAL && view == 1 ? (int)min((uint32_t)w0 + 1u, (uint32_t)INT_MAX) : 0;
+      const uint32_t keep_n = !col_on ? 0u
+                              : view == 0 ? (uint32_t)w0 + 1u
+                                          : (uint32_t)INT_MAX - (uint32_t)w0;
+
+      // ---- the column's query in fp32, pairs 32 u + 8 g4 + j, scaled by log2(e) / sqrt(d) and
+      // by the power of two that brings its largest value to [1, 2)
+      float qlo[16], qhi[16];
+      float q_back;  // what undoes the latter
+      {
+        const uint16_t* qrow = a.q + o_at + (size_t)min(hj, a.g - 1) * kHeadDim + 8 * g4;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          unpack8(load16(qrow + 32 * u), qlo + 8 * u);
+          unpack8(load16(qrow + 64 + 32 * u), qhi + 8 * u);
+        }
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, fmaxf(fabsf(qlo[i]), fabsf(qhi[i])));
+        top = max_over_groups(top);
+        const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
+        const float down = pow2f(-e);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          qlo[i] = qlo[i] * down * a.q_scale;
+          qhi[i] = qhi[i] * down * a.q_scale;
+        }
+        q_back = pow2f(e);
+      }
+
+      f32x4 acc[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] = f32x4{};
+      float m_run = -INFINITY, l_run = 0.f;
+
+      // the step in hand; its K registers take the next step's as soon as the scores are
+      // formed, its V registers when the product is
+      u32x4 kx[8], vx[8], row;
+      float ks, vs;
+      int k0;         // first position of the step's block, below 0: nothing to do
+      int k0n, phys;  // of the step that is loaded
+      auto look_up = [&](int i) __attribute__((always_inline)) {
+        const int2 at = sm.list[i];
+        k0n = __builtin_amdgcn_readfirstlane(at.x);
+        phys = __builtin_amdgcn_readfirstlane(at.y);
+      };
+      auto load_k = [&]() __attribute__((always_inline)) {
+        const unsigned char* kp = a.c.k + (size_t)phys * kBlkBytes;
+        ks = a.c.k_scale[phys];
+        const int kk = max(k0n, 0);
+        int r = qpos - kk;
+        if (BIFOCAL && lane >= 32) r = fq - (int)fastdiv((uint32_t)kk, gdiv);
+        row = *(const u32x4*)((const unsigned char*)a.table +
+                              (size_t)(uint32_t)max(r, 0) * (kHalf * 8) + 16 * (lane & 31));
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+          kx[n] = __builtin_nontemporal_load((const u32x4*)(kp + 1024 * n + 16 * lane));
+      };
+      auto load_v = [&]() __attribute__((always_inline)) {
+        const unsigned char* vp = a.c.v + (size_t)phys * kBlkBytes;
+        vs = a.c.v_scale[phys] * kD8Down;
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+          vx[n] = __builtin_nontemporal_load((const u32x4*)(vp + 1024 * n + 16 * lane));
+      };
+
+      // sc: the scores of four tiles of 16 keys, in units of the block's scale
+      f32x4 sc[4];
+      auto scores = [&]() __attribute__((always_inline)) {
+        // ---- the query rotated by q - k0 (base columns) or f(q) - f(k0) (remote)
+        f16x8 qop[4];
+        {
+          float2* rows = &sm.rows[wave][0][0];
+          ((u32x4*)rows)[lane] = row;
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+          const float4* cs = (const float4*)(rows + (BIFOCAL ? view * kHalf : 0));
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+              const float4 c = cs[16 * u + 4 * g4 + j / 2];
+              const int n = 8 * u + j;
+              f16x8& o = qop[2 * u + j / 4];
+              const int at = 2 * (j & 3);
+              o[at] = (_Float16)(qlo[n] * c.x - qhi[n] * c.y);
+              o[at + 1] = (_Float16)(qhi[n] * c.x + qlo[n] * c.y);
+              o[at + 2] = (_Float16)(qlo[n + 1] * c.z - qhi[n + 1] * c.w);
+              o[at + 3] = (_Float16)(qhi[n + 1] * c.z + qlo[n + 1] * c.w);
+            }
+          __builtin_amdgcn_wave_barrier();
+        }
+
+        const int fk0 = BIFOCAL ? (int)fastdiv_ge2((uint32_t)k0, gdiv) : 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int off = 16 * t + i16;  // of this lane's key in the block
+          int r = off;
+          if (BIFOCAL && qpos - (k0 + off) > w0)
+            r = (int)fastdiv_ge2((uint32_t)(k0 + off), gdiv) - fk0;
+          const unsigned char* row = sm.tab + r * kD8TabRow + 32 * g4;
+          sc[t] = f32x4{};
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const f16x8 c0 = *(const f16x8*)(row + 128 * u), c1 = *(const f16x8*)(row + 128 * u + 16);
+            const u32x4 x = kx[2 * t + u];
+            f16x8 y0, y1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const f16x8& c = i < 2 ? c0 : c1;
+              f16x8& y = i < 2 ? y0 : y1;
+              const int p = 4 * (i & 1);
+              const f16x2 ya = rotate_pair(e4m3_f16<false>(x[i]), f16x2{c[p], c[p + 1]});
+              const f16x2 yb = rotate_pair(e4m3_f16<true>(x[i]), f16x2{c[p + 2], c[p + 3]});
+              y[p] = ya[0];
+              y[p + 1] = ya[1];
+              y[p + 2] = yb[0];
+              y[p + 3] = yb[1];
+            }
+            sc[t] = mfma16h(y0, qop[2 * u], sc[t]);
+            sc[t] = mfma16h(y1, qop[2 * u + 1], sc[t]);
+          }
+        }
+
+      };
+
+      f16x8 p[2];
+      auto softmax = [&](float ks) __attribute__((always_inline)) {
+        // ---- each column keeps the keys of its own view; lane: keys 16 t + 4 g4 + i
+        const uint32_t dist = (uint32_t)(qpos - k0 - 4 * g4) - (uint32_t)keep_lo;
+        float mt = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sc[t][i] = dist - (uint32_t)(16 * t + i) < keep_n ? sc[t][i] : -INFINITY;
+            mt = fmaxf(mt, sc[t][i]);
+          }
+        // a power of two, so f times a score is exact; positive and finite, so that a masked
+        // score stays -inf
+        const float f = __builtin_amdgcn_fmed3f(ks * q_back, 0x1p-126f, 0x1p126f);
+        mt = max_over_groups(mt) * f;
+        // The reference lies kD8Up below the maximum: weights are at most 2^15, and fp16 holds
+        // 2^-29 .. 1 of the largest to 11 bits and 2^-39 of it at all.  (A maximum whose
+        // last bit is above 1 is the reference itself.)  The sum is that of the rounded
+        // weights.
+        mt = fabsf(mt) < 0x1p22f ? mt - kD8Up : mt;
+        const float m_new = fmaxf(m_run, mt);
+        const float m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = m_new == m_run ? 1.f : fast_exp2(m_run - m_use);
+        float l = 0.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const f16x2 one = {(_Float16)1.f, (_Float16)1.f};
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            const f16x2 pp = {(_Float16)fast_exp2(__builtin_fmaf(sc[t][i], f, -m_use)),
+                              (_Float16)fast_exp2(__builtin_fmaf(sc[t][i + 1], f, -m_use))};
+            l = __builtin_amdgcn_fdot2(pp, one, l, false);
+            p[t >> 1][4 * (t & 1) + i] = pp[0];
+            p[t >> 1][4 * (t & 1) + i + 1] = pp[1];
+          }
+        }
+        l_run = l_run * alpha + l;
+        m_run = m_new;
+        if (__ballot(alpha != 1.f) != 0) {  // most steps leave every maximum alone
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[i] *= alpha;
+        }
+      };
+
+      auto values = [&]() __attribute__((always_inline)) {
+        // ---- O += scale V^T P^T; where the sequence ends inside the block the values behind
+        // its end are zeroed, since 0 times what lies there may be NaN
+        const bool tail = k0 + kBlk > kv_len;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          u32x4 x[2] = {vx[c], vx[4 + c]};
+          if (tail) {
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+              for (int t = 0; t < 2; ++t) {
+                const int left = kv_len - (k0 + 32 * hf + 16 * t + 4 * g4);
+                const uint32_t keep = left >= 4 ? ~0u : left > 0 ? (1u << (8 * left)) - 1 : 0u;
+                x[hf][t] &= keep;
+                x[hf][2 + t] &= keep;
+              }
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            f32x4 d = f32x4{};
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              const f16x2 v0 = e4m3_f16<false>(x[hf][2 * e]), v1 = e4m3_f16<true>(x[hf][2 * e]);
+              const f16x2 v2 = e4m3_f16<false>(x[hf][2 * e + 1]), v3 = e4m3_f16<true>(x[hf][2 * e + 1]);
+              const f16x8 v = {v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+              d = mfma16h(v, p[hf], d);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              acc[2 * c + e][i] = __builtin_fmaf(d[i], vs, acc[2 * c + e][i]);
+          }
+        }
+      };
+
+      // ---- the steps, kD8List at a time
+      for (int s0 = 0; s0 < n_steps; s0 += kD8List) {
+        const int n = min(n_steps - s0, kD8List);
+        if (s0 > 0) __syncthreads();  // the list is read
+        for (int i = tid; i < n; i += kD8Threads) {
+          int blk = off + s0 + i;
+          if (LISTED) blk = a.blocks[((size_t)b * a.c.Hkv + h) * a.n_select + blk];
+          if (blk < 0 || blk >= a.c.n_blocks || blk * kBlk >= kv_len) {
+            sm.list[i] = make_int2(-1, 0);
+          } else {
+            const int page = min(max(page_of(a.c, b, blk), 0), a.c.n_pages - 1);
+            sm.list[i] = make_int2(blk * kBlk, pool_block(a.c, page, h, in_page(a.c, blk)));
+          }
+        }
+        __syncthreads();
+        if (wave < n) {
+          look_up(wave);
+          load_k();
+          load_v();
+        }
+        for (int i = wave; i < n; i += kD8Waves) {
+          const bool more = i + kD8Waves < n;
+          k0 = k0n;
+          if (k0 >= 0) scores();
+          const float ks_now = ks;
+          if (more) {
+            look_up(i + kD8Waves);
+            load_k();
+          }
+          if (k0 >= 0) {
+            softmax(ks_now);
+            values();
+          }
+          if (more) load_v();
+        }
+      }
+
+      // ---- the waves' states, and the two views of a head, into one (max-shifted)
+      l_run += __shfl_xor(l_run, 16);
+      l_run += __shfl_xor(l_run, 32);
+#pragma unroll
+      for (int db = 0; db < 8; ++db) *(f32x4*)&sm.o[wave][i16][16 * db + 4 * g4] = acc[db];
+      if (g4 == 0) {
+        sm.m[wave][i16] = m_run;
+        sm.l[wave][i16] = l_run * kD8Down;
+      }
+      __syncthreads();
+      const int wf = range_at(sg, pos), wl = range_at(sg, end - 1);
+      const int n_parts = wl - wf + 1;
+      const int j = tid >> 5, c4 = 4 * (tid & 31);  // head and channels of this thread
+      if (j < a.g) {
+        float M = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < 2 * kD8Waves; ++x) M = fmaxf(M, sm.m[x >> 1][(x & 1) * 8 + j]);
+        float den = 0.f;
+        f32x4 num = f32x4{};
+#pragma unroll
+        for (int x = 0; x < 2 * kD8Waves; ++x) {
+          const int col = (x & 1) * 8 + j;
+          const float mx = sm.m[x >> 1][col];
+          const float wt = mx == M ? 1.f : fast_exp2(mx - M);
+          den += wt * sm.l[x >> 1][col];
+          num += wt * *(const f32x4*)&sm.o[x >> 1][col][c4];
+        }
+        if (n_parts == 1) {
+          bf16x4 r;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r[i] = (__bf16)(den == 0.f ? 0.f : num[i] / den);
+          *(bf16x4*)(a.o + o_at + (size_t)j * kHeadDim + c4) = r;
+        } else {
+          float* st = a.states + ((size_t)(2 * w + (w == wf ? 1 : 0)) * a.g + j) * kD8State;
+          *(f32x4*)(st + 4 + c4) = num;
+          if (c4 == 0) *(float2*)st = make_float2(M, den);
+        }
+      }
+      if (n_parts > 1) {
+        // ---- the last of the segment's workgroups merges their states, in list order
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) {
+          const int seen = atomicAdd(a.counters + wf, 1);
+          sm.last = seen == n_parts - 1;
+          if (seen == n_parts - 1) a.counters[wf] = 0;  // as the next call expects it
+        }
+        __syncthreads();
+        if (sm.last) {
+          __threadfence();
+          auto state = [&](int p, int head) {
+            return a.states + ((size_t)(2 * (wf + p) + (p == 0 ? 1 : 0)) * a.g + head) * kD8State;
+          };
+          if (j < a.g) {  // 32 threads a head: the largest maximum, the weights, the sum
+            float M = -INFINITY;
+            for (int p = tid & 31; p < n_parts; p += 32) M = fmaxf(M, state(p, j)[0]);
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
+            float den = 0.f;
+            for (int p = tid & 31; p < n_parts; p += 32) {
+              const float2 ml = *(const float2*)state(p, j);
+              const float wt = ml.x == M ? 1.f : fast_exp2(ml.x - M);
+              sm.w[j][p] = wt;
+              den += wt * ml.y;
+            }
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) den += __shfl_xor(den, o);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            f32x4 num = f32x4{};
+#pragma unroll 8
+            for (int p = 0; p < n_parts; ++p)
+              num += sm.w[j][p] * *(const f32x4*)(state(p, j) + 4 + c4);
+            bf16x4 r;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = (__bf16)(den == 0.f ? 0.f : num[i] / den);
+            *(bf16x4*)(a.o + o_at + (size_t)j * kHeadDim + c4) = r;
+          }
+        }
+      }
+      __syncthreads();  // the merge area and the list are free again
+    }
+    // ---- the next segment
+    pos = end + kD8SegCost;
+    if (++h == a.c.Hkv) {
+      h = 0;
+      ++b;
     }
   }
 }
 
 // ---------------------------------------------------------------- launcher
-size_t decode8_workspace_bytes(int g) { return 4096 + (size_t)1024 * g * 528; }
+int cu_count();
+
+size_t decode8_workspace_bytes(int g) {
+  return kD8Counters * sizeof(int) + (size_t)2 * kD8MaxWg * g * kD8State * sizeof(float);
+}
+
+// list entries of a call: they must stay below 2^31
+long long decode8_entries(int B, int Hkv, int n) {
+  return (long long)B * Hkv * ((long long)n + kD8SegCost);
+}
 
 hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, const int32_t* kv_lens,
                           const int32_t* blocks, int n_select, uint16_t* o, const float2* table,
-                          int B, int Hq, int w_pre, int w0, void* /*ws*/, hipStream_t stream) {
-  Decode8Args a{c, q, kv_lens, blocks, o, table, B, Hq, Hq / c.Hkv, n_select, w_pre, w0,
+                          int B, int Hq, int w_pre, int w0, void* ws, hipStream_t stream) {
+  static_assert(kD8MaxWg <= kD8Counters, "a counter per workgroup");
+  Decode8Args a{c, q, kv_lens, blocks, o, table, (int*)ws, (float*)ws + kD8Counters, B, Hq,
+                Hq / c.Hkv, n_select, std::min(2 * cu_count(), kD8MaxWg), w_pre, w0,
                 1.4426950408889634f / sqrtf((float)kHeadDim)};
-  const long long wgs = (long long)B * c.Hkv;
-  if (wgs > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-  if (bifocal)
-    hipLaunchKernelGGL(decode8_kernel<true>, dim3((unsigned)wgs), dim3(256), 0, stream, a);
+  const dim3 grid(a.n_wg), block(kD8Threads);
+  if (bifocal && blocks != nullptr)
+    hipLaunchKernelGGL((decode8_kernel<true, true>), grid, block, 0, stream, a);
+  else if (bifocal)
+    hipLaunchKernelGGL((decode8_kernel<true, false>), grid, block, 0, stream, a);
+  else if (blocks != nullptr)
+    hipLaunchKernelGGL((decode8_kernel<false, true>), grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL(decode8_kernel<false>, dim3((unsigned)wgs), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((decode8_kernel<false, false>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
 

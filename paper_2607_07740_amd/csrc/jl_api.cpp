@@ -68,6 +68,7 @@ hipError_t launch_append8(const Cache8& c, const uint16_t* k, const uint16_t* v,
 hipError_t launch_read8(const Cache8& c, uint16_t* k, uint16_t* v, int B, int start, int n,
                         hipStream_t stream);
 size_t decode8_workspace_bytes(int g);
+long long decode8_entries(int B, int Hkv, int n);
 hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, const int32_t* kv_lens,
                           const int32_t* blocks, int n_select, uint16_t* o, const float2* table,
                           int B, int Hq, int w_pre, int w0, void* ws, hipStream_t stream);
@@ -681,10 +682,8 @@ int decode8_common(bool bifocal, const jl_cache8* cache, const int32_t* block_ta
   if (listed) {
     if (!aligned4(blocks)) return fail(JL_ERR_INVALID_ARG, "blocks must be non-null and aligned");
     if (n_select < 1) return fail(JL_ERR_INVALID_ARG, "n_select must be >= 1 (got %d)", n_select);
-    if ((long long)B * c.Hkv * n_select > 0x7fffffffLL)
-      return fail(JL_ERR_INVALID_ARG, "problem too large");
   }
-  if ((long long)B * c.Hkv * c.n_blocks > 0x7fffffffLL)
+  if (jl::decode8_entries(B, c.Hkv, std::max(c.n_blocks, listed ? n_select : 0)) > 0x7fffffffLL)
     return fail(JL_ERR_INVALID_ARG, "problem too large");
   const size_t need = jl::decode8_workspace_bytes(Hq / c.Hkv);
   if (ws == nullptr || ws_bytes < need)
