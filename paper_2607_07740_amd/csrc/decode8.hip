@@ -22,7 +22,7 @@ constexpr int kD8Waves = 4;
 constexpr int kD8Threads = 64 * kD8Waves;
 constexpr int kD8MaxWg = 512;    // workgroups of a call: workspaces are sized for as many
 constexpr int kD8List = 256;     // steps whose blocks are looked up at a time
-constexpr int kD8SegCost = 2;    // what a workgroup pays for a further segment, in steps
+constexpr int kD8SegCost = 6;    // what a workgroup pays for a further segment, in steps
 constexpr int kD8State = 132;    // floats of a state: m, l, pad, pad, O[128]
 constexpr float kD8Up = 15.f, kD8Down = 0x1p-15f;  // weights in fp16 are times 2^15
 constexpr int kD8Counters = 1024;  // at the front of the workspace (4096 bytes)
@@ -65,12 +65,66 @@ __device__ inline int range_at(const Segments& s, uint32_t x) {
   return (int)(x < head ? x / (s.q + 1) : s.r + (x - head) / s.q);
 }
 
+// floor(x / d) for a run-time d < 2^24 (make_fastdiv, whose 64-bit division is slow here,
+// by way of a double quotient that is corrected in integers).
+__device__ inline FastDiv make_fastdiv24(uint32_t d) {
+  FastDiv f;
+  f.d = d;
+  f.m = f.l = 0;
+  if (d <= 1) return f;
+  f.l = 32 - __builtin_clz(d - 1);
+  const uint32_t num = (1u << f.l) - d;
+  uint32_t m = (uint32_t)(4294967296.0 * (double)num / (double)d);
+  long long rem = ((long long)num << 32) - (long long)((unsigned long long)m * d);
+  if (rem < 0) {
+    --m;
+    rem += d;
+  }
+  if (rem >= (long long)d) ++m;
+  f.m = m + 1;
+  return f;
+}
+
+// A barrier for LDS alone: loads from memory stay in flight across it.
+__device__ inline void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 __device__ inline int len8(const Decode8Args& a, int b) {
   return min(max(a.kv_lens[b], 0), a.c.n_blocks * kBlk);
 }
 // list entries of a segment of sequence b
 __device__ inline int entries8(const Decode8Args& a, int b) {
   return (len8(a, b) + kBlk - 1) / kBlk + kD8SegCost;
+}
+
+// States pass between workgroups, and so between dies whose L2s know nothing of each
+// other: they are written through and read past the L2 (device scope, the sc1 bit),
+// with the writer's own wait before its arrival is counted.  A device-scope fence
+// instead writes the whole L2 back and empties it, in every workgroup: 145 us in place
+// of 57 for 131072 keys, 32/8 heads.
+typedef __amdgpu_buffer_rsrc_t buffer_t;
+constexpr int kDeviceScope = 16;  // sc1
+__device__ inline buffer_t make_buffer(const void* p, size_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)bytes, 0x00027000);
+}
+__device__ inline void put4(buffer_t r, uint32_t at, f32x4 x) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), r, at, 0, kDeviceScope);
+}
+__device__ inline f32x4 get4(buffer_t r, uint32_t at) {
+  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, kDeviceScope));
+}
+__device__ inline float2 get2(buffer_t r, uint32_t at) {
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, kDeviceScope);
+  return make_float2(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+// Byte offset of a state: a workgroup has one slot for the segment that came to it and one
+// for the segment that begins in it.
+__device__ inline uint32_t state_at(const Decode8Args& a, int w, bool begins, int head) {
+  return (uint32_t)((2 * w + (begins ? 1 : 0)) * a.g + head) * (kD8State * 4);
 }
 
 // Maximum over the lanes l, l ^ 16, l ^ 32, l ^ 48, by lane swaps in registers.
@@ -108,12 +162,17 @@ struct __attribute__((aligned(16))) Decode8Smem {
   int2 list[kD8List];                       // (block of the sequence or -1, block of the pools)
   union {
     float o[kD8Waves][16][kD8Row];          // the waves' states
-    float w[8][kD8MaxWg];                   // the weights of a segment's parts
+    struct {
+      float w[8][kD8MaxWg];                 // the parts' weights
+      float set_o[8][kD8Row];               // the sets' sums
+    };
   };
   float m[kD8Waves][16], l[kD8Waves][16];
-  float top[8][kD8Waves * 2];
-  unsigned long long sum[kD8Waves];
-  int last;
+  struct {
+    size_t o;   // where its output goes
+    int wf, n;  // its first workgroup, how many (0: no such segment)
+  } due[2];
+  int last[2];
 };
 
 // Workgroup w of four waves: its range's segments one after another; a wave takes every
@@ -138,45 +197,61 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
   const int i16 = lane & 15, g4 = lane >> 4;
   const int w = blockIdx.x;
 
-  // ---- offset rows, fp32 to fp16
-  for (int i = tid; i < kBlk * kHalf / 4; i += kD8Threads) {
-    const float4 x = ((const float4*)a.table)[2 * i], y = ((const float4*)a.table)[2 * i + 1];
-    const f16x8 h = {(_Float16)x.x, (_Float16)x.y, (_Float16)x.z, (_Float16)x.w,
-                     (_Float16)y.x, (_Float16)y.y, (_Float16)y.z, (_Float16)y.w};
-    *(f16x8*)(sm.tab + (i >> 4) * kD8TabRow + 16 * (i & 15)) = h;
-  }
+  // ---- offset rows: requested ahead of the lengths, converted behind them
+  float4 tab[8];
+#pragma unroll
+  for (int n = 0; n < 8; ++n)
+    tab[n] = ((const float4*)a.table)[2 * (tid + kD8Threads * (n >> 1)) + (n & 1)];
 
   // ---- this workgroup's range, and the sequence and head it begins in
-  Segments sg;
-  uint32_t pos;  // list entry of the current segment's first step
-  int b, h;
+  Segments sg = {};
+  uint32_t pos = 0;  // list entry of the current segment's first step
   uint32_t x0, x1;
-  if (LISTED) {
+  int b, h;
+  // Segments of one length, no more than workgroups: each gets the same number of them, and
+  // no workgroup works on two.
+  const int segs = a.B * a.c.Hkv;
+  const bool even = (LISTED || a.B == 1) && segs <= a.n_wg;
+  int first_wg = 0, parts = 0;
+  if (even) {
+    const int per = a.n_wg / segs;
+    const int seg = w / per;
+    if (seg >= segs) return;
+    b = seg / a.c.Hkv;
+    h = seg - b * a.c.Hkv;
+    const int n = LISTED ? a.n_select : (len8(a, 0) + kBlk - 1) / kBlk;
+    first_wg = seg * per;
+    parts = __builtin_amdgcn_readfirstlane(max(1, min(per, (n + kD8Waves - 1) / kD8Waves)));
+    x0 = (uint32_t)(w - first_wg);
+    if ((int)x0 >= parts) return;
+    x1 = UINT_MAX;
+  } else if (LISTED) {
     const uint32_t e = (uint32_t)(a.n_select + kD8SegCost);
-    make_ranges(sg, a.n_wg, e * (uint32_t)(a.B * a.c.Hkv));
+    make_ranges(sg, a.n_wg, e * (uint32_t)segs);
     if (w >= sg.n) return;
     x0 = range_start(sg, w);
     const uint32_t seg = x0 / e;
     b = (int)(seg / (uint32_t)a.c.Hkv);
     h = (int)(seg - (uint32_t)b * a.c.Hkv);
     pos = seg * e;
+    x1 = range_start(sg, (uint32_t)w + 1);
   } else {
     // all lengths, 64 at a time; every wave for itself
-    uint32_t V = 0;
+    uint32_t V = 0, v = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-      uint32_t v = b0 + lane < a.B ? (uint32_t)entries8(a, b0 + lane) * a.c.Hkv : 0;
+      v = b0 + lane < a.B ? (uint32_t)entries8(a, b0 + lane) * a.c.Hkv : 0;
+      uint32_t t = v;
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-      V += v;
+      for (int o = 1; o < 64; o <<= 1) t += __shfl_xor(t, o);
+      V += t;
     }
     make_ranges(sg, a.n_wg, __builtin_amdgcn_readfirstlane(V));
     if (w >= sg.n) return;
     x0 = range_start(sg, w);
     uint32_t before = 0;
     b = 0;
-    pos = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-      const uint32_t v = b0 + lane < a.B ? (uint32_t)entries8(a, b0 + lane) * a.c.Hkv : 0;
+      if (a.B > 64) v = b0 + lane < a.B ? (uint32_t)entries8(a, b0 + lane) * a.c.Hkv : 0;
       uint32_t incl = v;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
@@ -197,30 +272,58 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
     const uint32_t e = (uint32_t)entries8(a, b);
     h = (int)((x0 - pos) / e);
     pos += (uint32_t)h * e;
+    x1 = range_start(sg, (uint32_t)w + 1);
   }
-  x1 = range_start(sg, (uint32_t)w + 1);
   h = __builtin_amdgcn_readfirstlane(h);
-  __syncthreads();  // the offset rows
+  pos = __builtin_amdgcn_readfirstlane(pos);
+
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const int i = tid + kD8Threads * n;  // four pairs of row i / 16
+    const float4 x = tab[2 * n], y = tab[2 * n + 1];
+    const f16x8 t = {(_Float16)x.x, (_Float16)x.y, (_Float16)x.z, (_Float16)x.w,
+                     (_Float16)y.x, (_Float16)y.y, (_Float16)y.z, (_Float16)y.w};
+    *(f16x8*)(sm.tab + (i >> 4) * kD8TabRow + 16 * (i & 15)) = t;
+  }
 
   // query columns: col = (view, head); the distances q - k that a column keeps are
   // [keep_lo, keep_lo + keep_n) as one unsigned compare (none for unused columns)
   const int view = i16 >> 3, hj = i16 & 7;
   const bool col_on = hj < a.g && (BIFOCAL || view == 0);
 
+  const buffer_t states =
+      make_buffer(a.states, (size_t)2 * kD8MaxWg * a.g * kD8State * sizeof(float));
+  bool shared = false;  // some segment is shared with other workgroups
+  if (tid < 2) sm.due[tid].n = 0;
+
   for (; pos < x1 && b < a.B;) {
     const int kv_len = __builtin_amdgcn_readfirstlane(len8(a, b));
     const int n_real = LISTED ? a.n_select : (kv_len + kBlk - 1) / kBlk;
+    // this workgroup's steps of the segment
     const uint32_t end = pos + (uint32_t)n_real;
-    const uint32_t from = max(x0, pos);
-    const int off = (int)(from - pos);
-    const int n_steps = (int)min(x1, end) - (int)from;  // of this segment, here
+    int off, n_steps;
+    if (even) {
+      const int q = n_real / parts, r = n_real - q * parts;
+      off = q * (int)x0 + min((int)x0, r);
+      n_steps = q + ((int)x0 < r ? 1 : 0);
+    } else {
+      const uint32_t from = max(x0, pos);
+      off = (int)(from - pos);
+      n_steps = (int)min(x1, end) - (int)from;
+    }
     const size_t o_at = ((size_t)b * a.Hq + h * a.g) * kHeadDim;
-    if (n_real == 0 && pos >= x0) {  // a sequence without keys
+    if (n_real == 0 && (even || pos >= x0)) {  // a sequence without keys
       for (int i = tid; i < a.g * kHeadDim / 8; i += kD8Threads) ((u32x4*)(a.o + o_at))[i] = u32x4{};
     }
     if (n_steps > 0) {
-      const int G = BIFOCAL ? group_size(max(kv_len, 1), a.w_pre) : 1;
-      const FastDiv gdiv = make_fastdiv((uint32_t)G);
+      u32x4 qraw[4];
+      {
+        const uint16_t* qrow = a.q + o_at + (size_t)min(hj, a.g - 1) * kHeadDim + 8 * g4;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) qraw[u] = load16(qrow + 32 * u);
+      }
+      const int G = BIFOCAL ? max(1, (int)((uint32_t)(kv_len - 1) / (uint32_t)a.w_pre) + 1) : 1;
+      const FastDiv gdiv = make_fastdiv24((uint32_t)G);
       const int w0 = G > 1 ? a.w0 : INT_MAX;  // one view only where f is the identity
       const int qpos = max(kv_len - 1, 0);
       const int fq = (int)fastdiv((uint32_t)qpos, gdiv);
@@ -229,35 +332,15 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
                               : view == 0 ? (uint32_t)w0 + 1u
                                           : (uint32_t)INT_MAX - (uint32_t)w0;
 
-      // ---- the column's query in fp32, pairs 32 u + 8 g4 + j, scaled by log2(e) / sqrt(d) and
-      // by the power of two that brings its largest value to [1, 2)
-      float qlo[16], qhi[16];
-      float q_back;  // what undoes the latter
-      {
-        const uint16_t* qrow = a.q + o_at + (size_t)min(hj, a.g - 1) * kHeadDim + 8 * g4;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          unpack8(load16(qrow + 32 * u), qlo + 8 * u);
-          unpack8(load16(qrow + 64 + 32 * u), qhi + 8 * u);
-        }
-        float top = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, fmaxf(fabsf(qlo[i]), fabsf(qhi[i])));
-        top = max_over_groups(top);
-        const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
-        const float down = pow2f(-e);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          qlo[i] = qlo[i] * down * a.q_scale;
-          qhi[i] = qhi[i] * down * a.q_scale;
-        }
-        q_back = pow2f(e);
-      }
-
       f32x4 acc[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) acc[i] = f32x4{};
       float m_run = -INFINITY, l_run = 0.f;
+
+      // the column's query in fp32, pairs 32 u + 8 g4 + j, scaled by log2(e) / sqrt(d) and by
+      // the power of two that brings its largest value to [1, 2)
+      float qlo[16], qhi[16];
+      float q_back;  // what undoes the latter
 
       // the step in hand; its K registers take the next step's as soon as the scores are
       // formed, its V registers when the product is
@@ -265,8 +348,15 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
       float ks, vs;
       int k0;         // first position of the step's block, below 0: nothing to do
       int k0n, phys;  // of the step that is loaded
-      auto look_up = [&](int i) __attribute__((always_inline)) {
-        const int2 at = sm.list[i];
+      // (position, block of the pools) of the i-th step; (-1, 0) where there is nothing to do
+      auto find = [&](int i) __attribute__((always_inline)) {
+        int blk = off + i;
+        if (LISTED) blk = a.blocks[((size_t)b * a.c.Hkv + h) * a.n_select + blk];
+        if (blk < 0 || blk >= a.c.n_blocks || blk * kBlk >= kv_len) return make_int2(-1, 0);
+        const int page = min(max(page_of(a.c, b, blk), 0), a.c.n_pages - 1);
+        return make_int2(blk * kBlk, pool_block(a.c, page, h, in_page(a.c, blk)));
+      };
+      auto set_step = [&](int2 at) __attribute__((always_inline)) {
         k0n = __builtin_amdgcn_readfirstlane(at.x);
         phys = __builtin_amdgcn_readfirstlane(at.y);
       };
@@ -284,7 +374,7 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
       };
       auto load_v = [&]() __attribute__((always_inline)) {
         const unsigned char* vp = a.c.v + (size_t)phys * kBlkBytes;
-        vs = a.c.v_scale[phys] * kD8Down;
+        vs = a.c.v_scale[phys];
 #pragma unroll
         for (int n = 0; n < 8; ++n)
           vx[n] = __builtin_nontemporal_load((const u32x4*)(vp + 1024 * n + 16 * lane));
@@ -398,73 +488,105 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
       auto values = [&]() __attribute__((always_inline)) {
         // ---- O += scale V^T P^T; where the sequence ends inside the block the values behind
         // its end are zeroed, since 0 times what lies there may be NaN
-        const bool tail = k0 + kBlk > kv_len;
+        if (k0 + kBlk > kv_len) {
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              const int left = kv_len - (k0 + 32 * hf + 16 * t + 4 * g4);
+              const uint32_t keep = left >= 4 ? ~0u : left > 0 ? (1u << (8 * left)) - 1 : 0u;
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                vx[4 * hf + c][t] &= keep;
+                vx[4 * hf + c][2 + t] &= keep;
+              }
+            }
+        }
+        const float up = vs * kD8Down;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          u32x4 x[2] = {vx[c], vx[4 + c]};
-          if (tail) {
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-              for (int t = 0; t < 2; ++t) {
-                const int left = kv_len - (k0 + 32 * hf + 16 * t + 4 * g4);
-                const uint32_t keep = left >= 4 ? ~0u : left > 0 ? (1u << (8 * left)) - 1 : 0u;
-                x[hf][t] &= keep;
-                x[hf][2 + t] &= keep;
-              }
-          }
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             f32x4 d = f32x4{};
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-              const f16x2 v0 = e4m3_f16<false>(x[hf][2 * e]), v1 = e4m3_f16<true>(x[hf][2 * e]);
-              const f16x2 v2 = e4m3_f16<false>(x[hf][2 * e + 1]), v3 = e4m3_f16<true>(x[hf][2 * e + 1]);
+              const u32x4 x = vx[4 * hf + c];
+              const f16x2 v0 = e4m3_f16<false>(x[2 * e]), v1 = e4m3_f16<true>(x[2 * e]);
+              const f16x2 v2 = e4m3_f16<false>(x[2 * e + 1]), v3 = e4m3_f16<true>(x[2 * e + 1]);
               const f16x8 v = {v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
               d = mfma16h(v, p[hf], d);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              acc[2 * c + e][i] = __builtin_fmaf(d[i], vs, acc[2 * c + e][i]);
+              acc[2 * c + e][i] = __builtin_fmaf(d[i], up, acc[2 * c + e][i]);
           }
         }
       };
 
-      // ---- the steps, kD8List at a time
-      for (int s0 = 0; s0 < n_steps; s0 += kD8List) {
-        const int n = min(n_steps - s0, kD8List);
-        if (s0 > 0) __syncthreads();  // the list is read
-        for (int i = tid; i < n; i += kD8Threads) {
-          int blk = off + s0 + i;
-          if (LISTED) blk = a.blocks[((size_t)b * a.c.Hkv + h) * a.n_select + blk];
-          if (blk < 0 || blk >= a.c.n_blocks || blk * kBlk >= kv_len) {
-            sm.list[i] = make_int2(-1, 0);
-          } else {
-            const int page = min(max(page_of(a.c, b, blk), 0), a.c.n_pages - 1);
-            sm.list[i] = make_int2(blk * kBlk, pool_block(a.c, page, h, in_page(a.c, blk)));
-          }
-        }
-        __syncthreads();
+      // ---- the steps, kD8List at a time: their blocks are looked up, a wave's first one ahead
+      // of the list
+      static_assert(kD8List <= kD8Threads, "a step per thread");
+      auto begin = [&](int s0, int n) __attribute__((always_inline)) {
+        int2 mine = make_int2(-1, 0);
+        if (tid < n) mine = find(s0 + tid);
         if (wave < n) {
-          look_up(wave);
+          set_step(find(s0 + wave));
           load_k();
           load_v();
         }
-        for (int i = wave; i < n; i += kD8Waves) {
-          const bool more = i + kD8Waves < n;
+        if (tid < n) sm.list[tid] = mine;
+      };
+      int s0 = 0, n = min(n_steps, kD8List);
+      begin(s0, n);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        unpack8(qraw[u], qlo + 8 * u);
+        unpack8(qraw[2 + u], qhi + 8 * u);
+      }
+      {
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, fmaxf(fabsf(qlo[i]), fabsf(qhi[i])));
+        top = max_over_groups(top);
+        const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
+        const float down = pow2f(-e);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          qlo[i] = qlo[i] * down * a.q_scale;
+          qhi[i] = qhi[i] * down * a.q_scale;
+        }
+        q_back = pow2f(e);
+      }
+      lds_barrier();
+      for (;;) {
+        // the last step stands apart: where loads may or may not be in flight, every wait is
+        // for the path with fewer, which drains the pipeline
+        int i = wave;
+        for (; i + kD8Waves < n; i += kD8Waves) {
           k0 = k0n;
-          if (k0 >= 0) scores();
+          const bool on = !LISTED || k0 >= 0;
+          if (on) scores();
           const float ks_now = ks;
-          if (more) {
-            look_up(i + kD8Waves);
-            load_k();
-          }
-          if (k0 >= 0) {
+          set_step(sm.list[i + kD8Waves]);
+          load_k();
+          if (on) {
             softmax(ks_now);
             values();
           }
-          if (more) load_v();
+          load_v();
         }
+        k0 = k0n;
+        if (i < n && (!LISTED || k0 >= 0)) {
+          scores();
+          softmax(ks);
+          values();
+        }
+        s0 += kD8List;
+        if (s0 >= n_steps) break;
+        __syncthreads();  // the list is read
+        n = min(n_steps - s0, kD8List);
+        begin(s0, n);
+        lds_barrier();
       }
 
       // ---- the waves' states, and the two views of a head, into one (max-shifted)
@@ -477,8 +599,8 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
         sm.l[wave][i16] = l_run * kD8Down;
       }
       __syncthreads();
-      const int wf = range_at(sg, pos), wl = range_at(sg, end - 1);
-      const int n_parts = wl - wf + 1;
+      const int wf = even ? first_wg : range_at(sg, pos);
+      const int n_parts = even ? parts : range_at(sg, end - 1) - wf + 1;
       const int j = tid >> 5, c4 = 4 * (tid & 31);  // head and channels of this thread
       if (j < a.g) {
         float M = -INFINITY;
@@ -500,61 +622,105 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
           for (int i = 0; i < 4; ++i) r[i] = (__bf16)(den == 0.f ? 0.f : num[i] / den);
           *(bf16x4*)(a.o + o_at + (size_t)j * kHeadDim + c4) = r;
         } else {
-          float* st = a.states + ((size_t)(2 * w + (w == wf ? 1 : 0)) * a.g + j) * kD8State;
-          *(f32x4*)(st + 4 + c4) = num;
-          if (c4 == 0) *(float2*)st = make_float2(M, den);
+          const uint32_t at = state_at(a, w, w == wf, j);
+          put4(states, at + 16 + 4 * c4, num);
+          if (c4 == 0) put4(states, at, f32x4{M, den, 0.f, 0.f});
         }
       }
       if (n_parts > 1) {
-        // ---- the last of the segment's workgroups merges their states, in list order
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) {
-          const int seen = atomicAdd(a.counters + wf, 1);
-          sm.last = seen == n_parts - 1;
-          if (seen == n_parts - 1) a.counters[wf] = 0;  // as the next call expects it
-        }
-        __syncthreads();
-        if (sm.last) {
-          __threadfence();
-          auto state = [&](int p, int head) {
-            return a.states + ((size_t)(2 * (wf + p) + (p == 0 ? 1 : 0)) * a.g + head) * kD8State;
-          };
-          if (j < a.g) {  // 32 threads a head: the largest maximum, the weights, the sum
-            float M = -INFINITY;
-            for (int p = tid & 31; p < n_parts; p += 32) M = fmaxf(M, state(p, j)[0]);
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
-            float den = 0.f;
-            for (int p = tid & 31; p < n_parts; p += 32) {
-              const float2 ml = *(const float2*)state(p, j);
-              const float wt = ml.x == M ? 1.f : fast_exp2(ml.x - M);
-              sm.w[j][p] = wt;
-              den += wt * ml.y;
-            }
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) den += __shfl_xor(den, o);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            f32x4 num = f32x4{};
-#pragma unroll 8
-            for (int p = 0; p < n_parts; ++p)
-              num += sm.w[j][p] * *(const f32x4*)(state(p, j) + 4 + c4);
-            bf16x4 r;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = (__bf16)(den == 0.f ? 0.f : num[i] / den);
-            *(bf16x4*)(a.o + o_at + (size_t)j * kHeadDim + c4) = r;
-          }
-        }
+        shared = true;
+        if (tid == 0) sm.due[w == wf ? 1 : 0] = {o_at, wf, n_parts};
       }
       __syncthreads();  // the merge area and the list are free again
     }
+    if (even) break;
     // ---- the next segment
     pos = end + kD8SegCost;
     if (++h == a.c.Hkv) {
       h = 0;
       ++b;
     }
+  }
+
+  // ---- segments that this workgroup shares with others, two at most: the last of a
+  // segment's workgroups merges the states, in list order
+  if (!shared) return;
+  wait_vmem();  // this wave's states have arrived
+  __syncthreads();
+  if (tid < 2) {
+    bool last = false;
+    if (sm.due[tid].n > 0) {
+      int* counter = a.counters + sm.due[tid].wf;
+      last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+             sm.due[tid].n - 1;
+      if (last) *counter = 0;  // as the next call expects it
+    }
+    sm.last[tid] = last;
+  }
+  __syncthreads();
+  const int j = tid >> 5, l32 = tid & 31, c4 = 4 * l32;
+  // sets of 32 g threads: a thread has four channels of a head, a set every n_sets-th part
+  const int n_sets = kD8Threads / (32 * a.g);
+  const int set = j / a.g, head = j - set * a.g;
+  for (int slot = 0; slot < 2; ++slot) {
+    if (!sm.last[slot]) continue;
+    const int n = __builtin_amdgcn_readfirstlane(sm.due[slot].n);
+    const int wf = __builtin_amdgcn_readfirstlane(sm.due[slot].wf);
+    auto state = [&](int p) { return state_at(a, wf + p, p == 0, head); };
+    f32x4 num = f32x4{};
+    float den = 0.f;
+    // the maxima and a batch of states are requested together; the weights are formed while
+    // the states are under way
+    auto merge = [&]() __attribute__((always_inline)) {
+      constexpr int kBatch = 8;
+      f32x4 x[kBatch];
+      auto request = [&](int p0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+          x[i] = get4(states, state(min(p0 + i * n_sets, n - 1)) + 16 + 4 * c4);
+      };
+      const float2 ml0 = get2(states, state(min(l32, n - 1)));
+      const float2 ml1 = get2(states, state(min(l32 + 32, n - 1)));
+      request(set);
+      float M = fmaxf(ml0.x, ml1.x);
+      for (int p = l32 + 64; p < n; p += 32) M = fmaxf(M, get2(states, state(p)).x);
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
+      for (int p = l32; p < n; p += 32) {
+        float2 e = p == l32 ? ml0 : ml1;
+        if (p >= l32 + 64) e = get2(states, state(p));
+        const float wt = e.x == M ? 1.f : fast_exp2(e.x - M);
+        sm.w[j][p] = wt;
+        den += wt * e.y;
+      }
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) den += __shfl_xor(den, o);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      for (int p0 = set;;) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const int p = p0 + i * n_sets;
+          if (p < n) num += sm.w[j][p] * x[i];
+        }
+        p0 += kBatch * n_sets;
+        if (p0 >= n) break;
+        request(p0);
+      }
+    };
+    if (set < n_sets) {
+      merge();
+      *(f32x4*)&sm.set_o[j][c4] = num;
+    }
+    __syncthreads();
+    if (j < a.g) {
+      for (int t = 1; t < n_sets; ++t) num += *(const f32x4*)&sm.set_o[j + t * a.g][c4];
+      bf16x4 r;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = (__bf16)(den == 0.f ? 0.f : num[i] / den);
+      *(bf16x4*)(a.o + sm.due[slot].o + (size_t)j * kHeadDim + c4) = r;
+    }
+    __syncthreads();  // the sums are read
   }
 }
 
