@@ -1,5 +1,7 @@
 // blocks8.hip -- which blocks of an 8-bit cache a query attends to: a score per
 // block from its mean key, and the choice of the largest.
+#include <algorithm>
+
 #include "cache8.h"
 
 namespace jl {
@@ -11,65 +13,131 @@ struct ScoresArgs {
   float* scores;  // [B][Hkv][n_blocks]
   const float2* table;
   int B, Hq, g;
+  int n_tiles, n_runs, n_hgroups;  // tiles of 16 blocks, waves that share them, groups of 4 heads
   int w_pre;
   float q_scale;
 };
 
+constexpr int kScoreHeads = 4;  // kv heads of a workgroup: one wave each, on the same blocks
+
+// 16 pairs (x_f, x_{f+64}), f = 16 g4 .. 16 g4 + 15, of a bf16 row, rotated by the
+// cos/sin row's pairs, in fp32.
+struct Pairs {
+  float lo[16], hi[16];
+};
+__device__ inline void load_pairs(const uint16_t* row, int g4, u32x4* raw) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    raw[i] = load16(row + 16 * g4 + 8 * i);
+    raw[2 + i] = load16(row + kHalf + 16 * g4 + 8 * i);
+  }
+}
+__device__ inline void load_turns(const float2* table, int pos, int g4, float4* cs) {
+  const float4* row = (const float4*)(table + (size_t)pos * kHalf) + 8 * g4;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) cs[i] = row[i];
+}
+__device__ inline void rotate_pairs(const u32x4* raw, const float4* cs, Pairs& y) {
+  float lo[16], hi[16];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    unpack8(raw[i], lo + 8 * i);
+    unpack8(raw[2 + i], hi + 8 * i);
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float c = i & 1 ? cs[i / 2].z : cs[i / 2].x, s = i & 1 ? cs[i / 2].w : cs[i / 2].y;
+    y.lo[i] = lo[i] * c - hi[i] * s;
+    y.hi[i] = hi[i] * c + lo[i] * s;
+  }
+}
+
+// Maximum over the 8 lanes that share lane / 8, NaN above all.
+__device__ inline float max_of_8(float x) {
+  auto pick = [](float a, float b) { return a != a || b != b ? NAN : fmaxf(a, b); };
+#define JL_DPP(v, ctrl)                                                                       \
+  __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), ctrl, 0xf, \
+                                                        0xf, false))
+  x = pick(x, JL_DPP(x, 0xB1));   // lane ^ 1
+  x = pick(x, JL_DPP(x, 0x4E));   // lane ^ 2
+  x = pick(x, JL_DPP(x, 0x141));  // 7 - lane, inside 8
+#undef JL_DPP
+  return x;
+}
+
 // score[b][h][j] = max over the group's heads of <R(f(q)) x_q, R(f(64 j + 31)) mean_j>
 // / sqrt(d): what the block's middle key would score in the remote view if it were the
 // mean.  Blocks past the sequence get -inf.
+//
+// A wave takes 16 blocks of one kv head at a time: means and queries are rotated in
+// fp32 and meet in the fp32 matrix instruction (16 blocks x 16 columns, 4 channels
+// each time), so nothing is rounded to fewer bits.  The four waves of a workgroup read
+// the same cos/sin rows, 512 bytes a block beside its mean's 256, which then come
+// from the L1.  Bound by the chain length -> page -> mean at one sequence, and by the
+// rows' traffic at many.
 template <bool BIFOCAL>
-__global__ __launch_bounds__(256) void block_scores_kernel(ScoresArgs a) {
-  __shared__ float sq[8][kHeadDim];
-  const int tid = threadIdx.x;
-  const int n_wg = (a.c.n_blocks + 255) / 256;
-  const int bh = blockIdx.x / n_wg, part = blockIdx.x - bh * n_wg;
-  const int b = bh / a.c.Hkv, h = bh - b * a.c.Hkv;
+__global__ __launch_bounds__(64 * kScoreHeads) void block_scores_kernel(ScoresArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i16 = lane & 15, g4 = lane >> 4;
+  int w = blockIdx.x;
+  const int run = w % a.n_runs;
+  w /= a.n_runs;
+  const int hg = w % a.n_hgroups, b = w / a.n_hgroups;
+  const int h = hg * kScoreHeads + wave;
+  if (h >= a.c.Hkv) return;
   const int kv_len = min(max(a.kv_lens[b], 0), a.c.n_blocks * kBlk);
+  const int n_live = (kv_len + kBlk - 1) / kBlk;
   const int qpos = max(kv_len - 1, 0);
-  const FastDiv gdiv = make_fastdiv(BIFOCAL ? group_size(max(kv_len, 1), a.w_pre) : 1);
-  for (int i = tid; i < a.g * kHalf; i += 256) {
-    const int j = i >> 6, f = i & 63;
-    const uint16_t* q = a.q + ((size_t)b * a.Hq + h * a.g + j) * kHeadDim;
-    const float lo = __uint_as_float((uint32_t)q[f] << 16) * a.q_scale;
-    const float hi = __uint_as_float((uint32_t)q[f + 64] << 16) * a.q_scale;
-    const float2 cs = a.table[(size_t)remote_pos(qpos, gdiv) * kHalf + f];
-    sq[j][f] = lo * cs.x - hi * cs.y;
-    sq[j][f + 64] = hi * cs.x + lo * cs.y;
-  }
-  __syncthreads();
-  const int blk = part * 256 + tid;
-  if (blk >= a.c.n_blocks) return;
-  float best = -INFINITY;
-  if (blk * kBlk < kv_len) {
+  const uint32_t G = BIFOCAL ? max(1u, (uint32_t)qpos / (uint32_t)a.w_pre + 1) : 1u;
+  float* out = a.scores + ((size_t)b * a.c.Hkv + h) * a.c.n_blocks;
+
+  // ---- a tile's raw operands: requested a tile ahead
+  u32x4 raw[4];
+  float4 cs[8];
+  auto request = [&](int t) __attribute__((always_inline)) {
+    const int blk = min(16 * t + i16, max(n_live - 1, 0));
     const int page = min(max(page_of(a.c, b, blk), 0), a.c.n_pages - 1);
-    const uint16_t* mean =
-        a.c.k_mean + (size_t)pool_block(a.c, page, h, in_page(a.c, blk)) * kHeadDim;
-    const int mid = remote_pos(blk * kBlk + kBlk / 2 - 1, gdiv);
-    float sc[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sc[j] = 0.f;
-    for (int f = 0; f < kHalf; ++f) {
-      const float x = __uint_as_float((uint32_t)mean[f] << 16);
-      const float y = __uint_as_float((uint32_t)mean[f + 64] << 16);
-      const float2 cs = a.table[(size_t)mid * kHalf + f];
-      const float lo = x * cs.x - y * cs.y, hi = y * cs.x + x * cs.y;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < a.g) sc[j] += lo * sq[j][f] + hi * sq[j][f + 64];
-    }
-    bool nan = false;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (j >= a.g) continue;
-      best = fmaxf(best, sc[j]);
-      nan |= sc[j] != sc[j];
-    }
-    if (nan) best = NAN;
+    load_pairs(a.c.k_mean + (size_t)pool_block(a.c, page, h, in_page(a.c, blk)) * kHeadDim, g4, raw);
+    const uint32_t mid = (uint32_t)(blk * kBlk + kBlk / 2 - 1);
+    load_turns(a.table, (int)(BIFOCAL ? mid / G : mid), g4, cs);
+  };
+  int t = run;
+  if (16 * t < n_live) request(t);
+  Pairs q;
+  {
+    u32x4 qraw[4];
+    float4 qcs[8];
+    load_pairs(a.q + ((size_t)b * a.Hq + h * a.g + min(i16, a.g - 1)) * kHeadDim, g4, qraw);
+    load_turns(a.table, (int)(BIFOCAL ? (uint32_t)qpos / G : (uint32_t)qpos), g4, qcs);
+    rotate_pairs(qraw, qcs, q);
   }
-  a.scores[(size_t)bh * a.c.n_blocks + blk] = best;
+  for (; t < a.n_tiles; t += a.n_runs) {
+    f32x4 sc = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if (16 * t < n_live) {  // wave-uniform
+      Pairs m;
+      rotate_pairs(raw, cs, m);
+      if (16 * (t + a.n_runs) < n_live) request(t + a.n_runs);
+      f32x4 s0 = f32x4{}, s1 = f32x4{};
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(m.lo[i], q.lo[i], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(m.hi[i], q.hi[i], s1, 0, 0, 0);
+      }
+      // lane: column i16 (head), blocks 4 g4 + i; columns past the group repeat its last head
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = max_of_8((s0[i] + s1[i]) * a.q_scale);
+        sc[i] = 16 * t + 4 * g4 + i < n_live ? x : -INFINITY;
+      }
+    }
+    const int blk = 16 * t + 4 * g4 + (i16 & 3);
+    const float x = i16 == 0 ? sc[0] : i16 == 1 ? sc[1] : i16 == 2 ? sc[2] : sc[3];
+    if (i16 < 4 && blk < a.c.n_blocks) out[blk] = x;
+  }
 }
 
+// ------------------------------------------------------------------ choice
 struct SelectArgs {
   const float* scores;  // [B][Hkv][n_blocks]
   const int32_t* kv_lens;
@@ -84,68 +152,136 @@ __device__ inline uint32_t order_of(float x) {
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
-// Workgroup = one row.  The blocks that are always chosen count as the largest
-// number; the n-th largest number is found bit by bit.
-__global__ __launch_bounds__(256) void select_blocks_kernel(SelectArgs a) {
-  __shared__ int s_n[4];
-  const int tid = threadIdx.x, wave = tid >> 6;
+constexpr int kSelThreads = 512;
+
+// Workgroup = one row.  The blocks that are always chosen count as the largest number.
+// The want-th largest number is found eight bits at a time from counts of that digit
+// among the numbers that share the digits so far; then one scan in index order gives
+// every chosen block its place, the numbers equal to the last one in turn until the
+// list is full.  Every wave reads the counts for itself: one barrier a digit.
+// R: numbers a thread holds; a row of more than 512 R is read anew for each digit.
+// Latency-bound.
+template <int R>
+__global__ __launch_bounds__(kSelThreads) void select_blocks_kernel(SelectArgs a) {
+  __shared__ __attribute__((aligned(16))) int hist[4][256];
+  __shared__ unsigned long long s_sum[kSelThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b = blockIdx.x / a.Hkv;
   const int kv_len = max(a.kv_lens[b], 0);
   const int nb = (int)min((long long)a.n_blocks, ((long long)kv_len + kBlk - 1) / kBlk);
   const float* row = a.scores + (size_t)blockIdx.x * a.n_blocks;
   int32_t* out = a.blocks + (size_t)blockIdx.x * a.n_select;
-  auto value = [&](int j) {
-    const bool always = j < a.n_first || (long long)j * kBlk + kBlk - 1 >= (long long)kv_len - 1 - a.w0;
-    return always ? 0xffffffffu : order_of(row[j]);
-  };
-  auto total = [&](int n) {
-    for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o);
-    __syncthreads();
-    if ((tid & 63) == 0) s_n[wave] = n;
-    __syncthreads();
-    return s_n[0] + s_n[1] + s_n[2] + s_n[3];
-  };
   const int want = min(a.n_select, nb);
-  uint32_t cut = 0;  // the largest number that at least `want` blocks reach
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t t = cut | (1u << bit);
-    int n = 0;
-    for (int j = tid; j < nb; j += 256) n += value(j) >= t ? 1 : 0;
-    if (total(n) >= want) cut = t;
+  for (int i = want + tid; i < a.n_select; i += kSelThreads) out[i] = -1;
+  if (nb <= a.n_select) {
+    for (int i = tid; i < nb; i += kSelThreads) out[i] = i;
+    return;
   }
-  int above = 0;
-  for (int j = tid; j < nb; j += 256) above += value(j) > cut ? 1 : 0;
-  above = total(above);
-  if (tid < 64) {  // one wave writes the list in order
-    int n = 0, ties = want - above;
-    for (int j0 = 0; j0 < nb; j0 += 64) {
-      const int j = j0 + tid;
-      const uint32_t x = j < nb ? value(j) : 0;
-      const bool tie = j < nb && x == cut;
-      const unsigned long long below = (1ull << tid) - 1;
-      const unsigned long long mt = __ballot(tie);
-      const bool take = j < nb && (x > cut || (tie && __popcll(mt & below) < ties));
-      const unsigned long long mk = __ballot(take);
-      if (take) out[n + __popcll(mk & below)] = j;
-      n += __popcll(mk);
-      ties -= min(ties, (int)__popcll(mt));
+  // the first block that holds a key of the band
+  const long long first_key = (long long)kv_len - 1 - a.w0;
+  const int band = (int)min((long long)nb, first_key > 0 ? first_key / kBlk : 0LL);
+  uint32_t x[R];
+  auto load = [&](int j0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int j = j0 + tid * R + i;
+      const float s = row[min(j, nb - 1)];
+      x[i] = j < a.n_first || j >= band ? 0xffffffffu : order_of(s);
+      if (j >= nb) x[i] = 0;  // below every score
     }
-    for (int i = n + tid; i < a.n_select; i += 64) out[i] = -1;
+  };
+  const int tile = kSelThreads * R;
+  load(0);
+  for (int i = tid; i < 4 * 256; i += kSelThreads) (&hist[0][0])[i] = 0;
+  __syncthreads();
+  uint32_t cut = 0;  // the digits of the want-th largest number so far
+  int left = want;   // its place among the numbers that share them
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    const int shift = 24 - 8 * d;
+    for (int j0 = 0; j0 < nb; j0 += tile) {
+      if (nb > tile) load(j0);
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (j0 + tid * R + i < nb && (d == 0 || (x[i] ^ cut) >> (shift + 8 * (d > 0)) == 0))
+          atomicAdd(&hist[d][(x[i] >> shift) & 255], 1);
+    }
+    __syncthreads();
+    // counts of this lane's four digits, and how many numbers have a larger one
+    const int4 n = *(const int4*)&hist[d][4 * lane];
+    int above = n.x + n.y + n.z + n.w;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_down(above, o);
+      if (lane + o < 64) above += y;
+    }
+    above -= n.x + n.y + n.z + n.w;
+    const int c3 = above + n.w, c2 = c3 + n.z, c1 = c2 + n.y, c0 = c1 + n.x;
+    const bool mine = above < left && left <= c0;
+    const int digit = left <= c3 ? 3 : left <= c2 ? 2 : left <= c1 ? 1 : 0;
+    const int over = digit == 3 ? above : digit == 2 ? c3 : digit == 1 ? c2 : c1;
+    const int at = __ffsll(__ballot(mine)) - 1;
+    cut |= (uint32_t)__shfl(4 * lane + digit, at) << shift;
+    left -= __shfl(over, at);
+  }
+  // ---- places: `left` numbers equal to cut are taken, in index order
+  unsigned long long before = 0;  // taken so far and, in the upper word, equal ones so far
+  for (int j0 = 0; j0 < nb; j0 += tile) {
+    if (nb > tile) load(j0);
+    uint32_t n_more = 0, n_same = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const bool in = j0 + tid * R + i < nb;
+      n_more += in && x[i] > cut;
+      n_same += in && x[i] == cut;
+    }
+    unsigned long long sum = (unsigned long long)n_same << 32 | n_more;
+    const unsigned long long own = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const unsigned long long y = __shfl_up(sum, o);
+      if (lane >= o) sum += y;
+    }
+    __syncthreads();
+    if (lane == 63) s_sum[wave] = sum;
+    __syncthreads();
+    unsigned long long at = before + sum - own;
+#pragma unroll
+    for (int i = 0; i < kSelThreads / 64; ++i) {
+      if (i < wave) at += s_sum[i];
+      before += s_sum[i];
+    }
+    int more = (int)(uint32_t)at, same = (int)(at >> 32);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int j = j0 + tid * R + i;
+      if (j >= nb) continue;
+      if (x[i] > cut) out[more++ + min(same, left)] = j;
+      if (x[i] == cut && same++ < left) out[more + same - 1] = j;
+    }
   }
 }
 
 // ---------------------------------------------------------------- launchers
+int cu_count();
+
 hipError_t launch_block_scores8(bool bifocal, const Cache8& c, const uint16_t* q,
                                 const int32_t* kv_lens, float* scores, const float2* table, int B,
                                 int Hq, int w_pre, hipStream_t stream) {
-  ScoresArgs a{c, q, kv_lens, scores, table, B, Hq, Hq / c.Hkv, w_pre,
+  ScoresArgs a{c, q, kv_lens, scores, table, B, Hq, Hq / c.Hkv, 0, 0, 0, w_pre,
                1.f / sqrtf((float)kHeadDim)};
-  const long long wgs = (long long)B * c.Hkv * ((c.n_blocks + 255) / 256);
+  a.n_tiles = (c.n_blocks + 15) / 16;
+  a.n_hgroups = (c.Hkv + kScoreHeads - 1) / kScoreHeads;
+  // about two workgroups per CU; a wave rotates its query once for all of its tiles
+  const long long rows = (long long)B * a.n_hgroups;
+  a.n_runs = (int)std::max(1LL, std::min<long long>(a.n_tiles, (2LL * cu_count() + rows - 1) / rows));
+  const long long wgs = rows * a.n_runs;
   if (wgs > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)wgs), block(64 * kScoreHeads);
   if (bifocal)
-    hipLaunchKernelGGL(block_scores_kernel<true>, dim3((unsigned)wgs), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(block_scores_kernel<true>, grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL(block_scores_kernel<false>, dim3((unsigned)wgs), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(block_scores_kernel<false>, grid, block, 0, stream, a);
   return hipGetLastError();
 }
 
@@ -153,7 +289,11 @@ hipError_t launch_select_blocks(const float* scores, const int32_t* kv_lens, int
                                 int B, int Hkv, int n_blocks, int n_select, int w0, int n_first,
                                 hipStream_t stream) {
   SelectArgs a{scores, kv_lens, blocks, Hkv, n_blocks, n_select, w0, n_first};
-  hipLaunchKernelGGL(select_blocks_kernel, dim3((unsigned)B * Hkv), dim3(256), 0, stream, a);
+  const dim3 grid((unsigned)(B * Hkv)), block(kSelThreads);
+  if (n_blocks <= 4 * kSelThreads)
+    hipLaunchKernelGGL(select_blocks_kernel<4>, grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL(select_blocks_kernel<16>, grid, block, 0, stream, a);
   return hipGetLastError();
 }
 
