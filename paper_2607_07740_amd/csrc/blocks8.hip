@@ -20,35 +20,30 @@ struct ScoresArgs {
 
 constexpr int kScoreHeads = 4;  // kv heads of a workgroup: one wave each, on the same blocks
 
-// 16 pairs (x_f, x_{f+64}), f = 16 g4 .. 16 g4 + 15, of a bf16 row, rotated by the
-// cos/sin row's pairs, in fp32.
+// The 16 pairs (x_f, x_{f+64}) of lane group g4: f = 8 g4 + j and 32 + 8 g4 + j, j < 8.
 struct Pairs {
   float lo[16], hi[16];
 };
 __device__ inline void load_pairs(const uint16_t* row, int g4, u32x4* raw) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    raw[i] = load16(row + 16 * g4 + 8 * i);
-    raw[2 + i] = load16(row + kHalf + 16 * g4 + 8 * i);
-  }
+  for (int i = 0; i < 4; ++i) raw[i] = load16(row + 32 * i + 8 * g4);
 }
-__device__ inline void load_turns(const float2* table, int pos, int g4, float4* cs) {
-  const float4* row = (const float4*)(table + (size_t)pos * kHalf) + 8 * g4;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) cs[i] = row[i];
-}
-__device__ inline void rotate_pairs(const u32x4* raw, const float4* cs, Pairs& y) {
-  float lo[16], hi[16];
+// ... rotated by the row's cos/sin pairs, in fp32
+__device__ inline void rotate_pairs(const u32x4* raw, const float2* cs_row, int g4, Pairs& y) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    unpack8(raw[i], lo + 8 * i);
-    unpack8(raw[2 + i], hi + 8 * i);
-  }
+    float lo[8], hi[8];
+    unpack8(raw[i], lo);
+    unpack8(raw[2 + i], hi);
+    const float4* cs = (const float4*)(cs_row + 32 * i + 8 * g4);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float c = i & 1 ? cs[i / 2].z : cs[i / 2].x, s = i & 1 ? cs[i / 2].w : cs[i / 2].y;
-    y.lo[i] = lo[i] * c - hi[i] * s;
-    y.hi[i] = hi[i] * c + lo[i] * s;
+    for (int j = 0; j < 8; j += 2) {
+      const float4 c = cs[j / 2];
+      y.lo[8 * i + j] = lo[j] * c.x - hi[j] * c.y;
+      y.hi[8 * i + j] = hi[j] * c.x + lo[j] * c.y;
+      y.lo[8 * i + j + 1] = lo[j + 1] * c.z - hi[j + 1] * c.w;
+      y.hi[8 * i + j + 1] = hi[j + 1] * c.z + lo[j + 1] * c.w;
+    }
   }
 }
 
@@ -71,53 +66,71 @@ __device__ inline float max_of_8(float x) {
 //
 // A wave takes 16 blocks of one kv head at a time: means and queries are rotated in
 // fp32 and meet in the fp32 matrix instruction (16 blocks x 16 columns, 4 channels
-// each time), so nothing is rounded to fewer bits.  The four waves of a workgroup read
-// the same cos/sin rows, 512 bytes a block beside its mean's 256, which then come
-// from the L1.  Bound by the chain length -> page -> mean at one sequence, and by the
-// rows' traffic at many.
+// each time), so nothing is rounded to fewer bits.  The four waves of a workgroup, of
+// four heads, share the blocks' cos/sin rows, 512 bytes a block beside its mean's 256,
+// through LDS; means and rows are requested one tile ahead, page indices two.  Bound by
+// the chain length -> page -> mean at one sequence (131072 tokens, 32/8 heads: 4.3 us, 2.4 of
+// them an empty launch) and by that latency a tile at many (8 of 32K to 128K, 64/8 heads:
+// 12 us for 21 MB of means; rows through each wave's own loads took 17).
+constexpr int kScoreRow = kHalf + 2;  // float2s of a row in LDS: rows start 4 banks apart
 template <bool BIFOCAL>
 __global__ __launch_bounds__(64 * kScoreHeads) void block_scores_kernel(ScoresArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ __attribute__((aligned(16))) float2 rows[2][16][kScoreRow];
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, g4 = lane >> 4;
   int w = blockIdx.x;
   const int run = w % a.n_runs;
   w /= a.n_runs;
   const int hg = w % a.n_hgroups, b = w / a.n_hgroups;
-  const int h = hg * kScoreHeads + wave;
-  if (h >= a.c.Hkv) return;
+  const bool on = hg * kScoreHeads + wave < a.c.Hkv;
+  const int h = min(hg * kScoreHeads + wave, a.c.Hkv - 1);
   const int kv_len = min(max(a.kv_lens[b], 0), a.c.n_blocks * kBlk);
   const int n_live = (kv_len + kBlk - 1) / kBlk;
   const int qpos = max(kv_len - 1, 0);
   const uint32_t G = BIFOCAL ? max(1u, (uint32_t)qpos / (uint32_t)a.w_pre + 1) : 1u;
   float* out = a.scores + ((size_t)b * a.c.Hkv + h) * a.c.n_blocks;
 
-  // ---- a tile's raw operands: requested a tile ahead
+  auto block_of = [&](int t, int i) { return min(16 * t + i, max(n_live - 1, 0)); };
+  // this thread's half of the cos/sin row of block tid / 16 of a tile
+  u32x4 cs0, cs1;
+  auto request_rows = [&](int t) __attribute__((always_inline)) {
+    const uint32_t mid = (uint32_t)(block_of(t, tid >> 4) * kBlk + kBlk / 2 - 1);
+    const u32x4* row = (const u32x4*)(a.table + (size_t)(BIFOCAL ? mid / G : mid) * kHalf);
+    cs0 = row[tid & 15];
+    cs1 = row[16 + (tid & 15)];
+  };
   u32x4 raw[4];
-  float4 cs[8];
-  auto request = [&](int t) __attribute__((always_inline)) {
-    const int blk = min(16 * t + i16, max(n_live - 1, 0));
-    const int page = min(max(page_of(a.c, b, blk), 0), a.c.n_pages - 1);
+  auto request_mean = [&](int t, int page) __attribute__((always_inline)) {
+    const int blk = block_of(t, i16);
+    page = min(max(page, 0), a.c.n_pages - 1);
     load_pairs(a.c.k_mean + (size_t)pool_block(a.c, page, h, in_page(a.c, blk)) * kHeadDim, g4, raw);
-    const uint32_t mid = (uint32_t)(blk * kBlk + kBlk / 2 - 1);
-    load_turns(a.table, (int)(BIFOCAL ? mid / G : mid), g4, cs);
   };
   int t = run;
-  if (16 * t < n_live) request(t);
+  int page = page_of(a.c, b, block_of(t, i16));
+  request_rows(t);
+  int page_next = page_of(a.c, b, block_of(t + a.n_runs, i16));
   Pairs q;
   {
     u32x4 qraw[4];
-    float4 qcs[8];
     load_pairs(a.q + ((size_t)b * a.Hq + h * a.g + min(i16, a.g - 1)) * kHeadDim, g4, qraw);
-    load_turns(a.table, (int)(BIFOCAL ? (uint32_t)qpos / G : (uint32_t)qpos), g4, qcs);
-    rotate_pairs(qraw, qcs, q);
+    request_mean(t, page);
+    rotate_pairs(qraw, a.table + (size_t)(BIFOCAL ? (uint32_t)qpos / G : (uint32_t)qpos) * kHalf,
+                 g4, q);
   }
-  for (; t < a.n_tiles; t += a.n_runs) {
+  for (int n = 0; t < a.n_tiles; t += a.n_runs, ++n) {
     f32x4 sc = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    if (16 * t < n_live) {  // wave-uniform
+    if (16 * t < n_live) {  // the same for the whole workgroup
+      u32x4* dst = (u32x4*)rows[n & 1][tid >> 4];
+      dst[tid & 15] = cs0;
+      dst[16 + (tid & 15)] = cs1;
+      __syncthreads();  // one is enough: the other buffer was read in front of it
       Pairs m;
-      rotate_pairs(raw, cs, m);
-      if (16 * (t + a.n_runs) < n_live) request(t + a.n_runs);
+      rotate_pairs(raw, rows[n & 1][i16], g4, m);
+      request_rows(t + a.n_runs);  // past the end: the last block's again
+      request_mean(t + a.n_runs, page_next);
+      page_next = page_of(a.c, b, block_of(t + 2 * a.n_runs, i16));
       f32x4 s0 = f32x4{}, s1 = f32x4{};
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -133,7 +146,7 @@ __global__ __launch_bounds__(64 * kScoreHeads) void block_scores_kernel(ScoresAr
     }
     const int blk = 16 * t + 4 * g4 + (i16 & 3);
     const float x = i16 == 0 ? sc[0] : i16 == 1 ? sc[1] : i16 == 2 ? sc[2] : sc[3];
-    if (i16 < 4 && blk < a.c.n_blocks) out[blk] = x;
+    if (on && i16 < 4 && blk < a.c.n_blocks) out[blk] = x;
   }
 }
 
