@@ -567,7 +567,7 @@ class Cache8:
                 _dev(k_mean, "k_mean", torch.bfloat16, blocks + (D,), k.device)]
         self.k, self.v, self.k_scale, self.v_scale, self.k_mean = k, v, k_scale, v_scale, k_mean
         self.n_pages, self.page_size, self.Hkv, self.head_dim = n_pages, page_size, Hkv, D
-        self.device = k.device
+        self.device, self.index = k.device, k.get_device()
         self._struct = _Cache8Struct(*ptrs, n_pages, page_size, Hkv, D)
         self._ref = ctypes.cast(ctypes.pointer(self._struct), ctypes.c_void_p)
 
@@ -591,15 +591,44 @@ class _On:
     neither their fill nor their reuse crosses streams."""
 
     def __init__(self, stream):
-        self.ctx = None if stream is None else _t().cuda.stream(stream)
+        self.ctx = _t().cuda.stream(stream)
 
     def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
+        self.ctx.__enter__()
 
     def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
+        self.ctx.__exit__(*exc)
+
+
+def _new(like, stream, shape, dtype, fill=False):
+    """An output (or a zeroed workspace) of a call on `stream`."""
+    if stream is not None:
+        with _On(stream):
+            return like.new_zeros(shape, dtype=dtype) if fill else like.new_empty(shape, dtype=dtype)
+    return like.new_zeros(shape, dtype=dtype) if fill else like.new_empty(shape, dtype=dtype)
+
+
+def _on8(t, name, dtype, shape, index, device):
+    """_dev for a tensor of a call on device `index`: the common case in one test (a small
+    call's time on the host is a third of these checks), the error from _dev."""
+    try:
+        if (t.dtype is dtype and t.get_device() == index and t.is_contiguous()
+                and (shape is None or t.shape == shape)):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    return _dev(t, name, dtype, shape, device)
+
+
+def _current(index, device, name) -> None:
+    """The library launches on the current device."""
+    torch = _t()
+    try:
+        now = torch._C._cuda_getDevice()
+    except AttributeError:
+        now = torch.cuda.current_device()
+    if index != now:
+        raise ValueError("%s is on %s, the current device is cuda:%d" % (name, device, now))
 
 
 def _is_cache8(cache) -> None:
@@ -608,48 +637,48 @@ def _is_cache8(cache) -> None:
 
 
 def _query8(q, cache):
-    """(B, Hq, 128) of a query over an 8-bit cache."""
+    """(B, Hq, pointer) of a query over an 8-bit cache."""
     _is_cache8(cache)
-    if q.dim() != 3 or q.shape[2] != cache.head_dim:
+    ptr = _on8(q, "q", _t().bfloat16, None, cache.index, cache.device)
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != cache.head_dim:
         raise ValueError("q must be [B, Hq, %d]" % cache.head_dim)
-    return q.shape
+    return shape[0], shape[1], ptr
 
 
 def _cache8(cache, block_table, B):
     """The checks of a call of B sequences on a cache -> (jl_cache8 pointer, table pointer,
     max_pages, capacity)."""
-    torch = _t()
-    # the library launches on the current device
-    if cache.device.index != torch.cuda.current_device():
-        raise ValueError("cache is on %s, the current device is cuda:%d"
-                         % (cache.device, torch.cuda.current_device()))
+    _current(cache.index, cache.device, "cache")
     if block_table is None:
         if B > cache.n_pages:
             raise ValueError("a dense cache of %d sequences cannot hold %d" % (cache.n_pages, B))
         return cache._ref, None, 0, cache.page_size
+    table = _on8(block_table, "block_table", _t().int32, None, cache.index, cache.device)
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError("block_table must be [B, max_pages]")
     max_pages = block_table.shape[1]
-    return (cache._ref, _dev(block_table, "block_table", torch.int32, None, cache.device),
-            max_pages, max_pages * cache.page_size)
+    return cache._ref, table, max_pages, max_pages * cache.page_size
 
 
 def _ints(t, name, cache, shape):
-    return _dev(t, name, _t().int32, shape, cache.device)
+    return _on8(t, name, _t().int32, shape, cache.index, cache.device)
 
 
 def cache8_append(cache, k, v, starts, *, n_new=None, block_table=None, stream=None) -> None:
     """jl_cache8_append: rows k, v [B, n, Hkv, 128] bf16 to positions starts[b] .. of sequence
     b (starts int32 [B]); n_new int32 [B]: only the first n_new[b] of them."""
-    torch = _t()
     _is_cache8(cache)
-    if k.dim() != 4 or k.shape[2:] != (cache.Hkv, cache.head_dim):
+    bf16 = _t().bfloat16
+    kp = _on8(k, "k", bf16, None, cache.index, cache.device)
+    shape = k.shape
+    if len(shape) != 4 or shape[2] != cache.Hkv or shape[3] != cache.head_dim:
         raise ValueError("k and v must be [B, n, %d, %d]" % (cache.Hkv, cache.head_dim))
-    B, n = k.shape[:2]
+    B, n = shape[0], shape[1]
     ref, table, max_pages, _ = _cache8(cache, block_table, B)
     _check(lib().jl_cache8_append(
-        ref, table, max_pages, _dev(k, "k", torch.bfloat16, None, cache.device),
-        _dev(v, "v", torch.bfloat16, k.shape, cache.device), _ints(starts, "starts", cache, (B,)),
+        ref, table, max_pages, kp, _on8(v, "v", bf16, shape, cache.index, cache.device),
+        _ints(starts, "starts", cache, (B,)),
         None if n_new is None else _ints(n_new, "n_new", cache, (B,)), B, n, _stream(stream)))
 
 
@@ -657,21 +686,21 @@ def cache8_read(cache, n: int, *, start: int = 0, B=None, block_table=None, k_ou
                 stream=None):
     """jl_cache8_read: rows start .. start + n - 1 of every sequence as bf16 (k, v), each
     [B, n, Hkv, 128].  B: sequences of a dense cache, all of them if not given."""
-    torch = _t()
     _is_cache8(cache)
+    bf16 = _t().bfloat16
     if B is None:
         B = cache.n_pages if block_table is None else block_table.shape[0]
+    ref, table, max_pages, cap = _cache8(cache, block_table, B)
+    start, n = int(start), int(n)
     shape = (B, n, cache.Hkv, cache.head_dim)
-    ref, table, max_pages, _ = _cache8(cache, block_table, B)
-    with _On(stream):
+    if (k_out is None or v_out is None) and 0 < n <= cap:  # the library refuses other lengths
         if k_out is None:
-            k_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+            k_out = _new(cache.k_mean, stream, shape, bf16)
         if v_out is None:
-            v_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
-    _check(lib().jl_cache8_read(
-        ref, table, max_pages, _dev(k_out, "k_out", torch.bfloat16, shape, cache.device),
-        _dev(v_out, "v_out", torch.bfloat16, shape, cache.device), B, int(start), int(n),
-        _stream(stream)))
+            v_out = _new(cache.k_mean, stream, shape, bf16)
+    kp, vp = (None if t is None else _on8(t, name, bf16, shape, cache.index, cache.device)
+              for t, name in ((k_out, "k_out"), (v_out, "v_out")))
+    _check(lib().jl_cache8_read(ref, table, max_pages, kp, vp, B, start, n, _stream(stream)))
     return k_out, v_out
 
 
@@ -690,30 +719,33 @@ def decode8_workspace(Hq: int, Hkv: int, *, head_dim: int = 128, device="cuda"):
 def _decode8(q, cache, kv_lens, blocks, w_pretrained, w_local, rope_theta, bifocal, block_table,
              out, workspace, stream):
     torch = _t()
-    B, Hq, D = _query8(q, cache)
+    B, Hq, qp = _query8(q, cache)
     ref, table, max_pages, _ = _cache8(cache, block_table, B)
-    if out is None or workspace is None:
-        with _On(stream):
-            if out is None:
-                out = torch.empty_like(q)
-            if workspace is None:
-                workspace = torch.zeros(max(decode8_workspace_bytes(Hq, cache.Hkv, D), 16),
-                                        dtype=torch.uint8, device=q.device)
-    args = [ref, table, max_pages, _dev(q, "q", torch.bfloat16, None, cache.device),
-            _ints(kv_lens, "kv_lens", cache, (B,))]
-    name = "decode8"
-    if blocks is not None:
-        name = "decode8_blocks"
-        if blocks.dim() != 3 or blocks.shape[:2] != (B, cache.Hkv):
-            raise ValueError("blocks must be [B, Hkv, n_select]")
-        args += [_ints(blocks, "blocks", cache, None), blocks.shape[2]]
-    args += [_dev(out, "out", torch.bfloat16, q.shape, cache.device), B, Hq, float(rope_theta)]
-    ws = [_dev(workspace, "workspace", None, None, cache.device),
-          workspace.numel() * workspace.element_size(), _stream(stream)]
-    if bifocal:
-        _check(getattr(lib(), "jl_bifocal_" + name)(*args, int(w_pretrained), int(w_local), *ws))
+    if out is None:
+        out = _new(q, stream, q.shape, torch.bfloat16)
+        op = out.data_ptr()
     else:
-        _check(getattr(lib(), "jl_rope_attention_" + name)(*args, *ws))
+        op = _on8(out, "out", torch.bfloat16, q.shape, cache.index, cache.device)
+    if workspace is None:
+        need = decode8_workspace_bytes(Hq, cache.Hkv, cache.head_dim)
+        workspace = _new(q, stream, (max(need, 16),), torch.uint8, fill=True)
+    wp = _on8(workspace, "workspace", getattr(workspace, "dtype", None), None, cache.index, cache.device)
+    w_bytes = workspace.numel() * workspace.element_size()
+    lens = _ints(kv_lens, "kv_lens", cache, (B,))
+    L = lib()
+    if blocks is None:
+        args = (ref, table, max_pages, qp, lens, op, B, Hq, float(rope_theta))
+        call = L.jl_bifocal_decode8 if bifocal else L.jl_rope_attention_decode8
+    else:
+        bp = _ints(blocks, "blocks", cache, None)
+        if blocks.dim() != 3 or blocks.shape[0] != B or blocks.shape[1] != cache.Hkv:
+            raise ValueError("blocks must be [B, Hkv, n_select]")
+        args = (ref, table, max_pages, qp, lens, bp, blocks.shape[2], op, B, Hq, float(rope_theta))
+        call = L.jl_bifocal_decode8_blocks if bifocal else L.jl_rope_attention_decode8_blocks
+    if bifocal:
+        _check(call(*args, int(w_pretrained), int(w_local), wp, w_bytes, _stream(stream)))
+    else:
+        _check(call(*args, wp, w_bytes, _stream(stream)))
     return out
 
 
@@ -743,15 +775,16 @@ def block_scores8(q, cache, kv_lens, *, w_pretrained: int = 1, rope_theta: float
     """jl_bifocal_block_scores8 / jl_rope_block_scores8: fp32 [B, Hkv, capacity // 64], the score
     of every block's mean key, -inf past the sequence."""
     torch = _t()
-    B, Hq, _ = _query8(q, cache)
+    B, Hq, qp = _query8(q, cache)
     ref, table, max_pages, cap = _cache8(cache, block_table, B)
     shape = (B, cache.Hkv, cap // BLOCK8)
     if out is None:
-        with _On(stream):
-            out = torch.empty(shape, dtype=torch.float32, device=q.device)
-    args = [ref, table, max_pages, _dev(q, "q", torch.bfloat16, None, cache.device),
-            _ints(kv_lens, "kv_lens", cache, (B,)),
-            _dev(out, "out", torch.float32, shape, cache.device), B, Hq, float(rope_theta)]
+        out = _new(q, stream, shape, torch.float32)
+        op = out.data_ptr()
+    else:
+        op = _on8(out, "out", torch.float32, shape, cache.index, cache.device)
+    args = (ref, table, max_pages, qp, _ints(kv_lens, "kv_lens", cache, (B,)), op, B, Hq,
+            float(rope_theta))
     if bifocal:
         _check(lib().jl_bifocal_block_scores8(*args, int(w_pretrained), _stream(stream)))
     else:
@@ -765,21 +798,23 @@ def select_blocks(scores, kv_lens, n_select: int, *, w_local: int, n_first: int 
     n_first blocks and those of the local band always, then the largest scores; ascending,
     -1 behind the last."""
     torch = _t()
+    ptr = _dev(scores, "scores", torch.float32)
     if scores.dim() != 3:
         raise ValueError("scores must be [B, Hkv, n_blocks]")
     B, Hkv, n_blocks = scores.shape
-    if scores.is_cuda and scores.device.index != torch.cuda.current_device():
-        raise ValueError("scores are on %s, the current device is cuda:%d"
-                         % (scores.device, torch.cuda.current_device()))
-    shape = (B, Hkv, int(n_select))
-    ptr = _dev(scores, "scores", torch.float32)
+    index, device = scores.get_device(), scores.device
+    _current(index, device, "scores")
+    n_select = int(n_select)
     if out is None:
-        with _On(stream):
-            out = torch.empty(shape, dtype=torch.int32, device=scores.device)
+        if n_select < 1:
+            raise ValueError("n_select must be >= 1")
+        out = _new(scores, stream, (B, Hkv, n_select), torch.int32)
+        op = out.data_ptr()
+    else:
+        op = _on8(out, "out", torch.int32, (B, Hkv, n_select), index, device)
     _check(lib().jl_select_blocks(
-        ptr, _dev(kv_lens, "kv_lens", torch.int32, (B,), scores.device),
-        _dev(out, "out", torch.int32, shape, scores.device), B, Hkv, n_blocks, int(n_select),
-        int(w_local), int(n_first), _stream(stream)))
+        ptr, _on8(kv_lens, "kv_lens", torch.int32, (B,), index, device), op, B, Hkv, n_blocks,
+        n_select, int(w_local), int(n_first), _stream(stream)))
     return out
 
 
