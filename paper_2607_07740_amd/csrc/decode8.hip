@@ -18,10 +18,7 @@ namespace jl {
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kD8Waves = 4;
-constexpr int kD8Threads = 64 * kD8Waves;
 constexpr int kD8MaxWg = 512;    // workgroups of a call: workspaces are sized for as many
-constexpr int kD8List = 256;     // steps whose blocks are looked up at a time
 constexpr int kD8SegCost = 6;    // what a workgroup pays for a further segment, in steps
 constexpr int kD8State = 132;    // floats of a state: m, l, pad, pad, O[128]
 constexpr float kD8Up = 15.f, kD8Down = 0x1p-15f;  // weights in fp16 are times 2^15
@@ -34,6 +31,7 @@ struct Decode8Args {
   const int32_t* blocks;  // [B][Hkv][n_select], or nullptr: every block
   uint16_t* o;
   const float2* table;
+  const unsigned char* offsets;  // kD8TabBytes: see offset_rows_kernel
   int* counters;
   float* states;  // [2 n_wg][g][kD8State]
   int B, Hq, g, n_select;
@@ -46,14 +44,14 @@ struct Decode8Args {
 // ranges.  Two workgroups that share a segment meet in its counter: the first's
 // index names it, since only a range's last segment goes on in the next range.
 struct Segments {
-  uint32_t V, q, r;  // entries; per range, and ranges (the first ones) with one more
+  uint32_t q, r;  // entries per range, and ranges (the first ones) with one more
   int n;             // ranges
 };
 
-__device__ inline void make_ranges(Segments& s, int n_wg, uint32_t V) {
-  s.V = V;
+__device__ inline void make_ranges(Segments& s, int n_wg, int waves, uint32_t V) {
   // no range shorter than one step per wave and the cost of its segment
-  s.n = (int)min((uint32_t)n_wg, (V + kD8Waves + kD8SegCost - 1) / (kD8Waves + kD8SegCost));
+  const uint32_t least = (uint32_t)(waves + kD8SegCost);
+  s.n = (int)min((uint32_t)n_wg, (V + least - 1) / least);
   s.q = V / (uint32_t)s.n;
   s.r = V - s.q * (uint32_t)s.n;
 }
@@ -154,20 +152,43 @@ __device__ inline f16x2 rotate_pair(f16x2 x, f16x2 cs) {
 }
 
 constexpr int kD8TabRow = kHalf * 4 + 16;  // 64 fp16 (cos, sin) and 16 bytes, so that rows start 4 banks apart
+constexpr int kD8TabBytes = kBlk * kD8TabRow;
+static_assert(kD8TabBytes % 1024 == 0, "copied in pieces of 1 KB");
 constexpr int kD8Row = kHeadDim + 4;       // floats of a merge row
 
-struct __attribute__((aligned(16))) Decode8Smem {
-  unsigned char tab[kBlk * kD8TabRow];      // (cos, sin)(t omega_i), t < 64
+// The first 64 rows of a cos/sin table in fp16, as the decode kernel keeps them in LDS.
+__global__ void offset_rows_kernel(const float2* table, unsigned char* out) {
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i >= kD8TabBytes / 4) return;
+  const int r = i / (kD8TabRow / 4), f = i - r * (kD8TabRow / 4);
+  f16x2 h = {(_Float16)0.f, (_Float16)0.f};
+  if (f < kHalf) {
+    const float2 cs = table[r * kHalf + f];
+    h = f16x2{(_Float16)cs.x, (_Float16)cs.y};
+  }
+  ((f16x2*)out)[i] = h;
+}
+
+// What a call's workgroups share out: the steps of a batch's sequences, those of one
+// sequence, or lists of blocks.
+enum Decode8Mode : int { kBatch8 = 0, kOne8 = 1, kListed8 = 2 };
+// Waves of a workgroup.  One sequence: eight and a workgroup per CU leave half the states
+// to merge, which one workgroup per kv head reads at a CU's own rate (131072 keys, 32/8
+// heads: 54.6 -> 51.3 us; 32768 21.6 -> 19.4; 1999 keys, 16/8 heads 11.6 -> 11.8).
+// Otherwise four, two workgroups per CU, one of which streams while the other merges
+// (256 sequences of 0.2K to 2K: 124 -> 111 us; 128 listed blocks 14.6 -> 14.2).
+__host__ __device__ constexpr int decode8_waves(int mode) { return mode == kOne8 ? 8 : 4; }
+
+template <int kD8Waves>
+struct __attribute__((aligned(1024))) Decode8Smem {
+  unsigned char tab[kD8TabBytes];           // (cos, sin)(t omega_i), t < 64
   float2 rows[kD8Waves][2][kHalf];          // a step's (cos, sin) rows that rotate its query
-  int2 list[kD8List];                       // (block of the sequence or -1, block of the pools)
   union {
     float o[kD8Waves][16][kD8Row];          // the waves' states
-    struct {
-      float w[8][kD8MaxWg];                 // the parts' weights
-      float set_o[8][kD8Row];               // the sets' sums
-    };
+    float set_o[2 * kD8Waves][kD8Row];                 // the sums of the last workgroup's sets of threads
   };
   float m[kD8Waves][16], l[kD8Waves][16];
+  float set_m[2 * kD8Waves], set_l[2 * kD8Waves];
   struct {
     size_t o;   // where its output goes
     int wf, n;  // its first workgroup, how many (0: no such segment)
@@ -175,8 +196,8 @@ struct __attribute__((aligned(16))) Decode8Smem {
   int last[2];
 };
 
-// Workgroup w of four waves: its range's segments one after another; a wave takes every
-// fourth step of 64 keys and keeps the 16 columns' states in registers.
+// Workgroup w: its range's segments one after another; each of its waves takes every
+// fourth (eighth) step of 64 keys and keeps the 16 columns' states in registers.
 //
 // A step is 16 KB, K and V, that go from memory into registers, 16 bytes a lane and
 // 1 KB an instruction, one step ahead; the layout is the matrix operands' own.
@@ -188,20 +209,21 @@ struct __attribute__((aligned(16))) Decode8Smem {
 // it is: e4m3 numbers are exact in fp16, and with |x| <= 448 none overflows.  The
 // block's scale of K multiplies the scores, that of V the step's product.
 // The query is brought to [1, 2) by a power of two first, its own range aside.
-template <bool BIFOCAL, bool LISTED>
-__global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
-  __shared__ Decode8Smem sm;
+template <bool BIFOCAL, int MODE>
+__global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(Decode8Args a) {
+  constexpr int kD8Waves = decode8_waves(MODE);
+  constexpr int kD8Threads = 64 * kD8Waves;
+  constexpr bool LISTED = MODE == kListed8;
+  __shared__ Decode8Smem<kD8Waves> sm;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, g4 = lane >> 4;
   const int w = blockIdx.x;
 
-  // ---- offset rows: requested ahead of the lengths, converted behind them
-  float4 tab[8];
-#pragma unroll
-  for (int n = 0; n < 8; ++n)
-    tab[n] = ((const float4*)a.table)[2 * (tid + kD8Threads * (n >> 1)) + (n & 1)];
+  // ---- offset rows, straight into LDS
+  for (int n = wave; n < kD8TabBytes / 1024; n += kD8Waves)
+    dma16_s(a.offsets, 1024 * n + 16 * lane, lds_addr(sm.tab) + 1024 * n);
 
   // ---- this workgroup's range, and the sequence and head it begins in
   Segments sg = {};
@@ -211,7 +233,7 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
   // Segments of one length, no more than workgroups: each gets the same number of them, and
   // no workgroup works on two.
   const int segs = a.B * a.c.Hkv;
-  const bool even = (LISTED || a.B == 1) && segs <= a.n_wg;
+  const bool even = MODE == kOne8 || (LISTED && segs <= a.n_wg);
   int first_wg = 0, parts = 0;
   if (even) {
     const int per = a.n_wg / segs;
@@ -227,7 +249,7 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
     x1 = UINT_MAX;
   } else if (LISTED) {
     const uint32_t e = (uint32_t)(a.n_select + kD8SegCost);
-    make_ranges(sg, a.n_wg, e * (uint32_t)segs);
+    make_ranges(sg, a.n_wg, kD8Waves, e * (uint32_t)segs);
     if (w >= sg.n) return;
     x0 = range_start(sg, w);
     const uint32_t seg = x0 / e;
@@ -245,7 +267,7 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
       for (int o = 1; o < 64; o <<= 1) t += __shfl_xor(t, o);
       V += t;
     }
-    make_ranges(sg, a.n_wg, __builtin_amdgcn_readfirstlane(V));
+    make_ranges(sg, a.n_wg, kD8Waves, __builtin_amdgcn_readfirstlane(V));
     if (w >= sg.n) return;
     x0 = range_start(sg, w);
     uint32_t before = 0;
@@ -277,15 +299,6 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
   h = __builtin_amdgcn_readfirstlane(h);
   pos = __builtin_amdgcn_readfirstlane(pos);
 
-#pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    const int i = tid + kD8Threads * n;  // four pairs of row i / 16
-    const float4 x = tab[2 * n], y = tab[2 * n + 1];
-    const f16x8 t = {(_Float16)x.x, (_Float16)x.y, (_Float16)x.z, (_Float16)x.w,
-                     (_Float16)y.x, (_Float16)y.y, (_Float16)y.z, (_Float16)y.w};
-    *(f16x8*)(sm.tab + (i >> 4) * kD8TabRow + 16 * (i & 15)) = t;
-  }
-
   // query columns: col = (view, head); the distances q - k that a column keeps are
   // [keep_lo, keep_lo + keep_n) as one unsigned compare (none for unused columns)
   const int view = i16 >> 3, hj = i16 & 7;
@@ -295,6 +308,8 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
       make_buffer(a.states, (size_t)2 * kD8MaxWg * a.g * kD8State * sizeof(float));
   bool shared = false;  // some segment is shared with other workgroups
   if (tid < 2) sm.due[tid].n = 0;
+  wait_vmem();  // the offset rows have landed, in every wave
+  __syncthreads();
 
   for (; pos < x1 && b < a.B;) {
     const int kv_len = __builtin_amdgcn_readfirstlane(len8(a, b));
@@ -322,7 +337,7 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) qraw[u] = load16(qrow + 32 * u);
       }
-      const int G = BIFOCAL ? max(1, (int)((uint32_t)(kv_len - 1) / (uint32_t)a.w_pre) + 1) : 1;
+      const int G = BIFOCAL ? (int)((uint32_t)max(kv_len - 1, 0) / (uint32_t)a.w_pre) + 1 : 1;
       const FastDiv gdiv = make_fastdiv24((uint32_t)G);
       const int w0 = G > 1 ? a.w0 : INT_MAX;  // one view only where f is the identity
       const int qpos = max(kv_len - 1, 0);
@@ -348,20 +363,33 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
       float ks, vs;
       int k0;         // first position of the step's block, below 0: nothing to do
       int k0n, phys;  // of the step that is loaded
-      // (position, block of the pools) of the i-th step; (-1, 0) where there is nothing to do
-      auto find = [&](int i) __attribute__((always_inline)) {
-        int blk = off + i;
-        if (LISTED) blk = a.blocks[((size_t)b * a.c.Hkv + h) * a.n_select + blk];
-        if (blk < 0 || blk >= a.c.n_blocks || blk * kBlk >= kv_len) return make_int2(-1, 0);
-        const int page = min(max(page_of(a.c, b, blk), 0), a.c.n_pages - 1);
-        return make_int2(blk * kBlk, pool_block(a.c, page, h, in_page(a.c, blk)));
+      // Lane l holds this wave's l-th step of 64: its position (-1 where there is nothing to do)
+      // and its block of the pools.
+      int at_k0, at_phys;
+      auto look_up = [&](int first) __attribute__((always_inline)) {
+        const int i = first + kD8Waves * lane;
+        at_k0 = -1;
+        at_phys = 0;
+        if (i < n_steps) {
+          int blk = off + i;
+          if (LISTED) blk = a.blocks[((size_t)b * a.c.Hkv + h) * a.n_select + blk];
+          if (blk >= 0 && blk < a.c.n_blocks && blk * kBlk < kv_len) {
+            const int page = min(max(page_of(a.c, b, blk), 0), a.c.n_pages - 1);
+            at_k0 = blk * kBlk;
+            at_phys = pool_block(a.c, page, h, in_page(a.c, blk));
+          }
+        }
       };
-      auto set_step = [&](int2 at) __attribute__((always_inline)) {
-        k0n = __builtin_amdgcn_readfirstlane(at.x);
-        phys = __builtin_amdgcn_readfirstlane(at.y);
+      auto set_step = [&](int l) __attribute__((always_inline)) {
+        k0n = __builtin_amdgcn_readlane(at_k0, l);
+        phys = __builtin_amdgcn_readlane(at_phys, l);
       };
-      auto load_k = [&]() __attribute__((always_inline)) {
-        const unsigned char* kp = a.c.k + (size_t)phys * kBlkBytes;
+      // A load that is behind the last step reads one piece of the table, so that every turn of
+      // the loop has the same loads in flight: where they may or may not be, each wait is
+      // for the path with fewer, which drains the pipeline.
+      auto load_k = [&](bool more) __attribute__((always_inline)) {
+        const unsigned char* kp = more ? a.c.k + (size_t)phys * kBlkBytes : (const unsigned char*)a.table;
+        const int step = more ? 16 * lane : 0;
         ks = a.c.k_scale[phys];
         const int kk = max(k0n, 0);
         int r = qpos - kk;
@@ -370,14 +398,15 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
                               (size_t)(uint32_t)max(r, 0) * (kHalf * 8) + 16 * (lane & 31));
 #pragma unroll
         for (int n = 0; n < 8; ++n)
-          kx[n] = __builtin_nontemporal_load((const u32x4*)(kp + 1024 * n + 16 * lane));
+          kx[n] = __builtin_nontemporal_load((const u32x4*)(kp + 1024 * n + step));
       };
-      auto load_v = [&]() __attribute__((always_inline)) {
-        const unsigned char* vp = a.c.v + (size_t)phys * kBlkBytes;
+      auto load_v = [&](bool more) __attribute__((always_inline)) {
+        const unsigned char* vp = more ? a.c.v + (size_t)phys * kBlkBytes : (const unsigned char*)a.table;
+        const int step = more ? 16 * lane : 0;
         vs = a.c.v_scale[phys];
 #pragma unroll
         for (int n = 0; n < 8; ++n)
-          vx[n] = __builtin_nontemporal_load((const u32x4*)(vp + 1024 * n + 16 * lane));
+          vx[n] = __builtin_nontemporal_load((const u32x4*)(vp + 1024 * n + step));
       };
 
       // sc: the scores of four tiles of 16 keys, in units of the block's scale
@@ -523,21 +552,12 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
         }
       };
 
-      // ---- the steps, kD8List at a time: their blocks are looked up, a wave's first one ahead
-      // of the list
-      static_assert(kD8List <= kD8Threads, "a step per thread");
-      auto begin = [&](int s0, int n) __attribute__((always_inline)) {
-        int2 mine = make_int2(-1, 0);
-        if (tid < n) mine = find(s0 + tid);
-        if (wave < n) {
-          set_step(find(s0 + wave));
-          load_k();
-          load_v();
-        }
-        if (tid < n) sm.list[tid] = mine;
-      };
-      int s0 = 0, n = min(n_steps, kD8List);
-      begin(s0, n);
+      const int mine = (n_steps - wave + kD8Waves - 1) / kD8Waves;  // this wave's steps
+      look_up(wave);
+      set_step(0);
+      load_k(mine > 0);
+      load_v(mine > 0);
+
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         unpack8(qraw[u], qlo + 8 * u);
@@ -557,36 +577,20 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
         }
         q_back = pow2f(e);
       }
-      lds_barrier();
-      for (;;) {
-        // the last step stands apart: where loads may or may not be in flight, every wait is
-        // for the path with fewer, which drains the pipeline
-        int i = wave;
-        for (; i + kD8Waves < n; i += kD8Waves) {
-          k0 = k0n;
-          const bool on = !LISTED || k0 >= 0;
-          if (on) scores();
-          const float ks_now = ks;
-          set_step(sm.list[i + kD8Waves]);
-          load_k();
-          if (on) {
-            softmax(ks_now);
-            values();
-          }
-          load_v();
-        }
+      for (int i = 0; i < mine; ++i) {
         k0 = k0n;
-        if (i < n && (!LISTED || k0 >= 0)) {
-          scores();
-          softmax(ks);
+        const bool on = !LISTED || k0 >= 0;
+        if (on) scores();
+        const float ks_now = ks;
+        const bool more = i + 1 < mine;
+        if (((i + 1) & 63) == 0) look_up(wave + kD8Waves * (i + 1));
+        set_step((i + 1) & 63);
+        load_k(more);
+        if (on) {
+          softmax(ks_now);
           values();
         }
-        s0 += kD8List;
-        if (s0 >= n_steps) break;
-        __syncthreads();  // the list is read
-        n = min(n_steps - s0, kD8List);
-        begin(s0, n);
-        lds_barrier();
+        load_v(more);
       }
 
       // ---- the waves' states, and the two views of a head, into one (max-shifted)
@@ -667,54 +671,55 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
     const int n = __builtin_amdgcn_readfirstlane(sm.due[slot].n);
     const int wf = __builtin_amdgcn_readfirstlane(sm.due[slot].wf);
     auto state = [&](int p) { return state_at(a, wf + p, p == 0, head); };
-    f32x4 num = f32x4{};
-    float den = 0.f;
-    // the maxima and a batch of states are requested together; the weights are formed while
-    // the states are under way
-    auto merge = [&]() __attribute__((always_inline)) {
+    if (set < n_sets) {
+      f32x4 num = f32x4{};
+      float M = -INFINITY, den = 0.f;
       constexpr int kBatch = 8;
-      f32x4 x[kBatch];
-      auto request = [&](int p0) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i)
-          x[i] = get4(states, state(min(p0 + i * n_sets, n - 1)) + 16 + 4 * c4);
-      };
-      const float2 ml0 = get2(states, state(min(l32, n - 1)));
-      const float2 ml1 = get2(states, state(min(l32 + 32, n - 1)));
-      request(set);
-      float M = fmaxf(ml0.x, ml1.x);
-      for (int p = l32 + 64; p < n; p += 32) M = fmaxf(M, get2(states, state(p)).x);
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
-      for (int p = l32; p < n; p += 32) {
-        float2 e = p == l32 ? ml0 : ml1;
-        if (p >= l32 + 64) e = get2(states, state(p));
-        const float wt = e.x == M ? 1.f : fast_exp2(e.x - M);
-        sm.w[j][p] = wt;
-        den += wt * e.y;
-      }
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) den += __shfl_xor(den, o);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      for (int p0 = set;;) {
+      for (int p0 = set; p0 < n; p0 += kBatch * n_sets) {
+        f32x4 x[kBatch];
+        float2 ml[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-          const int p = p0 + i * n_sets;
-          if (p < n) num += sm.w[j][p] * x[i];
+          const uint32_t at = state(min(p0 + i * n_sets, n - 1));
+          ml[i] = get2(states, at);
+          x[i] = get4(states, at + 16 + 4 * c4);
         }
-        p0 += kBatch * n_sets;
-        if (p0 >= n) break;
-        request(p0);
+        float top = M;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          if (p0 + i * n_sets >= n) ml[i] = make_float2(-INFINITY, 0.f);
+          top = fmaxf(top, ml[i].x);
+        }
+        const float use = top == -INFINITY ? 0.f : top;
+        const float old = M == top ? 1.f : fast_exp2(M - use);
+        den *= old;
+        num *= old;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const float wt = ml[i].x == top && top != -INFINITY ? 1.f : fast_exp2(ml[i].x - use);
+          den += wt * ml[i].y;
+          num += wt * x[i];
+        }
+        M = top;
       }
-    };
-    if (set < n_sets) {
-      merge();
       *(f32x4*)&sm.set_o[j][c4] = num;
+      if (l32 == 0) {
+        sm.set_m[j] = M;
+        sm.set_l[j] = den;
+      }
     }
     __syncthreads();
     if (j < a.g) {
-      for (int t = 1; t < n_sets; ++t) num += *(const f32x4*)&sm.set_o[j + t * a.g][c4];
+      float M = -INFINITY;
+      for (int t = 0; t < n_sets; ++t) M = fmaxf(M, sm.set_m[j + t * a.g]);
+      float den = 0.f;
+      f32x4 num = f32x4{};
+      for (int t = 0; t < n_sets; ++t) {
+        const float mx = sm.set_m[j + t * a.g];
+        const float wt = mx == M ? 1.f : fast_exp2(mx - M);
+        den += wt * sm.set_l[j + t * a.g];
+        num += wt * *(const f32x4*)&sm.set_o[j + t * a.g][c4];
+      }
       bf16x4 r;
 #pragma unroll
       for (int i = 0; i < 4; ++i) r[i] = (__bf16)(den == 0.f ? 0.f : num[i] / den);
@@ -727,6 +732,13 @@ __global__ __launch_bounds__(kD8Threads, 2) void decode8_kernel(Decode8Args a) {
 // ---------------------------------------------------------------- launcher
 int cu_count();
 
+size_t offset_rows_bytes() { return kD8TabBytes; }
+hipError_t launch_offset_rows(const float2* table, void* out, hipStream_t stream) {
+  hipLaunchKernelGGL(offset_rows_kernel, dim3((kD8TabBytes / 4 + 255) / 256), dim3(256), 0, stream,
+                     table, (unsigned char*)out);
+  return hipGetLastError();
+}
+
 size_t decode8_workspace_bytes(int g) {
   return kD8Counters * sizeof(int) + (size_t)2 * kD8MaxWg * g * kD8State * sizeof(float);
 }
@@ -738,20 +750,29 @@ long long decode8_entries(int B, int Hkv, int n) {
 
 hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, const int32_t* kv_lens,
                           const int32_t* blocks, int n_select, uint16_t* o, const float2* table,
-                          int B, int Hq, int w_pre, int w0, void* ws, hipStream_t stream) {
+                          const void* offsets, int B, int Hq, int w_pre, int w0, void* ws,
+                          hipStream_t stream) {
   static_assert(kD8MaxWg <= kD8Counters, "a counter per workgroup");
-  Decode8Args a{c, q, kv_lens, blocks, o, table, (int*)ws, (float*)ws + kD8Counters, B, Hq,
-                Hq / c.Hkv, n_select, std::min(2 * cu_count(), kD8MaxWg), w_pre, w0,
-                1.4426950408889634f / sqrtf((float)kHeadDim)};
-  const dim3 grid(a.n_wg), block(kD8Threads);
-  if (bifocal && blocks != nullptr)
-    hipLaunchKernelGGL((decode8_kernel<true, true>), grid, block, 0, stream, a);
-  else if (bifocal)
-    hipLaunchKernelGGL((decode8_kernel<true, false>), grid, block, 0, stream, a);
-  else if (blocks != nullptr)
-    hipLaunchKernelGGL((decode8_kernel<false, true>), grid, block, 0, stream, a);
-  else
-    hipLaunchKernelGGL((decode8_kernel<false, false>), grid, block, 0, stream, a);
+  // one sequence: at least four workgroups for each of its heads
+  const int mode = blocks != nullptr ? kListed8 : B == 1 && c.Hkv <= 64 ? kOne8 : kBatch8;
+  const int waves = decode8_waves(mode);
+  const int per_cu = 8 / waves;  // registers for two waves per SIMD
+  Decode8Args a{c, q, kv_lens, blocks, o, table, (const unsigned char*)offsets, (int*)ws,
+                (float*)ws + kD8Counters, B, Hq, Hq / c.Hkv, n_select,
+                std::max(per_cu * std::min(cu_count(), kD8MaxWg / 2), mode == kOne8 ? c.Hkv : 1),
+                w_pre, w0, 1.4426950408889634f / sqrtf((float)kHeadDim)};
+  const dim3 grid(a.n_wg), block(64 * waves);
+#define JL_DECODE8(bif, m) hipLaunchKernelGGL((decode8_kernel<bif, m>), grid, block, 0, stream, a)
+  if (bifocal) {
+    if (mode == kListed8) JL_DECODE8(true, kListed8);
+    else if (mode == kOne8) JL_DECODE8(true, kOne8);
+    else JL_DECODE8(true, kBatch8);
+  } else {
+    if (mode == kListed8) JL_DECODE8(false, kListed8);
+    else if (mode == kOne8) JL_DECODE8(false, kOne8);
+    else JL_DECODE8(false, kBatch8);
+  }
+#undef JL_DECODE8
   return hipGetLastError();
 }
 

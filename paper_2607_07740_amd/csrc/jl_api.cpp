@@ -71,7 +71,10 @@ size_t decode8_workspace_bytes(int g);
 long long decode8_entries(int B, int Hkv, int n);
 hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, const int32_t* kv_lens,
                           const int32_t* blocks, int n_select, uint16_t* o, const float2* table,
-                          int B, int Hq, int w_pre, int w0, void* ws, hipStream_t stream);
+                          const void* offsets, int B, int Hq, int w_pre, int w0, void* ws,
+                          hipStream_t stream);
+size_t offset_rows_bytes();
+hipError_t launch_offset_rows(const float2* table, void* out, hipStream_t stream);
 hipError_t launch_block_scores8(bool bifocal, const Cache8& c, const uint16_t* q,
                                 const int32_t* kv_lens, float* scores, const float2* table, int B,
                                 int Hq, int w_pre, hipStream_t stream);
@@ -135,8 +138,9 @@ bool aligned4(const void* p) { return p != nullptr && (reinterpret_cast<uintptr_
 
 // ------------------------------------------------------------ table cache
 // A table of cap positions is one allocation: cap x 64 fp32 (cos, sin) pairs
-// (512 B per position), then the same pairs in fp16, one 32-bit word each
-// (256 B per position).
+// (512 B per position), then the same pairs in bf16, one 32-bit word each
+// (256 B per position); behind the base table of a theta also the rows of the
+// positions below 64 in fp16, as the 8-bit decode takes them.
 struct TableEntry {
   int device;
   double theta;
@@ -153,9 +157,14 @@ const uint32_t* table16_of(const float2* p, long long cap) {
   return reinterpret_cast<const uint32_t*>(p + (size_t)cap * 64);
 }
 
+const void* offsets_of(const float2* p, long long cap) {
+  return reinterpret_cast<const char*>(p) + table_bytes(cap);
+}
+
 struct Tables {
   const float2* f32;
   const uint32_t* f16;
+  const void* offsets;  // of a base table
 };
 
 // Returns device tables covering positions [0, n_pos) for the current device.
@@ -176,7 +185,7 @@ int get_table(double theta, int n_pos, hipStream_t stream, Tables* out) {
   for (auto& t : g_tables)
     if (t.device == dev && t.theta == theta) found = &t;
   if (found && found->cap >= n_pos) {
-    *out = Tables{found->ptr, table16_of(found->ptr, found->cap)};
+    *out = Tables{found->ptr, table16_of(found->ptr, found->cap), offsets_of(found->ptr, found->cap)};
     return JL_OK;
   }
   long long cap = 4096;
@@ -184,11 +193,12 @@ int get_table(double theta, int n_pos, hipStream_t stream, Tables* out) {
   if (found && cap < 2LL * found->cap) cap = 2LL * found->cap;
   if (cap > (1LL << 30) / 64) cap = n_pos;  // keep the element count in range
   float2* p = nullptr;
-  e = hipMalloc(&p, table_bytes(cap));
+  e = hipMalloc(&p, table_bytes(cap) + jl::offset_rows_bytes());
   if (e != hipSuccess) return hip_fail(e, "hipMalloc(rope table)");
   double omega[kHeadDim / 2];
   rope_omega(theta, omega);
   e = jl::launch_build_table(p, const_cast<uint32_t*>(table16_of(p, cap)), (int)cap, omega, stream);
+  if (e == hipSuccess) e = jl::launch_offset_rows(p, const_cast<void*>(offsets_of(p, cap)), stream);
   if (e == hipSuccess) e = hipStreamSynchronize(stream);  // usable from any stream afterwards
   if (e != hipSuccess) {
     (void)hipFree(p);
@@ -201,7 +211,7 @@ int get_table(double theta, int n_pos, hipStream_t stream, Tables* out) {
   } else {
     g_tables.push_back(TableEntry{dev, theta, (int)cap, p});
   }
-  *out = Tables{p, table16_of(p, cap)};
+  *out = Tables{p, table16_of(p, cap), offsets_of(p, cap)};
   return JL_OK;
 }
 
@@ -257,7 +267,7 @@ int get_freq_table(double theta, int L, int w_pre, hipStream_t stream, Tables* o
   for (auto& t : g_freq_tables)
     if (t.device == dev) found = &t;
   if (found && found->theta == theta && found->L == L && found->w_pre == w_pre) {
-    *out = Tables{found->ptr, table16_of(found->ptr, found->cap)};
+    *out = Tables{found->ptr, table16_of(found->ptr, found->cap), nullptr};
     return JL_OK;
   }
   if (found) {
@@ -296,7 +306,7 @@ int get_freq_table(double theta, int L, int w_pre, hipStream_t stream, Tables* o
   } else {
     g_freq_tables.push_back(FreqTable{dev, theta, L, w_pre, cap, p});
   }
-  *out = Tables{p, table16_of(p, cap)};
+  *out = Tables{p, table16_of(p, cap), nullptr};
   return JL_OK;
 }
 
@@ -695,7 +705,7 @@ int decode8_common(bool bifocal, const jl_cache8* cache, const int32_t* block_ta
   if (st != JL_OK) return st;
   const hipError_t e =
       jl::launch_decode8(bifocal, c, (const uint16_t*)q, kv_lens, listed ? blocks : nullptr,
-                         n_select, (uint16_t*)o, tab.f32, B, Hq, w_pre, w0, ws, s);
+                         n_select, (uint16_t*)o, tab.f32, tab.offsets, B, Hq, w_pre, w0, ws, s);
   if (e != hipSuccess) return hip_fail(e, "8-bit decode launch");
   return ok();
 }
