@@ -343,9 +343,9 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
       const int qpos = max(kv_len - 1, 0);
       const int fq = (int)fastdiv((uint32_t)qpos, gdiv);
       const int keep_lo = BIFOCAL && view == 1 ? (int)min((uint32_t)w0 + 1u, (uint32_t)INT_MAX) : 0;
-      const uint32_t keep_n = !col_on ? 0u
-                              : view == 0 ? (uint32_t)w0 + 1u
-                                          : (uint32_t)INT_MAX - (uint32_t)w0;
+      const uint32_t keep = !col_on ? 0u
+                            : view == 0 ? (uint32_t)w0 + 1u
+                                        : (uint32_t)INT_MAX - (uint32_t)w0;
 
       f32x4 acc[8];
 #pragma unroll
@@ -357,11 +357,11 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
       float qlo[16], qhi[16];
       float q_back;  // what undoes the latter
 
-      // the step in hand; its K registers take the next step's as soon as the scores are
-      // formed, its V registers when the product is
+      // the step in hand; each register takes the next step's piece as soon as its own is used
       u32x4 kx[8], vx[8], row;
       float ks, vs;
-      int k0;         // first position of the step's block, below 0: nothing to do
+      int k0;         // first position of the step's block
+      bool on;        // there is one (a list may name none)
       int k0n, phys;  // of the step that is loaded
       // Lane l holds this wave's l-th step of 64: its position (-1 where there is nothing to do)
       // and its block of the pools.
@@ -380,33 +380,29 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
           }
         }
       };
+      // Where the loaded step's pieces come from.  Behind the last step, and where a list names no
+      // block, that is one piece of the table: every turn of the loop has the same loads in
+      // flight.  (Where they may or may not be, each wait is for the path with fewer, which
+      // drains the pipeline.)
+      const unsigned char *kp, *vp;
+      int piece;
+      const unsigned char* rp;
       auto set_step = [&](int l) __attribute__((always_inline)) {
         k0n = __builtin_amdgcn_readlane(at_k0, l);
         phys = __builtin_amdgcn_readlane(at_phys, l);
-      };
-      // A load that is behind the last step reads one piece of the table, so that every turn of
-      // the loop has the same loads in flight: where they may or may not be, each wait is
-      // for the path with fewer, which drains the pipeline.
-      auto load_k = [&](bool more) __attribute__((always_inline)) {
-        const unsigned char* kp = more ? a.c.k + (size_t)phys * kBlkBytes : (const unsigned char*)a.table;
-        const int step = more ? 16 * lane : 0;
-        ks = a.c.k_scale[phys];
+        kp = k0n >= 0 ? a.c.k + (size_t)phys * kBlkBytes : (const unsigned char*)a.table;
+        vp = k0n >= 0 ? a.c.v + (size_t)phys * kBlkBytes : (const unsigned char*)a.table;
+        piece = k0n >= 0 ? 16 * lane : 0;
         const int kk = max(k0n, 0);
         int r = qpos - kk;
         if (BIFOCAL && lane >= 32) r = fq - (int)fastdiv((uint32_t)kk, gdiv);
-        row = *(const u32x4*)((const unsigned char*)a.table +
-                              (size_t)(uint32_t)max(r, 0) * (kHalf * 8) + 16 * (lane & 31));
-#pragma unroll
-        for (int n = 0; n < 8; ++n)
-          kx[n] = __builtin_nontemporal_load((const u32x4*)(kp + 1024 * n + step));
+        rp = (const unsigned char*)a.table + (size_t)(uint32_t)max(r, 0) * (kHalf * 8) + 16 * (lane & 31);
       };
-      auto load_v = [&](bool more) __attribute__((always_inline)) {
-        const unsigned char* vp = more ? a.c.v + (size_t)phys * kBlkBytes : (const unsigned char*)a.table;
-        const int step = more ? 16 * lane : 0;
-        vs = a.c.v_scale[phys];
-#pragma unroll
-        for (int n = 0; n < 8; ++n)
-          vx[n] = __builtin_nontemporal_load((const u32x4*)(vp + 1024 * n + step));
+      auto load_k = [&](int n) __attribute__((always_inline)) {
+        kx[n] = __builtin_nontemporal_load((const u32x4*)(kp + 1024 * n + piece));
+      };
+      auto load_v = [&](int n) __attribute__((always_inline)) {
+        vx[n] = __builtin_nontemporal_load((const u32x4*)(vp + 1024 * n + piece));
       };
 
       // sc: the scores of four tiles of 16 keys, in units of the block's scale
@@ -417,6 +413,7 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
         {
           float2* rows = &sm.rows[wave][0][0];
           ((u32x4*)rows)[lane] = row;
+          row = *(const u32x4*)rp;
           __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
           __builtin_amdgcn_wave_barrier();
           const float4* cs = (const float4*)(rows + (BIFOCAL ? view * kHalf : 0));
@@ -449,6 +446,7 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
           for (int u = 0; u < 2; ++u) {
             const f16x8 c0 = *(const f16x8*)(row + 128 * u), c1 = *(const f16x8*)(row + 128 * u + 16);
             const u32x4 x = kx[2 * t + u];
+            load_k(2 * t + u);
             f16x8 y0, y1;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -473,6 +471,7 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
       auto softmax = [&](float ks) __attribute__((always_inline)) {
         // ---- each column keeps the keys of its own view; lane: keys 16 t + 4 g4 + i
         const uint32_t dist = (uint32_t)(qpos - k0 - 4 * g4) - (uint32_t)keep_lo;
+        const uint32_t keep_n = LISTED && !on ? 0u : keep;
         float mt = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -517,12 +516,13 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
       auto values = [&]() __attribute__((always_inline)) {
         // ---- O += scale V^T P^T; where the sequence ends inside the block the values behind
         // its end are zeroed, since 0 times what lies there may be NaN
-        if (k0 + kBlk > kv_len) {
+        const int len = LISTED && !on ? 0 : kv_len;
+        if (k0 + kBlk > len) {
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-              const int left = kv_len - (k0 + 32 * hf + 16 * t + 4 * g4);
+              const int left = len - (k0 + 32 * hf + 16 * t + 4 * g4);
               const uint32_t keep = left >= 4 ? ~0u : left > 0 ? (1u << (8 * left)) - 1 : 0u;
 #pragma unroll
               for (int c = 0; c < 4; ++c) {
@@ -532,16 +532,19 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
             }
         }
         const float up = vs * kD8Down;
+        vs = a.c.v_scale[phys];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
+          const u32x4 x[2] = {vx[c], vx[4 + c]};
+          load_v(c);
+          load_v(4 + c);
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             f32x4 d = f32x4{};
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-              const u32x4 x = vx[4 * hf + c];
-              const f16x2 v0 = e4m3_f16<false>(x[2 * e]), v1 = e4m3_f16<true>(x[2 * e]);
-              const f16x2 v2 = e4m3_f16<false>(x[2 * e + 1]), v3 = e4m3_f16<true>(x[2 * e + 1]);
+              const f16x2 v0 = e4m3_f16<false>(x[hf][2 * e]), v1 = e4m3_f16<true>(x[hf][2 * e]);
+              const f16x2 v2 = e4m3_f16<false>(x[hf][2 * e + 1]), v3 = e4m3_f16<true>(x[hf][2 * e + 1]);
               const f16x8 v = {v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
               d = mfma16h(v, p[hf], d);
             }
@@ -555,8 +558,13 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
       const int mine = (n_steps - wave + kD8Waves - 1) / kD8Waves;  // this wave's steps
       look_up(wave);
       set_step(0);
-      load_k(mine > 0);
-      load_v(mine > 0);
+      ks = a.c.k_scale[phys];
+      row = *(const u32x4*)rp;
+#pragma unroll
+      for (int n = 0; n < 8; ++n) load_k(n);
+      vs = a.c.v_scale[phys];
+#pragma unroll
+      for (int n = 0; n < 8; ++n) load_v(n);
 
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -578,19 +586,15 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
         q_back = pow2f(e);
       }
       for (int i = 0; i < mine; ++i) {
-        k0 = k0n;
-        const bool on = !LISTED || k0 >= 0;
-        if (on) scores();
-        const float ks_now = ks;
-        const bool more = i + 1 < mine;
+        on = k0n >= 0;
+        k0 = max(k0n, 0);
         if (((i + 1) & 63) == 0) look_up(wave + kD8Waves * (i + 1));
         set_step((i + 1) & 63);
-        load_k(more);
-        if (on) {
-          softmax(ks_now);
-          values();
-        }
-        load_v(more);
+        const float ks_now = ks;
+        ks = a.c.k_scale[phys];
+        scores();
+        softmax(ks_now);
+        values();
       }
 
       // ---- the waves' states, and the two views of a head, into one (max-shifted)
