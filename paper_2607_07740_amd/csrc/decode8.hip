@@ -221,7 +221,8 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
   const int i16 = lane & 15, g4 = lane >> 4;
   const int w = blockIdx.x;
 
-  // ---- offset rows, straight into LDS
+  // ---- offset rows, straight into LDS (a workgroup without work waits for them too, while it
+  // holds the LDS they go to)
   for (int n = wave; n < kD8TabBytes / 1024; n += kD8Waves)
     dma16_s(a.offsets, 1024 * n + 16 * lane, lds_addr(sm.tab) + 1024 * n);
 
@@ -238,19 +239,19 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
   if (even) {
     const int per = a.n_wg / segs;
     const int seg = w / per;
-    if (seg >= segs) return;
+    if (seg >= segs) return wait_vmem();
     b = seg / a.c.Hkv;
     h = seg - b * a.c.Hkv;
     const int n = LISTED ? a.n_select : (len8(a, 0) + kBlk - 1) / kBlk;
     first_wg = seg * per;
     parts = __builtin_amdgcn_readfirstlane(max(1, min(per, (n + kD8Waves - 1) / kD8Waves)));
     x0 = (uint32_t)(w - first_wg);
-    if ((int)x0 >= parts) return;
+    if ((int)x0 >= parts) return wait_vmem();
     x1 = UINT_MAX;
   } else if (LISTED) {
     const uint32_t e = (uint32_t)(a.n_select + kD8SegCost);
     make_ranges(sg, a.n_wg, kD8Waves, e * (uint32_t)segs);
-    if (w >= sg.n) return;
+    if (w >= sg.n) return wait_vmem();
     x0 = range_start(sg, w);
     const uint32_t seg = x0 / e;
     b = (int)(seg / (uint32_t)a.c.Hkv);
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
       V += t;
     }
     make_ranges(sg, a.n_wg, kD8Waves, __builtin_amdgcn_readfirstlane(V));
-    if (w >= sg.n) return;
+    if (w >= sg.n) return wait_vmem();
     x0 = range_start(sg, w);
     uint32_t before = 0;
     b = 0;

@@ -492,6 +492,70 @@ def test_decode_over_long_lists_and_many_sequences(B, n_select):
     check(out, want, bound, "long lists")
 
 
+def _ones(rng_seed, n_pages, page, Hkv):
+    """A dense cache whose keys are zero and whose values are drawn from -1, 0, 1, 2, straight as
+    images (random bytes), with unit scales."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rng_seed)
+    cache = api.cache8_alloc(n_pages, page, Hkv)
+    number = torch.tensor([0xB8, 0, 0x38, 0x40], dtype=torch.uint8, device="cuda")
+    for h in range(Hkv):
+        for p in range(n_pages):
+            pick = torch.randint(0, 4, (page, 128), generator=g, device="cuda", dtype=torch.uint8)
+            cache.v[p, h] = number[pick.int()]
+    cache.k_scale.fill_(1)
+    cache.v_scale.fill_(1)
+    return cache
+
+
+@pytest.mark.parametrize("B,Hkv,n", [(1, 8, 1100000), (2, 1, 4194304), (1, 70, 1000)])
+def test_decode_of_millions_of_keys(B, Hkv, n):
+    """More steps than a wave looks up at once, in one sequence and in a batch, and one sequence of
+    more kv heads than share its workgroups: equal scores, so the output is the values' mean,
+    whose sum fp32 holds exactly."""
+    page = -(-n // 64) * 64
+    cache = _ones(n, B, page, Hkv)
+    lens = [n - 70 * b for b in range(B)]
+    q = dev(normals(np.random.default_rng(n), B, 2 * Hkv, C.D))
+    say("decode8 of %d keys, B=%d Hkv=%d" % (n, B, Hkv))
+    out = api.decode8(q, cache, ints(lens), w_pretrained=40000, w_local=5000).double()
+    for b in range(B):
+        total = torch.zeros((Hkv, C.D), dtype=torch.float64, device="cuda")
+        for s in range(0, lens[b], 1 << 18):
+            m = min(1 << 18, lens[b] - s)
+            _, v = api.cache8_read(cache, m, start=s, B=B)
+            total += v[b].double().sum(0)
+        want = (total / lens[b]).repeat_interleave(2, 0)
+        # the sums exact, one fp32 quotient rounded to bf16
+        assert bool(((out[b] - want).abs() <= want.abs() * C.UBF * (1 + 2.0 ** -14)).all())
+
+
+@pytest.mark.parametrize("B,n_select", [(128, 270), (200, 9), (300, 2)])
+def test_decode_over_more_lists_than_workgroups(B, n_select):
+    """Lists that a workgroup has for itself, of more entries than a wave looks up at once, and
+    more lists than workgroups."""
+    Hkv, nb = 4, 6
+    cache = _ones(B, B, nb * 64, Hkv)
+    rng = np.random.default_rng(B)
+    blocks = rng.integers(-1, nb + 1, (B, Hkv, n_select)).astype(np.int32)
+    lens = rng.integers(0, nb * 64 + 1, B)
+    q = dev(normals(rng, B, 2 * Hkv, C.D))
+    say("decode8_blocks B=%d n_select=%d" % (B, n_select))
+    out = api.decode8_blocks(q, cache, ints(lens), ints(blocks), w_pretrained=100, w_local=50)
+    _, v = api.cache8_read(cache, nb * 64)
+    v, got = v.double().cpu().numpy(), out.double().cpu().numpy()
+    for b in range(B):
+        for h in range(Hkv):
+            times = np.zeros(nb * 64)
+            for j in blocks[b, h]:
+                if 0 <= j < nb:
+                    times[64 * j:64 * j + 64] += 1
+            times[lens[b]:] = 0
+            want = times @ v[b, :, h] / max(times.sum(), 1)
+            for i in (2 * h, 2 * h + 1):
+                assert (np.abs(got[b, i] - want) <= np.abs(want) * C.UBF * (1 + 2.0 ** -14)).all()
+
+
 # ------------------------------------------------------------------ together
 def _serving(Hq=8, Hkv=2, n0=300, steps=5, w_pre=128, w0=64, seed=0):
     rng = np.random.default_rng(seed)
