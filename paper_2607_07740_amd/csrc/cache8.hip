@@ -230,7 +230,7 @@ struct ReadArgs {
   Cache8 c;
   uint16_t* k;  // [B][n][Hkv][128] bf16
   uint16_t* v;
-  int start, n, blk0, nb, units;
+  int start, n, blk0, nb;
 };
 
 __device__ inline uint32_t bf16_pair(float a, float b) {
@@ -243,10 +243,8 @@ __device__ inline uint32_t bf16_pair(float a, float b) {
 // magnitude of at least 2^-126 or zero, so bf16 holds it exactly.
 __global__ __launch_bounds__(256) void read8_kernel(ReadArgs a) {
   const int tid = threadIdx.x;
-  const int unit_id = unit_of(a.units, true);
-  if (unit_id >= a.units) return;
-  const int h = unit_id % a.c.Hkv;
-  const int bi = unit_id / a.c.Hkv;
+  const int h = blockIdx.x % a.c.Hkv;
+  const int bi = blockIdx.x / a.c.Hkv;
   const int b = bi / a.nb;
   const int blk = a.blk0 + bi - b * a.nb;
   const int page = min(max(page_of(a.c, b, blk), 0), a.c.n_pages - 1);
@@ -263,7 +261,7 @@ __global__ __launch_bounds__(256) void read8_kernel(ReadArgs a) {
       uint16_t* dst = a.k + out0 + (size_t)o * row;
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        const int d = 32 * q + 8 * kc;
+        const int d = 16 * kc + 8 * q;
         float f[16];
         e4m3_16(load16(src + k_offset(kr, d)), f);
         u32x4 lo, hi;
@@ -323,13 +321,11 @@ hipError_t launch_append8(const Cache8& c, const uint16_t* k, const uint16_t* v,
 
 hipError_t launch_read8(const Cache8& c, uint16_t* k, uint16_t* v, int B, int start, int n,
                         hipStream_t stream) {
-  ReadArgs a{c, k, v, start, n, start / kBlk, 0, 0};
+  ReadArgs a{c, k, v, start, n, start / kBlk, 0};
   a.nb = (start + n - 1) / kBlk - a.blk0 + 1;
-  const long long units = (long long)B * a.nb * c.Hkv;
-  const unsigned grid = grid_of(units);
-  if (grid == 0) return hipErrorInvalidConfiguration;
-  a.units = (int)units;
-  hipLaunchKernelGGL(read8_kernel, dim3(grid), dim3(256), 0, stream, a);
+  const long long wgs = (long long)B * a.nb * c.Hkv;
+  if (wgs > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL(read8_kernel, dim3((unsigned)wgs), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
