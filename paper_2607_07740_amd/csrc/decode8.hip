@@ -115,7 +115,6 @@ __device__ inline f32x4 get4(buffer_t r, uint32_t at) {
   return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, kDeviceScope));
 }
 __device__ inline float2 get2(buffer_t r, uint32_t at) {
-  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
   const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, kDeviceScope);
   return make_float2(__uint_as_float(x[0]), __uint_as_float(x[1]));
 }
@@ -127,7 +126,6 @@ __device__ inline uint32_t state_at(const Decode8Args& a, int w, bool begins, in
 
 // Maximum over the lanes l, l ^ 16, l ^ 32, l ^ 48, by lane swaps in registers.
 __device__ inline float max_over_groups(float x) {
-  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
   u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
   r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
