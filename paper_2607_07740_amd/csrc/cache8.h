@@ -16,6 +16,8 @@
 
 namespace jl {
 
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
 constexpr int kBlk = 64;                    // tokens of a block
 constexpr int kBlkBytes = kBlk * kHeadDim;  // one image: 8 KB
 constexpr int kScaleExpMin = -117, kScaleExpMax = 119;
