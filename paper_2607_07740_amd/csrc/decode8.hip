@@ -83,13 +83,6 @@ __device__ inline FastDiv make_fastdiv24(uint32_t d) {
   return f;
 }
 
-// A barrier for LDS alone: loads from memory stay in flight across it.
-__device__ inline void lds_barrier() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
 __device__ inline int len8(const Decode8Args& a, int b) {
   return min(max(a.kv_lens[b], 0), a.c.n_blocks * kBlk);
 }
@@ -530,7 +523,8 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
               }
             }
         }
-        const float up = vs * kD8Down;
+        // a step without a block holds some other block's scale, perhaps no number
+        const float up = LISTED && !on ? 0.f : vs * kD8Down;
         vs = a.c.v_scale[phys];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {

@@ -476,6 +476,30 @@ def test_decode_over_listed_blocks(g, Hkv, per):
         assert bool((out[4] == 0).all()) and bool((out[7] == 0).all())
 
 
+@pytest.mark.parametrize("fill", [math.nan, math.inf])
+def test_entries_that_name_no_block_take_nothing_from_the_pools(fill):
+    """The pools' first page belongs to no sequence and holds no numbers: the same bits as over
+    pools in which it holds zeros."""
+    rng = np.random.default_rng(31)
+    lens = [600, 130, 64, 0]
+    m = filled(rng, 4, 10, 2, lens)
+    table = np.arange(1, 41, dtype=np.int32).reshape(4, 10)
+    pools = C.pools(m, table, 41, 1)
+    q, blocks = normals(rng, 4, 8, C.D), rng.integers(-2, 12, (4, 2, 40)).astype(np.int32)
+    blocks[0, 0, 1:], blocks[1, 1] = -1, -1
+    outs = []
+    for x in (0.0, fill):
+        for a in pools[2:]:
+            a[0] = x
+        pools[0][0], pools[1][0] = (127, 127) if x else (0, 0)
+        say("decode8_blocks beside a page of", x)
+        outs.append(api.decode8_blocks(dev(q), upload(pools), ints(lens), ints(blocks),
+                                       w_pretrained=64, w_local=20, block_table=ints(table)))
+    assert torch.equal(outs[0], outs[1])
+    want, bound = C.decode(q, m, lens, 64, 20, True, blocks)
+    check(outs[1], want, bound, "beside a page without numbers")
+
+
 @pytest.mark.parametrize("B,n_select", [(1, 120), (2, 1000), (90, 3)])
 def test_decode_over_long_lists_and_many_sequences(B, n_select):
     rng = np.random.default_rng(B)
