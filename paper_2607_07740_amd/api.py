@@ -655,9 +655,10 @@ def _cache8(cache, block_table, B):
             raise ValueError("a dense cache of %d sequences cannot hold %d" % (cache.n_pages, B))
         return cache._ref, None, 0, cache.page_size
     table = _on8(block_table, "block_table", _t().int32, None, cache.index, cache.device)
-    if block_table.dim() != 2 or block_table.shape[0] != B:
+    shape = block_table.shape
+    if len(shape) != 2 or shape[0] != B or shape[1] < 1:
         raise ValueError("block_table must be [B, max_pages]")
-    max_pages = block_table.shape[1]
+    max_pages = shape[1]
     return cache._ref, table, max_pages, max_pages * cache.page_size
 
 

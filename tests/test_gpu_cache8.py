@@ -749,3 +749,17 @@ def test_refusals_of_the_binding():
             (lambda: api.cache8_alloc(2, 100, 2), ValueError)):
         with pytest.raises(err):
             bad()
+
+
+def test_a_table_without_pages_is_refused():
+    cache = api.cache8_alloc(2, 128, 2)
+    q, lens = torch.zeros((2, 4, 128), dtype=BF, device="cuda"), ints([5, 6])
+    none = torch.zeros((2, 0), dtype=torch.int32, device="cuda")
+    rows = torch.zeros((2, 3, 2, 128), dtype=BF, device="cuda")
+    say("empty table")
+    for call in (lambda: api.decode8(q, cache, lens, block_table=none),
+                 lambda: api.block_scores8(q, cache, lens, block_table=none),
+                 lambda: api.cache8_append(cache, rows, rows, lens, block_table=none),
+                 lambda: api.cache8_read(cache, 1, block_table=none)):
+        with pytest.raises(ValueError):
+            call()
