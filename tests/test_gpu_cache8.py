@@ -708,6 +708,36 @@ def test_calls_on_a_given_stream():
                                       C.select(sc.cpu().numpy(), lens, 3, 30, 1))
 
 
+def test_calls_on_two_streams_at_once():
+    """Each stream has a workspace of its own; every call gives the bits of the call alone."""
+    rng = np.random.default_rng(12)
+    lens = [3000, 64, 1, 2500, 700]
+    m = filled(rng, 5, 48, 2, lens)
+    cache, qd, ld = upload(C.pools(m)), dev(normals(rng, 5, 8, C.D)), ints(lens)
+    one = upload(C.pools(filled(rng, 1, 48, 2, [3000])))
+    lists = ints(np.tile(np.arange(48, dtype=np.int32), (5, 2, 1)))
+    kw = dict(w_pretrained=500, w_local=100)
+
+    def calls(ws, st=None):
+        return [api.decode8(qd, cache, ld, workspace=ws, stream=st, **kw),
+                api.decode8_blocks(qd, cache, ld, lists, workspace=ws, stream=st, **kw),
+                api.decode8(qd[:1], one, ld[:1], workspace=ws, stream=st, **kw),
+                api.block_scores8(qd, cache, ld, w_pretrained=500, stream=st)]
+
+    alone = calls(api.decode8_workspace(8, 2))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [api.decode8_workspace(8, 2) for _ in streams]
+    torch.cuda.synchronize()
+    say("two streams")
+    got = [calls(ws, st) for _ in range(8) for ws, st in zip(spaces, streams)]
+    torch.cuda.synchronize()
+    for outs in got:
+        for x, y in zip(outs, alone):
+            assert torch.equal(x, y)
+    for ws in spaces:
+        assert bool((ws[:4096] == 0).all())
+
+
 def test_refusals_of_the_binding():
     cache = api.cache8_alloc(2, 128, 2)
     q, lens = torch.zeros((2, 4, 128), dtype=BF, device="cuda"), ints([5, 6])
