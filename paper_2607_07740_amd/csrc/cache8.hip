@@ -3,17 +3,6 @@
 
 namespace jl {
 
-// Work units (sequence, block, head), heads fastest.  Workgroups go to the eight dies in
-// turn; grouped, each die takes a run of units, so that the heads of a block, which lie
-// side by side in the rows, meet in one L2.
-__device__ inline int unit_of(int units, bool grouped) {
-  const int w = (int)blockIdx.x;
-  if (!grouped) return w;
-  const int per = (units + 7) >> 3, i = w >> 3;
-  const int u = (w & 7) * per + i;
-  return u < units ? u : units;
-}
-
 struct AppendArgs {
   Cache8 c;
   const uint16_t* k;  // [B][n][Hkv][128] bf16
@@ -21,8 +10,6 @@ struct AppendArgs {
   const int32_t* starts;
   const int32_t* n_new;  // or nullptr: n rows of every sequence
   int n, nb;             // nb: blocks a sequence's new rows can touch
-  int units;
-  bool grouped;
 };
 
 // The sum over 16 lanes (a row) of 16 values each: lane i gets that of value i.  Each step
@@ -56,15 +43,20 @@ __device__ inline float sum_rows16(float (&v)[16], int lane) {
 // block held is requested with its new rows, and written back only where it changed:
 // a token of decode writes 72 of the 1024 16-byte units.  The mean key
 // sums e4m3 values, multiples of 2^-9 below 2^15 in all: exactly, in any order.
+//
+// Bound by memory for a prompt: 30001 rows of 8 heads 32 to 38 us (123 MB read and 62
+// written, as few as there are: 4.9 to 5.8 TB/s; one after another with the reading of
+// 32768 such rows, 75 us in all).  A row each of 16 sequences takes 6.3 us, 2.4 of them
+// an empty launch, the rest the chain length -> page -> block -> scale.  A run of units
+// on each die, whose L2 then has all heads of a row: 39.3 for 37.9 us, 7.7 for 7.7 with 64
+// sequences of one row.
 __global__ __launch_bounds__(256) void append8_kernel(AppendArgs a) {
   __shared__ __attribute__((aligned(16))) unsigned char img[2][kBlkBytes];
   __shared__ float s_top[2][4];
   __shared__ float s_sum[2][kHeadDim];
   const int tid = threadIdx.x;
-  const int unit_id = unit_of(a.units, a.grouped);
-  if (unit_id >= a.units) return;
-  const int h = unit_id % a.c.Hkv;
-  const int bi = unit_id / a.c.Hkv;
+  const int h = blockIdx.x % a.c.Hkv;
+  const int bi = blockIdx.x / a.c.Hkv;
   const int b = bi / a.nb;
   const long long start = a.starts[b];
   const long long cap = (long long)a.c.n_blocks * kBlk;
@@ -240,7 +232,8 @@ __device__ inline uint32_t bf16_pair(float a, float b) {
 }
 
 // Workgroup = one block of one kv head.  A value has 4 significant bits and a
-// magnitude of at least 2^-126 or zero, so bf16 holds it exactly.
+// magnitude of at least 2^-126 or zero, so bf16 holds it exactly.  Bound by memory:
+// 32768 rows of 8 heads 32 to 36 us, 67 MB read and 134 written.
 __global__ __launch_bounds__(256) void read8_kernel(ReadArgs a) {
   const int tid = threadIdx.x;
   const int h = blockIdx.x % a.c.Hkv;
@@ -254,8 +247,8 @@ __global__ __launch_bounds__(256) void read8_kernel(ReadArgs a) {
   const int pos0 = blk * kBlk - a.start;  // output row of the block's first key
   const float ks = a.c.k_scale[at], vs = a.c.v_scale[at];
   // Eight threads a key: a store instruction writes whole 128-byte lines and no cache need keep
-  // them (32768 rows of 8 heads, behind an append: 51 us with pieces of 32 bytes, which wrote
-  // 174 MB for 134; 45 with whole lines; 35 with the nontemporal hint on K and V too).
+  // them (those 32768 rows: 51 us with pieces of 32 bytes, which wrote 174 MB; 45 with whole
+  // lines; 35 with the nontemporal hint on K and V too).
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int key = 32 * i + (tid >> 3), d = 8 * (tid & 7);
@@ -296,24 +289,13 @@ __global__ __launch_bounds__(256) void read8_kernel(ReadArgs a) {
 }
 
 // ---------------------------------------------------------------- launchers
-// Units rounded up to whole rounds of the dies, or 0 where a grid cannot hold them
-static unsigned grid_of(long long units) {
-  const long long wgs = (units + 7) / 8 * 8;
-  return units < 1 || wgs > 0x7fffffffLL ? 0 : (unsigned)wgs;
-}
-
 hipError_t launch_append8(const Cache8& c, const uint16_t* k, const uint16_t* v,
                           const int32_t* starts, const int32_t* n_new, int B, int n,
                           hipStream_t stream) {
-  AppendArgs a{c, k, v, starts, n_new, n, (int)((n + kBlk - 2LL) / kBlk + 1), 0, false};
-  const long long units = (long long)B * a.nb * c.Hkv;
-  const unsigned grid = grid_of(units);
-  if (grid == 0) return hipErrorInvalidConfiguration;
-  a.units = (int)units;
-  // Tokens: 64 sequences of 8 heads 7.5 -> 6.6 us grouped.  Prompts, whose blocks follow one
-  // another: 30001 rows 40.2 -> 42.2 us.
-  a.grouped = n < kBlk;
-  hipLaunchKernelGGL(append8_kernel, dim3(grid), dim3(256), 0, stream, a);
+  AppendArgs a{c, k, v, starts, n_new, n, (int)((n + kBlk - 2LL) / kBlk + 1)};
+  const long long wgs = (long long)B * a.nb * c.Hkv;
+  if (wgs > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL(append8_kernel, dim3((unsigned)wgs), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
