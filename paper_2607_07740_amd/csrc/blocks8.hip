@@ -158,6 +158,8 @@ struct SelectArgs {
   int Hkv, n_blocks, n_select, w0, n_first;
 };
 
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // rows start anywhere
+
 // A score as an unsigned number of the same order: NaN above everything, both zeros equal.
 __device__ inline uint32_t order_of(float x) {
   if (x != x) return 0xfffffffeu;
@@ -165,19 +167,23 @@ __device__ inline uint32_t order_of(float x) {
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
-constexpr int kSelThreads = 512;
+// Most scores share a few values of the first digit: its counts are held four times, the copies
+// of a count in different banks (2048 scores: 6.3 -> 5.8 us).
+constexpr int kSelCopies = 4, kSelCopy = 256 + 16;
 
 // Workgroup = one row.  The blocks that are always chosen count as the largest number.
 // The want-th largest number is found eight bits at a time from counts of that digit
 // among the numbers that share the digits so far; then one scan in index order gives
 // every chosen block its place, the numbers equal to the last one in turn until the
 // list is full.  Every wave reads the counts for itself: one barrier a digit.
-// R: numbers a thread holds; a row of more than 512 R is read anew for each digit.
-// Latency-bound.
-template <int R>
-__global__ __launch_bounds__(kSelThreads) void select_blocks_kernel(SelectArgs a) {
-  __shared__ __attribute__((aligned(16))) int hist[4][256];
-  __shared__ unsigned long long s_sum[kSelThreads / 64];
+// T threads hold R numbers each, side by side; a longer row is read anew for each digit.
+// Bound by latency, 2.4 us of it an empty launch: 5.8 us for 2048 scores, one row or 64, 9.9 for
+// 8192, 14.5 for 16384 (a million tokens), 121 for 131072.
+template <int T, int R>
+__global__ __launch_bounds__(T) void select_blocks_kernel(SelectArgs a) {
+  __shared__ __attribute__((aligned(16))) int first[kSelCopies * kSelCopy];
+  __shared__ __attribute__((aligned(16))) int hist[3][256];
+  __shared__ unsigned long long s_sum[T / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b = blockIdx.x / a.Hkv;
   const int kv_len = max(a.kv_lens[b], 0);
@@ -185,9 +191,9 @@ __global__ __launch_bounds__(kSelThreads) void select_blocks_kernel(SelectArgs a
   const float* row = a.scores + (size_t)blockIdx.x * a.n_blocks;
   int32_t* out = a.blocks + (size_t)blockIdx.x * a.n_select;
   const int want = min(a.n_select, nb);
-  for (int i = want + tid; i < a.n_select; i += kSelThreads) out[i] = -1;
+  for (int i = want + tid; i < a.n_select; i += T) out[i] = -1;
   if (nb <= a.n_select) {
-    for (int i = tid; i < nb; i += kSelThreads) out[i] = i;
+    for (int i = tid; i < nb; i += T) out[i] = i;
     return;
   }
   // the first block that holds a key of the band
@@ -196,16 +202,28 @@ __global__ __launch_bounds__(kSelThreads) void select_blocks_kernel(SelectArgs a
   uint32_t x[R];
   auto load = [&](int j0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
+    for (int i = 0; i < R; i += 4) {
       const int j = j0 + tid * R + i;
-      const float s = row[min(j, nb - 1)];
-      x[i] = j < a.n_first || j >= band ? 0xffffffffu : order_of(s);
-      if (j >= nb) x[i] = 0;  // below every score
+      float s[4];
+      if (j + 3 < nb) {
+        const f32x4_any v = *(const f32x4_any*)(row + j);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) s[n] = v[n];
+      } else {
+#pragma unroll
+        for (int n = 0; n < 4; ++n) s[n] = row[min(j + n, nb - 1)];
+      }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        x[i + n] = j + n < a.n_first || j + n >= band ? 0xffffffffu : order_of(s[n]);
+        if (j + n >= nb) x[i + n] = 0;  // below every score
+      }
     }
   };
-  const int tile = kSelThreads * R;
+  const int tile = T * R;
   load(0);
-  for (int i = tid; i < 4 * 256; i += kSelThreads) (&hist[0][0])[i] = 0;
+  for (int i = tid; i < kSelCopies * kSelCopy; i += T) first[i] = 0;
+  for (int i = tid; i < 3 * 256; i += T) (&hist[0][0])[i] = 0;
   __syncthreads();
   uint32_t cut = 0;  // the digits of the want-th largest number so far
   int left = want;   // its place among the numbers that share them
@@ -217,11 +235,25 @@ __global__ __launch_bounds__(kSelThreads) void select_blocks_kernel(SelectArgs a
 #pragma unroll
       for (int i = 0; i < R; ++i)
         if (j0 + tid * R + i < nb && (d == 0 || (x[i] ^ cut) >> (shift + 8 * (d > 0)) == 0))
-          atomicAdd(&hist[d][(x[i] >> shift) & 255], 1);
+          atomicAdd(d == 0 ? &first[tid % kSelCopies * kSelCopy + (x[i] >> 24)]
+                           : &hist[max(d - 1, 0)][(x[i] >> shift) & 255], 1);
     }
     __syncthreads();
     // counts of this lane's four digits, and how many numbers have a larger one
-    const int4 n = *(const int4*)&hist[d][4 * lane];
+    int4 n;
+    if (d == 0) {
+      n = make_int4(0, 0, 0, 0);
+#pragma unroll
+      for (int c = 0; c < kSelCopies; ++c) {
+        const int4 f = *(const int4*)&first[c * kSelCopy + 4 * lane];
+        n.x += f.x;
+        n.y += f.y;
+        n.z += f.z;
+        n.w += f.w;
+      }
+    } else {
+      n = *(const int4*)&hist[max(d - 1, 0)][4 * lane];
+    }
     int above = n.x + n.y + n.z + n.w;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -260,7 +292,7 @@ __global__ __launch_bounds__(kSelThreads) void select_blocks_kernel(SelectArgs a
     __syncthreads();
     unsigned long long at = before + sum - own;
 #pragma unroll
-    for (int i = 0; i < kSelThreads / 64; ++i) {
+    for (int i = 0; i < T / 64; ++i) {
       if (i < wave) at += s_sum[i];
       before += s_sum[i];
     }
@@ -302,11 +334,17 @@ hipError_t launch_select_blocks(const float* scores, const int32_t* kv_lens, int
                                 int B, int Hkv, int n_blocks, int n_select, int w0, int n_first,
                                 hipStream_t stream) {
   SelectArgs a{scores, kv_lens, blocks, Hkv, n_blocks, n_select, w0, n_first};
-  const dim3 grid((unsigned)(B * Hkv)), block(kSelThreads);
-  if (n_blocks <= 4 * kSelThreads)
-    hipLaunchKernelGGL(select_blocks_kernel<4>, grid, block, 0, stream, a);
-  else
-    hipLaunchKernelGGL(select_blocks_kernel<16>, grid, block, 0, stream, a);
+  const dim3 grid((unsigned)(B * Hkv));
+#define JL_SELECT(t, r) \
+  hipLaunchKernelGGL((select_blocks_kernel<t, r>), grid, dim3(t), 0, stream, a)
+  // The smallest that holds a row: 2048 scores 5.8 us with (512, 4), 6.6 with (256, 8); 4096 7.0
+  // with (512, 8), 7.7 with (1024, 4), 9.0 with (1024, 8); 8192 9.9 with (1024, 8), 10.3 with
+  // (512, 16); 16384 14.5 with (1024, 16), 16.6 with (512, 32), 20.4 with (1024, 8).
+  if (n_blocks <= 512 * 4) JL_SELECT(512, 4);
+  else if (n_blocks <= 512 * 8) JL_SELECT(512, 8);
+  else if (n_blocks <= 1024 * 8) JL_SELECT(1024, 8);
+  else JL_SELECT(1024, 16);
+#undef JL_SELECT
   return hipGetLastError();
 }
 

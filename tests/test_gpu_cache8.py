@@ -443,6 +443,18 @@ def test_select_equals_a_sort(nb, n_select, w0, n_first, levels):
     np.testing.assert_array_equal(got.cpu().numpy(), C.select(s, lens, n_select, w0, n_first))
 
 
+@pytest.mark.parametrize("nb", [2047, 2049, 3000, 4096, 4097, 8192, 8193, 16385, 20003])
+def test_select_of_rows_of_every_length(nb):
+    """Rows that start at any address, with many equal scores; shorter sequences beside long ones."""
+    rng = np.random.default_rng(nb)
+    lens = [nb * 64, nb * 64 - 1, nb * 37 + 5, 64 * 300]
+    s = np.round(rng.standard_normal((4, 2, nb)) * 30).astype(np.float32)
+    say("select nb=%d" % nb)
+    for n, w0 in ((129, 4096), (nb // 2, 0)):
+        got = api.select_blocks(torch.from_numpy(s).cuda(), ints(lens), n, w_local=w0)
+        np.testing.assert_array_equal(got.cpu().numpy(), C.select(s, lens, n, w0, 1))
+
+
 def test_select_of_the_longest_row():
     rng = np.random.default_rng(1)
     nb, n = 131072, 700
