@@ -36,6 +36,7 @@ struct Decode8Args {
   float* states;  // [2 n_wg][g][kD8State]
   int B, Hq, g, n_select;
   int n_wg, w_pre, w0;
+  int n_sets, n_merge;  // of a merge: sets of threads, and states that one workgroup takes
   float q_scale;
 };
 
@@ -644,83 +645,134 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
   }
 
   // ---- segments that this workgroup shares with others, two at most: the last of a
-  // segment's workgroups merges the states, in list order
+  // segment's workgroups merges the states, in list order.  One workgroup reads them at a CU's
+  // own rate, 0.1 us for those of 8 heads, so more than n_merge go in two steps: the last of a
+  // group of sqrt(n) of them puts its sum in place of the group's first, and the last group's
+  // merges the sums (131072 keys, 8 heads: 1 kv head 29.3 -> 17.3 us, 2 of 8 25.4 -> 21.9,
+  // two sequences 44.4 -> 27.0; 32 states of 8 heads or fewer gain nothing: 50.5, 53.2 in two).
   if (!shared) return;
+  auto group_of = [&](int n) { return (int)ceilf(sqrtf((float)n)); };
+  auto arrive = [&](int i, int n) {
+    const bool last = __hip_atomic_fetch_add(a.counters + i, 1, __ATOMIC_RELAXED,
+                                             __HIP_MEMORY_SCOPE_AGENT) == n - 1;
+    if (last) a.counters[i] = 0;  // as the next call expects it
+    return last;
+  };
   wait_vmem();  // this wave's states have arrived
   __syncthreads();
   if (tid < 2) {
+    const int n = sm.due[tid].n, wf = sm.due[tid].wf;
     bool last = false;
-    if (sm.due[tid].n > 0) {
-      int* counter = a.counters + sm.due[tid].wf;
-      last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-             sm.due[tid].n - 1;
-      if (last) *counter = 0;  // as the next call expects it
+    if (n > 0) {
+      if (n <= a.n_merge) {
+        last = arrive(wf, n);
+      } else {
+        const int gs = group_of(n), first = (w - wf) / gs * gs;
+        last = arrive(first == 0 ? wf : kD8MaxWg + wf + first, min(gs, n - first));
+      }
     }
     sm.last[tid] = last;
   }
   __syncthreads();
   const int j = tid >> 5, l32 = tid & 31, c4 = 4 * l32;
   // sets of 32 g threads: a thread has four channels of a head, a set every n_sets-th part
-  const int n_sets = kD8Threads / (32 * a.g);
+  const int n_sets = a.n_sets;
   const int set = j / a.g, head = j - set * a.g;
   for (int slot = 0; slot < 2; ++slot) {
     if (!sm.last[slot]) continue;
-    const int n = __builtin_amdgcn_readfirstlane(sm.due[slot].n);
+    const int n_all = __builtin_amdgcn_readfirstlane(sm.due[slot].n);
     const int wf = __builtin_amdgcn_readfirstlane(sm.due[slot].wf);
-    auto state = [&](int p) { return state_at(a, wf + p, p == 0, head); };
-    if (set < n_sets) {
-      f32x4 num = f32x4{};
-      float M = -INFINITY, den = 0.f;
-      constexpr int kBatch = 8;
-      for (int p0 = set; p0 < n; p0 += kBatch * n_sets) {
-        f32x4 x[kBatch];
-        float2 ml[kBatch];
+    // the states of parts first + step p, p < n, as the sums of the sets in LDS ...
+    auto merge = [&](int first, int step, int n) __attribute__((always_inline)) {
+      const uint32_t at0 = state_at(a, wf + first, false, head), more = state_at(a, step, false, 0);
+      const uint32_t begins = first == 0 ? state_at(a, 0, true, 0) : 0;
+      auto state = [&](int p) { return at0 + (uint32_t)p * more + (p == 0 ? begins : 0); };
+      if (set < n_sets) {
+        f32x4 num = f32x4{};
+        float M = -INFINITY, den = 0.f;
+        constexpr int kBatch = 8;
+        for (int p0 = set; p0 < n; p0 += kBatch * n_sets) {
+          f32x4 x[kBatch];
+          float2 ml[kBatch];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-          const uint32_t at = state(min(p0 + i * n_sets, n - 1));
-          ml[i] = get2(states, at);
-          x[i] = get4(states, at + 16 + 4 * c4);
-        }
-        float top = M;
+          for (int i = 0; i < kBatch; ++i) {
+            const uint32_t at = state(min(p0 + i * n_sets, n - 1));
+            ml[i] = get2(states, at);
+            x[i] = get4(states, at + 16 + 4 * c4);
+          }
+          float top = M;
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-          if (p0 + i * n_sets >= n) ml[i] = make_float2(-INFINITY, 0.f);
-          top = fmaxf(top, ml[i].x);
-        }
-        const float use = top == -INFINITY ? 0.f : top;
-        const float old = M == top ? 1.f : fast_exp2(M - use);
-        den *= old;
-        num *= old;
+          for (int i = 0; i < kBatch; ++i) {
+            if (p0 + i * n_sets >= n) ml[i] = make_float2(-INFINITY, 0.f);
+            top = fmaxf(top, ml[i].x);
+          }
+          const float use = top == -INFINITY ? 0.f : top;
+          const float old = M == top ? 1.f : fast_exp2(M - use);
+          den *= old;
+          num *= old;
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-          const float wt = ml[i].x == top && top != -INFINITY ? 1.f : fast_exp2(ml[i].x - use);
-          den += wt * ml[i].y;
-          num += wt * x[i];
+          for (int i = 0; i < kBatch; ++i) {
+            const float wt = ml[i].x == top && top != -INFINITY ? 1.f : fast_exp2(ml[i].x - use);
+            den += wt * ml[i].y;
+            num += wt * x[i];
+          }
+          M = top;
         }
-        M = top;
+        *(f32x4*)&sm.set_o[j][c4] = num;
+        if (l32 == 0) {
+          sm.set_m[j] = M;
+          sm.set_l[j] = den;
+        }
       }
-      *(f32x4*)&sm.set_o[j][c4] = num;
-      if (l32 == 0) {
-        sm.set_m[j] = M;
-        sm.set_l[j] = den;
-      }
-    }
-    __syncthreads();
-    if (j < a.g) {
-      float M = -INFINITY;
+      __syncthreads();
+    };
+    // ... and the sets' as one, of head j
+    auto sum = [&](float& M, float& den, f32x4& num) __attribute__((always_inline)) {
+      M = -INFINITY;
       for (int t = 0; t < n_sets; ++t) M = fmaxf(M, sm.set_m[j + t * a.g]);
-      float den = 0.f;
-      f32x4 num = f32x4{};
+      den = 0.f;
+      num = f32x4{};
       for (int t = 0; t < n_sets; ++t) {
         const float mx = sm.set_m[j + t * a.g];
         const float wt = mx == M ? 1.f : fast_exp2(mx - M);
         den += wt * sm.set_l[j + t * a.g];
         num += wt * *(const f32x4*)&sm.set_o[j + t * a.g][c4];
       }
-      bf16x4 r;
+    };
+    auto finish = [&]() __attribute__((always_inline)) {
+      if (j < a.g) {
+        float M, den;
+        f32x4 num;
+        sum(M, den, num);
+        bf16x4 r;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = (__bf16)(den == 0.f ? 0.f : num[i] / den);
-      *(bf16x4*)(a.o + sm.due[slot].o + (size_t)j * kHeadDim + c4) = r;
+        for (int i = 0; i < 4; ++i) r[i] = (__bf16)(den == 0.f ? 0.f : num[i] / den);
+        *(bf16x4*)(a.o + sm.due[slot].o + (size_t)j * kHeadDim + c4) = r;
+      }
+    };
+    if (n_all <= a.n_merge) {
+      merge(0, 1, n_all);
+      finish();
+    } else {
+      const int gs = __builtin_amdgcn_readfirstlane(group_of(n_all));
+      const int first = (w - wf) / gs * gs, groups = (n_all + gs - 1) / gs;
+      merge(first, 1, min(gs, n_all - first));
+      if (j < a.g) {
+        float M, den;
+        f32x4 num;
+        sum(M, den, num);
+        const uint32_t at = state_at(a, wf + first, first == 0, j);
+        put4(states, at + 16 + 4 * c4, num);
+        if (c4 == 0) put4(states, at, f32x4{M, den, 0.f, 0.f});
+      }
+      wait_vmem();
+      __syncthreads();
+      if (tid == 0) sm.last[slot] = arrive(kD8MaxWg + wf + 1, groups);  // no group begins there
+      __syncthreads();
+      if (sm.last[slot]) {
+        merge(0, gs, groups);
+        finish();
+      }
     }
     __syncthreads();  // the sums are read
   }
@@ -749,7 +801,7 @@ hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, cons
                           const int32_t* blocks, int n_select, uint16_t* o, const float2* table,
                           const void* offsets, int B, int Hq, int w_pre, int w0, void* ws,
                           hipStream_t stream) {
-  static_assert(kD8MaxWg <= kD8Counters, "a counter per workgroup");
+  static_assert(2 * kD8MaxWg <= kD8Counters, "two counters per workgroup");
   // one sequence: at least four workgroups for each of its heads
   const int mode = blocks != nullptr ? kListed8 : B == 1 && c.Hkv <= 64 ? kOne8 : kBatch8;
   const int waves = decode8_waves(mode);
@@ -757,7 +809,8 @@ hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, cons
   Decode8Args a{c, q, kv_lens, blocks, o, table, (const unsigned char*)offsets, (int*)ws,
                 (float*)ws + kD8Counters, B, Hq, Hq / c.Hkv, n_select,
                 std::max(per_cu * std::min(cu_count(), kD8MaxWg / 2), mode == kOne8 ? c.Hkv : 1),
-                w_pre, w0, 1.4426950408889634f / sqrtf((float)kHeadDim)};
+                w_pre, w0, 2 * waves / (Hq / c.Hkv), 16 * (2 * waves / (Hq / c.Hkv)),
+                1.4426950408889634f / sqrtf((float)kHeadDim)};
   const dim3 grid(a.n_wg), block(64 * waves);
 #define JL_DECODE8(bif, m) hipLaunchKernelGGL((decode8_kernel<bif, m>), grid, block, 0, stream, a)
   if (bifocal) {

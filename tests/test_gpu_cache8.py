@@ -566,6 +566,30 @@ def test_decode_of_millions_of_keys(B, Hkv, n):
         assert bool(((out[b] - want).abs() <= want.abs() * C.UBF * (1 + 2.0 ** -14)).all())
 
 
+@pytest.mark.parametrize("lens,Hkv,g", [([70000], 1, 8), ([40001], 2, 7), ([66000], 1, 1),
+                                        ([60000, 100, 45000], 1, 8), ([9000, 0, 30000, 64], 2, 5),
+                                        ([33000, 20000], 1, 2)])
+def test_decode_of_sequences_shared_by_many_workgroups(lens, Hkv, g):
+    """Few kv heads and many keys: the states of a head pass through groups of workgroups.  The
+    same call gives the same bits, and the arrival counters are zero behind it."""
+    rng = np.random.default_rng(len(lens) + g)
+    B, nb = len(lens), -(-max(lens) // 64)
+    m = filled(rng, B, nb, Hkv, lens)
+    cache, q = upload(C.pools(m)), normals(rng, B, g * Hkv, C.D)
+    ws = api.decode8_workspace(g * Hkv, Hkv)
+    lists = np.tile(np.arange(nb, dtype=np.int32), (B, Hkv, 1))
+    lists[:, :, ::9] = -1
+    kw = dict(w_pretrained=16384, w_local=1000, workspace=ws)
+    for blocks in (None, lists):
+        say("decode8", lens, "Hkv=%d g=%d listed=%s" % (Hkv, g, blocks is not None))
+        want, bound = C.decode(q, m, lens, 16384, 1000, True, blocks)
+        outs = [api.decode8(dev(q), cache, ints(lens), **kw) if blocks is None else
+                api.decode8_blocks(dev(q), cache, ints(lens), ints(blocks), **kw) for _ in range(3)]
+        check(outs[0], want, bound, "many workgroups")
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+        assert bool((ws[:4096] == 0).all())
+
+
 @pytest.mark.parametrize("B,n_select", [(128, 270), (200, 9), (300, 2)])
 def test_decode_over_more_lists_than_workgroups(B, n_select):
     """Lists that a workgroup has for itself, of more entries than a wave looks up at once, and
