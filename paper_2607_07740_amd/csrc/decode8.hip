@@ -648,8 +648,9 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
   // segment's workgroups merges the states, in list order.  One workgroup reads them at a CU's
   // own rate, 0.1 us for those of 8 heads, so more than n_merge go in two steps: the last of a
   // group of sqrt(n) of them puts its sum in place of the group's first, and the last group's
-  // merges the sums (131072 keys, 8 heads: 1 kv head 29.3 -> 17.3 us, 2 of 8 25.4 -> 21.9,
-  // two sequences 44.4 -> 27.0; 32 states of 8 heads or fewer gain nothing: 50.5, 53.2 in two).
+  // merges the sums (131072 keys, 8 heads: 1 kv head 29.3 -> 17.1 us, 2 of 8 25.4 -> 21.9,
+  // two sequences 44.4 -> 27.0; but 32 states of 8 heads 50.5 -> 53.2, 21 of them in four waves
+  // 27.0 -> 28.6).
   if (!shared) return;
   auto group_of = [&](int n) { return (int)ceilf(sqrtf((float)n)); };
   auto arrive = [&](int i, int n) {
@@ -809,7 +810,7 @@ hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, cons
   Decode8Args a{c, q, kv_lens, blocks, o, table, (const unsigned char*)offsets, (int*)ws,
                 (float*)ws + kD8Counters, B, Hq, Hq / c.Hkv, n_select,
                 std::max(per_cu * std::min(cu_count(), kD8MaxWg / 2), mode == kOne8 ? c.Hkv : 1),
-                w_pre, w0, 2 * waves / (Hq / c.Hkv), 16 * (2 * waves / (Hq / c.Hkv)),
+                w_pre, w0, 2 * waves / (Hq / c.Hkv), 256 / (Hq / c.Hkv),
                 1.4426950408889634f / sqrtf((float)kHeadDim)};
   const dim3 grid(a.n_wg), block(64 * waves);
 #define JL_DECODE8(bif, m) hipLaunchKernelGGL((decode8_kernel<bif, m>), grid, block, 0, stream, a)
