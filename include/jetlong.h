@@ -31,8 +31,8 @@
  *    smaller shape, but for the prefill scratch: a call that cuts its blocks
  *    needs some where a larger call that fills the CUs needs none):
  *      - the RoPE cos/sin table (per device and rope_theta, grown by
- *        doubling to cover the call's positions): every prefill and decode
- *        entry point; growing allocates and waits for `stream`;
+ *        doubling to cover the call's positions): every prefill, decode and
+ *        block score entry point; growing allocates and waits for `stream`;
  *      - the prefill scratch (per device and stream): the _varlen forms with
  *        more than 64 sequences, or the frequency map past the window, and of
  *        jl_bifocal_prefill, jl_rope_attention, their _map and _chunk forms
@@ -530,8 +530,9 @@ size_t jl_decode8_workspace_bytes(int Hq, int Hkv, int head_dim);
  *   workspace, workspace_bytes: jl_decode8_workspace_bytes(Hq, Hkv, head_dim)
  *            bytes, 16-byte aligned, see there
  * Requires Hq % Hkv == 0 and Hq / Hkv <= 8.  Only the cos/sin table may be
- * allocated or grown (to the cache's capacity).  The
- * sums are kept in fp32; the same call gives the same bits.
+ * allocated or grown (to the cache's capacity).  Rotated queries and keys and
+ * the softmax weights are rounded to fp16 (11 bits; an e4m3 number is exact in
+ * it), everything else is kept in fp32; the same call gives the same bits.
  */
 int jl_bifocal_decode8(const jl_cache8* cache, const int32_t* block_table, int max_pages,
                        const void* q, const int32_t* kv_lens, void* o, int B, int Hq,

@@ -201,6 +201,14 @@ struct __attribute__((aligned(1024))) Decode8Smem {
 // it is: e4m3 numbers are exact in fp16, and with |x| <= 448 none overflows.  The
 // block's scale of K multiplies the scores, that of V the step's product.
 // The query is brought to [1, 2) by a power of two first, its own range aside.
+//
+// Bound by memory where keys are many: 8 sequences of 32K to 128K, 32/8 heads 210 us, 1.34 GB
+// at 6.4 TB/s (the loads alone 6.4 to 6.9); one of 1048576 320 us, 6.7; of 131072 48.8 us, 5.5;
+// 32 of 0.5K to 16K on pages of 64 tokens 67.5 us, 5.3.  A step's 675 VALU instructions fit
+// beside its loads: one without the masks of steps in one view took as long.  Bound by a chain
+// of latencies where they are few (1999 keys, 16/8 heads: 10.5 us; 192 keys 6.3): an empty
+// launch 2.4 us, length, page and step about 0.8 each from a request to the data, a step's work
+// 2, the waves' merge 0.9, a state's way to another workgroup and the merge there 2.6.
 template <bool BIFOCAL, int MODE>
 __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(Decode8Args a) {
   constexpr int kD8Waves = decode8_waves(MODE);
