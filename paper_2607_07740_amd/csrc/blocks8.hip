@@ -1,6 +1,7 @@
 // blocks8.hip -- which blocks of an 8-bit cache a query attends to: a score per
 // block from its mean key, and the choice of the largest.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache8.h"
 
@@ -47,17 +48,29 @@ __device__ inline void rotate_pairs(const u32x4* raw, const float2* cs_row, int 
   }
 }
 
-// Maximum over the 8 lanes that share lane / 8, NaN above all.
-__device__ inline float max_of_8(float x) {
-  auto pick = [](float a, float b) { return a != a || b != b ? NAN : fmaxf(a, b); };
-#define JL_DPP(v, ctrl)                                                                       \
-  __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), ctrl, 0xf, \
-                                                        0xf, false))
-  x = pick(x, JL_DPP(x, 0xB1));   // lane ^ 1
-  x = pick(x, JL_DPP(x, 0x4E));   // lane ^ 2
-  x = pick(x, JL_DPP(x, 0x141));  // 7 - lane, inside 8
-#undef JL_DPP
-  return x;
+// NaN above all.
+__device__ inline float max_nan(float a, float b) {
+  return a != a || b != b ? NAN : fmaxf(a, b);
+}
+// Four values of each lane, summed over the lanes l, l ^ 16, l ^ 32, l ^ 48: lane group g4 gets
+// the g4-th sum.
+__device__ inline float sum_of_groups(f32x4 x) {
+  auto add = [](u32x2 r) { return __uint_as_float(r[0]) + __uint_as_float(r[1]); };
+  auto u = [](float f) { return __float_as_uint(f); };
+  const float lo = add(__builtin_amdgcn_permlane32_swap(u(x[0]), u(x[2]), false, false));
+  const float hi = add(__builtin_amdgcn_permlane32_swap(u(x[1]), u(x[3]), false, false));
+  return add(__builtin_amdgcn_permlane16_swap(u(lo), u(hi), false, false));
+}
+__device__ inline float max_of_groups(float x) {
+  auto most = [](u32x2 r) { return max_nan(__uint_as_float(r[0]), __uint_as_float(r[1])); };
+  x = most(__builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  return most(__builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+}
+// acc += q value n of 32 (n = 4 c + x: of register c, from the lanes with l / 4 % 4 = x) times
+// the lane's own m, for the four heads of l % 4.
+template <int X>
+__device__ inline f32x4 mfma4(float q, float m, f32x4 acc) {
+  return __builtin_amdgcn_mfma_f32_4x4x1f32(q, m, acc, 2, X, 0);
 }
 
 // score[b][h][j] = max over the group's heads of <R(f(q)) x_q, R(f(64 j + 31)) mean_j>
@@ -65,15 +78,18 @@ __device__ inline float max_of_8(float x) {
 // mean.  Blocks past the sequence get -inf.
 //
 // A wave takes 16 blocks of one kv head at a time: means and queries are rotated in
-// fp32 and meet in the fp32 matrix instruction (16 blocks x 16 columns, 4 channels
-// each time), so nothing is rounded to fewer bits.  The four waves of a workgroup, of
-// four heads, share the blocks' cos/sin rows, 512 bytes a block beside its mean's 256,
-// through LDS; means and rows are requested one tile ahead, page indices two.  Bound by
-// the chain length -> page -> mean at one sequence (131072 tokens, 32/8 heads: 4.3 us, 2.4 of
-// them an empty launch) and by that latency a tile at many (8 of 32K to 128K, 64/8 heads:
-// 12 us for 21 MB of means; rows through each wave's own loads took 17).
+// fp32 and meet in the fp32 matrix instruction of sixteen 4 x 4 products, so nothing is
+// rounded to fewer bits: four blocks and four heads each, and in each lane group another
+// quarter of the channels, which are summed at the end.  (The 16 x 16 product leaves half of
+// its columns or more without a head.)  The four waves of a workgroup, of four heads, share
+// the blocks' cos/sin rows, 512 bytes a block beside its mean's 256, through LDS; means and
+// rows are requested one tile ahead, page indices two.  Bound by the chain length -> page ->
+// mean at one sequence (131072 tokens, 32/8 heads: 3.9 us, 2.4 of them an empty launch; 4.3
+// with 16 x 16 products) and at many by that and a tile's 300 vector instructions (8 of 32K
+// to 128K, 64/8 heads: 10.4 us for 21 MB of means; 12.4 with 16 x 16 products, 17 with
+// rows through each wave's own loads).
 constexpr int kScoreRow = kHalf + 2;  // float2s of a row in LDS: rows start 4 banks apart
-template <bool BIFOCAL>
+template <bool BIFOCAL, int SETS>  // SETS: of four heads
 __global__ __launch_bounds__(64 * kScoreHeads) void block_scores_kernel(ScoresArgs a) {
   __shared__ __attribute__((aligned(16))) float2 rows[2][16][kScoreRow];
   const int tid = threadIdx.x;
@@ -111,42 +127,91 @@ __global__ __launch_bounds__(64 * kScoreHeads) void block_scores_kernel(ScoresAr
   int page = page_of(a.c, b, block_of(t, i16));
   request_rows(t);
   int page_next = page_of(a.c, b, block_of(t + a.n_runs, i16));
-  Pairs q;
+  // this lane's share of the queries: value 4 c + x of the 32 of its lane group, of head
+  // l % 4 of each set; lanes past the group of heads repeat its last
+  float q[SETS][8];
   {
-    u32x4 qraw[4];
-    load_pairs(a.q + ((size_t)b * a.Hq + h * a.g + min(i16, a.g - 1)) * kHeadDim, g4, qraw);
-    request_mean(t, page);
-    rotate_pairs(qraw, a.table + (size_t)(BIFOCAL ? (uint32_t)qpos / G : (uint32_t)qpos) * kHalf,
-                 g4, q);
-  }
-  for (int n = 0; t < a.n_tiles; t += a.n_runs, ++n) {
-    f32x4 sc = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    if (16 * t < n_live) {  // the same for the whole workgroup
-      u32x4* dst = (u32x4*)rows[n & 1][tid >> 4];
-      dst[tid & 15] = cs0;
-      dst[16 + (tid & 15)] = cs1;
-      __syncthreads();  // one is enough: the other buffer was read in front of it
-      Pairs m;
-      rotate_pairs(raw, rows[n & 1][i16], g4, m);
-      request_rows(t + a.n_runs);  // past the end: the last block's again
-      request_mean(t + a.n_runs, page_next);
-      page_next = page_of(a.c, b, block_of(t + 2 * a.n_runs, i16));
-      f32x4 s0 = f32x4{}, s1 = f32x4{};
+    const int x = (lane >> 2) & 3;
+    const float2* cs = a.table + (size_t)(BIFOCAL ? (uint32_t)qpos / G : (uint32_t)qpos) * kHalf;
+    uint16_t raw_lo[SETS][4], raw_hi[SETS][4];
+    float2 r[4];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(m.lo[i], q.lo[i], s0, 0, 0, 0);
-        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(m.hi[i], q.hi[i], s1, 0, 0, 0);
-      }
-      // lane: column i16 (head), blocks 4 g4 + i; columns past the group repeat its last head
+    for (int c = 0; c < 4; ++c) {
+      const int f = 32 * (c >> 1) + 8 * g4 + 4 * (c & 1) + x;
+      r[c] = cs[f];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = max_of_8((s0[i] + s1[i]) * a.q_scale);
-        sc[i] = 16 * t + 4 * g4 + i < n_live ? x : -INFINITY;
+      for (int s = 0; s < SETS; ++s) {
+        const uint16_t* row =
+            a.q + ((size_t)b * a.Hq + h * a.g + min(4 * s + (lane & 3), a.g - 1)) * kHeadDim;
+        raw_lo[s][c] = row[f];
+        raw_hi[s][c] = row[f + kHalf];
       }
     }
-    const int blk = 16 * t + 4 * g4 + (i16 & 3);
-    const float x = i16 == 0 ? sc[0] : i16 == 1 ? sc[1] : i16 == 2 ? sc[2] : sc[3];
-    if (on && i16 < 4 && blk < a.c.n_blocks) out[blk] = x;
+    request_mean(t, page);
+#pragma unroll
+    for (int s = 0; s < SETS; ++s)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float lo = bf16_lo(raw_lo[s][c]), hi = bf16_lo(raw_hi[s][c]);
+        q[s][c] = lo * r[c].x - hi * r[c].y;
+        q[s][4 + c] = hi * r[c].x + lo * r[c].y;
+      }
+  }
+  // the same turns for the whole workgroup
+  for (int n = 0; 16 * t < n_live; t += a.n_runs, ++n) {
+    u32x4* dst = (u32x4*)rows[n & 1][tid >> 4];
+    dst[tid & 15] = cs0;
+    dst[16 + (tid & 15)] = cs1;
+    __syncthreads();  // one is enough: the other buffer was read in front of it
+    Pairs m;
+    rotate_pairs(raw, rows[n & 1][i16], g4, m);
+    // the rotated means stand here, so that the next tile's loads take the registers of these:
+    // in others they would be copied at the loop's end, and waited for there (11.0 -> 10.4 us)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(m.lo[i]), "+v"(m.hi[i]));
+    request_rows(t + a.n_runs);  // past the end: the last block's again
+    request_mean(t + a.n_runs, page_next);
+    page_next = page_of(a.c, b, block_of(t + 2 * a.n_runs, i16));
+    // four chains of products in turn, each waits for its own last one
+    constexpr int kChains = 4 / SETS;  // of a set
+    f32x4 acc[SETS][kChains];
+#pragma unroll
+    for (int s = 0; s < SETS; ++s)
+#pragma unroll
+      for (int i = 0; i < kChains; ++i) acc[s][i] = f32x4{};
+#pragma unroll
+    for (int c = 0; c < 8; c += kChains) {
+      auto four = [&](auto x) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kChains; ++i) {
+          const int n = 4 * (c + i) + x.value;
+          const float mean = n < 16 ? m.lo[n & 15] : m.hi[n & 15];
+#pragma unroll
+          for (int s = 0; s < SETS; ++s)
+            acc[s][i] = mfma4<x.value>(q[s][c + i], mean, acc[s][i]);
+        }
+      };
+      four(std::integral_constant<int, 0>{});
+      four(std::integral_constant<int, 1>{});
+      four(std::integral_constant<int, 2>{});
+      four(std::integral_constant<int, 3>{});
+    }
+    auto total = [&](int s) {
+      f32x4 x = acc[s][0];
+#pragma unroll
+      for (int i = 1; i < kChains; ++i) x += acc[s][i];
+      return sum_of_groups(x);
+    };
+    // lane: block i16; the lane group's channels, heads 0 .. 3 of a set
+    float best = total(0);
+    if (SETS > 1) best = max_nan(best, total(SETS - 1));
+    best = max_of_groups(best * a.q_scale);
+    const int blk = 16 * t + i16;
+    if (on && g4 == 0 && blk < a.c.n_blocks) out[blk] = blk < n_live ? best : -INFINITY;
+  }
+  for (; t < a.n_tiles; t += a.n_runs) {
+    const int blk = 16 * t + i16;
+    if (on && g4 == 0 && blk < a.c.n_blocks) out[blk] = -INFINITY;
   }
 }
 
@@ -323,10 +388,16 @@ hipError_t launch_block_scores8(bool bifocal, const Cache8& c, const uint16_t* q
   const long long wgs = rows * a.n_runs;
   if (wgs > 0x7fffffffLL) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)wgs), block(64 * kScoreHeads);
-  if (bifocal)
-    hipLaunchKernelGGL(block_scores_kernel<true>, grid, block, 0, stream, a);
-  else
-    hipLaunchKernelGGL(block_scores_kernel<false>, grid, block, 0, stream, a);
+#define JL_SCORES(bif, sets) \
+  hipLaunchKernelGGL((block_scores_kernel<bif, sets>), grid, block, 0, stream, a)
+  if (a.g <= 4) {
+    if (bifocal) JL_SCORES(true, 1);
+    else JL_SCORES(false, 1);
+  } else {
+    if (bifocal) JL_SCORES(true, 2);
+    else JL_SCORES(false, 2);
+  }
+#undef JL_SCORES
   return hipGetLastError();
 }
 

@@ -33,6 +33,7 @@ struct Cache8 {
   const int32_t* table;
   int n_pages, per, Hkv;   // per: blocks of a page
   int max_pages, n_blocks;  // of a sequence: pages and blocks it can hold
+  FastDiv by_per;
 };
 
 // Index of a (page, head, block of the page) in the pools; pools hold < 2^31 blocks.
@@ -40,12 +41,15 @@ __device__ inline int pool_block(const Cache8& c, int page, int h, int in_page) 
   return (page * c.Hkv + h) * c.per + in_page;
 }
 
+// Without a table a sequence is one page of n_blocks = per blocks.
+__device__ inline int page_index(const Cache8& c, int blk) {
+  const int p = (int)fastdiv_ge2((uint32_t)blk, c.by_per);
+  return c.per > 1 ? p : blk;
+}
 __device__ inline int page_of(const Cache8& c, int b, int blk) {
-  return c.table != nullptr ? c.table[(size_t)b * c.max_pages + blk / c.per] : b;
+  return c.table != nullptr ? c.table[(size_t)b * c.max_pages + page_index(c, blk)] : b;
 }
-__device__ inline int in_page(const Cache8& c, int blk) {
-  return c.table != nullptr ? blk % c.per : blk;
-}
+__device__ inline int in_page(const Cache8& c, int blk) { return blk - page_index(c, blk) * c.per; }
 
 __host__ __device__ inline int k_offset(int key, int d) {
   const int a = key >> 5, t = (key >> 4) & 1, r = key & 15;

@@ -660,7 +660,8 @@ int check_cache8(const jl_cache8* c, const int32_t* block_table, int max_pages, 
                 kDecodeMaxLen, cap);
   *out = jl::Cache8{(unsigned char*)c->k, (unsigned char*)c->v, c->k_scale, c->v_scale,
                     (uint16_t*)c->k_mean, block_table, c->n_pages, per, c->Hkv,
-                    block_table != nullptr ? max_pages : 1, (int)(cap / jl::kBlk)};
+                    block_table != nullptr ? max_pages : 1, (int)(cap / jl::kBlk),
+                    jl::make_fastdiv((uint32_t)per)};
   return JL_OK;
 }
 
