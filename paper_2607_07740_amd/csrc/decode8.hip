@@ -42,8 +42,11 @@ struct Decode8Args {
 
 // The (sequence, kv head) pairs are segments of a list, each as long as its steps of
 // 64 keys and kD8SegCost empty ones, and workgroup w takes the w-th of n equal
-// ranges.  Two workgroups that share a segment meet in its counter: the first's
+// ranges.  Workgroups that share a segment meet in its counter: the first's
 // index names it, since only a range's last segment goes on in the next range.
+// Where they merge in two steps, that is the first group's; the others' are in a
+// second row of counters, where one workgroup is a further one of one segment at
+// most, and the groups meet in the second workgroup's, whom no group begins with.
 struct Segments {
   uint32_t q, r;  // entries per range, and ranges (the first ones) with one more
   int n;             // ranges
