@@ -166,13 +166,15 @@ __global__ void offset_rows_kernel(const float2* table, unsigned char* out) {
 
 // What a call's workgroups share out: the steps of a batch's sequences, those of one
 // sequence, or lists of blocks.
-enum Decode8Mode : int { kBatch8 = 0, kOne8 = 1, kListed8 = 2 };
+enum Decode8Mode : int { kBatch8 = 0, kOne8 = 1, kListed8 = 2, kWideList8 = 3 };
 // Waves of a workgroup.  One sequence: eight and a workgroup per CU leave half the states
 // to merge, which one workgroup per kv head reads at a CU's own rate (131072 keys, 32/8
 // heads: 54.6 -> 51.3 us; 32768 21.6 -> 19.4; 1999 keys, 16/8 heads 11.6 -> 11.8).
 // Otherwise four, two workgroups per CU, one of which streams while the other merges
 // (256 sequences of 0.2K to 2K: 124 -> 111 us; 128 listed blocks 14.6 -> 14.2).
-__host__ __device__ constexpr int decode8_waves(int mode) { return mode == kOne8 ? 8 : 4; }
+__host__ __device__ constexpr int decode8_waves(int mode) {
+  return mode == kOne8 || mode == kWideList8 ? 8 : 4;
+}
 
 template <int kD8Waves>
 struct __attribute__((aligned(1024))) Decode8Smem {
@@ -216,7 +218,7 @@ template <bool BIFOCAL, int MODE>
 __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(Decode8Args a) {
   constexpr int kD8Waves = decode8_waves(MODE);
   constexpr int kD8Threads = 64 * kD8Waves;
-  constexpr bool LISTED = MODE == kListed8;
+  constexpr bool LISTED = MODE == kListed8 || MODE == kWideList8;
   __shared__ Decode8Smem<kD8Waves> sm;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -237,7 +239,7 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
   // Segments of one length, no more than workgroups: each gets the same number of them, and
   // no workgroup works on two.
   const int segs = a.B * a.c.Hkv;
-  const bool even = MODE == kOne8 || (LISTED && segs <= a.n_wg);
+  const bool even = MODE == kOne8 || MODE == kWideList8 || (LISTED && segs <= a.n_wg);
   int first_wg = 0, parts = 0;
   if (even) {
     const int per = a.n_wg / segs;
@@ -814,23 +816,30 @@ hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, cons
                           const void* offsets, int B, int Hq, int w_pre, int w0, void* ws,
                           hipStream_t stream) {
   static_assert(2 * kD8MaxWg <= kD8Counters, "two counters per workgroup");
-  // one sequence: at least four workgroups for each of its heads
-  const int mode = blocks != nullptr ? kListed8 : B == 1 && c.Hkv <= 64 ? kOne8 : kBatch8;
+  // One sequence: at least four workgroups for each of its heads.  Lists, where there is one for
+  // each of most CUs: a workgroup for each, and no state to merge (256 lists of 32 blocks 30.6 us
+  // in four waves and two workgroups, 26.5; 136 of 64 34.1, 32.6; but 512 of 32 48.5, 53).
+  const int cus = std::min(cu_count(), kD8MaxWg / 2);
+  const long long segs = (long long)B * c.Hkv;
+  const int mode = blocks == nullptr ? (B == 1 && c.Hkv <= 64 ? kOne8 : kBatch8)
+                                     : (2 * segs > cus && segs <= cus ? kWideList8 : kListed8);
   const int waves = decode8_waves(mode);
   const int per_cu = 8 / waves;  // registers for two waves per SIMD
   Decode8Args a{c, q, kv_lens, blocks, o, table, (const unsigned char*)offsets, (int*)ws,
                 (float*)ws + kD8Counters, B, Hq, Hq / c.Hkv, n_select,
-                std::max(per_cu * std::min(cu_count(), kD8MaxWg / 2), mode == kOne8 ? c.Hkv : 1),
+                std::max(per_cu * cus, mode == kOne8 ? c.Hkv : 1),
                 w_pre, w0, 2 * waves / (Hq / c.Hkv), 256 / (Hq / c.Hkv),
                 1.4426950408889634f / sqrtf((float)kHeadDim)};
   const dim3 grid(a.n_wg), block(64 * waves);
 #define JL_DECODE8(bif, m) hipLaunchKernelGGL((decode8_kernel<bif, m>), grid, block, 0, stream, a)
   if (bifocal) {
     if (mode == kListed8) JL_DECODE8(true, kListed8);
+    else if (mode == kWideList8) JL_DECODE8(true, kWideList8);
     else if (mode == kOne8) JL_DECODE8(true, kOne8);
     else JL_DECODE8(true, kBatch8);
   } else {
     if (mode == kListed8) JL_DECODE8(false, kListed8);
+    else if (mode == kWideList8) JL_DECODE8(false, kWideList8);
     else if (mode == kOne8) JL_DECODE8(false, kOne8);
     else JL_DECODE8(false, kBatch8);
   }

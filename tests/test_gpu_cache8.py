@@ -616,6 +616,33 @@ def test_decode_over_more_lists_than_workgroups(B, n_select):
                 assert (np.abs(got[b, i] - want) <= np.abs(want) * C.UBF * (1 + 2.0 ** -14)).all()
 
 
+@pytest.mark.parametrize("B,Hkv,g,per,n_select", [(33, 4, 2, 1, 3), (43, 3, 7, 0, 20), (256, 1, 8, 2, 1),
+                                                  (64, 4, 1, 0, 9), (64, 4, 4, 2, 70),
+                                                  (65, 2, 5, 1, 16)])
+def test_decode_over_a_list_for_every_compute_unit(B, Hkv, g, per, n_select):
+    """Some 129 to 256 lists: short and long ones, with entries outside the sequences, in both
+    rotations."""
+    rng = np.random.default_rng(B + g)
+    nb = 8
+    lens = rng.integers(0, nb * 64 + 1, B)
+    lens[:4] = [0, 1, 64, nb * 64]
+    m = filled(rng, B, nb, Hkv, list(lens))
+    table = None
+    if per:
+        table, n_pages = paged(B, nb // per, 1, B)
+    cache = upload(C.pools(m, table, *((n_pages, per, 0x7f) if per else ())))
+    q = normals(rng, B, g * Hkv, C.D)
+    blocks = rng.integers(-2, nb + 2, (B, Hkv, n_select)).astype(np.int32)
+    blocks[5], blocks[6, 0] = -1, 0
+    for bif in (True, False):
+        say("decode8_blocks of %d lists of %d, g=%d, per=%d, bifocal=%s" % (B * Hkv, n_select, g, per, bif))
+        want, bound = C.decode(q, m, lens, 100, 70, bif, blocks)
+        out = api.decode8_blocks(dev(q), cache, ints(lens), ints(blocks), w_pretrained=100,
+                                 w_local=70, bifocal=bif, block_table=ints(table) if per else None)
+        check(out, want, bound, "lists")
+        assert bool((out[0] == 0).all()) and bool((out[5] == 0).all())
+
+
 # ------------------------------------------------------------------ together
 def _serving(Hq=8, Hkv=2, n0=300, steps=5, w_pre=128, w0=64, seed=0):
     rng = np.random.default_rng(seed)
