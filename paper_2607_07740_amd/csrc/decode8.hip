@@ -474,6 +474,7 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
       };
 
       f16x8 p[2];
+      float weight;  // of the step's sums in the column's
       auto softmax = [&](float ks) __attribute__((always_inline)) {
         // ---- each column keeps the keys of its own view; lane: keys 16 t + 4 g4 + i
         const uint32_t dist = (uint32_t)(qpos - k0 - 4 * g4) - (uint32_t)keep_lo;
@@ -490,28 +491,32 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
         // score stays -inf
         const float f = __builtin_amdgcn_fmed3f(ks * q_back, 0x1p-126f, 0x1p126f);
         mt = max_over_groups(mt) * f;
-        // The reference lies kD8Up below the maximum: weights are at most 2^15, and fp16 holds
-        // 2^-29 .. 1 of the largest to 11 bits and 2^-39 of it at all.  (A maximum whose
-        // last bit is above 1 is the reference itself.)  The sum is that of the rounded
-        // weights.
+        // A step's weights are taken against a reference of its own, kD8Up below its maximum: they
+        // are at most 2^15, and fp16 holds 2^-29 .. 1 of the step's largest to 11 bits and 2^-39
+        // of it at all.  (A maximum whose last bit is above 1 is the reference itself: 2^-14 and
+        // 2^-24 of it.)  Against the column's maximum so far, whole blocks of small weights would
+        // be lost beside one large, and their values may be as much larger; the step's sums enter
+        // the column's in fp32, by `weight`.  The sum is that of the rounded weights.
         mt = fabsf(mt) < 0x1p22f ? mt - kD8Up : mt;
         const float m_new = fmaxf(m_run, mt);
         const float m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float m_step = mt == -INFINITY ? 0.f : mt;
         const float alpha = m_new == m_run ? 1.f : fast_exp2(m_run - m_use);
+        weight = m_new == mt ? 1.f : fast_exp2(mt - m_use);
         float l = 0.f;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const f16x2 one = {(_Float16)1.f, (_Float16)1.f};
 #pragma unroll
           for (int i = 0; i < 4; i += 2) {
-            const f16x2 pp = {(_Float16)fast_exp2(__builtin_fmaf(sc[t][i], f, -m_use)),
-                              (_Float16)fast_exp2(__builtin_fmaf(sc[t][i + 1], f, -m_use))};
+            const f16x2 pp = {(_Float16)fast_exp2(__builtin_fmaf(sc[t][i], f, -m_step)),
+                              (_Float16)fast_exp2(__builtin_fmaf(sc[t][i + 1], f, -m_step))};
             l = __builtin_amdgcn_fdot2(pp, one, l, false);
             p[t >> 1][4 * (t & 1) + i] = pp[0];
             p[t >> 1][4 * (t & 1) + i + 1] = pp[1];
           }
         }
-        l_run = l_run * alpha + l;
+        l_run = l_run * alpha + l * weight;
         m_run = m_new;
         if (__ballot(alpha != 1.f) != 0) {  // most steps leave every maximum alone
 #pragma unroll
@@ -538,7 +543,7 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
             }
         }
         // a step without a block holds some other block's scale, perhaps no number
-        const float up = LISTED && !on ? 0.f : vs * kD8Down;
+        const float up = LISTED && !on ? 0.f : vs * kD8Down * weight;
         vs = a.c.v_scale[phys];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
