@@ -205,7 +205,7 @@ struct __attribute__((aligned(1024))) Decode8Smem {
 // conversion and two packed fp16 instructions and goes to the matrix cores as
 // it is: e4m3 numbers are exact in fp16, and with |x| <= 448 none overflows.  The
 // block's scale of K multiplies the scores, that of V the step's product.
-// The query is brought to [1, 2) by a power of two first, its own range aside.
+// The query is brought to fp16's upper range by a power of two first, its own range aside.
 //
 // Bound by memory where keys are many: 8 sequences of 32K to 128K, 32/8 heads 210 us, 1.34 GB
 // at 6.4 TB/s (the loads alone 6.4 to 6.9); one of 1048576 320 us, 6.7; of 131072 48.8 us, 5.5;
@@ -359,7 +359,9 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
       float m_run = -INFINITY, l_run = 0.f;
 
       // the column's query in fp32, pairs 32 u + 8 g4 + j, scaled by log2(e) / sqrt(d) and by
-      // the power of two that brings its largest value to [1, 2)
+      // the power of two that brings its largest value to [2^16, 2^17): rotated, it is at most
+      // 0.1276 sqrt(2) 2^17 = 23700, which fp16 holds, and so it does the values down to 2^-27 of
+      // the largest to 11 bits and to 2^-37 at all
       float qlo[16], qhi[16];
       float q_back;  // what undoes the latter
 
@@ -588,7 +590,7 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, fmaxf(fabsf(qlo[i]), fabsf(qhi[i])));
         top = max_over_groups(top);
-        const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
+        const int e = max((int)(__float_as_uint(top) >> 23) - 127 - 16, -126);
         const float down = pow2f(-e);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {

@@ -102,3 +102,28 @@ def test_small_weights_on_large_values(B, Hkv, nb, n_select):
         want, bound = attend(q[b, h], kd[at, h].reshape(-1, C.D), vd[at, h].reshape(-1, C.D), pos,
                              lens[b], 700, 500)
         within(out[b, h], want, bound, "sequence %d head %d" % (b, h))
+
+
+@pytest.mark.parametrize("bits", [20, 26])
+def test_small_channels_of_a_query_count(bits):
+    """One channel of the query is 2^bits above the others, and the keys are zero there: the scores
+    come from the others alone."""
+    rng = np.random.default_rng(bits)
+    B, Hkv, nb = 2, 2, 6
+    q = normals(rng, B, Hkv, C.D)
+    q[..., 5] = 2.0 ** bits
+    k = normals(rng, B * nb, Hkv, C.BLOCK, C.D) * 2.0
+    k[..., 5] = k[..., 69] = 0
+    v = normals(rng, B * nb, Hkv, C.BLOCK, C.D)
+    table = rng.permutation(B * nb).reshape(B, nb)
+    cache, kd, vd, _ = block_pages(k, v, Hkv)
+    lens = [nb * 64, 201]
+    say("small channels", bits)
+    out = api.decode8(dev(q), cache, ints(lens), w_pretrained=150, w_local=60,
+                      block_table=ints(table + 1)).double().cpu().numpy()
+    for b in range(B):
+        for h in range(Hkv):
+            at = table[b, :-(-lens[b] // 64)]
+            want, bound = attend(q[b, h], kd[at, h].reshape(-1, C.D), vd[at, h].reshape(-1, C.D),
+                                 np.arange(64 * len(at)), lens[b], 150, 60)
+            within(out[b, h], want, bound, "sequence %d head %d" % (b, h))
