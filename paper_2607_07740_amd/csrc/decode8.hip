@@ -813,10 +813,8 @@ size_t decode8_workspace_bytes(int g) {
   return kD8Counters * sizeof(int) + (size_t)2 * kD8MaxWg * g * kD8State * sizeof(float);
 }
 
-// list entries of a call: they must stay below 2^31
-long long decode8_entries(int B, int Hkv, int n) {
-  return (long long)B * Hkv * ((long long)n + kD8SegCost);
-}
+// list entries of a segment of n steps: those of a call must stay below 2^31
+long long decode8_entries(int n) { return (long long)n + kD8SegCost; }
 
 hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, const int32_t* kv_lens,
                           const int32_t* blocks, int n_select, uint16_t* o, const float2* table,

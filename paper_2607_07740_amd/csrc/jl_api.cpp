@@ -68,7 +68,7 @@ hipError_t launch_append8(const Cache8& c, const uint16_t* k, const uint16_t* v,
 hipError_t launch_read8(const Cache8& c, uint16_t* k, uint16_t* v, int B, int start, int n,
                         hipStream_t stream);
 size_t decode8_workspace_bytes(int g);
-long long decode8_entries(int B, int Hkv, int n);
+long long decode8_entries(int n);
 hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, const int32_t* kv_lens,
                           const int32_t* blocks, int n_select, uint16_t* o, const float2* table,
                           const void* offsets, int B, int Hq, int w_pre, int w0, void* ws,
@@ -135,6 +135,9 @@ int hip_fail(hipError_t e, const char* what) {
 
 bool aligned16(const void* p) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 bool aligned4(const void* p) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+
+// a * b * c > 2^31 - 1 for positive a, b, c < 2^32: the product of three need not fit 64 bits
+bool past_int32(long long a, long long b, long long c) { return a * b > 0x7fffffffLL / c; }
 
 // ------------------------------------------------------------ table cache
 // A table of cap positions is one allocation: cap x 64 fp32 (cos, sin) pairs
@@ -644,7 +647,7 @@ int check_cache8(const jl_cache8* c, const int32_t* block_table, int max_pages, 
   if (!aligned4(c->k_scale) || !aligned4(c->v_scale))
     return fail(JL_ERR_INVALID_ARG, "the cache's scales must be non-null and 4-byte aligned");
   const int per = c->page_size / jl::kBlk;
-  if ((long long)c->n_pages * c->Hkv * per > 0x7fffffffLL)
+  if (past_int32(c->n_pages, c->Hkv, per))
     return fail(JL_ERR_UNSUPPORTED, "a cache holds fewer than 2^31 blocks");
   long long cap = c->page_size;
   if (block_table != nullptr) {
@@ -694,7 +697,7 @@ int decode8_common(bool bifocal, const jl_cache8* cache, const int32_t* block_ta
     if (!aligned4(blocks)) return fail(JL_ERR_INVALID_ARG, "blocks must be non-null and aligned");
     if (n_select < 1) return fail(JL_ERR_INVALID_ARG, "n_select must be >= 1 (got %d)", n_select);
   }
-  if (jl::decode8_entries(B, c.Hkv, std::max(c.n_blocks, listed ? n_select : 0)) > 0x7fffffffLL)
+  if (past_int32(B, c.Hkv, jl::decode8_entries(std::max(c.n_blocks, listed ? n_select : 0))))
     return fail(JL_ERR_INVALID_ARG, "problem too large");
   const size_t need = jl::decode8_workspace_bytes(Hq / c.Hkv);
   if (ws == nullptr || ws_bytes < need)
@@ -719,7 +722,7 @@ int block_scores8(bool bifocal, const jl_cache8* cache, const int32_t* block_tab
   if (st == JL_OK) st = check_query8(c, q, kv_lens, Hq, theta, bifocal, w_pre);
   if (st != JL_OK) return st;
   if (!aligned4(scores)) return fail(JL_ERR_INVALID_ARG, "scores must be non-null and aligned");
-  if ((long long)B * c.Hkv * c.n_blocks > 0x7fffffffLL)
+  if (past_int32(B, c.Hkv, c.n_blocks))
     return fail(JL_ERR_INVALID_ARG, "problem too large");
   Tables tab{};
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
@@ -1090,7 +1093,7 @@ int jl_select_blocks(const float* scores, const int32_t* kv_lens, int32_t* block
     return fail(JL_ERR_INVALID_ARG,
                 "n_select (%d) must hold the first n_first blocks and those of the band (%lld)",
                 n_select, always);
-  if ((long long)B * Hkv * std::max(n_blocks, n_select) > 0x7fffffffLL)
+  if (past_int32(B, Hkv, std::max(n_blocks, n_select)))
     return fail(JL_ERR_INVALID_ARG, "problem too large");
   const hipError_t e = jl::launch_select_blocks(scores, kv_lens, blocks, B, Hkv, n_blocks, n_select,
                                                 w_local, n_first,
