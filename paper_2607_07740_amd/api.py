@@ -551,7 +551,9 @@ class Cache8:
     """The pools of an 8-bit cache (jl_cache8): k, v uint8 [n_pages, Hkv, page_size, 128],
     k_scale, v_scale fp32 [n_pages, Hkv, page_size // 64], k_mean bf16 [n_pages, Hkv,
     page_size // 64, 128], contiguous on one device.  cache8_alloc makes an empty one.
-    Without a block table page b is sequence b."""
+    Without a block table page b is sequence b.  The library gets the addresses that the
+    tensors have here, so nothing of a Cache8 can be replaced, and a call on one whose tensors
+    have moved since (resize_, set_) is refused."""
 
     def __init__(self, k, v, k_scale, v_scale, k_mean):
         torch = _t()
@@ -565,11 +567,19 @@ class Cache8:
                 _dev(k_scale, "k_scale", torch.float32, blocks, k.device),
                 _dev(v_scale, "v_scale", torch.float32, blocks, k.device),
                 _dev(k_mean, "k_mean", torch.bfloat16, blocks + (D,), k.device)]
-        self.k, self.v, self.k_scale, self.v_scale, self.k_mean = k, v, k_scale, v_scale, k_mean
-        self.n_pages, self.page_size, self.Hkv, self.head_dim = n_pages, page_size, Hkv, D
-        self.device, self.index = k.device, k.get_device()
-        self._struct = _Cache8Struct(*ptrs, n_pages, page_size, Hkv, D)
-        self._ref = ctypes.cast(ctypes.pointer(self._struct), ctypes.c_void_p)
+        struct = _Cache8Struct(*ptrs, n_pages, page_size, Hkv, D)
+        self.__dict__.update(
+            k=k, v=v, k_scale=k_scale, v_scale=v_scale, k_mean=k_mean, n_pages=n_pages,
+            page_size=page_size, Hkv=Hkv, head_dim=D, device=k.device, index=k.get_device(),
+            _struct=struct, _ref=ctypes.cast(ctypes.pointer(struct), ctypes.c_void_p),
+            _ptrs=tuple(ptrs),
+            _now=tuple(t.data_ptr for t in (k, v, k_scale, v_scale, k_mean)))
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a Cache8 cannot be changed (%s): make another one" % name)
+
+    def __delattr__(self, name):
+        raise AttributeError("a Cache8 cannot be changed (%s): make another one" % name)
 
 
 def cache8_alloc(n_pages: int, page_size: int, Hkv: int, *, head_dim: int = 128,
@@ -650,6 +660,9 @@ def _cache8(cache, block_table, B):
     """The checks of a call of B sequences on a cache -> (jl_cache8 pointer, table pointer,
     max_pages, capacity)."""
     _current(cache.index, cache.device, "cache")
+    k, v, k_scale, v_scale, k_mean = cache._now
+    if (k(), v(), k_scale(), v_scale(), k_mean()) != cache._ptrs:
+        raise ValueError("the cache's tensors have moved since it was made")
     if block_table is None:
         if B > cache.n_pages:
             raise ValueError("a dense cache of %d sequences cannot hold %d" % (cache.n_pages, B))

@@ -1,0 +1,89 @@
+"""The Python side of the 8-bit calls, on the CPU: tensors of host memory, and a library that only
+notes which entry point it was given what."""
+import pytest
+
+from paper_2607_07740_amd import api
+
+torch = pytest.importorskip("torch")
+BF = torch.bfloat16
+
+
+class Noting:
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def entry(*args):
+            self.calls.append((name, args))
+            return 4096 if name.endswith("_bytes") else api.JL_OK
+        return entry
+
+    def launches(self):
+        return [c for c in self.calls if not c[0].endswith("_bytes")]
+
+
+@pytest.fixture
+def library(monkeypatch):
+    note = Noting()
+    monkeypatch.setattr(api, "lib", lambda: note)
+    monkeypatch.setattr(api, "_dev", lambda t, *a: t.data_ptr())
+    monkeypatch.setattr(api, "_current", lambda *a: None)
+    monkeypatch.setattr(api, "_stream", lambda stream: 0)
+    return note
+
+
+def ints(*x):
+    return torch.tensor(x, dtype=torch.int32)
+
+
+def calls(cache, kw=None):
+    """Every call on a cache, by name; kw changes arguments of those that have them."""
+    rows, q, lens = torch.zeros((2, 3, 2, 128), dtype=BF), torch.zeros((2, 4, 128), dtype=BF), ints(5, 6)
+    blocks = torch.zeros((2, 2, 3), dtype=torch.int32)
+    kw = kw or {}
+
+    def args(*names, **own):
+        return dict(own, **{n: kw[n] for n in names if n in kw})
+    return {
+        "append": lambda: api.cache8_append(cache, rows, rows, lens),
+        "read": lambda: api.cache8_read(cache, **args("n", "start", n=7)),
+        "decode": lambda: api.decode8(q, cache, lens, **args("w_pretrained", "w_local")),
+        "blocks": lambda: api.decode8_blocks(q, cache, lens, blocks,
+                                             **args("w_pretrained", "w_local")),
+        "scores": lambda: api.block_scores8(q, cache, lens, **args("w_pretrained")),
+    }
+
+
+def test_a_cache_cannot_be_changed(library):
+    cache = api.cache8_alloc(2, 128, 2, device="cpu")
+    for name in ("k", "v", "k_scale", "v_scale", "k_mean", "n_pages", "page_size", "Hkv", "head_dim",
+                 "device", "index", "other"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, None)
+    with pytest.raises(AttributeError):
+        del cache.k
+    assert (cache.n_pages, cache.page_size, cache.Hkv, cache.head_dim) == (2, 128, 2, 128)
+    for name, call in calls(cache).items():
+        call()
+    assert [c[0] for c in library.launches()] == [
+        "jl_cache8_append", "jl_cache8_read", "jl_bifocal_decode8", "jl_bifocal_decode8_blocks",
+        "jl_bifocal_block_scores8"]
+
+
+@pytest.mark.parametrize("name", ["k", "v", "k_scale", "v_scale", "k_mean"])
+@pytest.mark.parametrize("how", ["resize", "set", "data", "freed"])
+def test_a_cache_whose_tensors_moved_is_refused(library, name, how):
+    cache = api.cache8_alloc(2, 128, 2, device="cpu")
+    t = getattr(cache, name)
+    if how == "resize":
+        t.resize_((100, *t.shape[1:]))
+    elif how == "set":
+        t.set_(torch.zeros_like(t))
+    elif how == "data":
+        t.data = torch.zeros_like(t)
+    else:
+        t.untyped_storage().resize_(0)
+    for call in calls(cache).values():
+        with pytest.raises(ValueError, match="moved"):
+            call()
+    assert library.launches() == []
