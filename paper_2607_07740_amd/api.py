@@ -641,6 +641,14 @@ def _current(index, device, name) -> None:
         raise ValueError("%s is on %s, the current device is cuda:%d" % (name, device, now))
 
 
+def _int(x, name) -> int:
+    """An int argument of the library: ctypes would drop the bits past 32."""
+    x = int(x)
+    if not -0x80000000 <= x <= 0x7fffffff:
+        raise ValueError("%s must fit 32 bits, got %d" % (name, x))
+    return x
+
+
 def _is_cache8(cache) -> None:
     if not isinstance(cache, Cache8):
         raise TypeError("cache must be a Cache8")
@@ -671,7 +679,7 @@ def _cache8(cache, block_table, B):
     shape = block_table.shape
     if len(shape) != 2 or shape[0] != B or shape[1] < 1:
         raise ValueError("block_table must be [B, max_pages]")
-    max_pages = shape[1]
+    max_pages = _int(shape[1], "max_pages")
     return cache._ref, table, max_pages, max_pages * cache.page_size
 
 
@@ -705,7 +713,7 @@ def cache8_read(cache, n: int, *, start: int = 0, B=None, block_table=None, k_ou
     if B is None:
         B = cache.n_pages if block_table is None else block_table.shape[0]
     ref, table, max_pages, cap = _cache8(cache, block_table, B)
-    start, n = int(start), int(n)
+    start, n, B = _int(start, "start"), _int(n, "n"), _int(B, "B")
     shape = (B, n, cache.Hkv, cache.head_dim)
     if (k_out is None or v_out is None) and 0 < n <= cap:  # the library refuses other lengths
         if k_out is None:
@@ -754,10 +762,12 @@ def _decode8(q, cache, kv_lens, blocks, w_pretrained, w_local, rope_theta, bifoc
         bp = _ints(blocks, "blocks", cache, None)
         if blocks.dim() != 3 or blocks.shape[0] != B or blocks.shape[1] != cache.Hkv:
             raise ValueError("blocks must be [B, Hkv, n_select]")
-        args = (ref, table, max_pages, qp, lens, bp, blocks.shape[2], op, B, Hq, float(rope_theta))
+        args = (ref, table, max_pages, qp, lens, bp, _int(blocks.shape[2], "n_select"), op, B, Hq,
+                float(rope_theta))
         call = L.jl_bifocal_decode8_blocks if bifocal else L.jl_rope_attention_decode8_blocks
     if bifocal:
-        _check(call(*args, int(w_pretrained), int(w_local), wp, w_bytes, _stream(stream)))
+        _check(call(*args, _int(w_pretrained, "w_pretrained"), _int(w_local, "w_local"), wp, w_bytes,
+                    _stream(stream)))
     else:
         _check(call(*args, wp, w_bytes, _stream(stream)))
     return out
@@ -800,7 +810,8 @@ def block_scores8(q, cache, kv_lens, *, w_pretrained: int = 1, rope_theta: float
     args = (ref, table, max_pages, qp, _ints(kv_lens, "kv_lens", cache, (B,)), op, B, Hq,
             float(rope_theta))
     if bifocal:
-        _check(lib().jl_bifocal_block_scores8(*args, int(w_pretrained), _stream(stream)))
+        _check(lib().jl_bifocal_block_scores8(*args, _int(w_pretrained, "w_pretrained"),
+                                              _stream(stream)))
     else:
         _check(lib().jl_rope_block_scores8(*args, _stream(stream)))
     return out
@@ -818,7 +829,8 @@ def select_blocks(scores, kv_lens, n_select: int, *, w_local: int, n_first: int 
     B, Hkv, n_blocks = scores.shape
     index, device = scores.get_device(), scores.device
     _current(index, device, "scores")
-    n_select = int(n_select)
+    n_blocks, n_select = _int(n_blocks, "n_blocks"), _int(n_select, "n_select")
+    w_local, n_first = _int(w_local, "w_local"), _int(n_first, "n_first")
     if out is None:
         if n_select < 1:
             raise ValueError("n_select must be >= 1")
@@ -828,7 +840,7 @@ def select_blocks(scores, kv_lens, n_select: int, *, w_local: int, n_first: int 
         op = _on8(out, "out", torch.int32, (B, Hkv, n_select), index, device)
     _check(lib().jl_select_blocks(
         ptr, _on8(kv_lens, "kv_lens", torch.int32, (B,), index, device), op, B, Hkv, n_blocks,
-        n_select, int(w_local), int(n_first), _stream(stream)))
+        n_select, w_local, n_first, _stream(stream)))
     return out
 
 

@@ -87,3 +87,41 @@ def test_a_cache_whose_tensors_moved_is_refused(library, name, how):
         with pytest.raises(ValueError, match="moved"):
             call()
     assert library.launches() == []
+
+
+@pytest.mark.parametrize("value", [2 ** 31, 2 ** 32, 2 ** 32 + 5, 1 << 40, -2 ** 31 - 1])
+def test_integers_past_32_bits_are_refused(library, value):
+    """The library's are 32 bits: 2^32 + 5 would arrive as 5."""
+    cache = api.cache8_alloc(2, 128, 2, device="cpu")
+    for names, arg in ((("read",), "n"), (("read",), "start"), (("decode", "blocks"), "w_local"),
+                       (("decode", "blocks", "scores"), "w_pretrained")):
+        for name in names:
+            with pytest.raises(ValueError, match="32 bits"):
+                calls(cache, {arg: value})[name]()
+    scores, lens = torch.zeros((2, 2, 9)), ints(5, 6)
+    for kw in (dict(n_select=value), dict(w_local=value), dict(n_first=value)):
+        with pytest.raises(ValueError, match="32 bits"):
+            api.select_blocks(scores, lens, **dict(dict(n_select=5, w_local=0), **kw))
+    assert library.launches() == []
+
+
+def test_dimensions_past_32_bits_are_refused(library):
+    """Tensors of 2^32 + 5 entries in a dimension, which a card's memory can hold."""
+    long = 2 ** 32 + 5
+    cache = api.cache8_alloc(2, 128, 2, device="cpu")
+    q, lens = torch.zeros((1, 4, 128), dtype=BF), ints(5)
+    wide = torch.zeros((1, 1, 1), dtype=torch.int32).expand(1, 2, long)  # takes no memory
+    with pytest.raises(ValueError, match="32 bits"):
+        api.decode8_blocks(q, cache, lens, wide)
+    with pytest.raises(ValueError, match="32 bits"):
+        api.decode8(q, cache, lens, block_table=wide[:, 0])
+    with pytest.raises(ValueError, match="32 bits"):
+        api.select_blocks(torch.zeros(1, 1, 1).expand(1, 2, long), lens, 5, w_local=0)
+    assert library.launches() == []
+
+
+def test_integers_of_32_bits_arrive(library):
+    cache = api.cache8_alloc(2, 128, 2, device="cpu")
+    calls(cache, dict(w_local=2 ** 31 - 1, w_pretrained=2 ** 31 - 1))["decode"]()
+    name, args = library.launches()[0]
+    assert name == "jl_bifocal_decode8" and args.count(2 ** 31 - 1) == 2
