@@ -36,6 +36,7 @@ struct Decode8Args {
   float* states;  // [2 n_wg][g][kD8State]
   int B, Hq, g, n_select;
   int n_wg, w_pre, w0;
+  bool even;            // lists: each gets the same number of workgroups, none works on two
   int n_sets, n_merge;  // of a merge: sets of threads, and states that one workgroup takes
   float q_scale;
 };
@@ -236,10 +237,10 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
   uint32_t pos = 0;  // list entry of the current segment's first step
   uint32_t x0, x1;
   int b, h;
-  // Segments of one length, no more than workgroups: each gets the same number of them, and
+  // Segments of one length, no more than workgroups: each may get the same number of them, and
   // no workgroup works on two.
   const int segs = a.B * a.c.Hkv;
-  const bool even = MODE == kOne8 || MODE == kWideList8 || (LISTED && segs <= a.n_wg);
+  const bool even = MODE == kOne8 || MODE == kWideList8 || (LISTED && a.even);
   int first_wg = 0, parts = 0;
   if (even) {
     const int per = a.n_wg / segs;
@@ -821,19 +822,32 @@ hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, cons
                           const void* offsets, int B, int Hq, int w_pre, int w0, void* ws,
                           hipStream_t stream) {
   static_assert(2 * kD8MaxWg <= kD8Counters, "two counters per workgroup");
-  // One sequence: at least four workgroups for each of its heads.  Lists, where there is one for
-  // each of most CUs: a workgroup for each, and no state to merge (256 lists of 32 blocks 30.6 us
-  // in four waves and two workgroups, 26.5; 136 of 64 34.1, 32.6; but 512 of 32 48.5, 53).
+  // One sequence: at least four workgroups for each of its heads.
+  // Lists, where there is one for each of most CUs: a workgroup of eight waves for each, and no
+  // state to merge (256 lists of 32 blocks 31.6 us in four waves and two workgroups a list, 27.5;
+  // 200 of 128 76.5, 68.1; but 512 of 32 48.8, 53.3).  The other CUs have no work then, so long
+  // lists get three workgroups of four waves each where as many fit (136 of 512 204 -> 184 us, of
+  // 200 85.0 -> 80.3; 160 of 512 214 -> 205; 176 of 512, where two fit, would take 225 -> 255).
+  // Up to two lists a CU: a workgroup of four waves for each, none to merge, but some CUs have one
+  // and some two, so up to one and a half a CU long lists are cut into equal ranges (264 lists of
+  // 128 127 -> 98.6 us, of 512 477 -> 334; 320 of 512 490 -> 403; 360 of 180 183 -> 175; but 320
+  // of 32 39.5 -> 40.5, 440 of 512 541 -> 551).
+  // Long are lists of which idle CUs could take more than 80 steps each: the crossings lie
+  // between 45 (136 lists) and 75 (160), and between 20 (264) and 75 (360).
   const int cus = std::min(cu_count(), kD8MaxWg / 2);
   const long long segs = (long long)B * c.Hkv;
+  auto is_long = [&](long long slots) { return n_select * (slots - segs) > 80LL * cus; };
+  const bool wide = 2 * segs > cus && segs <= cus && (3 * segs > 2 * cus || !is_long(cus));
+  const bool cut = segs > 2 * cus || (segs > cus && 2 * segs <= 3 * cus && is_long(2 * cus));
   const int mode = blocks == nullptr ? (B == 1 && c.Hkv <= 64 ? kOne8 : kBatch8)
-                                     : (2 * segs > cus && segs <= cus ? kWideList8 : kListed8);
+                                     : (wide ? kWideList8 : kListed8);
   const int waves = decode8_waves(mode);
   const int per_cu = 8 / waves;  // registers for two waves per SIMD
   Decode8Args a{c, q, kv_lens, blocks, o, table, (const unsigned char*)offsets, (int*)ws,
                 (float*)ws + kD8Counters, B, Hq, Hq / c.Hkv, n_select,
                 std::max(per_cu * cus, mode == kOne8 ? c.Hkv : 1),
-                w_pre, w0, 2 * waves / (Hq / c.Hkv), 256 / (Hq / c.Hkv),
+                w_pre, w0, !cut,
+                2 * waves / (Hq / c.Hkv), 256 / (Hq / c.Hkv),
                 1.4426950408889634f / sqrtf((float)kHeadDim)};
   const dim3 grid(a.n_wg), block(64 * waves);
 #define JL_DECODE8(bif, m) hipLaunchKernelGGL((decode8_kernel<bif, m>), grid, block, 0, stream, a)
