@@ -596,26 +596,14 @@ def cache8_alloc(n_pages: int, page_size: int, Hkv: int, *, head_dim: int = 128,
                   torch.zeros(blocks + (head_dim,), dtype=torch.bfloat16, **kw))
 
 
-class _On:
-    """Allocations of a call that is given a stream come from that stream's pool, so that
-    neither their fill nor their reuse crosses streams."""
-
-    def __init__(self, stream):
-        self.ctx = _t().cuda.stream(stream)
-
-    def __enter__(self):
-        self.ctx.__enter__()
-
-    def __exit__(self, *exc):
-        self.ctx.__exit__(*exc)
-
-
 def _new(like, stream, shape, dtype, fill=False):
-    """An output (or a zeroed workspace) of a call on `stream`."""
-    if stream is not None:
-        with _On(stream):
-            return like.new_zeros(shape, dtype=dtype) if fill else like.new_empty(shape, dtype=dtype)
-    return like.new_zeros(shape, dtype=dtype) if fill else like.new_empty(shape, dtype=dtype)
+    """An output (or a zeroed workspace) of a call on `stream`: from that stream's pool, so that
+    neither its fill nor its reuse crosses streams."""
+    make = like.new_zeros if fill else like.new_empty
+    if stream is None:
+        return make(shape, dtype=dtype)
+    with _t().cuda.stream(stream):
+        return make(shape, dtype=dtype)
 
 
 def _on8(t, name, dtype, shape, index, device):
