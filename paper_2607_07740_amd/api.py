@@ -618,15 +618,18 @@ def _on8(t, name, dtype, shape, index, device):
     return _dev(t, name, dtype, shape, device)
 
 
-def _current(index, device, name) -> None:
-    """The library launches on the current device."""
+def _queue(stream, index, device, name):
+    """_stream of a call whose tensors are on device `index`: the library launches on the current
+    one, so that has to be it."""
     torch = _t()
     try:
         now = torch._C._cuda_getDevice()
+        raw = torch._C._cuda_getCurrentRawStream(now) if stream is None else stream.cuda_stream
     except AttributeError:
-        now = torch.cuda.current_device()
+        now, raw = torch.cuda.current_device(), _stream(stream)
     if index != now:
         raise ValueError("%s is on %s, the current device is cuda:%d" % (name, device, now))
+    return raw
 
 
 def _int(x, name) -> int:
@@ -637,14 +640,10 @@ def _int(x, name) -> int:
     return x
 
 
-def _is_cache8(cache) -> None:
-    if not isinstance(cache, Cache8):
-        raise TypeError("cache must be a Cache8")
-
-
 def _query8(q, cache):
     """(B, Hq, pointer) of a query over an 8-bit cache."""
-    _is_cache8(cache)
+    if not isinstance(cache, Cache8):
+        raise TypeError("cache must be a Cache8")
     ptr = _on8(q, "q", _t().bfloat16, None, cache.index, cache.device)
     shape = q.shape
     if len(shape) != 3 or shape[2] != cache.head_dim:
@@ -652,23 +651,23 @@ def _query8(q, cache):
     return shape[0], shape[1], ptr
 
 
-def _cache8(cache, block_table, B):
+def _cache8(cache, block_table, B, stream):
     """The checks of a call of B sequences on a cache -> (jl_cache8 pointer, table pointer,
-    max_pages, capacity)."""
-    _current(cache.index, cache.device, "cache")
+    max_pages, capacity, raw stream)."""
+    raw = _queue(stream, cache.index, cache.device, "cache")
     k, v, k_scale, v_scale, k_mean = cache._now
     if (k(), v(), k_scale(), v_scale(), k_mean()) != cache._ptrs:
         raise ValueError("the cache's tensors have moved since it was made")
     if block_table is None:
         if B > cache.n_pages:
             raise ValueError("a dense cache of %d sequences cannot hold %d" % (cache.n_pages, B))
-        return cache._ref, None, 0, cache.page_size
+        return cache._ref, None, 0, cache.page_size, raw
     table = _on8(block_table, "block_table", _t().int32, None, cache.index, cache.device)
     shape = block_table.shape
     if len(shape) != 2 or shape[0] != B or shape[1] < 1:
         raise ValueError("block_table must be [B, max_pages]")
     max_pages = _int(shape[1], "max_pages")
-    return cache._ref, table, max_pages, max_pages * cache.page_size
+    return cache._ref, table, max_pages, max_pages * cache.page_size, raw
 
 
 def _ints(t, name, cache, shape):
@@ -678,29 +677,31 @@ def _ints(t, name, cache, shape):
 def cache8_append(cache, k, v, starts, *, n_new=None, block_table=None, stream=None) -> None:
     """jl_cache8_append: rows k, v [B, n, Hkv, 128] bf16 to positions starts[b] .. of sequence
     b (starts int32 [B]); n_new int32 [B]: only the first n_new[b] of them."""
-    _is_cache8(cache)
+    if not isinstance(cache, Cache8):
+        raise TypeError("cache must be a Cache8")
     bf16 = _t().bfloat16
     kp = _on8(k, "k", bf16, None, cache.index, cache.device)
     shape = k.shape
     if len(shape) != 4 or shape[2] != cache.Hkv or shape[3] != cache.head_dim:
         raise ValueError("k and v must be [B, n, %d, %d]" % (cache.Hkv, cache.head_dim))
     B, n = shape[0], shape[1]
-    ref, table, max_pages, _ = _cache8(cache, block_table, B)
+    ref, table, max_pages, _, raw = _cache8(cache, block_table, B, stream)
     _check(lib().jl_cache8_append(
         ref, table, max_pages, kp, _on8(v, "v", bf16, shape, cache.index, cache.device),
         _ints(starts, "starts", cache, (B,)),
-        None if n_new is None else _ints(n_new, "n_new", cache, (B,)), B, n, _stream(stream)))
+        None if n_new is None else _ints(n_new, "n_new", cache, (B,)), B, n, raw))
 
 
 def cache8_read(cache, n: int, *, start: int = 0, B=None, block_table=None, k_out=None, v_out=None,
                 stream=None):
     """jl_cache8_read: rows start .. start + n - 1 of every sequence as bf16 (k, v), each
     [B, n, Hkv, 128].  B: sequences of a dense cache, all of them if not given."""
-    _is_cache8(cache)
+    if not isinstance(cache, Cache8):
+        raise TypeError("cache must be a Cache8")
     bf16 = _t().bfloat16
     if B is None:
         B = cache.n_pages if block_table is None else block_table.shape[0]
-    ref, table, max_pages, cap = _cache8(cache, block_table, B)
+    ref, table, max_pages, cap, raw = _cache8(cache, block_table, B, stream)
     start, n, B = _int(start, "start"), _int(n, "n"), _int(B, "B")
     shape = (B, n, cache.Hkv, cache.head_dim)
     if (k_out is None or v_out is None) and 0 < n <= cap:  # the library refuses other lengths
@@ -710,7 +711,7 @@ def cache8_read(cache, n: int, *, start: int = 0, B=None, block_table=None, k_ou
             v_out = _new(cache.k_mean, stream, shape, bf16)
     kp, vp = (None if t is None else _on8(t, name, bf16, shape, cache.index, cache.device)
               for t, name in ((k_out, "k_out"), (v_out, "v_out")))
-    _check(lib().jl_cache8_read(ref, table, max_pages, kp, vp, B, start, n, _stream(stream)))
+    _check(lib().jl_cache8_read(ref, table, max_pages, kp, vp, B, start, n, raw))
     return k_out, v_out
 
 
@@ -730,7 +731,7 @@ def _decode8(q, cache, kv_lens, blocks, w_pretrained, w_local, rope_theta, bifoc
              out, workspace, stream):
     torch = _t()
     B, Hq, qp = _query8(q, cache)
-    ref, table, max_pages, _ = _cache8(cache, block_table, B)
+    ref, table, max_pages, _, raw = _cache8(cache, block_table, B, stream)
     if out is None:
         out = _new(q, stream, q.shape, torch.bfloat16)
         op = out.data_ptr()
@@ -740,7 +741,6 @@ def _decode8(q, cache, kv_lens, blocks, w_pretrained, w_local, rope_theta, bifoc
         need = decode8_workspace_bytes(Hq, cache.Hkv, cache.head_dim)
         workspace = _new(q, stream, (max(need, 16),), torch.uint8, fill=True)
     wp = _on8(workspace, "workspace", getattr(workspace, "dtype", None), None, cache.index, cache.device)
-    w_bytes = workspace.numel() * workspace.element_size()
     lens = _ints(kv_lens, "kv_lens", cache, (B,))
     L = lib()
     if blocks is None:
@@ -754,10 +754,10 @@ def _decode8(q, cache, kv_lens, blocks, w_pretrained, w_local, rope_theta, bifoc
                 float(rope_theta))
         call = L.jl_bifocal_decode8_blocks if bifocal else L.jl_rope_attention_decode8_blocks
     if bifocal:
-        _check(call(*args, _int(w_pretrained, "w_pretrained"), _int(w_local, "w_local"), wp, w_bytes,
-                    _stream(stream)))
+        _check(call(*args, _int(w_pretrained, "w_pretrained"), _int(w_local, "w_local"), wp,
+                    workspace.nbytes, raw))
     else:
-        _check(call(*args, wp, w_bytes, _stream(stream)))
+        _check(call(*args, wp, workspace.nbytes, raw))
     return out
 
 
@@ -788,7 +788,7 @@ def block_scores8(q, cache, kv_lens, *, w_pretrained: int = 1, rope_theta: float
     of every block's mean key, -inf past the sequence."""
     torch = _t()
     B, Hq, qp = _query8(q, cache)
-    ref, table, max_pages, cap = _cache8(cache, block_table, B)
+    ref, table, max_pages, cap, raw = _cache8(cache, block_table, B, stream)
     shape = (B, cache.Hkv, cap // BLOCK8)
     if out is None:
         out = _new(q, stream, shape, torch.float32)
@@ -799,9 +799,9 @@ def block_scores8(q, cache, kv_lens, *, w_pretrained: int = 1, rope_theta: float
             float(rope_theta))
     if bifocal:
         _check(lib().jl_bifocal_block_scores8(*args, _int(w_pretrained, "w_pretrained"),
-                                              _stream(stream)))
+                                              raw))
     else:
-        _check(lib().jl_rope_block_scores8(*args, _stream(stream)))
+        _check(lib().jl_rope_block_scores8(*args, raw))
     return out
 
 
@@ -816,7 +816,7 @@ def select_blocks(scores, kv_lens, n_select: int, *, w_local: int, n_first: int 
         raise ValueError("scores must be [B, Hkv, n_blocks]")
     B, Hkv, n_blocks = scores.shape
     index, device = scores.get_device(), scores.device
-    _current(index, device, "scores")
+    raw = _queue(stream, index, device, "scores")
     n_blocks, n_select = _int(n_blocks, "n_blocks"), _int(n_select, "n_select")
     w_local, n_first = _int(w_local, "w_local"), _int(n_first, "n_first")
     if out is None:
@@ -828,7 +828,7 @@ def select_blocks(scores, kv_lens, n_select: int, *, w_local: int, n_first: int 
         op = _on8(out, "out", torch.int32, (B, Hkv, n_select), index, device)
     _check(lib().jl_select_blocks(
         ptr, _on8(kv_lens, "kv_lens", torch.int32, (B,), index, device), op, B, Hkv, n_blocks,
-        n_select, w_local, n_first, _stream(stream)))
+        n_select, w_local, n_first, raw))
     return out
 
 

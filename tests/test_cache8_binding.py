@@ -27,8 +27,7 @@ def library(monkeypatch):
     note = Noting()
     monkeypatch.setattr(api, "lib", lambda: note)
     monkeypatch.setattr(api, "_dev", lambda t, *a: t.data_ptr())
-    monkeypatch.setattr(api, "_current", lambda *a: None)
-    monkeypatch.setattr(api, "_stream", lambda stream: 0)
+    monkeypatch.setattr(api, "_queue", lambda *a: 0)
     return note
 
 
