@@ -530,9 +530,18 @@ size_t jl_decode8_workspace_bytes(int Hq, int Hkv, int head_dim);
  *   workspace, workspace_bytes: jl_decode8_workspace_bytes(Hq, Hkv, head_dim)
  *            bytes, 16-byte aligned, see there
  * Requires Hq % Hkv == 0 and Hq / Hkv <= 8.  Only the cos/sin table may be
- * allocated or grown (to the cache's capacity).  Rotated queries and keys and
- * the softmax weights are rounded to fp16 (11 bits; an e4m3 number is exact in
- * it), everything else is kept in fp32; the same call gives the same bits.
+ * allocated or grown (to the cache's capacity).  Rounded to fp16 (11 bits; an
+ * e4m3 number is exact in it) are
+ *   - the query, rotated in fp32, after a power of two has brought its row near
+ *     the top of fp16's range: values below 2^-27 of the row's largest may
+ *     hold fewer bits, those below 2^-38 become zero;
+ *   - a key's rotation inside its block: the (cos, sin) of its offset, one
+ *     product and the sum;
+ *   - the softmax weights, against the largest of their block of 64 keys and
+ *     view: weights below 2^-29 of it hold fewer bits, those below 2^-40 become
+ *     zero (2^-14 and 2^-25 where that block's largest score exceeds 2^22 in
+ *     units of log2).  The denominator sums the rounded weights.
+ * Everything else is kept in fp32; the same call gives the same bits.
  */
 int jl_bifocal_decode8(const jl_cache8* cache, const int32_t* block_table, int max_pages,
                        const void* q, const int32_t* kv_lens, void* o, int B, int Hq,
@@ -596,6 +605,9 @@ int jl_rope_block_scores8(const jl_cache8* cache, const int32_t* block_table, in
  *           last where the sequence has fewer blocks
  * n_select must hold the blocks that are always chosen: at least
  * min(n_blocks, (w_local + 127) / 64 + n_first).  n_blocks <= 131072.
+ * The band follows from kv_lens[b] as it is: unlike in the calls on a cache a
+ * length past 64 n_blocks is not clamped to it, so that the band may lie partly
+ * or wholly behind the last block.
  */
 int jl_select_blocks(const float* scores, const int32_t* kv_lens, int32_t* blocks, int B, int Hkv,
                      int n_blocks, int n_select, int w_local, int n_first, void* stream);

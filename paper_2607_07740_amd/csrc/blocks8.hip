@@ -86,8 +86,9 @@ __device__ inline f32x4 mfma4(float q, float m, f32x4 acc) {
 // rows are requested one tile ahead, page indices two.  Bound by the chain length -> page ->
 // mean at one sequence (131072 tokens, 32/8 heads: 3.9 us, 2.4 of them an empty launch; 4.3
 // with 16 x 16 products) and at many by that and a tile's 300 vector instructions (8 of 32K
-// to 128K, 64/8 heads: 10.4 us for 21 MB of means; 12.4 with 16 x 16 products, 17 with
-// rows through each wave's own loads).
+// to 128K, 64/8 heads: 9.7 to 10.4 us for 21 MB of means; 12.4 with 16 x 16 products, 17 with
+// rows through each wave's own loads).  These are times in a captured graph; a trace of single
+// kernels shows 4.3 and 10.7.
 constexpr int kScoreRow = kHalf + 2;  // float2s of a row in LDS: rows start 4 banks apart
 template <bool BIFOCAL, int SETS>  // SETS: of four heads
 __global__ __launch_bounds__(64 * kScoreHeads) void block_scores_kernel(ScoresArgs a) {
@@ -242,8 +243,9 @@ constexpr int kSelCopies = 4, kSelCopy = 256 + 16;
 // every chosen block its place, the numbers equal to the last one in turn until the
 // list is full.  Every wave reads the counts for itself: one barrier a digit.
 // T threads hold R numbers each, side by side; a longer row is read anew for each digit.
-// Bound by latency, 2.4 us of it an empty launch: 5.8 us for 2048 scores, one row or 64, 9.9 for
-// 8192, 14.5 for 16384 (a million tokens), 121 for 131072.
+// Bound by latency, 2.4 us of it an empty launch: 5.8 to 6.1 us for 2048 scores, one row or 64,
+// 9.9 for 8192, 14.6 for 16384 (a million tokens), 120 for 131072.
+// The band goes by the length as it is given, even past the row's end.
 template <int T, int R>
 __global__ __launch_bounds__(T) void select_blocks_kernel(SelectArgs a) {
   __shared__ __attribute__((aligned(16))) int first[kSelCopies * kSelCopy];

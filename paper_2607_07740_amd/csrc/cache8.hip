@@ -44,9 +44,9 @@ __device__ inline float sum_rows16(float (&v)[16], int lane) {
 // a token of decode writes 72 of the 1024 16-byte units.  The mean key
 // sums e4m3 values, multiples of 2^-9 below 2^15 in all: exactly, in any order.
 //
-// Bound by memory for a prompt: 30001 rows of 8 heads 32 to 38 us (123 MB read and 62
-// written, as few as there are: 4.9 to 5.8 TB/s; one after another with the reading of
-// 32768 such rows, 75 us in all).  A row each of 16 sequences takes 6.3 us, 2.4 of them
+// Bound by memory for a prompt: 30001 rows of 8 heads 31 us over the same pool, 40 over three in
+// turn (123 MB read and 62 written, as few as there are: 4.6 to 5.9 TB/s; one after another with
+// the reading of 32768 such rows, 73 us in all).  A row each of 16 sequences takes 6.0 us, 2.4 of them
 // an empty launch, the rest the chain length -> page -> block -> scale.  A run of units
 // on each die, whose L2 then has all heads of a row: 39.3 for 37.9 us, 7.7 for 7.7 with 64
 // sequences of one row.
@@ -233,7 +233,7 @@ __device__ inline uint32_t bf16_pair(float a, float b) {
 
 // Workgroup = one block of one kv head.  A value has 4 significant bits and a
 // magnitude of at least 2^-126 or zero, so bf16 holds it exactly.  Bound by memory:
-// 32768 rows of 8 heads 32 to 36 us, 67 MB read and 134 written.
+// 32768 rows of 8 heads 31 to 36 us, 67 MB read and 134 written.
 __global__ __launch_bounds__(256) void read8_kernel(ReadArgs a) {
   const int tid = threadIdx.x;
   const int h = blockIdx.x % a.c.Hkv;

@@ -54,7 +54,8 @@ struct Segments {
 };
 
 __device__ inline void make_ranges(Segments& s, int n_wg, int waves, uint32_t V) {
-  // no range shorter than one step per wave and the cost of its segment
+  // as many ranges as hold about one step per wave and the cost of a segment each: where that does
+  // not come out even they are shorter, none below half of that
   const uint32_t least = (uint32_t)(waves + kD8SegCost);
   s.n = (int)min((uint32_t)n_wg, (V + least - 1) / least);
   s.q = V / (uint32_t)s.n;
@@ -198,21 +199,25 @@ struct __attribute__((aligned(1024))) Decode8Smem {
 // fourth (eighth) step of 64 keys and keeps the 16 columns' states in registers.
 //
 // A step is 16 KB, K and V, that go from memory into registers, 16 bytes a lane and
-// 1 KB an instruction, one step ahead; the layout is the matrix operands' own.
+// 1 KB an instruction; the layout is the matrix operands' own.  K is requested one step
+// ahead.  V is written so too, but the compiler joins those requests with the first
+// step's at the head of the loop: a step's V is on its way during its own scores.
 // Rotation by offset in the block: with k0 the block's first position, a key is
 // rotated by t = k - k0 (base) or f(k) - f(k0) (remote), from 64 rows of fp16
 // (cos, sin) in LDS, and the query's columns by q - k0 or f(q) - f(k0) in fp32:
 // only relative positions matter (Sec. 3.2, Eq. (6)).  A rotated pair costs a
-// conversion and two packed fp16 instructions and goes to the matrix cores as
+// conversion and two packed fp16 instructions (cos and sin, the product with sin and the
+// sum each round to fp16) and goes to the matrix cores as
 // it is: e4m3 numbers are exact in fp16, and with |x| <= 448 none overflows.  The
 // block's scale of K multiplies the scores, that of V the step's product.
 // The query is brought to fp16's upper range by a power of two first, its own range aside.
 //
-// Bound by memory where keys are many: 8 sequences of 32K to 128K, 32/8 heads 210 us, 1.34 GB
-// at 6.4 TB/s (the loads alone 6.4 to 6.9); one of 1048576 320 us, 6.7; of 131072 48.8 us, 5.5;
-// 32 of 0.5K to 16K on pages of 64 tokens 67.5 us, 5.3.  A step's 675 VALU instructions fit
-// beside its loads: one without the masks of steps in one view took as long.  Bound by a chain
-// of latencies where they are few (1999 keys, 16/8 heads: 10.5 us; 192 keys 6.3): an empty
+// Bound by memory where keys are many: 8 sequences of 32K to 128K, 32/8 heads 208 to 219 us,
+// 1.34 GB at 6.1 to 6.4 TB/s (the loads alone 6.4 to 6.9); one of 1048576 318 to 334 us, 6.4 to
+// 6.8; of 131072 49 us, 5.5; 32 of 0.5K to 16K on pages of 64 tokens 67 to 71 us, 5.0 to 5.3.  A
+// step's 680 VALU instructions fit beside its loads: one without the masks of steps in one view
+// took as long.  Bound by a chain
+// of latencies where they are few (1999 keys, 16/8 heads: 10.6 to 11.3 us; 192 keys 6.4): an empty
 // launch 2.4 us, length, page and step about 0.8 each from a request to the data, a step's work
 // 2, the waves' merge 0.9, a state's way to another workgroup and the merge there 2.6.
 template <bool BIFOCAL, int MODE>
@@ -366,7 +371,8 @@ __global__ __launch_bounds__(64 * decode8_waves(MODE), 2) void decode8_kernel(De
       float qlo[16], qhi[16];
       float q_back;  // what undoes the latter
 
-      // the step in hand; each register takes the next step's piece as soon as its own is used
+      // the step in hand; each of K's registers takes the next step's piece as soon as its own is
+      // used
       u32x4 kx[8], vx[8], row;
       float ks, vs;
       int k0;         // first position of the step's block
