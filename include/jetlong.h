@@ -494,8 +494,9 @@ typedef struct jl_cache8 {
  *   new rows are x / scale rounded to nearest even e4m3, saturated at 448 (NaN
  *           stays NaN);
  *   rows behind the last new one become zero; the block's mean is taken anew.
- * Every other block is left as it was.  Two sequences whose new rows meet in one
- * block (a shared page) race.  Nothing is allocated and nothing waited for.
+ * Every other block is left as it was.  New rows of two sequences, or of two
+ * blocks of one, that meet in the same block of the pools (a page that is named
+ * twice) race.  Nothing is allocated and nothing waited for.
  */
 int jl_cache8_append(const jl_cache8* cache, const int32_t* block_table, int max_pages,
                      const void* k, const void* v, const int32_t* starts, const int32_t* n_new,
@@ -664,7 +665,8 @@ double jl_debug_prefill_rescale_log2(double log2_bound);
  * so hipEventElapsedTime(start, stop) is the attention alone (a packed call's
  * planning kernels stay outside).  which = 1: the
  * same around the split kernel of every decode call that takes a workspace
- * (all but jl_bifocal_decode_noalloc; the reduce stays outside).
+ * (all but jl_bifocal_decode_noalloc; the reduce stays outside, but the 8-bit
+ * decode's one kernel merges too).
  * start, stop: hipEvent_t created and owned by the caller; NULL, NULL clears
  * the hook.  JL_ERR_INVALID_ARG for another `which` or when only one event is
  * NULL.  The events must outlive every call that records them.

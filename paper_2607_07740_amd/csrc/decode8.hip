@@ -826,7 +826,7 @@ long long decode8_entries(int n) { return (long long)n + kD8SegCost; }
 hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, const int32_t* kv_lens,
                           const int32_t* blocks, int n_select, uint16_t* o, const float2* table,
                           const void* offsets, int B, int Hq, int w_pre, int w0, void* ws,
-                          hipStream_t stream) {
+                          hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1) {
   static_assert(2 * kD8MaxWg <= kD8Counters, "two counters per workgroup");
   // One sequence: at least four workgroups for each of its heads.
   // Lists, where there is one for each of most CUs: a workgroup of eight waves for each, and no
@@ -856,6 +856,9 @@ hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, cons
                 2 * waves / (Hq / c.Hkv), 256 / (Hq / c.Hkv),
                 1.4426950408889634f / sqrtf((float)kHeadDim)};
   const dim3 grid(a.n_wg), block(64 * waves);
+  // ev0 / ev1 (optional) are recorded on the stream around the kernel
+  hipError_t e;
+  if (ev0 != nullptr && (e = hipEventRecord(ev0, stream)) != hipSuccess) return e;
 #define JL_DECODE8(bif, m) hipLaunchKernelGGL((decode8_kernel<bif, m>), grid, block, 0, stream, a)
   if (bifocal) {
     if (mode == kListed8) JL_DECODE8(true, kListed8);
@@ -869,7 +872,9 @@ hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, cons
     else JL_DECODE8(false, kBatch8);
   }
 #undef JL_DECODE8
-  return hipGetLastError();
+  e = hipGetLastError();
+  if (e == hipSuccess && ev1 != nullptr) e = hipEventRecord(ev1, stream);
+  return e;
 }
 
 }  // namespace jl

@@ -72,7 +72,7 @@ long long decode8_entries(int n);
 hipError_t launch_decode8(bool bifocal, const Cache8& c, const uint16_t* q, const int32_t* kv_lens,
                           const int32_t* blocks, int n_select, uint16_t* o, const float2* table,
                           const void* offsets, int B, int Hq, int w_pre, int w0, void* ws,
-                          hipStream_t stream);
+                          hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1);
 size_t offset_rows_bytes();
 hipError_t launch_offset_rows(const float2* table, void* out, hipStream_t stream);
 hipError_t launch_block_scores8(bool bifocal, const Cache8& c, const uint16_t* q,
@@ -707,9 +707,11 @@ int decode8_common(bool bifocal, const jl_cache8* cache, const int32_t* block_ta
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   st = get_table(theta, c.n_blocks * jl::kBlk, s, &tab);
   if (st != JL_OK) return st;
-  const hipError_t e =
-      jl::launch_decode8(bifocal, c, (const uint16_t*)q, kv_lens, listed ? blocks : nullptr,
-                         n_select, (uint16_t*)o, tab.f32, tab.offsets, B, Hq, w_pre, w0, ws, s);
+  hipEvent_t ev0, ev1;
+  timing_events(1, &ev0, &ev1);
+  const hipError_t e = jl::launch_decode8(
+      bifocal, c, (const uint16_t*)q, kv_lens, listed ? blocks : nullptr, n_select, (uint16_t*)o,
+      tab.f32, tab.offsets, B, Hq, w_pre, w0, ws, s, ev0, ev1);
   if (e != hipSuccess) return hip_fail(e, "8-bit decode launch");
   return ok();
 }
