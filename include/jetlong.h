@@ -614,6 +614,108 @@ int jl_select_blocks(const float* scores, const int32_t* kv_lens, int32_t* block
                      int n_blocks, int n_select, int w_local, int n_first, void* stream);
 
 /*
+ * ---- pages of a batch ------------------------------------------------------
+ * The tables of B sequences over one pool of n_pages pages, as the paged entry
+ * points read them (table as block_table, lens as kv_lens), and how often each
+ * page is named.  All three are device arrays of the caller's:
+ *   table  int32 [B, max_pages]: the pages of sequence b are the first
+ *          ceil(lens[b] / page_size) entries of its row, the others are -1
+ *   lens   int32 [B]: tokens of each sequence, 0 for an empty row
+ *   refs   int32 [n_pages], 16-byte aligned: entries of the table that name the
+ *          page; a page is free where it is not positive
+ * -1 everywhere, zeros and zeros are an empty table.  Pages hold any number of
+ * tokens; the bf16 entry points take powers of two, the 8-bit ones multiples of 64.
+ * The calls below keep these rules; results follow from the arguments alone, and
+ * no call waits for the device or allocates.  Entries outside the pool are never
+ * followed.  B > 2048 or n_pages > 2^30 -> JL_ERR_UNSUPPORTED.  Calls on one table
+ * must be ordered by the caller.
+ */
+typedef struct jl_pages {
+  int32_t* table;
+  int32_t* lens;
+  int32_t* refs;
+  int B, max_pages, n_pages, page_size;
+} jl_pages;
+
+/*
+ * Forks, frees and reorders sequences, all rows at once: row b becomes what row
+ * parent[b] was before the call, sharing its pages (the partly filled last one
+ * too), and an empty row where parent[b] is outside [0, B).  parent[b] = b leaves
+ * row b as it is.  Pages that no row names any more are free.
+ *   parent  int32 [B] DEVICE array
+ */
+int jl_pages_fork(const jl_pages* pages, const int32_t* parent, void* stream);
+
+/*
+ * Makes room for n_new[b] rows behind every sequence (none where n_new[b] <= 0): the
+ * pages they need are taken from the free ones, in ascending order, sequence after
+ * sequence.  A sequence whose rows begin in a partly filled page that other sequences
+ * name too gets a page of its own in its place, to which the old one is to be copied
+ * (a sequence's last page that all name who write there stays with the last of them).
+ * All or nothing: if the pages do not suffice, or a sequence would pass max_pages, the
+ * table, lens and refs stay as they were.
+ *   n_new    int32 [B] DEVICE array
+ *   starts   int32 [B] (written): lens before the call, as the append calls take them
+ *   granted  int32 [B] (written): max(n_new, 0), or 0 for all if the pages do not
+ *            suffice; lens grows by it.  The append calls take it as n_new.
+ *   moves    int32 [B, 2] (written): page to copy from, page to copy to, in order of the
+ *            sequences; -1 behind the last.  jl_copy_pages has to run before rows are
+ *            appended.
+ *   info     int32 [4] (written): moves, pages taken, pages missing, sequences that would
+ *            pass max_pages
+ */
+int jl_pages_reserve(const jl_pages* pages, const int32_t* n_new, int32_t* starts,
+                     int32_t* granted, int32_t* moves, int32_t* info, void* stream);
+
+/*
+ * Makes the pages in use the first ones of the pool: with n of them, the i-th that is
+ * numbered n or more gets the number of the i-th free page below n.  Table and refs are
+ * rewritten; jl_copy_pages then moves the contents.
+ *   moves  int32 [n_pages / 2, 2] (written): from, to, ascending; -1 behind the last
+ *   to     int32 [n_pages]: workspace
+ *   info   int32 [4] (written): moves, pages in use, 0, 0
+ */
+int jl_pages_compact(const jl_pages* pages, int32_t* moves, int32_t* to, int32_t* info,
+                     void* stream);
+
+/* A pool of pages: page p is the page_bytes bytes (a multiple of 4) at ptr (4-byte
+ * aligned) + p * page_bytes. */
+typedef struct jl_page_pool {
+  void* ptr;
+  size_t page_bytes;
+} jl_page_pool;
+
+/*
+ * Copies pages inside each of n_pools pools (K and V of every layer, the five arrays of an
+ * 8-bit cache) as moves says: the first n_moves[0] pairs (from, to) of it, at most max_moves;
+ * pairs that name a page outside [0, n_pages) are passed over.  No page may be named as a
+ * target twice or as a source and a target; the lists of jl_pages_reserve and
+ * jl_pages_compact name none so.
+ *   pools    host array, not read after the call returns
+ *   moves    int32 [max_moves, 2], n_moves int32 [1]: DEVICE arrays (n_moves: info)
+ */
+int jl_copy_pages(const jl_page_pool* pools, int n_pools, int n_pages, const int32_t* moves,
+                  const int32_t* n_moves, int max_moves, void* stream);
+
+/*
+ * Appends rows to a bf16 cache, paged or dense.
+ *   k_cache, v_cache  bf16 [n_pages, page_size, Hkv, head_dim] (written)
+ *   block_table  int32 [B, max_pages] DEVICE array; NULL: a dense cache, sequence b is
+ *                page b (page_size = its capacity, B <= n_pages, max_pages is not read)
+ *   k, v     bf16 [B, n, Hkv, head_dim], or with cu_seqlens packed [n, Hkv, head_dim]
+ *   starts   int32 [B] DEVICE array: position of each sequence's first new row
+ *   n_new    int32 [B] DEVICE array or NULL: only the first n_new[b] rows of sequence b
+ *   cu_seqlens  int32 [B + 1] DEVICE array, non-decreasing, or NULL: sequence b's rows are
+ *            cu_seqlens[b] .. cu_seqlens[b + 1] - 1 of the packed ones
+ * Rows at positions outside [0, capacity), for a page outside the pool or of no sequence are
+ * dropped.  Two rows for one place of the pools race.  Nothing is allocated.
+ */
+int jl_cache_append(void* k_cache, void* v_cache, int n_pages, int page_size,
+                    const int32_t* block_table, int max_pages, const void* k, const void* v,
+                    const int32_t* starts, const int32_t* n_new, const int32_t* cu_seqlens, int B,
+                    int n, int Hkv, int head_dim, void* stream);
+
+/*
  * Debug view of the schedule as the device computes it (Eqs. (2), (3), (5)),
  * for bit-exact tests.  All pointers are device pointers.
  *   lengths    int32 [n_lengths]              sequence lengths L (>= 1)

@@ -128,6 +128,17 @@ def lib() -> ctypes.CDLL:
         L.jl_rope_block_scores8.argtypes = [vp, vp, i32, vp, vp, vp, i32, i32, dbl, vp]
         L.jl_select_blocks.restype = i32
         L.jl_select_blocks.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, i32, vp]
+        L.jl_pages_fork.restype = i32
+        L.jl_pages_fork.argtypes = [vp, vp, vp]
+        L.jl_pages_reserve.restype = i32
+        L.jl_pages_reserve.argtypes = [vp, vp, vp, vp, vp, vp, vp]
+        L.jl_pages_compact.restype = i32
+        L.jl_pages_compact.argtypes = [vp, vp, vp, vp, vp]
+        L.jl_copy_pages.restype = i32
+        L.jl_copy_pages.argtypes = [vp, i32, i32, vp, vp, i32, vp]
+        L.jl_cache_append.restype = i32
+        L.jl_cache_append.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, i32, i32, i32,
+                                      i32, vp]
         L.jl_debug_schedule.restype = i32
         L.jl_debug_schedule.argtypes = [vp, i32, vp, i32, i32, vp, vp, vp, vp]
         L.jl_debug_prefill_tiles.restype = i32
@@ -830,6 +841,163 @@ def select_blocks(scores, kv_lens, n_select: int, *, w_local: int, n_first: int 
         ptr, _on8(kv_lens, "kv_lens", torch.int32, (B,), index, device), op, B, Hkv, n_blocks,
         n_select, w_local, n_first, raw))
     return out
+
+
+# ------------------------------------------------------------ pages of a batch
+class _PagesStruct(ctypes.Structure):  # jl_pages
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("table", "lens", "refs")]
+                + [(n, ctypes.c_int) for n in ("B", "max_pages", "n_pages", "page_size")])
+
+
+class _PoolStruct(ctypes.Structure):  # jl_page_pool
+    _fields_ = [("ptr", ctypes.c_void_p), ("page_bytes", ctypes.c_size_t)]
+
+
+class PageTable:
+    """The tables of B sequences over a pool of pages (jl_pages): lens int32 [B], refs int32
+    [n_pages], table int32 [B, max_pages], on one device.  pages_alloc makes an empty one.  The
+    paged calls take table as block_table and lens as kv_lens.  The tensors are the caller's to
+    read and to restore by copy_; none can be replaced."""
+
+    def __init__(self, lens, refs, table, page_size: int):
+        if table.dim() != 2:
+            raise ValueError("table must be [B, max_pages]")
+        (B, max_pages), device, index = table.shape, table.device, table.get_device()
+        i32 = _t().int32
+        page_size = _int(page_size, "page_size")
+        struct = _PagesStruct(
+            _dev(table, "table", i32), _on8(lens, "lens", i32, (B,), index, device),
+            _on8(refs, "refs", i32, (refs.numel(),), index, device), B, max_pages, refs.numel(),
+            page_size)
+        self.__dict__.update(lens=lens, refs=refs, table=table, B=B, max_pages=max_pages,
+                             n_pages=refs.numel(), page_size=page_size, device=device,
+                             index=index, _struct=struct, _ref=ctypes.byref(struct),
+                             _ptrs=(table.data_ptr(), lens.data_ptr(), refs.data_ptr()))
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a PageTable cannot be changed (%s): make another one" % name)
+
+    def __delattr__(self, name):
+        raise AttributeError("a PageTable cannot be changed (%s): make another one" % name)
+
+
+def pages_alloc(B: int, max_pages: int, n_pages: int, page_size: int, *, device="cuda") -> PageTable:
+    """A table of B empty sequences over a pool of n_pages free pages."""
+    kw = dict(dtype=_t().int32, device=device)
+    return PageTable(_t().zeros(B, **kw), _t().zeros(n_pages, **kw),
+                     _t().full((B, max_pages), -1, **kw), page_size)
+
+
+def _pages(pages, stream):
+    """The checks of a call on a table -> (jl_pages pointer, raw stream)."""
+    if not isinstance(pages, PageTable):
+        raise TypeError("pages must be a PageTable")
+    if (pages.table.data_ptr(), pages.lens.data_ptr(), pages.refs.data_ptr()) != pages._ptrs:
+        raise ValueError("the table's tensors have moved since it was made")
+    return pages._ref, _queue(stream, pages.index, pages.device, "table")
+
+
+def pages_fork(pages, parent, *, stream=None) -> None:
+    """jl_pages_fork: row b becomes what row parent[b] was, or empty (parent int32 [B]; -1 frees),
+    all rows at once."""
+    ref, raw = _pages(pages, stream)
+    _check(lib().jl_pages_fork(ref, _on8(parent, "parent", _t().int32, (pages.B,), pages.index,
+                                         pages.device), raw))
+
+
+def pages_reserve(pages, n_new, *, stream=None):
+    """jl_pages_reserve: room for n_new[b] (int32 [B]) more rows of every sequence, whose lens
+    grow -> (starts, granted, moves, info): starts and granted for the append calls, moves and
+    info for copy_pages, which has to come before them."""
+    ref, raw = _pages(pages, stream)
+    B, i32 = pages.B, _t().int32
+    n = _on8(n_new, "n_new", i32, (B,), pages.index, pages.device)
+    out = _new(pages.lens, stream, (4 + 4 * B,), i32)
+    at = out.data_ptr()
+    info, moves, starts, granted = out.split((4, 2 * B, B, B))
+    _check(lib().jl_pages_reserve(ref, n, at + 16 + 8 * B, at + 16 + 12 * B, at + 16, at, raw))
+    return starts, granted, moves.view(B, 2), info
+
+
+def pages_compact(pages, *, stream=None):
+    """jl_pages_compact: the pages in use become the first ones of the pool -> (moves, info) for
+    copy_pages."""
+    ref, raw = _pages(pages, stream)
+    n, i32 = pages.n_pages, _t().int32
+    out = _new(pages.lens, stream, (4 + n // 2 * 2,), i32)
+    to = _new(pages.lens, stream, (n,), i32)
+    at = out.data_ptr()
+    _check(lib().jl_pages_compact(ref, at + 16, to.data_ptr(), at, raw))
+    return out[4:].view(n // 2, 2), out[:4]
+
+
+def copy_pages(pools, moves, info, *, stream=None) -> None:
+    """jl_copy_pages: pages of every pool are copied as moves int32 [m, 2] says, the first info[0]
+    pairs.  pools: tensors [n_pages, ...] or Cache8s, all of as many pages and on one device."""
+    torch = _t()
+    tensors = []
+    for p in pools if isinstance(pools, (list, tuple)) else [pools]:
+        tensors.extend([p.k, p.v, p.k_scale, p.v_scale, p.k_mean] if isinstance(p, Cache8) else [p])
+    if not tensors:
+        raise ValueError("pools must name a tensor")
+    index, device = moves.get_device(), moves.device
+    mp = _dev(moves, "moves", torch.int32)
+    if moves.dim() != 2 or moves.shape[1] != 2:
+        raise ValueError("moves must be [m, 2]")
+    ip = _on8(info, "info", torch.int32, None, index, device)
+    if info.numel() < 1:
+        raise ValueError("info must hold the number of moves")
+    raw = _queue(stream, index, device, "moves")
+    n_pages = tensors[0].shape[0] if tensors[0].dim() else 0
+    array = (_PoolStruct * len(tensors))()
+    for slot, t in zip(array, tensors):
+        if t.dim() < 1 or t.shape[0] != n_pages or n_pages < 1:
+            raise ValueError("every pool must be [n_pages, ...] of the same n_pages")
+        slot.ptr = _on8(t, "pool", t.dtype, None, index, device)
+        slot.page_bytes = t.nbytes // n_pages
+    _check(lib().jl_copy_pages(array, len(tensors), _int(n_pages, "n_pages"), mp, ip,
+                               _int(moves.shape[0], "max_moves"), raw))
+
+
+def cache_append(k_cache, v_cache, k, v, starts, *, n_new=None, cu_seqlens=None, block_table=None,
+                 stream=None) -> None:
+    """jl_cache_append: rows k, v [B, n, Hkv, 128] bf16, or packed [T, Hkv, 128] with cu_seqlens int32
+    [B + 1], to positions starts[b] .. of sequence b in caches [B, max_len, Hkv, 128] or, with
+    block_table int32 [B, max_pages], pools [n_pages, page_size, Hkv, 128].  n_new int32 [B]: only
+    the first n_new[b] rows of sequence b."""
+    torch = _t()
+    bf16, i32 = torch.bfloat16, torch.int32
+    kcp = _dev(k_cache, "k_cache", bf16)
+    index, device = k_cache.get_device(), k_cache.device
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache must be [n_pages, page_size, Hkv, D]")
+    n_pages, page_size, Hkv, D = k_cache.shape
+    vcp = _on8(v_cache, "v_cache", bf16, k_cache.shape, index, device)
+    kp = _on8(k, "k", bf16, None, index, device)
+    vp = _on8(v, "v", bf16, k.shape, index, device)
+    shape = k.shape
+    if cu_seqlens is not None:
+        if len(shape) != 3 or shape[1:] != (Hkv, D):
+            raise ValueError("packed k and v must be [T, %d, %d]" % (Hkv, D))
+        if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+            raise ValueError("cu_seqlens must be [B + 1] with B >= 1")
+        B, n = cu_seqlens.numel() - 1, shape[0]
+        cp = _on8(cu_seqlens, "cu_seqlens", i32, None, index, device)
+    else:
+        if len(shape) != 4 or shape[2:] != (Hkv, D):
+            raise ValueError("k and v must be [B, n, %d, %d]" % (Hkv, D))
+        B, n, cp = shape[0], shape[1], None
+    tp, max_pages = None, 0
+    if block_table is not None:
+        tp = _on8(block_table, "block_table", i32, None, index, device)
+        if block_table.dim() != 2 or block_table.shape[0] != B:
+            raise ValueError("block_table must be [B, max_pages]")
+        max_pages = block_table.shape[1]
+    _check(lib().jl_cache_append(
+        kcp, vcp, _int(n_pages, "n_pages"), _int(page_size, "page_size"), tp,
+        _int(max_pages, "max_pages"), kp, vp, _on8(starts, "starts", i32, (B,), index, device),
+        None if n_new is None else _on8(n_new, "n_new", i32, (B,), index, device), cp,
+        _int(B, "B"), _int(n, "n"), _int(Hkv, "Hkv"), D, _queue(stream, index, device, "k_cache")))
 
 
 def debug_schedule(lengths, positions, w_pretrained: int, stream=None):

@@ -16,9 +16,10 @@
 
 #include "../../include/jetlong.h"
 #include "cache8.h"
+#include "pages.h"
 
 namespace jl {
-// kernels (prefill.hip, decode.hip, cache8.hip, decode8.hip, blocks8.hip, aux.hip)
+// kernels (prefill.hip, decode.hip, cache8.hip, decode8.hip, blocks8.hip, pages.hip, aux.hip)
 hipError_t launch_prefill_chunk(bool bifocal, const uint16_t* q, const uint16_t* k,
                                 const uint16_t* v, uint16_t* o, float* lse, const float2* table,
                                 const float2* rtable, const uint32_t* table16,
@@ -81,6 +82,19 @@ hipError_t launch_block_scores8(bool bifocal, const Cache8& c, const uint16_t* q
 hipError_t launch_select_blocks(const float* scores, const int32_t* kv_lens, int32_t* blocks,
                                 int B, int Hkv, int n_blocks, int n_select, int w0, int n_first,
                                 hipStream_t stream);
+hipError_t launch_pages_fork(const Pages& p, const int32_t* parent, hipStream_t stream);
+hipError_t launch_pages_reserve(const Pages& p, const int32_t* n_new, int32_t* starts,
+                                int32_t* granted, int32_t* moves, int32_t* info,
+                                hipStream_t stream);
+hipError_t launch_pages_compact(const Pages& p, int32_t* moves, int32_t* to, int32_t* info,
+                                hipStream_t stream);
+long long copy_units(CopyPools& a);
+hipError_t launch_copy_pages(const CopyPools& a, const int32_t* moves, const int32_t* info,
+                             int n_cu, hipStream_t stream);
+hipError_t launch_cache_append(const uint16_t* k, const uint16_t* v, uint16_t* kc, uint16_t* vc,
+                               const int32_t* table, int max_pages, int n_pages, int page,
+                               const int32_t* starts, const int32_t* n_new, const int32_t* cu,
+                               int B, int n, int Hkv, hipStream_t stream);
 hipError_t launch_build_table(float2* table, uint32_t* table16, int n_pos, const double* omega,
                               hipStream_t stream);
 hipError_t launch_debug_schedule(const int32_t* lengths, int nl, const int32_t* positions, int np,
@@ -736,6 +750,28 @@ int block_scores8(bool bifocal, const jl_cache8* cache, const int32_t* block_tab
   return ok();
 }
 
+// ------------------------------------------------------------------ pages
+int check_pages(const jl_pages* t, jl::Pages* out) {
+  if (t == nullptr) return fail(JL_ERR_INVALID_ARG, "pages must be non-null");
+  if (t->B < 1 || t->max_pages < 1 || t->n_pages < 1 || t->page_size < 1)
+    return fail(JL_ERR_INVALID_ARG,
+                "B, max_pages, n_pages, page_size must be >= 1 (got %d, %d, %d, %d)", t->B,
+                t->max_pages, t->n_pages, t->page_size);
+  if (!aligned4(t->table) || !aligned4(t->lens))
+    return fail(JL_ERR_INVALID_ARG, "table and lens must be non-null and 4-byte aligned");
+  if (!aligned16(t->refs))
+    return fail(JL_ERR_INVALID_ARG, "refs must be non-null and 16-byte aligned");
+  if ((long long)t->max_pages * t->page_size > 0x7fffffffLL)
+    return fail(JL_ERR_INVALID_ARG, "max_pages * page_size too large");
+  if (t->B > jl::kPagesMaxSeqs)
+    return fail(JL_ERR_UNSUPPORTED, "%d sequences in one table (at most %d)", t->B,
+                jl::kPagesMaxSeqs);
+  if (t->n_pages > jl::kPagesMaxPages)
+    return fail(JL_ERR_UNSUPPORTED, "%d pages (at most %d)", t->n_pages, jl::kPagesMaxPages);
+  *out = jl::Pages{t->table, t->lens, t->refs, t->B, t->max_pages, t->n_pages, t->page_size};
+  return JL_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1101,6 +1137,117 @@ int jl_select_blocks(const float* scores, const int32_t* kv_lens, int32_t* block
                                                 w_local, n_first,
                                                 reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "block choice launch");
+  return ok();
+}
+
+int jl_pages_fork(const jl_pages* pages, const int32_t* parent, void* stream) {
+  jl::Pages p;
+  const int st = check_pages(pages, &p);
+  if (st != JL_OK) return st;
+  if (!aligned4(parent)) return fail(JL_ERR_INVALID_ARG, "parent must be non-null and aligned");
+  const hipError_t e =
+      jl::launch_pages_fork(p, parent, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "fork launch");
+  return ok();
+}
+
+int jl_pages_reserve(const jl_pages* pages, const int32_t* n_new, int32_t* starts,
+                     int32_t* granted, int32_t* moves, int32_t* info, void* stream) {
+  jl::Pages p;
+  const int st = check_pages(pages, &p);
+  if (st != JL_OK) return st;
+  if (!aligned4(n_new) || !aligned4(starts) || !aligned4(granted) || !aligned4(moves) ||
+      !aligned4(info))
+    return fail(JL_ERR_INVALID_ARG, "n_new, starts, granted, moves, info must be non-null and aligned");
+  const hipError_t e = jl::launch_pages_reserve(p, n_new, starts, granted, moves, info,
+                                                reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "reserve launch");
+  return ok();
+}
+
+int jl_pages_compact(const jl_pages* pages, int32_t* moves, int32_t* to, int32_t* info,
+                     void* stream) {
+  jl::Pages p;
+  const int st = check_pages(pages, &p);
+  if (st != JL_OK) return st;
+  if ((p.n_pages > 1 && !aligned4(moves)) || !aligned4(to) || !aligned4(info))
+    return fail(JL_ERR_INVALID_ARG, "moves, to, info must be non-null and aligned");
+  const hipError_t e = jl::launch_pages_compact(p, moves, to, info,
+                                                reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "compact launch");
+  return ok();
+}
+
+int jl_copy_pages(const jl_page_pool* pools, int n_pools, int n_pages, const int32_t* moves,
+                  const int32_t* n_moves, int max_moves, void* stream) {
+  if (pools == nullptr || n_pools < 1 || n_pages < 1 || max_moves < 0)
+    return fail(JL_ERR_INVALID_ARG,
+                "pools must be non-null, n_pools and n_pages >= 1, max_moves >= 0 (got %d, %d, %d)",
+                n_pools, n_pages, max_moves);
+  for (int i = 0; i < n_pools; ++i) {
+    if (!aligned4(pools[i].ptr) || pools[i].page_bytes < 4 || pools[i].page_bytes % 4 != 0)
+      return fail(JL_ERR_INVALID_ARG,
+                  "pool %d must be non-null and 4-byte aligned, its pages a multiple of 4 bytes", i);
+    if (pools[i].page_bytes > ((size_t)1 << 62) / (size_t)n_pages)
+      return fail(JL_ERR_INVALID_ARG, "pool %d: problem too large", i);
+  }
+  if (max_moves == 0) return ok();
+  if (!aligned4(moves) || !aligned4(n_moves))
+    return fail(JL_ERR_INVALID_ARG, "moves and n_moves must be non-null and aligned");
+  // every launch's units fit 32 bits, checked before the first of them runs
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int at = 0; at < n_pools; at += jl::kCopyPools) {
+      jl::CopyPools c = {};
+      c.n_pools = std::min(jl::kCopyPools, n_pools - at);
+      c.n_pages = n_pages;
+      c.max_moves = max_moves;
+      for (int i = 0; i < c.n_pools; ++i) {
+        c.ptr[i] = (unsigned char*)pools[at + i].ptr;
+        c.bytes[i] = pools[at + i].page_bytes;
+      }
+      if (jl::copy_units(c) < 0) return fail(JL_ERR_INVALID_ARG, "problem too large");
+      if (pass == 0) continue;
+      const hipError_t e = jl::launch_copy_pages(c, moves, n_moves, jl::cu_count(),
+                                                 reinterpret_cast<hipStream_t>(stream));
+      if (e != hipSuccess) return hip_fail(e, "page copy launch");
+    }
+  }
+  return ok();
+}
+
+int jl_cache_append(void* k_cache, void* v_cache, int n_pages, int page_size,
+                    const int32_t* block_table, int max_pages, const void* k, const void* v,
+                    const int32_t* starts, const int32_t* n_new, const int32_t* cu_seqlens, int B,
+                    int n, int Hkv, int head_dim, void* stream) {
+  if (B < 1 || Hkv < 1 || n < 1 || n_pages < 1 || page_size < 1)
+    return fail(JL_ERR_INVALID_ARG,
+                "B, n, Hkv, n_pages, page_size must be >= 1 (got %d, %d, %d, %d, %d)", B, n, Hkv,
+                n_pages, page_size);
+  if (head_dim < 2 || head_dim % 2 != 0)
+    return fail(JL_ERR_INVALID_ARG, "head_dim must be even and >= 2 (got %d)", head_dim);
+  if (head_dim != kHeadDim)
+    return fail(JL_ERR_UNSUPPORTED, "head_dim %d not built (only 128)", head_dim);
+  if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(k) || !aligned16(v))
+    return fail(JL_ERR_INVALID_ARG, "k_cache, v_cache, k, v must be non-null and 16-byte aligned");
+  if (!aligned4(starts)) return fail(JL_ERR_INVALID_ARG, "starts must be non-null and aligned");
+  if ((n_new != nullptr && !aligned4(n_new)) || (cu_seqlens != nullptr && !aligned4(cu_seqlens)))
+    return fail(JL_ERR_INVALID_ARG, "n_new and cu_seqlens must be 4-byte aligned");
+  if (block_table != nullptr) {
+    if (!aligned4(block_table))
+      return fail(JL_ERR_INVALID_ARG, "block_table must be 4-byte aligned");
+    if (max_pages < 1) return fail(JL_ERR_INVALID_ARG, "max_pages must be >= 1 (got %d)", max_pages);
+    if ((long long)max_pages * page_size > 0x7fffffffLL)
+      return fail(JL_ERR_INVALID_ARG, "max_pages * page_size too large");
+  } else if (B > n_pages) {
+    return fail(JL_ERR_INVALID_ARG, "a dense cache of %d sequences cannot hold %d", n_pages, B);
+  }
+  if (Hkv > 0x7fffffff / (kHeadDim / 8) || (cu_seqlens == nullptr && past_int32(B, n, 1)))
+    return fail(JL_ERR_INVALID_ARG, "problem too large");
+  const hipError_t e = jl::launch_cache_append(
+      (const uint16_t*)k, (const uint16_t*)v, (uint16_t*)k_cache, (uint16_t*)v_cache, block_table,
+      max_pages, n_pages, page_size, starts, n_new, cu_seqlens, B, n, Hkv,
+      reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "append launch");
   return ok();
 }
 

@@ -1,0 +1,501 @@
+// pages.hip -- the pages of a batch's caches: forks, growth with copy on write,
+// compaction, the copies that these ask for, and new rows of bf16 caches.
+//
+// The bookkeeping is whole numbers and every result follows from the arguments
+// alone: free pages are dealt in ascending order, sequence after sequence, and the
+// only atomics are integer sums.  refs counts the entries that name a page, so a
+// page is free where it is not positive.
+#include <algorithm>
+
+#include "jl_device.h"
+#include "pages.h"
+
+namespace jl {
+
+__device__ inline int pages_of(int len, int page, int max_pages) {
+  return len <= 0 ? 0 : min((len - 1) / page + 1, max_pages);
+}
+__device__ inline bool in_pool(int p, int n_pages) { return (unsigned)p < (unsigned)n_pages; }
+
+constexpr int kBookThreads = 1024;  // of the calls that one workgroup makes
+constexpr int kBookWaves = kBookThreads / 64;
+
+// Inclusive sums over the workgroup's threads, in thread order, of one value or a
+// pair; s: kBookWaves entries.  Everyone gets the total too.
+template <typename T>
+__device__ inline T block_scan(T v, T* s, T* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  T incl = v;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const T x = __shfl_up(incl, d);
+    if (lane >= d) incl += x;
+  }
+  __syncthreads();  // s may still be read from the last scan
+  if (lane == 63) s[wave] = incl;
+  __syncthreads();
+  T before = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < kBookWaves; ++i) {
+    const T x = s[i];
+    if (i < wave) before += x;
+    all += x;
+  }
+  *total = all;
+  return before + incl;
+}
+
+// ------------------------------------------------------------------- fork
+// Row b becomes what row parent[b] was, or empty where parent[b] names none, all
+// rows at once.  A workgroup takes some columns of every row: what the rows get
+// goes to LDS before any of them is written.  Rows that stay are not read.
+// lens is read and written by the first workgroup alone.
+struct ForkArgs {
+  Pages p;
+  const int32_t* parent;
+  int cols;  // columns of a workgroup
+};
+
+__global__ __launch_bounds__(kBookThreads) void fork_kernel(ForkArgs a) {
+  extern __shared__ int32_t s_new[];  // [B][cols]
+  const Pages& p = a.p;
+  const int c0 = blockIdx.x * a.cols;
+  const int n = p.B * a.cols;
+  for (int i = threadIdx.x; i < n; i += kBookThreads) {
+    const int b = i / a.cols, c = c0 + i - b * a.cols;
+    const int from = a.parent[b];
+    int page = -1;
+    if (from != b && (unsigned)from < (unsigned)p.B && c < p.max_pages)
+      page = p.table[(size_t)from * p.max_pages + c];
+    s_new[i] = page;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kBookThreads) {
+    const int b = i / a.cols, c = c0 + i - b * a.cols;
+    if (a.parent[b] == b || c >= p.max_pages) continue;
+    int32_t* at = p.table + (size_t)b * p.max_pages + c;
+    const int was = *at, now = s_new[i];
+    if (was == now) continue;
+    *at = now;
+    if (in_pool(was, p.n_pages)) atomicAdd(p.refs + was, -1);
+    if (in_pool(now, p.n_pages)) atomicAdd(p.refs + now, 1);
+  }
+  if (blockIdx.x != 0) return;
+  __syncthreads();
+  for (int b = threadIdx.x; b < p.B; b += kBookThreads) {
+    const int from = a.parent[b];
+    s_new[b] = (unsigned)from < (unsigned)p.B ? p.lens[from] : 0;
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < p.B; b += kBookThreads) p.lens[b] = s_new[b];
+}
+
+// ---------------------------------------------------------------- reserve
+// Pages for n_new[b] more rows of every sequence.  One workgroup: the needs of the
+// sequences (thread t: a run of them, so that the scan follows their order), how
+// many pages are free, then the k-th free page goes to the sequence whose range of
+// needs holds k.  A sequence that writes into a partly filled page which others
+// name too gets a fresh one for it, but for the last writer of a page that only
+// writers name.  If the pages do not suffice nothing is changed.
+struct ReserveArgs {
+  Pages p;
+  const int32_t* n_new;
+  int32_t* starts;
+  int32_t* granted;
+  int32_t* moves;  // [B][2]: from, to
+  int32_t* info;   // moves, pages dealt, pages missing, sequences past max_pages
+};
+
+constexpr int kStripPer = 16;  // counts a thread reads at once
+constexpr int kStrip = kStripPer * kBookThreads;
+
+// Bits of the free ones among 16 counts from `at` on
+__device__ inline uint32_t free_mask(const int32_t* refs, int at, int n_pages) {
+  uint32_t m = 0;
+  if (at + kStripPer <= n_pages) {
+    int4 v[kStripPer / 4];
+#pragma unroll
+    for (int i = 0; i < kStripPer / 4; ++i) v[i] = ((const int4*)(refs + at))[i];
+#pragma unroll
+    for (int i = 0; i < kStripPer / 4; ++i)
+      m |= (uint32_t)((v[i].x <= 0) | (v[i].y <= 0) << 1 | (v[i].z <= 0) << 2 | (v[i].w <= 0) << 3)
+           << (4 * i);
+  } else {
+    for (int i = 0; i < kStripPer && at + i < n_pages; ++i) m |= (uint32_t)(refs[at + i] <= 0) << i;
+  }
+  return m;
+}
+
+__global__ __launch_bounds__(kBookThreads) void reserve_kernel(ReserveArgs a) {
+  extern __shared__ int32_t smem[];
+  __shared__ unsigned long long s_scan[kBookWaves];
+  const Pages& p = a.p;
+  int32_t* const s_first = smem;            // needs before sequence b
+  int32_t* const s_had = s_first + p.B;     // its pages
+  int32_t* const s_move = s_had + p.B;      // its move; -1: no page is replaced, -2: without a copy
+  int32_t* const s_last = s_move + p.B;     // the shared page it writes into, else -1
+  const int tid = threadIdx.x;
+
+  // the counts of the first strip, on their way while the needs are formed
+  const int n_strips = (p.n_pages + kStrip - 1) / kStrip;
+  uint32_t mask0 = free_mask(p.refs, min(tid * kStripPer, p.n_pages), p.n_pages);
+
+  for (int b = tid; b < p.B; b += kBookThreads) {
+    const int len = max(p.lens[b], 0);
+    int last = -1;
+    if (a.n_new[b] > 0 && len % p.page != 0 && len / p.page < p.max_pages) {
+      const int e = p.table[(size_t)b * p.max_pages + len / p.page];
+      last = in_pool(e, p.n_pages) ? (p.refs[e] > 1 ? e : -1) : -2;
+    }
+    s_last[b] = last;
+  }
+  __syncthreads();
+  const int per = (p.B + kBookThreads - 1) / kBookThreads;
+  const int b0 = min(tid * per, p.B), b1 = min(b0 + per, p.B);
+  long long need = 0;
+  int n_moves = 0, over = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int len = max(p.lens[b], 0), n = max(a.n_new[b], 0);
+    const long long has = ((long long)len + n + p.page - 1) / p.page;
+    const int had = (int)(((long long)len + p.page - 1) / p.page);
+    const int last = s_last[b];
+    int move = -1;
+    if (last == -2) {
+      move = -2;
+    } else if (last >= 0) {
+      int left = p.refs[last];  // less the writers before this one
+      for (int e = 0; e < b; ++e) left -= s_last[e] == last;
+      if (left > 1) move = n_moves++;
+    }
+    over += has > p.max_pages && n > 0;
+    s_first[b] = (int)min(need, 0x7fffffffLL);
+    s_had[b] = had;
+    s_move[b] = move;
+    need += (n > 0 ? has - had : 0) + (move != -1);
+  }
+  // a run's needs may pass 32 bits only where a sequence is past max_pages
+  unsigned long long tot, tot2;
+  const unsigned long long mine =
+      (unsigned long long)min(need, 0x7fffffffLL) | (unsigned long long)n_moves << 44;
+  const unsigned long long incl = block_scan(mine, s_scan, &tot);
+  const unsigned long long over_free =
+      (unsigned long long)over << 40;
+  uint32_t n_free = __popc(mask0);
+  for (int s = 1; s < n_strips; ++s)
+    n_free += __popc(free_mask(p.refs, min(s * kStrip + tid * kStripPer, p.n_pages), p.n_pages));
+  block_scan(over_free + n_free, s_scan, &tot2);
+  const long long total = (long long)(tot & ((1ull << 44) - 1));
+  const long long all_free = (long long)(tot2 & ((1ull << 40) - 1));
+  const int all_over = (int)(tot2 >> 40), all_moves = (int)(tot >> 44);
+  const bool fits = all_over == 0 && total <= all_free;
+  const unsigned long long before = incl - mine;
+  for (int b = b0; b < b1; ++b) {
+    s_first[b] += (int)(before & ((1ull << 44) - 1));
+    if (s_move[b] >= 0) s_move[b] += (int)(before >> 44);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    a.info[0] = fits ? all_moves : 0;
+    a.info[1] = fits ? (int)total : 0;
+    a.info[2] = (int)min(max(total - all_free, 0LL), 0x7fffffffLL);
+    a.info[3] = all_over;
+  }
+  for (int b = tid; b < p.B; b += kBookThreads) {
+    const int n = fits ? max(a.n_new[b], 0) : 0;
+    const int len = max(p.lens[b], 0);
+    a.starts[b] = len;
+    a.granted[b] = n;
+    if (n > 0) p.lens[b] = len + n;
+    if (fits && s_move[b] >= 0) {
+      a.moves[2 * s_move[b]] = s_last[b];
+      atomicAdd(p.refs + s_last[b], -1);
+    }
+    if (b >= (fits ? all_moves : 0)) a.moves[2 * b] = a.moves[2 * b + 1] = -1;
+  }
+  if (!fits || total == 0) return;
+  unsigned long long base = 0;
+  for (int s = 0; s < n_strips && base < (unsigned long long)total; ++s) {
+    const int at = min(s * kStrip + tid * kStripPer, p.n_pages);
+    // pages dealt in an earlier strip are not read again, and the counts lowered
+    // above stay positive
+    uint32_t m = s == 0 ? mask0 : free_mask(p.refs, at, p.n_pages);
+    unsigned long long strip;
+    const int cnt = __popc(m);
+    long long k = (long long)(base + block_scan((unsigned long long)cnt, s_scan, &strip) - cnt);
+    base += strip;
+    int b = -1;
+    for (; m != 0 && k < total; m &= m - 1, ++k) {
+      const int page = at + __builtin_ctz(m);
+      if (b < 0 || (b + 1 < p.B && s_first[b + 1] <= k)) {  // the last sequence that begins at or before k
+        int lo = 0, hi = p.B - 1;
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) >> 1;
+          if (s_first[mid] <= k) lo = mid; else hi = mid - 1;
+        }
+        b = lo;
+      }
+      const int off = (int)(k - s_first[b]), move = s_move[b];
+      const int slot = s_had[b] + off - (move != -1);
+      p.table[(size_t)b * p.max_pages + slot] = page;
+      p.refs[page] = 1;
+      if (off == 0 && move >= 0) a.moves[2 * move + 1] = page;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- compact
+// With n pages in use, the i-th of those numbered n or more moves to the i-th free
+// one below n.  One workgroup lists the moves and where each page went; then the
+// tables follow.
+struct CompactArgs {
+  Pages p;
+  int32_t* moves;  // [n_pages / 2][2]
+  int32_t* to;     // [n_pages]: new number of the pages that move
+  int32_t* info;   // moves, pages in use, 0, 0
+};
+
+__global__ __launch_bounds__(kBookThreads) void compact_kernel(CompactArgs a) {
+  __shared__ unsigned long long s_scan[kBookWaves];
+  const Pages& p = a.p;
+  const int tid = threadIdx.x;
+  const int n_strips = (p.n_pages + kStrip - 1) / kStrip;
+  uint32_t mask0 = 0;
+  unsigned long long used = 0, n_live;
+  for (int s = 0; s < n_strips; ++s) {
+    const int at = min(s * kStrip + tid * kStripPer, p.n_pages);
+    const uint32_t m = free_mask(p.refs, at, p.n_pages);
+    if (s == 0) mask0 = m;
+    used += min(kStripPer, p.n_pages - at) - __popc(m);
+  }
+  block_scan(used, s_scan, &n_live);
+  const int live = (int)n_live;
+  unsigned long long base = 0;  // free pages below `live` (low half), used ones above it
+  for (int s = 0; s < n_strips; ++s) {
+    const int at = min(s * kStrip + tid * kStripPer, p.n_pages);
+    const uint32_t m = s == 0 ? mask0 : free_mask(p.refs, at, p.n_pages);
+    const int n = min(kStripPer, p.n_pages - at);
+    const uint32_t below = live >= at + 16 ? 0xffffu : live <= at ? 0u : (1u << (live - at)) - 1;
+    uint32_t holes = m & below, high = ~m & ~below & ((1u << n) - 1);
+    unsigned long long strip;
+    const unsigned long long cnt =
+        (unsigned long long)__popc(holes) | (unsigned long long)__popc(high) << 32;
+    const unsigned long long k = base + block_scan(cnt, s_scan, &strip) - cnt;
+    base += strip;
+    int i = (int)(uint32_t)k, j = (int)(k >> 32);
+    for (; holes != 0; holes &= holes - 1) a.moves[2 * i++ + 1] = at + __builtin_ctz(holes);
+    for (; high != 0; high &= high - 1) a.moves[2 * j++] = at + __builtin_ctz(high);
+  }
+  const int n_moves = (int)(uint32_t)base;  // as many free ones below as used ones above
+  __syncthreads();
+  for (int i = tid; i < p.n_pages / 2; i += kBookThreads) {
+    if (i < n_moves) {
+      const int from = a.moves[2 * i], to = a.moves[2 * i + 1];
+      a.to[from] = to;
+      p.refs[to] = p.refs[from];
+      p.refs[from] = 0;
+    } else {
+      a.moves[2 * i] = a.moves[2 * i + 1] = -1;
+    }
+  }
+  if (tid == 0) {
+    a.info[0] = n_moves;
+    a.info[1] = live;
+    a.info[2] = a.info[3] = 0;
+  }
+}
+
+__global__ __launch_bounds__(256) void retable_kernel(CompactArgs a) {
+  const Pages& p = a.p;
+  const size_t n = (size_t)p.B * p.max_pages;
+  const int live = a.info[1];
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
+    const int e = p.table[i];
+    if (e >= live && e < p.n_pages) p.table[i] = a.to[e];
+  }
+}
+
+// ------------------------------------------------------------- page copies
+// Moves are cut into units of 16 KB of one pool, dealt to the workgroups in turn.
+// Bound by HBM.
+constexpr int kCopyUnit = 16384;
+
+template <typename V>
+__device__ inline void copy_unit(const unsigned char* src, unsigned char* dst, int bytes) {
+  constexpr int kPer = 4;
+  const int n = bytes / (int)sizeof(V);
+  for (int i0 = 0; i0 < n; i0 += 256 * kPer) {
+    V v[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int i = i0 + 256 * j + threadIdx.x;
+      if (i < n) v[j] = __builtin_nontemporal_load((const V*)src + i);
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int i = i0 + 256 * j + threadIdx.x;
+      if (i < n) __builtin_nontemporal_store(v[j], (V*)dst + i);
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void copy_pages_kernel(CopyPools a, const int32_t* moves,
+                                                         const int32_t* info) {
+  const int per = a.first[a.n_pools];
+  const long long n = (long long)min(max(info[0], 0), a.max_moves) * per;
+  for (long long u = blockIdx.x; u < n; u += gridDim.x) {
+    const int mv = (int)(u / per), at = (int)(u - (long long)mv * per);
+    const int from = moves[2 * mv], to = moves[2 * mv + 1];
+    if (!in_pool(from, a.n_pages) || !in_pool(to, a.n_pages)) continue;
+    int i = 0;
+    while (at >= a.first[i + 1]) ++i;
+    const unsigned long long bytes = a.bytes[i], off = (unsigned long long)(at - a.first[i]) * kCopyUnit;
+    const int len = (int)min(bytes - off, (unsigned long long)kCopyUnit);
+    const unsigned char* src = a.ptr[i] + (unsigned long long)from * bytes + off;
+    unsigned char* dst = a.ptr[i] + (unsigned long long)to * bytes + off;
+    if ((((uintptr_t)a.ptr[i] | bytes) & 15) == 0)
+      copy_unit<u32x4>(src, dst, len);
+    else
+      copy_unit<unsigned int>(src, dst, len);
+  }
+}
+
+// ------------------------------------------------------------------ append
+// Rows of bf16 caches: a wave takes one new token (or several in turn), whose K and
+// V rows of all heads are contiguous on both sides, 16 bytes a lane.
+struct AppendArgs {
+  const u32x4* k;
+  const u32x4* v;
+  u32x4* kc;
+  u32x4* vc;
+  const int32_t* table;  // nullptr: page b is sequence b
+  const int32_t* starts;
+  const int32_t* n_new;  // nullptr: all
+  const int32_t* cu;     // packed rows; nullptr: n rows per sequence
+  int B, n, max_pages, n_pages, page, chunks;  // chunks: 16-byte pieces of a token's K
+  int rows_per_wave;
+  long long rows, cap;
+};
+
+constexpr int kAppendWaves = 4;
+
+__global__ __launch_bounds__(64 * kAppendWaves) void append_kernel(AppendArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long r0 = ((long long)blockIdx.x * kAppendWaves + wave) * a.rows_per_wave;
+  for (int i = 0; i < a.rows_per_wave; ++i) {
+    const long long t = r0 + i;
+    if (t >= a.rows) return;
+    int b, at;
+    if (a.cu != nullptr) {  // the last sequence that begins at or before t: cu is not decreasing
+      int before = 0;
+      for (int c = lane; c - lane < a.B; c += 64)
+        before += __popcll(__ballot(c < a.B && a.cu[c + 1] <= t));
+      b = __builtin_amdgcn_readfirstlane(before);
+      if (b >= a.B) continue;
+      const long long o = t - a.cu[b];
+      if (o < 0) continue;
+      at = (int)o;
+    } else {
+      b = (int)(t / a.n);
+      at = (int)(t - (long long)b * a.n);
+    }
+    if (a.n_new != nullptr && at >= a.n_new[b]) continue;
+    const long long pos = (long long)a.starts[b] + at;
+    if (pos < 0 || pos >= a.cap) continue;
+    const int slot = (int)(pos / a.page);
+    const int page = a.table != nullptr ? a.table[(size_t)b * a.max_pages + slot] : b;
+    if (!in_pool(page, a.n_pages)) continue;
+    const size_t to = ((size_t)page * a.page + (size_t)(pos - (long long)slot * a.page)) * a.chunks;
+    const size_t from = (size_t)t * a.chunks;
+    for (int c = lane; c < a.chunks; c += 64) {
+      const u32x4 x = a.k[from + c], y = a.v[from + c];
+      a.kc[to + c] = x;
+      a.vc[to + c] = y;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- launchers
+static int fork_cols(int B) {
+  int c = 32;  // 128 bytes of a row, 64 KB in all
+  while (c > 1 && (size_t)c * B * sizeof(int32_t) > (size_t)64 * 1024) c /= 2;
+  return c;
+}
+
+hipError_t launch_pages_fork(const Pages& p, const int32_t* parent, hipStream_t stream) {
+  ForkArgs a{p, parent, fork_cols(p.B)};
+  const int grid = (int)(((long long)p.max_pages + a.cols - 1) / a.cols);
+  const size_t lds = (size_t)a.cols * p.B * sizeof(int32_t);
+  hipLaunchKernelGGL(fork_kernel, dim3(grid), dim3(kBookThreads), lds, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_reserve(const Pages& p, const int32_t* n_new, int32_t* starts,
+                                int32_t* granted, int32_t* moves, int32_t* info,
+                                hipStream_t stream) {
+  ReserveArgs a{p, n_new, starts, granted, moves, info};
+  hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kBookThreads), (size_t)p.B * 16, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(const Pages& p, int32_t* moves, int32_t* to, int32_t* info,
+                                hipStream_t stream) {
+  CompactArgs a{p, moves, to, info};
+  hipLaunchKernelGGL(compact_kernel, dim3(1), dim3(kBookThreads), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const size_t n = (size_t)p.B * p.max_pages;
+  hipLaunchKernelGGL(retable_kernel, dim3((unsigned)std::min<size_t>((n + 255) / 256, 2048)),
+                     dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+// Units of one move over these pools; a.first is filled in.
+long long copy_units(CopyPools& a) {
+  long long at = 0;
+  for (int i = 0; i < a.n_pools; ++i) {
+    a.first[i] = (int)at;
+    at += (long long)((a.bytes[i] + kCopyUnit - 1) / kCopyUnit);
+    if (at > 0x7fffffffLL) return -1;
+  }
+  a.first[a.n_pools] = (int)at;
+  return at;
+}
+
+hipError_t launch_copy_pages(const CopyPools& a, const int32_t* moves, const int32_t* info,
+                             int n_cu, hipStream_t stream) {
+  const long long units = (long long)a.first[a.n_pools] * a.max_moves;
+  hipLaunchKernelGGL(copy_pages_kernel, dim3((unsigned)std::min<long long>(units, 8LL * n_cu)),
+                     dim3(256), 0, stream, a, moves, info);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_append(const uint16_t* k, const uint16_t* v, uint16_t* kc, uint16_t* vc,
+                               const int32_t* table, int max_pages, int n_pages, int page,
+                               const int32_t* starts, const int32_t* n_new, const int32_t* cu,
+                               int B, int n, int Hkv, hipStream_t stream) {
+  AppendArgs a;
+  a.k = (const u32x4*)k;
+  a.v = (const u32x4*)v;
+  a.kc = (u32x4*)kc;
+  a.vc = (u32x4*)vc;
+  a.table = table;
+  a.starts = starts;
+  a.n_new = n_new;
+  a.cu = cu;
+  a.B = B;
+  a.n = n;
+  a.max_pages = max_pages;
+  a.n_pages = n_pages;
+  a.page = page;
+  a.chunks = Hkv * (kHeadDim / 8);
+  a.rows = cu != nullptr ? n : (long long)B * n;
+  a.cap = table != nullptr ? (long long)max_pages * page : page;
+  a.rows_per_wave = 1;
+  const long long per = (long long)kAppendWaves * a.rows_per_wave;
+  hipLaunchKernelGGL(append_kernel, dim3((unsigned)((a.rows + per - 1) / per)),
+                     dim3(64 * kAppendWaves), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace jl
