@@ -716,6 +716,76 @@ int jl_cache_append(void* k_cache, void* v_cache, int n_pages, int page_size,
                     int n, int Hkv, int head_dim, void* stream);
 
 /*
+ * ---- decode over shared prefixes -------------------------------------------
+ * jl_bifocal_decode_paged for batches in which groups of sequences begin with the same
+ * tokens on the same pages (forks of a prompt, chats behind one system prompt): the keys
+ * and values of a prefix are read once for all the sequences of its group.  What a step's
+ * calls have in common is planned once, from the lengths, and serves every layer.
+ *
+ *   kv_lens       int32 [B] DEVICE array, the new token appended; clamped into
+ *                 [0, max_pages * page_size].  A sequence of length 0 gets zeros.
+ *   members       int32 [B] DEVICE array or NULL (0 .. B - 1): the sequences, group after
+ *                 group, each at most once; others than 0 .. B - 1 are passed over
+ *   group_starts  int32 [n_groups + 1] DEVICE array, non-decreasing in [0, B]: group i is
+ *                 members[group_starts[i]] .. members[group_starts[i + 1] - 1].  A group may
+ *                 be one sequence.  Sequences of no group are left out: their rows of the
+ *                 output stay as they were.
+ *   shared        int32 [n_groups] DEVICE array: tokens that the group's sequences have in
+ *                 common.  Of these whole pages below the shortest length count, and they
+ *                 are read from the pages of any of the group's sequences.
+ *   plan          jl_shared_plan_bytes(B, n_groups, Hq, Hkv) bytes on the device, 16-byte
+ *                 aligned (written).  It holds for decode calls of the same B, n_groups, Hq,
+ *                 Hkv, max_pages, page_size and views; a decode call whose plan was made for
+ *                 other sizes leaves its output as it was.
+ * page_size is a power of two, at least 16.  Hq / Hkv > 8, B or n_groups > 2048, or more than
+ * 8388608 (2^23) positions a sequence -> JL_ERR_UNSUPPORTED.  Nothing is allocated.
+ */
+size_t jl_shared_plan_bytes(int B, int n_groups, int Hq, int Hkv);
+
+int jl_bifocal_shared_plan(const int32_t* kv_lens, const int32_t* members,
+                           const int32_t* group_starts, const int32_t* shared, int B, int n_groups,
+                           int Hq, int Hkv, int head_dim, int max_pages, int page_size,
+                           int w_pretrained, int w_local, void* plan, size_t plan_bytes,
+                           void* stream);
+
+/* The plan of the vanilla decode (base rotations). */
+int jl_rope_shared_plan(const int32_t* kv_lens, const int32_t* members,
+                        const int32_t* group_starts, const int32_t* shared, int B, int n_groups,
+                        int Hq, int Hkv, int head_dim, int max_pages, int page_size, void* plan,
+                        size_t plan_bytes, void* stream);
+
+/* Bytes of workspace the shared decode needs; 0 for invalid arguments. */
+size_t jl_decode_shared_workspace_bytes(int B, int Hq, int Hkv, int head_dim);
+
+/*
+ * The decode: the result of jl_bifocal_decode_paged, up to rounding and the order of the
+ * sums, for every sequence of the plan.
+ *   q          bf16 [B, Hq, head_dim]  raw queries, sequence b's at kv_lens[b] - 1
+ *   k_pages, v_pages, block_table, page_size, n_pages: as in jl_bifocal_decode_paged; page
+ *              indices are clamped into the pool, which holds fewer than 2^31 tokens
+ *   plan       of jl_bifocal_shared_plan with the same sizes and windows
+ *   o          bf16 [B, Hq, head_dim]  output (written)
+ *   workspace  jl_decode_shared_workspace_bytes(B, Hq, Hkv, head_dim) bytes, 16-byte
+ *              aligned; contents on entry do not matter
+ * Rounded to bf16 are the rotated queries, the keys' cos and sin, the rotated keys and the
+ * softmax weights, whose rounded values the denominator sums; everything else is fp32.  The
+ * same plan and inputs give the same bits.  Only the cos/sin table may be allocated or grown.
+ */
+int jl_bifocal_decode_shared(const void* q, const void* k_pages, const void* v_pages,
+                             const int32_t* block_table, int max_pages, int page_size, int n_pages,
+                             const void* plan, size_t plan_bytes, void* o, int B, int n_groups,
+                             int Hq, int Hkv, int head_dim, double rope_theta, int w_pretrained,
+                             int w_local, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The vanilla counterpart, with a plan of jl_rope_shared_plan. */
+int jl_rope_attention_decode_shared(const void* q, const void* k_pages, const void* v_pages,
+                                    const int32_t* block_table, int max_pages, int page_size,
+                                    int n_pages, const void* plan, size_t plan_bytes, void* o,
+                                    int B, int n_groups, int Hq, int Hkv, int head_dim,
+                                    double rope_theta, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
+/*
  * Debug view of the schedule as the device computes it (Eqs. (2), (3), (5)),
  * for bit-exact tests.  All pointers are device pointers.
  *   lengths    int32 [n_lengths]              sequence lengths L (>= 1)

@@ -139,6 +139,22 @@ def lib() -> ctypes.CDLL:
         L.jl_cache_append.restype = i32
         L.jl_cache_append.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, i32, i32, i32,
                                       i32, vp]
+        L.jl_shared_plan_bytes.restype = sz
+        L.jl_shared_plan_bytes.argtypes = [i32, i32, i32, i32]
+        L.jl_bifocal_shared_plan.restype = i32
+        L.jl_bifocal_shared_plan.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, i32,
+                                             i32, vp, sz, vp]
+        L.jl_rope_shared_plan.restype = i32
+        L.jl_rope_shared_plan.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, sz,
+                                          vp]
+        L.jl_decode_shared_workspace_bytes.restype = sz
+        L.jl_decode_shared_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.jl_bifocal_decode_shared.restype = i32
+        L.jl_bifocal_decode_shared.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, sz, vp, i32, i32,
+                                               i32, i32, i32, dbl, i32, i32, vp, sz, vp]
+        L.jl_rope_attention_decode_shared.restype = i32
+        L.jl_rope_attention_decode_shared.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, sz, vp, i32,
+                                                      i32, i32, i32, i32, dbl, vp, sz, vp]
         L.jl_debug_schedule.restype = i32
         L.jl_debug_schedule.argtypes = [vp, i32, vp, i32, i32, vp, vp, vp, vp]
         L.jl_debug_prefill_tiles.restype = i32
@@ -998,6 +1014,102 @@ def cache_append(k_cache, v_cache, k, v, starts, *, n_new=None, cu_seqlens=None,
         _int(max_pages, "max_pages"), kp, vp, _on8(starts, "starts", i32, (B,), index, device),
         None if n_new is None else _on8(n_new, "n_new", i32, (B,), index, device), cp,
         _int(B, "B"), _int(n, "n"), _int(Hkv, "Hkv"), D, _queue(stream, index, device, "k_cache")))
+
+
+# ------------------------------------------- decode over shared prefixes
+class SharedPlan:
+    """What the decode calls of one step have in common (shared_plan): made for these sizes, windows
+    and lengths, for every layer."""
+
+    __slots__ = ("buf", "B", "n_groups", "Hq", "Hkv", "page_size", "max_pages", "w_pretrained",
+                 "w_local", "bifocal", "index", "device", "ptr", "nbytes")
+
+
+def shared_plan_bytes(B: int, n_groups: int, Hq: int, Hkv: int) -> int:
+    return int(lib().jl_shared_plan_bytes(B, n_groups, Hq, Hkv))
+
+
+def shared_plan(kv_lens, group_starts, shared, *, Hq: int, Hkv: int, page_size: int,
+                max_pages: int, members=None, w_pretrained: int = 1, w_local: int = 0,
+                bifocal: bool = True, out=None, stream=None) -> SharedPlan:
+    """jl_bifocal_shared_plan / jl_rope_shared_plan: kv_lens int32 [B]; group i is the sequences
+    members[group_starts[i]] .. members[group_starts[i + 1] - 1] (group_starts int32 [n_groups + 1],
+    members int32 [B], all in order if not given), which have their first shared[i] (int32
+    [n_groups]) tokens' pages in common.  out: a plan of the same sizes to write again, as a
+    captured step does."""
+    i32 = _t().int32
+    lp = _dev(kv_lens, "kv_lens", i32)
+    index, device = kv_lens.get_device(), kv_lens.device
+    if kv_lens.dim() != 1 or shared.dim() != 1:
+        raise ValueError("kv_lens must be [B], shared [n_groups]")
+    B, n = _int(kv_lens.shape[0], "B"), _int(shared.shape[0], "n_groups")
+    Hq, Hkv = _int(Hq, "Hq"), _int(Hkv, "Hkv")
+    page_size, max_pages = _int(page_size, "page_size"), _int(max_pages, "max_pages")
+    w_pretrained, w_local = _int(w_pretrained, "w_pretrained"), _int(w_local, "w_local")
+    raw = _queue(stream, index, device, "kv_lens")
+    key = (B, n, Hq, Hkv, page_size, max_pages, w_pretrained, w_local, bool(bifocal), index)
+    if out is None:
+        p = SharedPlan()
+        (p.B, p.n_groups, p.Hq, p.Hkv, p.page_size, p.max_pages, p.w_pretrained, p.w_local,
+         p.bifocal, p.index) = key
+        p.device = device
+        p.buf = _new(kv_lens, stream, (max(shared_plan_bytes(B, n, Hq, Hkv), 16),), _t().uint8)
+        p.ptr, p.nbytes = p.buf.data_ptr(), p.buf.numel()
+    else:
+        p = out
+        if not isinstance(p, SharedPlan) or key != (
+                p.B, p.n_groups, p.Hq, p.Hkv, p.page_size, p.max_pages, p.w_pretrained, p.w_local,
+                p.bifocal, p.index):
+            raise ValueError("out must be a plan of the same sizes and windows")
+    args = (lp, None if members is None else _on8(members, "members", i32, (B,), index, device),
+            _on8(group_starts, "group_starts", i32, (n + 1,), index, device),
+            _on8(shared, "shared", i32, (n,), index, device), B, n, Hq, Hkv, 128, max_pages,
+            page_size)
+    if bifocal:
+        _check(lib().jl_bifocal_shared_plan(*args, w_pretrained, w_local, p.ptr, p.nbytes, raw))
+    else:
+        _check(lib().jl_rope_shared_plan(*args, p.ptr, p.nbytes, raw))
+    return p
+
+
+def decode_shared_workspace_bytes(B: int, Hq: int, Hkv: int, head_dim: int = 128) -> int:
+    return int(lib().jl_decode_shared_workspace_bytes(B, Hq, Hkv, head_dim))
+
+
+def decode_shared(q, k_pages, v_pages, block_table, plan, *, rope_theta: float = 1e6, out=None,
+                  workspace=None, stream=None):
+    """jl_bifocal_decode_shared / jl_rope_attention_decode_shared, as the plan was made: q [B, Hq,
+    128] raw over pools [n_pages, page_size, Hkv, 128] raw, block_table int32 [B, max_pages].  Rows
+    of `out` for sequences that no group of the plan has stay as they were."""
+    torch = _t()
+    if not isinstance(plan, SharedPlan):
+        raise TypeError("plan must be a SharedPlan")
+    bf16, index, device = torch.bfloat16, plan.index, plan.device
+    B, Hq, Hkv = plan.B, plan.Hq, plan.Hkv
+    qp = _on8(q, "q", bf16, (B, Hq, 128), index, device)
+    kp = _on8(k_pages, "k_pages", bf16, None, index, device)
+    shape = k_pages.shape
+    if len(shape) != 4 or shape[1:] != (plan.page_size, Hkv, 128):
+        raise ValueError("page pools must be [n_pages, %d, %d, 128]" % (plan.page_size, Hkv))
+    vp = _on8(v_pages, "v_pages", bf16, shape, index, device)
+    tp = _on8(block_table, "block_table", torch.int32, (B, plan.max_pages), index, device)
+    raw = _queue(stream, index, device, "plan")
+    if out is None:
+        out = _new(q, stream, q.shape, bf16)
+        op = out.data_ptr()
+    else:
+        op = _on8(out, "out", bf16, (B, Hq, 128), index, device)
+    if workspace is None:
+        workspace = _new(q, stream, (decode_shared_workspace_bytes(B, Hq, Hkv),), torch.uint8)
+    wp = _on8(workspace, "workspace", getattr(workspace, "dtype", None), None, index, device)
+    args = (qp, kp, vp, tp, plan.max_pages, plan.page_size, _int(shape[0], "n_pages"), plan.ptr,
+            plan.nbytes, op, B, plan.n_groups, Hq, Hkv, 128, float(rope_theta))
+    if plan.bifocal:
+        _check(lib().jl_bifocal_decode_shared(*args, plan.w_pretrained, plan.w_local, wp,
+                                              workspace.nbytes, raw))
+    else:
+        _check(lib().jl_rope_attention_decode_shared(*args, wp, workspace.nbytes, raw))
+    return out
 
 
 def debug_schedule(lengths, positions, w_pretrained: int, stream=None):

@@ -17,8 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libjetlong.so")
 SOURCES = ["prefill.hip", "decode.hip", "cache8.hip", "decode8.hip", "blocks8.hip", "pages.hip",
-           "aux.hip",
-           "jl_api.cpp"]
+           "decode_shared.hip", "aux.hip", "jl_api.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -16,10 +16,12 @@
 
 #include "../../include/jetlong.h"
 #include "cache8.h"
+#include "decode_shared.h"
 #include "pages.h"
 
 namespace jl {
-// kernels (prefill.hip, decode.hip, cache8.hip, decode8.hip, blocks8.hip, pages.hip, aux.hip)
+// kernels (prefill.hip, decode.hip, cache8.hip, decode8.hip, blocks8.hip, pages.hip,
+// decode_shared.hip, aux.hip)
 hipError_t launch_prefill_chunk(bool bifocal, const uint16_t* q, const uint16_t* k,
                                 const uint16_t* v, uint16_t* o, float* lse, const float2* table,
                                 const float2* rtable, const uint32_t* table16,
@@ -82,6 +84,18 @@ hipError_t launch_block_scores8(bool bifocal, const Cache8& c, const uint16_t* q
 hipError_t launch_select_blocks(const float* scores, const int32_t* kv_lens, int32_t* blocks,
                                 int B, int Hkv, int n_blocks, int n_select, int w0, int n_first,
                                 hipStream_t stream);
+size_t shared_plan_bytes(int B, int n_groups, int g);
+size_t decode_shared_workspace_bytes(int B, int Hq, int Hkv);
+hipError_t launch_shared_plan(bool bifocal, const int32_t* kv_lens, const int32_t* members,
+                              const int32_t* group_starts, const int32_t* shared, int B,
+                              int n_groups, int Hq, int Hkv, int max_pages, int page, int w_pre,
+                              int w0, int n_cu, void* plan, hipStream_t stream);
+hipError_t launch_decode_shared(bool bifocal, const uint16_t* q, const uint16_t* k,
+                                const uint16_t* v, const int32_t* table, int max_pages,
+                                int n_pages, int page_shift, void* plan, uint16_t* o,
+                                const float2* rope, const uint32_t* rope16, int B, int n_groups,
+                                int Hq, int Hkv, int w_pre, int w0, int n_cu, void* ws,
+                                hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1);
 hipError_t launch_pages_fork(const Pages& p, const int32_t* parent, hipStream_t stream);
 hipError_t launch_pages_reserve(const Pages& p, const int32_t* n_new, int32_t* starts,
                                 int32_t* granted, int32_t* moves, int32_t* info,
@@ -772,6 +786,95 @@ int check_pages(const jl_pages* t, jl::Pages* out) {
   return JL_OK;
 }
 
+// ----------------------------------------- decode over shared prefixes
+// What the plan and the decode call have in common; *page_shift is set.
+int check_shared(int B, int n_groups, int Hq, int Hkv, int head_dim, int max_pages, int page_size,
+                 bool bifocal, int w_pre, int w0, int* page_shift) {
+  const int st = check_common(B, Hq, Hkv, head_dim, 1.0);
+  if (st != JL_OK) return st;
+  if (Hq / Hkv > 8) return fail(JL_ERR_UNSUPPORTED, "decode GQA group %d > 8", Hq / Hkv);
+  if (n_groups < 1) return fail(JL_ERR_INVALID_ARG, "n_groups must be >= 1 (got %d)", n_groups);
+  if (B > jl::kShMaxSeqs || n_groups > jl::kShMaxSeqs)
+    return fail(JL_ERR_UNSUPPORTED, "%d sequences in %d groups (at most %d of each)", B, n_groups,
+                jl::kShMaxSeqs);
+  if (page_size < 16 || page_size > (1 << 20) || (page_size & (page_size - 1)) != 0)
+    return fail(JL_ERR_INVALID_ARG, "page_size must be a power of two in [16, 2^20] (got %d)",
+                page_size);
+  if (max_pages < 1) return fail(JL_ERR_INVALID_ARG, "max_pages must be >= 1 (got %d)", max_pages);
+  if ((long long)max_pages * page_size > kDecodeMaxLen)
+    return fail(JL_ERR_UNSUPPORTED, "max_pages * page_size exceeds %d positions", kDecodeMaxLen);
+  if (Hkv > 65535) return fail(JL_ERR_INVALID_ARG, "Hkv too large");
+  if (bifocal && w_pre < 1)
+    return fail(JL_ERR_INVALID_ARG, "w_pretrained must be >= 1 (got %d)", w_pre);
+  if (bifocal && w0 < 0) return fail(JL_ERR_INVALID_ARG, "w_local must be >= 0 (got %d)", w0);
+  *page_shift = 0;
+  while ((1 << *page_shift) < page_size) ++*page_shift;
+  return JL_OK;
+}
+
+int shared_plan(bool bifocal, const int32_t* kv_lens, const int32_t* members,
+                const int32_t* group_starts, const int32_t* shared, int B, int n_groups, int Hq,
+                int Hkv, int head_dim, int max_pages, int page_size, int w_pre, int w0, void* plan,
+                size_t plan_bytes, void* stream) {
+  int shift = 0;
+  const int st = check_shared(B, n_groups, Hq, Hkv, head_dim, max_pages, page_size, bifocal, w_pre,
+                              w0, &shift);
+  if (st != JL_OK) return st;
+  if (!aligned4(kv_lens) || !aligned4(group_starts) || !aligned4(shared))
+    return fail(JL_ERR_INVALID_ARG, "kv_lens, group_starts, shared must be non-null and aligned");
+  if (members != nullptr && !aligned4(members))
+    return fail(JL_ERR_INVALID_ARG, "members must be 4-byte aligned");
+  const size_t need = jl::shared_plan_bytes(B, n_groups, Hq / Hkv);
+  if (plan == nullptr || plan_bytes < need)
+    return fail(JL_ERR_WORKSPACE, "plan needs %zu bytes, got %zu", need, plan_bytes);
+  if (!aligned16(plan)) return fail(JL_ERR_INVALID_ARG, "plan must be 16-byte aligned");
+  const hipError_t e = jl::launch_shared_plan(
+      bifocal, kv_lens, members, group_starts, shared, B, n_groups, Hq, Hkv, max_pages, page_size,
+      w_pre, w0, jl::cu_count(), plan, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "shared plan launch");
+  return ok();
+}
+
+int decode_shared(bool bifocal, const void* q, const void* kp, const void* vp,
+                  const int32_t* table, int max_pages, int page_size, int n_pages,
+                  const void* plan, size_t plan_bytes, void* o, int B, int n_groups, int Hq,
+                  int Hkv, int head_dim, double theta, int w_pre, int w0, void* ws,
+                  size_t ws_bytes, void* stream) {
+  int shift = 0;
+  int st = check_shared(B, n_groups, Hq, Hkv, head_dim, max_pages, page_size, bifocal, w_pre, w0,
+                        &shift);
+  if (st != JL_OK) return st;
+  if (!(theta > 0.0) || !std::isfinite(theta))
+    return fail(JL_ERR_INVALID_ARG, "rope_theta must be finite and > 0");
+  if (n_pages < 1) return fail(JL_ERR_INVALID_ARG, "n_pages must be >= 1 (got %d)", n_pages);
+  if ((long long)n_pages * page_size > 0x7fffffffLL)
+    return fail(JL_ERR_UNSUPPORTED, "a pool of %lld tokens (at most 2^31 - 1)",
+                (long long)n_pages * page_size);
+  if (!aligned16(q) || !aligned16(kp) || !aligned16(vp) || !aligned16(o))
+    return fail(JL_ERR_INVALID_ARG, "q, k_pages, v_pages, o must be non-null and 16-byte aligned");
+  if (!aligned4(table)) return fail(JL_ERR_INVALID_ARG, "block_table must be non-null and aligned");
+  if (plan == nullptr || plan_bytes < jl::shared_plan_bytes(B, n_groups, Hq / Hkv))
+    return fail(JL_ERR_WORKSPACE, "plan needs %zu bytes, got %zu",
+                jl::shared_plan_bytes(B, n_groups, Hq / Hkv), plan_bytes);
+  const size_t need = jl::decode_shared_workspace_bytes(B, Hq, Hkv);
+  if (ws == nullptr || ws_bytes < need)
+    return fail(JL_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, ws_bytes);
+  if (!aligned16(plan) || !aligned16(ws))
+    return fail(JL_ERR_INVALID_ARG, "plan and workspace must be 16-byte aligned");
+  Tables tab{};
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  st = get_table(theta, max_pages * page_size, s, &tab);
+  if (st != JL_OK) return st;
+  hipEvent_t ev0, ev1;
+  timing_events(1, &ev0, &ev1);
+  const hipError_t e = jl::launch_decode_shared(
+      bifocal, (const uint16_t*)q, (const uint16_t*)kp, (const uint16_t*)vp, table, max_pages,
+      n_pages, shift, const_cast<void*>(plan), (uint16_t*)o, tab.f32, tab.f16, B, n_groups, Hq, Hkv,
+      w_pre, w0, jl::cu_count(), ws, s, ev0, ev1);
+  if (e != hipSuccess) return hip_fail(e, "shared decode launch");
+  return ok();
+}
+
 }  // namespace
 
 extern "C" {
@@ -1249,6 +1352,58 @@ int jl_cache_append(void* k_cache, void* v_cache, int n_pages, int page_size,
       reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "append launch");
   return ok();
+}
+
+size_t jl_shared_plan_bytes(int B, int n_groups, int Hq, int Hkv) {
+  if (B < 1 || n_groups < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq / Hkv > 8 ||
+      B > jl::kShMaxSeqs || n_groups > jl::kShMaxSeqs)
+    return 0;
+  return jl::shared_plan_bytes(B, n_groups, Hq / Hkv);
+}
+
+int jl_bifocal_shared_plan(const int32_t* kv_lens, const int32_t* members,
+                           const int32_t* group_starts, const int32_t* shared, int B, int n_groups,
+                           int Hq, int Hkv, int head_dim, int max_pages, int page_size,
+                           int w_pretrained, int w_local, void* plan, size_t plan_bytes,
+                           void* stream) {
+  return shared_plan(true, kv_lens, members, group_starts, shared, B, n_groups, Hq, Hkv, head_dim,
+                     max_pages, page_size, w_pretrained, w_local, plan, plan_bytes, stream);
+}
+
+int jl_rope_shared_plan(const int32_t* kv_lens, const int32_t* members,
+                        const int32_t* group_starts, const int32_t* shared, int B, int n_groups,
+                        int Hq, int Hkv, int head_dim, int max_pages, int page_size, void* plan,
+                        size_t plan_bytes, void* stream) {
+  return shared_plan(false, kv_lens, members, group_starts, shared, B, n_groups, Hq, Hkv, head_dim,
+                     max_pages, page_size, 1, 0, plan, plan_bytes, stream);
+}
+
+size_t jl_decode_shared_workspace_bytes(int B, int Hq, int Hkv, int head_dim) {
+  if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq / Hkv > 8 || head_dim != kHeadDim ||
+      B > jl::kShMaxSeqs)
+    return 0;
+  return jl::decode_shared_workspace_bytes(B, Hq, Hkv);
+}
+
+int jl_bifocal_decode_shared(const void* q, const void* k_pages, const void* v_pages,
+                             const int32_t* block_table, int max_pages, int page_size, int n_pages,
+                             const void* plan, size_t plan_bytes, void* o, int B, int n_groups,
+                             int Hq, int Hkv, int head_dim, double rope_theta, int w_pretrained,
+                             int w_local, void* workspace, size_t workspace_bytes, void* stream) {
+  return decode_shared(true, q, k_pages, v_pages, block_table, max_pages, page_size, n_pages, plan,
+                       plan_bytes, o, B, n_groups, Hq, Hkv, head_dim, rope_theta, w_pretrained,
+                       w_local, workspace, workspace_bytes, stream);
+}
+
+int jl_rope_attention_decode_shared(const void* q, const void* k_pages, const void* v_pages,
+                                    const int32_t* block_table, int max_pages, int page_size,
+                                    int n_pages, const void* plan, size_t plan_bytes, void* o,
+                                    int B, int n_groups, int Hq, int Hkv, int head_dim,
+                                    double rope_theta, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
+  return decode_shared(false, q, k_pages, v_pages, block_table, max_pages, page_size, n_pages,
+                       plan, plan_bytes, o, B, n_groups, Hq, Hkv, head_dim, rope_theta, 1, 0,
+                       workspace, workspace_bytes, stream);
 }
 
 int jl_debug_schedule(const int32_t* lengths, int n_lengths, const int32_t* positions,

@@ -110,3 +110,58 @@ def test_the_model_keeps_its_counts():
         m.count()
         assert refs == m.refs
         assert all(sum(p >= 0 for p in r) == n_pages_of(n, 8) for r, n in zip(m.table, m.lens))
+
+
+def _plan(fn="jl_bifocal_shared_plan", **kw):
+    d = dict(lens=A, members=None, starts=A, shared=A, B=4, n=2, Hq=8, Hkv=2, d=128, max_pages=8,
+             page=64, w=32, w0=4, plan=A, bytes=1 << 20)
+    d.update(kw)
+    views = (d["w"], d["w0"]) if "bifocal" in fn else ()
+    return getattr(api.lib(), fn)(d["lens"], d["members"], d["starts"], d["shared"], d["B"], d["n"],
+                                  d["Hq"], d["Hkv"], d["d"], d["max_pages"], d["page"], *views,
+                                  d["plan"], d["bytes"], None)
+
+
+SIZES = [(dict(B=0), BAD), (dict(n=0), BAD), (dict(Hq=7), BAD), (dict(Hkv=0), BAD), (dict(d=64), UNS),
+         (dict(d=3), BAD), (dict(Hq=18), UNS), (dict(B=2049), UNS), (dict(n=2049), UNS),
+         (dict(page=8), BAD), (dict(page=48), BAD), (dict(max_pages=0), BAD),
+         (dict(max_pages=1 << 18), UNS), (dict(Hq=1 << 17, Hkv=1 << 17), BAD)]
+
+
+@pytest.mark.parametrize("kw,code", SIZES + [
+    (dict(lens=None), BAD), (dict(starts=MIS), BAD), (dict(shared=None), BAD), (dict(members=MIS), BAD),
+    (dict(plan=None), api.JL_ERR_WORKSPACE), (dict(bytes=64), api.JL_ERR_WORKSPACE),
+    (dict(plan=P(0x1008)), BAD)])
+def test_plan_arguments_are_checked(kw, code):
+    assert _plan(**kw) == code
+    assert _plan("jl_rope_shared_plan", **kw) == code
+
+
+def test_plan_windows_are_checked():
+    assert _plan(w=0) == BAD and _plan(w0=-1) == BAD
+
+
+@pytest.mark.parametrize("kw,code", SIZES + [
+    (dict(q=None), BAD), (dict(k=MIS), BAD), (dict(v=None), BAD), (dict(o=P(0x1004)), BAD),
+    (dict(table=None), BAD), (dict(plan=None), api.JL_ERR_WORKSPACE), (dict(theta=0.0), BAD),
+    (dict(plan_bytes=8), api.JL_ERR_WORKSPACE), (dict(ws=None), api.JL_ERR_WORKSPACE),
+    (dict(ws_bytes=100), api.JL_ERR_WORKSPACE), (dict(ws=P(0x1004)), BAD), (dict(n_pages=0), BAD),
+    (dict(n_pages=1 << 26), UNS), (dict(theta=float("inf")), BAD)])
+def test_shared_decode_arguments_are_checked(kw, code):
+    d = dict(q=A, k=A, v=A, table=A, max_pages=8, page=64, n_pages=32, plan=A, plan_bytes=1 << 24, o=A,
+             B=4, n=2, Hq=8, Hkv=2, d=128, theta=1e6, ws=A, ws_bytes=1 << 40)
+    d.update(kw)
+    head = (d["q"], d["k"], d["v"], d["table"], d["max_pages"], d["page"], d["n_pages"], d["plan"],
+            d["plan_bytes"], d["o"], d["B"], d["n"], d["Hq"], d["Hkv"], d["d"], d["theta"])
+    L = api.lib()
+    assert L.jl_bifocal_decode_shared(*head, 32, 4, d["ws"], d["ws_bytes"], None) == code
+    assert L.jl_rope_attention_decode_shared(*head, d["ws"], d["ws_bytes"], None) == code
+
+
+def test_sizes_of_plans_and_workspaces():
+    assert api.shared_plan_bytes(4, 2, 8, 2) > 0
+    assert api.decode_shared_workspace_bytes(4, 8, 2) % 16 == 0
+    for bad in ((0, 1, 8, 2), (4, 0, 8, 2), (4, 1, 7, 2), (4, 1, 18, 2), (4096, 1, 8, 2)):
+        assert api.shared_plan_bytes(*bad) == 0
+    assert api.decode_shared_workspace_bytes(4, 8, 2, 64) == 0
+    assert api.decode_shared_workspace_bytes(4096, 8, 2) == 0
