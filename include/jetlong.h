@@ -786,6 +786,41 @@ int jl_rope_attention_decode_shared(const void* q, const void* k_pages, const vo
                                     void* stream);
 
 /*
+ * Packed chunks behind paged caches of different lengths: the next turns of several
+ * sequences, drafts to be verified, or single tokens among them, in one call.
+ *   q, o         bf16 [total_tokens, Hq, head_dim]: sequence b's rows are cu_seqlens[b] ..
+ *                cu_seqlens[b + 1] - 1, n of them, at its positions kv_lens[b] - n ..
+ *                kv_lens[b] - 1
+ *   lse          NULL or fp32 [Hq, total_tokens], natural-log row sums
+ *   kv_lens      int32 [B] DEVICE array: keys of each sequence, the chunk's own (written
+ *                before the call) among them; clamped into [0, max_pages * page_size]
+ *   cu_seqlens   int32 [B + 1] DEVICE array, non-decreasing from 0 to total_tokens; other
+ *                bounds are clamped, a decreasing one gives an empty sequence
+ *   k_pages, v_pages, block_table, page_size, n_pages: as in jl_bifocal_decode_shared
+ * Every sequence has its own G = max(1, ceil(kv_lens[b] / w_pretrained)), as a chunk of
+ * jl_bifocal_prefill_chunk_paged that ends there: the same result up to rounding and the
+ * order of the sums.  Rows of no sequence, or before position 0 (more rows than keys), are
+ * left as they were.  Hq / Hkv at most 256; B > 2048, or about a million rows (total_tokens *
+ * Hq / Hkv) in one call -> JL_ERR_UNSUPPORTED.  Scratch (the prefill scratch of the stream):
+ * 528 bytes for every query row and kv head twice, and up to 35 MB.  The same call gives the
+ * same bits.
+ */
+int jl_bifocal_prefill_varlen_paged(const void* q, const void* k_pages, const void* v_pages,
+                                    const int32_t* block_table, int max_pages, int page_size,
+                                    int n_pages, const int32_t* cu_seqlens,
+                                    const int32_t* kv_lens, void* o, float* lse, int B,
+                                    int total_tokens, int Hq, int Hkv, int head_dim,
+                                    double rope_theta, int w_pretrained, int w_local,
+                                    void* stream);
+
+/* The vanilla counterpart of jl_bifocal_prefill_varlen_paged. */
+int jl_rope_attention_varlen_paged(const void* q, const void* k_pages, const void* v_pages,
+                                   const int32_t* block_table, int max_pages, int page_size,
+                                   int n_pages, const int32_t* cu_seqlens, const int32_t* kv_lens,
+                                   void* o, float* lse, int B, int total_tokens, int Hq, int Hkv,
+                                   int head_dim, double rope_theta, void* stream);
+
+/*
  * Debug view of the schedule as the device computes it (Eqs. (2), (3), (5)),
  * for bit-exact tests.  All pointers are device pointers.
  *   lengths    int32 [n_lengths]              sequence lengths L (>= 1)

@@ -155,6 +155,12 @@ def lib() -> ctypes.CDLL:
         L.jl_rope_attention_decode_shared.restype = i32
         L.jl_rope_attention_decode_shared.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, sz, vp, i32,
                                                       i32, i32, i32, i32, dbl, vp, sz, vp]
+        L.jl_bifocal_prefill_varlen_paged.restype = i32
+        L.jl_bifocal_prefill_varlen_paged.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp,
+                                                      i32, i32, i32, i32, i32, dbl, i32, i32, vp]
+        L.jl_rope_attention_varlen_paged.restype = i32
+        L.jl_rope_attention_varlen_paged.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp,
+                                                     i32, i32, i32, i32, i32, dbl, vp]
         L.jl_debug_schedule.restype = i32
         L.jl_debug_schedule.argtypes = [vp, i32, vp, i32, i32, vp, vp, vp, vp]
         L.jl_debug_prefill_tiles.restype = i32
@@ -1110,6 +1116,51 @@ def decode_shared(q, k_pages, v_pages, block_table, plan, *, rope_theta: float =
     else:
         _check(lib().jl_rope_attention_decode_shared(*args, wp, workspace.nbytes, raw))
     return out
+
+
+def prefill_varlen_paged(q, k_pages, v_pages, block_table, cu_seqlens, kv_lens, *,
+                         w_pretrained: int = 1, w_local: int = 0, rope_theta: float = 1e6,
+                         bifocal: bool = True, out=None, lse=None, want_lse: bool = False,
+                         stream=None):
+    """jl_bifocal_prefill_varlen_paged / jl_rope_attention_varlen_paged: packed raw queries q [T, Hq,
+    128], sequence b's cu_seqlens[b] .. cu_seqlens[b + 1] - 1 (int32 [B + 1]) at the last of its
+    kv_lens[b] (int32 [B]) positions, over pools [n_pages, page_size, Hkv, 128] raw, block_table
+    int32 [B, max_pages]; lse is [Hq, T]."""
+    torch = _t()
+    bf16, i32 = torch.bfloat16, torch.int32
+    qp = _dev(q, "q", bf16)
+    index, device = q.get_device(), q.device
+    kp = _on8(k_pages, "k_pages", bf16, None, index, device)
+    shape = k_pages.shape
+    if q.dim() != 3 or len(shape) != 4 or shape[3] != q.shape[2]:
+        raise ValueError("q must be [T, Hq, D], page pools [n_pages, page_size, Hkv, D]")
+    T, Hq, D = q.shape
+    vp = _on8(v_pages, "v_pages", bf16, shape, index, device)
+    tp = _on8(block_table, "block_table", i32, None, index, device)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_pages]")
+    B, max_pages = block_table.shape
+    cp = _on8(cu_seqlens, "cu_seqlens", i32, (B + 1,), index, device)
+    lp = _on8(kv_lens, "kv_lens", i32, (B,), index, device)
+    raw = _queue(stream, index, device, "q")
+    if out is None:
+        out = _new(q, stream, q.shape, bf16)
+        op = out.data_ptr()
+    else:
+        op = _on8(out, "out", bf16, q.shape, index, device)
+    want_lse = want_lse or lse is not None
+    if lse is None and want_lse:
+        lse = _new(q, stream, (Hq, T), torch.float32)
+    args = (qp, kp, vp, tp, _int(max_pages, "max_pages"), _int(shape[1], "page_size"),
+            _int(shape[0], "n_pages"), cp, lp, op,
+            None if lse is None else _on8(lse, "lse", torch.float32, (Hq, T), index, device),
+            _int(B, "B"), _int(T, "T"), Hq, _int(shape[2], "Hkv"), D, float(rope_theta))
+    if bifocal:
+        _check(lib().jl_bifocal_prefill_varlen_paged(*args, _int(w_pretrained, "w_pretrained"),
+                                                     _int(w_local, "w_local"), raw))
+    else:
+        _check(lib().jl_rope_attention_varlen_paged(*args, raw))
+    return (out, lse) if want_lse else out
 
 
 def debug_schedule(lengths, positions, w_pretrained: int, stream=None):

@@ -1,27 +1,30 @@
-// decode_shared.hip -- one new token of every sequence over a paged bf16 cache in
-// which sequences share a prefix: its keys and values are read once for all of them.
+// decode_shared.hip -- attention of few query rows over long paged bf16 caches: one new
+// token of every sequence, where groups of sequences share a prefix whose keys and
+// values are read once for all of them, and packed chunks of new tokens behind caches
+// of different lengths.
 //
-// Jet-Long (arXiv 2607.07740): the query of sequence b sits at q = L - 1, L its length,
-// and takes a key k in the base view where q - k <= w0, else in the remote view of its
-// own G = max(1, ceil(L / w_pretrained)) (Sec. 3, Eqs. (1)-(3)).  The softmax over a
-// sequence's keys is the merge (Eq. (7)) of those over any parts of them, so the keys
-// that n sequences share make one attention of n g rows (g query heads of a kv head),
-// matrix shaped, and the rest of each sequence one of g rows.
+// Jet-Long (arXiv 2607.07740): the query of a sequence of L tokens at position q takes a
+// key k <= q in the base view where q - k <= w0, else in the remote view of G = max(1,
+// ceil(L / w_pretrained)) (Sec. 3, Eqs. (1)-(3)).  The softmax over a row's keys is the
+// merge (Eq. (7)) of those over any parts of them, so the keys that n sequences share
+// make one attention of n g rows (g query heads of a kv head), matrix shaped, and the
+// rest of each sequence one of g rows; n tokens of a chunk make one of n g.
 //
-// Plan (once per step, for every layer).  A segment is such an attention: up to 256
-// rows, i.e. up to 256 / g sequences of a group, over the group's prefix, or one
-// sequence over what lies behind it.  Its visits are grouped by the view that the
-// keys are rotated to: one phase for each G >= 2 that occurs among its sequences, over
-// the tiles that hold a remote key for one of these, and one in the base view.  The phases of
-// all segments are one list, in which a tile of 32 keys counts what it costs; the
-// workgroups of a kv head take equal ranges of it, whatever segments these span.
+// Plan.  A segment is such an attention: up to 256 rows over one range of keys, in
+// visits of 32 keys: a visit in the remote view for each tile that holds a remote key and each G >= 2
+// that occurs among its rows (one tile's visits follow each other, so that the later ones
+// find it in the L2), then one in the base view for each tile that holds a local key.
+// All segments' visits are one list, in which a visit counts what it costs; the
+// workgroups of a kv head take equal ranges of it, whatever segments these span.  The plan
+// follows from the lengths, so that a decoding step makes it once for all layers.
 //
 // Kernel: a workgroup (8 waves, one CU) streams the tiles of its range through a ring
 // in LDS, K, V and the cos/sin rows of the keys' positions, four tiles in flight.  While
-// tile i is multiplied, tile i + 1 is rotated in place, four keys a wave.  A wave owns
-// 32 rows: S^T = K Q^T, online softmax of a row per lane pair, O^T += V^T P^T, as the
-// prefill kernel.  Each (workgroup, segment) leaves its rows' states (m, l, O) in fp32,
-// and the merge kernel joins those of a row.
+// tile i is multiplied, tile i + 1 is rotated in place, four keys a wave.  Up to 128
+// rows, a wave takes 32 rows and half of the tile's keys, on 16 x 16 matrix instructions;
+// above, 32 rows and all keys, on 32 x 32 ones.  Each (workgroup, segment) leaves its
+// rows' states (m, l, O) in fp32, one for each half of the keys, and the merge kernel joins
+// those of a row.
 #include <algorithm>
 #include <climits>
 
@@ -32,77 +35,107 @@ namespace jl {
 
 constexpr int kShThreads = 512, kShWaves = 8;
 constexpr int kShRows = 32 * kShWaves;  // rows of a segment at most
+constexpr int kShSmall = kShRows / 2;   // rows of a segment whose keys two waves share
 constexpr int kShTile = 32;             // keys of a tile
-constexpr int kShImg = kShTile * kHeadDim * 2;       // K or V of a tile: 8 KB
-constexpr int kShBuf = 2 * kShImg + kShTile * 256;   // and its 32 rows of bf16 (cos, sin)
+constexpr int kShImg = kShTile * kHeadDim * 2;      // K or V of a tile: 8 KB
+constexpr int kShBuf = 2 * kShImg + kShTile * 256;  // and its 32 rows of bf16 (cos, sin)
 constexpr int kShBufs = 6;
 constexpr int kShAhead = kShBufs - 1;  // tiles requested before the first is used
-constexpr int kShList = 256;           // tiles whose addresses are formed at once
+constexpr int kShList = 256;           // visits whose addresses are held; refilled by halves
+constexpr int kShSegs = 64;            // segments whose records are held
 constexpr int kShCopies = 3;           // of a wave per tile
 
-// What a tile costs in the list, and a phase beside its tiles.
-constexpr int kTileCost = 4, kPhaseCost = 16;
-__host__ __device__ inline int tile_cost(int rows) { return rows <= 128 ? kTileCost : kTileCost + 2; }
-constexpr int kMaxStep = kTileCost + 2 + kPhaseCost;  // most between two tiles that follow each other
+// What a visit costs in the list, and a segment beside its visits.
+constexpr int kVisitCost = 4, kSegCost = 16;
+__host__ __device__ inline int visit_cost(int rows) {
+  return rows <= kShSmall ? kVisitCost : kVisitCost + 2;
+}
+constexpr int kMaxStep = kVisitCost + 2 + kSegCost;  // most between two visits that follow each other
 
-struct Phase {
-  int seg, G;      // G: the remote view of this G (>= 2), 0: the base view
-  int k0, n;       // first key, tiles
-  uint32_t start_lo, start_hi;  // cost before the phase
-  int cost, kend;  // of a tile; end of the segment's keys
-  uint32_t m, l;   // division by G
-  int pad[2];
-};
 struct Segment {
-  int m0, rows, g_seqs, kend;  // first member, rows, sequences, end of its keys
-  int w_first, n_w;            // workgroups that hold some of its tiles
-  int row0;                    // state rows before it
-  int seq;                     // whose table row names its pages
+  int m0, rows, kend, seq;        // first member, rows, end of its keys, whose table row names its pages
+  int k0, n_views, n_rem, loc0;   // first key; remote tiles and views of each; first tile with local keys
+  int visits, view0, len, pad;    // view0: its views' place; len: its rows' length for G, 0: each its own
+  uint32_t start_lo, start_hi;    // cost before it
+  int w_first, n_w;               // workgroups that hold some of its visits
+  int row0, pad2[3];              // state rows before it
 };
+struct View {
+  int G;
+  uint32_t m, l;  // division by G
+  int pad;
+};
+// A query row per kv head's query head: a sequence of a decode step, a token of a chunk
 struct Member {
-  int seq, len;
+  int seq;       // row of q and o
+  int len;       // its position + 1
   int pre, suf;  // its segments, -1: none
 };
+// States that a (workgroup, segment) leaves
+__host__ __device__ inline int state_halves(int rows) { return rows <= kShSmall ? 2 : 1; }
 
 struct PlanView {
   int* header;
   int* wg_first;
   Member* members;
+  View* views;
   Segment* segs;
-  Phase* phases;
 };
-
-__host__ __device__ inline size_t plan_blocks(int B, int n_groups, int g) {
-  return (size_t)n_groups + (size_t)B / (kShRows / g) + 1;
+// members, views, segments of a plan
+struct PlanSizes {
+  size_t members, views, segs;
+};
+__host__ __device__ inline PlanSizes decode_sizes(int B, int n_groups, int g) {
+  PlanSizes s;
+  s.members = (size_t)B;
+  s.views = 2 * (size_t)B;
+  s.segs = (size_t)n_groups + (size_t)B / (kShRows / g) + 1 + B;
+  return s;
 }
-__host__ __device__ inline PlanView plan_view(void* p, int B, int n_groups, int g) {
+__host__ __device__ inline PlanSizes chunk_sizes(int B, int T, int g) {
+  PlanSizes s;
+  s.members = (size_t)T;
+  s.segs = (size_t)B + (size_t)T / (kShRows / g) + 1;
+  s.views = s.segs;
+  return s;
+}
+constexpr size_t kPlanHead = 128 + 4 * kShMaxWg;
+__host__ __device__ inline PlanView plan_view(void* p, const PlanSizes& z) {
   PlanView v;
   char* c = (char*)p;
   v.header = (int*)c;
   v.wg_first = (int*)(c + 128);
-  v.members = (Member*)(c + 128 + 4 * kShMaxWg);
-  v.segs = (Segment*)(v.members + B);
-  v.phases = (Phase*)(v.segs + plan_blocks(B, n_groups, g) + B);
+  v.members = (Member*)(c + kPlanHead);
+  v.views = (View*)(v.members + z.members);
+  v.segs = (Segment*)(v.views + z.views);
   return v;
 }
-enum { kHdPhases = 0, kHdWg, kHdTotLo, kHdTotHi, kHdRows, kHdB, kHdG, kHdPage, kHdMaxPages,
-       kHdHkv, kHdGroups, kHdBifocal, kHdWPre, kHdW0 };
-
-size_t shared_plan_bytes(int B, int n_groups, int g) {
-  const size_t blocks = plan_blocks(B, n_groups, g);
-  return 128 + 4 * kShMaxWg + (size_t)B * sizeof(Member) + (blocks + B) * sizeof(Segment) +
-         (blocks + 3 * (size_t)B) * sizeof(Phase);
+static size_t plan_bytes(const PlanSizes& z) {
+  return kPlanHead + z.members * sizeof(Member) + z.views * sizeof(View) + z.segs * sizeof(Segment);
 }
-// State rows of one kv head: every segment's once, and a segment's again where a
+size_t shared_plan_bytes(int B, int n_groups, int g) { return plan_bytes(decode_sizes(B, n_groups, g)); }
+
+enum { kHdSegs = 0, kHdWg, kHdTotLo, kHdTotHi, kHdRows, kHdB, kHdG, kHdPage, kHdMaxPages, kHdHkv,
+       kHdGroups, kHdBifocal, kHdWPre, kHdW0 };
+
+// State rows of one kv head: every segment's, for each of its halves, and again where a
 // workgroup's range ends inside it.
-static size_t state_rows(int B, int g, int n_wg) {
-  return 2 * (size_t)B * g + (size_t)(n_wg - 1) * std::min<size_t>(kShRows, (size_t)B * g);
+static size_t state_rows(size_t rows, int most, int n_wg) {
+  return 2 * rows + (size_t)(n_wg - 1) * std::min<size_t>(kShRows, 2 * (size_t)most);
 }
 static int head_workgroups(int n_cu, int Hkv) { return std::max(1, std::min(n_cu, kShMaxWg) / Hkv); }
 constexpr int kShStateFloats = kHeadDim + 4;  // O, (m, l), and 8 bytes that keep 16-byte alignment
 size_t decode_shared_workspace_bytes(int B, int Hq, int Hkv) {
-  return (size_t)Hkv * state_rows(B, Hq / Hkv, head_workgroups(kShMaxWg, Hkv)) * kShStateFloats *
-         sizeof(float);
+  const int g = Hq / Hkv;
+  return (size_t)Hkv * state_rows(2 * (size_t)B * g, B * g, head_workgroups(kShMaxWg, Hkv)) *
+         kShStateFloats * sizeof(float);
+}
+// Of a chunk call: plan, then states
+size_t chunk_scratch_bytes(int B, int T, int Hq, int Hkv) {
+  const int g = Hq / Hkv;
+  return (plan_bytes(chunk_sizes(B, T, g)) + 255) / 256 * 256 +
+         (size_t)Hkv * state_rows((size_t)T * g, kShRows, head_workgroups(kShMaxWg, Hkv)) *
+             kShStateFloats * sizeof(float);
 }
 
 // ------------------------------------------------------------------- plan
@@ -111,12 +144,14 @@ struct SharedPlanArgs {
   const int32_t* members;  // nullptr: 0 .. B - 1
   const int32_t* group_starts;
   const int32_t* shared;
+  const int32_t* cu;       // chunks: T packed rows
   void* plan;
-  int B, n_groups, g, Hkv, max_pages, page, n_wg, bifocal, w_pre, w0;
+  int B, n_groups, T, g, Hkv, max_pages, page, n_wg, bifocal, w_pre, w0;
 };
 
 constexpr int kPlThreads = 1024, kPlWaves = kPlThreads / 64;
 
+// Inclusive sums over the workgroup's threads, in thread order; everyone gets the total
 template <typename T>
 __device__ inline T plan_scan(T v, T* s, T* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -151,100 +186,156 @@ __device__ inline int wave_max(int v) {
   return v;
 }
 
-// A row's views: G, and its first key in the base view (0 where all are)
 __device__ inline int plan_group(const SharedPlanArgs& a, int len) {
   return a.bifocal ? group_size(len, a.w_pre) : 1;
 }
-__device__ inline int first_local(int G, int len, int w0) {
-  return G > 1 ? max(0, len - 1 - w0) : 0;
+// The first key that a query at position q takes in the base view (0 where it takes all so)
+__device__ inline int first_local(int G, int q, int w0) { return G > 1 ? max(0, q - w0) : 0; }
+
+__device__ inline View view_of(int G) {
+  const FastDiv f = make_fastdiv((uint32_t)G);
+  return View{G, f.m, f.l, 0};
 }
 
-__device__ inline void put_phase(Phase* p, int seg, int G, int k0, int n, int rows, int kend) {
-  const FastDiv f = make_fastdiv((uint32_t)max(G, 1));
-  Phase x;
-  x.seg = seg;
-  x.G = G;
-  x.k0 = k0;
-  x.n = n;
-  x.start_lo = x.start_hi = 0;
-  x.cost = tile_cost(rows);
-  x.kend = kend;
-  x.m = f.m;
-  x.l = f.l;
-  x.pad[0] = x.pad[1] = 0;
-  *p = x;
+// Visits of keys [k0, kend) for rows whose first local keys lie between `low` and, among
+// those of some G >= 2, `far`, in n_views remote views
+__device__ inline void set_visits(Segment& s, int low, int far, int n_views) {
+  const int tiles = (s.kend - s.k0 + kShTile - 1) / kShTile;
+  s.n_views = max(n_views, 1);
+  s.n_rem = n_views > 0 && far > s.k0 ? min(tiles, (far - s.k0 + kShTile - 1) / kShTile) : 0;
+  s.loc0 = min(tiles, max(low - s.k0, 0) / kShTile);
+  s.visits = s.n_rem * s.n_views + tiles - s.loc0;
 }
 
-// The phases of a prefix block, by one wave (lane -> every 64th of its sequences):
-// counts them, or writes them where `out` is given.
-__device__ inline int block_phases(const SharedPlanArgs& a, const int* s_len, int m0, int n, int P,
-                                   int seg, Phase* out) {
-  const int lane = threadIdx.x & 63;
-  const int tiles = (P + kShTile - 1) / kShTile;
-  int count = 0, low = INT_MAX, G = 1;
-  for (;;) {
-    int next = INT_MAX, far = 0;  // the smallest G above the last, its furthest first local key
-    for (int i = lane; i < n; i += 64) {
-      const int len = s_len[m0 + i];
-      if (len <= 0) continue;
-      const int Gi = plan_group(a, len), lim = first_local(Gi, len, a.w0);
-      if (G == 1) low = min(low, lim);
-      if (Gi > G && Gi < next) {
-        next = Gi;
-        far = lim;
-      } else if (Gi == next) {
-        far = max(far, lim);
-      }
-    }
-    const int nx = wave_min(next);
-    far = wave_max(next == nx ? far : 0);
-    if (G == 1) low = wave_min(low);
-    if (nx == INT_MAX) break;
-    G = nx;
-    const int t = min(tiles, (far + kShTile - 1) / kShTile);
-    if (t > 0) {
-      if (out != nullptr && lane == 0) put_phase(out + count, seg, G, 0, t, n * a.g, P);
-      ++count;
-    }
+// Equal ranges of the list for n_wg workgroups: the first r of them one longer
+struct Ranges {
+  unsigned long long q, r;
+  int n_wg;
+  __device__ inline unsigned long long begin(int w) const { return q * w + min((unsigned long long)w, r); }
+  __device__ inline int owner(unsigned long long x) const {
+    const unsigned long long head = r * (q + 1);
+    if (((q + 1) * n_wg) >> 32 == 0)
+      return (int)(x < head ? (uint32_t)x / (uint32_t)(q + 1)
+                            : (uint32_t)r + (uint32_t)(x - head) / (uint32_t)q);
+    return (int)(x < head ? x / (q + 1) : r + (x - head) / q);
   }
-  const int t0 = low / kShTile;
-  if (t0 < tiles) {
-    if (out != nullptr && lane == 0)
-      put_phase(out + count, seg, 0, t0 * kShTile, tiles - t0, n * a.g, P);
-    ++count;
+};
+__device__ inline Ranges ranges_of(unsigned long long total, int n_wg) {
+  Ranges r;
+  r.n_wg = n_wg;
+  if (total >> 32 == 0) {
+    r.q = (uint32_t)total / (uint32_t)n_wg;
+  } else {
+    r.q = total / (unsigned)n_wg;
   }
-  return count;
+  r.r = total - r.q * n_wg;
+  return r;
 }
 
-// One workgroup.  LDS: the members' lengths and groups' bounds.
+// The end of both plans: costs before each segment, the workgroups' ranges, and the places of
+// the states.  s_visits, s_rows: visits and rows of n_segs segments; a thread takes a run of them.
+__device__ inline void plan_ranges(const SharedPlanArgs& a, const PlanView& v, int n_segs,
+                                   const int* s_visits, const short* s_rows,
+                                   unsigned long long* s_scan) {
+  const int tid = threadIdx.x;
+  const int per = (n_segs + kPlThreads - 1) / kPlThreads;
+  const int i0 = min(tid * per, n_segs), i1 = min(i0 + per, n_segs);
+  auto cost = [&](int i) {
+    const int n = s_visits[i];
+    return n > 0 ? kSegCost + (unsigned long long)n * visit_cost(s_rows[i]) : 0ull;
+  };
+  unsigned long long mine = 0, total;
+  for (int i = i0; i < i1; ++i) mine += cost(i);
+  unsigned long long st = plan_scan(mine, s_scan, &total) - mine;
+  // ranges that hold a visit wherever they lie inside a segment
+  const int n_wg = total == 0 ? 0 : (int)max(1ull, min((unsigned long long)a.n_wg, total / kMaxStep));
+  Ranges rg = {};
+  if (n_wg > 0) rg = ranges_of(total, n_wg);
+  unsigned long long rows = 0;
+  const unsigned long long st0 = st;
+  for (int i = i0; i < i1; ++i) {
+    const unsigned long long c = cost(i);
+    if (c == 0) continue;
+    const int w0 = rg.owner(st + kSegCost), w1 = rg.owner(st + c - visit_cost(s_rows[i]));
+    rows += (unsigned long long)(w1 - w0 + 1) * s_rows[i] * state_halves(s_rows[i]);
+    int w = rg.owner(st);  // workgroups whose ranges begin inside this segment
+    if (rg.begin(w) < st) ++w;
+    for (; w < n_wg && rg.begin(w) < st + c; ++w) v.wg_first[w] = i;
+    st += c;
+  }
+  unsigned long long all_rows;
+  unsigned long long row = plan_scan(rows, s_scan, &all_rows) - rows;
+  st = st0;
+  for (int i = i0; i < i1; ++i) {
+    const unsigned long long c = cost(i);
+    Segment& s = v.segs[i];
+    s.start_lo = (uint32_t)st;
+    s.start_hi = (uint32_t)(st >> 32);
+    if (c == 0) {
+      s.w_first = s.n_w = 0;
+      s.row0 = 0;
+      continue;
+    }
+    const int w0 = rg.owner(st + kSegCost), w1 = rg.owner(st + c - visit_cost(s_rows[i]));
+    s.w_first = w0;
+    s.n_w = w1 - w0 + 1;
+    s.row0 = (int)row;
+    row += (unsigned long long)(w1 - w0 + 1) * s_rows[i] * state_halves(s_rows[i]);
+    st += c;
+  }
+  if (tid == 0) {
+    v.header[kHdSegs] = n_segs;
+    v.header[kHdWg] = n_wg;
+    v.header[kHdTotLo] = (int)(uint32_t)total;
+    v.header[kHdTotHi] = (int)(uint32_t)(total >> 32);
+    v.header[kHdRows] = (int)all_rows;
+    v.header[kHdB] = a.B;
+    v.header[kHdG] = a.g;
+    v.header[kHdPage] = a.page;
+    v.header[kHdMaxPages] = a.max_pages;
+    v.header[kHdHkv] = a.Hkv;
+    v.header[kHdGroups] = a.n_groups;
+    v.header[kHdBifocal] = a.bifocal;
+    v.header[kHdWPre] = a.w_pre;
+    v.header[kHdW0] = a.w0;
+  }
+}
+
+// A decode step's plan, by one workgroup.
 __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs a) {
   extern __shared__ int s_mem[];
   __shared__ unsigned long long s_scan[kPlWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const PlanView v = plan_view(a.plan, a.B, a.n_groups, a.g);
+  const PlanSizes z = decode_sizes(a.B, a.n_groups, a.g);
+  const PlanView v = plan_view(a.plan, z);
   int* const s_len = s_mem;                    // [B] by member, -1: no such sequence
-  int* const s_start = s_len + a.B;            // [n_groups + 1]
+  int* const s_seq = s_len + a.B;              // [B]
+  int* const s_start = s_seq + a.B;            // [n_groups + 1]
   int* const s_pre = s_start + a.n_groups + 1; // [n_groups]: shared keys
   int* const s_blk = s_pre + a.n_groups;       // [n_groups + 1]: prefix blocks before the group
-  int* const s_cnt = s_blk + a.n_groups + 1;   // [blocks + 1]: phases of a prefix block
-  const int cap = (int)min((long long)a.max_pages * a.page, (long long)INT_MAX);
+  int* const s_visits = s_blk + a.n_groups + 1;
+  short* const s_rows = (short*)(s_visits + z.segs);
+  const int cap = a.max_pages * a.page;
   const int per_block = kShRows / a.g;
 
-  for (int i = tid; i <= a.n_groups; i += kPlThreads)
-    s_blk[i] = min(max(a.group_starts[i], 0), a.B);
+  bool bad = false;
+  for (int i = tid; i <= a.n_groups; i += kPlThreads) {
+    const int x = min(max(a.group_starts[i], 0), a.B);
+    s_start[i] = x;
+    if (i > 0) bad |= min(max(a.group_starts[i - 1], 0), a.B) > x;
+  }
+  for (int i = tid; i < a.n_groups; i += kPlThreads) s_pre[i] = INT_MAX;
   for (int i = tid; i < a.B; i += kPlThreads) {
     const int seq = a.members != nullptr ? a.members[i] : i;
     const bool ok = (unsigned)seq < (unsigned)a.B;
+    s_seq[i] = ok ? seq : -1;
     s_len[i] = ok ? min(max(a.kv_lens[seq], 0), cap) : -1;
   }
-  __syncthreads();
-  for (int i = tid; i <= a.n_groups; i += kPlThreads) {  // a start below an earlier one counts as that
-    int top = 0;
-    for (int j = 0; j <= i; ++j) top = max(top, s_blk[j]);
-    s_start[i] = top;
-    if (i < a.n_groups) s_pre[i] = INT_MAX;
+  if (__syncthreads_or(bad)) {  // a start below an earlier one counts as that
+    if (tid == 0)
+      for (int i = 1; i <= a.n_groups; ++i) s_start[i] = max(s_start[i], s_start[i - 1]);
+    __syncthreads();
   }
-  __syncthreads();
   // a member's group: the first whose end lies behind it
   auto group_of = [&](int m) {
     int lo = 0, hi = a.n_groups;
@@ -259,191 +350,194 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
     if (gi >= 0 && s_len[i] > 0) atomicMin(&s_pre[gi], s_len[i]);
   }
   __syncthreads();
-  for (int i = tid; i < a.n_groups; i += kPlThreads) {
-    const int n = s_start[i + 1] - s_start[i];
-    s_pre[i] = n > 1 && s_pre[i] != INT_MAX ? min(max(a.shared[i], 0), s_pre[i]) / a.page * a.page : 0;
-    s_blk[i] = n > 1 && s_pre[i] > 0 ? (n + per_block - 1) / per_block : 0;
-  }
-  __syncthreads();
-  // prefix blocks before each group
+  // the groups' shared keys and their blocks of up to 256 rows
   int n_blocks = 0;
   for (int c0 = 0; c0 < a.n_groups; c0 += kPlThreads) {
     const int i = c0 + tid;
-    const unsigned long long x = i < a.n_groups ? (unsigned long long)s_blk[i] : 0ull;
-    unsigned long long tot;
+    unsigned long long x = 0, tot;
+    if (i < a.n_groups) {
+      const int n = s_start[i + 1] - s_start[i], low = s_pre[i];
+      const int P = n > 1 && low != INT_MAX ? min(max(a.shared[i], 0), low) / a.page * a.page : 0;
+      s_pre[i] = P;
+      x = P > 0 ? (n + per_block - 1) / per_block : 0;
+    }
     const unsigned long long incl = plan_scan(x, s_scan, &tot);
     if (i < a.n_groups) s_blk[i] = n_blocks + (int)(incl - x);
     n_blocks += (int)tot;
   }
   if (tid == 0) s_blk[a.n_groups] = n_blocks;
   __syncthreads();
-  auto block_of = [&](int blk, int* m0, int* n, int* P) {  // the last group that begins at or before it
-    int lo = 0, hi = a.n_groups - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s_blk[mid] <= blk) lo = mid; else hi = mid - 1;
+  // prefix blocks, a wave each, lane -> every 64th of its sequences
+  for (int blk = wave; blk < n_blocks; blk += kPlWaves) {
+    int gi = 0, hi = a.n_groups - 1;  // the last group that begins at or before it
+    while (gi < hi) {
+      const int mid = (gi + hi + 1) >> 1;
+      if (s_blk[mid] <= blk) gi = mid; else hi = mid - 1;
     }
-    *m0 = s_start[lo] + (blk - s_blk[lo]) * per_block;
-    *n = min(per_block, s_start[lo + 1] - *m0);
-    *P = s_pre[lo];
-  };
-  for (int blk = wave; blk < n_blocks; blk += kPlWaves) {
-    int m0, n, P;
-    block_of(blk, &m0, &n, &P);
-    const int c = block_phases(a, s_len, m0, n, P, blk, nullptr);
-    if (lane == 0) s_cnt[blk] = c;
-  }
-  __syncthreads();
-  int at = 0;  // phases of the blocks
-  for (int c0 = 0; c0 < n_blocks; c0 += kPlThreads) {
-    const int i = c0 + tid;
-    const unsigned long long x = i < n_blocks ? (unsigned long long)s_cnt[i] : 0ull;
-    unsigned long long tot;
-    const unsigned long long incl = plan_scan(x, s_scan, &tot);
-    if (i < n_blocks) s_cnt[i] = at + (int)(incl - x);
-    at += (int)tot;
-  }
-  __syncthreads();
-  for (int blk = wave; blk < n_blocks; blk += kPlWaves) {
-    int m0, n, P;
-    block_of(blk, &m0, &n, &P);
-    block_phases(a, s_len, m0, n, P, blk, v.phases + s_cnt[blk]);
-    int from = INT_MAX;  // any sequence of the block that has keys
-    for (int i = lane; i < n; i += 64)
-      if (s_len[m0 + i] > 0) from = min(from, m0 + i);
+    const int m0 = s_start[gi] + (blk - s_blk[gi]) * per_block;
+    const int n = min(per_block, s_start[gi + 1] - m0);
+    int low = INT_MAX, far = 0, from = INT_MAX, G = 1, n_views = 0;
+    for (;;) {  // the values of G above 1, ascending
+      int next = INT_MAX;
+      for (int i = lane; i < n; i += 64) {
+        const int len = s_len[m0 + i];
+        if (len <= 0) continue;
+        const int Gi = plan_group(a, len), lim = first_local(Gi, len - 1, a.w0);
+        if (Gi > G) next = min(next, Gi);
+        if (G == 1) {
+          low = min(low, lim);
+          far = max(far, lim);
+          from = min(from, i);
+        }
+      }
+      G = wave_min(next);
+      if (G == INT_MAX) break;
+      if (lane == 0) v.views[m0 + n_views] = view_of(G);
+      ++n_views;
+    }
+    low = wave_min(low);
+    far = wave_max(far);
     from = wave_min(from);
     if (lane == 0) {
-      const int seq = from == INT_MAX ? 0 : a.members != nullptr ? a.members[from] : from;
-      v.segs[blk] = Segment{m0, n * a.g, n, P, 0, 0, 0, seq};
+      Segment s = {};
+      s.m0 = m0;
+      s.rows = n * a.g;
+      s.kend = s_pre[gi];
+      s.seq = from == INT_MAX ? 0 : s_seq[m0 + from];
+      s.view0 = m0;
+      if (from != INT_MAX) set_visits(s, low, far, n_views);
+      v.segs[blk] = s;
+      s_visits[blk] = s.visits;
+      s_rows[blk] = (short)s.rows;
     }
   }
   // the members' own keys
-  for (int c0 = 0; c0 < a.B; c0 += kPlThreads) {
-    const int i = c0 + tid;
-    int gi = -1, len = -1, P = 0, near = 0, G = 1, n_rem = 0, t0 = 0, tiles = 0;
-    unsigned long long cnt = 0;
-    if (i < a.B) {
-      gi = group_of(i);
-      len = s_len[i];
-      if (gi >= 0 && len > 0) {
-        P = s_pre[gi];
-        G = plan_group(a, len);
-        near = first_local(G, len, a.w0);
-        tiles = (len - P + kShTile - 1) / kShTile;
-        n_rem = near > P ? (near - P + kShTile - 1) / kShTile : 0;
-        t0 = max(near - P, 0) / kShTile;
-        cnt = (n_rem > 0) + (t0 < tiles);
-      }
+  for (int i = tid; i < a.B; i += kPlThreads) {
+    const int gi = group_of(i), len = s_len[i], seg = n_blocks + i;
+    Segment s = {};
+    Member m = {gi >= 0 && len >= 0 ? s_seq[i] : -1, max(len, 0), -1, -1};
+    if (gi >= 0 && len > 0) {
+      const int P = s_pre[gi], G = plan_group(a, len), lim = first_local(G, len - 1, a.w0);
+      s.m0 = i;
+      s.rows = a.g;
+      s.k0 = P;
+      s.kend = len;
+      s.seq = m.seq;
+      s.view0 = a.B + i;
+      set_visits(s, lim, lim, G > 1 ? 1 : 0);
+      if (G > 1) v.views[a.B + i] = view_of(G);
+      if (P > 0) m.pre = s_blk[gi] + (i - s_start[gi]) / per_block;
+      if (s.visits > 0) m.suf = seg;
     }
-    unsigned long long tot;
-    const unsigned long long incl = plan_scan(cnt, s_scan, &tot);
-    if (i < a.B) {
-      const int seg = n_blocks + i;
-      Phase* p = v.phases + at + (int)(incl - cnt);
-      if (cnt > 0) {
-        if (n_rem > 0) put_phase(p++, seg, G, P, n_rem, a.g, len);
-        if (t0 < tiles) put_phase(p, seg, 0, P + t0 * kShTile, tiles - t0, a.g, len);
-      }
-      Member m;
-      m.seq = gi >= 0 && len >= 0 ? (a.members != nullptr ? a.members[i] : i) : -1;
-      m.len = max(len, 0);
-      v.segs[seg] = Segment{i, cnt > 0 ? a.g : 0, 1, len, 0, 0, 0, m.seq};
-      m.pre = P > 0 ? s_blk[gi] + (i - s_start[gi]) / per_block : -1;
-      m.suf = cnt > 0 ? seg : -1;
-      v.members[i] = m;
-    }
-    at += (int)tot;
-  }
-  const int n_phases = at;
-  __syncthreads();
-  // costs before each phase
-  unsigned long long total = 0;
-  for (int c0 = 0; c0 < n_phases; c0 += kPlThreads) {
-    const int i = c0 + tid;
-    unsigned long long x = 0;
-    if (i < n_phases) x = kPhaseCost + (unsigned long long)v.phases[i].n * v.phases[i].cost;
-    unsigned long long tot;
-    const unsigned long long incl = plan_scan(x, s_scan, &tot);
-    if (i < n_phases) {
-      const unsigned long long st = total + incl - x;
-      v.phases[i].start_lo = (uint32_t)st;
-      v.phases[i].start_hi = (uint32_t)(st >> 32);
-    }
-    total += tot;
-  }
-  // ranges that hold a tile wherever they lie inside a segment
-  const unsigned long long most = total / kMaxStep;
-  const int n_wg = total == 0 ? 0 : (int)max(1ull, min((unsigned long long)a.n_wg, most));
-  __syncthreads();
-  auto owner = [&](unsigned long long x) {  // the workgroup whose range holds x
-    int w = (int)min((unsigned long long)(n_wg - 1), (unsigned long long)((double)x * n_wg / (double)total));
-    while (w > 0 && total * w / n_wg > x) --w;
-    while (w + 1 < n_wg && total * (w + 1) / n_wg <= x) ++w;
-    return w;
-  };
-  for (int i = tid; i < n_phases; i += kPlThreads) {
-    const Phase p = v.phases[i];
-    const unsigned long long st = p.start_lo | (unsigned long long)p.start_hi << 32;
-    const unsigned long long end = st + kPhaseCost + (unsigned long long)p.n * p.cost;
-    // the workgroups whose ranges begin inside this phase
-    int w = owner(st);
-    if (total * w / n_wg < st) ++w;
-    for (; w < n_wg && total * w / n_wg < end; ++w) v.wg_first[w] = i;
-    if (i == 0 || v.phases[i - 1].seg != p.seg) v.segs[p.seg].w_first = owner(st + kPhaseCost);
-    if (i == n_phases - 1 || v.phases[i + 1].seg != p.seg) v.segs[p.seg].n_w = owner(end - p.cost);
+    v.members[i] = m;
+    v.segs[seg] = s;
+    s_visits[seg] = s.visits;
+    s_rows[seg] = (short)s.rows;
   }
   __syncthreads();
-  int rows = 0;
-  for (int c0 = 0; c0 < n_blocks + a.B; c0 += kPlThreads) {
-    const int i = c0 + tid;
-    unsigned long long x = 0;
-    int n_w = 0;
-    if (i < n_blocks + a.B && v.segs[i].rows > 0) {
-      n_w = v.segs[i].n_w - v.segs[i].w_first + 1;
-      x = (unsigned long long)n_w * v.segs[i].rows;
-    }
-    unsigned long long tot;
-    const unsigned long long incl = plan_scan(x, s_scan, &tot);
-    if (i < n_blocks + a.B) {
-      v.segs[i].n_w = n_w;
-      v.segs[i].row0 = rows + (int)(incl - x);
-    }
-    rows += (int)tot;
-  }
-  if (tid == 0) {
-    v.header[kHdPhases] = n_phases;
-    v.header[kHdWg] = n_wg;
-    v.header[kHdTotLo] = (int)(uint32_t)total;
-    v.header[kHdTotHi] = (int)(uint32_t)(total >> 32);
-    v.header[kHdRows] = rows;
-    v.header[kHdB] = a.B;
-    v.header[kHdG] = a.g;
-    v.header[kHdPage] = a.page;
-    v.header[kHdMaxPages] = a.max_pages;
-    v.header[kHdHkv] = a.Hkv;
-    v.header[kHdGroups] = a.n_groups;
-    v.header[kHdBifocal] = a.bifocal;
-    v.header[kHdWPre] = a.w_pre;
-    v.header[kHdW0] = a.w0;
-  }
+  plan_ranges(a, v, n_blocks + a.B, s_visits, s_rows, s_scan);
 }
 
-// ------------------------------------------------------------------ decode
+// The plan of packed chunks: sequence b's rows are cu[b] .. cu[b + 1] - 1 of the packed ones,
+// the last kv_lens[b] - n .. kv_lens[b] - 1 of its positions (rows that would lie before
+// position 0 are left out).  Segments: blocks of up to 256 / g tokens, the last of a sequence
+// shorter.
+__global__ __launch_bounds__(kPlThreads) void chunk_plan_kernel(SharedPlanArgs a) {
+  extern __shared__ int s_mem[];
+  __shared__ unsigned long long s_scan[kPlWaves];
+  const int tid = threadIdx.x;
+  const PlanSizes z = chunk_sizes(a.B, a.T, a.g);
+  const PlanView v = plan_view(a.plan, z);
+  int* const s_start = s_mem;               // [B + 1]
+  int* const s_len = s_start + a.B + 1;     // [B]
+  int* const s_blk = s_len + a.B;           // [B + 1]: blocks before the sequence
+  int* const s_visits = s_blk + a.B + 1;
+  short* const s_rows = (short*)(s_visits + z.segs);
+  const int cap = a.max_pages * a.page;
+  const int per_block = kShRows / a.g;
+  bool bad = false;
+  for (int i = tid; i <= a.B; i += kPlThreads) {
+    const int x = min(max(a.cu[i], 0), a.T);
+    s_start[i] = x;
+    if (i > 0) bad |= min(max(a.cu[i - 1], 0), a.T) > x;
+    if (i < a.B) s_len[i] = min(max(a.kv_lens[i], 0), cap);
+  }
+  if (__syncthreads_or(bad)) {  // a start below an earlier one counts as that
+    if (tid == 0)
+      for (int i = 1; i <= a.B; ++i) s_start[i] = max(s_start[i], s_start[i - 1]);
+    __syncthreads();
+  }
+  int n_segs = 0;
+  for (int c0 = 0; c0 < a.B; c0 += kPlThreads) {
+    const int i = c0 + tid;
+    unsigned long long x = 0, tot;
+    if (i < a.B) x = (unsigned long long)((s_start[i + 1] - s_start[i] + per_block - 1) / per_block);
+    const unsigned long long incl = plan_scan(x, s_scan, &tot);
+    if (i < a.B) s_blk[i] = n_segs + (int)(incl - x);
+    n_segs += (int)tot;
+  }
+  if (tid == 0) s_blk[a.B] = n_segs;
+  __syncthreads();
+  for (int seg = tid; seg < n_segs; seg += kPlThreads) {
+    int b = 0, hi = a.B - 1;  // the last sequence that begins at or before it
+    while (b < hi) {
+      const int mid = (b + hi + 1) >> 1;
+      if (s_blk[mid] <= seg) b = mid; else hi = mid - 1;
+    }
+    const int n = s_start[b + 1] - s_start[b], t0 = (seg - s_blk[b]) * per_block;
+    const int cnt = min(per_block, n - t0), len = s_len[b];
+    const int p0 = len - n + t0, p1 = p0 + cnt - 1;  // positions of its first and last token
+    const int G = plan_group(a, len);
+    Segment s = {};
+    s.m0 = s_start[b] + t0;
+    s.rows = cnt * a.g;
+    s.kend = max(p1 + 1, 0);
+    s.seq = b;
+    s.view0 = seg;
+    s.len = max(len, 1);
+    set_visits(s, first_local(G, p0, a.w0), first_local(G, p1, a.w0), G > 1 ? 1 : 0);
+    if (G > 1) v.views[seg] = view_of(G);
+    v.segs[seg] = s;
+    s_visits[seg] = s.visits;
+    s_rows[seg] = (short)s.rows;
+  }
+  for (int t = tid; t < a.T; t += kPlThreads) {
+    int b = 0, hi = a.B;  // the first sequence whose end lies behind the token
+    while (b < hi) {
+      const int mid = (b + hi) >> 1;
+      if (s_start[mid + 1] > t) hi = mid; else b = mid + 1;
+    }
+    Member m = {-1, 0, -1, -1};
+    if (b < a.B && s_start[b] <= t) {
+      const int i = t - s_start[b], pos = s_len[b] - (s_start[b + 1] - s_start[b]) + i;
+      if (pos >= 0) m = Member{t, pos + 1, s_blk[b] + i / per_block, -1};
+    }
+    v.members[t] = m;
+  }
+  __syncthreads();
+  plan_ranges(a, v, n_segs, s_visits, s_rows, s_scan);
+}
+
+// --------------------------------------------------------------- attention
 struct SharedArgs {
   const uint16_t* q;
   const uint16_t* k;
   const uint16_t* v;
   const int32_t* table;
   uint16_t* o;
+  float* lse;  // [Hq][T] of a chunk, or nullptr
   const float2* rope;
   const uint32_t* rope16;
   void* plan;
   float* states;
-  int B, n_groups, Hq, Hkv, g, max_pages, n_pages, page, page_shift, n_wg;
-  int bifocal, w_pre, w0;
+  int B, n_groups, T, Hq, Hkv, g, max_pages, n_pages, page, page_shift, n_wg;
+  int chunk, bifocal, w_pre, w0;
   float q_scale;
 };
 
+__device__ inline PlanView plan_of(const SharedArgs& a) {
+  return plan_view(a.plan, a.chunk ? chunk_sizes(a.B, a.T, a.g) : decode_sizes(a.B, a.n_groups, a.g));
+}
 // Whether the plan is one for this call: else nothing is computed.
 __device__ inline bool plan_fits(const SharedArgs& a, const int* h) {
   return h[kHdB] == a.B && h[kHdG] == a.g && h[kHdPage] == a.page && h[kHdMaxPages] == a.max_pages &&
@@ -451,100 +545,115 @@ __device__ inline bool plan_fits(const SharedArgs& a, const int* h) {
          h[kHdWPre] == a.w_pre && h[kHdW0] == a.w0 && h[kHdWg] <= a.n_wg;
 }
 
-// LDS layouts: K key r at r * 256, its 16-byte chunk c in slot c ^ sh_kswz(r); V as
-// the prefill kernel's tiles; cos/sin row of key r at r * 256.
+// LDS layouts: K key r at r * 256, its 16-byte chunk c in slot c ^ sh_kswz(r) (16 keys read
+// at one chunk, and a key's halves, hit distinct banks); V key r in slot c ^ sh_vswz(r) (so do
+// the transposing reads of 8 keys x 32 B and of 4 keys x 64 B); cos/sin row of key r at r * 256.
 __device__ inline int sh_kswz(int r) { return ((r & 15) >> 1) | ((r & 1) << 3); }
+__device__ inline int sh_vswz(int r) { return 4 * (r & 3) | 2 * ((r >> 2) & 1); }
 __device__ inline int sh_koff(int r, int c) { return r * 256 + 16 * (c ^ sh_kswz(r)); }
-__device__ inline int sh_voff(int r, int c) { return r * 256 + 16 * (c ^ (4 * (r & 3))); }
+__device__ inline int sh_voff(int r, int c) { return r * 256 + 16 * (c ^ sh_vswz(r)); }
 
-// A tile of the list
+// A visit of the list
 struct Tile {
   int row0, row1;  // pool rows of its first and its 17th key
   int k0;
-  int flags;  // bits 0..4: last valid key of the tile; kTf*; the phase from bit 9 on
+  int flags;       // bits 0..4: last valid key of the tile; kTfLast; the held segment from bit 9 on
   int f0, km;      // remote view: f(k0) and k0 - G f(k0)
-  uint32_t m, l;
+  uint32_t m, lG;  // its view: l and, from bit 6 on, G (0: the base view)
 };
-constexpr int kTfRemote = 32, kTfView = 64, kTfSeg = 128, kTfLast = 256, kTfPhase = 9;
-
-// The slice of fp32 head row `row` that a lane feeds as B operand: as the prefill's.
-__device__ inline void sh_load_q(const uint16_t* qrow, int half, const float2* table, int pos,
-                                 float scale, bf16x8* out) {
-#pragma unroll
-  for (int s = 0; s < 4; ++s) {
-    const int d = 16 * s + 8 * half;
-    float lo[8], hi[8], ylo[8], yhi[8];
-    unpack8(load16(qrow + d), lo);
-    unpack8(load16(qrow + d + kHalf), hi);
-    const float4* c4 = (const float4*)(table + (size_t)pos * kHalf + d);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const float4 w = c4[t];
-      const int j = 2 * t;
-      ylo[j] = (lo[j] * w.x - hi[j] * w.y) * scale;
-      yhi[j] = (hi[j] * w.x + lo[j] * w.y) * scale;
-      ylo[j + 1] = (lo[j + 1] * w.z - hi[j + 1] * w.w) * scale;
-      yhi[j + 1] = (hi[j + 1] * w.z + lo[j + 1] * w.w) * scale;
-    }
-    out[s] = pack8(ylo);
-    out[s + 4] = pack8(yhi);
-  }
-}
+constexpr int kTfLast = 32, kTfSeg = 9;
 
 typedef __bf16 sh_bf16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned sh_u32x2 __attribute__((ext_vector_type(2)));
 
-// Scores may exceed the row's reference by this (log2 units) before it moves: weights
+// One rotate-half slice pair of a query row: channels d .. d + 7 and d + 64 .. d + 71,
+// rotated to position pos and scaled, as matrix operands.
+__device__ inline void sh_rotate_q(const uint16_t* qrow, int d, const float2* table, int pos,
+                                   float scale, bf16x8& olo, bf16x8& ohi) {
+  float lo[8], hi[8], ylo[8], yhi[8];
+  unpack8(load16(qrow + d), lo);
+  unpack8(load16(qrow + d + kHalf), hi);
+  const float4* c4 = (const float4*)(table + (size_t)pos * kHalf + d);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const float4 w = c4[t];
+    const int j = 2 * t;
+    ylo[j] = (lo[j] * w.x - hi[j] * w.y) * scale;
+    yhi[j] = (hi[j] * w.x + lo[j] * w.y) * scale;
+    ylo[j + 1] = (lo[j + 1] * w.z - hi[j + 1] * w.w) * scale;
+    yhi[j + 1] = (hi[j + 1] * w.z + lo[j + 1] * w.w) * scale;
+  }
+  olo = pack8(ylo);
+  ohi = pack8(yhi);
+}
+
+__device__ inline f32x4 sh_mfma16k16(i16x4 a, bf16x4 b, f32x4 c) {
+  typedef short i16x4v __attribute__((ext_vector_type(4)));
+  return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, __builtin_bit_cast(i16x4v, b), c, 0, 0, 0);
+}
+__device__ inline float sh_max32(float x) {  // over lanes l and l ^ 32
+  const sh_u32x2 r =
+      __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float sh_max16_32(float x) {  // over lanes l, l ^ 16, l ^ 32, l ^ 48
+  const sh_u32x2 r =
+      __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return sh_max32(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+
+// Scores may exceed a row's reference by this (log2 units) before it moves: weights
 // stay below 2^16, far inside fp32 and bf16.
 constexpr float kShSlack = 16.f;
 
-__global__ __launch_bounds__(kShThreads, 2) void decode_shared_kernel(SharedArgs a) {
+__global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[kShBufs * kShBuf];
   __shared__ __attribute__((aligned(16))) Tile s_tiles[kShList];
+  __shared__ __attribute__((aligned(16))) Segment s_segs[kShSegs];
+  __shared__ int s_from[kShSegs], s_before[kShSegs];  // first visit here, visits of earlier ones
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int hl32 = lane >> 5;
   const int h = blockIdx.x % a.Hkv;
   const int w = blockIdx.x / a.Hkv;
-  const PlanView pv = plan_view(a.plan, a.B, a.n_groups, a.g);
+  const PlanView pv = plan_of(a);
   if (!plan_fits(a, pv.header) || w >= pv.header[kHdWg]) return;
-  const int n_phases = pv.header[kHdPhases], n_wg = pv.header[kHdWg];
-  const unsigned long long total =
-      (uint32_t)pv.header[kHdTotLo] | (unsigned long long)(uint32_t)pv.header[kHdTotHi] << 32;
-  const unsigned long long x0 = total * w / n_wg, x1 = total * (w + 1) / n_wg;
+  auto uni = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  const int n_segs = uni(pv.header[kHdSegs]), all_rows = uni(pv.header[kHdRows]);
+  unsigned long long x0, x1;
+  {
+    const unsigned long long total =
+        (uint32_t)pv.header[kHdTotLo] | (unsigned long long)(uint32_t)pv.header[kHdTotHi] << 32;
+    const Ranges rg = ranges_of(total, pv.header[kHdWg]);
+    auto uni64 = [&](unsigned long long x) {
+      return (uint32_t)uni((int)(uint32_t)x) | (unsigned long long)(uint32_t)uni((int)(x >> 32)) << 32;
+    };
+    x0 = uni64(rg.begin(w));
+    x1 = uni64(rg.begin(w + 1));
+  }
   const uint32_t smem_base = lds_addr(smem);
   const uint32_t kv_row_bytes = (uint32_t)a.Hkv * (kHeadDim * 2);
   const unsigned char* kbase = (const unsigned char*)(a.k + (size_t)h * kHeadDim);
   const unsigned char* vbase = (const unsigned char*)(a.v + (size_t)h * kHeadDim);
 
-  // tiles [ta, tb) of a phase that this workgroup holds
-  auto tiles_of = [&](const Phase& p, int* ta, int* tb) {
-    const unsigned long long st = (p.start_lo | (unsigned long long)p.start_hi << 32) + kPhaseCost;
-    auto below = [&](unsigned long long x) {
-      return x <= st ? 0 : (int)min((unsigned long long)p.n, (x - st + p.cost - 1) / p.cost);
-    };
-    *ta = below(x0);
-    *tb = below(x1);
-  };
-
   // ---- copies of a tile: keys 4 wave .. + 3 of K, V and their cos/sin rows
   const int cp_key = 4 * wave + (lane >> 4), cp_slot = lane & 15;
   const uint32_t cp_k = 16 * (cp_slot ^ sh_kswz(cp_key));
-  const uint32_t cp_v = 16 * (cp_slot ^ (4 * (cp_key & 3)));
-  auto uni = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  const uint32_t cp_v = 16 * (cp_slot ^ sh_vswz(cp_key));
   auto issue = [&](int j) __attribute__((always_inline)) {
-    const Tile& s = s_tiles[j];
+    const Tile& s = s_tiles[j & (kShList - 1)];
     const int flags = uni(s.flags), klim = flags & 31, k0 = uni(s.k0);
     const int row = min(4 * wave, klim) < 16 ? uni(s.row0) : uni(s.row1);
     const int key = min(cp_key, klim);
     const size_t off = (size_t)(uint32_t)row * kv_row_bytes;
     const uint32_t buf = smem_base + (uint32_t)(j % kShBufs) * kShBuf + 1024 * wave;
     const uint32_t ro = (uint32_t)(key & 15) * kv_row_bytes;
-    dma16_s_nt(kbase + off, ro + cp_k, buf);
-    dma16_s_nt(vbase + off, ro + cp_v, buf + kShImg);
+    dma16_s(kbase + off, ro + cp_k, buf);
+    dma16_s(vbase + off, ro + cp_v, buf + kShImg);
     int pos = k0 + key;
-    if (flags & kTfRemote) {
-      const FastDiv f = {(uint32_t)uni((int)s.m), (uint32_t)uni((int)s.l), 2};
+    const int lG = uni((int)s.lG);
+    if (lG != 0) {
+      const FastDiv f = {(uint32_t)uni((int)s.m), (uint32_t)lG & 63, 2};
       pos = uni(s.f0) + (int)fastdiv_ge2((uint32_t)(uni(s.km) + key), f);
     }
     dma16_s(a.rope16, (uint32_t)pos * 256 + 16 * cp_slot, buf + 2 * kShImg);
@@ -555,255 +664,420 @@ __global__ __launch_bounds__(kShThreads, 2) void decode_shared_kernel(SharedArgs
   const int rt_cs = 2 * kShImg + rt_key * 256 + 32 * rt_c + 16 * rt_h;
   auto rotate = [&](int j) __attribute__((always_inline)) {
     unsigned char* b = smem + (j % kShBufs) * kShBuf;
-    typedef unsigned u32x2v __attribute__((ext_vector_type(2)));
-    const u32x2v xl = *(const u32x2v*)(b + rt_lo), xh = *(const u32x2v*)(b + rt_hi);
+    const sh_u32x2 xl = *(const sh_u32x2*)(b + rt_lo), xh = *(const sh_u32x2*)(b + rt_hi);
     const u32x4 cs = *(const u32x4*)(b + rt_cs);
     uint32_t l0, h0, l1, h1;
     rot_word_dot2(xl[0], xh[0], cs[0], cs[1], l0, h0);
     rot_word_dot2(xl[1], xh[1], cs[2], cs[3], l1, h1);
-    *(u32x2v*)(b + rt_lo) = u32x2v{l0, l1};
-    *(u32x2v*)(b + rt_hi) = u32x2v{h0, h1};
+    *(sh_u32x2*)(b + rt_lo) = sh_u32x2{l0, l1};
+    *(sh_u32x2*)(b + rt_hi) = sh_u32x2{h0, h1};
   };
 
-  // ---- state of this lane's row
-  bf16x8 qop[8];
-  f32x16 acc_o[4];
-  f32x16 neg_m = f32x16{};
-  float m_ref = 0.f, l_run = 0.f;
-  int rows = 0, kend = 0;              // of the segment
-  int lim = 0, row_G = 1, qpos = 0;    // of the row: first key in its base view, G, position
-  const uint16_t* qrow = a.q;
-  int ph_G = 0;                        // the phase's view
+  int n = 0;  // visits of the held segments
+  // Addresses of visits j0 .. j0 + 127, by as many threads
+  auto fill = [&](int j0) __attribute__((always_inline)) {
+    const int j = j0 + tid;
+    if (tid >= kShList / 2 || j >= n) return;
+    int i = 0;  // the held segment: the last that begins at or before the visit
 #pragma unroll
-  for (int i = 0; i < 4; ++i) acc_o[i] = f32x16{};
-#pragma unroll
-  for (int s = 0; s < 8; ++s) qop[s] = bf16x8{};
-  const int row = 32 * wave + (lane & 31);
-  const int kr_lane = lane & 31;
-  const int vk_lane = 4 * hl32 + ((lane & 15) >> 2);
-  const int vc_lane = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-
-  int ph = pv.wg_first[w];  // next phase of the list, and its first tile that is not listed yet
-  int ph_t = -1;
-  int seg_now = -1;         // the segment of the last listed tile
-  while (ph < n_phases) {
-    // ---- list the next tiles of the range
-    int n = 0;
-    while (ph < n_phases && n < kShList) {
-      const Phase p = pv.phases[ph];
-      int ta, tb;
-      tiles_of(p, &ta, &tb);
-      if ((p.start_lo | (unsigned long long)p.start_hi << 32) >= x1) {
-        ph = n_phases;
-        break;
-      }
-      const bool first = ph_t < 0;  // of the phase, here
-      const int t0 = first ? ta : ph_t;
-      const int cnt = min(tb - t0, kShList - n);
-      if (cnt > 0) {
-        const int32_t* bt = a.table + (size_t)pv.segs[p.seg].seq * a.max_pages;
-        const FastDiv f = {p.m, p.l, (uint32_t)p.G};
-        for (int i = tid; i < cnt; i += kShThreads) {
-          Tile s;
-          s.k0 = p.k0 + (t0 + i) * kShTile;
-          const int klim = min(kShTile - 1, p.kend - 1 - s.k0);
-          auto pool_row = [&](int k) {
-            const int pg = min(max(bt[k >> a.page_shift], 0), a.n_pages - 1);
-            return (pg << a.page_shift) + (k & (a.page - 1));
-          };
-          s.row0 = pool_row(s.k0);
-          s.row1 = klim >= 16 ? pool_row(s.k0 + 16) : s.row0;
-          const bool fl = first && i == 0;  // the phase's first tile of this workgroup
-          s.flags = klim | (p.G > 0 ? kTfRemote : 0) | (fl ? kTfView : 0) |
-                    (fl && p.seg != seg_now ? kTfSeg : 0) | ph << kTfPhase;
-          s.f0 = p.G > 0 ? (int)fastdiv((uint32_t)s.k0, f) : 0;
-          s.km = p.G > 0 ? s.k0 - p.G * s.f0 : 0;
-          s.m = p.m;
-          s.l = p.l;
-          // the last tile here of its segment: the next phase is another segment's, or lies
-          // behind the range
-          if (t0 + i == tb - 1) {
-            bool last = true;
-            if (tb == p.n && ph + 1 < n_phases) {
-              const Phase nx = pv.phases[ph + 1];
-              int na, nb;
-              tiles_of(nx, &na, &nb);
-              last = nx.seg != p.seg || nb <= na;
-            }
-            if (last) s.flags |= kTfLast;
-          }
-          s_tiles[n + i] = s;
-        }
-        seg_now = p.seg;
-        n += cnt;
-      }
-      if (t0 + cnt < tb) {
-        ph_t = t0 + cnt;
-      } else {
-        ph_t = -1;
-        ++ph;
-      }
+    for (int d = kShSegs / 2; d > 0; d >>= 1)
+      if (s_before[i + d] <= j) i += d;
+    const Segment& sg = s_segs[i];
+    const int vis = s_from[i] + j - s_before[i];
+    const int rem = sg.n_rem * sg.n_views;
+    Tile s = {};
+    int t = sg.loc0 + vis - rem;
+    View vw = {};
+    if (vis < rem) {
+      t = sg.n_views == 1 ? vis : vis / sg.n_views;
+      vw = pv.views[sg.view0 + vis - t * sg.n_views];
     }
-    __syncthreads();
-    if (n == 0) break;
+    s.k0 = sg.k0 + t * kShTile;
+    const int klim = min(kShTile - 1, sg.kend - 1 - s.k0);
+    const int32_t* bt = a.table + (size_t)sg.seq * a.max_pages;
+    auto pool_row = [&](int k) {
+      const int pg = min(max(bt[k >> a.page_shift], 0), a.n_pages - 1);
+      return (pg << a.page_shift) + (k & (a.page - 1));
+    };
+    s.row0 = pool_row(s.k0);
+    s.row1 = klim < 16 ? s.row0 : a.page >= kShTile && (s.k0 & (a.page - 1)) + 16 < a.page
+                                      ? s.row0 + 16
+                                      : pool_row(s.k0 + 16);
+    const bool last = j + 1 == n || (i + 1 < kShSegs && s_before[i + 1] == j + 1);
+    s.flags = klim | (last ? kTfLast : 0) | i << kTfSeg;
+    if (vis < rem) {
+      const FastDiv f = {vw.m, vw.l, (uint32_t)vw.G};
+      s.f0 = (int)fastdiv_ge2((uint32_t)s.k0, f);
+      s.km = s.k0 - vw.G * s.f0;
+      s.m = vw.m;
+      s.lG = vw.l | (uint32_t)vw.G << 6;
+    }
+    s_tiles[j & (kShList - 1)] = s;
+  };
 
-    // ---- stream them
-    const int n_first = min(n, kShAhead);
-    for (int j = 0; j < n_first; ++j) issue(j);
-    if (n_first >= 5)
-      wait_vmem_n<4 * kShCopies>();
+  // What comes before visit i is multiplied: its copies and its rotation, the next one's
+  // rotation, and the request of the one that takes the buffer of visit i - 1.
+  auto advance = [&](int i) __attribute__((always_inline)) {
+    // this wave's copies of tile i + 1 have landed; the next three may fly
+    if (i + 4 < n)
+      wait_vmem_n<3 * kShCopies>();
+    else if (i + 3 < n)
+      wait_vmem_n<2 * kShCopies>();
+    else if (i + 2 < n)
+      wait_vmem_n<kShCopies>();
     else
       wait_vmem();
-    rotate(0);
-    for (int i = 0; i < n; ++i) {
-      // this wave's copies of tile i + 1 have landed; the next three may fly
-      if (i + 4 < n)
-        wait_vmem_n<3 * kShCopies>();
-      else if (i + 3 < n)
-        wait_vmem_n<2 * kShCopies>();
-      else if (i + 2 < n)
-        wait_vmem_n<kShCopies>();
-      else
-        wait_vmem();
-      __syncthreads();  // tile i is rotated everywhere, tile i - 1 used by all
-      if (i + kShAhead < n) issue(i + kShAhead);
-      if (i + 1 < n) rotate(i + 1);
-      const int flags = uni(s_tiles[i].flags), k0 = uni(s_tiles[i].k0);
-      if (flags & kTfView) {
-        const Phase p = pv.phases[flags >> kTfPhase];
-        ph_G = p.G;
-        if (flags & kTfSeg) {
-          const Segment sg = pv.segs[p.seg];
-          rows = sg.rows;
-          kend = sg.kend;
-          const int r = min(row, rows - 1);
-          const Member mb = pv.members[sg.m0 + r / a.g];
-          qpos = max(mb.len - 1, 0);
-          row_G = a.bifocal ? group_size(mb.len, a.w_pre) : 1;
-          lim = first_local(row_G, mb.len, a.w0);
-          qrow = a.q + ((size_t)max(mb.seq, 0) * a.Hq + h * a.g + r % a.g) * kHeadDim;
+    __syncthreads();  // tile i is rotated everywhere, tile i - 1 used by all
+    if (i + kShAhead < n) issue(i + kShAhead);
+    if (i + 1 < n) rotate(i + 1);
+    if ((i & (kShList / 2 - 1)) == 0 && i > 0 && i + kShList / 2 < n) fill(i + kShList / 2);
+  };
+
+  // The row that a lane serves: its query, position, G and first local key
+  struct Row {
+    const uint16_t* q;
+    int pos, G, lim;
+  };
+  auto row_of = [&](const Segment& sg, int r) {
+    Row x;
+    r = min(r, sg.rows - 1);
+    const Member mb = pv.members[sg.m0 + r / a.g];
+    x.pos = max(mb.len - 1, 0);
+    x.G = a.bifocal ? group_size(sg.len > 0 ? sg.len : mb.len, a.w_pre) : 1;
+    x.lim = first_local(x.G, x.pos, a.w0);
+    x.q = a.q + ((size_t)max(mb.seq, 0) * a.Hq + h * a.g + r % a.g) * kHeadDim;
+    return x;
+  };
+  // Keys [lo, hi) of the tile that a row keeps: in the remote view those before its first
+  // local key, if its G is the view's, else those from it on; none behind itself
+  auto keep = [&](const Row& x, int view_G, int k0, int kend, int* lo, int* hi) __attribute__((always_inline)) {
+    *hi = min(kend, x.pos + 1) - k0;
+    *lo = 0;
+    if (view_G > 0)
+      *hi = x.G == view_G ? min(*hi, x.lim - k0) : 0;
+    else
+      *lo = x.lim - k0;
+  };
+  auto state_at = [&](const Segment& sg, int half) {
+    const int rows = uni(sg.rows), halves = state_halves(rows);
+    return a.states + ((size_t)h * all_rows + uni(sg.row0) +
+                       (size_t)((w - uni(sg.w_first)) * halves + half) * rows) * kShStateFloats;
+  };
+
+  // ---- up to 128 rows: wave -> half of the keys, 32 rows as two blocks of 16 columns
+  auto run_small = [&](int i) __attribute__((always_inline)) {
+    int ln = lane;  // what follows from it is formed here: held across both loops it would spill
+    asm volatile("" : "+v"(ln));
+    const Segment& sg = s_segs[uni(s_tiles[i & (kShList - 1)].flags) >> kTfSeg];
+    const int rows = uni(sg.rows), kend = uni(sg.kend);
+    const int kh = wave & 1, r0 = 32 * (wave >> 1);
+    const int i16 = ln & 15, g4 = ln >> 4;
+    const bool on = r0 < rows, two = r0 + 16 < rows;
+    Row x[2];
+    bf16x8 qop[2][4];
+    f32x4 acc[2][8];
+    float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+    if (on) {
 #pragma unroll
-          for (int d = 0; d < 4; ++d) acc_o[d] = f32x16{};
-          neg_m = f32x16{};
-          m_ref = 0.f;
-          l_run = 0.f;
+      for (int c = 0; c < 2; ++c) x[c] = row_of(sg, r0 + 16 * c + i16);
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+      for (int d = 0; d < 8; ++d) acc[c][d] = f32x4{};
+#pragma unroll
+      for (int s = 0; s < 4; ++s) qop[c][s] = bf16x8{};
+    }
+    int q_view = -1;
+    for (;; ++i) {
+      advance(i);
+      const Tile& tl = s_tiles[i & (kShList - 1)];
+      const int flags = uni(tl.flags), k0 = uni(tl.k0);
+      if (on) {
+        const int view_G = uni((int)tl.lG) >> 6;
+        if ((view_G > 0) != q_view) {
+          q_view = view_G > 0;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            if (c == 1 && !two) break;
+            const int pos = view_G > 0 ? x[c].pos / x[c].G : x[c].pos;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+              sh_rotate_q(x[c].q, 32 * s + 8 * g4, a.rope, pos, a.q_scale, qop[c][s], qop[c][s + 2]);
+          }
         }
-        if (32 * wave < rows)
-          sh_load_q(qrow, hl32, a.rope, ph_G > 0 ? qpos / row_G : qpos, a.q_scale, qop);
-      }
-      if (32 * wave >= rows) continue;
-      const unsigned char* kb = smem + (i % kShBufs) * kShBuf;
-      const unsigned char* vb = kb + kShImg;
-      // S^T = K Q^T - m
-      f32x16 sc;
-      {
-        bf16x8 ring[4];
+        const unsigned char* kb = smem + (i % kShBufs) * kShBuf;
+        const unsigned char* vb = kb + kShImg;
+        bf16x8 kr[4];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) ring[s] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * s + hl32));
-        sc = neg_m;
+        for (int s = 0; s < 4; ++s) kr[s] = *(const bf16x8*)(kb + sh_koff(16 * kh + i16, 4 * s + g4));
+        i16x4 vr[8];
+        const int vt = 16 * kh + 4 * g4 + (i16 >> 2);
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {
-          sc = mfma32(ring[s & 3], qop[s], sc);
-          if (s + 4 < 8) ring[s & 3] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * (s + 4) + hl32));
+        for (int d = 0; d < 8; ++d)
+          vr[d] = lds_read_tr4(vb + sh_voff(vt, 2 * d + ((i16 & 3) >> 1)) + 8 * (i16 & 1));
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          if (c == 1 && !two) break;
+          f32x4 sc = f32x4{};
+#pragma unroll
+          for (int s = 0; s < 4; ++s) sc = mfma16(kr[s], qop[c][s], sc);
+          int lo, hi;
+          keep(x[c], view_G, k0, kend, &lo, &hi);
+          if (__ballot(lo > 0 || hi < kShTile) != 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int t = 16 * kh + 4 * g4 + e;
+              sc[e] = t >= lo && t < hi ? sc[e] : -INFINITY;
+            }
+          }
+          const float mt = sh_max16_32(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])));
+          const bool upd = mt > m_run[c] + kShSlack || (m_run[c] == -INFINITY && mt != -INFINITY);
+          if (__ballot(upd) != 0) {
+            const float alpha = upd && m_run[c] != -INFINITY ? fast_exp2(m_run[c] - mt) : 1.f;
+            l_run[c] *= alpha;
+#pragma unroll
+            for (int d = 0; d < 8; ++d) acc[c][d] *= alpha;
+            if (upd) m_run[c] = mt;
+          }
+          const float m_use = m_run[c] == -INFINITY ? 0.f : m_run[c];
+          f32x4 p;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[e] = fast_exp2(sc[e] - m_use);
+          const bf16x4 pb = __builtin_convertvector(p, bf16x4);
+          const f32x4 pr = __builtin_convertvector(pb, f32x4);
+          l_run[c] += (pr[0] + pr[1]) + (pr[2] + pr[3]);
+#pragma unroll
+          for (int d = 0; d < 8; ++d) acc[c][d] = sh_mfma16k16(vr[d], pb, acc[c][d]);
         }
       }
-      auto vop = [&](int m) __attribute__((always_inline)) {
-        const unsigned char* p = vb + 4096 * (m >> 2) + sh_voff(vk_lane, 4 * (m & 3) + vc_lane) + 8 * (lane & 1);
-        return concat_tr(lds_read_tr4(p), lds_read_tr4(p + 2048));
-      };
-      bf16x8 vr[4];
+      if (flags & kTfLast) break;
+    }
+    if (on) {
+      float* st = state_at(sg, kh);
 #pragma unroll
-      for (int m = 0; m < 4; ++m) vr[m] = vop(m);
-      // keep the keys [lo, hi) of the tile: in the remote view those before the row's
-      // first local key, where its G is the phase's, else those from it on
-      int lo = 0, hi = kend - k0;
-      if (ph_G > 0)
-        hi = row_G == ph_G ? min(hi, lim - k0) : 0;
-      else
-        lo = lim - k0;
-      if (__ballot(lo > 0 || hi < kShTile) != 0) {
+      for (int c = 0; c < 2; ++c) {
+        const int r = r0 + 16 * c + i16;
+        float l = l_run[c] + __shfl_xor(l_run[c], 16);
+        l += __shfl_xor(l, 32);
+        if (r < rows) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int t = 8 * (e >> 2) + (e & 3) + 4 * hl32;
-          sc[e] = t >= lo && t < hi ? sc[e] : -INFINITY;
+          for (int d = 0; d < 8; ++d) *(f32x4*)(st + ((size_t)(4 * d + g4) * rows + r) * 4) = acc[c][d];
+          if (g4 == 0) *(float2*)(st + (size_t)rows * kHeadDim + 2 * r) = make_float2(m_run[c], l);
         }
       }
-      float mt = fmaxf(sc[0], sc[1]);
+    }
+    return i + 1;
+  };
+
+  // ---- above: wave -> 32 rows and all keys
+  auto run_large = [&](int i) __attribute__((always_inline)) {
+    int ln = lane;  // what follows from it is formed here: held across both loops it would spill
+    asm volatile("" : "+v"(ln));
+    const Segment& sg = s_segs[uni(s_tiles[i & (kShList - 1)].flags) >> kTfSeg];
+    const int rows = uni(sg.rows), kend = uni(sg.kend);
+    const int hl32 = ln >> 5, kr_lane = ln & 31;
+    const int vk_lane = 4 * hl32 + ((ln & 15) >> 2);
+    const int vc_lane = 2 * ((ln >> 4) & 1) + ((ln & 3) >> 1);
+    const int row = 32 * wave + kr_lane;
+    const bool on = 32 * wave < rows;
+    const Row x = row_of(sg, row);
+    bf16x8 qop[8];
+    f32x16 acc[4], neg_m = f32x16{};
+    float m_ref = 0.f, l_run = 0.f;
 #pragma unroll
-      for (int e = 2; e < 16; e += 2) mt = fmaxf(mt, fmaxf(sc[e], sc[e + 1]));
-      {
-        typedef unsigned u32x2v __attribute__((ext_vector_type(2)));
-        const u32x2v r =
-            __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
-        mt = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-      }
-      // the reference follows the first keys of a row, and scores far above it
-      const float l_both = l_run;  // zero in both lanes of the row or in neither, see below
-      const bool upd = mt != -INFINITY && (mt > kShSlack || l_both == 0.f);
-      if (__ballot(upd) != 0) {
-        const float shift = upd ? mt : 0.f;
-        const float alpha = l_both == 0.f ? 1.f : fast_exp2(-shift);
+    for (int d = 0; d < 4; ++d) acc[d] = f32x16{};
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sc[e] -= shift;
+    for (int s = 0; s < 8; ++s) qop[s] = bf16x8{};
+    int q_view = -1;
+    for (;; ++i) {
+      advance(i);
+      const Tile& tl = s_tiles[i & (kShList - 1)];
+      const int flags = uni(tl.flags), k0 = uni(tl.k0);
+      if (on) {
+        const int view_G = uni((int)tl.lG) >> 6;
+        if ((view_G > 0) != q_view) {
+          q_view = view_G > 0;
+          const int pos = view_G > 0 ? x.pos / x.G : x.pos;
 #pragma unroll
-        for (int d = 0; d < 4; ++d) acc_o[d] *= alpha;
-        l_run *= alpha;
-        m_ref += shift;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) neg_m[e] = -m_ref;
-      }
-      bf16x8 pb[2];
-      float ps0 = 0.f, ps1 = 0.f;
-      const sh_bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        float p[8];
-#pragma unroll
-        for (int t = 0; t < 8; ++t) p[t] = fast_exp2(sc[8 * q + t]);
-        pb[q] = pack8(p);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const sh_bf16x2 pr = {pb[q][2 * u], pb[q][2 * u + 1]};
-          if (u & 1)
-            ps1 = __builtin_amdgcn_fdot2_f32_bf16(pr, one, ps1, false);
-          else
-            ps0 = __builtin_amdgcn_fdot2_f32_bf16(pr, one, ps0, false);
+          for (int s = 0; s < 4; ++s)
+            sh_rotate_q(x.q, 16 * s + 8 * hl32, a.rope, pos, a.q_scale, qop[s], qop[s + 4]);
         }
-      }
-      // both lanes of a row add the row's whole sum, so that l_run says in either
-      // whether the row has a key
-      float ps = ps0 + ps1;
-      {
-        typedef unsigned u32x2v __attribute__((ext_vector_type(2)));
-        const u32x2v r =
+        const unsigned char* kb = smem + (i % kShBufs) * kShBuf;
+        const unsigned char* vb = kb + kShImg;
+        // S^T = K Q^T - m
+        f32x16 sc = neg_m;
+        {
+          bf16x8 ring[4];
+#pragma unroll
+          for (int s = 0; s < 4; ++s) ring[s] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * s + hl32));
+#pragma unroll
+          for (int s = 0; s < 8; ++s) {
+            sc = mfma32(ring[s & 3], qop[s], sc);
+            if (s + 4 < 8) ring[s & 3] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * (s + 4) + hl32));
+          }
+        }
+        auto vop = [&](int m) __attribute__((always_inline)) {
+          const unsigned char* p =
+              vb + 4096 * (m >> 2) + sh_voff(vk_lane, 4 * (m & 3) + vc_lane) + 8 * (ln & 1);
+          return concat_tr(lds_read_tr4(p), lds_read_tr4(p + 2048));
+        };
+        bf16x8 vr[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) vr[m] = vop(m);
+        int lo, hi;
+        keep(x, view_G, k0, kend, &lo, &hi);
+        if (__ballot(lo > 0 || hi < kShTile) != 0) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int t = 8 * (e >> 2) + (e & 3) + 4 * hl32;
+            sc[e] = t >= lo && t < hi ? sc[e] : -INFINITY;
+          }
+        }
+        float mt = fmaxf(sc[0], sc[1]);
+#pragma unroll
+        for (int e = 2; e < 16; e += 2) mt = fmaxf(mt, fmaxf(sc[e], sc[e + 1]));
+        mt = sh_max32(mt);
+        // the reference follows the first keys of a row, and scores far above it.  l_run is
+        // the row's whole sum in both of its lanes.
+        const bool upd = mt != -INFINITY && (mt > kShSlack || l_run == 0.f);
+        if (__ballot(upd) != 0) {
+          const float shift = upd ? mt : 0.f;
+          const float alpha = l_run == 0.f ? 1.f : fast_exp2(-shift);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sc[e] -= shift;
+#pragma unroll
+          for (int d = 0; d < 4; ++d) acc[d] *= alpha;
+          l_run *= alpha;
+          m_ref += shift;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) neg_m[e] = -m_ref;
+        }
+        bf16x8 pb[2];
+        float ps0 = 0.f, ps1 = 0.f;
+        const sh_bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          float p[8];
+#pragma unroll
+          for (int t = 0; t < 8; ++t) p[t] = fast_exp2(sc[8 * q + t]);
+          pb[q] = pack8(p);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const sh_bf16x2 pr = {pb[q][2 * u], pb[q][2 * u + 1]};
+            if (u & 1)
+              ps1 = __builtin_amdgcn_fdot2_f32_bf16(pr, one, ps1, false);
+            else
+              ps0 = __builtin_amdgcn_fdot2_f32_bf16(pr, one, ps0, false);
+          }
+        }
+        const float ps = ps0 + ps1;
+        const sh_u32x2 both =
             __builtin_amdgcn_permlane32_swap(__float_as_uint(ps), __float_as_uint(ps), false, false);
-        ps = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-      }
-      l_run += ps;
+        l_run += __uint_as_float(both[0]) + __uint_as_float(both[1]);
 #pragma unroll
-      for (int m = 0; m < 8; ++m) {
-        acc_o[m & 3] = mfma32(vr[m & 3], pb[m >> 2], acc_o[m & 3]);
-        if (m + 4 < 8) vr[m & 3] = vop(m + 4);
+        for (int m = 0; m < 8; ++m) {
+          acc[m & 3] = mfma32(vr[m & 3], pb[m >> 2], acc[m & 3]);
+          if (m + 4 < 8) vr[m & 3] = vop(m + 4);
+        }
       }
-      if ((flags & kTfLast) && row < rows) {
-        const Phase p = pv.phases[flags >> kTfPhase];
-        const Segment sg = pv.segs[p.seg];
-        float* st = a.states + ((size_t)h * pv.header[kHdRows] + sg.row0 + (size_t)(w - sg.w_first) * rows) *
-                                   kShStateFloats;
+      if (flags & kTfLast) break;
+    }
+    if (row < rows) {
+      if (sg.len > 0 && sg.n_w == 1) {  // a chunk's block that is whole here
+        const Member mb = pv.members[sg.m0 + row / a.g];
+        if (mb.seq >= 0) {
+          const float inv = 1.f / l_run;
+          const int hd = h * a.g + row % a.g;
+          uint16_t* o = a.o + ((size_t)mb.seq * a.Hq + hd) * kHeadDim;
+          if (a.lse != nullptr && hl32 == 0)
+            a.lse[(size_t)hd * a.T + mb.seq] = (m_ref + log2f(l_run)) * 0.69314718055994531f;
+#pragma unroll
+          for (int db = 0; db < 4; ++db) {
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+              f32x4 t;
+#pragma unroll
+              for (int jj = 0; jj < 4; ++jj) t[jj] = acc[db][4 * q4 + jj] * inv;
+              *(bf16x4*)(o + 32 * db + 8 * q4 + 4 * hl32) = __builtin_convertvector(t, bf16x4);
+            }
+          }
+        }
+      } else {
+        float* st = state_at(sg, 0);
 #pragma unroll
         for (int db = 0; db < 4; ++db) {
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
             f32x4 t;
 #pragma unroll
-            for (int jj = 0; jj < 4; ++jj) t[jj] = acc_o[db][4 * q4 + jj];
+            for (int jj = 0; jj < 4; ++jj) t[jj] = acc[db][4 * q4 + jj];
             *(f32x4*)(st + ((size_t)(8 * db + 2 * q4 + hl32) * rows + row) * 4) = t;
           }
         }
-        if (hl32 == 0) *(float2*)(st + (size_t)rows * kHeadDim + 2 * row) = make_float2(m_ref, l_run);
+        if (hl32 == 0)
+          *(float2*)(st + (size_t)rows * kHeadDim + 2 * row) =
+              make_float2(l_run == 0.f ? -INFINITY : m_ref, l_run);
       }
     }
-    __syncthreads();  // the list and the buffers are free
+    return i + 1;
+  };
+
+  // ---- the segments of the range, up to 64 at a time
+  for (int s0 = uni(pv.wg_first[w]); s0 < n_segs; s0 += kShSegs) {
+    int more = 0;
+    if (wave == 0) {
+      const int i = s0 + lane;
+      int va = 0, vb = 0;
+      bool past = true;
+      if (i < n_segs) {
+        const Segment sg = pv.segs[i];
+        s_segs[lane] = sg;
+        const unsigned long long st = sg.start_lo | (unsigned long long)sg.start_hi << 32;
+        const uint32_t c = (uint32_t)visit_cost(sg.rows);
+        auto below = [&](unsigned long long x) {  // its visits that begin before x
+          if (x <= st + kSegCost) return 0;
+          const unsigned long long d = x - st - kSegCost;
+          return d >= (unsigned long long)sg.visits * c ? sg.visits
+                                                        : (int)(((uint32_t)d + c - 1) / c);
+        };
+        va = below(x0);
+        vb = below(x1);
+        past = st >= x1;
+      }
+      int incl = vb - va;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(incl, d);
+        if (lane >= d) incl += y;
+      }
+      s_from[lane] = va;
+      s_before[lane] = incl - (vb - va);
+      if (lane == 63) s_tiles[0].k0 = incl;
+      if (lane == 0) s_tiles[0].m = __ballot(past) == 0;
+    }
+    __syncthreads();
+    n = uni(s_tiles[0].k0);
+    more = uni((int)s_tiles[0].m);
+    __syncthreads();
+    if (n > 0) {
+      fill(0);
+      fill(kShList / 2);
+      __syncthreads();
+      const int n_first = min(n, kShAhead);
+      for (int j = 0; j < n_first; ++j) issue(j);
+      if (n_first == kShAhead)
+        wait_vmem_n<(kShAhead - 1) * kShCopies>();
+      else
+        wait_vmem();
+      rotate(0);
+      for (int i = 0; i < n;) {
+        const int rows = uni(s_segs[uni(s_tiles[i & (kShList - 1)].flags) >> kTfSeg].rows);
+        i = rows <= kShSmall ? run_small(i) : run_large(i);
+      }
+    }
+    if (!more) break;
+    __syncthreads();  // the lists and the buffers are free
   }
 }
 
@@ -813,31 +1087,54 @@ constexpr int kMgRows = 8;
 __global__ __launch_bounds__(512) void merge_shared_kernel(SharedArgs a) {
   __shared__ f32x4 s_o[32][kMgRows];
   __shared__ float2 s_ml[32][kMgRows];
-  const PlanView pv = plan_view(a.plan, a.B, a.n_groups, a.g);
+  const PlanView pv = plan_of(a);
   if (!plan_fits(a, pv.header)) return;
   const int h = blockIdx.y;
   const int rl = threadIdx.x & (kMgRows - 1), c = (threadIdx.x / kMgRows) & 31, half = threadIdx.x >> 8;
   const int r = blockIdx.x * kMgRows + rl;
-  const int mi = min(r / a.g, a.B - 1);
-  const Member mb = pv.members[mi];
-  const bool on = r < a.B * a.g && mb.seq >= 0;
+  const int n_members = a.chunk ? a.T : a.B;
+  const Member mb = pv.members[min(r / a.g, n_members - 1)];
+  bool on = r < n_members * a.g && mb.seq >= 0;
   float M = -INFINITY, den = 0.f;
   f32x4 acc = f32x4{};
   const float* base = a.states + (size_t)h * pv.header[kHdRows] * kShStateFloats;
-  auto join = [&](int seg, bool prefix) {
+  auto join = [&](int seg, bool block) {
     if (seg < 0) return;
     const Segment sg = pv.segs[seg];
-    const int at = prefix ? r - sg.m0 * a.g : r % a.g;
-    for (int i = half; i < sg.n_w; i += 2) {
-      const float* st = base + (size_t)(sg.row0 + i * sg.rows) * kShStateFloats;
-      const float2 ml = *(const float2*)(st + (size_t)sg.rows * kHeadDim + 2 * at);
-      const f32x4 x = *(const f32x4*)(st + ((size_t)c * sg.rows + at) * 4);
-      if (ml.y == 0.f) continue;  // no key of this row
-      const float m = fmaxf(M, ml.x);
-      const float wa = M == -INFINITY ? 0.f : fast_exp2(M - m), wb = fast_exp2(ml.x - m);
-      den = wa * den + wb * ml.y;
-      acc = wa * acc + wb * x;
-      M = m;
+    const int n = sg.n_w * state_halves(sg.rows);
+    if (sg.len > 0 && n == 1) {  // written by its workgroup
+      on = false;
+      return;
+    }
+    const int at = block ? r - sg.m0 * a.g : r % a.g;
+    constexpr int kAtOnce = 4;
+    for (int i0 = half; i0 < n; i0 += 2 * kAtOnce) {
+      float2 ml[kAtOnce];
+      f32x4 x[kAtOnce];
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const float* st = base + (size_t)(sg.row0 + min(i0 + 2 * j, n - 1) * sg.rows) * kShStateFloats;
+        ml[j] = *(const float2*)(st + (size_t)sg.rows * kHeadDim + 2 * at);
+        x[j] = *(const f32x4*)(st + ((size_t)c * sg.rows + at) * 4);
+        if (i0 + 2 * j >= n) ml[j] = make_float2(-INFINITY, 0.f);
+      }
+      float top = M;
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        if (ml[j].y == 0.f) ml[j].x = -INFINITY;  // no key of this row
+        top = fmaxf(top, ml[j].x);
+      }
+      const float wa = M == -INFINITY ? 0.f : fast_exp2(M - top);
+      den *= wa;
+      acc *= wa;
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        if (ml[j].y == 0.f) continue;
+        const float wb = fast_exp2(ml[j].x - top);
+        den += wb * ml[j].y;
+        acc += wb * x[j];
+      }
+      M = top;
     }
   };
   if (on) {
@@ -853,34 +1150,68 @@ __global__ __launch_bounds__(512) void merge_shared_kernel(SharedArgs a) {
   const float2 ml = s_ml[c][rl];
   const float top = fmaxf(M, ml.x);
   f32x4 out = f32x4{};
-  if (top != -INFINITY) {
-    const float wa = M == -INFINITY ? 0.f : fast_exp2(M - top);
-    const float wb = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - top);
-    out = (wa * acc + wb * s_o[c][rl]) * (1.f / (wa * den + wb * ml.y));
+  float lse = -INFINITY;
+  if (den != 0.f || ml.y != 0.f) {
+    const float wa = den == 0.f ? 0.f : fast_exp2(M - top);
+    const float wb = ml.y == 0.f ? 0.f : fast_exp2(ml.x - top);
+    f32x4 sum = f32x4{};
+    if (den != 0.f) sum += wa * acc;
+    if (ml.y != 0.f) sum += wb * s_o[c][rl];
+    const float all = wa * den + wb * ml.y;
+    out = sum * (1.f / all);
+    lse = (top + log2f(all)) * 0.69314718055994531f;
   }
-  *(bf16x4*)(a.o + ((size_t)mb.seq * a.Hq + h * a.g + r % a.g) * kHeadDim + 4 * c) =
+  const int hd = h * a.g + r % a.g;
+  *(bf16x4*)(a.o + ((size_t)mb.seq * a.Hq + hd) * kHeadDim + 4 * c) =
       __builtin_convertvector(out, bf16x4);
+  if (a.lse != nullptr && c == 0) a.lse[(size_t)hd * a.T + mb.seq] = lse;
 }
 
 // ---------------------------------------------------------------- launchers
+static size_t chunk_plan_lds(int B, int T, int g) {
+  return (3 * (size_t)B + 2) * sizeof(int) + chunk_sizes(B, T, g).segs * 6 + 8;
+}
+bool chunk_rows_fit(int B, int T, int g) { return chunk_plan_lds(B, T, g) <= 60 * 1024; }
+
+static hipError_t launch_plan(bool chunk, SharedPlanArgs& a, hipStream_t stream) {
+  if (chunk) {
+    hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(kPlThreads), chunk_plan_lds(a.B, a.T, a.g), stream, a);
+  } else {
+    const PlanSizes z = decode_sizes(a.B, a.n_groups, a.g);
+    const size_t lists = z.segs * 6 + 8;
+    const size_t lds = (2 * (size_t)a.B + 3 * (size_t)a.n_groups + 2) * sizeof(int) + lists;
+    hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(kPlThreads), lds, stream, a);
+  }
+  return hipGetLastError();
+}
+
 hipError_t launch_shared_plan(bool bifocal, const int32_t* kv_lens, const int32_t* members,
                               const int32_t* group_starts, const int32_t* shared, int B,
                               int n_groups, int Hq, int Hkv, int max_pages, int page, int w_pre,
                               int w0, int n_cu, void* plan, hipStream_t stream) {
-  SharedPlanArgs a{kv_lens, members, group_starts, shared, plan, B, n_groups, Hq / Hkv, Hkv,
-                   max_pages, page, head_workgroups(n_cu, Hkv), bifocal ? 1 : 0, w_pre, w0};
-  const size_t lds = ((size_t)B + 3 * n_groups + 2 + plan_blocks(B, n_groups, a.g) + 1) * sizeof(int);
-  hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(kPlThreads), lds, stream, a);
+  SharedPlanArgs a{kv_lens, members, group_starts, shared, nullptr, plan, B, n_groups, 0, Hq / Hkv,
+                   Hkv, max_pages, page, head_workgroups(n_cu, Hkv), bifocal ? 1 : 0, w_pre, w0};
+  return launch_plan(false, a, stream);
+}
+
+static hipError_t launch_rows(SharedArgs& a, hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1) {
+  const long long rows = (long long)(a.chunk ? a.T : a.B) * a.g;
+  hipError_t e = hipSuccess;
+  if (ev0 != nullptr && (e = hipEventRecord(ev0, stream)) != hipSuccess) return e;
+  hipLaunchKernelGGL(shared_rows_kernel, dim3((unsigned)a.n_wg * a.Hkv), dim3(kShThreads), 0, stream, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (ev1 != nullptr && (e = hipEventRecord(ev1, stream)) != hipSuccess) return e;
+  hipLaunchKernelGGL(merge_shared_kernel, dim3((unsigned)((rows + kMgRows - 1) / kMgRows), (unsigned)a.Hkv),
+                     dim3(512), 0, stream, a);
   return hipGetLastError();
 }
 
-hipError_t launch_decode_shared(bool bifocal, const uint16_t* q, const uint16_t* k,
-                                const uint16_t* v, const int32_t* table, int max_pages,
-                                int n_pages, int page_shift, void* plan, uint16_t* o,
-                                const float2* rope, const uint32_t* rope16, int B, int n_groups,
-                                int Hq, int Hkv, int w_pre, int w0, int n_cu, void* ws,
-                                hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1) {
-  SharedArgs a;
+static SharedArgs rows_args(bool bifocal, const uint16_t* q, const uint16_t* k, const uint16_t* v,
+                            const int32_t* table, int max_pages, int n_pages, int page_shift,
+                            void* plan, void* states, uint16_t* o, const float2* rope,
+                            const uint32_t* rope16, int B, int Hq, int Hkv, int w_pre, int w0,
+                            int n_cu) {
+  SharedArgs a = {};
   a.q = q;
   a.k = k;
   a.v = v;
@@ -889,9 +1220,8 @@ hipError_t launch_decode_shared(bool bifocal, const uint16_t* q, const uint16_t*
   a.rope = rope;
   a.rope16 = rope16;
   a.plan = plan;
-  a.states = (float*)ws;
+  a.states = (float*)states;
   a.B = B;
-  a.n_groups = n_groups;
   a.Hq = Hq;
   a.Hkv = Hkv;
   a.g = Hq / Hkv;
@@ -904,15 +1234,40 @@ hipError_t launch_decode_shared(bool bifocal, const uint16_t* q, const uint16_t*
   a.w_pre = w_pre;
   a.w0 = w0;
   a.q_scale = 1.4426950408889634f / sqrtf((float)kHeadDim);
-  hipError_t e = hipSuccess;
-  if (ev0 != nullptr && (e = hipEventRecord(ev0, stream)) != hipSuccess) return e;
-  hipLaunchKernelGGL(decode_shared_kernel, dim3((unsigned)a.n_wg * Hkv), dim3(kShThreads), 0, stream, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (ev1 != nullptr && (e = hipEventRecord(ev1, stream)) != hipSuccess) return e;
-  hipLaunchKernelGGL(merge_shared_kernel,
-                     dim3((unsigned)((B * a.g + kMgRows - 1) / kMgRows), (unsigned)Hkv), dim3(512), 0,
-                     stream, a);
-  return hipGetLastError();
+  return a;
+}
+
+hipError_t launch_decode_shared(bool bifocal, const uint16_t* q, const uint16_t* k,
+                                const uint16_t* v, const int32_t* table, int max_pages,
+                                int n_pages, int page_shift, void* plan, uint16_t* o,
+                                const float2* rope, const uint32_t* rope16, int B, int n_groups,
+                                int Hq, int Hkv, int w_pre, int w0, int n_cu, void* ws,
+                                hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1) {
+  SharedArgs a = rows_args(bifocal, q, k, v, table, max_pages, n_pages, page_shift, plan, ws, o, rope,
+                           rope16, B, Hq, Hkv, w_pre, w0, n_cu);
+  a.n_groups = n_groups;
+  return launch_rows(a, stream, ev0, ev1);
+}
+
+// scratch: chunk_scratch_bytes
+hipError_t launch_chunk_rows(bool bifocal, const uint16_t* q, const uint16_t* k, const uint16_t* v,
+                             const int32_t* table, int max_pages, int n_pages, int page_shift,
+                             const int32_t* cu, const int32_t* kv_lens, uint16_t* o, float* lse,
+                             const float2* rope, const uint32_t* rope16, int B, int T, int Hq,
+                             int Hkv, int w_pre, int w0, int n_cu, void* scratch,
+                             hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1) {
+  const int g = Hq / Hkv;
+  void* states = (char*)scratch + (plan_bytes(chunk_sizes(B, T, g)) + 255) / 256 * 256;
+  SharedPlanArgs p{kv_lens, nullptr, nullptr, nullptr, cu, scratch, B, 0, T, g, Hkv, max_pages,
+                   1 << page_shift, head_workgroups(n_cu, Hkv), bifocal ? 1 : 0, w_pre, w0};
+  const hipError_t e = launch_plan(true, p, stream);
+  if (e != hipSuccess) return e;
+  SharedArgs a = rows_args(bifocal, q, k, v, table, max_pages, n_pages, page_shift, scratch, states, o,
+                           rope, rope16, B, Hq, Hkv, w_pre, w0, n_cu);
+  a.chunk = 1;
+  a.T = T;
+  a.lse = lse;
+  return launch_rows(a, stream, ev0, ev1);
 }
 
 }  // namespace jl

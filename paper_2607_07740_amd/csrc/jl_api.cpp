@@ -96,6 +96,14 @@ hipError_t launch_decode_shared(bool bifocal, const uint16_t* q, const uint16_t*
                                 const float2* rope, const uint32_t* rope16, int B, int n_groups,
                                 int Hq, int Hkv, int w_pre, int w0, int n_cu, void* ws,
                                 hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1);
+size_t chunk_scratch_bytes(int B, int T, int Hq, int Hkv);
+bool chunk_rows_fit(int B, int T, int g);
+hipError_t launch_chunk_rows(bool bifocal, const uint16_t* q, const uint16_t* k, const uint16_t* v,
+                             const int32_t* table, int max_pages, int n_pages, int page_shift,
+                             const int32_t* cu, const int32_t* kv_lens, uint16_t* o, float* lse,
+                             const float2* rope, const uint32_t* rope16, int B, int T, int Hq,
+                             int Hkv, int w_pre, int w0, int n_cu, void* scratch,
+                             hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1);
 hipError_t launch_pages_fork(const Pages& p, const int32_t* parent, hipStream_t stream);
 hipError_t launch_pages_reserve(const Pages& p, const int32_t* n_new, int32_t* starts,
                                 int32_t* granted, int32_t* moves, int32_t* info,
@@ -786,17 +794,13 @@ int check_pages(const jl_pages* t, jl::Pages* out) {
   return JL_OK;
 }
 
-// ----------------------------------------- decode over shared prefixes
-// What the plan and the decode call have in common; *page_shift is set.
-int check_shared(int B, int n_groups, int Hq, int Hkv, int head_dim, int max_pages, int page_size,
-                 bool bifocal, int w_pre, int w0, int* page_shift) {
+// ----------------- rows over paged caches: shared prefixes, packed chunks
+// What the plan, the decode and the chunk call have in common; *page_shift is set.
+int check_rows(int B, int Hq, int Hkv, int head_dim, int most_g, int max_pages, int page_size,
+               bool bifocal, int w_pre, int w0, int* page_shift) {
   const int st = check_common(B, Hq, Hkv, head_dim, 1.0);
   if (st != JL_OK) return st;
-  if (Hq / Hkv > 8) return fail(JL_ERR_UNSUPPORTED, "decode GQA group %d > 8", Hq / Hkv);
-  if (n_groups < 1) return fail(JL_ERR_INVALID_ARG, "n_groups must be >= 1 (got %d)", n_groups);
-  if (B > jl::kShMaxSeqs || n_groups > jl::kShMaxSeqs)
-    return fail(JL_ERR_UNSUPPORTED, "%d sequences in %d groups (at most %d of each)", B, n_groups,
-                jl::kShMaxSeqs);
+  if (Hq / Hkv > most_g) return fail(JL_ERR_UNSUPPORTED, "GQA group %d > %d", Hq / Hkv, most_g);
   if (page_size < 16 || page_size > (1 << 20) || (page_size & (page_size - 1)) != 0)
     return fail(JL_ERR_INVALID_ARG, "page_size must be a power of two in [16, 2^20] (got %d)",
                 page_size);
@@ -810,6 +814,59 @@ int check_shared(int B, int n_groups, int Hq, int Hkv, int head_dim, int max_pag
   *page_shift = 0;
   while ((1 << *page_shift) < page_size) ++*page_shift;
   return JL_OK;
+}
+
+int check_shared(int B, int n_groups, int Hq, int Hkv, int head_dim, int max_pages, int page_size,
+                 bool bifocal, int w_pre, int w0, int* page_shift) {
+  if (n_groups < 1) return fail(JL_ERR_INVALID_ARG, "n_groups must be >= 1 (got %d)", n_groups);
+  if (B > jl::kShMaxSeqs || n_groups > jl::kShMaxSeqs)
+    return fail(JL_ERR_UNSUPPORTED, "%d sequences in %d groups (at most %d of each)", B, n_groups,
+                jl::kShMaxSeqs);
+  return check_rows(B, Hq, Hkv, head_dim, 8, max_pages, page_size, bifocal, w_pre, w0, page_shift);
+}
+
+int varlen_paged(bool bifocal, const void* q, const void* kp, const void* vp, const int32_t* table,
+                 int max_pages, int page_size, int n_pages, const int32_t* cu,
+                 const int32_t* kv_lens, void* o, float* lse, int B, int T, int Hq, int Hkv,
+                 int head_dim, double theta, int w_pre, int w0, void* stream) {
+  int shift = 0;
+  int st = check_rows(B, Hq, Hkv, head_dim, jl::kShMaxGroup, max_pages, page_size, bifocal, w_pre,
+                      w0, &shift);
+  if (st != JL_OK) return st;
+  if (!(theta > 0.0) || !std::isfinite(theta))
+    return fail(JL_ERR_INVALID_ARG, "rope_theta must be finite and > 0");
+  if (T < 1) return fail(JL_ERR_INVALID_ARG, "total_tokens must be >= 1 (got %d)", T);
+  if (n_pages < 1) return fail(JL_ERR_INVALID_ARG, "n_pages must be >= 1 (got %d)", n_pages);
+  if ((long long)n_pages * page_size > 0x7fffffffLL)
+    return fail(JL_ERR_UNSUPPORTED, "a pool of %lld tokens (at most 2^31 - 1)",
+                (long long)n_pages * page_size);
+  if (B > jl::kShMaxSeqs || past_int32(T, Hq, 1) || !jl::chunk_rows_fit(B, T, Hq / Hkv))
+    return fail(JL_ERR_UNSUPPORTED, "%d tokens of %d sequences in one call", T, B);
+  if (!aligned16(q) || !aligned16(kp) || !aligned16(vp) || !aligned16(o))
+    return fail(JL_ERR_INVALID_ARG, "q, k_pages, v_pages, o must be non-null and 16-byte aligned");
+  if (lse != nullptr && !aligned4(lse)) return fail(JL_ERR_INVALID_ARG, "lse must be 4-byte aligned");
+  if (!aligned4(table) || !aligned4(cu) || !aligned4(kv_lens))
+    return fail(JL_ERR_INVALID_ARG, "block_table, cu_seqlens, kv_lens must be non-null and aligned");
+  Tables tab{};
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  st = get_table(theta, max_pages * page_size, s, &tab);
+  if (st != JL_OK) return st;
+  std::lock_guard<std::mutex> launch_lock(g_prefill_mu);
+  void* scratch = nullptr;
+  const size_t bytes = jl::chunk_scratch_bytes(B, T, Hq, Hkv);
+  st = get_scratch(s, bytes, &scratch);
+  if (st != JL_OK) return st;
+  if (scratch == nullptr)
+    return fail(JL_ERR_HIP, "packed chunks: %zu bytes of scratch cannot be allocated under "
+                "stream capture (make the call once before)", bytes);
+  hipEvent_t ev0, ev1;
+  timing_events(0, &ev0, &ev1);
+  const hipError_t e = jl::launch_chunk_rows(
+      bifocal, (const uint16_t*)q, (const uint16_t*)kp, (const uint16_t*)vp, table, max_pages,
+      n_pages, shift, cu, kv_lens, (uint16_t*)o, lse, tab.f32, tab.f16, B, T, Hq, Hkv, w_pre, w0,
+      jl::cu_count(), scratch, s, ev0, ev1);
+  if (e != hipSuccess) return hip_fail(e, "packed chunk launch");
+  return ok();
 }
 
 int shared_plan(bool bifocal, const int32_t* kv_lens, const int32_t* members,
@@ -1404,6 +1461,28 @@ int jl_rope_attention_decode_shared(const void* q, const void* k_pages, const vo
   return decode_shared(false, q, k_pages, v_pages, block_table, max_pages, page_size, n_pages,
                        plan, plan_bytes, o, B, n_groups, Hq, Hkv, head_dim, rope_theta, 1, 0,
                        workspace, workspace_bytes, stream);
+}
+
+int jl_bifocal_prefill_varlen_paged(const void* q, const void* k_pages, const void* v_pages,
+                                    const int32_t* block_table, int max_pages, int page_size,
+                                    int n_pages, const int32_t* cu_seqlens,
+                                    const int32_t* kv_lens, void* o, float* lse, int B,
+                                    int total_tokens, int Hq, int Hkv, int head_dim,
+                                    double rope_theta, int w_pretrained, int w_local,
+                                    void* stream) {
+  return varlen_paged(true, q, k_pages, v_pages, block_table, max_pages, page_size, n_pages,
+                      cu_seqlens, kv_lens, o, lse, B, total_tokens, Hq, Hkv, head_dim, rope_theta,
+                      w_pretrained, w_local, stream);
+}
+
+int jl_rope_attention_varlen_paged(const void* q, const void* k_pages, const void* v_pages,
+                                   const int32_t* block_table, int max_pages, int page_size,
+                                   int n_pages, const int32_t* cu_seqlens, const int32_t* kv_lens,
+                                   void* o, float* lse, int B, int total_tokens, int Hq, int Hkv,
+                                   int head_dim, double rope_theta, void* stream) {
+  return varlen_paged(false, q, k_pages, v_pages, block_table, max_pages, page_size, n_pages,
+                      cu_seqlens, kv_lens, o, lse, B, total_tokens, Hq, Hkv, head_dim, rope_theta,
+                      1, 0, stream);
 }
 
 int jl_debug_schedule(const int32_t* lengths, int n_lengths, const int32_t* positions,

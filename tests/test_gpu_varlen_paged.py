@@ -1,0 +1,232 @@
+"""Packed chunks behind paged caches against the fp64 oracle's prefill of each whole sequence.
+
+Tolerances: the parity bounds of the prefill tests, whose roundings these are (rotated queries and
+keys, cos and sin of the keys, softmax weights in bf16, u = 2^-8): scores of unit normals are off
+by 0.007 rms at most, which moves an output, a weighted mean of values of size 1, by less than
+0.004 rms; with its own rounding 2e-2 at most and 2e-3 in the mean.  The row sums carry the scores' errors averaged
+over the weights: 2e-2."""
+import numpy as np
+import pytest
+
+from oracle import oracle as O
+from paper_2607_07740_amd import api, synth
+from parity_util import assert_close, say, to_dev, to_f64
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+NAN = np.uint16(0x7FC0)
+
+
+def _i32(x):
+    return torch.tensor(np.asarray(x, np.int32), device="cuda")
+
+
+class Chunks:
+    """Sequences of `lens` keys on shuffled pages, the last n[b] positions of each in the call; rows
+    and pages that none has hold NaN."""
+
+    def __init__(self, lens, n, Hq, Hkv, page, seed, spare=1):
+        rng = np.random.default_rng(seed)
+        self.lens, self.n, self.Hq, self.Hkv, self.page = list(lens), list(n), Hq, Hkv, page
+        self.max_pages = -(-max(max(lens), 1) // page) + spare
+        n_pages = sum(-(-x // page) for x in lens) + 2
+        deal = iter(rng.permutation(n_pages))
+        self.kp = np.full((n_pages, page, Hkv, 128), NAN, np.uint16)
+        self.vp = np.full_like(self.kp, NAN)
+        self.table = np.full((len(lens), self.max_pages), -1, np.int32)
+        self.seqs, rows = [], []
+        for b, L in enumerate(lens):
+            q, k, v = synth.prefill_inputs(1, Hq, Hkv, max(L, 1), 128, seed=seed + 1 + b,
+                                           outlier_channels=8)
+            self.seqs.append((q, k, v))
+            rows.append(q[0, L - n[b]:L] if n[b] <= L else
+                        np.concatenate([np.full((n[b] - L, Hq, 128), NAN, np.uint16), q[0, :L]]))
+            for j in range(-(-L // page)):
+                p = next(deal)
+                self.table[b, j] = p
+                part = slice(j * page, min((j + 1) * page, L))
+                m = part.stop - part.start
+                self.kp[p, :m], self.vp[p, :m] = k[0, part], v[0, part]
+        self.q = np.concatenate(rows)
+        self.cu = np.concatenate([[0], np.cumsum(n)])
+
+    def run(self, w_pre=1, w0=0, bifocal=True, **kw):
+        r = api.prefill_varlen_paged(to_dev(self.q), to_dev(self.kp), to_dev(self.vp),
+                                     _i32(self.table), _i32(self.cu), _i32(self.lens),
+                                     w_pretrained=w_pre, w_local=w0, bifocal=bifocal, **kw)
+        torch.cuda.synchronize()
+        return r
+
+    def want(self, w_pre=1, w0=0, bifocal=True):
+        outs, lses = [], []
+        for (q, k, v), L, n in zip(self.seqs, self.lens, self.n):
+            if L == 0 or n == 0:
+                continue
+            o, lse = O.prefill(q, k, v, theta=1e6, w_pretrained=w_pre if bifocal else 1 << 30,
+                               w_local=w0)[:2]
+            m = min(n, L)
+            outs.append(o[0, L - m:])
+            lses.append(lse[0, :, L - m:])
+        return np.concatenate(outs), np.concatenate(lses, 1)
+
+
+# lens, rows: single tokens, whole prompts, blocks of one and of several, lengths beside tile and
+# page ends, sequences without rows or without keys
+SHAPES = [([1], [1]), ([5, 64, 65, 200], [5, 64, 1, 33]), ([300, 0, 129, 31, 700], [0, 0, 129, 30, 65]),
+          ([640] * 3, [8, 1, 640]), ([97, 96, 33, 32, 17, 16], [1, 2, 3, 4, 5, 6]),
+          ([500], [300])]
+
+
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("bifocal", [True, False])
+def test_matches_oracle(shape, page, bifocal):
+    Hq, Hkv = [(4, 2), (8, 2), (6, 2), (16, 2), (8, 1), (32, 2)][shape]
+    c = Chunks(*SHAPES[shape], Hq, Hkv, page, seed=shape + page)
+    say("varlen_paged", shape, page, bifocal)
+    out, lse = c.run(96, 40, bifocal, want_lse=True)
+    o, l = c.want(96, 40, bifocal)
+    assert_close(to_f64(out), o, what="out")
+    assert_close(lse.cpu().numpy(), l, what="lse")
+
+
+@pytest.mark.parametrize("w_pre,w0", [(1, 0), (50, 0), (64, 7), (300, 33), (10, 2147483647)])
+def test_windows(w_pre, w0):
+    c = Chunks([640, 100, 333, 64], [70, 100, 3, 1], 8, 2, 64, seed=w_pre)
+    say("windows", w_pre, w0)
+    assert_close(to_f64(c.run(w_pre, w0)), c.want(w_pre, w0)[0], what="w_pre %d w0 %d" % (w_pre, w0))
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (3, 1), (7, 1), (20, 2), (16, 1), (64, 1), (256, 1), (8, 8)])
+def test_groups_of_heads(Hq, Hkv):
+    """Any number of query heads for a kv head, up to a block's rows."""
+    c = Chunks([200, 90, 40], [100, 2, 40], Hq, Hkv, 32, seed=Hq)
+    say("heads", Hq, Hkv)
+    assert_close(to_f64(c.run(64, 20)), c.want(64, 20)[0], what="heads %d/%d" % (Hq, Hkv))
+
+
+def test_agrees_with_the_chunk_of_one_start_and_repeats_its_bits():
+    c = Chunks([900, 900], [130, 130], 8, 2, 64, seed=3)
+    say("one start")
+    one, two = c.run(256, 100), c.run(256, 100)
+    q = to_dev(c.q).view(2, 130, 8, 128)
+    ref = api.prefill_chunk_paged(q, to_dev(c.kp), to_dev(c.vp), _i32(c.table), q_start=770,
+                                  w_pretrained=256, w_local=100)
+    torch.cuda.synchronize()
+    assert torch.equal(one, two)
+    assert_close(to_f64(one), to_f64(ref.view(260, 8, 128)), what="chunk of one start")
+
+
+def test_rows_of_no_sequence_and_before_the_first_position_stay():
+    c = Chunks([40, 3, 70], [10, 5, 7], 4, 2, 16, seed=9)
+    out = torch.full((24, 4, 128), 3.0, device="cuda").to(torch.bfloat16)
+    lse = torch.full((4, 24), 5.0, device="cuda")
+    q = torch.cat([to_dev(c.q), torch.full((2, 4, 128), float("nan"), device="cuda").to(torch.bfloat16)])
+    say("rows that stay")
+    api.prefill_varlen_paged(q, to_dev(c.kp), to_dev(c.vp), _i32(c.table), _i32(c.cu), _i32(c.lens),
+                             w_pretrained=30, w_local=9, out=out, lse=lse)
+    torch.cuda.synchronize()
+    o, l = c.want(30, 9)
+    left = [10, 11, 22, 23]  # two rows more than keys, two of no sequence
+    done = [i for i in range(24) if i not in left]
+    assert (out[left] == 3.0).all() and (lse[:, left] == 5.0).all()
+    assert_close(to_f64(out[done]), o, what="out")
+    assert_close(lse[:, done].cpu().numpy(), l, what="lse")
+
+
+def test_bad_lists_do_not_leave_the_arrays():
+    c = Chunks([40, 30, 70], [10, 5, 7], 4, 2, 16, seed=10)
+    table = c.table.copy()
+    table[0, :2] = [1 << 30, -(1 << 31)]
+    for cu, lens in (([-9, 2147483647, 3, 22], [40, 30, 70]), ([22, 11, 5, 0], [2147483647, -9, 1]),
+                     ([0, 0, 0, 0], [0, 0, 0]), ([5, 6, 6, 22], [2147483647] * 3)):
+        say("bad lists", cu)
+        api.prefill_varlen_paged(to_dev(c.q), to_dev(c.kp), to_dev(c.vp), _i32(table), _i32(cu),
+                                 _i32(lens), w_pretrained=30, w_local=9)
+        torch.cuda.synchronize()
+
+
+def test_captured_on_a_stream_of_its_own():
+    c = Chunks([500, 90], [3, 40], 8, 2, 64, seed=13)
+    q, k, v, t, cu, lens = (to_dev(c.q), to_dev(c.kp), to_dev(c.vp), _i32(c.table), _i32(c.cu),
+                            _i32(c.lens))
+    out = torch.empty_like(q)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        api.prefill_varlen_paged(q, k, v, t, cu, lens, w_pretrained=100, w_local=30, out=out)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            api.prefill_varlen_paged(q, k, v, t, cu, lens, w_pretrained=100, w_local=30, out=out)
+    want = c.want(100, 30)[0]
+    for i in range(4):
+        if i == 2:  # other lengths in the same arrays
+            cu.copy_(_i32([0, 1, 43]))
+            lens.copy_(_i32([498, 90]))
+        say("replay", i)
+        out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = api.prefill_varlen_paged(q, k, v, t, cu, lens, w_pretrained=100, w_local=30)
+        torch.cuda.synchronize()
+        if i < 2:
+            assert_close(to_f64(out), want, what="replay %d" % i)
+        rows = slice(0, 43) if i < 2 else slice(1 - 1, 43)
+        assert torch.equal(out[rows], eager[rows])
+
+
+def test_the_rows_of_a_forked_batch_from_prompt_to_tokens():
+    """What a server does: prompts enter forked pages in packed rows, are prefilled behind what they
+    share, and every sequence decodes a token over the shared prefix."""
+    rng = np.random.default_rng(1)
+    Hq, Hkv, page, w_pre, w0 = 8, 2, 16, 100, 30
+    pages = api.pages_alloc(4, 20, 70, page)
+    kp = torch.zeros((70, page, Hkv, 128), device="cuda", dtype=torch.bfloat16)
+    vp = torch.zeros_like(kp)
+    hist = [np.zeros((3, 0, Hq, 128), np.uint16) for _ in range(4)]
+
+    def turn(n):
+        """n[b] more tokens of every sequence; the outputs of their rows, packed."""
+        x = [synth.prefill_inputs(1, Hq, Hq, max(m, 1), 128, seed=int(rng.integers(1 << 30))) for m in n]
+        for b, m in enumerate(n):
+            hist[b] = np.concatenate([hist[b], np.stack([t[0, :m] for t in x[b]])], 1)
+        rows = [np.concatenate([t[i][0, :m] for t, m in zip(x, n)]) for i in range(3)]
+        cu = _i32(np.concatenate([[0], np.cumsum(n)]))
+        starts, granted, moves, info = api.pages_reserve(pages, _i32(n))
+        api.copy_pages([kp, vp], moves, info)
+        q, k, v = to_dev(rows[0]), to_dev(rows[1][:, :Hkv]), to_dev(rows[2][:, :Hkv])
+        api.cache_append(kp, vp, k, v, starts, n_new=granted, block_table=pages.table, cu_seqlens=cu)
+        return q, cu
+
+    def want(b, m):
+        q, k, v = hist[b]
+        o = O.prefill(q[None], k[None, :, :Hkv], v[None, :, :Hkv], theta=1e6, w_pretrained=w_pre,
+                      w_local=w0)[0]
+        return o[0, -m:]
+
+    say("server: prompt")
+    q, cu = turn([140, 0, 0, 9])
+    out = api.prefill_varlen_paged(q, kp, vp, pages.table, cu, pages.lens, w_pretrained=w_pre,
+                                   w_local=w0)
+    torch.cuda.synchronize()
+    assert_close(to_f64(out), np.concatenate([want(0, 140), want(3, 9)]), what="prompt")
+    say("server: forks and their turns")
+    api.pages_fork(pages, _i32([0, 0, 0, 3]))
+    hist[1], hist[2] = hist[0].copy(), hist[0].copy()
+    q, cu = turn([5, 33, 1, 60])
+    out = api.prefill_varlen_paged(q, kp, vp, pages.table, cu, pages.lens, w_pretrained=w_pre,
+                                   w_local=w0)
+    torch.cuda.synchronize()
+    assert_close(to_f64(out), np.concatenate([want(0, 5), want(1, 33), want(2, 1), want(3, 60)]),
+                 what="turns")
+    for i in range(3):
+        say("server: token", i)
+        q, _ = turn([1, 1, 1, 1])
+        plan = api.shared_plan(pages.lens, _i32([0, 3, 4]), _i32([140, 0]), Hq=Hq, Hkv=Hkv,
+                               page_size=page, max_pages=20, w_pretrained=w_pre, w_local=w0)
+        out = api.decode_shared(q, kp, vp, pages.table, plan)
+        torch.cuda.synchronize()
+        assert_close(to_f64(out), np.concatenate([want(b, 1) for b in range(4)]), what="token %d" % i)

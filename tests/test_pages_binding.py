@@ -165,3 +165,24 @@ def test_sizes_of_plans_and_workspaces():
         assert api.shared_plan_bytes(*bad) == 0
     assert api.decode_shared_workspace_bytes(4, 8, 2, 64) == 0
     assert api.decode_shared_workspace_bytes(4096, 8, 2) == 0
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(B=0), BAD), (dict(T=0), BAD), (dict(Hq=7), BAD), (dict(Hkv=0), BAD), (dict(d=64), UNS),
+    (dict(d=5), BAD), (dict(Hq=514), UNS), (dict(B=2049), UNS), (dict(T=1 << 21), UNS),
+    (dict(T=1 << 30, Hq=512, Hkv=256), UNS), (dict(page=8), BAD), (dict(page=80), BAD),
+    (dict(max_pages=0), BAD), (dict(max_pages=1 << 18), UNS), (dict(n_pages=0), BAD),
+    (dict(n_pages=1 << 26), UNS), (dict(theta=-1.0), BAD), (dict(q=None), BAD), (dict(k=MIS), BAD),
+    (dict(v=None), BAD), (dict(o=P(0x1008)), BAD), (dict(lse=MIS), BAD), (dict(table=None), BAD),
+    (dict(cu=MIS), BAD), (dict(lens=None), BAD)])
+def test_chunk_arguments_are_checked(kw, code):
+    d = dict(q=A, k=A, v=A, table=A, max_pages=8, page=64, n_pages=32, cu=A, lens=A, o=A, lse=None,
+             B=4, T=20, Hq=8, Hkv=2, d=128, theta=1e6)
+    d.update(kw)
+    head = (d["q"], d["k"], d["v"], d["table"], d["max_pages"], d["page"], d["n_pages"], d["cu"],
+            d["lens"], d["o"], d["lse"], d["B"], d["T"], d["Hq"], d["Hkv"], d["d"], d["theta"])
+    L = api.lib()
+    assert L.jl_bifocal_prefill_varlen_paged(*head, 32, 4, None) == code
+    assert L.jl_rope_attention_varlen_paged(*head, None) == code
+    for w in ((0, 4), (32, -1)):
+        assert L.jl_bifocal_prefill_varlen_paged(*head, *w, None) in (BAD, code)
