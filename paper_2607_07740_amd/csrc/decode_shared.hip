@@ -27,6 +27,7 @@
 // those of a row.
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "decode_shared.h"
 #include "jl_device.h"
@@ -72,7 +73,7 @@ struct Member {
   int pre, suf;  // its segments, -1: none
 };
 // States that a (workgroup, segment) leaves
-__host__ __device__ inline int state_halves(int rows) { return rows <= kShSmall ? 2 : 1; }
+__host__ __device__ inline int state_halves(int) { return 1; }
 
 struct PlanView {
   int* header;
@@ -636,48 +637,78 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
   const unsigned char* kbase = (const unsigned char*)(a.k + (size_t)h * kHeadDim);
   const unsigned char* vbase = (const unsigned char*)(a.v + (size_t)h * kHeadDim);
 
-  // ---- copies of a tile: keys 4 wave .. + 3 of K, V and their cos/sin rows
-  const int cp_key = 4 * wave + (lane >> 4), cp_slot = lane & 15;
-  const uint32_t cp_k = 16 * (cp_slot ^ sh_kswz(cp_key));
-  const uint32_t cp_v = 16 * (cp_slot ^ sh_vswz(cp_key));
-  auto issue = [&](int j) __attribute__((always_inline)) {
+  // ---- what a wave does of a tile's copies and rotation: with ALL keys 4 wave .. + 3, else
+  // the last four waves take 8 each
+  auto uni_tile = [&](int j) __attribute__((always_inline)) {
     const Tile& s = s_tiles[j & (kShList - 1)];
-    const int flags = uni(s.flags), klim = flags & 31, k0 = uni(s.k0);
-    const int row = min(4 * wave, klim) < 16 ? uni(s.row0) : uni(s.row1);
-    const int key = min(cp_key, klim);
-    const size_t off = (size_t)(uint32_t)row * kv_row_bytes;
-    const uint32_t buf = smem_base + (uint32_t)(j % kShBufs) * kShBuf + 1024 * wave;
-    const uint32_t ro = (uint32_t)(key & 15) * kv_row_bytes;
-    dma16_s(kbase + off, ro + cp_k, buf);
-    dma16_s(vbase + off, ro + cp_v, buf + kShImg);
-    int pos = k0 + key;
-    const int lG = uni((int)s.lG);
-    if (lG != 0) {
-      const FastDiv f = {(uint32_t)uni((int)s.m), (uint32_t)lG & 63, 2};
-      pos = uni(s.f0) + (int)fastdiv_ge2((uint32_t)(uni(s.km) + key), f);
-    }
-    dma16_s(a.rope16, (uint32_t)pos * 256 + 16 * cp_slot, buf + 2 * kShImg);
+    return Tile{uni(s.row0), uni(s.row1), uni(s.k0), uni(s.flags), uni(s.f0), uni(s.km),
+                (uint32_t)uni((int)s.m), (uint32_t)uni((int)s.lG)};
   };
-  // Rotation of this wave's four keys, in place: lane -> key, a chunk pair's half
-  const int rt_key = 4 * wave + (lane >> 4), rt_c = (lane >> 1) & 7, rt_h = lane & 1;
-  const int rt_lo = sh_koff(rt_key, rt_c) + 8 * rt_h, rt_hi = sh_koff(rt_key, rt_c + 8) + 8 * rt_h;
-  const int rt_cs = 2 * kShImg + rt_key * 256 + 32 * rt_c + 16 * rt_h;
-  auto rotate = [&](int j) __attribute__((always_inline)) {
+  // requests keys key0 .. key0 + 3 of K and V, and their cos/sin rows
+  auto copy4 = [&](const Tile& t, int ln, int key0, uint32_t buf) __attribute__((always_inline)) {
+    const int klim = t.flags & 31, slot = ln & 15;
+    const int mine = key0 + (ln >> 4), key = min(mine, klim);
+    const size_t off = (size_t)(uint32_t)(min(key0, klim) < 16 ? t.row0 : t.row1) * kv_row_bytes;
+    const uint32_t ro = (uint32_t)(key & 15) * kv_row_bytes;
+    const uint32_t dst = buf + 256 * key0;
+    dma16_s(kbase + off, ro + 16 * (slot ^ sh_kswz(mine)), dst);
+    dma16_s(vbase + off, ro + 16 * (slot ^ sh_vswz(mine)), dst + kShImg);
+    int pos = t.k0 + key;
+    if (t.lG != 0) {
+      const FastDiv f = {t.m, t.lG & 63, 2};
+      pos = t.f0 + (int)fastdiv_ge2((uint32_t)(t.km + key), f);
+    }
+    dma16_s(a.rope16, (uint32_t)pos * 256 + 16 * slot, dst + 2 * kShImg);
+  };
+  auto issue = [&](auto all, int ln, int j) __attribute__((always_inline)) {
+    const Tile t = uni_tile(j);
+    const uint32_t buf = smem_base + (uint32_t)(j % kShBufs) * kShBuf;
+    if constexpr (decltype(all)::value) {
+      copy4(t, ln, 4 * wave, buf);
+    } else {
+      copy4(t, ln, 8 * (wave - 4), buf);
+      copy4(t, ln, 8 * (wave - 4) + 4, buf);
+    }
+  };
+  // Rotation in place.  4 keys: lane -> key, half of a chunk pair; 8 keys: lane -> key, chunk pair
+  auto rotate = [&](auto all, int ln, int j) __attribute__((always_inline)) {
     unsigned char* b = smem + (j % kShBufs) * kShBuf;
-    const sh_u32x2 xl = *(const sh_u32x2*)(b + rt_lo), xh = *(const sh_u32x2*)(b + rt_hi);
-    const u32x4 cs = *(const u32x4*)(b + rt_cs);
-    uint32_t l0, h0, l1, h1;
-    rot_word_dot2(xl[0], xh[0], cs[0], cs[1], l0, h0);
-    rot_word_dot2(xl[1], xh[1], cs[2], cs[3], l1, h1);
-    *(sh_u32x2*)(b + rt_lo) = sh_u32x2{l0, l1};
-    *(sh_u32x2*)(b + rt_hi) = sh_u32x2{h0, h1};
+    if constexpr (decltype(all)::value) {
+      const int r4_key = 4 * wave + (ln >> 4), r4_c = (ln >> 1) & 7, r4_h = ln & 1;
+      const int r4_lo = sh_koff(r4_key, r4_c) + 8 * r4_h, r4_hi = sh_koff(r4_key, r4_c + 8) + 8 * r4_h;
+      const int r4_cs = 2 * kShImg + r4_key * 256 + 32 * r4_c + 16 * r4_h;
+      const sh_u32x2 xl = *(const sh_u32x2*)(b + r4_lo), xh = *(const sh_u32x2*)(b + r4_hi);
+      const u32x4 cs = *(const u32x4*)(b + r4_cs);
+      uint32_t l0, h0, l1, h1;
+      rot_word_dot2(xl[0], xh[0], cs[0], cs[1], l0, h0);
+      rot_word_dot2(xl[1], xh[1], cs[2], cs[3], l1, h1);
+      *(sh_u32x2*)(b + r4_lo) = sh_u32x2{l0, l1};
+      *(sh_u32x2*)(b + r4_hi) = sh_u32x2{h0, h1};
+    } else {
+      const int r8_key = 8 * (wave - 4) + (ln >> 3), r8_c = ln & 7;
+      const int r8_lo = sh_koff(r8_key, r8_c), r8_hi = sh_koff(r8_key, r8_c + 8);
+      const int r8_cs = 2 * kShImg + r8_key * 256 + 32 * r8_c;
+      const u32x4 xl = *(const u32x4*)(b + r8_lo), xh = *(const u32x4*)(b + r8_hi);
+      const u32x4 ca = *(const u32x4*)(b + r8_cs), cb = *(const u32x4*)(b + r8_cs + 16);
+      u32x4 lo, hi;
+#pragma unroll
+      for (int w2 = 0; w2 < 4; ++w2) {
+        uint32_t l, hh;
+        rot_word_dot2(xl[w2], xh[w2], w2 < 2 ? ca[2 * w2] : cb[2 * w2 - 4],
+                      w2 < 2 ? ca[2 * w2 + 1] : cb[2 * w2 - 3], l, hh);
+        lo[w2] = l;
+        hi[w2] = hh;
+      }
+      *(u32x4*)(b + r8_lo) = lo;
+      *(u32x4*)(b + r8_hi) = hi;
+    }
   };
 
   int n = 0;  // visits of the held segments
-  // Addresses of visits j0 .. j0 + 127, by as many threads
+  // Addresses of visits j0 .. j0 + 127, by the last two waves
   auto fill = [&](int j0) __attribute__((always_inline)) {
-    const int j = j0 + tid;
-    if (tid >= kShList / 2 || j >= n) return;
+    const int at = tid - (kShThreads - kShList / 2), j = j0 + at;
+    if (at < 0 || j >= n) return;
     int i = 0;  // the held segment: the last that begins at or before the visit
 #pragma unroll
     for (int d = kShSegs / 2; d > 0; d >>= 1)
@@ -715,22 +746,36 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     s_tiles[j & (kShList - 1)] = s;
   };
 
-  // What comes before visit i is multiplied: its copies and its rotation, the next one's
-  // rotation, and the request of the one that takes the buffer of visit i - 1.
-  auto advance = [&](int i) __attribute__((always_inline)) {
-    // this wave's copies of tile i + 1 have landed; the next three may fly
+  // A wave's copies of tile i + 1 have landed; those of the next three may fly
+  auto landed = [&](auto all, int i) __attribute__((always_inline)) {
+    constexpr int k = decltype(all)::value ? kShCopies : 2 * kShCopies;
     if (i + 4 < n)
-      wait_vmem_n<3 * kShCopies>();
+      wait_vmem_n<3 * k>();
     else if (i + 3 < n)
-      wait_vmem_n<2 * kShCopies>();
+      wait_vmem_n<2 * k>();
     else if (i + 2 < n)
-      wait_vmem_n<kShCopies>();
+      wait_vmem_n<k>();
     else
       wait_vmem();
-    __syncthreads();  // tile i is rotated everywhere, tile i - 1 used by all
-    if (i + kShAhead < n) issue(i + kShAhead);
-    if (i + 1 < n) rotate(i + 1);
+  };
+  // Beside visit i: the request of the tile that takes visit i - 1's buffer, the next one's
+  // rotation
+  auto produce = [&](auto all, int ln, int i) __attribute__((always_inline)) {
+    if (i + kShAhead < n) issue(all, ln, i + kShAhead);
+    if (i + 1 < n) rotate(all, ln, i + 1);
+  };
+  auto refill = [&](int i) __attribute__((always_inline)) {
     if ((i & (kShList / 2 - 1)) == 0 && i > 0 && i + kShList / 2 < n) fill(i + kShList / 2);
+  };
+  auto start = [&](auto all, int ln) __attribute__((always_inline)) {
+    constexpr int k = decltype(all)::value ? kShCopies : 2 * kShCopies;
+    const int first = min(n, kShAhead);
+    for (int j = 0; j < first; ++j) issue(all, ln, j);
+    if (first == kShAhead)
+      wait_vmem_n<(kShAhead - 1) * k>();
+    else
+      wait_vmem();
+    rotate(all, ln, 0);
   };
 
   // The row that a lane serves: its query, position, G and first local key
@@ -764,115 +809,10 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
                        (size_t)((w - uni(sg.w_first)) * halves + half) * rows) * kShStateFloats;
   };
 
-  // ---- up to 128 rows: wave -> half of the keys, 32 rows as two blocks of 16 columns
-  auto run_small = [&](int i) __attribute__((always_inline)) {
-    int ln = lane;  // what follows from it is formed here: held across both loops it would spill
-    asm volatile("" : "+v"(ln));
-    const Segment& sg = s_segs[uni(s_tiles[i & (kShList - 1)].flags) >> kTfSeg];
-    const int rows = uni(sg.rows), kend = uni(sg.kend);
-    const int kh = wave & 1, r0 = 32 * (wave >> 1);
-    const int i16 = ln & 15, g4 = ln >> 4;
-    const bool on = r0 < rows, two = r0 + 16 < rows;
-    Row x[2];
-    bf16x8 qop[2][4];
-    f32x4 acc[2][8];
-    float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
-    if (on) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) x[c] = row_of(sg, r0 + 16 * c + i16);
-    }
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-#pragma unroll
-      for (int d = 0; d < 8; ++d) acc[c][d] = f32x4{};
-#pragma unroll
-      for (int s = 0; s < 4; ++s) qop[c][s] = bf16x8{};
-    }
-    int q_view = -1;
-    for (;; ++i) {
-      advance(i);
-      const Tile& tl = s_tiles[i & (kShList - 1)];
-      const int flags = uni(tl.flags), k0 = uni(tl.k0);
-      if (on) {
-        const int view_G = uni((int)tl.lG) >> 6;
-        if ((view_G > 0) != q_view) {
-          q_view = view_G > 0;
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            if (c == 1 && !two) break;
-            const int pos = view_G > 0 ? x[c].pos / x[c].G : x[c].pos;
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-              sh_rotate_q(x[c].q, 32 * s + 8 * g4, a.rope, pos, a.q_scale, qop[c][s], qop[c][s + 2]);
-          }
-        }
-        const unsigned char* kb = smem + (i % kShBufs) * kShBuf;
-        const unsigned char* vb = kb + kShImg;
-        bf16x8 kr[4];
-#pragma unroll
-        for (int s = 0; s < 4; ++s) kr[s] = *(const bf16x8*)(kb + sh_koff(16 * kh + i16, 4 * s + g4));
-        i16x4 vr[8];
-        const int vt = 16 * kh + 4 * g4 + (i16 >> 2);
-#pragma unroll
-        for (int d = 0; d < 8; ++d)
-          vr[d] = lds_read_tr4(vb + sh_voff(vt, 2 * d + ((i16 & 3) >> 1)) + 8 * (i16 & 1));
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          if (c == 1 && !two) break;
-          f32x4 sc = f32x4{};
-#pragma unroll
-          for (int s = 0; s < 4; ++s) sc = mfma16(kr[s], qop[c][s], sc);
-          int lo, hi;
-          keep(x[c], view_G, k0, kend, &lo, &hi);
-          if (__ballot(lo > 0 || hi < kShTile) != 0) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int t = 16 * kh + 4 * g4 + e;
-              sc[e] = t >= lo && t < hi ? sc[e] : -INFINITY;
-            }
-          }
-          const float mt = sh_max16_32(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])));
-          const bool upd = mt > m_run[c] + kShSlack || (m_run[c] == -INFINITY && mt != -INFINITY);
-          if (__ballot(upd) != 0) {
-            const float alpha = upd && m_run[c] != -INFINITY ? fast_exp2(m_run[c] - mt) : 1.f;
-            l_run[c] *= alpha;
-#pragma unroll
-            for (int d = 0; d < 8; ++d) acc[c][d] *= alpha;
-            if (upd) m_run[c] = mt;
-          }
-          const float m_use = m_run[c] == -INFINITY ? 0.f : m_run[c];
-          f32x4 p;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) p[e] = fast_exp2(sc[e] - m_use);
-          const bf16x4 pb = __builtin_convertvector(p, bf16x4);
-          const f32x4 pr = __builtin_convertvector(pb, f32x4);
-          l_run[c] += (pr[0] + pr[1]) + (pr[2] + pr[3]);
-#pragma unroll
-          for (int d = 0; d < 8; ++d) acc[c][d] = sh_mfma16k16(vr[d], pb, acc[c][d]);
-        }
-      }
-      if (flags & kTfLast) break;
-    }
-    if (on) {
-      float* st = state_at(sg, kh);
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int r = r0 + 16 * c + i16;
-        float l = l_run[c] + __shfl_xor(l_run[c], 16);
-        l += __shfl_xor(l, 32);
-        if (r < rows) {
-#pragma unroll
-          for (int d = 0; d < 8; ++d) *(f32x4*)(st + ((size_t)(4 * d + g4) * rows + r) * 4) = acc[c][d];
-          if (g4 == 0) *(float2*)(st + (size_t)rows * kHeadDim + 2 * r) = make_float2(m_run[c], l);
-        }
-      }
-    }
-    return i + 1;
-  };
-
-  // ---- above: wave -> 32 rows and all keys
-  auto run_large = [&](int i) __attribute__((always_inline)) {
-    int ln = lane;  // what follows from it is formed here: held across both loops it would spill
+  // ---- the visits of a segment from i on, by the waves that hold its rows: 32 of them and all
+  // keys of a tile each
+  auto consume = [&](auto all, int i) __attribute__((always_inline)) {
+    int ln = lane;  // what follows from it is formed here: held across all loops it would spill
     asm volatile("" : "+v"(ln));
     const Segment& sg = s_segs[uni(s_tiles[i & (kShList - 1)].flags) >> kTfSeg];
     const int rows = uni(sg.rows), kend = uni(sg.kend);
@@ -883,7 +823,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     const bool on = 32 * wave < rows;
     const Row x = row_of(sg, row);
     bf16x8 qop[8];
-    f32x16 acc[4], neg_m = f32x16{};
+    f32x16 acc[4];
     float m_ref = 0.f, l_run = 0.f;
 #pragma unroll
     for (int d = 0; d < 4; ++d) acc[d] = f32x16{};
@@ -891,11 +831,15 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     for (int s = 0; s < 8; ++s) qop[s] = bf16x8{};
     int q_view = -1;
     for (;; ++i) {
-      advance(i);
+      if constexpr (decltype(all)::value) landed(all, i);
       const Tile& tl = s_tiles[i & (kShList - 1)];
-      const int flags = uni(tl.flags), k0 = uni(tl.k0);
+      const int flags = uni(tl.flags), k0 = uni(tl.k0), view_G = uni((int)tl.lG) >> 6;
+      __syncthreads();  // tile i is rotated, tile i - 1 used by all
+      if constexpr (decltype(all)::value) {
+        produce(all, ln, i);
+        refill(i);
+      }
       if (on) {
-        const int view_G = uni((int)tl.lG) >> 6;
         if ((view_G > 0) != q_view) {
           q_view = view_G > 0;
           const int pos = view_G > 0 ? x.pos / x.G : x.pos;
@@ -906,15 +850,28 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
         const unsigned char* kb = smem + (i % kShBufs) * kShBuf;
         const unsigned char* vb = kb + kShImg;
         // S^T = K Q^T - m
-        f32x16 sc = neg_m;
+        f32x16 sc;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] = -m_ref;
         {
-          bf16x8 ring[4];
+          constexpr int kRing = decltype(all)::value ? 4 : 8;
+          bf16x8 ring[kRing];
 #pragma unroll
-          for (int s = 0; s < 4; ++s) ring[s] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * s + hl32));
+          for (int s = 0; s < kRing; ++s) ring[s] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * s + hl32));
+          if constexpr (decltype(all)::value) {
 #pragma unroll
-          for (int s = 0; s < 8; ++s) {
-            sc = mfma32(ring[s & 3], qop[s], sc);
-            if (s + 4 < 8) ring[s & 3] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * (s + 4) + hl32));
+            for (int s = 0; s < 8; ++s) {
+              sc = mfma32(ring[s & 3], qop[s], sc);
+              if (s + 4 < 8) ring[s & 3] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * (s + 4) + hl32));
+            }
+          } else {  // alone on its SIMD's matrix core: two chains
+            f32x16 odd = f32x16{};
+#pragma unroll
+            for (int s = 0; s < 8; s += 2) {
+              sc = mfma32(ring[s], qop[s], sc);
+              odd = mfma32(ring[s + 1], qop[s + 1], odd);
+            }
+            sc += odd;
           }
         }
         auto vop = [&](int m) __attribute__((always_inline)) {
@@ -950,8 +907,6 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
           for (int d = 0; d < 4; ++d) acc[d] *= alpha;
           l_run *= alpha;
           m_ref += shift;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) neg_m[e] = -m_ref;
         }
         bf16x8 pb[2];
         float ps0 = 0.f, ps1 = 0.f;
@@ -1023,13 +978,12 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     return i + 1;
   };
 
-  // ---- the segments of the range, up to 64 at a time
-  for (int s0 = uni(pv.wg_first[w]); s0 < n_segs; s0 += kShSegs) {
-    int more = 0;
+  // ---- the segments of the range, up to 64 of one kind at a time
+  for (int s0 = uni(pv.wg_first[w]); s0 < n_segs;) {
     if (wave == 0) {
       const int i = s0 + lane;
       int va = 0, vb = 0;
-      bool past = true;
+      bool past = true, large = false;
       if (i < n_segs) {
         const Segment sg = pv.segs[i];
         s_segs[lane] = sg;
@@ -1044,7 +998,14 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
         va = below(x0);
         vb = below(x1);
         past = st >= x1;
+        large = sg.rows > kShSmall;
       }
+      // those before the first of the other kind
+      const unsigned long long some = __ballot(vb > va), big = __ballot(vb > va && large);
+      const bool kind = some != 0 && (big >> __builtin_ctzll(some) & 1) != 0;
+      const unsigned long long other = some & (kind ? ~big : big);
+      const int stop = other != 0 ? __builtin_ctzll(other) : kShSegs;
+      if (lane >= stop) vb = va;
       int incl = vb - va;
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
@@ -1054,30 +1015,42 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       s_from[lane] = va;
       s_before[lane] = incl - (vb - va);
       if (lane == 63) s_tiles[0].k0 = incl;
-      if (lane == 0) s_tiles[0].m = __ballot(past) == 0;
+      if (__ballot(past && lane < stop) == 0 || stop < kShSegs) {
+        if (lane == 0) s_tiles[0].row0 = s0 + stop;
+      } else if (lane == 0) {
+        s_tiles[0].row0 = n_segs;
+      }
+      if (lane == 0) s_tiles[0].row1 = kind;
     }
     __syncthreads();
     n = uni(s_tiles[0].k0);
-    more = uni((int)s_tiles[0].m);
+    const int next = uni(s_tiles[0].row0), kind = uni(s_tiles[0].row1);
     __syncthreads();
     if (n > 0) {
       fill(0);
       fill(kShList / 2);
       __syncthreads();
-      const int n_first = min(n, kShAhead);
-      for (int j = 0; j < n_first; ++j) issue(j);
-      if (n_first == kShAhead)
-        wait_vmem_n<(kShAhead - 1) * kShCopies>();
-      else
-        wait_vmem();
-      rotate(0);
-      for (int i = 0; i < n;) {
-        const int rows = uni(s_segs[uni(s_tiles[i & (kShList - 1)].flags) >> kTfSeg].rows);
-        i = rows <= kShSmall ? run_small(i) : run_large(i);
+      if (kind) {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        start(std::true_type{}, ln);
+        for (int i = 0; i < n;) i = consume(std::true_type{}, i);
+      } else if (wave < 4) {
+        for (int i = 0; i < n;) i = consume(std::false_type{}, i);
+      } else {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        start(std::false_type{}, ln);
+        for (int i = 0; i < n; ++i) {
+          landed(std::false_type{}, i);
+          __syncthreads();
+          produce(std::false_type{}, ln, i);
+          refill(i);
+        }
       }
     }
-    if (!more) break;
-    __syncthreads();  // the lists and the buffers are free
+    s0 = next;
+    if (s0 < n_segs) __syncthreads();  // the lists and the buffers are free
   }
 }
 
