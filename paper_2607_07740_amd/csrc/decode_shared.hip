@@ -41,7 +41,7 @@ constexpr int kShTile = 32;             // keys of a tile
 constexpr int kShImg = kShTile * kHeadDim * 2;      // K or V of a tile: 8 KB
 constexpr int kShBuf = 2 * kShImg + kShTile * 256;  // and its 32 rows of bf16 (cos, sin)
 constexpr int kShBufs = 6;
-constexpr int kShAhead = kShBufs - 1;  // tiles requested before the first is used
+constexpr int kShAhead = kShBufs - 2;  // tiles requested before the first is used
 constexpr int kShList = 256;           // visits whose addresses are held; refilled by halves
 constexpr int kShSegs = 64;            // segments whose records are held
 constexpr int kShCopies = 3;           // of a wave per tile
@@ -603,9 +603,9 @@ __device__ inline float sh_max16_32(float x) {  // over lanes l, l ^ 16, l ^ 32,
   return sh_max32(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
 }
 
-// Scores may exceed a row's reference by this (log2 units) before it moves: weights
-// stay below 2^16, far inside fp32 and bf16.
-constexpr float kShSlack = 16.f;
+// A tile's weights of a row may add up to this before the row's reference moves: far inside
+// fp32 and bf16.
+constexpr float kShMaxSum = 65536.f;
 
 __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[kShBufs * kShBuf];
@@ -615,8 +615,17 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int h = blockIdx.x % a.Hkv;
-  const int w = blockIdx.x / a.Hkv;
+  // The kv heads of one range run on one XCD (blocks go to the 8 of them in turn): they read
+  // neighbouring pieces of the same pool rows, and the same cos/sin rows.
+  int h, w;
+  if ((a.n_wg & 7) == 0) {
+    const int t = blockIdx.x >> 3, u = t / a.Hkv;
+    h = t - u * a.Hkv;
+    w = 8 * u + (blockIdx.x & 7);
+  } else {
+    w = blockIdx.x / a.Hkv;
+    h = blockIdx.x - w * a.Hkv;
+  }
   const PlanView pv = plan_of(a);
   if (!plan_fits(a, pv.header) || w >= pv.header[kHdWg]) return;
   auto uni = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
@@ -639,35 +648,72 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
 
   // ---- what a wave does of a tile's copies and rotation: with ALL keys 4 wave .. + 3, else
   // the last four waves take 8 each
-  auto uni_tile = [&](int j) __attribute__((always_inline)) {
-    const Tile& s = s_tiles[j & (kShList - 1)];
-    return Tile{uni(s.row0), uni(s.row1), uni(s.k0), uni(s.flags), uni(s.f0), uni(s.km),
-                (uint32_t)uni((int)s.m), (uint32_t)uni((int)s.lG)};
+  // Per lane and copy of 4 keys: byte offsets of its piece of K, V and the cos/sin rows inside a
+  // whole tile
+  struct Piece {
+    uint32_t k, v, cs;
+  };
+  auto piece_of = [&](int ln, int key0) {
+    const int slot = ln & 15, key = key0 + (ln >> 4);
+    const uint32_t ro = (uint32_t)(key & 15) * kv_row_bytes;
+    return Piece{ro + 16 * (slot ^ sh_kswz(key)), ro + 16 * (slot ^ sh_vswz(key)),
+                 (uint32_t)(256 * key + 16 * slot)};
   };
   // requests keys key0 .. key0 + 3 of K and V, and their cos/sin rows
-  auto copy4 = [&](const Tile& t, int ln, int key0, uint32_t buf) __attribute__((always_inline)) {
-    const int klim = t.flags & 31, slot = ln & 15;
-    const int mine = key0 + (ln >> 4), key = min(mine, klim);
-    const size_t off = (size_t)(uint32_t)(min(key0, klim) < 16 ? t.row0 : t.row1) * kv_row_bytes;
-    const uint32_t ro = (uint32_t)(key & 15) * kv_row_bytes;
+  auto copy4 = [&](auto all, const Tile& t, int ln, int key0, const Piece& pc, uint32_t buf) __attribute__((always_inline)) {
+    const int klim = t.flags & 31;
     const uint32_t dst = buf + 256 * key0;
-    dma16_s(kbase + off, ro + 16 * (slot ^ sh_kswz(mine)), dst);
-    dma16_s(vbase + off, ro + 16 * (slot ^ sh_vswz(mine)), dst + kShImg);
-    int pos = t.k0 + key;
+    uint32_t ko = pc.k, vo = pc.v, co = pc.cs;
+    int row = key0 < 16 ? t.row0 : t.row1;
+    int key = key0 + (ln >> 4);
+    if (klim != kShTile - 1) {  // keys behind the last one repeat it
+      const int slot = ln & 15, mine = key;
+      row = min(key0, klim) < 16 ? t.row0 : t.row1;
+      key = min(key, klim);
+      const uint32_t ro = (uint32_t)(key & 15) * kv_row_bytes;
+      ko = ro + 16 * (slot ^ sh_kswz(mine));
+      vo = ro + 16 * (slot ^ sh_vswz(mine));
+      co = 256 * key + 16 * slot;
+    }
+    const size_t off = (size_t)(uint32_t)row * kv_row_bytes;
+    // few rows: their keys are theirs alone, and not kept in the caches (64 chats: 109 -> 97 us
+    // for the copies alone); blocks of many rows mostly share theirs with others
+    if constexpr (decltype(all)::value) {
+      dma16_s(kbase + off, ko, dst);
+      dma16_s(vbase + off, vo, dst + kShImg);
+    } else {
+      dma16_s_nt(kbase + off, ko, dst);
+      dma16_s_nt(vbase + off, vo, dst + kShImg);
+    }
     if (t.lG != 0) {
       const FastDiv f = {t.m, t.lG & 63, 2};
-      pos = t.f0 + (int)fastdiv_ge2((uint32_t)(t.km + key), f);
+      co = fastdiv_ge2((uint32_t)(t.km + key), f) * 256 + 16 * (ln & 15);
     }
-    dma16_s(a.rope16, (uint32_t)pos * 256 + 16 * slot, dst + 2 * kShImg);
+    dma16_s(a.rope16 + (size_t)(t.lG != 0 ? t.f0 : t.k0) * 64, co, dst + 2 * kShImg);
   };
-  auto issue = [&](auto all, int ln, int j) __attribute__((always_inline)) {
-    const Tile t = uni_tile(j);
+  // The copies of a wave, in the order of the list; a visit's description is read one ahead
+  struct Copier {
+    Piece pc[2];
+    Tile nx;
+  };
+  auto peek = [&](Copier& c, int j) __attribute__((always_inline)) { c.nx = s_tiles[j & (kShList - 1)]; };
+  auto copier = [&](auto all, int ln) __attribute__((always_inline)) {
+    Copier c;
+    c.pc[0] = piece_of(ln, decltype(all)::value ? 4 * wave : 8 * (wave - 4));
+    c.pc[1] = piece_of(ln, decltype(all)::value ? 4 * wave : 8 * (wave - 4) + 4);
+    peek(c, 0);
+    return c;
+  };
+  auto issue = [&](auto all, Copier& c, int ln, int j) __attribute__((always_inline)) {
+    const Tile t = {uni(c.nx.row0), uni(c.nx.row1), uni(c.nx.k0), uni(c.nx.flags), uni(c.nx.f0),
+                    uni(c.nx.km), (uint32_t)uni((int)c.nx.m), (uint32_t)uni((int)c.nx.lG)};
+    peek(c, j + 1);
     const uint32_t buf = smem_base + (uint32_t)(j % kShBufs) * kShBuf;
     if constexpr (decltype(all)::value) {
-      copy4(t, ln, 4 * wave, buf);
+      copy4(all, t, ln, 4 * wave, c.pc[0], buf);
     } else {
-      copy4(t, ln, 8 * (wave - 4), buf);
-      copy4(t, ln, 8 * (wave - 4) + 4, buf);
+      copy4(all, t, ln, 8 * (wave - 4), c.pc[0], buf);
+      copy4(all, t, ln, 8 * (wave - 4) + 4, c.pc[1], buf);
     }
   };
   // Rotation in place.  4 keys: lane -> key, half of a chunk pair; 8 keys: lane -> key, chunk pair
@@ -746,31 +792,29 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     s_tiles[j & (kShList - 1)] = s;
   };
 
-  // A wave's copies of tile i + 1 have landed; those of the next three may fly
+  // A wave's copies of tile i + 1 have landed; those of the next two may fly
   auto landed = [&](auto all, int i) __attribute__((always_inline)) {
     constexpr int k = decltype(all)::value ? kShCopies : 2 * kShCopies;
-    if (i + 4 < n)
-      wait_vmem_n<3 * k>();
-    else if (i + 3 < n)
+    if (i + 3 < n)
       wait_vmem_n<2 * k>();
     else if (i + 2 < n)
       wait_vmem_n<k>();
     else
       wait_vmem();
   };
-  // Beside visit i: the request of the tile that takes visit i - 1's buffer, the next one's
+  // Beside visit i: the request of the tile that takes visit i - 2's buffer, the next one's
   // rotation
-  auto produce = [&](auto all, int ln, int i) __attribute__((always_inline)) {
-    if (i + kShAhead < n) issue(all, ln, i + kShAhead);
+  auto produce = [&](auto all, Copier& cp, int ln, int i) __attribute__((always_inline)) {
+    if (i + kShAhead < n) issue(all, cp, ln, i + kShAhead);
     if (i + 1 < n) rotate(all, ln, i + 1);
   };
   auto refill = [&](int i) __attribute__((always_inline)) {
     if ((i & (kShList / 2 - 1)) == 0 && i > 0 && i + kShList / 2 < n) fill(i + kShList / 2);
   };
-  auto start = [&](auto all, int ln) __attribute__((always_inline)) {
+  auto start = [&](auto all, Copier& cp, int ln) __attribute__((always_inline)) {
     constexpr int k = decltype(all)::value ? kShCopies : 2 * kShCopies;
     const int first = min(n, kShAhead);
-    for (int j = 0; j < first; ++j) issue(all, ln, j);
+    for (int j = 0; j < first; ++j) issue(all, cp, ln, j);
     if (first == kShAhead)
       wait_vmem_n<(kShAhead - 1) * k>();
     else
@@ -810,8 +854,9 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
   };
 
   // ---- the visits of a segment from i on, by the waves that hold its rows: 32 of them and all
-  // keys of a tile each
-  auto consume = [&](auto all, int i) __attribute__((always_inline)) {
+  // keys of a tile each.  The scores of visit i are formed beside the softmax and the value
+  // product of visit i - 1, whose tile stays in its buffer until then.
+  auto consume = [&](auto all, Copier& cp, int i) __attribute__((always_inline)) {
     int ln = lane;  // what follows from it is formed here: held across all loops it would spill
     asm volatile("" : "+v"(ln));
     const Segment& sg = s_segs[uni(s_tiles[i & (kShList - 1)].flags) >> kTfSeg];
@@ -823,120 +868,162 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     const bool on = 32 * wave < rows;
     const Row x = row_of(sg, row);
     bf16x8 qop[8];
-    f32x16 acc[4];
+    f32x16 acc[4], sc = f32x16{}, nx_sc = f32x16{}, neg_m = f32x16{};
     float m_ref = 0.f, l_run = 0.f;
 #pragma unroll
     for (int d = 0; d < 4; ++d) acc[d] = f32x16{};
 #pragma unroll
     for (int s = 0; s < 8; ++s) qop[s] = bf16x8{};
     int q_view = -1;
-    for (;; ++i) {
+
+    // the visit's scalars, read a visit ahead
+    int nx_flags = s_tiles[i & (kShList - 1)].flags, nx_k0 = s_tiles[i & (kShList - 1)].k0;
+    uint32_t nx_lG = s_tiles[i & (kShList - 1)].lG;
+    int flags, k0, view_G;
+    auto enter = [&]() __attribute__((always_inline)) {
       if constexpr (decltype(all)::value) landed(all, i);
-      const Tile& tl = s_tiles[i & (kShList - 1)];
-      const int flags = uni(tl.flags), k0 = uni(tl.k0), view_G = uni((int)tl.lG) >> 6;
-      __syncthreads();  // tile i is rotated, tile i - 1 used by all
+      flags = uni(nx_flags);
+      k0 = uni(nx_k0);
+      view_G = uni((int)nx_lG) >> 6;
+      __syncthreads();  // tile i is rotated, tile i - 2 used by all
+      const Tile& t = s_tiles[(i + 1) & (kShList - 1)];
+      nx_flags = t.flags;
+      nx_k0 = t.k0;
+      nx_lG = t.lG;
       if constexpr (decltype(all)::value) {
-        produce(all, ln, i);
+        produce(all, cp, ln, i);
         refill(i);
       }
-      if (on) {
-        if ((view_G > 0) != q_view) {
-          q_view = view_G > 0;
-          const int pos = view_G > 0 ? x.pos / x.G : x.pos;
+      if (on && (view_G > 0) != q_view) {
+        q_view = view_G > 0;
+        const int pos = view_G > 0 ? x.pos / x.G : x.pos;
 #pragma unroll
-          for (int s = 0; s < 4; ++s)
-            sh_rotate_q(x.q, 16 * s + 8 * hl32, a.rope, pos, a.q_scale, qop[s], qop[s + 4]);
+        for (int s = 0; s < 4; ++s)
+          sh_rotate_q(x.q, 16 * s + 8 * hl32, a.rope, pos, a.q_scale, qop[s], qop[s + 4]);
+      }
+    };
+    // S^T = K Q^T - m of visit i
+    auto scores = [&]() __attribute__((always_inline)) {
+      const unsigned char* kb = smem + (i % kShBufs) * kShBuf;
+      bf16x8 ring[4];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) ring[s] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * s + hl32));
+      if constexpr (decltype(all)::value) {  // -m takes no registers between visits
+#pragma unroll
+        for (int e = 0; e < 16; ++e) nx_sc[e] = -m_ref;
+      } else {
+        nx_sc = neg_m;
+      }
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        nx_sc = mfma32(ring[s & 3], qop[s], nx_sc);
+        if (s + 4 < 8) ring[s & 3] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * (s + 4) + hl32));
+      }
+    };
+    // Scores of a visit at key c0 in view cG, masked
+    bool has = false;  // whether the row has a key in that tile
+    auto mask = [&](int c0, int cG) __attribute__((always_inline)) {
+      sc = nx_sc;
+      int lo, hi;
+      keep(x, cG, c0, kend, &lo, &hi);
+      has = lo < min(hi, kShTile);
+      if (__ballot(lo > 0 || hi < kShTile) != 0) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int t = 8 * (e >> 2) + (e & 3) + 4 * hl32;
+          sc[e] = t >= lo && t < hi ? sc[e] : -INFINITY;
         }
-        const unsigned char* kb = smem + (i % kShBufs) * kShBuf;
-        const unsigned char* vb = kb + kShImg;
-        // S^T = K Q^T - m
-        f32x16 sc;
+      }
+    };
+    bf16x8 pb[2];
+    // The weights and their sum over both lanes of a row
+    auto weights = [&]() __attribute__((always_inline)) {
+      float ps0 = 0.f, ps1 = 0.f;
+      const sh_bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sc[e] = -m_ref;
-        {
-          constexpr int kRing = decltype(all)::value ? 4 : 8;
-          bf16x8 ring[kRing];
+      for (int q = 0; q < 2; ++q) {
+        float p[8];
 #pragma unroll
-          for (int s = 0; s < kRing; ++s) ring[s] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * s + hl32));
-          if constexpr (decltype(all)::value) {
+        for (int t = 0; t < 8; ++t) p[t] = fast_exp2(sc[8 * q + t]);
+        pb[q] = pack8(p);
 #pragma unroll
-            for (int s = 0; s < 8; ++s) {
-              sc = mfma32(ring[s & 3], qop[s], sc);
-              if (s + 4 < 8) ring[s & 3] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * (s + 4) + hl32));
-            }
-          } else {  // alone on its SIMD's matrix core: two chains
-            f32x16 odd = f32x16{};
-#pragma unroll
-            for (int s = 0; s < 8; s += 2) {
-              sc = mfma32(ring[s], qop[s], sc);
-              odd = mfma32(ring[s + 1], qop[s + 1], odd);
-            }
-            sc += odd;
-          }
+        for (int u = 0; u < 4; ++u) {
+          const sh_bf16x2 pr = {pb[q][2 * u], pb[q][2 * u + 1]};
+          if (u & 1)
+            ps1 = __builtin_amdgcn_fdot2_f32_bf16(pr, one, ps1, false);
+          else
+            ps0 = __builtin_amdgcn_fdot2_f32_bf16(pr, one, ps0, false);
         }
-        auto vop = [&](int m) __attribute__((always_inline)) {
-          const unsigned char* p =
-              vb + 4096 * (m >> 2) + sh_voff(vk_lane, 4 * (m & 3) + vc_lane) + 8 * (ln & 1);
-          return concat_tr(lds_read_tr4(p), lds_read_tr4(p + 2048));
-        };
-        bf16x8 vr[4];
-#pragma unroll
-        for (int m = 0; m < 4; ++m) vr[m] = vop(m);
-        int lo, hi;
-        keep(x, view_G, k0, kend, &lo, &hi);
-        if (__ballot(lo > 0 || hi < kShTile) != 0) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int t = 8 * (e >> 2) + (e & 3) + 4 * hl32;
-            sc[e] = t >= lo && t < hi ? sc[e] : -INFINITY;
-          }
-        }
+      }
+      const float ps = ps0 + ps1;
+      const sh_u32x2 both =
+          __builtin_amdgcn_permlane32_swap(__float_as_uint(ps), __float_as_uint(ps), false, false);
+      return __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    };
+    // The row's reference follows its first keys, and scores far above it: noticed by the sum of the
+    // weights, which are then formed again (and the next visit's scores, which were taken
+    // against the old reference, moved)
+    auto settle = [&](float ps, bool next) __attribute__((always_inline)) {
+      const bool bad = !(ps <= kShMaxSum) || (l_run == 0.f && has && ps < 1.f);
+      if (__ballot(bad) != 0) {
         float mt = fmaxf(sc[0], sc[1]);
 #pragma unroll
         for (int e = 2; e < 16; e += 2) mt = fmaxf(mt, fmaxf(sc[e], sc[e + 1]));
         mt = sh_max32(mt);
-        // the reference follows the first keys of a row, and scores far above it.  l_run is
-        // the row's whole sum in both of its lanes.
-        const bool upd = mt != -INFINITY && (mt > kShSlack || l_run == 0.f);
-        if (__ballot(upd) != 0) {
-          const float shift = upd ? mt : 0.f;
-          const float alpha = l_run == 0.f ? 1.f : fast_exp2(-shift);
+        const float shift = bad && mt != -INFINITY ? mt : 0.f;
+        const float alpha = l_run == 0.f ? 1.f : fast_exp2(-shift);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sc[e] -= shift;
+        for (int e = 0; e < 16; ++e) sc[e] -= shift;
+        if (next) {
 #pragma unroll
-          for (int d = 0; d < 4; ++d) acc[d] *= alpha;
-          l_run *= alpha;
-          m_ref += shift;
+          for (int e = 0; e < 16; ++e) nx_sc[e] -= shift;
         }
-        bf16x8 pb[2];
-        float ps0 = 0.f, ps1 = 0.f;
-        const sh_bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          float p[8];
+        for (int d = 0; d < 4; ++d) acc[d] *= alpha;
+        l_run *= alpha;
+        m_ref += shift;
 #pragma unroll
-          for (int t = 0; t < 8; ++t) p[t] = fast_exp2(sc[8 * q + t]);
-          pb[q] = pack8(p);
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const sh_bf16x2 pr = {pb[q][2 * u], pb[q][2 * u + 1]};
-            if (u & 1)
-              ps1 = __builtin_amdgcn_fdot2_f32_bf16(pr, one, ps1, false);
-            else
-              ps0 = __builtin_amdgcn_fdot2_f32_bf16(pr, one, ps0, false);
-          }
-        }
-        const float ps = ps0 + ps1;
-        const sh_u32x2 both =
-            __builtin_amdgcn_permlane32_swap(__float_as_uint(ps), __float_as_uint(ps), false, false);
-        l_run += __uint_as_float(both[0]) + __uint_as_float(both[1]);
-#pragma unroll
-        for (int m = 0; m < 8; ++m) {
-          acc[m & 3] = mfma32(vr[m & 3], pb[m >> 2], acc[m & 3]);
-          if (m + 4 < 8) vr[m & 3] = vop(m + 4);
-        }
+        for (int e = 0; e < 16; ++e) neg_m[e] = -m_ref;
+        ps = weights();
       }
-      if (flags & kTfLast) break;
+      l_run += ps;
+    };
+    auto values = [&](int j) __attribute__((always_inline)) {  // value product of visit j
+      const unsigned char* vb = smem + (j % kShBufs) * kShBuf + kShImg;
+      auto vop = [&](int m) __attribute__((always_inline)) {
+        const unsigned char* p =
+            vb + 4096 * (m >> 2) + sh_voff(vk_lane, 4 * (m & 3) + vc_lane) + 8 * (ln & 1);
+        return concat_tr(lds_read_tr4(p), lds_read_tr4(p + 2048));
+      };
+      bf16x8 vr[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) vr[m] = vop(m);
+#pragma unroll
+      for (int m = 0; m < 8; ++m) {
+        acc[m & 3] = mfma32(vr[m & 3], pb[m >> 2], acc[m & 3]);
+        if (m + 4 < 8) vr[m & 3] = vop(m + 4);
+      }
+    };
+
+    enter();
+    if (on) scores();
+    while ((flags & kTfLast) == 0) {
+      const int c0 = k0, cG = view_G;
+      ++i;
+      enter();
+      if (on) {
+        mask(c0, cG);
+        scores();
+        const float ps = weights();
+        settle(ps, true);
+        values(i - 1);
+      }
+    }
+    if (on) {
+      mask(k0, view_G);
+      const float ps = weights();
+      settle(ps, false);
+      values(i);
     }
     if (row < rows) {
       if (sg.len > 0 && sg.n_w == 1) {  // a chunk's block that is whole here
@@ -1033,18 +1120,21 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       if (kind) {
         int ln = lane;
         asm volatile("" : "+v"(ln));
-        start(std::true_type{}, ln);
-        for (int i = 0; i < n;) i = consume(std::true_type{}, i);
+        Copier cp = copier(std::true_type{}, ln);
+        start(std::true_type{}, cp, ln);
+        for (int i = 0; i < n;) i = consume(std::true_type{}, cp, i);
       } else if (wave < 4) {
-        for (int i = 0; i < n;) i = consume(std::false_type{}, i);
+        Copier none;
+        for (int i = 0; i < n;) i = consume(std::false_type{}, none, i);
       } else {
         int ln = lane;
         asm volatile("" : "+v"(ln));
-        start(std::false_type{}, ln);
+        Copier cp = copier(std::false_type{}, ln);
+        start(std::false_type{}, cp, ln);
         for (int i = 0; i < n; ++i) {
           landed(std::false_type{}, i);
           __syncthreads();
-          produce(std::false_type{}, ln, i);
+          produce(std::false_type{}, cp, ln, i);
           refill(i);
         }
       }
