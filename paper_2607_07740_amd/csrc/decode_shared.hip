@@ -36,7 +36,8 @@ namespace jl {
 
 constexpr int kShThreads = 512, kShWaves = 8;
 constexpr int kShRows = 32 * kShWaves;  // rows of a segment at most
-constexpr int kShSmall = kShRows / 2;   // rows of a segment whose keys two waves share
+constexpr int kShSmall = kShRows / 2;   // rows that four waves hold, while the others copy and rotate
+constexpr int kShFew = kShRows / 4;     // rows that two waves hold: two pairs take the visits in turn
 constexpr int kShTile = 32;             // keys of a tile
 constexpr int kShImg = kShTile * kHeadDim * 2;      // K or V of a tile: 8 KB
 constexpr int kShBuf = 2 * kShImg + kShTile * 256;  // and its 32 rows of bf16 (cos, sin)
@@ -56,11 +57,13 @@ constexpr int kMaxStep = kVisitCost + 2 + kSegCost;  // most between two visits 
 struct Segment {
   int m0, rows, kend, seq;        // first member, rows, end of its keys, whose table row names its pages
   int k0, n_views, n_rem, loc0;   // first key; remote tiles and views of each; first tile with local keys
-  int visits, view0, len, pad;    // view0: its views' place; len: its rows' length for G, 0: each its own
+  int visits, view0, len, kind;   // view0: its views' place; len: its rows' length for G, 0: each its own
   uint32_t start_lo, start_hi;    // cost before it
   int w_first, n_w;               // workgroups that hold some of its visits
   int row0, pad2[3];              // state rows before it
 };
+// Whose rows a segment has: several sequences, one, or consecutive tokens of one
+enum { kSegShared = 0, kSegOwn = 1, kSegChunk = 2 };
 struct View {
   int G;
   uint32_t m, l;  // division by G
@@ -73,7 +76,9 @@ struct Member {
   int pre, suf;  // its segments, -1: none
 };
 // States that a (workgroup, segment) leaves
-__host__ __device__ inline int state_halves(int) { return 1; }
+__host__ __device__ inline int state_halves(int rows, int n_views) {
+  return rows <= kShFew && n_views > 1 ? 2 : 1;
+}
 
 struct PlanView {
   int* header;
@@ -234,9 +239,10 @@ __device__ inline Ranges ranges_of(unsigned long long total, int n_wg) {
 }
 
 // The end of both plans: costs before each segment, the workgroups' ranges, and the places of
-// the states.  s_visits, s_rows: visits and rows of n_segs segments; a thread takes a run of them.
+// the states.  s_visits, s_rows, s_states: visits, rows and rows of states of n_segs segments; a
+// thread takes a run of them.
 __device__ inline void plan_ranges(const SharedPlanArgs& a, const PlanView& v, int n_segs,
-                                   const int* s_visits, const short* s_rows,
+                                   const int* s_visits, const short* s_rows, const short* s_states,
                                    unsigned long long* s_scan) {
   const int tid = threadIdx.x;
   const int per = (n_segs + kPlThreads - 1) / kPlThreads;
@@ -258,7 +264,7 @@ __device__ inline void plan_ranges(const SharedPlanArgs& a, const PlanView& v, i
     const unsigned long long c = cost(i);
     if (c == 0) continue;
     const int w0 = rg.owner(st + kSegCost), w1 = rg.owner(st + c - visit_cost(s_rows[i]));
-    rows += (unsigned long long)(w1 - w0 + 1) * s_rows[i] * state_halves(s_rows[i]);
+    rows += (unsigned long long)(w1 - w0 + 1) * s_states[i];
     int w = rg.owner(st);  // workgroups whose ranges begin inside this segment
     if (rg.begin(w) < st) ++w;
     for (; w < n_wg && rg.begin(w) < st + c; ++w) v.wg_first[w] = i;
@@ -281,7 +287,7 @@ __device__ inline void plan_ranges(const SharedPlanArgs& a, const PlanView& v, i
     s.w_first = w0;
     s.n_w = w1 - w0 + 1;
     s.row0 = (int)row;
-    row += (unsigned long long)(w1 - w0 + 1) * s_rows[i] * state_halves(s_rows[i]);
+    row += (unsigned long long)(w1 - w0 + 1) * s_states[i];
     st += c;
   }
   if (tid == 0) {
@@ -316,6 +322,7 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
   int* const s_blk = s_pre + a.n_groups;       // [n_groups + 1]: prefix blocks before the group
   int* const s_visits = s_blk + a.n_groups + 1;
   short* const s_rows = (short*)(s_visits + z.segs);
+  short* const s_states = s_rows + z.segs;
   const int cap = a.max_pages * a.page;
   const int per_block = kShRows / a.g;
 
@@ -410,6 +417,7 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
       v.segs[blk] = s;
       s_visits[blk] = s.visits;
       s_rows[blk] = (short)s.rows;
+      s_states[blk] = (short)(s.rows * state_halves(s.rows, s.n_views));
     }
   }
   // the members' own keys
@@ -420,6 +428,7 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
     if (gi >= 0 && len > 0) {
       const int P = s_pre[gi], G = plan_group(a, len), lim = first_local(G, len - 1, a.w0);
       s.m0 = i;
+      s.kind = kSegOwn;
       s.rows = a.g;
       s.k0 = P;
       s.kend = len;
@@ -434,9 +443,10 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
     v.segs[seg] = s;
     s_visits[seg] = s.visits;
     s_rows[seg] = (short)s.rows;
+    s_states[seg] = (short)(s.rows * state_halves(s.rows, s.n_views));
   }
   __syncthreads();
-  plan_ranges(a, v, n_blocks + a.B, s_visits, s_rows, s_scan);
+  plan_ranges(a, v, n_blocks + a.B, s_visits, s_rows, s_states, s_scan);
 }
 
 // The plan of packed chunks: sequence b's rows are cu[b] .. cu[b + 1] - 1 of the packed ones,
@@ -454,6 +464,7 @@ __global__ __launch_bounds__(kPlThreads) void chunk_plan_kernel(SharedPlanArgs a
   int* const s_blk = s_len + a.B;           // [B + 1]: blocks before the sequence
   int* const s_visits = s_blk + a.B + 1;
   short* const s_rows = (short*)(s_visits + z.segs);
+  short* const s_states = s_rows + z.segs;
   const int cap = a.max_pages * a.page;
   const int per_block = kShRows / a.g;
   bool bad = false;
@@ -496,11 +507,13 @@ __global__ __launch_bounds__(kPlThreads) void chunk_plan_kernel(SharedPlanArgs a
     s.seq = b;
     s.view0 = seg;
     s.len = max(len, 1);
+    s.kind = kSegChunk;
     set_visits(s, first_local(G, p0, a.w0), first_local(G, p1, a.w0), G > 1 ? 1 : 0);
     if (G > 1) v.views[seg] = view_of(G);
     v.segs[seg] = s;
     s_visits[seg] = s.visits;
     s_rows[seg] = (short)s.rows;
+    s_states[seg] = (short)(s.rows * state_halves(s.rows, s.n_views));
   }
   for (int t = tid; t < a.T; t += kPlThreads) {
     int b = 0, hi = a.B;  // the first sequence whose end lies behind the token
@@ -516,7 +529,7 @@ __global__ __launch_bounds__(kPlThreads) void chunk_plan_kernel(SharedPlanArgs a
     v.members[t] = m;
   }
   __syncthreads();
-  plan_ranges(a, v, n_segs, s_visits, s_rows, s_scan);
+  plan_ranges(a, v, n_segs, s_visits, s_rows, s_states, s_scan);
 }
 
 // --------------------------------------------------------------- attention
@@ -753,7 +766,9 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
   int n = 0;  // visits of the held segments
   // Addresses of visits j0 .. j0 + 127, by the last two waves
   auto fill = [&](int j0) __attribute__((always_inline)) {
-    const int at = tid - (kShThreads - kShList / 2), j = j0 + at;
+    int me = tid;
+    asm volatile("" : "+v"(me));  // as above: nothing of this is held in between
+    const int at = me - (kShThreads - kShList / 2), j = j0 + at;
     if (at < 0 || j >= n) return;
     int i = 0;  // the held segment: the last that begins at or before the visit
 #pragma unroll
@@ -830,11 +845,23 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
   auto row_of = [&](const Segment& sg, int r) {
     Row x;
     r = min(r, sg.rows - 1);
-    const Member mb = pv.members[sg.m0 + r / a.g];
-    x.pos = max(mb.len - 1, 0);
-    x.G = a.bifocal ? group_size(sg.len > 0 ? sg.len : mb.len, a.w_pre) : 1;
+    const int t = r / a.g;
+    int seq, len;
+    if (sg.kind == kSegShared) {
+      const Member mb = pv.members[sg.m0 + t];
+      seq = mb.seq;
+      len = mb.len;
+    } else if (sg.kind == kSegOwn) {
+      seq = sg.seq;
+      len = sg.kend;
+    } else {  // the last row's position is kend - 1
+      seq = sg.m0 + t;
+      len = sg.kend - (sg.rows / a.g - 1 - t);
+    }
+    x.pos = max(len - 1, 0);
+    x.G = a.bifocal ? group_size(sg.len > 0 ? sg.len : len, a.w_pre) : 1;
     x.lim = first_local(x.G, x.pos, a.w0);
-    x.q = a.q + ((size_t)max(mb.seq, 0) * a.Hq + h * a.g + r % a.g) * kHeadDim;
+    x.q = a.q + ((size_t)max(seq, 0) * a.Hq + h * a.g + r % a.g) * kHeadDim;
     return x;
   };
   // Keys [lo, hi) of the tile that a row keeps: in the remote view those before its first
@@ -848,7 +875,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       *lo = x.lim - k0;
   };
   auto state_at = [&](const Segment& sg, int half) {
-    const int rows = uni(sg.rows), halves = state_halves(rows);
+    const int rows = uni(sg.rows), halves = state_halves(rows, uni(sg.n_views));
     return a.states + ((size_t)h * all_rows + uni(sg.row0) +
                        (size_t)((w - uni(sg.w_first)) * halves + half) * rows) * kShStateFloats;
   };
@@ -856,7 +883,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
   // ---- the visits of a segment from i on, by the waves that hold its rows: 32 of them and all
   // keys of a tile each.  The scores of visit i are formed beside the softmax and the value
   // product of visit i - 1, whose tile stays in its buffer until then.
-  auto consume = [&](auto all, Copier& cp, int i) __attribute__((always_inline)) {
+  auto consume = [&](auto all, auto few, Copier& cp, int i) __attribute__((always_inline)) {
     int ln = lane;  // what follows from it is formed here: held across all loops it would spill
     asm volatile("" : "+v"(ln));
     const Segment& sg = s_segs[uni(s_tiles[i & (kShList - 1)].flags) >> kTfSeg];
@@ -864,11 +891,13 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     const int hl32 = ln >> 5, kr_lane = ln & 31;
     const int vk_lane = 4 * hl32 + ((ln & 15) >> 2);
     const int vc_lane = 2 * ((ln >> 4) & 1) + ((ln & 3) >> 1);
-    const int row = 32 * wave + kr_lane;
-    const bool on = 32 * wave < rows;
+    constexpr bool ALL = decltype(all)::value, FEW = decltype(few)::value;
+    const int rw = FEW ? wave & 1 : wave, set = wave >> 1;
+    const int row = 32 * rw + kr_lane;
+    const bool on = 32 * rw < rows;
     const Row x = row_of(sg, row);
     bf16x8 qop[8];
-    f32x16 acc[4], sc = f32x16{}, nx_sc = f32x16{}, neg_m = f32x16{};
+    f32x16 acc[4], nx_sc = f32x16{}, neg_m = f32x16{};
     float m_ref = 0.f, l_run = 0.f;
 #pragma unroll
     for (int d = 0; d < 4; ++d) acc[d] = f32x16{};
@@ -894,7 +923,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
         produce(all, cp, ln, i);
         refill(i);
       }
-      if (on && (view_G > 0) != q_view) {
+      if (on && (view_G > 0) != q_view && (!FEW || (i & 1) == set)) {
         q_view = view_G > 0;
         const int pos = view_G > 0 ? x.pos / x.G : x.pos;
 #pragma unroll
@@ -902,13 +931,18 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
           sh_rotate_q(x.q, 16 * s + 8 * hl32, a.rope, pos, a.q_scale, qop[s], qop[s + 4]);
       }
     };
-    // S^T = K Q^T - m of visit i
-    auto scores = [&]() __attribute__((always_inline)) {
-      const unsigned char* kb = smem + (i % kShBufs) * kShBuf;
-      bf16x8 ring[4];
+    // S^T = K Q^T - m of visit i: its key operands are requested ahead, then multiplied
+    constexpr int kKr = ALL ? 4 : 8;
+    bf16x8 kr[kKr];
+    auto kop = [&](int s) __attribute__((always_inline)) {
+      return *(const bf16x8*)(smem + (i % kShBufs) * kShBuf + sh_koff(kr_lane, 2 * s + hl32));
+    };
+    auto keys = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int s = 0; s < 4; ++s) ring[s] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * s + hl32));
-      if constexpr (decltype(all)::value) {  // -m takes no registers between visits
+      for (int s = 0; s < kKr; ++s) kr[s] = kop(s);
+    };
+    auto scores = [&]() __attribute__((always_inline)) {
+      if constexpr (!FEW) {  // -m takes no registers between visits
 #pragma unroll
         for (int e = 0; e < 16; ++e) nx_sc[e] = -m_ref;
       } else {
@@ -916,14 +950,13 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       }
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
-        nx_sc = mfma32(ring[s & 3], qop[s], nx_sc);
-        if (s + 4 < 8) ring[s & 3] = *(const bf16x8*)(kb + sh_koff(kr_lane, 2 * (s + 4) + hl32));
+        nx_sc = mfma32(kr[s & (kKr - 1)], qop[s], nx_sc);
+        if (s + kKr < 8) kr[s & (kKr - 1)] = kop(s + kKr);
       }
     };
     // Scores of a visit at key c0 in view cG, masked
     bool has = false;  // whether the row has a key in that tile
-    auto mask = [&](int c0, int cG) __attribute__((always_inline)) {
-      sc = nx_sc;
+    auto mask = [&](f32x16& sc, int c0, int cG) __attribute__((always_inline)) {
       int lo, hi;
       keep(x, cG, c0, kend, &lo, &hi);
       has = lo < min(hi, kShTile);
@@ -937,7 +970,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     };
     bf16x8 pb[2];
     // The weights and their sum over both lanes of a row
-    auto weights = [&]() __attribute__((always_inline)) {
+    auto weights = [&](const f32x16& sc) __attribute__((always_inline)) {
       float ps0 = 0.f, ps1 = 0.f;
       const sh_bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
@@ -963,7 +996,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     // The row's reference follows its first keys, and scores far above it: noticed by the sum of the
     // weights, which are then formed again (and the next visit's scores, which were taken
     // against the old reference, moved)
-    auto settle = [&](float ps, bool next) __attribute__((always_inline)) {
+    auto settle = [&](f32x16& sc, float ps, bool next) __attribute__((always_inline)) {
       const bool bad = !(ps <= kShMaxSum) || (l_run == 0.f && has && ps < 1.f);
       if (__ballot(bad) != 0) {
         float mt = fmaxf(sc[0], sc[1]);
@@ -982,51 +1015,101 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
         for (int d = 0; d < 4; ++d) acc[d] *= alpha;
         l_run *= alpha;
         m_ref += shift;
+        if constexpr (FEW) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) neg_m[e] = -m_ref;
-        ps = weights();
+          for (int e = 0; e < 16; ++e) neg_m[e] = -m_ref;
+        }
+        ps = weights(sc);
       }
       l_run += ps;
     };
-    auto values = [&](int j) __attribute__((always_inline)) {  // value product of visit j
-      const unsigned char* vb = smem + (j % kShBufs) * kShBuf + kShImg;
-      auto vop = [&](int m) __attribute__((always_inline)) {
-        const unsigned char* p =
-            vb + 4096 * (m >> 2) + sh_voff(vk_lane, 4 * (m & 3) + vc_lane) + 8 * (ln & 1);
-        return concat_tr(lds_read_tr4(p), lds_read_tr4(p + 2048));
-      };
-      bf16x8 vr[4];
+    // Value operand m of visit j, and the product: the first of them requested ahead
+    constexpr int kVr = FEW ? 8 : 4;
+    bf16x8 vr[kVr];
+    auto vop = [&](int j, int m) __attribute__((always_inline)) {
+      const unsigned char* p = smem + (j % kShBufs) * kShBuf + kShImg + 4096 * (m >> 2) +
+                               sh_voff(vk_lane, 4 * (m & 3) + vc_lane) + 8 * (ln & 1);
+      return concat_tr(lds_read_tr4(p), lds_read_tr4(p + 2048));
+    };
+    auto tile_values = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-      for (int m = 0; m < 4; ++m) vr[m] = vop(m);
+      for (int m = 0; m < kVr; ++m) vr[m] = vop(j, m);
+    };
+    auto values = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
       for (int m = 0; m < 8; ++m) {
-        acc[m & 3] = mfma32(vr[m & 3], pb[m >> 2], acc[m & 3]);
-        if (m + 4 < 8) vr[m & 3] = vop(m + 4);
+        acc[m & 3] = mfma32(vr[m & (kVr - 1)], pb[m >> 2], acc[m & 3]);
+        if (m + kVr < 8) vr[m & (kVr - 1)] = vop(j, m + kVr);
       }
     };
+    auto fence = []() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
 
-    enter();
-    if (on) scores();
-    while ((flags & kTfLast) == 0) {
-      const int c0 = k0, cG = view_G;
-      ++i;
+    if constexpr (FEW) {
+      // A pair's visit takes two barriers' time: its scores, then the softmax and the value product
+      bool last = false;
+      if ((i & 1) != set) {  // begins with the other pair's
+        enter();
+        last = (flags & kTfLast) != 0;
+        if (!last) ++i;
+      }
+      while (!last) {
+        enter();
+        last = (flags & kTfLast) != 0;
+        const int own_i = i, own_k0 = k0, own_G = view_G;
+        if (on) {
+          keys();
+          fence();
+          scores();
+        }
+        if (!last) {
+          ++i;
+          enter();
+          last = (flags & kTfLast) != 0;
+          if (!last) ++i;
+        }
+        if (on) {
+          tile_values(own_i);
+          fence();
+          mask(nx_sc, own_k0, own_G);
+          const float ps = weights(nx_sc);
+          settle(nx_sc, ps, false);
+          values(own_i);
+        }
+      }
+    } else {
       enter();
       if (on) {
-        mask(c0, cG);
+        keys();
+        fence();
         scores();
-        const float ps = weights();
-        settle(ps, true);
-        values(i - 1);
+      }
+      while ((flags & kTfLast) == 0) {
+        const int c0 = k0, cG = view_G;
+        ++i;
+        enter();
+        if (on) {
+          keys();
+          tile_values(i - 1);
+          fence();
+          f32x16 sc = nx_sc;
+          mask(sc, c0, cG);
+          scores();
+          const float ps = weights(sc);
+          settle(sc, ps, true);
+          values(i - 1);
+        }
+      }
+      if (on) {
+        tile_values(i);
+        fence();
+        mask(nx_sc, k0, view_G);
+        const float ps = weights(nx_sc);
+        settle(nx_sc, ps, false);
+        values(i);
       }
     }
-    if (on) {
-      mask(k0, view_G);
-      const float ps = weights();
-      settle(ps, false);
-      values(i);
-    }
     if (row < rows) {
-      if (sg.len > 0 && sg.n_w == 1) {  // a chunk's block that is whole here
+      if (!FEW && sg.len > 0 && sg.n_w == 1) {  // a chunk's block that is whole here
         const Member mb = pv.members[sg.m0 + row / a.g];
         if (mb.seq >= 0) {
           const float inv = 1.f / l_run;
@@ -1046,7 +1129,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
           }
         }
       } else {
-        float* st = state_at(sg, 0);
+        float* st = state_at(sg, FEW ? set : 0);
 #pragma unroll
         for (int db = 0; db < 4; ++db) {
 #pragma unroll
@@ -1068,12 +1151,14 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
   // ---- the segments of the range, up to 64 of one kind at a time
   for (int s0 = uni(pv.wg_first[w]); s0 < n_segs;) {
     if (wave == 0) {
-      const int i = s0 + lane;
+      int ln = lane;
+      asm volatile("" : "+v"(ln));
+      const int i = s0 + ln;
       int va = 0, vb = 0;
       bool past = true, large = false;
       if (i < n_segs) {
         const Segment sg = pv.segs[i];
-        s_segs[lane] = sg;
+        s_segs[ln] = sg;
         const unsigned long long st = sg.start_lo | (unsigned long long)sg.start_hi << 32;
         const uint32_t c = (uint32_t)visit_cost(sg.rows);
         auto below = [&](unsigned long long x) {  // its visits that begin before x
@@ -1092,22 +1177,22 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       const bool kind = some != 0 && (big >> __builtin_ctzll(some) & 1) != 0;
       const unsigned long long other = some & (kind ? ~big : big);
       const int stop = other != 0 ? __builtin_ctzll(other) : kShSegs;
-      if (lane >= stop) vb = va;
+      if (ln >= stop) vb = va;
       int incl = vb - va;
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
         const int y = __shfl_up(incl, d);
-        if (lane >= d) incl += y;
+        if (ln >= d) incl += y;
       }
-      s_from[lane] = va;
-      s_before[lane] = incl - (vb - va);
-      if (lane == 63) s_tiles[0].k0 = incl;
-      if (__ballot(past && lane < stop) == 0 || stop < kShSegs) {
-        if (lane == 0) s_tiles[0].row0 = s0 + stop;
-      } else if (lane == 0) {
+      s_from[ln] = va;
+      s_before[ln] = incl - (vb - va);
+      if (ln == 63) s_tiles[0].k0 = incl;
+      if (__ballot(past && ln < stop) == 0 || stop < kShSegs) {
+        if (ln == 0) s_tiles[0].row0 = s0 + stop;
+      } else if (ln == 0) {
         s_tiles[0].row0 = n_segs;
       }
-      if (lane == 0) s_tiles[0].row1 = kind;
+      if (ln == 0) s_tiles[0].row1 = kind;
     }
     __syncthreads();
     n = uni(s_tiles[0].k0);
@@ -1122,10 +1207,14 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
         asm volatile("" : "+v"(ln));
         Copier cp = copier(std::true_type{}, ln);
         start(std::true_type{}, cp, ln);
-        for (int i = 0; i < n;) i = consume(std::true_type{}, cp, i);
+        for (int i = 0; i < n;) i = consume(std::true_type{}, std::false_type{}, cp, i);
       } else if (wave < 4) {
         Copier none;
-        for (int i = 0; i < n;) i = consume(std::false_type{}, none, i);
+        for (int i = 0; i < n;) {
+          const Segment& sg = s_segs[uni(s_tiles[i & (kShList - 1)].flags) >> kTfSeg];
+          i = state_halves(uni(sg.rows), uni(sg.n_views)) == 2 ? consume(std::false_type{}, std::true_type{}, none, i)
+                             : consume(std::false_type{}, std::false_type{}, none, i);
+        }
       } else {
         int ln = lane;
         asm volatile("" : "+v"(ln));
@@ -1164,7 +1253,7 @@ __global__ __launch_bounds__(512) void merge_shared_kernel(SharedArgs a) {
   auto join = [&](int seg, bool block) {
     if (seg < 0) return;
     const Segment sg = pv.segs[seg];
-    const int n = sg.n_w * state_halves(sg.rows);
+    const int n = sg.n_w * state_halves(sg.rows, sg.n_views);
     if (sg.len > 0 && n == 1) {  // written by its workgroup
       on = false;
       return;
@@ -1232,7 +1321,7 @@ __global__ __launch_bounds__(512) void merge_shared_kernel(SharedArgs a) {
 
 // ---------------------------------------------------------------- launchers
 static size_t chunk_plan_lds(int B, int T, int g) {
-  return (3 * (size_t)B + 2) * sizeof(int) + chunk_sizes(B, T, g).segs * 6 + 8;
+  return (3 * (size_t)B + 2) * sizeof(int) + chunk_sizes(B, T, g).segs * 8 + 8;
 }
 bool chunk_rows_fit(int B, int T, int g) { return chunk_plan_lds(B, T, g) <= 60 * 1024; }
 
@@ -1241,7 +1330,7 @@ static hipError_t launch_plan(bool chunk, SharedPlanArgs& a, hipStream_t stream)
     hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(kPlThreads), chunk_plan_lds(a.B, a.T, a.g), stream, a);
   } else {
     const PlanSizes z = decode_sizes(a.B, a.n_groups, a.g);
-    const size_t lists = z.segs * 6 + 8;
+    const size_t lists = z.segs * 8 + 8;
     const size_t lds = (2 * (size_t)a.B + 3 * (size_t)a.n_groups + 2) * sizeof(int) + lists;
     hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(kPlThreads), lds, stream, a);
   }

@@ -287,3 +287,26 @@ def test_two_plans_on_two_streams():
     torch.cuda.synchronize()
     for i, o in enumerate(outs):
         assert_close(to_f64(o), want[i % 2], what="stream %d" % (i % 2))
+
+
+@pytest.mark.parametrize("B,n", [(2048, 2048), (2048, 1), (1, 2048), (1500, 700)])
+def test_the_largest_batches(B, n):
+    """As many sequences and groups as a plan takes: every sequence of a few tokens, every tenth long."""
+    page, Hkv = 16, 1
+    g = torch.Generator(device="cuda").manual_seed(B + n)
+    starts = np.minimum(np.arange(n + 1) * -(-B // n), B)
+    share = np.full(n, 16)
+    lens = np.where(np.arange(B) % 10 == 0, 90, 20) + np.arange(B) % 5
+    first = starts[np.searchsorted(starts, np.arange(B), side="right") - 1]
+    table = 8 * np.arange(B)[:, None] + np.arange(8)
+    table[:, 0] = 8 * first  # the prefix page is the first one's
+    kp = torch.randn((8 * B, page, Hkv, 128), generator=g, device="cuda").to(torch.bfloat16)
+    vp = torch.randn((8 * B, page, Hkv, 128), generator=g, device="cuda").to(torch.bfloat16)
+    q = torch.randn((B, 2, 128), generator=g, device="cuda").to(torch.bfloat16)
+    say("largest batches", B, n)
+    plan = api.shared_plan(_i32(lens), _i32(starts), _i32(share), Hq=2, Hkv=Hkv, page_size=page,
+                           max_pages=8, w_pretrained=40, w_local=30)
+    out = api.decode_shared(q, kp, vp, _i32(table), plan)
+    ref = api.decode_paged(q, kp, vp, _i32(table), _i32(lens), w_pretrained=40, w_local=30)
+    torch.cuda.synchronize()
+    assert_close(to_f64(out), to_f64(ref), what="largest batches")
