@@ -31,6 +31,7 @@
 
 #include "decode_shared.h"
 #include "jl_device.h"
+#include "prefill_chunks.h"
 
 namespace jl {
 
@@ -119,10 +120,26 @@ __host__ __device__ inline PlanView plan_view(void* p, const PlanSizes& z) {
 static size_t plan_bytes(const PlanSizes& z) {
   return kPlanHead + z.members * sizeof(Member) + z.views * sizeof(View) + z.segs * sizeof(Segment);
 }
+// Parts of the chunks whose blocks the prefill kernel takes, at most: each block rounded up, and
+// kPartWaves times the workgroups of a kv head; of these a block's that is cut at most 4/3 of the
+// latter.
+constexpr int kPartWaves = 3;
+static size_t most_parts(int B, int T, int g, int n_wg) {
+  return 2 * chunk_sizes(B, T, g).segs + (size_t)kPartWaves * n_wg;
+}
+static size_t most_slots(int n_wg) { return (size_t)kPartWaves * n_wg * 4 / 3 + 2; }
+size_t prefill_chunk_state_bytes();
+int prefill_chunk_max_pages();
+hipError_t launch_prefill_chunks(bool bifocal, const uint16_t* q, const uint16_t* k,
+                                 const uint16_t* v, uint16_t* o, float* lse, const float2* table,
+                                 const uint32_t* table16, const int32_t* block_table,
+                                 int max_pages, int page_shift, int n_pages, int T, int Hq, int Hkv,
+                                 int w0, float slack, const ChunkPart* parts, const int* n_parts,
+                                 int max_parts, float* states, hipStream_t stream);
 size_t shared_plan_bytes(int B, int n_groups, int g) { return plan_bytes(decode_sizes(B, n_groups, g)); }
 
 enum { kHdSegs = 0, kHdWg, kHdTotLo, kHdTotHi, kHdRows, kHdB, kHdG, kHdPage, kHdMaxPages, kHdHkv,
-       kHdGroups, kHdBifocal, kHdWPre, kHdW0 };
+       kHdGroups, kHdBifocal, kHdWPre, kHdW0, kHdParts };
 
 // State rows of one kv head: every segment's, for each of its halves, and again where a
 // workgroup's range ends inside it.
@@ -136,12 +153,34 @@ size_t decode_shared_workspace_bytes(int B, int Hq, int Hkv) {
   return (size_t)Hkv * state_rows(2 * (size_t)B * g, B * g, head_workgroups(kShMaxWg, Hkv)) *
          kShStateFloats * sizeof(float);
 }
-// Of a chunk call: plan, then states
-size_t chunk_scratch_bytes(int B, int T, int Hq, int Hkv) {
-  const int g = Hq / Hkv;
-  return (plan_bytes(chunk_sizes(B, T, g)) + 255) / 256 * 256 +
-         (size_t)Hkv * state_rows((size_t)T * g, kShRows, head_workgroups(kShMaxWg, Hkv)) *
-             kShStateFloats * sizeof(float);
+static size_t round256(size_t x) { return (x + 255) / 256 * 256; }
+
+// Whether the blocks of longer chunks go to the prefill kernel, which takes 64 keys of 256 rows in
+// the time of 32 here (rows 512 and 600 of 15000 and 34000 keys, 32/8 heads: 735 -> 452 us with
+// both): where the rows beyond a token per sequence make a few of its blocks, and with what it
+// asks of the cache.  A sequence's go there if they are more than 128.
+static bool chunk_blocks(int B, int T, int g, int max_pages, int page) {
+  return kChunkBlockRows % g == 0 && page >= kChunkTile && max_pages <= prefill_chunk_max_pages() &&
+         ((long long)T - B) * g >= 4 * kChunkBlockRows;
+}
+
+// Scratch of a chunk call: plan, parts, the states of either kernel
+struct ChunkScratch {
+  size_t parts, states, part_states, end;
+};
+static ChunkScratch chunk_scratch(int B, int T, int Hq, int Hkv, int max_pages, int page) {
+  const int g = Hq / Hkv, n_wg = head_workgroups(kShMaxWg, Hkv);
+  const bool blocks = chunk_blocks(B, T, g, max_pages, page);
+  ChunkScratch c;
+  c.parts = round256(plan_bytes(chunk_sizes(B, T, g)));
+  c.states = round256(c.parts + (blocks ? most_parts(B, T, g, n_wg) * sizeof(ChunkPart) : 0));
+  c.part_states = round256(c.states + (size_t)Hkv * state_rows((size_t)T * g, kShRows, n_wg) *
+                                          kShStateFloats * sizeof(float));
+  c.end = c.part_states + (blocks ? most_slots(n_wg) * Hkv * prefill_chunk_state_bytes() : 0);
+  return c;
+}
+size_t chunk_scratch_bytes(int B, int T, int Hq, int Hkv, int max_pages, int page) {
+  return chunk_scratch(B, T, Hq, Hkv, max_pages, page).end;
 }
 
 // ------------------------------------------------------------------- plan
@@ -153,6 +192,7 @@ struct SharedPlanArgs {
   const int32_t* cu;       // chunks: T packed rows
   void* plan;
   int B, n_groups, T, g, Hkv, max_pages, page, n_wg, bifocal, w_pre, w0;
+  ChunkPart* parts;        // chunks: of those whose blocks the prefill kernel takes; nullptr: none
 };
 
 constexpr int kPlThreads = 1024, kPlWaves = kPlThreads / 64;
@@ -462,7 +502,8 @@ __global__ __launch_bounds__(kPlThreads) void chunk_plan_kernel(SharedPlanArgs a
   int* const s_start = s_mem;               // [B + 1]
   int* const s_len = s_start + a.B + 1;     // [B]
   int* const s_blk = s_len + a.B;           // [B + 1]: blocks before the sequence
-  int* const s_visits = s_blk + a.B + 1;
+  int* const s_big = s_blk + a.B + 1;       // [B + 1]: the prefill kernel's blocks before it
+  int* const s_visits = s_big + a.B + 1;
   short* const s_rows = (short*)(s_visits + z.segs);
   short* const s_states = s_rows + z.segs;
   const int cap = a.max_pages * a.page;
@@ -479,17 +520,76 @@ __global__ __launch_bounds__(kPlThreads) void chunk_plan_kernel(SharedPlanArgs a
       for (int i = 1; i <= a.B; ++i) s_start[i] = max(s_start[i], s_start[i - 1]);
     __syncthreads();
   }
-  int n_segs = 0;
+  // blocks of each sequence: of one kind or the other
+  auto is_big = [&](int b) {
+    const int n = s_start[b + 1] - s_start[b];
+    return a.parts != nullptr && n * a.g > kShSmall && s_len[b] >= n;
+  };
+  int n_segs = 0, n_big = 0;
   for (int c0 = 0; c0 < a.B; c0 += kPlThreads) {
     const int i = c0 + tid;
     unsigned long long x = 0, tot;
-    if (i < a.B) x = (unsigned long long)((s_start[i + 1] - s_start[i] + per_block - 1) / per_block);
+    if (i < a.B) {
+      x = (unsigned long long)((s_start[i + 1] - s_start[i] + per_block - 1) / per_block);
+      if (is_big(i)) x <<= 32;
+    }
     const unsigned long long incl = plan_scan(x, s_scan, &tot);
-    if (i < a.B) s_blk[i] = n_segs + (int)(incl - x);
-    n_segs += (int)tot;
+    if (i < a.B) {
+      s_blk[i] = n_segs + (int)(uint32_t)(incl - x);
+      s_big[i] = n_big + (int)((incl - x) >> 32);
+    }
+    n_segs += (int)(uint32_t)tot;
+    n_big += (int)(tot >> 32);
   }
-  if (tid == 0) s_blk[a.B] = n_segs;
+  if (tid == 0) {
+    s_blk[a.B] = n_segs;
+    s_big[a.B] = n_big;
+  }
   __syncthreads();
+  // The prefill kernel's blocks, cut into parts of about the same visits: kPartWaves for every
+  // workgroup of a kv head.  A thread takes a run of them.
+  int n_parts = 0;
+  if (n_big > 0) {
+    const int per = (n_big + kPlThreads - 1) / kPlThreads;
+    const int j0 = min(tid * per, n_big), j1 = min(j0 + per, n_big);
+    auto block_of = [&](int j, ChunkPart* p) {  // visits of block j
+      int b = 0, hi = a.B - 1;  // the last sequence that begins at or before it
+      while (b < hi) {
+        const int mid = (b + hi + 1) >> 1;
+        if (s_big[mid] <= j) b = mid; else hi = mid - 1;
+      }
+      p->seq = b;
+      p->row0 = s_start[b];
+      p->n = s_start[b + 1] - s_start[b];
+      p->L = s_len[b];
+      p->block = j - s_big[b];
+      p->G = plan_group(a, p->L);
+      const int q0 = p->L - p->n + p->block * per_block, q1 = min(q0 + per_block, p->L) - 1;
+      const VisitRanges vr = visit_ranges(q0, q1, p->G > 1 ? a.w0 : INT_MAX, kChunkTile);
+      return vr.n_r + vr.n_kt - vr.kt_l;
+    };
+    unsigned long long mine = 0, all, tot;
+    ChunkPart p = {};
+    for (int j = j0; j < j1; ++j) mine += (unsigned long long)block_of(j, &p);
+    plan_scan(mine, s_scan, &all);
+    const long long even = (long long)((all + kPartWaves * a.n_wg - 1) / (unsigned)(kPartWaves * a.n_wg));
+    const int target = (int)min(max(even, (long long)kChunkMinPart), 0x3fffffffLL);
+    auto parts_of = [&](int visits) { return max(1, min(16, (visits + target / 2) / target)); };
+    mine = 0;  // parts, and those of blocks that are cut
+    for (int j = j0; j < j1; ++j) {
+      const unsigned long long c = (unsigned long long)parts_of(block_of(j, &p));
+      mine += c | (c > 1 ? c : 0) << 32;
+    }
+    unsigned long long at = plan_scan(mine, s_scan, &tot) - mine;
+    n_parts = (int)(uint32_t)tot;
+    for (int j = j0; j < j1; ++j) {
+      p.parts = parts_of(block_of(j, &p));
+      p.slot = (int)(at >> 32);
+      for (p.part = 0; p.part < p.parts; ++p.part) a.parts[(uint32_t)at + p.part] = p;
+      at += (unsigned long long)p.parts | (unsigned long long)(p.parts > 1 ? p.parts : 0) << 32;
+    }
+  }
+  if (tid == 0) v.header[kHdParts] = n_parts;
   for (int seg = tid; seg < n_segs; seg += kPlThreads) {
     int b = 0, hi = a.B - 1;  // the last sequence that begins at or before it
     while (b < hi) {
@@ -522,7 +622,7 @@ __global__ __launch_bounds__(kPlThreads) void chunk_plan_kernel(SharedPlanArgs a
       if (s_start[mid + 1] > t) hi = mid; else b = mid + 1;
     }
     Member m = {-1, 0, -1, -1};
-    if (b < a.B && s_start[b] <= t) {
+    if (b < a.B && s_start[b] <= t && !is_big(b)) {
       const int i = t - s_start[b], pos = s_len[b] - (s_start[b + 1] - s_start[b]) + i;
       if (pos >= 0) m = Member{t, pos + 1, s_blk[b] + i / per_block, -1};
     }
@@ -932,7 +1032,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       }
     };
     // S^T = K Q^T - m of visit i: its key operands are requested ahead, then multiplied
-    constexpr int kKr = ALL ? 4 : 8;
+    constexpr int kKr = FEW ? 8 : 4;
     bf16x8 kr[kKr];
     auto kop = [&](int s) __attribute__((always_inline)) {
       return *(const bf16x8*)(smem + (i % kShBufs) * kShBuf + sh_koff(kr_lane, 2 * s + hl32));
@@ -1089,13 +1189,12 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
         enter();
         if (on) {
           keys();
-          tile_values(i - 1);
-          fence();
           f32x16 sc = nx_sc;
           mask(sc, c0, cG);
           scores();
           const float ps = weights(sc);
           settle(sc, ps, true);
+          tile_values(i - 1);
           values(i - 1);
         }
       }
@@ -1321,7 +1420,7 @@ __global__ __launch_bounds__(512) void merge_shared_kernel(SharedArgs a) {
 
 // ---------------------------------------------------------------- launchers
 static size_t chunk_plan_lds(int B, int T, int g) {
-  return (3 * (size_t)B + 2) * sizeof(int) + chunk_sizes(B, T, g).segs * 8 + 8;
+  return (4 * (size_t)B + 3) * sizeof(int) + chunk_sizes(B, T, g).segs * 8 + 8;
 }
 bool chunk_rows_fit(int B, int T, int g) { return chunk_plan_lds(B, T, g) <= 60 * 1024; }
 
@@ -1342,7 +1441,8 @@ hipError_t launch_shared_plan(bool bifocal, const int32_t* kv_lens, const int32_
                               int n_groups, int Hq, int Hkv, int max_pages, int page, int w_pre,
                               int w0, int n_cu, void* plan, hipStream_t stream) {
   SharedPlanArgs a{kv_lens, members, group_starts, shared, nullptr, plan, B, n_groups, 0, Hq / Hkv,
-                   Hkv, max_pages, page, head_workgroups(n_cu, Hkv), bifocal ? 1 : 0, w_pre, w0};
+                   Hkv, max_pages, page, head_workgroups(n_cu, Hkv), bifocal ? 1 : 0, w_pre, w0,
+                   nullptr};
   return launch_plan(false, a, stream);
 }
 
@@ -1406,20 +1506,32 @@ hipError_t launch_chunk_rows(bool bifocal, const uint16_t* q, const uint16_t* k,
                              const int32_t* table, int max_pages, int n_pages, int page_shift,
                              const int32_t* cu, const int32_t* kv_lens, uint16_t* o, float* lse,
                              const float2* rope, const uint32_t* rope16, int B, int T, int Hq,
-                             int Hkv, int w_pre, int w0, int n_cu, void* scratch,
+                             int Hkv, int w_pre, int w0, float slack, int n_cu, void* scratch,
                              hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1) {
-  const int g = Hq / Hkv;
-  void* states = (char*)scratch + (plan_bytes(chunk_sizes(B, T, g)) + 255) / 256 * 256;
+  const int g = Hq / Hkv, page = 1 << page_shift;
+  const ChunkScratch at = chunk_scratch(B, T, Hq, Hkv, max_pages, page);
+  char* const mem = (char*)scratch;
+  const bool blocks = chunk_blocks(B, T, g, max_pages, page);
   SharedPlanArgs p{kv_lens, nullptr, nullptr, nullptr, cu, scratch, B, 0, T, g, Hkv, max_pages,
-                   1 << page_shift, head_workgroups(n_cu, Hkv), bifocal ? 1 : 0, w_pre, w0};
-  const hipError_t e = launch_plan(true, p, stream);
+                   page, head_workgroups(n_cu, Hkv), bifocal ? 1 : 0, w_pre, w0,
+                   blocks ? (ChunkPart*)(mem + at.parts) : nullptr};
+  hipError_t e = launch_plan(true, p, stream);
   if (e != hipSuccess) return e;
-  SharedArgs a = rows_args(bifocal, q, k, v, table, max_pages, n_pages, page_shift, scratch, states, o,
-                           rope, rope16, B, Hq, Hkv, w_pre, w0, n_cu);
+  if (ev0 != nullptr && (e = hipEventRecord(ev0, stream)) != hipSuccess) return e;
+  if (blocks) {
+    // no sequence past the window: G = 1 for all, and the vanilla kernel does
+    const bool fused = bifocal && (long long)max_pages * page > w_pre;
+    e = launch_prefill_chunks(fused, q, k, v, o, lse, rope, rope16, table, max_pages, page_shift,
+                              n_pages, T, Hq, Hkv, w0, slack, p.parts, (int*)scratch + kHdParts,
+                              (int)most_parts(B, T, g, p.n_wg), (float*)(mem + at.part_states), stream);
+    if (e != hipSuccess) return e;
+  }
+  SharedArgs a = rows_args(bifocal, q, k, v, table, max_pages, n_pages, page_shift, scratch,
+                           mem + at.states, o, rope, rope16, B, Hq, Hkv, w_pre, w0, n_cu);
   a.chunk = 1;
   a.T = T;
   a.lse = lse;
-  return launch_rows(a, stream, ev0, ev1);
+  return launch_rows(a, stream, nullptr, ev1);
 }
 
 }  // namespace jl

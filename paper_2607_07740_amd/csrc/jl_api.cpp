@@ -96,13 +96,13 @@ hipError_t launch_decode_shared(bool bifocal, const uint16_t* q, const uint16_t*
                                 const float2* rope, const uint32_t* rope16, int B, int n_groups,
                                 int Hq, int Hkv, int w_pre, int w0, int n_cu, void* ws,
                                 hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1);
-size_t chunk_scratch_bytes(int B, int T, int Hq, int Hkv);
+size_t chunk_scratch_bytes(int B, int T, int Hq, int Hkv, int max_pages, int page);
 bool chunk_rows_fit(int B, int T, int g);
 hipError_t launch_chunk_rows(bool bifocal, const uint16_t* q, const uint16_t* k, const uint16_t* v,
                              const int32_t* table, int max_pages, int n_pages, int page_shift,
                              const int32_t* cu, const int32_t* kv_lens, uint16_t* o, float* lse,
                              const float2* rope, const uint32_t* rope16, int B, int T, int Hq,
-                             int Hkv, int w_pre, int w0, int n_cu, void* scratch,
+                             int Hkv, int w_pre, int w0, float slack, int n_cu, void* scratch,
                              hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1);
 hipError_t launch_pages_fork(const Pages& p, const int32_t* parent, hipStream_t stream);
 hipError_t launch_pages_reserve(const Pages& p, const int32_t* n_new, int32_t* starts,
@@ -840,7 +840,7 @@ int varlen_paged(bool bifocal, const void* q, const void* kp, const void* vp, co
   if ((long long)n_pages * page_size > 0x7fffffffLL)
     return fail(JL_ERR_UNSUPPORTED, "a pool of %lld tokens (at most 2^31 - 1)",
                 (long long)n_pages * page_size);
-  if (B > jl::kShMaxSeqs || past_int32(T, Hq, 1) || !jl::chunk_rows_fit(B, T, Hq / Hkv))
+  if (B > jl::kShMaxSeqs || past_int32(T, Hq, 2) || past_int32(2LL * B + 1024, Hkv, 1) || !jl::chunk_rows_fit(B, T, Hq / Hkv))
     return fail(JL_ERR_UNSUPPORTED, "%d tokens of %d sequences in one call", T, B);
   if (!aligned16(q) || !aligned16(kp) || !aligned16(vp) || !aligned16(o))
     return fail(JL_ERR_INVALID_ARG, "q, k_pages, v_pages, o must be non-null and 16-byte aligned");
@@ -853,7 +853,7 @@ int varlen_paged(bool bifocal, const void* q, const void* kp, const void* vp, co
   if (st != JL_OK) return st;
   std::lock_guard<std::mutex> launch_lock(g_prefill_mu);
   void* scratch = nullptr;
-  const size_t bytes = jl::chunk_scratch_bytes(B, T, Hq, Hkv);
+  const size_t bytes = jl::chunk_scratch_bytes(B, T, Hq, Hkv, max_pages, page_size);
   st = get_scratch(s, bytes, &scratch);
   if (st != JL_OK) return st;
   if (scratch == nullptr)
@@ -864,7 +864,7 @@ int varlen_paged(bool bifocal, const void* q, const void* kp, const void* vp, co
   const hipError_t e = jl::launch_chunk_rows(
       bifocal, (const uint16_t*)q, (const uint16_t*)kp, (const uint16_t*)vp, table, max_pages,
       n_pages, shift, cu, kv_lens, (uint16_t*)o, lse, tab.f32, tab.f16, B, T, Hq, Hkv, w_pre, w0,
-      jl::cu_count(), scratch, s, ev0, ev1);
+      (float)g_rescale_log2.load(), jl::cu_count(), scratch, s, ev0, ev1);
   if (e != hipSuccess) return hip_fail(e, "packed chunk launch");
   return ok();
 }

@@ -47,6 +47,7 @@
 #include <climits>
 
 #include "jl_device.h"
+#include "prefill_chunks.h"
 
 namespace jl {
 
@@ -123,6 +124,9 @@ struct PrefillArgs {
   // parts, part-major, whose states meet in merge_parts_kernel
   int n_blocks, n_whole, n_tail, n_part;
   float* states;
+  // packed chunks behind paged caches (prefill_chunks_kernel): their parts, and how many
+  const ChunkPart* chunk_parts;
+  const int* n_chunk_parts;
 };
 
 // Most pages of one sequence a paged prefill block looks up (LDS table)
@@ -870,6 +874,45 @@ __device__ __forceinline__ bool prefill_block(const PrefillArgs& a, const Work& 
   return false;
 }
 
+// Packed chunks behind paged caches: the parts of a list of query blocks of different sequences,
+// which a planning kernel has cut to about the same length, one per workgroup and kv head.
+__device__ inline Work chunk_work(const PrefillArgs& a, const ChunkPart& p, int kvh) {
+  Work W;
+  W.b = p.seq;
+  W.kvh = kvh;
+  W.qblk = p.block;
+  W.q_start = p.L - p.n;
+  W.q_end = p.L;
+  W.w0 = p.G > 1 ? a.w0 : INT_MAX;
+  W.Lk = p.L;
+  W.row_base = W.lse_base = (size_t)p.row0;
+  W.kv_row0 = W.rtab_row = 0;
+  W.gdiv = make_fastdiv((uint32_t)p.G);
+  return W;
+}
+__device__ inline float* chunk_state(const PrefillArgs& a, const ChunkPart& p, int part, int kvh) {
+  return a.states + ((size_t)(p.slot + part) * a.Hkv + kvh) * kPartFloats;
+}
+
+template <int MODE>
+__global__ __launch_bounds__(kPfThreads, 2) void prefill_chunks_kernel(PrefillArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[kSmemBytes];
+  __shared__ int s_bad;
+  __shared__ int s_pages[kMaxSeqPages];
+  typedef __attribute__((address_space(4))) const int const_int;  // scalar loads
+  const int at = blockIdx.x / a.Hkv, kvh = blockIdx.x - at * a.Hkv;
+  if (at >= *(const const_int*)a.n_chunk_parts) return;
+  const const_int* src = (const const_int*)(a.chunk_parts + at);
+  const ChunkPart p = {src[0], src[1], src[2], src[3], src[4], src[5], src[6], src[7], src[8], {}};
+  const Work W = chunk_work(a, p, kvh);
+  float* state = chunk_state(a, p, p.part, kvh);
+  if (prefill_block<MODE, false, true, true, kPfWaves>(a, W, smem, &s_bad, s_pages, p.part, p.parts,
+                                                       state)) {
+    __syncthreads();
+    prefill_block<MODE, true, true, true, kPfWaves>(a, W, smem, &s_bad, s_pages, p.part, p.parts, state);
+  }
+}
+
 template <int MODE, bool PAGED = false, bool SPLIT = false, int WAVES = kPfWaves>
 __global__ __launch_bounds__(64 * WAVES, WAVES == kPfWaves ? 2 : 1) void prefill_kernel(PrefillArgs a) {
   // LDS: rotated K tiles and V tiles, two buffers each
@@ -935,6 +978,42 @@ __global__ __launch_bounds__(256) void merge_parts_kernel(PrefillArgs a) {
   for (int i = 0; i < 4; ++i) *(bf16x4*)(o + 4 * i) = __builtin_convertvector(acc[i] * inv, bf16x4);
   if (a.lse != nullptr && dg == 0)
     a.lse[W.lse_base + (size_t)hd * a.Lq + qr] = (M + log2f(den)) * 0.69314718055994531f;
+}
+
+// The same for the blocks of packed chunks that were cut.
+__global__ __launch_bounds__(256) void merge_chunks_kernel(PrefillArgs a) {
+  const int at = blockIdx.x / a.Hkv, kvh = blockIdx.x - at * a.Hkv;
+  if (at >= *a.n_chunk_parts) return;
+  const ChunkPart p = a.chunk_parts[at];
+  if (p.part != 0 || p.parts <= 1) return;
+  const int row = 32 * blockIdx.y + (threadIdx.x & 31);
+  const int dg = threadIdx.x >> 5;
+  const int hl = row / a.BQ;
+  const int qr = p.block * a.BQ + (row - hl * a.BQ);  // row of the sequence's chunk
+  if (qr >= p.n) return;
+  float M = -INFINITY;
+  for (int s = 0; s < p.parts; ++s) {
+    const float2 ml = ((const float2*)(chunk_state(a, p, s, kvh) + kPfRows * kHeadDim))[row];
+    if (ml.y != 0.f) M = fmaxf(M, ml.x);
+  }
+  float den = 0.f;
+  f32x4 acc[4] = {};
+  for (int s = 0; s < p.parts; ++s) {
+    const float* st = chunk_state(a, p, s, kvh);
+    const float2 ml = ((const float2*)(st + kPfRows * kHeadDim))[row];
+    if (ml.y == 0.f) continue;
+    const float w = fast_exp2(ml.x - M);
+    den += w * ml.y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] += w * ((const f32x4*)st)[(4 * dg + i) * kPfRows + row];
+  }
+  const int hd = kvh * a.g + hl;
+  const float inv = 1.f / den;
+  uint16_t* o = a.o + (((size_t)p.row0 + qr) * a.Hq + hd) * kHeadDim + 16 * dg;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) *(bf16x4*)(o + 4 * i) = __builtin_convertvector(acc[i] * inv, bf16x4);
+  if (a.lse != nullptr && dg == 0)
+    a.lse[(size_t)p.row0 + (size_t)hd * a.Lq + qr] = (M + log2f(den)) * 0.69314718055994531f;
 }
 
 // ------------------------------------------------------ Eq. (7) merge kernel
@@ -1448,6 +1527,39 @@ hipError_t launch_prefill_varlen(bool bifocal, const uint16_t* q, const uint16_t
               : launch_blocks<kModeVanilla>(a, grid, stream);
   if (e == hipSuccess && ev1 != nullptr) e = hipEventRecord(ev1, stream);
   return e;
+}
+
+// ------------------------------------------- packed chunks behind paged caches
+size_t prefill_chunk_state_bytes() { return kPartFloats * sizeof(float); }
+int prefill_chunk_max_pages() { return kMaxSeqPages; }
+
+// The parts that a planning kernel has listed: at most max_parts.  q, o [T][Hq][128], lse [Hq][T].
+hipError_t launch_prefill_chunks(bool bifocal, const uint16_t* q, const uint16_t* k,
+                                 const uint16_t* v, uint16_t* o, float* lse, const float2* table,
+                                 const uint32_t* table16, const int32_t* block_table,
+                                 int max_pages, int page_shift, int n_pages, int T, int Hq, int Hkv,
+                                 int w0, float slack, const ChunkPart* parts,
+                                 const int* n_parts, int max_parts, float* states,
+                                 hipStream_t stream) {
+  PrefillArgs a = {};
+  fill_geometry(a, 1, Hq, Hkv, 1, 0, T, slack);
+  fill_inputs(a, q, k, v, table, table, table16, table16, 0, 0, 1,
+              Paging{block_table, max_pages, page_shift, n_pages});
+  a.o = o;
+  a.lse = lse;
+  a.w0 = bifocal ? w0 : INT_MAX;
+  a.chunk_parts = parts;
+  a.n_chunk_parts = n_parts;
+  a.states = states;
+  const unsigned grid = (unsigned)max_parts * Hkv;
+  if (bifocal)
+    hipLaunchKernelGGL(prefill_chunks_kernel<kModeFused>, dim3(grid), dim3(kPfThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL(prefill_chunks_kernel<kModeVanilla>, dim3(grid), dim3(kPfThreads), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(merge_chunks_kernel, dim3(grid, kPfRows / 32), dim3(256), 0, stream, a);
+  return hipGetLastError();
 }
 
 int prefill_rows_per_block() { return kPfRows; }

@@ -106,6 +106,50 @@ def test_groups_of_heads(Hq, Hkv):
     assert_close(to_f64(c.run(64, 20)), c.want(64, 20)[0], what="heads %d/%d" % (Hq, Hkv))
 
 
+@pytest.mark.parametrize("lens,n,w_pre,w0,page", [
+    ([6000, 900, 40, 3000], [300, 1, 40, 70], 2000, 500, 64),  # blocks in parts, beside few rows
+    ([5000, 4999], [260, 4], 1 << 20, 9, 128),                 # every G 1
+    ([2500, 1300, 260], [65, 400, 260], 600, 0, 1024),         # a block that ends the chunk, a page of all
+    ([300] * 12, [30] * 12, 100, 50, 64)])                     # no sequence has a block's rows
+def test_long_chunks_in_blocks(lens, n, w_pre, w0, page):
+    """Enough rows that longer chunks run as whole blocks, whose key ranges are cut."""
+    c = Chunks(lens, n, 8, 2, page, seed=len(lens))
+    say("blocks", lens, n)
+    for bifocal in (True, False):
+        out, lse = c.run(w_pre, w0, bifocal, want_lse=True)
+        at = 0
+        for (q, k, v), L, m in zip(c.seqs, c.lens, c.n):
+            rows = np.asarray([(0, h, L - m + i) for h in range(8) for i in range(m)], np.int64)
+            o, l, _ = O.prefill_rows(q, k, v, rows, theta=1e6, w_pretrained=w_pre, w_local=w0,
+                                     bifocal=bifocal, want_lse=True)
+            got = to_f64(out[at:at + m]).transpose(1, 0, 2).reshape(8 * m, 128)
+            assert_close(got, o, what="L %d n %d" % (L, m))
+            assert_close(lse[:, at:at + m].reshape(-1).cpu().numpy(), l, what="lse")
+            at += m
+
+
+def test_scores_far_from_the_first_reference():
+    """Keys whose scores lie hundreds of log2 units apart, rising and falling: the references move."""
+    for n, sign in ((3, 1), (3, -1), (150, 1), (300, -1)):
+        c = Chunks([700, 64], [n, 5], 8, 2, 64, seed=n)
+        for b, (q, k, v) in enumerate(c.seqs):
+            big = synth.bf16_bits(np.full(q.shape, 20.0, np.float32))
+            ramp = np.linspace(-sign, sign, c.lens[b], dtype=np.float32)[None, :, None, None]
+            kk = synth.bf16_bits(np.broadcast_to(20 * ramp, k.shape).copy())
+            c.seqs[b] = (big, kk, v)
+            for j in range(-(-c.lens[b] // 64)):
+                part = slice(64 * j, min(64 * j + 64, c.lens[b]))
+                c.kp[c.table[b, j], :part.stop - part.start] = kk[0, part]
+        c.q = np.concatenate([s[0][0, L - m:] for s, L, m in zip(c.seqs, c.lens, c.n)])
+        say("far scores", n, sign)
+        # a weight of size 1 over scores of this size keeps no better than their own rounding, 2^-8
+        # of about 2000: the mean over few keys, values of size 1
+        out = c.run(256, 90)
+        assert torch.isfinite(out.float()).all()
+        want = c.want(256, 90)[0]
+        assert np.abs(to_f64(out) - want).mean() < 1.0
+
+
 def test_agrees_with_the_chunk_of_one_start_and_repeats_its_bits():
     c = Chunks([900, 900], [130, 130], 8, 2, 64, seed=3)
     say("one start")
