@@ -61,7 +61,7 @@ struct Segment {
   int visits, view0, len, kind;   // view0: its views' place; len: its rows' length for G, 0: each its own
   uint32_t start_lo, start_hi;    // cost before it
   int w_first, n_w;               // workgroups that hold some of its visits
-  int row0, pad2[3];              // state rows before it
+  int row0, q0, pad[2];           // state rows before it; a chunk's first row of q
 };
 // Whose rows a segment has: several sequences, one, or consecutive tokens of one
 enum { kSegShared = 0, kSegOwn = 1, kSegChunk = 2 };
@@ -120,12 +120,13 @@ __host__ __device__ inline PlanView plan_view(void* p, const PlanSizes& z) {
 static size_t plan_bytes(const PlanSizes& z) {
   return kPlanHead + z.members * sizeof(Member) + z.views * sizeof(View) + z.segs * sizeof(Segment);
 }
-// Parts of the chunks whose blocks the prefill kernel takes, at most: each block rounded up, and
-// kPartWaves times the workgroups of a kv head; of these a block's that is cut at most 4/3 of the
-// latter.
+// Parts of the chunks whose blocks the prefill kernel takes, at most: kPartWaves times the
+// workgroups of a kv head and each block rounded up, both twice for the empty ones (a block of a
+// whole prompt has half of the longest's visits in the mean).  Of a block that is cut, at
+// most 4/3 of its share have states.
 constexpr int kPartWaves = 3;
 static size_t most_parts(int B, int T, int g, int n_wg) {
-  return 2 * chunk_sizes(B, T, g).segs + (size_t)kPartWaves * n_wg;
+  return 2 * (chunk_sizes(B, T, g).segs + (size_t)kPartWaves * n_wg);
 }
 static size_t most_slots(int n_wg) { return (size_t)kPartWaves * n_wg * 4 / 3 + 2; }
 size_t prefill_chunk_state_bytes();
@@ -139,7 +140,7 @@ hipError_t launch_prefill_chunks(bool bifocal, const uint16_t* q, const uint16_t
 size_t shared_plan_bytes(int B, int n_groups, int g) { return plan_bytes(decode_sizes(B, n_groups, g)); }
 
 enum { kHdSegs = 0, kHdWg, kHdTotLo, kHdTotHi, kHdRows, kHdB, kHdG, kHdPage, kHdMaxPages, kHdHkv,
-       kHdGroups, kHdBifocal, kHdWPre, kHdW0, kHdParts };
+       kHdGroups, kHdBifocal, kHdWPre, kHdW0, kHdParts, kHdMembers };
 
 // State rows of one kv head: every segment's, for each of its halves, and again where a
 // workgroup's range ends inside it.
@@ -193,9 +194,10 @@ struct SharedPlanArgs {
   void* plan;
   int B, n_groups, T, g, Hkv, max_pages, page, n_wg, bifocal, w_pre, w0;
   ChunkPart* parts;        // chunks: of those whose blocks the prefill kernel takes; nullptr: none
+  int most_parts;
 };
 
-constexpr int kPlThreads = 1024, kPlWaves = kPlThreads / 64;
+constexpr int kPlThreads = 1024, kPlWaves = kPlThreads / 64;  // at most; few sequences take 256
 
 // Inclusive sums over the workgroup's threads, in thread order; everyone gets the total
 template <typename T>
@@ -212,10 +214,14 @@ __device__ inline T plan_scan(T v, T* s, T* total) {
   __syncthreads();
   T before = 0, all = 0;
 #pragma unroll
-  for (int i = 0; i < kPlWaves; ++i) {
-    const T x = s[i];
-    if (i < wave) before += x;
-    all += x;
+  for (int i = 0; i < kPlWaves; i += 4) {
+    if (64 * i >= (int)blockDim.x) break;
+#pragma unroll
+    for (int j = i; j < i + 4; ++j) {
+      const T x = s[j];
+      if (j < wave) before += x;
+      all += x;
+    }
   }
   *total = all;
   return before + incl;
@@ -232,15 +238,24 @@ __device__ inline int wave_max(int v) {
   return v;
 }
 
+// max(1, ceil(len / w_pre)) for len <= 2^23, without a 64-bit division
+__device__ inline int rows_group(int len, int bifocal, int w_pre) {
+  return !bifocal || len <= w_pre ? 1 : (int)(((uint32_t)len + (uint32_t)w_pre - 1) / (uint32_t)w_pre);
+}
 __device__ inline int plan_group(const SharedPlanArgs& a, int len) {
-  return a.bifocal ? group_size(len, a.w_pre) : 1;
+  return rows_group(len, a.bifocal, a.w_pre);
 }
 // The first key that a query at position q takes in the base view (0 where it takes all so)
 __device__ inline int first_local(int G, int q, int w0) { return G > 1 ? max(0, q - w0) : 0; }
 
+// make_fastdiv for 2 <= G <= 2^23: its quotient 2^32 (2^l - G) / G, whose numerator a double
+// holds, by a division of doubles, one too large at most
 __device__ inline View view_of(int G) {
-  const FastDiv f = make_fastdiv((uint32_t)G);
-  return View{G, f.m, f.l, 0};
+  const uint32_t l = 32 - __builtin_clz((uint32_t)G - 1);
+  const uint64_t num = (((uint64_t)1 << l) - (uint32_t)G) << 32;
+  uint32_t m = (uint32_t)((double)num / (double)G);
+  if ((uint64_t)m * (uint32_t)G > num) --m;
+  return View{G, m + 1, l, 0};
 }
 
 // Visits of keys [k0, kend) for rows whose first local keys lie between `low` and, among
@@ -285,7 +300,7 @@ __device__ inline void plan_ranges(const SharedPlanArgs& a, const PlanView& v, i
                                    const int* s_visits, const short* s_rows, const short* s_states,
                                    unsigned long long* s_scan) {
   const int tid = threadIdx.x;
-  const int per = (n_segs + kPlThreads - 1) / kPlThreads;
+  const int per = (n_segs + (int)blockDim.x - 1) >> (31 - __builtin_clz(blockDim.x));
   const int i0 = min(tid * per, n_segs), i1 = min(i0 + per, n_segs);
   auto cost = [&](int i) {
     const int n = s_visits[i];
@@ -345,6 +360,7 @@ __device__ inline void plan_ranges(const SharedPlanArgs& a, const PlanView& v, i
     v.header[kHdBifocal] = a.bifocal;
     v.header[kHdWPre] = a.w_pre;
     v.header[kHdW0] = a.w0;
+    if (a.cu == nullptr) v.header[kHdMembers] = a.B;
   }
 }
 
@@ -352,7 +368,7 @@ __device__ inline void plan_ranges(const SharedPlanArgs& a, const PlanView& v, i
 __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs a) {
   extern __shared__ int s_mem[];
   __shared__ unsigned long long s_scan[kPlWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nt = blockDim.x;
   const PlanSizes z = decode_sizes(a.B, a.n_groups, a.g);
   const PlanView v = plan_view(a.plan, z);
   int* const s_len = s_mem;                    // [B] by member, -1: no such sequence
@@ -367,13 +383,13 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
   const int per_block = kShRows / a.g;
 
   bool bad = false;
-  for (int i = tid; i <= a.n_groups; i += kPlThreads) {
+  for (int i = tid; i <= a.n_groups; i += nt) {
     const int x = min(max(a.group_starts[i], 0), a.B);
     s_start[i] = x;
     if (i > 0) bad |= min(max(a.group_starts[i - 1], 0), a.B) > x;
   }
-  for (int i = tid; i < a.n_groups; i += kPlThreads) s_pre[i] = INT_MAX;
-  for (int i = tid; i < a.B; i += kPlThreads) {
+  for (int i = tid; i < a.n_groups; i += nt) s_pre[i] = INT_MAX;
+  for (int i = tid; i < a.B; i += nt) {
     const int seq = a.members != nullptr ? a.members[i] : i;
     const bool ok = (unsigned)seq < (unsigned)a.B;
     s_seq[i] = ok ? seq : -1;
@@ -393,19 +409,19 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
     }
     return lo < a.n_groups && s_start[lo] <= m ? lo : -1;
   };
-  for (int i = tid; i < a.B; i += kPlThreads) {
+  for (int i = tid; i < a.B; i += nt) {
     const int gi = group_of(i);
     if (gi >= 0 && s_len[i] > 0) atomicMin(&s_pre[gi], s_len[i]);
   }
   __syncthreads();
   // the groups' shared keys and their blocks of up to 256 rows
   int n_blocks = 0;
-  for (int c0 = 0; c0 < a.n_groups; c0 += kPlThreads) {
+  for (int c0 = 0; c0 < a.n_groups; c0 += nt) {
     const int i = c0 + tid;
     unsigned long long x = 0, tot;
     if (i < a.n_groups) {
       const int n = s_start[i + 1] - s_start[i], low = s_pre[i];
-      const int P = n > 1 && low != INT_MAX ? min(max(a.shared[i], 0), low) / a.page * a.page : 0;
+      const int P = n > 1 && low != INT_MAX ? min(max(a.shared[i], 0), low) & -a.page : 0;
       s_pre[i] = P;
       x = P > 0 ? (n + per_block - 1) / per_block : 0;
     }
@@ -416,7 +432,7 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
   if (tid == 0) s_blk[a.n_groups] = n_blocks;
   __syncthreads();
   // prefix blocks, a wave each, lane -> every 64th of its sequences
-  for (int blk = wave; blk < n_blocks; blk += kPlWaves) {
+  for (int blk = wave; blk < n_blocks; blk += nt >> 6) {
     int gi = 0, hi = a.n_groups - 1;  // the last group that begins at or before it
     while (gi < hi) {
       const int mid = (gi + hi + 1) >> 1;
@@ -461,7 +477,7 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
     }
   }
   // the members' own keys
-  for (int i = tid; i < a.B; i += kPlThreads) {
+  for (int i = tid; i < a.B; i += nt) {
     const int gi = group_of(i), len = s_len[i], seg = n_blocks + i;
     Segment s = {};
     Member m = {gi >= 0 && len >= 0 ? s_seq[i] : -1, max(len, 0), -1, -1};
@@ -491,25 +507,28 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
 
 // The plan of packed chunks: sequence b's rows are cu[b] .. cu[b + 1] - 1 of the packed ones,
 // the last kv_lens[b] - n .. kv_lens[b] - 1 of its positions (rows that would lie before
-// position 0 are left out).  Segments: blocks of up to 256 / g tokens, the last of a sequence
-// shorter.
+// position 0 are left out).  Blocks of up to 256 / g tokens, the last of a sequence shorter,
+// are segments, or parts for the prefill kernel; the members are the tokens of segments.
 __global__ __launch_bounds__(kPlThreads) void chunk_plan_kernel(SharedPlanArgs a) {
   extern __shared__ int s_mem[];
   __shared__ unsigned long long s_scan[kPlWaves];
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, nt = blockDim.x;
+  const int log_nt = 31 - __builtin_clz(nt);
   const PlanSizes z = chunk_sizes(a.B, a.T, a.g);
   const PlanView v = plan_view(a.plan, z);
   int* const s_start = s_mem;               // [B + 1]
   int* const s_len = s_start + a.B + 1;     // [B]
-  int* const s_blk = s_len + a.B;           // [B + 1]: blocks before the sequence
+  int* const s_blk = s_len + a.B;           // [B + 1]: segments before the sequence
   int* const s_big = s_blk + a.B + 1;       // [B + 1]: the prefill kernel's blocks before it
-  int* const s_visits = s_big + a.B + 1;
-  short* const s_rows = (short*)(s_visits + z.segs);
+  int* const s_tok = s_big + a.B + 1;       // [B + 1]: members before it; then parts
+  int* const s_visits = s_tok + a.B + 1;
+  int* const s_slot = s_visits + z.segs;    // states before a block of the prefill kernel
+  short* const s_rows = (short*)(s_slot + z.segs);
   short* const s_states = s_rows + z.segs;
   const int cap = a.max_pages * a.page;
   const int per_block = kShRows / a.g;
   bool bad = false;
-  for (int i = tid; i <= a.B; i += kPlThreads) {
+  for (int i = tid; i <= a.B; i += nt) {
     const int x = min(max(a.cu[i], 0), a.T);
     s_start[i] = x;
     if (i > 0) bad |= min(max(a.cu[i - 1], 0), a.T) > x;
@@ -520,94 +539,60 @@ __global__ __launch_bounds__(kPlThreads) void chunk_plan_kernel(SharedPlanArgs a
       for (int i = 1; i <= a.B; ++i) s_start[i] = max(s_start[i], s_start[i - 1]);
     __syncthreads();
   }
-  // blocks of each sequence: of one kind or the other
   auto is_big = [&](int b) {
     const int n = s_start[b + 1] - s_start[b];
     return a.parts != nullptr && n * a.g > kShSmall && s_len[b] >= n;
   };
-  int n_segs = 0, n_big = 0;
-  for (int c0 = 0; c0 < a.B; c0 += kPlThreads) {
+  // the last b whose entry of `list` is at or below x
+  auto find = [&](const int* list, int x) {
+    int b = 0, hi = a.B - 1;
+    while (b < hi) {
+      const int mid = (b + hi + 1) >> 1;
+      if (list[mid] <= x) b = mid; else hi = mid - 1;
+    }
+    return b;
+  };
+  int n_segs = 0, n_big = 0, n_tok = 0;
+  for (int c0 = 0; c0 < a.B; c0 += nt) {
     const int i = c0 + tid;
-    unsigned long long x = 0, tot;
+    unsigned long long x = 0, tot;  // members, segments, blocks: 24, 20 and 20 bits
     if (i < a.B) {
-      x = (unsigned long long)((s_start[i + 1] - s_start[i] + per_block - 1) / per_block);
-      if (is_big(i)) x <<= 32;
+      const int n = s_start[i + 1] - s_start[i];
+      const unsigned long long blocks = (unsigned)(n + per_block - 1) / (unsigned)per_block;
+      x = is_big(i) ? blocks << 44 : blocks << 24 | (unsigned)n;
     }
     const unsigned long long incl = plan_scan(x, s_scan, &tot);
+    const unsigned long long before = incl - x;
     if (i < a.B) {
-      s_blk[i] = n_segs + (int)(uint32_t)(incl - x);
-      s_big[i] = n_big + (int)((incl - x) >> 32);
+      s_tok[i] = n_tok + (int)(before & 0xffffff);
+      s_blk[i] = n_segs + (int)(before >> 24 & 0xfffff);
+      s_big[i] = n_big + (int)(before >> 44);
     }
-    n_segs += (int)(uint32_t)tot;
-    n_big += (int)(tot >> 32);
+    n_tok += (int)(tot & 0xffffff);
+    n_segs += (int)(tot >> 24 & 0xfffff);
+    n_big += (int)(tot >> 44);
   }
   if (tid == 0) {
+    s_tok[a.B] = n_tok;
     s_blk[a.B] = n_segs;
     s_big[a.B] = n_big;
   }
   __syncthreads();
-  // The prefill kernel's blocks, cut into parts of about the same visits: kPartWaves for every
-  // workgroup of a kv head.  A thread takes a run of them.
-  int n_parts = 0;
-  if (n_big > 0) {
-    const int per = (n_big + kPlThreads - 1) / kPlThreads;
-    const int j0 = min(tid * per, n_big), j1 = min(j0 + per, n_big);
-    auto block_of = [&](int j, ChunkPart* p) {  // visits of block j
-      int b = 0, hi = a.B - 1;  // the last sequence that begins at or before it
-      while (b < hi) {
-        const int mid = (b + hi + 1) >> 1;
-        if (s_big[mid] <= j) b = mid; else hi = mid - 1;
-      }
-      p->seq = b;
-      p->row0 = s_start[b];
-      p->n = s_start[b + 1] - s_start[b];
-      p->L = s_len[b];
-      p->block = j - s_big[b];
-      p->G = plan_group(a, p->L);
-      const int q0 = p->L - p->n + p->block * per_block, q1 = min(q0 + per_block, p->L) - 1;
-      const VisitRanges vr = visit_ranges(q0, q1, p->G > 1 ? a.w0 : INT_MAX, kChunkTile);
-      return vr.n_r + vr.n_kt - vr.kt_l;
-    };
-    unsigned long long mine = 0, all, tot;
-    ChunkPart p = {};
-    for (int j = j0; j < j1; ++j) mine += (unsigned long long)block_of(j, &p);
-    plan_scan(mine, s_scan, &all);
-    const long long even = (long long)((all + kPartWaves * a.n_wg - 1) / (unsigned)(kPartWaves * a.n_wg));
-    const int target = (int)min(max(even, (long long)kChunkMinPart), 0x3fffffffLL);
-    auto parts_of = [&](int visits) { return max(1, min(16, (visits + target / 2) / target)); };
-    mine = 0;  // parts, and those of blocks that are cut
-    for (int j = j0; j < j1; ++j) {
-      const unsigned long long c = (unsigned long long)parts_of(block_of(j, &p));
-      mine += c | (c > 1 ? c : 0) << 32;
-    }
-    unsigned long long at = plan_scan(mine, s_scan, &tot) - mine;
-    n_parts = (int)(uint32_t)tot;
-    for (int j = j0; j < j1; ++j) {
-      p.parts = parts_of(block_of(j, &p));
-      p.slot = (int)(at >> 32);
-      for (p.part = 0; p.part < p.parts; ++p.part) a.parts[(uint32_t)at + p.part] = p;
-      at += (unsigned long long)p.parts | (unsigned long long)(p.parts > 1 ? p.parts : 0) << 32;
-    }
-  }
-  if (tid == 0) v.header[kHdParts] = n_parts;
-  for (int seg = tid; seg < n_segs; seg += kPlThreads) {
-    int b = 0, hi = a.B - 1;  // the last sequence that begins at or before it
-    while (b < hi) {
-      const int mid = (b + hi + 1) >> 1;
-      if (s_blk[mid] <= seg) b = mid; else hi = mid - 1;
-    }
+  for (int seg = tid; seg < n_segs; seg += nt) {
+    const int b = find(s_blk, seg);
     const int n = s_start[b + 1] - s_start[b], t0 = (seg - s_blk[b]) * per_block;
     const int cnt = min(per_block, n - t0), len = s_len[b];
     const int p0 = len - n + t0, p1 = p0 + cnt - 1;  // positions of its first and last token
     const int G = plan_group(a, len);
     Segment s = {};
-    s.m0 = s_start[b] + t0;
+    s.m0 = s_tok[b] + t0;
     s.rows = cnt * a.g;
     s.kend = max(p1 + 1, 0);
     s.seq = b;
     s.view0 = seg;
     s.len = max(len, 1);
     s.kind = kSegChunk;
+    s.q0 = s_start[b] + t0;
     set_visits(s, first_local(G, p0, a.w0), first_local(G, p1, a.w0), G > 1 ? 1 : 0);
     if (G > 1) v.views[seg] = view_of(G);
     v.segs[seg] = s;
@@ -615,20 +600,81 @@ __global__ __launch_bounds__(kPlThreads) void chunk_plan_kernel(SharedPlanArgs a
     s_rows[seg] = (short)s.rows;
     s_states[seg] = (short)(s.rows * state_halves(s.rows, s.n_views));
   }
-  for (int t = tid; t < a.T; t += kPlThreads) {
-    int b = 0, hi = a.B;  // the first sequence whose end lies behind the token
-    while (b < hi) {
-      const int mid = (b + hi) >> 1;
-      if (s_start[mid + 1] > t) hi = mid; else b = mid + 1;
-    }
-    Member m = {-1, 0, -1, -1};
-    if (b < a.B && s_start[b] <= t && !is_big(b)) {
-      const int i = t - s_start[b], pos = s_len[b] - (s_start[b + 1] - s_start[b]) + i;
-      if (pos >= 0) m = Member{t, pos + 1, s_blk[b] + i / per_block, -1};
-    }
-    v.members[t] = m;
+  for (int t = tid; t < n_tok; t += nt) {
+    const int b = find(s_tok, t), i = t - s_tok[b];
+    const int pos = s_len[b] - (s_start[b + 1] - s_start[b]) + i;
+    v.members[t] = pos >= 0 ? Member{s_start[b] + i, pos + 1, s_blk[b] + i / per_block, -1}
+                            : Member{-1, 0, -1, -1};
   }
   __syncthreads();
+  // The prefill kernel's blocks, cut into parts of about the same visits: kPartWaves for every
+  // workgroup of a kv head.  A sequence's parts are listed part after part, so that the
+  // blocks that run beside each other read the same keys; blocks of fewer parts leave empty ones.
+  int n_parts = 0;
+  if (n_big > 0) {
+    auto visits_of = [&](int b, int block) {
+      const int len = s_len[b], n = s_start[b + 1] - s_start[b];
+      const int q0 = len - n + block * per_block, q1 = min(q0 + per_block, len) - 1;
+      const VisitRanges vr = visit_ranges(q0, q1, plan_group(a, len) > 1 ? a.w0 : INT_MAX, kChunkTile);
+      return vr.n_r + vr.n_kt - vr.kt_l;
+    };
+    const int per = (n_big + nt - 1) >> log_nt;
+    const int j0 = min(tid * per, n_big), j1 = min(j0 + per, n_big);
+    unsigned long long mine = 0, all, tot;
+    for (int j = j0; j < j1; ++j) {
+      const int b = find(s_big, j);
+      mine += (unsigned long long)visits_of(b, j - s_big[b]);
+    }
+    plan_scan(mine, s_scan, &all);
+    const unsigned shares = (unsigned)(kPartWaves * a.n_wg);
+    const unsigned long long even = all >> 32 == 0 ? ((unsigned)all + shares - 1) / shares : all / shares + 1;
+    int target = (int)min(max(even, (unsigned long long)kChunkMinPart), 0x1fffffffull);
+    auto parts_of = [&](int visits) { return max(1, min(16, (visits + target / 2) / target)); };
+    // entries of each sequence: its blocks times the parts of its last block, the longest
+    for (;; target *= 2) {  // longer parts where the list could not hold them
+      n_parts = 0;
+      for (int c0 = 0; c0 < a.B; c0 += nt) {
+        const int b = c0 + tid;
+        unsigned long long x = 0;
+        if (b < a.B && s_big[b + 1] > s_big[b]) {
+          const int blocks = s_big[b + 1] - s_big[b];
+          x = (unsigned long long)(blocks * parts_of(visits_of(b, blocks - 1)));
+        }
+        const unsigned long long incl = plan_scan(x, s_scan, &tot);
+        if (b < a.B) s_tok[b] = n_parts + (int)(incl - x);
+        n_parts += (int)tot;
+      }
+      if (n_parts <= a.most_parts || target > 0x1fffffff) break;
+    }
+    mine = 0;  // parts of blocks that are cut
+    for (int j = j0; j < j1; ++j) {
+      const int b = find(s_big, j), c = parts_of(visits_of(b, j - s_big[b]));
+      s_slot[j] = (int)mine;
+      mine += c > 1 ? c : 0;
+    }
+    const int slot0 = (int)(plan_scan(mine, s_scan, &tot) - mine);
+    for (int j = j0; j < j1; ++j) s_slot[j] += slot0;
+    __syncthreads();
+    for (int e = tid; e < n_parts; e += nt) {
+      const int b = find(s_tok, e), blocks = s_big[b + 1] - s_big[b], r = e - s_tok[b];
+      ChunkPart p = {};
+      p.part = r / blocks;
+      p.block = r - p.part * blocks;
+      p.seq = b;
+      p.row0 = s_start[b];
+      p.n = s_start[b + 1] - s_start[b];
+      p.L = s_len[b];
+      p.G = plan_group(a, p.L);
+      p.parts = parts_of(visits_of(b, p.block));
+      p.slot = s_slot[s_big[b] + p.block];
+      if (p.part >= p.parts) p.parts = 0;
+      a.parts[e] = p;
+    }
+  }
+  if (tid == 0) {
+    v.header[kHdParts] = n_parts;
+    v.header[kHdMembers] = n_tok;
+  }
   plan_ranges(a, v, n_segs, s_visits, s_rows, s_states, s_scan);
 }
 
@@ -955,11 +1001,11 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       seq = sg.seq;
       len = sg.kend;
     } else {  // the last row's position is kend - 1
-      seq = sg.m0 + t;
+      seq = sg.q0 + t;
       len = sg.kend - (sg.rows / a.g - 1 - t);
     }
     x.pos = max(len - 1, 0);
-    x.G = a.bifocal ? group_size(sg.len > 0 ? sg.len : len, a.w_pre) : 1;
+    x.G = rows_group(sg.len > 0 ? sg.len : len, a.bifocal, a.w_pre);
     x.lim = first_local(x.G, x.pos, a.w0);
     x.q = a.q + ((size_t)max(seq, 0) * a.Hq + h * a.g + r % a.g) * kHeadDim;
     return x;
@@ -1342,96 +1388,103 @@ __global__ __launch_bounds__(512) void merge_shared_kernel(SharedArgs a) {
   if (!plan_fits(a, pv.header)) return;
   const int h = blockIdx.y;
   const int rl = threadIdx.x & (kMgRows - 1), c = (threadIdx.x / kMgRows) & 31, half = threadIdx.x >> 8;
-  const int r = blockIdx.x * kMgRows + rl;
-  const int n_members = a.chunk ? a.T : a.B;
-  const Member mb = pv.members[min(r / a.g, n_members - 1)];
-  bool on = r < n_members * a.g && mb.seq >= 0;
-  float M = -INFINITY, den = 0.f;
-  f32x4 acc = f32x4{};
-  const float* base = a.states + (size_t)h * pv.header[kHdRows] * kShStateFloats;
-  auto join = [&](int seg, bool block) {
-    if (seg < 0) return;
-    const Segment sg = pv.segs[seg];
-    const int n = sg.n_w * state_halves(sg.rows, sg.n_views);
-    if (sg.len > 0 && n == 1) {  // written by its workgroup
-      on = false;
-      return;
+  const int n_rows = pv.header[kHdMembers] * a.g;
+  for (int r0 = blockIdx.x * kMgRows; r0 < n_rows; r0 += gridDim.x * kMgRows) {
+    const int r = r0 + rl;
+    const Member mb = pv.members[min(r, n_rows - 1) / a.g];
+    bool on = r < n_rows && mb.seq >= 0;
+    float M = -INFINITY, den = 0.f;
+    f32x4 acc = f32x4{};
+    const float* base = a.states + (size_t)h * pv.header[kHdRows] * kShStateFloats;
+    auto join = [&](int seg, bool block) {
+      if (seg < 0) return;
+      const Segment sg = pv.segs[seg];
+      const int n = sg.n_w * state_halves(sg.rows, sg.n_views);
+      if (sg.len > 0 && n == 1) {  // written by its workgroup
+        on = false;
+        return;
+      }
+      const int at = block ? r - sg.m0 * a.g : r % a.g;
+      constexpr int kAtOnce = 4;
+      for (int i0 = half; i0 < n; i0 += 2 * kAtOnce) {
+        float2 ml[kAtOnce];
+        f32x4 x[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+          const float* st = base + (size_t)(sg.row0 + min(i0 + 2 * j, n - 1) * sg.rows) * kShStateFloats;
+          ml[j] = *(const float2*)(st + (size_t)sg.rows * kHeadDim + 2 * at);
+          x[j] = *(const f32x4*)(st + ((size_t)c * sg.rows + at) * 4);
+          if (i0 + 2 * j >= n) ml[j] = make_float2(-INFINITY, 0.f);
+        }
+        float top = M;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+          if (ml[j].y == 0.f) ml[j].x = -INFINITY;  // no key of this row
+          top = fmaxf(top, ml[j].x);
+        }
+        const float wa = M == -INFINITY ? 0.f : fast_exp2(M - top);
+        den *= wa;
+        acc *= wa;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+          if (ml[j].y == 0.f) continue;
+          const float wb = fast_exp2(ml[j].x - top);
+          den += wb * ml[j].y;
+          acc += wb * x[j];
+        }
+        M = top;
+      }
+    };
+    if (on) {
+      join(mb.pre, true);
+      join(mb.suf, false);
     }
-    const int at = block ? r - sg.m0 * a.g : r % a.g;
-    constexpr int kAtOnce = 4;
-    for (int i0 = half; i0 < n; i0 += 2 * kAtOnce) {
-      float2 ml[kAtOnce];
-      f32x4 x[kAtOnce];
-#pragma unroll
-      for (int j = 0; j < kAtOnce; ++j) {
-        const float* st = base + (size_t)(sg.row0 + min(i0 + 2 * j, n - 1) * sg.rows) * kShStateFloats;
-        ml[j] = *(const float2*)(st + (size_t)sg.rows * kHeadDim + 2 * at);
-        x[j] = *(const f32x4*)(st + ((size_t)c * sg.rows + at) * 4);
-        if (i0 + 2 * j >= n) ml[j] = make_float2(-INFINITY, 0.f);
-      }
-      float top = M;
-#pragma unroll
-      for (int j = 0; j < kAtOnce; ++j) {
-        if (ml[j].y == 0.f) ml[j].x = -INFINITY;  // no key of this row
-        top = fmaxf(top, ml[j].x);
-      }
-      const float wa = M == -INFINITY ? 0.f : fast_exp2(M - top);
-      den *= wa;
-      acc *= wa;
-#pragma unroll
-      for (int j = 0; j < kAtOnce; ++j) {
-        if (ml[j].y == 0.f) continue;
-        const float wb = fast_exp2(ml[j].x - top);
-        den += wb * ml[j].y;
-        acc += wb * x[j];
-      }
-      M = top;
+    if (half == 1) {
+      s_o[c][rl] = acc;
+      s_ml[c][rl] = make_float2(M, den);
     }
-  };
-  if (on) {
-    join(mb.pre, true);
-    join(mb.suf, false);
+    __syncthreads();
+    if (half == 0 && on) {
+      const float2 ml = s_ml[c][rl];
+      const float top = fmaxf(M, ml.x);
+      f32x4 out = f32x4{};
+      float lse = -INFINITY;
+      if (den != 0.f || ml.y != 0.f) {
+        const float wa = den == 0.f ? 0.f : fast_exp2(M - top);
+        const float wb = ml.y == 0.f ? 0.f : fast_exp2(ml.x - top);
+        f32x4 sum = f32x4{};
+        if (den != 0.f) sum += wa * acc;
+        if (ml.y != 0.f) sum += wb * s_o[c][rl];
+        const float all = wa * den + wb * ml.y;
+        out = sum * (1.f / all);
+        lse = (top + log2f(all)) * 0.69314718055994531f;
+      }
+      const int hd = h * a.g + r % a.g;
+      *(bf16x4*)(a.o + ((size_t)mb.seq * a.Hq + hd) * kHeadDim + 4 * c) =
+          __builtin_convertvector(out, bf16x4);
+      if (a.lse != nullptr && c == 0) a.lse[(size_t)hd * a.T + mb.seq] = lse;
+    }
+    __syncthreads();  // s_o and s_ml are read
   }
-  if (half == 1) {
-    s_o[c][rl] = acc;
-    s_ml[c][rl] = make_float2(M, den);
-  }
-  __syncthreads();
-  if (half == 1 || !on) return;
-  const float2 ml = s_ml[c][rl];
-  const float top = fmaxf(M, ml.x);
-  f32x4 out = f32x4{};
-  float lse = -INFINITY;
-  if (den != 0.f || ml.y != 0.f) {
-    const float wa = den == 0.f ? 0.f : fast_exp2(M - top);
-    const float wb = ml.y == 0.f ? 0.f : fast_exp2(ml.x - top);
-    f32x4 sum = f32x4{};
-    if (den != 0.f) sum += wa * acc;
-    if (ml.y != 0.f) sum += wb * s_o[c][rl];
-    const float all = wa * den + wb * ml.y;
-    out = sum * (1.f / all);
-    lse = (top + log2f(all)) * 0.69314718055994531f;
-  }
-  const int hd = h * a.g + r % a.g;
-  *(bf16x4*)(a.o + ((size_t)mb.seq * a.Hq + hd) * kHeadDim + 4 * c) =
-      __builtin_convertvector(out, bf16x4);
-  if (a.lse != nullptr && c == 0) a.lse[(size_t)hd * a.T + mb.seq] = lse;
 }
 
 // ---------------------------------------------------------------- launchers
 static size_t chunk_plan_lds(int B, int T, int g) {
-  return (4 * (size_t)B + 3) * sizeof(int) + chunk_sizes(B, T, g).segs * 8 + 8;
+  return (5 * (size_t)B + 4) * sizeof(int) + chunk_sizes(B, T, g).segs * 12 + 8;
 }
 bool chunk_rows_fit(int B, int T, int g) { return chunk_plan_lds(B, T, g) <= 60 * 1024; }
 
 static hipError_t launch_plan(bool chunk, SharedPlanArgs& a, hipStream_t stream) {
   if (chunk) {
-    hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(kPlThreads), chunk_plan_lds(a.B, a.T, a.g), stream, a);
+    const bool few = a.B <= 256 && a.T <= 4096;
+    hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(few ? 256 : kPlThreads),
+                       chunk_plan_lds(a.B, a.T, a.g), stream, a);
   } else {
     const PlanSizes z = decode_sizes(a.B, a.n_groups, a.g);
     const size_t lists = z.segs * 8 + 8;
     const size_t lds = (2 * (size_t)a.B + 3 * (size_t)a.n_groups + 2) * sizeof(int) + lists;
-    hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(kPlThreads), lds, stream, a);
+    const bool few = a.B <= 128 && a.n_groups <= 128;
+    hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(few ? 256 : kPlThreads), lds, stream, a);
   }
   return hipGetLastError();
 }
@@ -1442,18 +1495,21 @@ hipError_t launch_shared_plan(bool bifocal, const int32_t* kv_lens, const int32_
                               int w0, int n_cu, void* plan, hipStream_t stream) {
   SharedPlanArgs a{kv_lens, members, group_starts, shared, nullptr, plan, B, n_groups, 0, Hq / Hkv,
                    Hkv, max_pages, page, head_workgroups(n_cu, Hkv), bifocal ? 1 : 0, w_pre, w0,
-                   nullptr};
+                   nullptr, 0};
   return launch_plan(false, a, stream);
 }
 
 static hipError_t launch_rows(SharedArgs& a, hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1) {
+  // a chunk's tokens may all be the prefill kernel's
   const long long rows = (long long)(a.chunk ? a.T : a.B) * a.g;
+  long long merges = (rows + kMgRows - 1) / kMgRows;
+  if (a.chunk) merges = std::min<long long>(merges, std::max(1, 512 / a.Hkv));
   hipError_t e = hipSuccess;
   if (ev0 != nullptr && (e = hipEventRecord(ev0, stream)) != hipSuccess) return e;
   hipLaunchKernelGGL(shared_rows_kernel, dim3((unsigned)a.n_wg * a.Hkv), dim3(kShThreads), 0, stream, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (ev1 != nullptr && (e = hipEventRecord(ev1, stream)) != hipSuccess) return e;
-  hipLaunchKernelGGL(merge_shared_kernel, dim3((unsigned)((rows + kMgRows - 1) / kMgRows), (unsigned)a.Hkv),
+  hipLaunchKernelGGL(merge_shared_kernel, dim3((unsigned)merges, (unsigned)a.Hkv),
                      dim3(512), 0, stream, a);
   return hipGetLastError();
 }
@@ -1514,7 +1570,8 @@ hipError_t launch_chunk_rows(bool bifocal, const uint16_t* q, const uint16_t* k,
   const bool blocks = chunk_blocks(B, T, g, max_pages, page);
   SharedPlanArgs p{kv_lens, nullptr, nullptr, nullptr, cu, scratch, B, 0, T, g, Hkv, max_pages,
                    page, head_workgroups(n_cu, Hkv), bifocal ? 1 : 0, w_pre, w0,
-                   blocks ? (ChunkPart*)(mem + at.parts) : nullptr};
+                   blocks ? (ChunkPart*)(mem + at.parts) : nullptr,
+                   (int)most_parts(B, T, g, head_workgroups(kShMaxWg, Hkv))};
   hipError_t e = launch_plan(true, p, stream);
   if (e != hipSuccess) return e;
   if (ev0 != nullptr && (e = hipEventRecord(ev0, stream)) != hipSuccess) return e;
@@ -1523,7 +1580,7 @@ hipError_t launch_chunk_rows(bool bifocal, const uint16_t* q, const uint16_t* k,
     const bool fused = bifocal && (long long)max_pages * page > w_pre;
     e = launch_prefill_chunks(fused, q, k, v, o, lse, rope, rope16, table, max_pages, page_shift,
                               n_pages, T, Hq, Hkv, w0, slack, p.parts, (int*)scratch + kHdParts,
-                              (int)most_parts(B, T, g, p.n_wg), (float*)(mem + at.part_states), stream);
+                              p.most_parts, (float*)(mem + at.part_states), stream);
     if (e != hipSuccess) return e;
   }
   SharedArgs a = rows_args(bifocal, q, k, v, table, max_pages, n_pages, page_shift, scratch,

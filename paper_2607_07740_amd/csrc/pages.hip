@@ -17,7 +17,7 @@ __device__ inline int pages_of(int len, int page, int max_pages) {
 }
 __device__ inline bool in_pool(int p, int n_pages) { return (unsigned)p < (unsigned)n_pages; }
 
-constexpr int kBookThreads = 1024;  // of the calls that one workgroup makes
+constexpr int kBookThreads = 1024;  // of the calls that one workgroup makes; small ones take 256
 constexpr int kBookWaves = kBookThreads / 64;
 
 // Inclusive sums over the workgroup's threads, in thread order, of one value or a
@@ -36,10 +36,14 @@ __device__ inline T block_scan(T v, T* s, T* total) {
   __syncthreads();
   T before = 0, all = 0;
 #pragma unroll
-  for (int i = 0; i < kBookWaves; ++i) {
-    const T x = s[i];
-    if (i < wave) before += x;
-    all += x;
+  for (int i = 0; i < kBookWaves; i += 4) {
+    if (64 * i >= (int)blockDim.x) break;
+#pragma unroll
+    for (int j = i; j < i + 4; ++j) {
+      const T x = s[j];
+      if (j < wave) before += x;
+      all += x;
+    }
   }
   *total = all;
   return before + incl;
@@ -61,7 +65,7 @@ __global__ __launch_bounds__(kBookThreads) void fork_kernel(ForkArgs a) {
   const Pages& p = a.p;
   const int c0 = blockIdx.x * a.cols;
   const int n = p.B * a.cols;
-  for (int i = threadIdx.x; i < n; i += kBookThreads) {
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
     const int b = i / a.cols, c = c0 + i - b * a.cols;
     const int from = a.parent[b];
     int page = -1;
@@ -70,7 +74,7 @@ __global__ __launch_bounds__(kBookThreads) void fork_kernel(ForkArgs a) {
     s_new[i] = page;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kBookThreads) {
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
     const int b = i / a.cols, c = c0 + i - b * a.cols;
     if (a.parent[b] == b || c >= p.max_pages) continue;
     int32_t* at = p.table + (size_t)b * p.max_pages + c;
@@ -82,12 +86,12 @@ __global__ __launch_bounds__(kBookThreads) void fork_kernel(ForkArgs a) {
   }
   if (blockIdx.x != 0) return;
   __syncthreads();
-  for (int b = threadIdx.x; b < p.B; b += kBookThreads) {
+  for (int b = threadIdx.x; b < p.B; b += blockDim.x) {
     const int from = a.parent[b];
     s_new[b] = (unsigned)from < (unsigned)p.B ? p.lens[from] : 0;
   }
   __syncthreads();
-  for (int b = threadIdx.x; b < p.B; b += kBookThreads) p.lens[b] = s_new[b];
+  for (int b = threadIdx.x; b < p.B; b += blockDim.x) p.lens[b] = s_new[b];
 }
 
 // ---------------------------------------------------------------- reserve
@@ -106,8 +110,7 @@ struct ReserveArgs {
   int32_t* info;   // moves, pages dealt, pages missing, sequences past max_pages
 };
 
-constexpr int kStripPer = 16;  // counts a thread reads at once
-constexpr int kStrip = kStripPer * kBookThreads;
+constexpr int kStripPer = 16;  // counts a thread reads at once; a strip: what the workgroup does
 
 // Bits of the free ones among 16 counts from `at` on
 __device__ inline uint32_t free_mask(const int32_t* refs, int at, int n_pages) {
@@ -130,41 +133,61 @@ __global__ __launch_bounds__(kBookThreads) void reserve_kernel(ReserveArgs a) {
   extern __shared__ int32_t smem[];
   __shared__ unsigned long long s_scan[kBookWaves];
   const Pages& p = a.p;
-  int32_t* const s_first = smem;            // needs before sequence b
-  int32_t* const s_had = s_first + p.B;     // its pages
-  int32_t* const s_move = s_had + p.B;      // its move; -1: no page is replaced, -2: without a copy
-  int32_t* const s_last = s_move + p.B;     // the shared page it writes into, else -1
-  const int tid = threadIdx.x;
+  int32_t* const s_last = smem;              // the shared page it writes into, else -1 (16-byte aligned)
+  int32_t* const s_first = s_last + ((p.B + 3) & ~3);  // needs before sequence b
+  int32_t* const s_had = s_first + p.B;      // its pages
+  int32_t* const s_move = s_had + p.B;       // its move; -1: no page is replaced, -2: without a copy
+  int32_t* const s_len = s_move + p.B;
+  const int tid = threadIdx.x, nt = blockDim.x, strip_pages = kStripPer * nt;
 
   // the counts of the first strip, on their way while the needs are formed
-  const int n_strips = (p.n_pages + kStrip - 1) / kStrip;
+  const int n_strips = (p.n_pages + strip_pages - 1) / strip_pages;
   uint32_t mask0 = free_mask(p.refs, min(tid * kStripPer, p.n_pages), p.n_pages);
 
-  for (int b = tid; b < p.B; b += kBookThreads) {
+  const int per = (p.B + nt - 1) >> (31 - __builtin_clz(nt));
+  const int b0 = min(tid * per, p.B), b1 = min(b0 + per, p.B);
+  for (int b = b0; b < b1; ++b) {
     const int len = max(p.lens[b], 0);
-    int last = -1;
-    if (a.n_new[b] > 0 && len % p.page != 0 && len / p.page < p.max_pages) {
-      const int e = p.table[(size_t)b * p.max_pages + len / p.page];
-      last = in_pool(e, p.n_pages) ? (p.refs[e] > 1 ? e : -1) : -2;
+    int last = -1, count = 0;
+    const int slot = (int)((unsigned)len / (unsigned)p.page);
+    if (a.n_new[b] > 0 && len != slot * p.page && slot < p.max_pages) {
+      const int e = p.table[(size_t)b * p.max_pages + slot];
+      last = -2;
+      if (in_pool(e, p.n_pages)) {
+        count = p.refs[e];
+        last = count > 1 ? e : -1;
+      }
     }
     s_last[b] = last;
+    s_first[b] = count;
+    s_len[b] = len;
   }
   __syncthreads();
-  const int per = (p.B + kBookThreads - 1) / kBookThreads;
-  const int b0 = min(tid * per, p.B), b1 = min(b0 + per, p.B);
+  const int cap = p.max_pages * p.page;
   long long need = 0;
   int n_moves = 0, over = 0;
   for (int b = b0; b < b1; ++b) {
-    const int len = max(p.lens[b], 0), n = max(a.n_new[b], 0);
-    const long long has = ((long long)len + n + p.page - 1) / p.page;
-    const int had = (int)(((long long)len + p.page - 1) / p.page);
+    // a length of any kind past the capacity counts as one just past it
+    const int len = s_len[b], n = max(a.n_new[b], 0);
+    const unsigned end = min((unsigned)len + (unsigned)n, (unsigned)cap + 1u);
+    const int has = end == 0 ? 0 : (int)((end - 1) / (unsigned)p.page + 1);
+    const int had = min(len == 0 ? 0 : (int)((unsigned)(len - 1) / (unsigned)p.page + 1), has);
     const int last = s_last[b];
     int move = -1;
     if (last == -2) {
       move = -2;
     } else if (last >= 0) {
-      int left = p.refs[last];  // less the writers before this one
-      for (int e = 0; e < b; ++e) left -= s_last[e] == last;
+      int left = s_first[b];  // less the writers before this one
+      int e = 0;
+      for (; e + 16 <= b; e += 16) {
+        int4 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = ((const int4*)(s_last + e))[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          left -= (x[i].x == last) + (x[i].y == last) + (x[i].z == last) + (x[i].w == last);
+      }
+      for (; e < b; ++e) left -= s_last[e] == last;
       if (left > 1) move = n_moves++;
     }
     over += has > p.max_pages && n > 0;
@@ -182,7 +205,7 @@ __global__ __launch_bounds__(kBookThreads) void reserve_kernel(ReserveArgs a) {
       (unsigned long long)over << 40;
   uint32_t n_free = __popc(mask0);
   for (int s = 1; s < n_strips; ++s)
-    n_free += __popc(free_mask(p.refs, min(s * kStrip + tid * kStripPer, p.n_pages), p.n_pages));
+    n_free += __popc(free_mask(p.refs, min(s * strip_pages + tid * kStripPer, p.n_pages), p.n_pages));
   block_scan(over_free + n_free, s_scan, &tot2);
   const long long total = (long long)(tot & ((1ull << 44) - 1));
   const long long all_free = (long long)(tot2 & ((1ull << 40) - 1));
@@ -200,9 +223,9 @@ __global__ __launch_bounds__(kBookThreads) void reserve_kernel(ReserveArgs a) {
     a.info[2] = (int)min(max(total - all_free, 0LL), 0x7fffffffLL);
     a.info[3] = all_over;
   }
-  for (int b = tid; b < p.B; b += kBookThreads) {
+  for (int b = tid; b < p.B; b += nt) {
     const int n = fits ? max(a.n_new[b], 0) : 0;
-    const int len = max(p.lens[b], 0);
+    const int len = s_len[b];
     a.starts[b] = len;
     a.granted[b] = n;
     if (n > 0) p.lens[b] = len + n;
@@ -215,7 +238,7 @@ __global__ __launch_bounds__(kBookThreads) void reserve_kernel(ReserveArgs a) {
   if (!fits || total == 0) return;
   unsigned long long base = 0;
   for (int s = 0; s < n_strips && base < (unsigned long long)total; ++s) {
-    const int at = min(s * kStrip + tid * kStripPer, p.n_pages);
+    const int at = min(s * strip_pages + tid * kStripPer, p.n_pages);
     // pages dealt in an earlier strip are not read again, and the counts lowered
     // above stay positive
     uint32_t m = s == 0 ? mask0 : free_mask(p.refs, at, p.n_pages);
@@ -257,12 +280,12 @@ struct CompactArgs {
 __global__ __launch_bounds__(kBookThreads) void compact_kernel(CompactArgs a) {
   __shared__ unsigned long long s_scan[kBookWaves];
   const Pages& p = a.p;
-  const int tid = threadIdx.x;
-  const int n_strips = (p.n_pages + kStrip - 1) / kStrip;
+  const int tid = threadIdx.x, nt = blockDim.x, strip_pages = kStripPer * nt;
+  const int n_strips = (p.n_pages + strip_pages - 1) / strip_pages;
   uint32_t mask0 = 0;
   unsigned long long used = 0, n_live;
   for (int s = 0; s < n_strips; ++s) {
-    const int at = min(s * kStrip + tid * kStripPer, p.n_pages);
+    const int at = min(s * strip_pages + tid * kStripPer, p.n_pages);
     const uint32_t m = free_mask(p.refs, at, p.n_pages);
     if (s == 0) mask0 = m;
     used += min(kStripPer, p.n_pages - at) - __popc(m);
@@ -271,7 +294,7 @@ __global__ __launch_bounds__(kBookThreads) void compact_kernel(CompactArgs a) {
   const int live = (int)n_live;
   unsigned long long base = 0;  // free pages below `live` (low half), used ones above it
   for (int s = 0; s < n_strips; ++s) {
-    const int at = min(s * kStrip + tid * kStripPer, p.n_pages);
+    const int at = min(s * strip_pages + tid * kStripPer, p.n_pages);
     const uint32_t m = s == 0 ? mask0 : free_mask(p.refs, at, p.n_pages);
     const int n = min(kStripPer, p.n_pages - at);
     const uint32_t below = live >= at + 16 ? 0xffffu : live <= at ? 0u : (1u << (live - at)) - 1;
@@ -287,7 +310,7 @@ __global__ __launch_bounds__(kBookThreads) void compact_kernel(CompactArgs a) {
   }
   const int n_moves = (int)(uint32_t)base;  // as many free ones below as used ones above
   __syncthreads();
-  for (int i = tid; i < p.n_pages / 2; i += kBookThreads) {
+  for (int i = tid; i < p.n_pages / 2; i += nt) {
     if (i < n_moves) {
       const int from = a.moves[2 * i], to = a.moves[2 * i + 1];
       a.to[from] = to;
@@ -416,17 +439,22 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_kernel(AppendArgs a)
 }
 
 // ---------------------------------------------------------------- launchers
-static int fork_cols(int B) {
-  int c = 32;  // 128 bytes of a row, 64 KB in all
+// Barriers of four waves cost less; more counts than four of their strips take the larger one
+static int book_threads(const Pages& p) {
+  return p.B <= 256 && p.n_pages <= 4 * 256 * kStripPer ? 256 : kBookThreads;
+}
+static int fork_cols(int B, int max_pages) {
+  int c = 32;  // 128 bytes of a row, 64 KB in all; fewer where the grid would not fill the CUs
+  while (c > 8 && max_pages / c < 128) c /= 2;
   while (c > 1 && (size_t)c * B * sizeof(int32_t) > (size_t)64 * 1024) c /= 2;
   return c;
 }
 
 hipError_t launch_pages_fork(const Pages& p, const int32_t* parent, hipStream_t stream) {
-  ForkArgs a{p, parent, fork_cols(p.B)};
+  ForkArgs a{p, parent, fork_cols(p.B, p.max_pages)};
   const int grid = (int)(((long long)p.max_pages + a.cols - 1) / a.cols);
   const size_t lds = (size_t)a.cols * p.B * sizeof(int32_t);
-  hipLaunchKernelGGL(fork_kernel, dim3(grid), dim3(kBookThreads), lds, stream, a);
+  hipLaunchKernelGGL(fork_kernel, dim3(grid), dim3(p.B * a.cols <= 1024 ? 256 : kBookThreads), lds, stream, a);
   return hipGetLastError();
 }
 
@@ -434,14 +462,14 @@ hipError_t launch_pages_reserve(const Pages& p, const int32_t* n_new, int32_t* s
                                 int32_t* granted, int32_t* moves, int32_t* info,
                                 hipStream_t stream) {
   ReserveArgs a{p, n_new, starts, granted, moves, info};
-  hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kBookThreads), (size_t)p.B * 16, stream, a);
+  hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(book_threads(p)), (size_t)(p.B + 3) * 20, stream, a);
   return hipGetLastError();
 }
 
 hipError_t launch_pages_compact(const Pages& p, int32_t* moves, int32_t* to, int32_t* info,
                                 hipStream_t stream) {
   CompactArgs a{p, moves, to, info};
-  hipLaunchKernelGGL(compact_kernel, dim3(1), dim3(kBookThreads), 0, stream, a);
+  hipLaunchKernelGGL(compact_kernel, dim3(1), dim3(book_threads(p)), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const size_t n = (size_t)p.B * p.max_pages;

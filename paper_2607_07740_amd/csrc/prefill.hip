@@ -904,6 +904,7 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_chunks_kernel(PrefillAr
   if (at >= *(const const_int*)a.n_chunk_parts) return;
   const const_int* src = (const const_int*)(a.chunk_parts + at);
   const ChunkPart p = {src[0], src[1], src[2], src[3], src[4], src[5], src[6], src[7], src[8], {}};
+  if (p.parts == 0) return;
   const Work W = chunk_work(a, p, kvh);
   float* state = chunk_state(a, p, p.part, kvh);
   if (prefill_block<MODE, false, true, true, kPfWaves>(a, W, smem, &s_bad, s_pages, p.part, p.parts,
