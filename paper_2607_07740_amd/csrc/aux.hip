@@ -34,6 +34,20 @@ __global__ void build_table_kernel(float2* table, uint32_t* table16, int n_pos, 
   if (table16 != nullptr) table16[idx] = bf16_bits_rne(c) | (bf16_bits_rne(s) << 16);
 }
 
+// The same pairs in fp16
+__global__ void half_table_kernel(const float2* table, uint32_t* half, int n_pos) {
+  const long long idx = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  if (idx >= (long long)n_pos * kHalf) return;
+  half[idx] = pack_f16(table[idx].x, table[idx].y);
+}
+
+hipError_t launch_half_table(const float2* table, uint32_t* half, int n_pos, hipStream_t stream) {
+  const long long n = (long long)n_pos * kHalf;
+  hipLaunchKernelGGL(half_table_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream,
+                     table, half, n_pos);
+  return hipGetLastError();
+}
+
 hipError_t launch_build_table(float2* table, uint32_t* table16, int n_pos, const double* omega,
                               hipStream_t stream) {
   Omega om;

@@ -76,9 +76,12 @@ struct Member {
   int len;       // its position + 1
   int pre, suf;  // its segments, -1: none
 };
-// States that a (workgroup, segment) leaves
-__host__ __device__ inline int state_halves(int rows, int n_views) {
-  return rows <= kShFew && n_views > 1 ? 2 : 1;
+// States that a (workgroup, segment) leaves.  Up to 64 rows, two pairs of waves take the visits in
+// turn where most tiles have two, their second from the caches (16 samples of 32K, G = 1 and 2: 104 ->
+// 96 us); where memory sets the pace the second states cost more (64 chats: 130 -> 137).
+__host__ __device__ inline int state_halves(const Segment& s) {
+  const int tiles = (s.kend - s.k0 + kShTile - 1) / kShTile;
+  return s.rows <= kShFew && 2LL * s.visits > 3LL * tiles ? 2 : 1;
 }
 
 struct PlanView {
@@ -473,7 +476,7 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
       v.segs[blk] = s;
       s_visits[blk] = s.visits;
       s_rows[blk] = (short)s.rows;
-      s_states[blk] = (short)(s.rows * state_halves(s.rows, s.n_views));
+      s_states[blk] = (short)(s.rows * state_halves(s));
     }
   }
   // the members' own keys
@@ -499,7 +502,7 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
     v.segs[seg] = s;
     s_visits[seg] = s.visits;
     s_rows[seg] = (short)s.rows;
-    s_states[seg] = (short)(s.rows * state_halves(s.rows, s.n_views));
+    s_states[seg] = (short)(s.rows * state_halves(s));
   }
   __syncthreads();
   plan_ranges(a, v, n_blocks + a.B, s_visits, s_rows, s_states, s_scan);
@@ -598,7 +601,7 @@ __global__ __launch_bounds__(kPlThreads) void chunk_plan_kernel(SharedPlanArgs a
     v.segs[seg] = s;
     s_visits[seg] = s.visits;
     s_rows[seg] = (short)s.rows;
-    s_states[seg] = (short)(s.rows * state_halves(s.rows, s.n_views));
+    s_states[seg] = (short)(s.rows * state_halves(s));
   }
   for (int t = tid; t < n_tok; t += nt) {
     const int b = find(s_tok, t), i = t - s_tok[b];
@@ -687,12 +690,14 @@ struct SharedArgs {
   uint16_t* o;
   float* lse;  // [Hq][T] of a chunk, or nullptr
   const float2* rope;
-  const uint32_t* rope16;
+  const uint32_t* half;    // the same in fp16, one word a pair
+  const uint32_t* rope16;  // and in bf16
   void* plan;
   float* states;
   int B, n_groups, T, Hq, Hkv, g, max_pages, n_pages, page, page_shift, n_wg;
   int chunk, bifocal, w_pre, w0;
   float q_scale;
+  int g_inv;  // floor(2^16 / g) + 1
 };
 
 __device__ inline PlanView plan_of(const SharedArgs& a) {
@@ -726,10 +731,25 @@ constexpr int kTfLast = 32, kTfSeg = 9;
 typedef __bf16 sh_bf16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned sh_u32x2 __attribute__((ext_vector_type(2)));
 
-// One rotate-half slice pair of a query row: channels d .. d + 7 and d + 64 .. d + 71,
-// rotated to position pos and scaled, as matrix operands.
+// Keys and queries are multiplied in fp16, whose 11 bits hold the rotated values eight times as
+// well as bf16 would: at 16 samples of 32K the output's distance from 64 bits falls from 0.0047
+// of its size to 0.0024 (0.0017 is the output's own rounding).  A range that meets a row whose
+// largest channel fp16 holds less well, outside [2^-8, 2^15), is done again in bf16.
+constexpr float kShLow = 1.f / 256.f, kShHigh = 32768.f;
+__device__ inline bool sh_outside(float amax) {  // of a whole row; nor does bf16 help inf and NaN
+  return (amax > 0.f && amax < kShLow) || (amax >= kShHigh && amax < INFINITY);
+}
+
+__device__ inline float sh_max32(float x) {  // over lanes l and l ^ 32
+  const sh_u32x2 r =
+      __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+// Channels d .. d + 7 and d + 64 .. d + 71 of a query row, rotated to position pos and scaled, as
+// operands; amax: the largest of them
+template <typename Op>
 __device__ inline void sh_rotate_q(const uint16_t* qrow, int d, const float2* table, int pos,
-                                   float scale, bf16x8& olo, bf16x8& ohi) {
+                                   float scale, Op& olo, Op& ohi, float& amax) {
   float lo[8], hi[8], ylo[8], yhi[8];
   unpack8(load16(qrow + d), lo);
   unpack8(load16(qrow + d + kHalf), hi);
@@ -743,23 +763,17 @@ __device__ inline void sh_rotate_q(const uint16_t* qrow, int d, const float2* ta
     ylo[j + 1] = (lo[j + 1] * w.z - hi[j + 1] * w.w) * scale;
     yhi[j + 1] = (hi[j + 1] * w.z + lo[j + 1] * w.w) * scale;
   }
-  olo = pack8(ylo);
-  ohi = pack8(yhi);
-}
-
-__device__ inline f32x4 sh_mfma16k16(i16x4 a, bf16x4 b, f32x4 c) {
-  typedef short i16x4v __attribute__((ext_vector_type(4)));
-  return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, __builtin_bit_cast(i16x4v, b), c, 0, 0, 0);
-}
-__device__ inline float sh_max32(float x) {  // over lanes l and l ^ 32
-  const sh_u32x2 r =
-      __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ inline float sh_max16_32(float x) {  // over lanes l, l ^ 16, l ^ 32, l ^ 48
-  const sh_u32x2 r =
-      __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return sh_max32(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+  if constexpr (std::is_same_v<Op, bf16x8>) {
+    olo = pack8(ylo);
+    ohi = pack8(yhi);
+  } else {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      olo[t] = (_Float16)ylo[t];
+      ohi[t] = (_Float16)yhi[t];
+      amax = fmaxf(amax, fmaxf(fabsf(ylo[t]), fabsf(yhi[t])));
+    }
+  }
 }
 
 // A tile's weights of a row may add up to this before the row's reference moves: far inside
@@ -771,6 +785,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
   __shared__ __attribute__((aligned(16))) Tile s_tiles[kShList];
   __shared__ __attribute__((aligned(16))) Segment s_segs[kShSegs];
   __shared__ int s_from[kShSegs], s_before[kShSegs];  // first visit here, visits of earlier ones
+  __shared__ int s_again;                             // rows that fp16 does not hold were met
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -819,7 +834,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
                  (uint32_t)(256 * key + 16 * slot)};
   };
   // requests keys key0 .. key0 + 3 of K and V, and their cos/sin rows
-  auto copy4 = [&](auto all, const Tile& t, int ln, int key0, const Piece& pc, uint32_t buf) __attribute__((always_inline)) {
+  auto copy4 = [&](auto all, auto half, const Tile& t, int ln, int key0, const Piece& pc, uint32_t buf) __attribute__((always_inline)) {
     const int klim = t.flags & 31;
     const uint32_t dst = buf + 256 * key0;
     uint32_t ko = pc.k, vo = pc.v, co = pc.cs;
@@ -848,7 +863,8 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       const FastDiv f = {t.m, t.lG & 63, 2};
       co = fastdiv_ge2((uint32_t)(t.km + key), f) * 256 + 16 * (ln & 15);
     }
-    dma16_s(a.rope16 + (size_t)(t.lG != 0 ? t.f0 : t.k0) * 64, co, dst + 2 * kShImg);
+    const uint32_t* const cs = decltype(half)::value ? a.half : a.rope16;
+    dma16_s(cs + (size_t)(t.lG != 0 ? t.f0 : t.k0) * 64, co, dst + 2 * kShImg);
   };
   // The copies of a wave, in the order of the list; a visit's description is read one ahead
   struct Copier {
@@ -863,20 +879,26 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     peek(c, 0);
     return c;
   };
-  auto issue = [&](auto all, Copier& c, int ln, int j) __attribute__((always_inline)) {
+  auto issue = [&](auto all, auto half, Copier& c, int ln, int j) __attribute__((always_inline)) {
     const Tile t = {uni(c.nx.row0), uni(c.nx.row1), uni(c.nx.k0), uni(c.nx.flags), uni(c.nx.f0),
                     uni(c.nx.km), (uint32_t)uni((int)c.nx.m), (uint32_t)uni((int)c.nx.lG)};
     peek(c, j + 1);
     const uint32_t buf = smem_base + (uint32_t)(j % kShBufs) * kShBuf;
     if constexpr (decltype(all)::value) {
-      copy4(all, t, ln, 4 * wave, c.pc[0], buf);
+      copy4(all, half, t, ln, 4 * wave, c.pc[0], buf);
     } else {
-      copy4(all, t, ln, 8 * (wave - 4), c.pc[0], buf);
-      copy4(all, t, ln, 8 * (wave - 4) + 4, c.pc[1], buf);
+      copy4(all, half, t, ln, 8 * (wave - 4), c.pc[0], buf);
+      copy4(all, half, t, ln, 8 * (wave - 4) + 4, c.pc[1], buf);
     }
   };
+  // Whether fp16 holds the keys of a wave, each spread over some lanes
+  auto check = [&](float amax, int lanes) __attribute__((always_inline)) {
+    if (__ballot(!(amax >= kShLow && amax < kShHigh)) == 0) return;
+    for (int d = 1; d < lanes; d <<= 1) amax = fmaxf(amax, __shfl_xor(amax, d));
+    if (sh_outside(amax)) s_again = 1;
+  };
   // Rotation in place.  4 keys: lane -> key, half of a chunk pair; 8 keys: lane -> key, chunk pair
-  auto rotate = [&](auto all, int ln, int j) __attribute__((always_inline)) {
+  auto rotate = [&](auto all, auto half, int ln, int j) __attribute__((always_inline)) {
     unsigned char* b = smem + (j % kShBufs) * kShBuf;
     if constexpr (decltype(all)::value) {
       const int r4_key = 4 * wave + (ln >> 4), r4_c = (ln >> 1) & 7, r4_h = ln & 1;
@@ -884,6 +906,15 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       const int r4_cs = 2 * kShImg + r4_key * 256 + 32 * r4_c + 16 * r4_h;
       const sh_u32x2 xl = *(const sh_u32x2*)(b + r4_lo), xh = *(const sh_u32x2*)(b + r4_hi);
       const u32x4 cs = *(const u32x4*)(b + r4_cs);
+      if constexpr (decltype(half)::value) {
+        float v[8], amax = 0.f;
+        rot_pairs_f16(xl[0], xh[0], cs[0], cs[1], v, amax);
+        rot_pairs_f16(xl[1], xh[1], cs[2], cs[3], v + 4, amax);
+        *(sh_u32x2*)(b + r4_lo) = sh_u32x2{pack_f16(v[0], v[1]), pack_f16(v[4], v[5])};
+        *(sh_u32x2*)(b + r4_hi) = sh_u32x2{pack_f16(v[2], v[3]), pack_f16(v[6], v[7])};
+        check(amax, 16);
+        return;
+      }
       uint32_t l0, h0, l1, h1;
       rot_word_dot2(xl[0], xh[0], cs[0], cs[1], l0, h0);
       rot_word_dot2(xl[1], xh[1], cs[2], cs[3], l1, h1);
@@ -896,6 +927,21 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       const u32x4 xl = *(const u32x4*)(b + r8_lo), xh = *(const u32x4*)(b + r8_hi);
       const u32x4 ca = *(const u32x4*)(b + r8_cs), cb = *(const u32x4*)(b + r8_cs + 16);
       u32x4 lo, hi;
+      if constexpr (decltype(half)::value) {
+        float amax = 0.f;
+#pragma unroll
+        for (int w2 = 0; w2 < 4; ++w2) {
+          float v[4];
+          rot_pairs_f16(xl[w2], xh[w2], w2 < 2 ? ca[2 * w2] : cb[2 * w2 - 4],
+                        w2 < 2 ? ca[2 * w2 + 1] : cb[2 * w2 - 3], v, amax);
+          lo[w2] = pack_f16(v[0], v[1]);
+          hi[w2] = pack_f16(v[2], v[3]);
+        }
+        *(u32x4*)(b + r8_lo) = lo;
+        *(u32x4*)(b + r8_hi) = hi;
+        check(amax, 8);
+        return;
+      }
 #pragma unroll
       for (int w2 = 0; w2 < 4; ++w2) {
         uint32_t l, hh;
@@ -965,24 +1011,27 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
   };
   // Beside visit i: the request of the tile that takes visit i - 2's buffer, the next one's
   // rotation
-  auto produce = [&](auto all, Copier& cp, int ln, int i) __attribute__((always_inline)) {
-    if (i + kShAhead < n) issue(all, cp, ln, i + kShAhead);
-    if (i + 1 < n) rotate(all, ln, i + 1);
+  auto produce = [&](auto all, auto half, Copier& cp, int ln, int i) __attribute__((always_inline)) {
+    if (i + kShAhead < n) issue(all, half, cp, ln, i + kShAhead);
+    if (i + 1 < n) rotate(all, half, ln, i + 1);
   };
   auto refill = [&](int i) __attribute__((always_inline)) {
     if ((i & (kShList / 2 - 1)) == 0 && i > 0 && i + kShList / 2 < n) fill(i + kShList / 2);
   };
-  auto start = [&](auto all, Copier& cp, int ln) __attribute__((always_inline)) {
+  auto start = [&](auto all, auto half, Copier& cp, int ln) __attribute__((always_inline)) {
     constexpr int k = decltype(all)::value ? kShCopies : 2 * kShCopies;
     const int first = min(n, kShAhead);
-    for (int j = 0; j < first; ++j) issue(all, cp, ln, j);
+    for (int j = 0; j < first; ++j) issue(all, half, cp, ln, j);
     if (first == kShAhead)
       wait_vmem_n<(kShAhead - 1) * k>();
     else
       wait_vmem();
-    rotate(all, ln, 0);
+    rotate(all, half, ln, 0);
   };
 
+  // Row of a segment (up to 256) over the query heads of a kv head: the inverse is less than
+  // 2^-16 too large, so the quotient of 256 less than 1 / g
+  auto by_g = [&](int r) { return (int)((uint32_t)r * (uint32_t)a.g_inv >> 16); };
   // The row that a lane serves: its query, position, G and first local key
   struct Row {
     const uint16_t* q;
@@ -991,7 +1040,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
   auto row_of = [&](const Segment& sg, int r) {
     Row x;
     r = min(r, sg.rows - 1);
-    const int t = r / a.g;
+    const int t = by_g(r);
     int seq, len;
     if (sg.kind == kSegShared) {
       const Member mb = pv.members[sg.m0 + t];
@@ -1002,12 +1051,12 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       len = sg.kend;
     } else {  // the last row's position is kend - 1
       seq = sg.q0 + t;
-      len = sg.kend - (sg.rows / a.g - 1 - t);
+      len = sg.kend - (by_g(sg.rows) - 1 - t);
     }
     x.pos = max(len - 1, 0);
     x.G = rows_group(sg.len > 0 ? sg.len : len, a.bifocal, a.w_pre);
     x.lim = first_local(x.G, x.pos, a.w0);
-    x.q = a.q + ((size_t)max(seq, 0) * a.Hq + h * a.g + r % a.g) * kHeadDim;
+    x.q = a.q + ((size_t)max(seq, 0) * a.Hq + h * a.g + r - t * a.g) * kHeadDim;
     return x;
   };
   // Keys [lo, hi) of the tile that a row keeps: in the remote view those before its first
@@ -1021,7 +1070,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       *lo = x.lim - k0;
   };
   auto state_at = [&](const Segment& sg, int half) {
-    const int rows = uni(sg.rows), halves = state_halves(rows, uni(sg.n_views));
+    const int rows = uni(sg.rows), halves = uni(state_halves(sg));
     return a.states + ((size_t)h * all_rows + uni(sg.row0) +
                        (size_t)((w - uni(sg.w_first)) * halves + half) * rows) * kShStateFloats;
   };
@@ -1029,7 +1078,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
   // ---- the visits of a segment from i on, by the waves that hold its rows: 32 of them and all
   // keys of a tile each.  The scores of visit i are formed beside the softmax and the value
   // product of visit i - 1, whose tile stays in its buffer until then.
-  auto consume = [&](auto all, auto few, Copier& cp, int i) __attribute__((always_inline)) {
+  auto consume = [&](auto all, auto few, auto half, Copier& cp, int i) __attribute__((always_inline)) {
     int ln = lane;  // what follows from it is formed here: held across all loops it would spill
     asm volatile("" : "+v"(ln));
     const Segment& sg = s_segs[uni(s_tiles[i & (kShList - 1)].flags) >> kTfSeg];
@@ -1037,18 +1086,19 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     const int hl32 = ln >> 5, kr_lane = ln & 31;
     const int vk_lane = 4 * hl32 + ((ln & 15) >> 2);
     const int vc_lane = 2 * ((ln >> 4) & 1) + ((ln & 3) >> 1);
-    constexpr bool ALL = decltype(all)::value, FEW = decltype(few)::value;
+    constexpr bool FEW = decltype(few)::value;
+    using Op = std::conditional_t<decltype(half)::value, f16x8, bf16x8>;
     const int rw = FEW ? wave & 1 : wave, set = wave >> 1;
     const int row = 32 * rw + kr_lane;
     const bool on = 32 * rw < rows;
     const Row x = row_of(sg, row);
-    bf16x8 qop[8];
+    Op qop[8];
     f32x16 acc[4], nx_sc = f32x16{}, neg_m = f32x16{};
     float m_ref = 0.f, l_run = 0.f;
 #pragma unroll
     for (int d = 0; d < 4; ++d) acc[d] = f32x16{};
 #pragma unroll
-    for (int s = 0; s < 8; ++s) qop[s] = bf16x8{};
+    for (int s = 0; s < 8; ++s) qop[s] = Op{};
     int q_view = -1;
 
     // the visit's scalars, read a visit ahead
@@ -1066,22 +1116,26 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       nx_k0 = t.k0;
       nx_lG = t.lG;
       if constexpr (decltype(all)::value) {
-        produce(all, cp, ln, i);
+        produce(all, half, cp, ln, i);
         refill(i);
       }
       if (on && (view_G > 0) != q_view && (!FEW || (i & 1) == set)) {
         q_view = view_G > 0;
         const int pos = view_G > 0 ? x.pos / x.G : x.pos;
+        float amax = 0.f;
 #pragma unroll
         for (int s = 0; s < 4; ++s)
-          sh_rotate_q(x.q, 16 * s + 8 * hl32, a.rope, pos, a.q_scale, qop[s], qop[s + 4]);
+          sh_rotate_q(x.q, 16 * s + 8 * hl32, a.rope, pos, a.q_scale, qop[s], qop[s + 4], amax);
+        if constexpr (decltype(half)::value) {
+          if (sh_outside(sh_max32(amax))) s_again = 1;
+        }
       }
     };
     // S^T = K Q^T - m of visit i: its key operands are requested ahead, then multiplied
     constexpr int kKr = FEW ? 8 : 4;
-    bf16x8 kr[kKr];
+    Op kr[kKr];
     auto kop = [&](int s) __attribute__((always_inline)) {
-      return *(const bf16x8*)(smem + (i % kShBufs) * kShBuf + sh_koff(kr_lane, 2 * s + hl32));
+      return *(const Op*)(smem + (i % kShBufs) * kShBuf + sh_koff(kr_lane, 2 * s + hl32));
     };
     auto keys = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -1255,10 +1309,11 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     }
     if (row < rows) {
       if (!FEW && sg.len > 0 && sg.n_w == 1) {  // a chunk's block that is whole here
-        const Member mb = pv.members[sg.m0 + row / a.g];
+        const int t = by_g(row);
+        const Member mb = pv.members[sg.m0 + t];
         if (mb.seq >= 0) {
           const float inv = 1.f / l_run;
-          const int hd = h * a.g + row % a.g;
+          const int hd = h * a.g + row - t * a.g;
           uint16_t* o = a.o + ((size_t)mb.seq * a.Hq + hd) * kHeadDim;
           if (a.lse != nullptr && hl32 == 0)
             a.lse[(size_t)hd * a.T + mb.seq] = (m_ref + log2f(l_run)) * 0.69314718055994531f;
@@ -1266,10 +1321,10 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
           for (int db = 0; db < 4; ++db) {
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4) {
-              f32x4 t;
+              f32x4 y;
 #pragma unroll
-              for (int jj = 0; jj < 4; ++jj) t[jj] = acc[db][4 * q4 + jj] * inv;
-              *(bf16x4*)(o + 32 * db + 8 * q4 + 4 * hl32) = __builtin_convertvector(t, bf16x4);
+              for (int jj = 0; jj < 4; ++jj) y[jj] = acc[db][4 * q4 + jj] * inv;
+              *(bf16x4*)(o + 32 * db + 8 * q4 + 4 * hl32) = __builtin_convertvector(y, bf16x4);
             }
           }
         }
@@ -1288,6 +1343,10 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
         if (hl32 == 0)
           *(float2*)(st + (size_t)rows * kHeadDim + 2 * row) =
               make_float2(l_run == 0.f ? -INFINITY : m_ref, l_run);
+        if constexpr (!decltype(half)::value) {  // all by one wave here: the second state is empty
+          if (hl32 == 0 && uni(state_halves(sg)) == 2)
+            *(float2*)(state_at(sg, 1) + (size_t)rows * kHeadDim + 2 * row) = make_float2(-INFINITY, 0.f);
+        }
       }
     }
     return i + 1;
@@ -1343,7 +1402,8 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     n = uni(s_tiles[0].k0);
     const int next = uni(s_tiles[0].row0), kind = uni(s_tiles[0].row1);
     __syncthreads();
-    if (n > 0) {
+    auto run = [&](auto half) __attribute__((always_inline)) {
+      if (tid == 0) s_again = 0;
       fill(0);
       fill(kShList / 2);
       __syncthreads();
@@ -1351,26 +1411,35 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
         int ln = lane;
         asm volatile("" : "+v"(ln));
         Copier cp = copier(std::true_type{}, ln);
-        start(std::true_type{}, cp, ln);
-        for (int i = 0; i < n;) i = consume(std::true_type{}, std::false_type{}, cp, i);
+        start(std::true_type{}, half, cp, ln);
+        for (int i = 0; i < n;) i = consume(std::true_type{}, std::false_type{}, half, cp, i);
       } else if (wave < 4) {
         Copier none;
         for (int i = 0; i < n;) {
           const Segment& sg = s_segs[uni(s_tiles[i & (kShList - 1)].flags) >> kTfSeg];
-          i = state_halves(uni(sg.rows), uni(sg.n_views)) == 2 ? consume(std::false_type{}, std::true_type{}, none, i)
-                             : consume(std::false_type{}, std::false_type{}, none, i);
+          i = decltype(half)::value && uni(state_halves(sg)) == 2
+                  ? consume(std::false_type{}, std::true_type{}, half, none, i)
+                  : consume(std::false_type{}, std::false_type{}, half, none, i);
         }
       } else {
         int ln = lane;
         asm volatile("" : "+v"(ln));
         Copier cp = copier(std::false_type{}, ln);
-        start(std::false_type{}, cp, ln);
+        start(std::false_type{}, half, cp, ln);
         for (int i = 0; i < n; ++i) {
           landed(std::false_type{}, i);
           __syncthreads();
-          produce(std::false_type{}, cp, ln, i);
+          produce(std::false_type{}, half, cp, ln, i);
           refill(i);
         }
+      }
+    };
+    if (n > 0) {
+      run(std::true_type{});
+      __syncthreads();
+      if (uni(s_again) != 0) {
+        __syncthreads();
+        run(std::false_type{});
       }
     }
     s0 = next;
@@ -1399,7 +1468,7 @@ __global__ __launch_bounds__(512) void merge_shared_kernel(SharedArgs a) {
     auto join = [&](int seg, bool block) {
       if (seg < 0) return;
       const Segment sg = pv.segs[seg];
-      const int n = sg.n_w * state_halves(sg.rows, sg.n_views);
+      const int n = sg.n_w * state_halves(sg);
       if (sg.len > 0 && n == 1) {  // written by its workgroup
         on = false;
         return;
@@ -1517,7 +1586,7 @@ static hipError_t launch_rows(SharedArgs& a, hipStream_t stream, hipEvent_t ev0,
 static SharedArgs rows_args(bool bifocal, const uint16_t* q, const uint16_t* k, const uint16_t* v,
                             const int32_t* table, int max_pages, int n_pages, int page_shift,
                             void* plan, void* states, uint16_t* o, const float2* rope,
-                            const uint32_t* rope16, int B, int Hq, int Hkv, int w_pre, int w0,
+                            const uint32_t* half, const uint32_t* rope16, int B, int Hq, int Hkv, int w_pre, int w0,
                             int n_cu) {
   SharedArgs a = {};
   a.q = q;
@@ -1526,6 +1595,7 @@ static SharedArgs rows_args(bool bifocal, const uint16_t* q, const uint16_t* k, 
   a.table = table;
   a.o = o;
   a.rope = rope;
+  a.half = half;
   a.rope16 = rope16;
   a.plan = plan;
   a.states = (float*)states;
@@ -1533,6 +1603,7 @@ static SharedArgs rows_args(bool bifocal, const uint16_t* q, const uint16_t* k, 
   a.Hq = Hq;
   a.Hkv = Hkv;
   a.g = Hq / Hkv;
+  a.g_inv = 65536 / a.g + 1;
   a.max_pages = max_pages;
   a.n_pages = n_pages;
   a.page = 1 << page_shift;
@@ -1548,11 +1619,12 @@ static SharedArgs rows_args(bool bifocal, const uint16_t* q, const uint16_t* k, 
 hipError_t launch_decode_shared(bool bifocal, const uint16_t* q, const uint16_t* k,
                                 const uint16_t* v, const int32_t* table, int max_pages,
                                 int n_pages, int page_shift, void* plan, uint16_t* o,
-                                const float2* rope, const uint32_t* rope16, int B, int n_groups,
+                                const float2* rope, const uint32_t* half, const uint32_t* rope16,
+                                int B, int n_groups,
                                 int Hq, int Hkv, int w_pre, int w0, int n_cu, void* ws,
                                 hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1) {
   SharedArgs a = rows_args(bifocal, q, k, v, table, max_pages, n_pages, page_shift, plan, ws, o, rope,
-                           rope16, B, Hq, Hkv, w_pre, w0, n_cu);
+                           half, rope16, B, Hq, Hkv, w_pre, w0, n_cu);
   a.n_groups = n_groups;
   return launch_rows(a, stream, ev0, ev1);
 }
@@ -1561,8 +1633,8 @@ hipError_t launch_decode_shared(bool bifocal, const uint16_t* q, const uint16_t*
 hipError_t launch_chunk_rows(bool bifocal, const uint16_t* q, const uint16_t* k, const uint16_t* v,
                              const int32_t* table, int max_pages, int n_pages, int page_shift,
                              const int32_t* cu, const int32_t* kv_lens, uint16_t* o, float* lse,
-                             const float2* rope, const uint32_t* rope16, int B, int T, int Hq,
-                             int Hkv, int w_pre, int w0, float slack, int n_cu, void* scratch,
+                             const float2* rope, const uint32_t* half, const uint32_t* rope16,
+                             int B, int T, int Hq, int Hkv, int w_pre, int w0, float slack, int n_cu, void* scratch,
                              hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1) {
   const int g = Hq / Hkv, page = 1 << page_shift;
   const ChunkScratch at = chunk_scratch(B, T, Hq, Hkv, max_pages, page);
@@ -1584,7 +1656,7 @@ hipError_t launch_chunk_rows(bool bifocal, const uint16_t* q, const uint16_t* k,
     if (e != hipSuccess) return e;
   }
   SharedArgs a = rows_args(bifocal, q, k, v, table, max_pages, n_pages, page_shift, scratch,
-                           mem + at.states, o, rope, rope16, B, Hq, Hkv, w_pre, w0, n_cu);
+                           mem + at.states, o, rope, half, rope16, B, Hq, Hkv, w_pre, w0, n_cu);
   a.chunk = 1;
   a.T = T;
   a.lse = lse;

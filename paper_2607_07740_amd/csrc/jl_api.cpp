@@ -93,16 +93,16 @@ hipError_t launch_shared_plan(bool bifocal, const int32_t* kv_lens, const int32_
 hipError_t launch_decode_shared(bool bifocal, const uint16_t* q, const uint16_t* k,
                                 const uint16_t* v, const int32_t* table, int max_pages,
                                 int n_pages, int page_shift, void* plan, uint16_t* o,
-                                const float2* rope, const uint32_t* rope16, int B, int n_groups,
-                                int Hq, int Hkv, int w_pre, int w0, int n_cu, void* ws,
+                                const float2* rope, const uint32_t* half, const uint32_t* rope16,
+                                int B, int n_groups, int Hq, int Hkv, int w_pre, int w0, int n_cu, void* ws,
                                 hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1);
 size_t chunk_scratch_bytes(int B, int T, int Hq, int Hkv, int max_pages, int page);
 bool chunk_rows_fit(int B, int T, int g);
 hipError_t launch_chunk_rows(bool bifocal, const uint16_t* q, const uint16_t* k, const uint16_t* v,
                              const int32_t* table, int max_pages, int n_pages, int page_shift,
                              const int32_t* cu, const int32_t* kv_lens, uint16_t* o, float* lse,
-                             const float2* rope, const uint32_t* rope16, int B, int T, int Hq,
-                             int Hkv, int w_pre, int w0, float slack, int n_cu, void* scratch,
+                             const float2* rope, const uint32_t* half, const uint32_t* rope16,
+                             int B, int T, int Hq, int Hkv, int w_pre, int w0, float slack, int n_cu, void* scratch,
                              hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1);
 hipError_t launch_pages_fork(const Pages& p, const int32_t* parent, hipStream_t stream);
 hipError_t launch_pages_reserve(const Pages& p, const int32_t* n_new, int32_t* starts,
@@ -119,6 +119,7 @@ hipError_t launch_cache_append(const uint16_t* k, const uint16_t* v, uint16_t* k
                                int B, int n, int Hkv, hipStream_t stream);
 hipError_t launch_build_table(float2* table, uint32_t* table16, int n_pos, const double* omega,
                               hipStream_t stream);
+hipError_t launch_half_table(const float2* table, uint32_t* half, int n_pos, hipStream_t stream);
 hipError_t launch_debug_schedule(const int32_t* lengths, int nl, const int32_t* positions, int np,
                                  int w, int32_t* gout, int32_t* fout, int32_t* dout,
                                  hipStream_t stream);
@@ -179,7 +180,8 @@ bool past_int32(long long a, long long b, long long c) { return a * b > 0x7fffff
 // A table of cap positions is one allocation: cap x 64 fp32 (cos, sin) pairs
 // (512 B per position), then the same pairs in bf16, one 32-bit word each
 // (256 B per position); behind the base table of a theta also the rows of the
-// positions below 64 in fp16, as the 8-bit decode takes them.
+// positions below 64 in fp16, as the 8-bit decode takes them, and the pairs in
+// fp16, one word each, as the rows over paged caches take them.
 struct TableEntry {
   int device;
   double theta;
@@ -200,10 +202,16 @@ const void* offsets_of(const float2* p, long long cap) {
   return reinterpret_cast<const char*>(p) + table_bytes(cap);
 }
 
+const uint32_t* half_of(const float2* p, long long cap) {
+  return reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(p) + table_bytes(cap) +
+                                           (jl::offset_rows_bytes() + 255) / 256 * 256);
+}
+
 struct Tables {
   const float2* f32;
   const uint32_t* f16;
-  const void* offsets;  // of a base table
+  const void* offsets;   // of a base table
+  const uint32_t* half;  // of a base table
 };
 
 // Returns device tables covering positions [0, n_pos) for the current device.
@@ -224,7 +232,8 @@ int get_table(double theta, int n_pos, hipStream_t stream, Tables* out) {
   for (auto& t : g_tables)
     if (t.device == dev && t.theta == theta) found = &t;
   if (found && found->cap >= n_pos) {
-    *out = Tables{found->ptr, table16_of(found->ptr, found->cap), offsets_of(found->ptr, found->cap)};
+    *out = Tables{found->ptr, table16_of(found->ptr, found->cap), offsets_of(found->ptr, found->cap),
+                  half_of(found->ptr, found->cap)};
     return JL_OK;
   }
   long long cap = 4096;
@@ -232,12 +241,15 @@ int get_table(double theta, int n_pos, hipStream_t stream, Tables* out) {
   if (found && cap < 2LL * found->cap) cap = 2LL * found->cap;
   if (cap > (1LL << 30) / 64) cap = n_pos;  // keep the element count in range
   float2* p = nullptr;
-  e = hipMalloc(&p, table_bytes(cap) + jl::offset_rows_bytes());
+  e = hipMalloc(&p, table_bytes(cap) + (jl::offset_rows_bytes() + 255) / 256 * 256 +
+                        (size_t)cap * (kHeadDim / 2) * sizeof(uint32_t));
   if (e != hipSuccess) return hip_fail(e, "hipMalloc(rope table)");
   double omega[kHeadDim / 2];
   rope_omega(theta, omega);
   e = jl::launch_build_table(p, const_cast<uint32_t*>(table16_of(p, cap)), (int)cap, omega, stream);
   if (e == hipSuccess) e = jl::launch_offset_rows(p, const_cast<void*>(offsets_of(p, cap)), stream);
+  if (e == hipSuccess)
+    e = jl::launch_half_table(p, const_cast<uint32_t*>(half_of(p, cap)), (int)cap, stream);
   if (e == hipSuccess) e = hipStreamSynchronize(stream);  // usable from any stream afterwards
   if (e != hipSuccess) {
     (void)hipFree(p);
@@ -250,7 +262,7 @@ int get_table(double theta, int n_pos, hipStream_t stream, Tables* out) {
   } else {
     g_tables.push_back(TableEntry{dev, theta, (int)cap, p});
   }
-  *out = Tables{p, table16_of(p, cap), offsets_of(p, cap)};
+  *out = Tables{p, table16_of(p, cap), offsets_of(p, cap), half_of(p, cap)};
   return JL_OK;
 }
 
@@ -306,7 +318,7 @@ int get_freq_table(double theta, int L, int w_pre, hipStream_t stream, Tables* o
   for (auto& t : g_freq_tables)
     if (t.device == dev) found = &t;
   if (found && found->theta == theta && found->L == L && found->w_pre == w_pre) {
-    *out = Tables{found->ptr, table16_of(found->ptr, found->cap), nullptr};
+    *out = Tables{found->ptr, table16_of(found->ptr, found->cap), nullptr, nullptr};
     return JL_OK;
   }
   if (found) {
@@ -345,7 +357,7 @@ int get_freq_table(double theta, int L, int w_pre, hipStream_t stream, Tables* o
   } else {
     g_freq_tables.push_back(FreqTable{dev, theta, L, w_pre, cap, p});
   }
-  *out = Tables{p, table16_of(p, cap), nullptr};
+  *out = Tables{p, table16_of(p, cap), nullptr, nullptr};
   return JL_OK;
 }
 
@@ -863,7 +875,7 @@ int varlen_paged(bool bifocal, const void* q, const void* kp, const void* vp, co
   timing_events(0, &ev0, &ev1);
   const hipError_t e = jl::launch_chunk_rows(
       bifocal, (const uint16_t*)q, (const uint16_t*)kp, (const uint16_t*)vp, table, max_pages,
-      n_pages, shift, cu, kv_lens, (uint16_t*)o, lse, tab.f32, tab.f16, B, T, Hq, Hkv, w_pre, w0,
+      n_pages, shift, cu, kv_lens, (uint16_t*)o, lse, tab.f32, tab.half, tab.f16, B, T, Hq, Hkv, w_pre, w0,
       (float)g_rescale_log2.load(), jl::cu_count(), scratch, s, ev0, ev1);
   if (e != hipSuccess) return hip_fail(e, "packed chunk launch");
   return ok();
@@ -926,8 +938,8 @@ int decode_shared(bool bifocal, const void* q, const void* kp, const void* vp,
   timing_events(1, &ev0, &ev1);
   const hipError_t e = jl::launch_decode_shared(
       bifocal, (const uint16_t*)q, (const uint16_t*)kp, (const uint16_t*)vp, table, max_pages,
-      n_pages, shift, const_cast<void*>(plan), (uint16_t*)o, tab.f32, tab.f16, B, n_groups, Hq, Hkv,
-      w_pre, w0, jl::cu_count(), ws, s, ev0, ev1);
+      n_pages, shift, const_cast<void*>(plan), (uint16_t*)o, tab.f32, tab.half, tab.f16, B, n_groups, Hq,
+      Hkv, w_pre, w0, jl::cu_count(), ws, s, ev0, ev1);
   if (e != hipSuccess) return hip_fail(e, "shared decode launch");
   return ok();
 }

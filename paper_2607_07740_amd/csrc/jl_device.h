@@ -14,6 +14,8 @@ constexpr int kHalf = 64;  // rotate-half partner offset and number of RoPE freq
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
@@ -152,6 +154,10 @@ __device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+__device__ inline f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
 __device__ inline u32x4 load16(const void* p) { return *(const u32x4*)p; }
 
 // Two rotate-half pairs by v_dot2_f32_bf16 (exact bf16 products, one fp32
@@ -184,6 +190,25 @@ __device__ inline void rot_word_dot2(uint32_t wl, uint32_t wh, uint32_t cs_a, ui
         "=&v"(p1), "=&v"(q1)
       : "v"(wl), "v"(wh), "v"(cs_a), "v"(cs_b), "s"(0x05040100u), "s"(0x01000504u),
         "s"(0x07060302u), "s"(0x03020706u));
+}
+
+// The same pairs in fp32, by fp16 (cos, sin): lo_a, lo_b, hi_a, hi_b.  amax takes the largest
+// magnitude of the four channels.
+__device__ inline void rot_pairs_f16(uint32_t wl, uint32_t wh, uint32_t cs_a, uint32_t cs_b,
+                                     float* v, float& amax) {
+  const float xa = __uint_as_float(wl << 16), xb = __uint_as_float(wl & 0xffff0000u);
+  const float ya = __uint_as_float(wh << 16), yb = __uint_as_float(wh & 0xffff0000u);
+  const f16x2 a = __builtin_bit_cast(f16x2, cs_a), b = __builtin_bit_cast(f16x2, cs_b);
+  asm("v_max3_f32 %0, |%1|, |%2|, %0" : "+v"(amax) : "v"(xa), "v"(xb));
+  asm("v_max3_f32 %0, |%1|, |%2|, %0" : "+v"(amax) : "v"(ya), "v"(yb));
+  v[0] = fmaf((float)a[0], xa, -((float)a[1] * ya));
+  v[1] = fmaf((float)b[0], xb, -((float)b[1] * yb));
+  v[2] = fmaf((float)a[0], ya, (float)a[1] * xa);
+  v[3] = fmaf((float)b[0], yb, (float)b[1] * xb);
+}
+__device__ inline uint32_t pack_f16(float a, float b) {
+  typedef float f32x2v __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v{a, b}), f16x2));
 }
 
 // ------------------------------------------------- direct-to-LDS staging

@@ -274,3 +274,18 @@ def test_the_rows_of_a_forked_batch_from_prompt_to_tokens():
         out = api.decode_shared(q, kp, vp, pages.table, plan)
         torch.cuda.synchronize()
         assert_close(to_f64(out), np.concatenate([want(b, 1) for b in range(4)]), what="token %d" % i)
+
+
+@pytest.mark.parametrize("n", [[3, 70, 1], [30, 33, 20], [300, 260, 200]])
+def test_keys_and_queries_of_any_magnitude(n):
+    """Keys times 2^e, their queries times 2^-e, another e for each sequence: the same scores."""
+    c = Chunks([400, 300, 260], n, 8, 2, 64, seed=51)
+    want = c.want(150, 60)[0]
+    on = lambda x: ((x & 0x7F80) != 0) & ((x & 0x7F80) != 0x7F80)  # noqa: E731
+    times = lambda x, e: np.where(on(x), x + (e << 7), x).astype(np.uint16)  # noqa: E731
+    for b, e in enumerate((18, 0, -20)):
+        c.q[c.cu[b]:c.cu[b + 1]] = times(c.q[c.cu[b]:c.cu[b + 1]].astype(np.int32), -e)
+        for j in c.table[b][c.table[b] >= 0]:
+            c.kp[j] = times(c.kp[j].astype(np.int32), e)
+    say("magnitudes", n)
+    assert_close(to_f64(c.run(150, 60)), want, what="magnitudes")
