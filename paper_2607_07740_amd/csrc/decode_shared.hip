@@ -136,7 +136,7 @@ size_t prefill_chunk_state_bytes();
 int prefill_chunk_max_pages();
 hipError_t launch_prefill_chunks(bool bifocal, const uint16_t* q, const uint16_t* k,
                                  const uint16_t* v, uint16_t* o, float* lse, const float2* table,
-                                 const uint32_t* table16, const int32_t* block_table,
+                                 const uint32_t* table16, const uint32_t* half, const int32_t* block_table,
                                  int max_pages, int page_shift, int n_pages, int T, int Hq, int Hkv,
                                  int w0, float slack, const ChunkPart* parts, const int* n_parts,
                                  int max_parts, float* states, hipStream_t stream);
@@ -1650,7 +1650,7 @@ hipError_t launch_chunk_rows(bool bifocal, const uint16_t* q, const uint16_t* k,
   if (blocks) {
     // no sequence past the window: G = 1 for all, and the vanilla kernel does
     const bool fused = bifocal && (long long)max_pages * page > w_pre;
-    e = launch_prefill_chunks(fused, q, k, v, o, lse, rope, rope16, table, max_pages, page_shift,
+    e = launch_prefill_chunks(fused, q, k, v, o, lse, rope, rope16, half, table, max_pages, page_shift,
                               n_pages, T, Hq, Hkv, w0, slack, p.parts, (int*)scratch + kHdParts,
                               p.most_parts, (float*)(mem + at.part_states), stream);
     if (e != hipSuccess) return e;

@@ -45,6 +45,7 @@
 // rescales the state.  So every probability stays below 2^64.
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "jl_device.h"
 #include "prefill_chunks.h"
@@ -127,6 +128,7 @@ struct PrefillArgs {
   // packed chunks behind paged caches (prefill_chunks_kernel): their parts, and how many
   const ChunkPart* chunk_parts;
   const int* n_chunk_parts;
+  const uint32_t* half;  // packed chunks: the base table as fp16 pairs
 };
 
 // Most pages of one sequence a paged prefill block looks up (LDS table)
@@ -243,10 +245,18 @@ enum PrefillMode : int { kModeFused = 0, kModeVanilla = 1, kModeWinA = 2, kModeW
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 __device__ inline bf16x2 bf16_one2() { return bf16x2{(__bf16)1.0f, (__bf16)1.0f}; }
 
+// fp16 holds 16 or more channels (its last place is 2^-13 of the largest of them, or less) whose largest
+// is zero or in [2^-12, 2^15): a rotated one is below 2^15.5.
+constexpr float kHalfLow = 1.f / 4096.f, kHalfHigh = 32768.f;
+__device__ inline bool half_holds(float amax) { return amax < kHalfHigh && !(amax > 0.f && amax < kHalfLow); }
+
 // Load one query row's B operand: 8 k-steps of 8 bf16 (d = 16 s + 8 half + j),
 // rotated to position pos and scaled.  Pairs (s, s + 4) are rotate-half partners.
-__device__ inline void load_q_operand(const uint16_t* qrow, int half, const float2* table,
-                                      int pos, float scale, bf16x8* out) {
+// Op = f16x8: in fp16, and whether that holds the lane's channels (see kHalfLow).
+template <typename Op>
+__device__ inline bool load_q_operand(const uint16_t* qrow, int half, const float2* table,
+                                      int pos, float scale, Op* out) {
+  float amax = 0.f;
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
     const int d = 16 * s + 8 * half;
@@ -263,9 +273,19 @@ __device__ inline void load_q_operand(const uint16_t* qrow, int half, const floa
       ylo[j + 1] = (lo[j + 1] * w.z - hi[j + 1] * w.w) * scale;
       yhi[j + 1] = (hi[j + 1] * w.z + lo[j + 1] * w.w) * scale;
     }
-    out[s] = pack8(ylo);
-    out[s + 4] = pack8(yhi);
+    if constexpr (std::is_same_v<Op, bf16x8>) {
+      out[s] = pack8(ylo);
+      out[s + 4] = pack8(yhi);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        out[s][t] = (_Float16)ylo[t];
+        out[s + 4][t] = (_Float16)yhi[t];
+        amax = fmaxf(amax, fmaxf(fabsf(ylo[t]), fabsf(yhi[t])));
+      }
+    }
   }
+  return half_holds(amax);
 }
 
 
@@ -301,11 +321,16 @@ __device__ inline float* part_state(const PrefillArgs& a, int tail_block, int pa
 // total fell below 2^-slack.  A block with either writes no output and returns
 // true; the kernel then runs it again with SAFE = true: the per-tile check,
 // which moves the reference as needed.  Every mode runs so.
-template <int MODE, bool SAFE, bool PAGED, bool SPLIT, int WAVES>
+// HALF: the fast pass multiplies rotated keys and queries in fp16, by a.half for the tables, which
+// halves the output's distance from 64 bits; keys and queries outside its range send
+// the block to the checked pass, which is in bf16.
+template <int MODE, bool SAFE, bool PAGED, bool SPLIT, int WAVES, bool HALF = false>
 __device__ __forceinline__ bool prefill_block(const PrefillArgs& a, const Work& W,
                                               unsigned char* smem, int* s_bad, int* s_pages,
                                               int part, int parts, float* state) {
   constexpr bool CHECK_LATE = !SAFE;
+  using Op = std::conditional_t<HALF, f16x8, bf16x8>;
+  unsigned long long late_bad = 0;
   constexpr int kKeys = kPfBK / WAVES;  // each wave's share of a tile: 8 keys, or 16
   constexpr int kRots = kKeys / 8;
   // The visit list has at most two segments: the fused kernel's remote tiles
@@ -449,7 +474,7 @@ __device__ __forceinline__ bool prefill_block(const PrefillArgs& a, const Work& 
     const uint16_t* kr =
         (const uint16_t*)((const unsigned char*)(a.k + e.off) + __umul24((uint32_t)key, kv_row_bytes));
     const uint32_t* tr =
-        (e.remote ? rtable16 : a.table16) + (size_t)(e.row0 + row) * kHalf + 8 * rt_c;
+        (HALF ? a.half : e.remote ? rtable16 : a.table16) + (size_t)(e.row0 + row) * kHalf + 8 * rt_c;
     RotIn r;
     // the vanilla kernel reads a row of its own for every key, 16 KB a tile (the
     // remote view shares rows): asked for first, 122.2 -> 121.6 ms at 131072
@@ -488,8 +513,21 @@ __device__ __forceinline__ bool prefill_block(const PrefillArgs& a, const Work& 
 #pragma unroll
     for (int h = 0; h < kRots; ++h) {
       u32x4 lo, hi;
+      if constexpr (!HALF) {
 #pragma unroll
-      for (int w = 0; w < 4; ++w) rot_word(s.r[h], w, lo, hi);
+        for (int w = 0; w < 4; ++w) rot_word(s.r[h], w, lo, hi);
+      } else {
+        float amax = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          float v[4];
+          rot_pairs_f16(s.r[h].xl[w], s.r[h].xh[w], w < 2 ? s.r[h].ca[2 * w] : s.r[h].cb[2 * w - 4],
+                        w < 2 ? s.r[h].ca[2 * w + 1] : s.r[h].cb[2 * w - 3], v, amax);
+          lo[w] = pack_f16(v[0], v[1]);
+          hi[w] = pack_f16(v[2], v[3]);
+        }
+        late_bad |= __ballot(!half_holds(amax));
+      }
       *(u32x4*)(dst + rt_lo[h]) = lo;
       *(u32x4*)(dst + rt_hi[h]) = hi;
     }
@@ -506,7 +544,7 @@ __device__ __forceinline__ bool prefill_block(const PrefillArgs& a, const Work& 
   // k-step of every QK product accumulates onto neg_m = -m_ref in each entry
   // (all 16 accumulator entries of a lane belong to its query column).  The
   // reference moves only on the rare path below.
-  bf16x8 qop[8];
+  Op qop[8];
   f32x16 acc_o[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) acc_o[i] = f32x16{};
@@ -522,9 +560,9 @@ __device__ __forceinline__ bool prefill_block(const PrefillArgs& a, const Work& 
   auto qk = [&](const unsigned char* kb, f32x16* sc) __attribute__((always_inline)) {
     auto kop = [&](int m) __attribute__((always_inline)) {
       const int r = 32 * (m & 1) + kr_lane;
-      return *(const bf16x8*)(kb + kimg_off(r, 2 * (m >> 1) + hl32));
+      return *(const Op*)(kb + kimg_off(r, 2 * (m >> 1) + hl32));
     };
-    bf16x8 ring[4];
+    Op ring[4];
 #pragma unroll
     for (int m = 0; m < 4; ++m) ring[m] = kop(m);
 #pragma unroll
@@ -629,7 +667,6 @@ __device__ __forceinline__ bool prefill_block(const PrefillArgs& a, const Work& 
   // re-bases the tile's scores and the next tile's (computed against the old
   // reference), rescales the running state and redoes the tile's softmax.
   const float p_hi = exp2f(a.slack), p_lo = exp2f(-a.slack);
-  unsigned long long late_bad = 0;
   auto ref_fix = [&](f32x16* sc, f32x16* nx, bf16x8* pb, float& ps) __attribute__((always_inline)) {
     const bool bad = ps > p_hi || (l_run == 0.f && ps < p_lo);
     if (__ballot(bad) == 0) return;
@@ -689,18 +726,18 @@ __device__ __forceinline__ bool prefill_block(const PrefillArgs& a, const Work& 
       const unsigned char* kb = kbuf(j + 1);
       auto kop = [&](int m) __attribute__((always_inline)) {
         const int r = 32 * (m & 1) + kr_lane;
-        return *(const bf16x8*)(kb + kimg_off(r, 2 * (m >> 1) + hl32));
+        return *(const Op*)(kb + kimg_off(r, 2 * (m >> 1) + hl32));
       };
-      bf16x8 ring[4];
+      Op kring[4];
 #pragma unroll
-      for (int m = 0; m < 4; ++m) ring[m] = kop(m);
+      for (int m = 0; m < 4; ++m) kring[m] = kop(m);
       __builtin_amdgcn_sched_barrier(0);
       RotSet rin;
 #pragma unroll
       for (int m = 0; m < 16; ++m) {
         const int blk = m & 1, st = m >> 1;
-        nxt[blk] = mfma32(ring[m & 3], qop[st], st == 0 ? neg_m : nxt[blk]);
-        if (m + 4 < 16) ring[m & 3] = kop(m + 4);
+        nxt[blk] = mfma32(kring[m & 3], qop[st], st == 0 ? neg_m : nxt[blk]);
+        if (m + 4 < 16) kring[m & 3] = kop(m + 4);
         __builtin_amdgcn_sched_barrier(0);
         if (m == 5) {
           // V(j+1) into the buffer PV(j-1) released, and raw K(j+2) with its
@@ -730,6 +767,7 @@ __device__ __forceinline__ bool prefill_block(const PrefillArgs& a, const Work& 
       const Ent e3 = ent_of(min(j + 3, n_steps - 1));
       const unsigned char* vb = vbuf(j);
       auto vop = [&](int m) __attribute__((always_inline)) { return v_operand(vb, m); };
+      bf16x8 ring[4];
 #pragma unroll
       for (int m = 0; m < 4; ++m) ring[m] = vop(m);
 #pragma unroll
@@ -780,8 +818,11 @@ __device__ __forceinline__ bool prefill_block(const PrefillArgs& a, const Work& 
   // ---- prologue: the first view's query operand; K(0), K(1) rotated into
   // their buffers, V(0) in flight
   const bool q_remote = n_r > 0 || REMOTE2;
-  load_q_operand(qrow, hl32, q_remote ? rtable : a.table,
-                 q_remote && !a.freq_map ? remote_pos(qp, gdiv) : qp, a.q_scale, qop);
+  auto load_q = [&](const float2* table, int pos) __attribute__((always_inline)) {
+    const bool holds = load_q_operand(qrow, hl32, table, pos, a.q_scale, qop);
+    if constexpr (HALF) late_bad |= __ballot(!holds);
+  };
+  load_q(q_remote ? rtable : a.table, q_remote && !a.freq_map ? remote_pos(qp, gdiv) : qp);
   if (CHECK_LATE && tid == 0) *s_bad = 0;  // read after the end-of-block barrier
   const int last = n_steps - 1;
   if constexpr (PAGED) {  // the sequence's page list, clamped into the pool
@@ -812,7 +853,7 @@ __device__ __forceinline__ bool prefill_block(const PrefillArgs& a, const Work& 
     // segment 2 in the base view: its first tile, already rotated to the base
     // view (buffer n_r & 1, not overwritten since), is scored again with the
     // base-rotated query operand
-    load_q_operand(qrow, hl32, a.table, qp, a.q_scale, qop);
+    load_q(a.table, qp);
     qk(kbuf(n_r), sc_a);
   }
   {
@@ -907,8 +948,8 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_chunks_kernel(PrefillAr
   if (p.parts == 0) return;
   const Work W = chunk_work(a, p, kvh);
   float* state = chunk_state(a, p, p.part, kvh);
-  if (prefill_block<MODE, false, true, true, kPfWaves>(a, W, smem, &s_bad, s_pages, p.part, p.parts,
-                                                       state)) {
+  if (prefill_block<MODE, false, true, true, kPfWaves, true>(a, W, smem, &s_bad, s_pages, p.part,
+                                                             p.parts, state)) {
     __syncthreads();
     prefill_block<MODE, true, true, true, kPfWaves>(a, W, smem, &s_bad, s_pages, p.part, p.parts, state);
   }
@@ -1537,9 +1578,10 @@ int prefill_chunk_max_pages() { return kMaxSeqPages; }
 // The parts that a planning kernel has listed: at most max_parts.  q, o [T][Hq][128], lse [Hq][T].
 hipError_t launch_prefill_chunks(bool bifocal, const uint16_t* q, const uint16_t* k,
                                  const uint16_t* v, uint16_t* o, float* lse, const float2* table,
-                                 const uint32_t* table16, const int32_t* block_table,
-                                 int max_pages, int page_shift, int n_pages, int T, int Hq, int Hkv,
-                                 int w0, float slack, const ChunkPart* parts,
+                                 const uint32_t* table16, const uint32_t* half,
+                                 const int32_t* block_table, int max_pages, int page_shift,
+                                 int n_pages, int T, int Hq, int Hkv, int w0, float slack,
+                                 const ChunkPart* parts,
                                  const int* n_parts, int max_parts, float* states,
                                  hipStream_t stream) {
   PrefillArgs a = {};
@@ -1551,6 +1593,7 @@ hipError_t launch_prefill_chunks(bool bifocal, const uint16_t* q, const uint16_t
   a.w0 = bifocal ? w0 : INT_MAX;
   a.chunk_parts = parts;
   a.n_chunk_parts = n_parts;
+  a.half = half;
   a.states = states;
   const unsigned grid = (unsigned)max_parts * Hkv;
   if (bifocal)
