@@ -33,14 +33,14 @@
  *      - the RoPE cos/sin table (per device and rope_theta, grown by
  *        doubling to cover the call's positions): every prefill, decode and
  *        block score entry point; growing allocates and waits for `stream`;
- *      - the prefill scratch (per device and stream): the _varlen forms with
- *        more than 64 sequences, or the frequency map past the window, and of
- *        jl_bifocal_prefill, jl_rope_attention, their _map and _chunk forms
- *        the calls whose query blocks leave CUs idle (see there); growing
- *        waits for `stream`, frees the old buffer and allocates.  Under
- *        stream capture it does not grow: a call that would cut its blocks
- *        runs them whole, a packed call that needs more returns JL_ERR_HIP.
- *        A buffer that a captured call uses is kept until
+ *      - the prefill scratch (per device and stream): the _varlen_paged forms,
+ *        the _varlen forms with more than 64 sequences, or the frequency map
+ *        past the window, and of jl_bifocal_prefill, jl_rope_attention, their
+ *        _map and _chunk forms the calls whose query blocks leave CUs idle
+ *        (see there); growing waits for `stream`, frees the old buffer and
+ *        allocates.  Under stream capture it does not grow: a call that would
+ *        cut its blocks runs them whole, a packed call that needs more returns
+ *        JL_ERR_HIP.  A buffer that a captured call uses is kept until
  *        jl_release_caches;
  *      - the frequency-map table (one per device): jl_bifocal_prefill_map
  *        with JL_REMOTE_FREQ; a new (rope_theta, L, w_pretrained) waits for
@@ -767,9 +767,11 @@ size_t jl_decode_shared_workspace_bytes(int B, int Hq, int Hkv, int head_dim);
  *   o          bf16 [B, Hq, head_dim]  output (written)
  *   workspace  jl_decode_shared_workspace_bytes(B, Hq, Hkv, head_dim) bytes, 16-byte
  *              aligned; contents on entry do not matter
- * Rounded to bf16 are the rotated queries, the keys' cos and sin, the rotated keys and the
- * softmax weights, whose rounded values the denominator sums; everything else is fp32.  The
- * same plan and inputs give the same bits.  Only the cos/sin table may be allocated or grown.
+ * Rounded are the rotated queries, the keys' cos and sin and the rotated keys, to fp16, and the
+ * softmax weights, to bf16, whose rounded values the denominator sums; everything else is fp32.
+ * Beside a key or a query whose largest channel lies outside [2^-8, 2^15) the first three are
+ * rounded to bf16, for all that the same workgroup holds, in twice the time.  The same plan and
+ * inputs give the same bits.  Only the cos/sin table may be allocated or grown.
  */
 int jl_bifocal_decode_shared(const void* q, const void* k_pages, const void* v_pages,
                              const int32_t* block_table, int max_pages, int page_size, int n_pages,
@@ -801,9 +803,10 @@ int jl_rope_attention_decode_shared(const void* q, const void* k_pages, const vo
  * jl_bifocal_prefill_chunk_paged that ends there: the same result up to rounding and the
  * order of the sums.  Rows of no sequence, or before position 0 (more rows than keys), are
  * left as they were.  Hq / Hkv at most 256; B > 2048, or about a million rows (total_tokens *
- * Hq / Hkv) in one call -> JL_ERR_UNSUPPORTED.  Scratch (the prefill scratch of the stream):
- * 528 bytes for every query row and kv head twice, and up to 35 MB.  The same call gives the
- * same bits.
+ * Hq / Hkv) in one call -> JL_ERR_UNSUPPORTED.  Roundings as in jl_bifocal_decode_shared.
+ * Scratch (the prefill scratch of the stream): 1056 bytes for every token and query head, up to
+ * 35 MB, and up to 140 MB more where longer chunks run as blocks of the prefill kernel.  The same
+ * call gives the same bits.
  */
 int jl_bifocal_prefill_varlen_paged(const void* q, const void* k_pages, const void* v_pages,
                                     const int32_t* block_table, int max_pages, int page_size,

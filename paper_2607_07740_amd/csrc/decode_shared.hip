@@ -19,12 +19,21 @@
 // follows from the lengths, so that a decoding step makes it once for all layers.
 //
 // Kernel: a workgroup (8 waves, one CU) streams the tiles of its range through a ring
-// in LDS, K, V and the cos/sin rows of the keys' positions, four tiles in flight.  While
-// tile i is multiplied, tile i + 1 is rotated in place, four keys a wave.  Up to 128
-// rows, a wave takes 32 rows and half of the tile's keys, on 16 x 16 matrix instructions;
-// above, 32 rows and all keys, on 32 x 32 ones.  Each (workgroup, segment) leaves its
-// rows' states (m, l, O) in fp32, one for each half of the keys, and the merge kernel joins
-// those of a row.
+// in LDS, K, V and the cos/sin rows of the keys' positions, four tiles in flight, and
+// rotates tile i + 1 in place while tile i is multiplied.  Rows are the columns of 32 x 32 matrix
+// instructions, 32 to a wave.  Up to 128 rows, four waves multiply and the other four copy and
+// rotate, so that neither waits for the other (64 chats: 187 -> 134 us when this was
+// split off); above, all eight do both.  A wave forms the scores of visit i beside the softmax and
+// the value product of visit i - 1.  Each (workgroup, segment) leaves its rows' states (m, l, O)
+// in fp32, and the merge kernel joins those of a row; a chunk's block that lies in one range is
+// written at once.
+//
+// What bounds it: HBM where most tiles have one visit (64 chats behind 4 prompts, 536 MB: 118 us
+// with 32/8 heads, 4.5 TB/s; the copies alone take 97 to 101), the multiplying waves where tiles
+// have several (16 samples of 32K with G = 1 and 2, 222 MB: 89 us, 67 without them; 8 of 128K with
+// G = 4 and 5, 544 MB: 218, 179 without), latency where there are few keys (2 sequences of 1.2K: 13).
+// Tiles of 32 keys keep four of them in flight beside the two in use, and cut 1000 keys into enough visits
+// for 32 workgroups of each of 8 kv heads.
 #include <algorithm>
 #include <climits>
 #include <type_traits>
@@ -38,10 +47,10 @@ namespace jl {
 constexpr int kShThreads = 512, kShWaves = 8;
 constexpr int kShRows = 32 * kShWaves;  // rows of a segment at most
 constexpr int kShSmall = kShRows / 2;   // rows that four waves hold, while the others copy and rotate
-constexpr int kShFew = kShRows / 4;     // rows that two waves hold: two pairs take the visits in turn
+constexpr int kShFew = kShRows / 4;     // rows that two waves hold: see state_halves
 constexpr int kShTile = 32;             // keys of a tile
 constexpr int kShImg = kShTile * kHeadDim * 2;      // K or V of a tile: 8 KB
-constexpr int kShBuf = 2 * kShImg + kShTile * 256;  // and its 32 rows of bf16 (cos, sin)
+constexpr int kShBuf = 2 * kShImg + kShTile * 256;  // and its 32 rows of (cos, sin), 16 bits each
 constexpr int kShBufs = 6;
 constexpr int kShAhead = kShBufs - 2;  // tiles requested before the first is used
 constexpr int kShList = 256;           // visits whose addresses are held; refilled by halves
@@ -77,8 +86,9 @@ struct Member {
   int pre, suf;  // its segments, -1: none
 };
 // States that a (workgroup, segment) leaves.  Up to 64 rows, two pairs of waves take the visits in
-// turn where most tiles have two, their second from the caches (16 samples of 32K, G = 1 and 2: 104 ->
-// 96 us); where memory sets the pace the second states cost more (64 chats: 130 -> 137).
+// turn where most tiles have two, their second from the caches (16 samples of 32K, G = 1 and 2: 99 ->
+// 89 us, 8 of 128K 266 -> 218); where memory sets the pace the second states cost more (64 chats:
+// 121 -> 128).
 __host__ __device__ inline int state_halves(const Segment& s) {
   const int tiles = (s.kend - s.k0 + kShTile - 1) / kShTile;
   return s.rows <= kShFew && 2LL * s.visits > 3LL * tiles ? 2 : 1;
@@ -160,8 +170,8 @@ size_t decode_shared_workspace_bytes(int B, int Hq, int Hkv) {
 static size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 
 // Whether the blocks of longer chunks go to the prefill kernel, which takes 64 keys of 256 rows in
-// the time of 32 here (rows 512 and 600 of 15000 and 34000 keys, 32/8 heads: 735 -> 452 us with
-// both): where the rows beyond a token per sequence make a few of its blocks, and with what it
+// the time of 32 here (turns of 512, 600, 1 and 700 rows behind 15000, 34000, 9000 and 0 keys, 32/8
+// heads: 754 -> 600 us): where the rows beyond a token per sequence make a few of its blocks, and with what it
 // asks of the cache.  A sequence's go there if they are more than 128.
 static bool chunk_blocks(int B, int T, int g, int max_pages, int page) {
   return kChunkBlockRows % g == 0 && page >= kChunkTile && max_pages <= prefill_chunk_max_pages() &&
@@ -367,7 +377,9 @@ __device__ inline void plan_ranges(const SharedPlanArgs& a, const PlanView& v, i
   }
 }
 
-// A decode step's plan, by one workgroup.
+// A decode step's plan, by one workgroup: bound by the latency of its dependent reads and scans (8.5 us
+// for 2 sequences, 12 for 16 with views of two G; 256 threads instead of 1024 up to 128
+// sequences: 10.4 -> 8.6).  One plan serves every layer of a step.
 __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs a) {
   extern __shared__ int s_mem[];
   __shared__ unsigned long long s_scan[kPlWaves];
@@ -1448,7 +1460,9 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
 }
 
 // The states of a row, joined: O = sum 2^(m - M) O~ / sum 2^(m - M) l.  Workgroup: 8
-// rows of one kv head in member order; thread -> row, 4 channels, every other state.
+// rows of one kv head in member order; thread -> row, 4 channels, every other state, four of
+// them requested at once.  4.6 us for 2 sequences, 8.8 for the 64 states of a row that
+// all workgroups of a kv head leave: latency.
 constexpr int kMgRows = 8;
 __global__ __launch_bounds__(512) void merge_shared_kernel(SharedArgs a) {
   __shared__ f32x4 s_o[32][kMgRows];

@@ -53,7 +53,8 @@ __device__ inline T block_scan(T v, T* s, T* total) {
 // Row b becomes what row parent[b] was, or empty where parent[b] names none, all
 // rows at once.  A workgroup takes some columns of every row: what the rows get
 // goes to LDS before any of them is written.  Rows that stay are not read.
-// lens is read and written by the first workgroup alone.
+// lens is read and written by the first workgroup alone.  Bound by the counts' atomics (256
+// rows of 2048 columns of which 64 change: 9.4 us, 7.8 without them; 32 rows of 64: 3.9, a launch).
 struct ForkArgs {
   Pages p;
   const int32_t* parent;
@@ -100,7 +101,9 @@ __global__ __launch_bounds__(kBookThreads) void fork_kernel(ForkArgs a) {
 // many pages are free, then the k-th free page goes to the sequence whose range of
 // needs holds k.  A sequence that writes into a partly filled page which others
 // name too gets a fresh one for it, but for the last writer of a page that only
-// writers name.  If the pages do not suffice nothing is changed.
+// writers name.  If the pages do not suffice nothing is changed.  Bound by latency: length, entry,
+// count, sums and the second read of the counts follow each other (16 sequences, 512 pages: 11 us;
+// 12.7 with 1024 threads and 64-bit divisions).
 struct ReserveArgs {
   Pages p;
   const int32_t* n_new;
@@ -269,7 +272,7 @@ __global__ __launch_bounds__(kBookThreads) void reserve_kernel(ReserveArgs a) {
 // ---------------------------------------------------------------- compact
 // With n pages in use, the i-th of those numbered n or more moves to the i-th free
 // one below n.  One workgroup lists the moves and where each page went; then the
-// tables follow.
+// tables follow.  Latency: 3.3 us and 2.2 with 512 pages, 5.3 with 4096.
 struct CompactArgs {
   Pages p;
   int32_t* moves;  // [n_pages / 2][2]
@@ -339,7 +342,7 @@ __global__ __launch_bounds__(256) void retable_kernel(CompactArgs a) {
 
 // ------------------------------------------------------------- page copies
 // Moves are cut into units of 16 KB of one pool, dealt to the workgroups in turn.
-// Bound by HBM.
+// Bound by HBM: 8 pools, 1.9 GB read and written in 370 us, 5.1 TB/s; few moves are a launch (4 us).
 constexpr int kCopyUnit = 16384;
 
 template <typename V>
@@ -384,7 +387,8 @@ __global__ __launch_bounds__(256) void copy_pages_kernel(CopyPools a, const int3
 
 // ------------------------------------------------------------------ append
 // Rows of bf16 caches: a wave takes one new token (or several in turn), whose K and
-// V rows of all heads are contiguous on both sides, 16 bytes a lane.
+// V rows of all heads are contiguous on both sides, 16 bytes a lane.  Bound by HBM: prompts of 266 MB
+// read and written in 41 us, 6.5 TB/s; a token of 16 sequences 3.5 us, a launch.
 struct AppendArgs {
   const u32x4* k;
   const u32x4* v;
