@@ -33,21 +33,21 @@
  *      - the RoPE cos/sin table (per device and rope_theta, grown by
  *        doubling to cover the call's positions): every prefill, decode and
  *        block score entry point; growing allocates and waits for `stream`;
- *      - the prefill scratch (per device and stream): the _varlen_paged forms,
- *        the _varlen forms with more than 64 sequences, or the frequency map
- *        past the window, and of jl_bifocal_prefill, jl_rope_attention, their
- *        _map and _chunk forms the calls whose query blocks leave CUs idle
- *        (see there); growing waits for `stream`, frees the old buffer and
- *        allocates.  Under stream capture it does not grow: a call that would
- *        cut its blocks runs them whole, a packed call that needs more returns
- *        JL_ERR_HIP.  A buffer that a captured call uses is kept until
+ *      - the prefill scratch (per device and stream): the _varlen forms with
+ *        more than 64 sequences, or the frequency map past the window, and of
+ *        jl_bifocal_prefill, jl_rope_attention, their _map and _chunk forms
+ *        the calls whose query blocks leave CUs idle (see there); growing
+ *        waits for `stream`, frees the old buffer and allocates.  Under
+ *        stream capture it does not grow: a call that would cut its blocks
+ *        runs them whole, a packed call that needs more returns JL_ERR_HIP.
+ *        A buffer that a captured call uses is kept until
  *        jl_release_caches;
  *      - the frequency-map table (one per device): jl_bifocal_prefill_map
  *        with JL_REMOTE_FREQ; a new (rope_theta, L, w_pretrained) waits for
  *        the whole device, then rebuilds the table in place, or in a buffer
  *        of at least twice the capacity when L does not fit.
- *    The literal and decode entry points use the caller's workspace and
- *    allocate nothing else.  jl_release_caches frees every cache.
+ *    The literal, decode and _varlen_paged entry points use the caller's
+ *    workspace and allocate nothing else.  jl_release_caches frees every cache.
  *  - Thread safety: calls may come from several host threads; the library's
  *    shared state (the caches above and the debug settings below) is guarded
  *    by mutexes.  Calls that share output buffers must be ordered by the
@@ -803,25 +803,32 @@ int jl_rope_attention_decode_shared(const void* q, const void* k_pages, const vo
  * jl_bifocal_prefill_chunk_paged that ends there: the same result up to rounding and the
  * order of the sums.  Rows of no sequence, or before position 0 (more rows than keys), are
  * left as they were.  Hq / Hkv at most 256; B > 2048, or about a million rows (total_tokens *
- * Hq / Hkv) in one call -> JL_ERR_UNSUPPORTED.  Roundings as in jl_bifocal_decode_shared.
- * Scratch (the prefill scratch of the stream): 1056 bytes for every token and query head, up to
- * 35 MB, and up to 140 MB more where longer chunks run as blocks of the prefill kernel.  The same
- * call gives the same bits.
+ * Hq / Hkv) in one call -> JL_ERR_UNSUPPORTED.  Roundings as in jl_bifocal_decode_shared.  The
+ * same call gives the same bits.
+ *   workspace    jl_varlen_paged_workspace_bytes(...) bytes, 16-byte aligned; contents on entry do
+ *                not matter.  1056 bytes for every token and query head, up to 35 MB, and up to
+ *                140 MB more where longer chunks run as blocks of the prefill kernel.
+ * Only the cos/sin table may be allocated or grown.
  */
+/* 0 for arguments that the calls refuse. */
+size_t jl_varlen_paged_workspace_bytes(int B, int total_tokens, int Hq, int Hkv, int head_dim,
+                                       int max_pages, int page_size);
+
 int jl_bifocal_prefill_varlen_paged(const void* q, const void* k_pages, const void* v_pages,
                                     const int32_t* block_table, int max_pages, int page_size,
                                     int n_pages, const int32_t* cu_seqlens,
                                     const int32_t* kv_lens, void* o, float* lse, int B,
                                     int total_tokens, int Hq, int Hkv, int head_dim,
                                     double rope_theta, int w_pretrained, int w_local,
-                                    void* stream);
+                                    void* workspace, size_t workspace_bytes, void* stream);
 
 /* The vanilla counterpart of jl_bifocal_prefill_varlen_paged. */
 int jl_rope_attention_varlen_paged(const void* q, const void* k_pages, const void* v_pages,
                                    const int32_t* block_table, int max_pages, int page_size,
                                    int n_pages, const int32_t* cu_seqlens, const int32_t* kv_lens,
                                    void* o, float* lse, int B, int total_tokens, int Hq, int Hkv,
-                                   int head_dim, double rope_theta, void* stream);
+                                   int head_dim, double rope_theta, void* workspace,
+                                   size_t workspace_bytes, void* stream);
 
 /*
  * Debug view of the schedule as the device computes it (Eqs. (2), (3), (5)),

@@ -155,12 +155,15 @@ def lib() -> ctypes.CDLL:
         L.jl_rope_attention_decode_shared.restype = i32
         L.jl_rope_attention_decode_shared.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, sz, vp, i32,
                                                       i32, i32, i32, i32, dbl, vp, sz, vp]
+        L.jl_varlen_paged_workspace_bytes.restype = sz
+        L.jl_varlen_paged_workspace_bytes.argtypes = [i32] * 7
         L.jl_bifocal_prefill_varlen_paged.restype = i32
         L.jl_bifocal_prefill_varlen_paged.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp,
-                                                      i32, i32, i32, i32, i32, dbl, i32, i32, vp]
+                                                      i32, i32, i32, i32, i32, dbl, i32, i32, vp, sz,
+                                                      vp]
         L.jl_rope_attention_varlen_paged.restype = i32
         L.jl_rope_attention_varlen_paged.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp,
-                                                     i32, i32, i32, i32, i32, dbl, vp]
+                                                     i32, i32, i32, i32, i32, dbl, vp, sz, vp]
         L.jl_debug_schedule.restype = i32
         L.jl_debug_schedule.argtypes = [vp, i32, vp, i32, i32, vp, vp, vp, vp]
         L.jl_debug_prefill_tiles.restype = i32
@@ -1118,10 +1121,15 @@ def decode_shared(q, k_pages, v_pages, block_table, plan, *, rope_theta: float =
     return out
 
 
+def varlen_paged_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, max_pages: int, page_size: int,
+                                 head_dim: int = 128) -> int:
+    return int(lib().jl_varlen_paged_workspace_bytes(B, T, Hq, Hkv, head_dim, max_pages, page_size))
+
+
 def prefill_varlen_paged(q, k_pages, v_pages, block_table, cu_seqlens, kv_lens, *,
                          w_pretrained: int = 1, w_local: int = 0, rope_theta: float = 1e6,
                          bifocal: bool = True, out=None, lse=None, want_lse: bool = False,
-                         stream=None):
+                         workspace=None, stream=None):
     """jl_bifocal_prefill_varlen_paged / jl_rope_attention_varlen_paged: packed raw queries q [T, Hq,
     128], sequence b's cu_seqlens[b] .. cu_seqlens[b + 1] - 1 (int32 [B + 1]) at the last of its
     kv_lens[b] (int32 [B]) positions, over pools [n_pages, page_size, Hkv, 128] raw, block_table
@@ -1155,11 +1163,16 @@ def prefill_varlen_paged(q, k_pages, v_pages, block_table, cu_seqlens, kv_lens, 
             _int(shape[0], "n_pages"), cp, lp, op,
             None if lse is None else _on8(lse, "lse", torch.float32, (Hq, T), index, device),
             _int(B, "B"), _int(T, "T"), Hq, _int(shape[2], "Hkv"), D, float(rope_theta))
+    if workspace is None:
+        workspace = _new(q, stream, (varlen_paged_workspace_bytes(
+            B, T, Hq, shape[2], max_pages, shape[1], D),), torch.uint8)
+    wp = _on8(workspace, "workspace", getattr(workspace, "dtype", None), None, index, device)
     if bifocal:
-        _check(lib().jl_bifocal_prefill_varlen_paged(*args, _int(w_pretrained, "w_pretrained"),
-                                                     _int(w_local, "w_local"), raw))
+        _check(lib().jl_bifocal_prefill_varlen_paged(
+            *args, _int(w_pretrained, "w_pretrained"), _int(w_local, "w_local"), wp,
+            workspace.nbytes, raw))
     else:
-        _check(lib().jl_rope_attention_varlen_paged(*args, raw))
+        _check(lib().jl_rope_attention_varlen_paged(*args, wp, workspace.nbytes, raw))
     return (out, lse) if want_lse else out
 
 

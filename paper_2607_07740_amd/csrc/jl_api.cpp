@@ -837,10 +837,16 @@ int check_shared(int B, int n_groups, int Hq, int Hkv, int head_dim, int max_pag
   return check_rows(B, Hq, Hkv, head_dim, 8, max_pages, page_size, bifocal, w_pre, w0, page_shift);
 }
 
+bool chunk_sizes_ok(int B, int T, int Hq, int Hkv) {
+  return B <= jl::kShMaxSeqs && !past_int32(T, Hq, 2) && !past_int32(2LL * B + 1024, Hkv, 1) &&
+         jl::chunk_rows_fit(B, T, Hq / Hkv);
+}
+
 int varlen_paged(bool bifocal, const void* q, const void* kp, const void* vp, const int32_t* table,
                  int max_pages, int page_size, int n_pages, const int32_t* cu,
                  const int32_t* kv_lens, void* o, float* lse, int B, int T, int Hq, int Hkv,
-                 int head_dim, double theta, int w_pre, int w0, void* stream) {
+                 int head_dim, double theta, int w_pre, int w0, void* ws, size_t ws_bytes,
+                 void* stream) {
   int shift = 0;
   int st = check_rows(B, Hq, Hkv, head_dim, jl::kShMaxGroup, max_pages, page_size, bifocal, w_pre,
                       w0, &shift);
@@ -852,31 +858,27 @@ int varlen_paged(bool bifocal, const void* q, const void* kp, const void* vp, co
   if ((long long)n_pages * page_size > 0x7fffffffLL)
     return fail(JL_ERR_UNSUPPORTED, "a pool of %lld tokens (at most 2^31 - 1)",
                 (long long)n_pages * page_size);
-  if (B > jl::kShMaxSeqs || past_int32(T, Hq, 2) || past_int32(2LL * B + 1024, Hkv, 1) || !jl::chunk_rows_fit(B, T, Hq / Hkv))
+  if (!chunk_sizes_ok(B, T, Hq, Hkv))
     return fail(JL_ERR_UNSUPPORTED, "%d tokens of %d sequences in one call", T, B);
   if (!aligned16(q) || !aligned16(kp) || !aligned16(vp) || !aligned16(o))
     return fail(JL_ERR_INVALID_ARG, "q, k_pages, v_pages, o must be non-null and 16-byte aligned");
   if (lse != nullptr && !aligned4(lse)) return fail(JL_ERR_INVALID_ARG, "lse must be 4-byte aligned");
   if (!aligned4(table) || !aligned4(cu) || !aligned4(kv_lens))
     return fail(JL_ERR_INVALID_ARG, "block_table, cu_seqlens, kv_lens must be non-null and aligned");
+  const size_t need = jl::chunk_scratch_bytes(B, T, Hq, Hkv, max_pages, page_size);
+  if (ws == nullptr || ws_bytes < need)
+    return fail(JL_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, ws_bytes);
+  if (!aligned16(ws)) return fail(JL_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
   Tables tab{};
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   st = get_table(theta, max_pages * page_size, s, &tab);
   if (st != JL_OK) return st;
-  std::lock_guard<std::mutex> launch_lock(g_prefill_mu);
-  void* scratch = nullptr;
-  const size_t bytes = jl::chunk_scratch_bytes(B, T, Hq, Hkv, max_pages, page_size);
-  st = get_scratch(s, bytes, &scratch);
-  if (st != JL_OK) return st;
-  if (scratch == nullptr)
-    return fail(JL_ERR_HIP, "packed chunks: %zu bytes of scratch cannot be allocated under "
-                "stream capture (make the call once before)", bytes);
   hipEvent_t ev0, ev1;
   timing_events(0, &ev0, &ev1);
   const hipError_t e = jl::launch_chunk_rows(
       bifocal, (const uint16_t*)q, (const uint16_t*)kp, (const uint16_t*)vp, table, max_pages,
-      n_pages, shift, cu, kv_lens, (uint16_t*)o, lse, tab.f32, tab.half, tab.f16, B, T, Hq, Hkv, w_pre, w0,
-      (float)g_rescale_log2.load(), jl::cu_count(), scratch, s, ev0, ev1);
+      n_pages, shift, cu, kv_lens, (uint16_t*)o, lse, tab.f32, tab.half, tab.f16, B, T, Hq, Hkv,
+      w_pre, w0, (float)g_rescale_log2.load(), jl::cu_count(), ws, s, ev0, ev1);
   if (e != hipSuccess) return hip_fail(e, "packed chunk launch");
   return ok();
 }
@@ -1475,26 +1477,37 @@ int jl_rope_attention_decode_shared(const void* q, const void* k_pages, const vo
                        workspace, workspace_bytes, stream);
 }
 
+size_t jl_varlen_paged_workspace_bytes(int B, int total_tokens, int Hq, int Hkv, int head_dim,
+                                       int max_pages, int page_size) {
+  int shift = 0;
+  if (total_tokens < 1 || check_rows(B, Hq, Hkv, head_dim, jl::kShMaxGroup, max_pages, page_size,
+                                     false, 1, 0, &shift) != JL_OK ||
+      !chunk_sizes_ok(B, total_tokens, Hq, Hkv))
+    return 0;
+  return jl::chunk_scratch_bytes(B, total_tokens, Hq, Hkv, max_pages, page_size);
+}
+
 int jl_bifocal_prefill_varlen_paged(const void* q, const void* k_pages, const void* v_pages,
                                     const int32_t* block_table, int max_pages, int page_size,
                                     int n_pages, const int32_t* cu_seqlens,
                                     const int32_t* kv_lens, void* o, float* lse, int B,
                                     int total_tokens, int Hq, int Hkv, int head_dim,
                                     double rope_theta, int w_pretrained, int w_local,
-                                    void* stream) {
+                                    void* workspace, size_t workspace_bytes, void* stream) {
   return varlen_paged(true, q, k_pages, v_pages, block_table, max_pages, page_size, n_pages,
                       cu_seqlens, kv_lens, o, lse, B, total_tokens, Hq, Hkv, head_dim, rope_theta,
-                      w_pretrained, w_local, stream);
+                      w_pretrained, w_local, workspace, workspace_bytes, stream);
 }
 
 int jl_rope_attention_varlen_paged(const void* q, const void* k_pages, const void* v_pages,
                                    const int32_t* block_table, int max_pages, int page_size,
                                    int n_pages, const int32_t* cu_seqlens, const int32_t* kv_lens,
                                    void* o, float* lse, int B, int total_tokens, int Hq, int Hkv,
-                                   int head_dim, double rope_theta, void* stream) {
+                                   int head_dim, double rope_theta, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
   return varlen_paged(false, q, k_pages, v_pages, block_table, max_pages, page_size, n_pages,
                       cu_seqlens, kv_lens, o, lse, B, total_tokens, Hq, Hkv, head_dim, rope_theta,
-                      1, 0, stream);
+                      1, 0, workspace, workspace_bytes, stream);
 }
 
 int jl_debug_schedule(const int32_t* lengths, int n_lengths, const int32_t* positions,

@@ -289,3 +289,50 @@ def test_keys_and_queries_of_any_magnitude(n):
             c.kp[j] = times(c.kp[j].astype(np.int32), e)
     say("magnitudes", n)
     assert_close(to_f64(c.run(150, 60)), want, what="magnitudes")
+
+
+def test_two_graphs_and_an_eager_call_at_once():
+    """Calls of different sizes on three streams, two of them replays of graphs that one stream captured:
+    none sees another's workspace."""
+    cs = [Chunks([900, 300], [260, 200], 8, 2, 64, seed=61), Chunks([400, 77, 500], [3, 70, 130], 8, 2, 64, seed=62),
+          Chunks([1200], [700], 8, 2, 64, seed=63)]
+    data = [(to_dev(c.q), to_dev(c.kp), to_dev(c.vp), _i32(c.table), _i32(c.cu), _i32(c.lens)) for c in cs]
+    run = lambda i, **kw: api.prefill_varlen_paged(*data[i], w_pretrained=150, w_local=60, **kw)  # noqa: E731
+    say("at once")
+    want = [run(i) for i in range(3)]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(run(i))
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for turn in range(4):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+        with torch.cuda.stream(streams[2]):
+            outs[2:] = [run(2)]
+        torch.cuda.synchronize()
+        for i in range(3):
+            assert torch.equal(outs[i], want[i]), (turn, i)
+
+
+def test_the_workspace_is_the_callers():
+    c = Chunks([300, 90], [150, 2], 8, 2, 64, seed=65)
+    data = (to_dev(c.q), to_dev(c.kp), to_dev(c.vp), _i32(c.table), _i32(c.cu), _i32(c.lens))
+    n = api.varlen_paged_workspace_bytes(2, 152, 8, 2, c.max_pages, 64)
+    say("workspace")
+    ws = torch.full((n + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    one = api.prefill_varlen_paged(*data, w_pretrained=100, w_local=30, workspace=ws[:n])
+    torch.cuda.synchronize()
+    assert (ws[n:] == 0xFF).all()
+    assert torch.equal(one, api.prefill_varlen_paged(*data, w_pretrained=100, w_local=30))
+    with pytest.raises(api.JetLongError) as e:
+        api.prefill_varlen_paged(*data, w_pretrained=100, w_local=30, workspace=ws[:n - 16])
+    assert e.value.status == api.JL_ERR_WORKSPACE

@@ -165,6 +165,12 @@ def test_sizes_of_plans_and_workspaces():
         assert api.shared_plan_bytes(*bad) == 0
     assert api.decode_shared_workspace_bytes(4, 8, 2, 64) == 0
     assert api.decode_shared_workspace_bytes(4096, 8, 2) == 0
+    one, two = (api.varlen_paged_workspace_bytes(4, t, 8, 2, 64, 64) for t in (40, 4000))
+    assert 0 < one < two
+    for bad in ((0, 40, 8, 2, 64, 64), (4, 0, 8, 2, 64, 64), (4, 40, 7, 2, 64, 64),
+                (4, 40, 8, 2, 0, 64), (4, 40, 8, 2, 64, 48), (2049, 40, 8, 2, 64, 64),
+                (4, 40, 8, 2, 64, 64, 96), (4, 1 << 21, 8, 2, 64, 64)):
+        assert api.varlen_paged_workspace_bytes(*bad) == 0
 
 
 @pytest.mark.parametrize("kw,code", [
@@ -174,15 +180,18 @@ def test_sizes_of_plans_and_workspaces():
     (dict(max_pages=0), BAD), (dict(max_pages=1 << 18), UNS), (dict(n_pages=0), BAD),
     (dict(n_pages=1 << 26), UNS), (dict(theta=-1.0), BAD), (dict(q=None), BAD), (dict(k=MIS), BAD),
     (dict(v=None), BAD), (dict(o=P(0x1008)), BAD), (dict(lse=MIS), BAD), (dict(table=None), BAD),
-    (dict(cu=MIS), BAD), (dict(lens=None), BAD)])
+    (dict(cu=MIS), BAD), (dict(lens=None), BAD), (dict(ws=None), api.JL_ERR_WORKSPACE),
+    (dict(ws_bytes=4096), api.JL_ERR_WORKSPACE),
+    (dict(ws=P(0x1008)), BAD)])
 def test_chunk_arguments_are_checked(kw, code):
     d = dict(q=A, k=A, v=A, table=A, max_pages=8, page=64, n_pages=32, cu=A, lens=A, o=A, lse=None,
-             B=4, T=20, Hq=8, Hkv=2, d=128, theta=1e6)
+             B=4, T=20, Hq=8, Hkv=2, d=128, theta=1e6, ws=A, ws_bytes=1 << 40)
     d.update(kw)
+    ws = (d["ws"], d["ws_bytes"], None)
     head = (d["q"], d["k"], d["v"], d["table"], d["max_pages"], d["page"], d["n_pages"], d["cu"],
             d["lens"], d["o"], d["lse"], d["B"], d["T"], d["Hq"], d["Hkv"], d["d"], d["theta"])
     L = api.lib()
-    assert L.jl_bifocal_prefill_varlen_paged(*head, 32, 4, None) == code
-    assert L.jl_rope_attention_varlen_paged(*head, None) == code
+    assert L.jl_bifocal_prefill_varlen_paged(*head, 32, 4, *ws) == code
+    assert L.jl_rope_attention_varlen_paged(*head, *ws) == code
     for w in ((0, 4), (32, -1)):
-        assert L.jl_bifocal_prefill_varlen_paged(*head, *w, None) in (BAD, code)
+        assert L.jl_bifocal_prefill_varlen_paged(*head, *w, *ws) in (BAD, code)
