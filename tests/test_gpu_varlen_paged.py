@@ -336,3 +336,32 @@ def test_the_workspace_is_the_callers():
     with pytest.raises(api.JetLongError) as e:
         api.prefill_varlen_paged(*data, w_pretrained=100, w_local=30, workspace=ws[:n - 16])
     assert e.value.status == api.JL_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("n", [3, 100, 300])
+@pytest.mark.parametrize("shape", ["rising", "falling", "zigzag", "one peak"])
+def test_references_follow_exact_scores(n, shape):
+    """One slow channel holds whole numbers: its rotation is the identity to 1e-3 and to 1e-6 in the
+    scores, 4.08 log2 units a step, whose differences bf16 holds to 2^-8: the weight of a step, 0.06, is
+    off by 0.0007.  The references move by hundreds; tolerances as above."""
+    c = Chunks([700, 300], [n, 5], 8, 2, 64, seed=70)
+    for b, (q, k, v) in enumerate(c.seqs):
+        L = c.lens[b]
+        x = {"rising": np.linspace(-120, 120, L), "falling": np.linspace(120, -120, L),
+             "zigzag": 100 * np.cos(np.arange(L) / 9.0),
+             "one peak": np.where(np.arange(L) == L // 3, 110, -110)}[shape].round()
+        qq, kk = np.zeros(q.shape, np.float32), np.zeros(k.shape, np.float32)
+        qq[..., 63], kk[..., 63] = 32.0, x.astype(np.float32)[None, :, None]
+        c.seqs[b] = (synth.bf16_bits(qq), synth.bf16_bits(kk), v)
+        for j in range(-(-L // 64)):
+            part = slice(64 * j, min(64 * j + 64, L))
+            c.kp[c.table[b, j], :part.stop - part.start] = c.seqs[b][1][0, part]
+    c.q = np.concatenate([s[0][0, L - m:] for s, L, m in zip(c.seqs, c.lens, c.n)])
+    say("exact scores", n, shape)
+    for bifocal in (True, False):
+        out, lse = c.run(256, 90, bifocal, want_lse=True)
+        o, l = c.want(256, 90, bifocal)
+        assert_close(to_f64(out), o, what="out")
+        # row sums of 340 at most, by a query that is rounded to half a step of bf16, 2^-8 of itself:
+        # 4.0803 to 4.09375
+        assert np.abs(lse.cpu().numpy() - l).max() < 340 * 2.0 ** -8 + 2e-2
