@@ -862,10 +862,16 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       co = 256 * key + 16 * slot;
     }
     const size_t off = (size_t)(uint32_t)row * kv_row_bytes;
-    // without the nontemporal hint, with which a tile's next view finds nothing in the L2: 8 samples of
-    // 128K fetched 774 MB for 569 (a branch between the two costs more than the hint gives)
-    dma16_s(kbase + off, ko, dst);
-    dma16_s(vbase + off, vo, dst + kShImg);
+    // few rows: their keys are theirs alone, and not kept in the caches (passes over new inputs: 64
+    // chats 133 -> 126 us, drafts 111 -> 107, 8 samples of 128K 230 -> 228, though their tiles' next
+    // views then miss the L2: 774 MB fetched for 569); blocks of many rows mostly share theirs
+    if constexpr (decltype(all)::value) {
+      dma16_s(kbase + off, ko, dst);
+      dma16_s(vbase + off, vo, dst + kShImg);
+    } else {
+      dma16_s_nt(kbase + off, ko, dst);
+      dma16_s_nt(vbase + off, vo, dst + kShImg);
+    }
     if (t.lG != 0) {
       const FastDiv f = {t.m, t.lG & 63, 2};
       co = fastdiv_ge2((uint32_t)(t.km + key), f) * 256 + 16 * (ln & 15);
