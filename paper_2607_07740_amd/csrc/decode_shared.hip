@@ -969,11 +969,11 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
   };
 
   int n = 0;  // visits of the held segments
-  // Addresses of visits j0 .. j0 + 127, by the last two waves
-  auto fill = [&](int j0) __attribute__((always_inline)) {
+  // Addresses of visits j0 .. j0 + count - 1, a thread each: the last waves
+  auto fill = [&](int j0, int count) __attribute__((always_inline)) {
     int me = tid;
     asm volatile("" : "+v"(me));  // as above: nothing of this is held in between
-    const int at = me - (kShThreads - kShList / 2), j = j0 + at;
+    const int at = me - (kShThreads - count), j = j0 + at;
     if (at < 0 || j >= n) return;
     int i = 0;  // the held segment: the last that begins at or before the visit
 #pragma unroll
@@ -1029,7 +1029,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     if (i + 1 < n) rotate(all, half, ln, i + 1);
   };
   auto refill = [&](int i) __attribute__((always_inline)) {
-    if ((i & (kShList / 2 - 1)) == 0 && i > 0 && i + kShList / 2 < n) fill(i + kShList / 2);
+    if ((i & (kShList / 2 - 1)) == 0 && i > 0 && i + kShList / 2 < n) fill(i + kShList / 2, kShList / 2);
   };
   auto start = [&](auto all, auto half, Copier& cp, int ln) __attribute__((always_inline)) {
     constexpr int k = decltype(all)::value ? kShCopies : 2 * kShCopies;
@@ -1417,8 +1417,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
     __syncthreads();
     auto run = [&](auto half) __attribute__((always_inline)) {
       if (tid == 0) s_again = 0;
-      fill(0);
-      fill(kShList / 2);
+      fill(0, kShList);
       __syncthreads();
       if (kind) {
         int ln = lane;
