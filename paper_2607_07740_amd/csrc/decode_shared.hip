@@ -328,15 +328,32 @@ __device__ inline void plan_ranges(const SharedPlanArgs& a, const PlanView& v, i
   if (n_wg > 0) rg = ranges_of(total, n_wg);
   unsigned long long rows = 0;
   const unsigned long long st0 = st;
+  __shared__ unsigned long long s_first[kPlThreads];
+  const bool one_each = per == 1;
   for (int i = i0; i < i1; ++i) {
     const unsigned long long c = cost(i);
     if (c == 0) continue;
     const int w0 = rg.owner(st + kSegCost), w1 = rg.owner(st + c - visit_cost(s_rows[i]));
     rows += (unsigned long long)(w1 - w0 + 1) * s_states[i];
-    int w = rg.owner(st);  // workgroups whose ranges begin inside this segment
-    if (rg.begin(w) < st) ++w;
-    for (; w < n_wg && rg.begin(w) < st + c; ++w) v.wg_first[w] = i;
+    if (!one_each) {
+      int w = rg.owner(st);  // workgroups whose ranges begin inside this segment
+      if (rg.begin(w) < st) ++w;
+      for (; w < n_wg && rg.begin(w) < st + c; ++w) v.wg_first[w] = i;
+    }
     st += c;
+  }
+  if (one_each) {  // a thread for each workgroup: the last segment that begins at or before its range
+    if (tid < n_segs) s_first[tid] = st0;
+    __syncthreads();
+    for (int w = tid; w < n_wg; w += (int)blockDim.x) {
+      const unsigned long long x = rg.begin(w);
+      int lo = 0, hi = n_segs - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (s_first[mid] <= x) lo = mid; else hi = mid - 1;
+      }
+      v.wg_first[w] = lo;
+    }
   }
   unsigned long long all_rows;
   unsigned long long row = plan_scan(rows, s_scan, &all_rows) - rows;
@@ -403,7 +420,10 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
     s_start[i] = x;
     if (i > 0) bad |= min(max(a.group_starts[i - 1], 0), a.B) > x;
   }
-  for (int i = tid; i < a.n_groups; i += nt) s_pre[i] = INT_MAX;
+  for (int i = tid; i < a.n_groups; i += nt) {
+    s_pre[i] = INT_MAX;
+    s_blk[i] = a.shared[i];  // until the blocks are counted
+  }
   for (int i = tid; i < a.B; i += nt) {
     const int seq = a.members != nullptr ? a.members[i] : i;
     const bool ok = (unsigned)seq < (unsigned)a.B;
@@ -436,7 +456,7 @@ __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs 
     unsigned long long x = 0, tot;
     if (i < a.n_groups) {
       const int n = s_start[i + 1] - s_start[i], low = s_pre[i];
-      const int P = n > 1 && low != INT_MAX ? min(max(a.shared[i], 0), low) & -a.page : 0;
+      const int P = n > 1 && low != INT_MAX ? min(max(s_blk[i], 0), low) & -a.page : 0;
       s_pre[i] = P;
       x = P > 0 ? (n + per_block - 1) / per_block : 0;
     }
