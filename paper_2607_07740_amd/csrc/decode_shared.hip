@@ -216,12 +216,7 @@ constexpr int kPlThreads = 1024, kPlWaves = kPlThreads / 64;  // at most; few se
 template <typename T>
 __device__ inline T plan_scan(T v, T* s, T* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  T incl = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const T x = __shfl_up(incl, d);
-    if (lane >= d) incl += x;
-  }
+  const T incl = wave_scan(v);
   __syncthreads();
   if (lane == 63) s[wave] = incl;
   __syncthreads();
@@ -238,17 +233,6 @@ __device__ inline T plan_scan(T v, T* s, T* total) {
   }
   *total = all;
   return before + incl;
-}
-
-__device__ inline int wave_min(int v) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v = min(v, __shfl_xor(v, d));
-  return v;
-}
-__device__ inline int wave_max(int v) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v = max(v, __shfl_xor(v, d));
-  return v;
 }
 
 // max(1, ceil(len / w_pre)) for len <= 2^23, without a 64-bit division
@@ -394,9 +378,10 @@ __device__ inline void plan_ranges(const SharedPlanArgs& a, const PlanView& v, i
   }
 }
 
-// A decode step's plan, by one workgroup: bound by the latency of its dependent reads and scans (8.5 us
-// for 2 sequences, 12 for 16 with views of two G; 256 threads instead of 1024 up to 128
-// sequences: 10.4 -> 8.6).  One plan serves every layer of a step.
+// A decode step's plan, by one workgroup: bound by the latency of its dependent reads and scans (7.0 us
+// for 2 sequences, 8.0 for 16 with views of two G, 8.6 for 64; 8.5, 11.1 and 11.0 with scans by
+// exchanges through LDS and one thread naming a segment's workgroups; 256 threads, not 1024, up to
+// 128 sequences: two microseconds).  One plan serves every layer of a step.
 __global__ __launch_bounds__(kPlThreads) void shared_plan_kernel(SharedPlanArgs a) {
   extern __shared__ int s_mem[];
   __shared__ unsigned long long s_scan[kPlWaves];
@@ -1415,12 +1400,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       const unsigned long long other = some & (kind ? ~big : big);
       const int stop = other != 0 ? __builtin_ctzll(other) : kShSegs;
       if (ln >= stop) vb = va;
-      int incl = vb - va;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(incl, d);
-        if (ln >= d) incl += y;
-      }
+      const int incl = wave_scan(vb - va);
       s_from[ln] = va;
       s_before[ln] = incl - (vb - va);
       if (ln == 63) s_tiles[0].k0 = incl;

@@ -160,6 +160,46 @@ __device__ inline f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
 
 __device__ inline u32x4 load16(const void* p) { return *(const u32x4*)p; }
 
+// Scans over a wave by lane shifts inside rows of 16 and broadcasts of their last lanes, which take a
+// few cycles each where an exchange through LDS takes a hundred.  wave_step: the value that comes to a
+// lane in one of the six steps, `none` where none does.
+template <int step>
+__device__ inline uint32_t wave_step(uint32_t x, uint32_t none) {
+  constexpr int ctrl = step == 0 ? 0x111 : step == 1 ? 0x112 : step == 2 ? 0x114
+                       : step == 3 ? 0x118 : step == 4 ? 0x142 : 0x143;  // row_shr 1 2 4 8, row_bcast 15 31
+  constexpr int rows = step == 4 ? 0xa : step == 5 ? 0xc : 0xf;
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)x, ctrl, rows, 0xf, false);
+}
+template <int step, typename T>
+__device__ inline T wave_add_step(T x) {
+  if constexpr (sizeof(T) == 8) {
+    const uint64_t u = (uint64_t)x;
+    const uint32_t lo = wave_step<step>((uint32_t)u, 0u), hi = wave_step<step>((uint32_t)(u >> 32), 0u);
+    return x + (T)((uint64_t)hi << 32 | lo);
+  } else {
+    return x + (T)wave_step<step>((uint32_t)x, 0u);
+  }
+}
+template <typename T>
+__device__ inline T wave_scan(T x) {  // inclusive sums, in lane order
+  x = wave_add_step<0>(x);
+  x = wave_add_step<1>(x);
+  x = wave_add_step<2>(x);
+  x = wave_add_step<3>(x);
+  x = wave_add_step<4>(x);
+  return wave_add_step<5>(x);
+}
+__device__ inline int wave_min(int v) {
+  v = min(v, (int)wave_step<0>((uint32_t)v, 0x7fffffffu));
+  v = min(v, (int)wave_step<1>((uint32_t)v, 0x7fffffffu));
+  v = min(v, (int)wave_step<2>((uint32_t)v, 0x7fffffffu));
+  v = min(v, (int)wave_step<3>((uint32_t)v, 0x7fffffffu));
+  v = min(v, (int)wave_step<4>((uint32_t)v, 0x7fffffffu));
+  v = min(v, (int)wave_step<5>((uint32_t)v, 0x7fffffffu));
+  return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ inline int wave_max(int v) { return ~wave_min(~v); }  // ~ turns the order round
+
 // Two rotate-half pairs by v_dot2_f32_bf16 (exact bf16 products, one fp32
 // rounding each), rounded to bf16 and packed.  From the raw words
 // wl = (x_a, x_b), wh = (x_{a+64}, x_{b+64}) and the bf16 (cos, sin) of

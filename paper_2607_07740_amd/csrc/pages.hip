@@ -25,12 +25,7 @@ constexpr int kBookWaves = kBookThreads / 64;
 template <typename T>
 __device__ inline T block_scan(T v, T* s, T* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  T incl = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const T x = __shfl_up(incl, d);
-    if (lane >= d) incl += x;
-  }
+  const T incl = wave_scan(v);
   __syncthreads();  // s may still be read from the last scan
   if (lane == 63) s[wave] = incl;
   __syncthreads();
@@ -102,8 +97,8 @@ __global__ __launch_bounds__(kBookThreads) void fork_kernel(ForkArgs a) {
 // needs holds k.  A sequence that writes into a partly filled page which others
 // name too gets a fresh one for it, but for the last writer of a page that only
 // writers name.  If the pages do not suffice nothing is changed.  Bound by latency: length, entry,
-// count, sums and the second read of the counts follow each other (16 sequences, 512 pages: 11 us;
-// 12.7 with 1024 threads and 64-bit divisions).
+// count, sums and the second read of the counts follow each other (16 sequences, 512 pages: 11.2
+// us; 12.7 with 1024 threads and 64-bit divisions).
 struct ReserveArgs {
   Pages p;
   const int32_t* n_new;
