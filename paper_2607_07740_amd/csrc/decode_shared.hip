@@ -31,7 +31,7 @@
 // What bounds it: HBM where most tiles have one visit (64 chats behind 4 prompts, 536 MB: 118 us
 // with 32/8 heads, 4.5 TB/s; the copies alone take 97 to 101), the multiplying waves where tiles
 // have several (16 samples of 32K with G = 1 and 2, 222 MB: 89 us, 67 without them; 8 of 128K with
-// G = 4 and 5, 544 MB: 218, 179 without), latency where there are few keys (2 sequences of 1.2K: 13).
+// G = 4 and 5, 544 MB: 220, 179 without), latency where there are few keys (2 sequences of 1.2K: 13).
 // Tiles of 32 keys keep four of them in flight beside the two in use, and cut 1000 keys into enough visits
 // for 32 workgroups of each of 8 kv heads.
 #include <algorithm>
@@ -171,7 +171,7 @@ static size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 
 // Whether the blocks of longer chunks go to the prefill kernel, which takes 64 keys of 256 rows in
 // the time of 32 here (turns of 512, 600, 1 and 700 rows behind 15000, 34000, 9000 and 0 keys, 32/8
-// heads: 754 -> 600 us): where the rows beyond a token per sequence make a few of its blocks, and with what it
+// heads: 754 -> 560 us): where the rows beyond a token per sequence make a few of its blocks, and with what it
 // asks of the cache.  A sequence's go there if they are more than 128.
 static bool chunk_blocks(int B, int T, int g, int max_pages, int page) {
   return kChunkBlockRows % g == 0 && page >= kChunkTile && max_pages <= prefill_chunk_max_pages() &&
@@ -627,8 +627,9 @@ __global__ __launch_bounds__(kPlThreads) void chunk_plan_kernel(SharedPlanArgs a
                             : Member{-1, 0, -1, -1};
   }
   __syncthreads();
-  // The prefill kernel's blocks, cut into parts of about the same visits: kPartWaves for every
-  // workgroup of a kv head.  A sequence's parts are listed part after part, so that the
+  // The prefill kernel's blocks, cut into parts of about the same visits: for every workgroup of a
+  // kv head as many as there are blocks for it, rounded up, at most kPartWaves (29 blocks for 32
+  // workgroups, the turns above: one 550 us, three 590; 88 blocks: one 1440, three 1170).  A sequence's parts are listed part after part, so that the
   // blocks that run beside each other read the same keys; blocks of fewer parts leave empty ones.
   int n_parts = 0;
   if (n_big > 0) {
@@ -646,7 +647,8 @@ __global__ __launch_bounds__(kPlThreads) void chunk_plan_kernel(SharedPlanArgs a
       mine += (unsigned long long)visits_of(b, j - s_big[b]);
     }
     plan_scan(mine, s_scan, &all);
-    const unsigned shares = (unsigned)(kPartWaves * a.n_wg);
+    const unsigned shares =
+        (unsigned)min(kPartWaves, (n_big + a.n_wg - 1) / a.n_wg) * (unsigned)a.n_wg;
     const unsigned long long even = all >> 32 == 0 ? ((unsigned)all + shares - 1) / shares : all / shares + 1;
     int target = (int)min(max(even, (unsigned long long)kChunkMinPart), 0x1fffffffull);
     auto parts_of = [&](int visits) { return max(1, min(16, (visits + target / 2) / target)); };

@@ -918,7 +918,7 @@ __device__ __forceinline__ bool prefill_block(const PrefillArgs& a, const Work& 
 // Packed chunks behind paged caches: the parts of a list of query blocks of different sequences,
 // which a planning kernel has cut to about the same length, one per workgroup and kv head.  Bound by the
 // matrix cores: turns of 512, 600 and 700 rows behind 15000, 34000 and 0 keys (32/8 heads, 459
-// GFLOP) in 524 to 567 us, 0.81 to 0.88 PFLOP/s.  A loop over parts in a workgroup spilled registers
+// GFLOP) in 502 to 527 us, 0.87 to 0.91 PFLOP/s.  A loop over parts in a workgroup spilled registers
 // of the block's loops; a part has one, with an exit where the list has ended.
 __device__ inline Work chunk_work(const PrefillArgs& a, const ChunkPart& p, int kvh) {
   Work W;
@@ -1026,7 +1026,7 @@ __global__ __launch_bounds__(256) void merge_parts_kernel(PrefillArgs a) {
 }
 
 // The same for the blocks of packed chunks that were cut.  Bound by reading the states (the turns above:
-// 23 us for about 100 MB); two groups of 128 rows instead of 8 of 32 took 42.
+// 9.7 us for about 40 MB); with 100 MB two groups of 128 rows took 42 us, 8 of 32 23.
 __global__ __launch_bounds__(256) void merge_chunks_kernel(PrefillArgs a) {
   const int at = blockIdx.x / a.Hkv, kvh = blockIdx.x - at * a.Hkv;
   if (at >= *a.n_chunk_parts) return;
