@@ -1026,7 +1026,7 @@ __global__ __launch_bounds__(256) void merge_parts_kernel(PrefillArgs a) {
 }
 
 // The same for the blocks of packed chunks that were cut.  Bound by reading the states (the turns above:
-// 9.7 us for about 40 MB); with 100 MB two groups of 128 rows took 42 us, 8 of 32 23.
+// 9.7 us for 20 MB, a chain of reads); with 100 MB two groups of 128 rows took 42 us, 8 of 32 23.
 __global__ __launch_bounds__(256) void merge_chunks_kernel(PrefillArgs a) {
   const int at = blockIdx.x / a.Hkv, kvh = blockIdx.x - at * a.Hkv;
   if (at >= *a.n_chunk_parts) return;
