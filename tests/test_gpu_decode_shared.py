@@ -3,7 +3,7 @@ dense cache of its own.
 
 Tolerances: the parity bounds of the decode and prefill tests.  With u = 2^-8 the unit roundoff of
 bf16, a score <q, k> / sqrt(128) of unit normals carries the roundings of the rotated query, of
-cos and sin and of the rotated key: three of relative size u / sqrt(3) in the mean square on
+cos and sin and of the rotated key (where they are not in fp16): three of relative size u / sqrt(3) in the mean square on
 products whose root sum of squares is 1, so 0.004 to 0.007 rms.  That shifts an output,
 a weighted mean of values of size 1, by less than its own size times the root of the
 sum of the squared weights: below 0.004 rms, 0.02 at five times that with the output's own
@@ -366,3 +366,51 @@ def test_distance_from_64_bits():
         off = np.linalg.norm(to_f64(out) - want) / np.linalg.norm(want)
         say("distance", w_pre, off)
         assert off < 3e-3
+
+
+def test_two_graphs_at_once():
+    """Steps captured on one stream, plan and workspace their own, replayed on two at once."""
+    bs = [Batch([(256, [3, 50, 70]), (0, [300])], 8, 2, 64, seed=71), Batch([(640, [9, 1]), (64, [64] * 5)], 8, 2, 64, seed=72)]
+    data = [(to_dev(b.q), to_dev(b.kp), to_dev(b.vp), _i32(b.table), _i32(b.lens), _i32(b.starts), _i32(b.share)) for b in bs]
+
+    def step(b, d):
+        plan = api.shared_plan(d[4], d[5], d[6], Hq=8, Hkv=2, page_size=64, max_pages=b.max_pages,
+                               w_pretrained=120, w_local=30)
+        return api.decode_shared(*d[:4], plan)
+
+    say("two graphs")
+    want = [step(b, d) for b, d in zip(bs, data)]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for b, d in zip(bs, data):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(step(b, d))
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in bs]
+    for turn in range(4):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert torch.equal(outs[i], want[i]), (turn, i)
+            assert_close(to_f64(outs[i]), bs[i].want(120, 30, True), what="graph %d" % i)
+
+
+def test_one_sequence_of_large_keys_leaves_the_others_right():
+    """Its ranges run in bf16; what stands beside them is right too, and the same twice."""
+    b = Batch([(192, [40, 9]), (0, [700]), (0, [100])], 8, 2, 64, seed=73)
+    want = b.want(100, 40, True)
+    b.q[2] = _times(b.q[2], -30)
+    for j in b.table[2][b.table[2] >= 0]:
+        b.kp[j] = _times(b.kp[j], 30)
+    plan = b.plan(100, 40, True)
+    say("large keys of one")
+    one, two = b.run(plan), b.run(plan)
+    torch.cuda.synchronize()
+    assert torch.equal(one, two)
+    assert_close(to_f64(one), want, what="large keys of one")

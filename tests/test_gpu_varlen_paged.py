@@ -1,7 +1,7 @@
 """Packed chunks behind paged caches against the fp64 oracle's prefill of each whole sequence.
 
 Tolerances: the parity bounds of the prefill tests, whose roundings these are (rotated queries and
-keys, cos and sin of the keys, softmax weights in bf16, u = 2^-8): scores of unit normals are off
+keys, cos and sin of the keys, softmax weights in bf16 at worst, u = 2^-8): scores of unit normals are off
 by 0.007 rms at most, which moves an output, a weighted mean of values of size 1, by less than
 0.004 rms; with its own rounding 2e-2 at most and 2e-3 in the mean.  The row sums carry the scores' errors averaged
 over the weights: 2e-2."""
