@@ -93,6 +93,12 @@ __host__ __device__ inline int state_halves(const Segment& s) {
   const int tiles = (s.kend - s.k0 + kShTile - 1) / kShTile;
   return s.rows <= kShFew && 2LL * s.visits > 3LL * tiles ? 2 : 1;
 }
+// Whether a chunk's segment is whole in one range and has one state: then its workgroup writes the
+// rows, and the merge passes them over.  Where it has two, no run of it may write them, one in
+// bf16 neither: the merge would put the states over them.
+__host__ __device__ inline bool written_whole(const Segment& s) {
+  return s.len > 0 && s.n_w == 1 && state_halves(s) == 1;
+}
 
 struct PlanView {
   int* header;
@@ -1328,7 +1334,7 @@ __global__ __launch_bounds__(kShThreads, 2) void shared_rows_kernel(SharedArgs a
       }
     }
     if (row < rows) {
-      if (!FEW && sg.len > 0 && sg.n_w == 1) {  // a chunk's block that is whole here
+      if (!FEW && written_whole(sg)) {
         const int t = by_g(row);
         const Member mb = pv.members[sg.m0 + t];
         if (mb.seq >= 0) {
@@ -1485,7 +1491,7 @@ __global__ __launch_bounds__(512) void merge_shared_kernel(SharedArgs a) {
       if (seg < 0) return;
       const Segment sg = pv.segs[seg];
       const int n = sg.n_w * state_halves(sg);
-      if (sg.len > 0 && n == 1) {  // written by its workgroup
+      if (written_whole(sg)) {
         on = false;
         return;
       }

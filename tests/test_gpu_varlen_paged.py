@@ -365,3 +365,24 @@ def test_references_follow_exact_scores(n, shape):
         # row sums of 340 at most, by a query that is rounded to half a step of bf16, 2^-8 of itself:
         # 4.0803 to 4.09375
         assert np.abs(lse.cpu().numpy() - l).max() < 340 * 2.0 ** -8 + 2e-2
+
+
+@pytest.mark.parametrize("lens,n,w_pre,w0", [
+    ([30], [4], 16, 8), ([60], [16], 32, 20), ([80], [16], 64, 40),
+    ([80, 30, 40, 60], [16, 1, 3, 16], 16, 8)])
+@pytest.mark.parametrize("exp", [18, -30])
+def test_short_sequences_of_any_magnitude(lens, n, w_pre, w0, exp):
+    """As above, where a few rows of a short sequence are whole in one workgroup and two pairs of waves
+    take its visits: the second run's result has to stand, its row sums too.  The softmax has 27 keys
+    at least, so its weights' squares sum to 0.16 at most, and the scores' 0.007 rms move outputs and row
+    sums by 0.0028 rms, 0.0025 in the mean with the outputs' and the weights' own rounding; 3e-3, and ten
+    times that for the largest.  The run in fp16 gives NaN (exp 18) or equal weights (-30)."""
+    c = Chunks(lens, n, 8, 2, 16, seed=sum(lens))
+    o, l = c.want(w_pre, w0)
+    on = lambda x: ((x & 0x7F80) != 0) & ((x & 0x7F80) != 0x7F80)  # noqa: E731
+    times = lambda x, e: np.where(on(x), x + (e << 7), x).astype(np.uint16)  # noqa: E731
+    c.q, c.kp = times(c.q.astype(np.int32), -exp), times(c.kp.astype(np.int32), exp)
+    say("short magnitudes", lens, exp)
+    out, lse = c.run(w_pre, w0, want_lse=True)
+    assert_close(to_f64(out), o, 3e-2, 3e-3, what="out")
+    assert_close(lse.cpu().numpy(), l, 3e-2, 3e-3, what="lse")
