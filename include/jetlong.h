@@ -626,7 +626,11 @@ int jl_select_blocks(const float* scores, const int32_t* kv_lens, int32_t* block
  * -1 everywhere, zeros and zeros are an empty table.  Pages hold any number of
  * tokens; the bf16 entry points take powers of two, the 8-bit ones multiples of 64.
  * The calls below keep these rules; results follow from the arguments alone, and
- * no call waits for the device or allocates.  Entries outside the pool are never
+ * no call waits for the device or allocates.  The caller may lower lens (rows that
+ * are taken back, as rejected drafts are): the pages behind the new end stay the
+ * sequence's, counted in refs and copied by forks, until jl_pages_reserve frees
+ * them.  Nothing else of the three is the caller's to change, but for restoring
+ * all of them to an earlier state.  Entries outside the pool are never
  * followed.  B > 2048 or n_pages > 2^30 -> JL_ERR_UNSUPPORTED.  Calls on one table
  * must be ordered by the caller.
  */
@@ -653,7 +657,9 @@ int jl_pages_fork(const jl_pages* pages, const int32_t* parent, void* stream);
  * name too gets a page of its own in its place, to which the old one is to be copied
  * (a sequence's last page that all name who write there stays with the last of them).
  * All or nothing: if the pages do not suffice, or a sequence would pass max_pages, the
- * table, lens and refs stay as they were.
+ * table, lens and refs stay as they were.  Before all this and in any case, entries behind
+ * the first ceil(lens[b] / page_size) of every row, up to the first that names no page, become
+ * -1 and refs follow: the pages of rows that were taken back are free again.
  *   n_new    int32 [B] DEVICE array
  *   starts   int32 [B] (written): lens before the call, as the append calls take them
  *   granted  int32 [B] (written): max(n_new, 0), or 0 for all if the pages do not

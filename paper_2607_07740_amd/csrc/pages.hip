@@ -96,9 +96,11 @@ __global__ __launch_bounds__(kBookThreads) void fork_kernel(ForkArgs a) {
 // many pages are free, then the k-th free page goes to the sequence whose range of
 // needs holds k.  A sequence that writes into a partly filled page which others
 // name too gets a fresh one for it, but for the last writer of a page that only
-// writers name.  If the pages do not suffice nothing is changed.  Bound by latency: length, entry,
-// count, sums and the second read of the counts follow each other (16 sequences, 512 pages: 11.2
-// us; 12.7 with 1024 threads and 64-bit divisions).
+// writers name.  If the pages do not suffice nothing is changed.  Before all this, pages that
+// a sequence still names behind its last one (its length was lowered) are given up.  Bound by
+// latency: length, entries, count, sums and the second read of the counts follow each other (16
+// sequences, 512 pages: 11.6 us, 0.4 of them for the entries behind; 12.7 with 1024 threads and
+// 64-bit divisions, without those).
 struct ReserveArgs {
   Pages p;
   const int32_t* n_new;
@@ -130,6 +132,7 @@ __device__ inline uint32_t free_mask(const int32_t* refs, int at, int n_pages) {
 __global__ __launch_bounds__(kBookThreads) void reserve_kernel(ReserveArgs a) {
   extern __shared__ int32_t smem[];
   __shared__ unsigned long long s_scan[kBookWaves];
+  __shared__ int s_behind[kBookWaves];
   const Pages& p = a.p;
   int32_t* const s_last = smem;              // the shared page it writes into, else -1 (16-byte aligned)
   int32_t* const s_first = s_last + ((p.B + 3) & ~3);  // needs before sequence b
@@ -138,29 +141,60 @@ __global__ __launch_bounds__(kBookThreads) void reserve_kernel(ReserveArgs a) {
   int32_t* const s_len = s_move + p.B;
   const int tid = threadIdx.x, nt = blockDim.x, strip_pages = kStripPer * nt;
 
-  // the counts of the first strip, on their way while the needs are formed
   const int n_strips = (p.n_pages + strip_pages - 1) / strip_pages;
-  uint32_t mask0 = free_mask(p.refs, min(tid * kStripPer, p.n_pages), p.n_pages);
+  uint32_t mask0;  // the counts of the first strip, on their way while the needs are formed
 
   const int per = (p.B + nt - 1) >> (31 - __builtin_clz(nt));
   const int b0 = min(tid * per, p.B), b1 = min(b0 + per, p.B);
-  for (int b = b0; b < b1; ++b) {
-    const int len = max(p.lens[b], 0);
-    int last = -1, count = 0;
-    const int slot = (int)((unsigned)len / (unsigned)p.page);
-    if (a.n_new[b] > 0 && len != slot * p.page && slot < p.max_pages) {
-      const int e = p.table[(size_t)b * p.max_pages + slot];
-      last = -2;
-      if (in_pool(e, p.n_pages)) {
-        count = p.refs[e];
-        last = count > 1 ? e : -1;
+  for (int turn = 0;; ++turn) {
+    mask0 = free_mask(p.refs, min(tid * kStripPer, p.n_pages), p.n_pages);
+    bool behind = false;  // one of this thread's names pages behind its last one: the first in s_had
+    for (int b = b0; b < b1; ++b) {
+      const int len = max(p.lens[b], 0), n = a.n_new[b];
+      const int32_t* const row = p.table + (size_t)b * p.max_pages;
+      const int slot = (int)((unsigned)len / (unsigned)p.page);
+      const int end = slot + (len != slot * p.page);
+      const int e = row[min(slot, p.max_pages - 1)], f = row[min(end, p.max_pages - 1)];
+      int last = -1, count = 0, next = -1;
+      if (end < p.max_pages && in_pool(f, p.n_pages)) {
+        next = end;
+        behind = true;
+      }
+      if (n > 0 && end != slot && slot < p.max_pages) {
+        last = -2;
+        if (in_pool(e, p.n_pages)) {
+          count = p.refs[e];
+          last = count > 1 ? e : -1;
+        }
+      }
+      s_last[b] = last;
+      s_first[b] = count;
+      s_len[b] = len;
+      s_had[b] = next;
+    }
+    const unsigned long long some = __ballot(behind);
+    if ((tid & 63) == 0) s_behind[tid >> 6] = some != 0;
+    __syncthreads();
+    bool any = false;
+    for (int i = 0; i < nt >> 6; ++i) any |= s_behind[i] != 0;
+    if (!any || turn == 1) break;
+    for (int b = tid >> 6; b < p.B; b += nt >> 6) {  // a wave for each
+      if (s_had[b] < 0) continue;
+      int32_t* const row = p.table + (size_t)b * p.max_pages;
+      for (unsigned c = s_had[b] + (tid & 63);; c += 64) {
+        const int e = c < (unsigned)p.max_pages ? row[c] : -1;
+        const unsigned long long none = __ballot(!in_pool(e, p.n_pages));
+        if (none == 0 || (tid & 63) < __builtin_ctzll(none)) {
+          row[c] = -1;
+          atomicAdd(p.refs + e, -1);
+        }
+        if (none != 0) break;
       }
     }
-    s_last[b] = last;
-    s_first[b] = count;
-    s_len[b] = len;
+    __threadfence();  // entries and counts are written
+    __syncthreads();
+    __threadfence();  // and read anew
   }
-  __syncthreads();
   const int cap = p.max_pages * p.page;
   long long need = 0;
   int n_moves = 0, over = 0;
