@@ -1563,7 +1563,8 @@ __global__ __launch_bounds__(512) void merge_shared_kernel(SharedArgs a) {
 static size_t chunk_plan_lds(int B, int T, int g) {
   return (5 * (size_t)B + 4) * sizeof(int) + chunk_sizes(B, T, g).segs * 12 + 8;
 }
-bool chunk_rows_fit(int B, int T, int g) { return chunk_plan_lds(B, T, g) <= 60 * 1024; }
+// 60 KB for the segments that the rows fill, beside 32 bytes for each of up to 2048 sequences
+bool chunk_rows_fit(int T, int g) { return chunk_plan_lds(0, T, g) <= 60 * 1024; }
 
 static hipError_t launch_plan(bool chunk, SharedPlanArgs& a, hipStream_t stream) {
   if (chunk) {

@@ -97,7 +97,7 @@ hipError_t launch_decode_shared(bool bifocal, const uint16_t* q, const uint16_t*
                                 int B, int n_groups, int Hq, int Hkv, int w_pre, int w0, int n_cu, void* ws,
                                 hipStream_t stream, hipEvent_t ev0, hipEvent_t ev1);
 size_t chunk_scratch_bytes(int B, int T, int Hq, int Hkv, int max_pages, int page);
-bool chunk_rows_fit(int B, int T, int g);
+bool chunk_rows_fit(int T, int g);
 hipError_t launch_chunk_rows(bool bifocal, const uint16_t* q, const uint16_t* k, const uint16_t* v,
                              const int32_t* table, int max_pages, int n_pages, int page_shift,
                              const int32_t* cu, const int32_t* kv_lens, uint16_t* o, float* lse,
@@ -839,7 +839,7 @@ int check_shared(int B, int n_groups, int Hq, int Hkv, int head_dim, int max_pag
 
 bool chunk_sizes_ok(int B, int T, int Hq, int Hkv) {
   return B <= jl::kShMaxSeqs && !past_int32(T, Hq, 2) && !past_int32(2LL * B + 1024, Hkv, 1) &&
-         jl::chunk_rows_fit(B, T, Hq / Hkv);
+         jl::chunk_rows_fit(T, Hq / Hkv);
 }
 
 int varlen_paged(bool bifocal, const void* q, const void* kp, const void* vp, const int32_t* table,

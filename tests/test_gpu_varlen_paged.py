@@ -386,3 +386,43 @@ def test_short_sequences_of_any_magnitude(lens, n, w_pre, w0, exp):
     out, lse = c.run(w_pre, w0, want_lse=True)
     assert_close(to_f64(out), o, 3e-2, 3e-3, what="out")
     assert_close(lse.cpu().numpy(), l, 3e-2, 3e-3, what="lse")
+
+
+@pytest.mark.parametrize("page", [16, 64])
+def test_the_largest_batch(page):
+    """2048 sequences of a token each, every hundredth a prompt, which with the larger pages run as
+    blocks."""
+    b = np.arange(2048)
+    lens = np.where(b % 100 == 7, 90, 1 + b % 37).tolist()
+    n = np.where(b % 100 == 7, 85, 1).tolist()
+    c = Chunks(lens, n, 2, 1, page, seed=71)
+    say("largest batch", page)
+    out, lse = c.run(40, 30, want_lse=True)
+    o, l = c.want(40, 30)
+    assert_close(to_f64(out), o, what="out")
+    # the row sum of a single key carries its score's error, in fp16 an eighth of 0.007 rms
+    assert_close(lse.cpu().numpy(), l, what="lse")
+
+
+@pytest.mark.parametrize("page", [16, 64])
+def test_as_many_sequences_and_rows_as_a_call_takes(page):
+    """2048 whole prompts of 1.3 million rows in all, against the packed prefill without pages."""
+    g = torch.Generator(device="cuda").manual_seed(page)
+    B, most = 2048, 256
+    n = 128 + np.arange(B) % 63
+    T, per = int(n.sum()), most // page
+    assert api.varlen_paged_workspace_bytes(B, T, 4, 1, per, page) > 0
+    assert api.varlen_paged_workspace_bytes(B, T + 6000, 4, 1, per, page) == 0
+    table = torch.randperm(B * per, generator=g, device="cuda").view(B, per)
+    q, k, v = (torch.randn((T, h, 128), generator=g, device="cuda").to(torch.bfloat16) for h in (4, 1, 1))
+    cu = np.concatenate([[0], np.cumsum(n)])
+    kp, vp = (torch.zeros((B * per, page, 1, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = table.to(torch.int32)
+    say("most rows", page, T)
+    api.cache_append(kp, vp, k, v, torch.zeros(B, dtype=torch.int32, device="cuda"), block_table=table,
+                     cu_seqlens=_i32(cu))
+    out = api.prefill_varlen_paged(q, kp, vp, table, _i32(cu), _i32(n), w_pretrained=100, w_local=40)
+    want = api.prefill_varlen(q, k, v, _i32(cu), max_seqlen=int(n.max()), w_pretrained=100, w_local=40)
+    torch.cuda.synchronize()
+    off = (out.float() - want.float()).abs()  # each is within half of these bounds of 64 bits
+    assert off.max().item() <= 4e-2 and off.mean().item() <= 4e-3

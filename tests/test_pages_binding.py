@@ -195,3 +195,12 @@ def test_chunk_arguments_are_checked(kw, code):
     assert L.jl_rope_attention_varlen_paged(*head, *ws) == code
     for w in ((0, 4), (32, -1)):
         assert L.jl_bifocal_prefill_varlen_paged(*head, *w, *ws) in (BAD, code)
+
+
+def test_packed_chunks_take_as_many_sequences_as_they_say():
+    """2048 of them, of a token each or with as many rows as a few sequences may have."""
+    for g, T in ((1, 1300000), (4, 327000), (8, 163000), (100, 10000), (256, 5000)):
+        few, many = (api.varlen_paged_workspace_bytes(B, T, g, 1, 64, 64) for B in (1, 2048))
+        assert 0 < few < many
+        assert api.varlen_paged_workspace_bytes(2048, 2048, g, 1, 64, 64) > 0
+        assert api.varlen_paged_workspace_bytes(1, 2 * T, g, 1, 64, 64) == 0
