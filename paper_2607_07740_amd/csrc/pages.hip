@@ -428,19 +428,18 @@ struct AppendArgs {
   const int32_t* n_new;  // nullptr: all
   const int32_t* cu;     // packed rows; nullptr: n rows per sequence
   int B, n, max_pages, n_pages, page, chunks;  // chunks: 16-byte pieces of a token's K
-  int rows_per_wave;
   long long rows, cap;
 };
 
 constexpr int kAppendWaves = 4;
+// Workgroups at most: a launch counts its threads in 32 bits and drops what lies past them
+constexpr int kAppendGrid = 1 << 22;
 
 __global__ __launch_bounds__(64 * kAppendWaves) void append_kernel(AppendArgs a) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long r0 = ((long long)blockIdx.x * kAppendWaves + wave) * a.rows_per_wave;
-  for (int i = 0; i < a.rows_per_wave; ++i) {
-    const long long t = r0 + i;
-    if (t >= a.rows) return;
+  const long long stride = (long long)gridDim.x * kAppendWaves;
+  for (long long t = (long long)blockIdx.x * kAppendWaves + wave; t < a.rows; t += stride) {
     int b, at;
     if (a.cu != nullptr) {  // the last sequence that begins at or before t: cu is not decreasing
       int before = 0;
@@ -552,10 +551,8 @@ hipError_t launch_cache_append(const uint16_t* k, const uint16_t* v, uint16_t* k
   a.chunks = Hkv * (kHeadDim / 8);
   a.rows = cu != nullptr ? n : (long long)B * n;
   a.cap = table != nullptr ? (long long)max_pages * page : page;
-  a.rows_per_wave = 1;
-  const long long per = (long long)kAppendWaves * a.rows_per_wave;
-  hipLaunchKernelGGL(append_kernel, dim3((unsigned)((a.rows + per - 1) / per)),
-                     dim3(64 * kAppendWaves), 0, stream, a);
+  const long long grid = std::min<long long>((a.rows + kAppendWaves - 1) / kAppendWaves, kAppendGrid);
+  hipLaunchKernelGGL(append_kernel, dim3((unsigned)grid), dim3(64 * kAppendWaves), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -296,3 +296,19 @@ def test_calls_on_two_streams_do_not_meet():
         for _ in range(3):
             m.fork(u.tolist())
         same(t, m)
+
+
+def test_more_rows_than_a_launch_has_waves():
+    """2^26 rows and a few, of which the last three have a place."""
+    n = (1 << 26) + 5
+    k, v = (torch.empty((1, n, 1, 128), device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    x = torch.randn((2, 3, 1, 128), device="cuda").to(torch.bfloat16)
+    k[0, n - 3:], v[0, n - 3:] = x[0], x[1]
+    kc, vc = (torch.zeros((1, 8, 1, 128), device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    say("append", n)
+    api.cache_append(kc, vc, k, v, _i32([3 - n]))
+    torch.cuda.synchronize()
+    for c, rows in ((kc, x[0]), (vc, x[1])):
+        assert torch.equal(c[0, :3], rows) and (c[0, 3:] == 0).all()
+    del k, v
+    torch.cuda.empty_cache()
