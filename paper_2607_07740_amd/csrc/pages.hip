@@ -479,6 +479,8 @@ static int fork_cols(int B, int max_pages) {
   int c = 32;  // 128 bytes of a row, 64 KB in all; fewer where the grid would not fill the CUs
   while (c > 8 && max_pages / c < 128) c /= 2;
   while (c > 1 && (size_t)c * B * sizeof(int32_t) > (size_t)64 * 1024) c /= 2;
+  // more where the launch would pass the threads that 32 bits count
+  while (max_pages / c >= 1 << 20 && (size_t)2 * c * B * sizeof(int32_t) <= (size_t)64 * 1024) c *= 2;
   return c;
 }
 

@@ -312,3 +312,17 @@ def test_more_rows_than_a_launch_has_waves():
         assert torch.equal(c[0, :3], rows) and (c[0, 3:] == 0).all()
     del k, v
     torch.cuda.empty_cache()
+
+
+def test_a_table_row_of_more_entries_than_a_launch_has_threads():
+    cols = (1 << 29) + 9
+    table = torch.full((1, cols), -1, dtype=torch.int32, device="cuda")
+    table[0, :2], table[0, cols - 2:] = _i32([3, 1]), _i32([0, 2])
+    pages = api.PageTable(_i32([cols]), _i32([1, 1, 1, 1, 0]), table, 1)
+    say("fork", cols)
+    api.pages_fork(pages, _i32([-1]))
+    torch.cuda.synchronize()
+    assert pages.refs.tolist() == [0] * 5 and pages.lens.tolist() == [0]
+    assert (table[0, :2] == -1).all() and (table[0, cols - 2:] == -1).all()
+    del pages, table
+    torch.cuda.empty_cache()
