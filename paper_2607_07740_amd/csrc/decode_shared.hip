@@ -179,9 +179,11 @@ static size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 // the time of 32 here (turns of 512, 600, 1 and 700 rows behind 15000, 34000, 9000 and 0 keys, 32/8
 // heads: 754 -> 560 us): where the rows beyond a token per sequence make a few of its blocks, and with what it
 // asks of the cache.  A sequence's go there if they are more than 128.
-static bool chunk_blocks(int B, int T, int g, int max_pages, int page) {
+static bool chunk_blocks(int B, int T, int Hkv, int g, int max_pages, int page) {
+  // a launch of its parts, 512 threads for each kv head, drops those past 32 bits
+  const size_t parts = most_parts(B, T, g, head_workgroups(kShMaxWg, Hkv));
   return kChunkBlockRows % g == 0 && page >= kChunkTile && max_pages <= prefill_chunk_max_pages() &&
-         ((long long)T - B) * g >= 4 * kChunkBlockRows;
+         ((long long)T - B) * g >= 4 * kChunkBlockRows && parts * Hkv < ((size_t)1 << 32) / 512;
 }
 
 // Scratch of a chunk call: plan, parts, the states of either kernel
@@ -190,7 +192,7 @@ struct ChunkScratch {
 };
 static ChunkScratch chunk_scratch(int B, int T, int Hq, int Hkv, int max_pages, int page) {
   const int g = Hq / Hkv, n_wg = head_workgroups(kShMaxWg, Hkv);
-  const bool blocks = chunk_blocks(B, T, g, max_pages, page);
+  const bool blocks = chunk_blocks(B, T, Hkv, g, max_pages, page);
   ChunkScratch c;
   c.parts = round256(plan_bytes(chunk_sizes(B, T, g)));
   c.states = round256(c.parts + (blocks ? most_parts(B, T, g, n_wg) * sizeof(ChunkPart) : 0));
@@ -1662,7 +1664,7 @@ hipError_t launch_chunk_rows(bool bifocal, const uint16_t* q, const uint16_t* k,
   const int g = Hq / Hkv, page = 1 << page_shift;
   const ChunkScratch at = chunk_scratch(B, T, Hq, Hkv, max_pages, page);
   char* const mem = (char*)scratch;
-  const bool blocks = chunk_blocks(B, T, g, max_pages, page);
+  const bool blocks = chunk_blocks(B, T, Hkv, g, max_pages, page);
   SharedPlanArgs p{kv_lens, nullptr, nullptr, nullptr, cu, scratch, B, 0, T, g, Hkv, max_pages,
                    page, head_workgroups(n_cu, Hkv), bifocal ? 1 : 0, w_pre, w0,
                    blocks ? (ChunkPart*)(mem + at.parts) : nullptr,

@@ -426,3 +426,29 @@ def test_as_many_sequences_and_rows_as_a_call_takes(page):
     torch.cuda.synchronize()
     off = (out.float() - want.float()).abs()  # each is within half of these bounds of 64 bits
     assert off.max().item() <= 4e-2 and off.mean().item() <= 4e-3
+
+
+def test_more_parts_than_a_launch_has_threads():
+    """A prompt beside a thousand tokens, of so many kv heads that the blocks' parts pass 2^32 threads:
+    the last heads are right too."""
+    Hkv, B, L, page = 4096, 1013, 1100, 64
+    g = torch.Generator(device="cuda").manual_seed(9)
+    kp, vp = (torch.randn((18, page, Hkv, 128), generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    table = torch.zeros((B, 18), dtype=torch.int32, device="cuda")
+    table[0] = torch.arange(18)
+    T = L + B - 1
+    q = torch.randn((T, Hkv, 128), generator=g, device="cuda", dtype=torch.bfloat16)
+    cu = torch.cat([_i32([0]), L + torch.arange(B, device="cuda", dtype=torch.int32)])
+    lens = _i32([L] + [3] * (B - 1))
+    say("parts past 32 bits")
+    out = torch.full_like(q, float("nan"))
+    api.prefill_varlen_paged(q, kp, vp, table, cu, lens, w_pretrained=600, w_local=300, out=out)
+    few = [0, 1, Hkv // 2, Hkv - 1]
+    pools = [x[:, :, few].contiguous() for x in (kp, vp)]
+    want = api.prefill_varlen_paged(q[:, few].contiguous(), *pools, table, cu, lens, w_pretrained=600,
+                                    w_local=300)
+    torch.cuda.synchronize()
+    off = (out[:, few].float() - want.float()).abs()  # each is within half of these bounds of 64 bits
+    assert off.max().item() <= 4e-2 and off.mean().item() <= 4e-3
+    del out, q, kp, vp
+    torch.cuda.empty_cache()
