@@ -12,9 +12,6 @@
 
 namespace jl {
 
-__device__ inline int pages_of(int len, int page, int max_pages) {
-  return len <= 0 ? 0 : min((len - 1) / page + 1, max_pages);
-}
 __device__ inline bool in_pool(int p, int n_pages) { return (unsigned)p < (unsigned)n_pages; }
 
 constexpr int kBookThreads = 1024;  // of the calls that one workgroup makes; small ones take 256
@@ -418,7 +415,7 @@ __global__ __launch_bounds__(256) void copy_pages_kernel(CopyPools a, const int3
 // Rows of bf16 caches: a wave takes one new token (or several in turn), whose K and
 // V rows of all heads are contiguous on both sides, 16 bytes a lane.  Bound by HBM: prompts of 266 MB
 // read and written in 41 us, 6.5 TB/s; a token of 16 sequences 3.5 us, a launch.
-struct AppendArgs {
+struct RowsArgs {
   const u32x4* k;
   const u32x4* v;
   u32x4* kc;
@@ -435,7 +432,7 @@ constexpr int kAppendWaves = 4;
 // Workgroups at most: a launch counts its threads in 32 bits and drops what lies past them
 constexpr int kAppendGrid = 1 << 22;
 
-__global__ __launch_bounds__(64 * kAppendWaves) void append_kernel(AppendArgs a) {
+__global__ __launch_bounds__(64 * kAppendWaves) void append_kernel(RowsArgs a) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long long stride = (long long)gridDim.x * kAppendWaves;
@@ -536,7 +533,7 @@ hipError_t launch_cache_append(const uint16_t* k, const uint16_t* v, uint16_t* k
                                const int32_t* table, int max_pages, int n_pages, int page,
                                const int32_t* starts, const int32_t* n_new, const int32_t* cu,
                                int B, int n, int Hkv, hipStream_t stream) {
-  AppendArgs a;
+  RowsArgs a;
   a.k = (const u32x4*)k;
   a.v = (const u32x4*)v;
   a.kc = (u32x4*)kc;
