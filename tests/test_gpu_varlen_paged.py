@@ -452,3 +452,34 @@ def test_more_parts_than_a_launch_has_threads():
     assert off.max().item() <= 4e-2 and off.mean().item() <= 4e-3
     del out, q, kp, vp
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n", [[3, 70, 1], [300, 260, 200]])
+@pytest.mark.parametrize("small", [1e-5, 1e-30, 0.0])
+def test_a_few_small_channels_in_a_normal_row(n, small):
+    """Every ninth key of one sequence and every fifth query of another have eight channels and their
+    partners, and half of them, near nothing, below fp16's normal values: blocks take their second
+    run, the rows' kernel does not."""
+    c = Chunks([400, 300, 260], n, 8, 2, 64, seed=81)
+    tiny = np.concatenate([np.arange(24, 32), np.arange(88, 96)])
+    some = np.concatenate([np.arange(8, 128, 16) + i for i in range(8)])
+    q, k, v = c.seqs[0]
+    k = k.copy()
+    x = small * np.random.default_rng(1).standard_normal(k[:, ::9][..., tiny].shape)
+    for i, ch in enumerate(tiny):
+        k[:, ::9, :, ch] = synth.bf16_bits(x[..., i].astype(np.float32))
+    c.seqs[0] = (q, k, v)
+    for j in range(-(-400 // 64)):
+        part = slice(64 * j, min(64 * j + 64, 400))
+        c.kp[c.table[0, j], :part.stop - part.start] = k[0, part]
+    q, k, v = c.seqs[1]
+    q = q.copy()
+    for ch in some:
+        q[:, ::5, :, ch] = synth.bf16_bits(np.full(q[:, ::5, :, ch].shape, small, np.float32))
+    c.seqs[1] = (q, k, v)
+    c.q = np.concatenate([s[0][0, L - m:] for s, L, m in zip(c.seqs, c.lens, c.n)])
+    say("small channels", n, small)
+    out, lse = c.run(150, 60, want_lse=True)
+    o, l = c.want(150, 60)
+    assert_close(to_f64(out), o, what="out")
+    assert_close(lse.cpu().numpy(), l, what="lse")
