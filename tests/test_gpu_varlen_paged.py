@@ -483,3 +483,43 @@ def test_a_few_small_channels_in_a_normal_row(n, small):
     o, l = c.want(150, 60)
     assert_close(to_f64(out), o, what="out")
     assert_close(lse.cpu().numpy(), l, what="lse")
+
+
+def test_pools_past_32_bits():
+    """The same pages at the end of pools of 4.7 GB: appended, copied, decoded over and behind chunks,
+    the same bits as in small ones."""
+    Hq, Hkv, page, far = 16, 8, 64, 36000
+    lens, n = [700, 640, 300], [300, 90, 1]
+    c = Chunks(lens, n, Hq, Hkv, page, seed=91)
+    kp, vp, q, cu, L = to_dev(c.kp), to_dev(c.vp), to_dev(c.q), _i32(c.cu), _i32(lens)
+    table = _i32(c.table)
+    big = [torch.zeros((far, page, Hkv, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    at = torch.where(table >= 0, far - 1 - table, table)
+    say("pools past 32 bits")
+    for b, m in enumerate(lens):  # through the append, but the last page, which a copy brings
+        rows = [torch.cat([x[p] for p in c.table[b][c.table[b] >= 0]])[:m] for x in (kp, vp)]
+        api.cache_append(*big, *[x[None].contiguous() for x in rows], _i32([0]),
+                         block_table=at[b:b + 1].contiguous())
+    p = int(c.table[0, 2])
+    for x in big:
+        x[5] = x[far - 1 - p]
+        x[far - 1 - p] = 0
+    api.copy_pages(big, _i32([[5, far - 1 - p]]), _i32([1]))
+    for x, small in zip(big, (kp, vp)):
+        for b, m in enumerate(lens):
+            for j in range(-(-m // page)):
+                e, k = int(c.table[b, j]), min(page, m - j * page)
+                assert torch.equal(x[far - 1 - e, :k], small[e, :k])
+    for kw in (dict(w_pretrained=200, w_local=70), dict(bifocal=False)):
+        for rows in (c.cu[-1], 6):  # blocks and the rows' kernel, the latter alone
+            cut = cu if rows == c.cu[-1] else _i32([0, 2, 5, 6])
+            a, z = (api.prefill_varlen_paged(q[:rows].contiguous(), *pools, t, cut, L, **kw)
+                    for pools, t in (((kp, vp), table), (big, at)))
+            assert torch.equal(a, z)
+        plan = api.shared_plan(L, _i32([0, 1, 2, 3]), _i32([0, 0, 0]), Hq=Hq, Hkv=Hkv, page_size=page,
+                               max_pages=c.max_pages, **kw)
+        a, z = (api.decode_shared(q[:3].contiguous(), *pools, t, plan)
+                for pools, t in (((kp, vp), table), (big, at)))
+        assert torch.equal(a, z) and torch.isfinite(a.float()).all()
+    del big
+    torch.cuda.empty_cache()
