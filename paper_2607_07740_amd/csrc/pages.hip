@@ -45,8 +45,9 @@ __device__ inline T block_scan(T v, T* s, T* total) {
 // Row b becomes what row parent[b] was, or empty where parent[b] names none, all
 // rows at once.  A workgroup takes some columns of every row: what the rows get
 // goes to LDS before any of them is written.  Rows that stay are not read.
-// lens is read and written by the first workgroup alone.  Bound by the counts' atomics (256
-// rows of 2048 columns of which 64 change: 9.4 us, 7.8 without them; 32 rows of 64: 3.9, a launch).
+// lens is read and written by the first workgroup alone.  Bound by reads that follow each other
+// (parent, the parent's entry, the row's own): 256 rows of 2048 columns of which 64 change 9.4 us,
+// 7.8 without the counts' atomics; 32 rows of 64: 3.9, a launch.
 struct ForkArgs {
   Pages p;
   const int32_t* parent;
