@@ -776,8 +776,8 @@ size_t jl_decode_shared_workspace_bytes(int B, int Hq, int Hkv, int head_dim);
  * Rounded are the rotated queries, the keys' cos and sin and the rotated keys, to fp16, and the
  * softmax weights, to bf16, whose rounded values the denominator sums; everything else is fp32.
  * Beside a key, or a rotated and scaled query, whose largest channel lies outside [2^-8, 2^15) the
- * first three are rounded to bf16, for all that the same workgroup holds, in twice the time.  The same plan and
- * inputs give the same bits.  Only the cos/sin table may be allocated or grown.
+ * first three are rounded to bf16, for all that the same workgroup holds, in twice the time.  The
+ * same plan and inputs give the same bits.  Only the cos/sin table may be allocated or grown.
  */
 int jl_bifocal_decode_shared(const void* q, const void* k_pages, const void* v_pages,
                              const int32_t* block_table, int max_pages, int page_size, int n_pages,
@@ -814,9 +814,10 @@ int jl_rope_attention_decode_shared(const void* q, const void* k_pages, const vo
  * Sequences of more than 128 rows (tokens * Hq / Hkv) run as blocks of the prefill kernel where
  * Hq / Hkv divides 256, page_size is 64 or more, max_pages 4096 or less, and (total_tokens - B) *
  * Hq / Hkv 1024 or more; without one of these in the kernel of the short ones, which takes a third
- * longer.  Roundings as in jl_bifocal_decode_shared; a part of a block is done again in bf16 where eight
- * consecutive channels of a key and their partners (from a multiple of eight on), or half the channels of
- * a rotated and scaled query (every other eight), are not all zero and their largest is outside [2^-12, 2^15).
+ * longer.  Roundings as in jl_bifocal_decode_shared, but that a part of a block is done again in
+ * bf16 by another rule: where eight channels of a key from a multiple of eight on and their
+ * partners, or every other eight channels of a rotated and scaled query, are not all zero and
+ * the largest of them is outside [2^-12, 2^15).
  *   workspace    jl_varlen_paged_workspace_bytes(...) bytes, 16-byte aligned; contents on entry do
  *                not matter.  The sum of 1056 bytes for every token and query head, 35 MB for the
  *                workgroups, 140 MB where there are blocks, and lists: 310 MB for 8192 tokens of 32

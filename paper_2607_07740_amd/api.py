@@ -882,8 +882,8 @@ class PageTable:
     """The tables of B sequences over a pool of pages (jl_pages): lens int32 [B], refs int32
     [n_pages], table int32 [B, max_pages], on one device.  pages_alloc makes an empty one.  The
     paged calls take table as block_table and lens as kv_lens.  The tensors are the caller's to
-    read and to restore by copy_; none can be replaced.  lens may be lowered in place (rejected drafts):
-    the next pages_reserve frees the pages behind."""
+    read and to restore by copy_; none can be replaced.  lens may be lowered in place (rejected
+    drafts): the next pages_reserve frees the pages behind."""
 
     def __init__(self, lens, refs, table, page_size: int):
         if table.dim() != 2:

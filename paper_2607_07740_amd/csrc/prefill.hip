@@ -916,10 +916,10 @@ __device__ __forceinline__ bool prefill_block(const PrefillArgs& a, const Work& 
 }
 
 // Packed chunks behind paged caches: the parts of a list of query blocks of different sequences,
-// which a planning kernel has cut to about the same length, one per workgroup and kv head.  Bound by the
-// matrix cores: turns of 512, 600 and 700 rows behind 15000, 34000 and 0 keys (32/8 heads, 459
-// GFLOP) in 502 to 567 us from card to card, 0.81 to 0.91 PFLOP/s.  A loop over parts in a workgroup spilled registers
-// of the block's loops; a part has one, with an exit where the list has ended.
+// which a planning kernel has cut to about the same length, one per workgroup and kv head.  Bound by
+// the matrix cores: turns of 512, 600 and 700 rows behind 15000, 34000 and 0 keys (32/8 heads, 459
+// GFLOP) in 502 to 567 us from card to card, 0.81 to 0.91 PFLOP/s.  A loop over parts in a workgroup
+// spilled registers of the block's loops; a part has one, with an exit where the list has ended.
 __device__ inline Work chunk_work(const PrefillArgs& a, const ChunkPart& p, int kvh) {
   Work W;
   W.b = p.seq;
